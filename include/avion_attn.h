@@ -288,6 +288,89 @@ int avion_column_sum(const void *x, void *sum, long long M, int F, unsigned flag
                      void *workspace, size_t workspace_bytes, void *stream);
 
 /*
+ * Token table: the entry of the text encoder, a GPT-like Transformer over at most 77 tokens (implementation details of the
+ * video-language model): lookup with scaling, and the table's gradient.
+ *     y_i = scale * table[t_i]          dtable[v] = scale * sum over i with t_i = v of dy_i
+ *   tokens : in,  [n] int64 (int32 with AVION_FLAG_TOKENS_I32), naturally aligned.  A token outside [0, V) names no row: its
+ *            row of y is zeros and it adds to no gradient (a slot without a word).
+ *   table  : in,  [V, D]; dtable: out, same shape and format, fully overwritten (rows that no token names: zeros).  The format
+ *            of y, or fp32 with AVION_FLAG_WIDE_F32
+ *   y, dy  : [n, D] bf16 (fp16 with AVION_FLAG_F16)
+ *   n >= 0; V >= 1; scale finite; D a multiple of 8 up to 65536, n and V up to 2^28, n * D up to 2^37
+ *   workspace (backward): 256-byte aligned, avion_embedding_bwd_workspace_bytes(n, V, D) bytes, contents ignored and left
+ *   unspecified; calls that overlap in time must not share one
+ * The gradient sorts the slots by token and sums each token's rows in fp32 in a fixed order, rounded once: no atomics on
+ * floating-point values, bit-reproducible, whatever share of the slots one token fills.  The tokens must not change
+ * while the call runs.  n = 0: y is not touched, dtable becomes zeros.
+ */
+#define AVION_FLAG_WIDE_F32 8u
+#define AVION_FLAG_TOKENS_I32 16u
+
+int avion_embedding_fwd(const void *tokens, const void *table, void *y, long long n, long long V, int D,
+                        float scale, unsigned flags, void *stream);
+
+size_t avion_embedding_bwd_workspace_bytes(long long n, long long V, int D);
+
+int avion_embedding_bwd(const void *tokens, const void *dy, void *dtable, long long n, long long V, int D,
+                        float scale, unsigned flags,
+                        void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * Root-mean-square normalisation with the residual's addition in front of it: what stands before the attention and the MLP of
+ * an encoder layer whose norm has no mean and no bias.  Per token row:
+ *     h = x + residual (rounded to the residual's format),  rstd = 1/sqrt(mean(h^2) + eps),  y = h * rstd * weight
+ *     dweight = sum_rows dy * xhat;  g = dy * weight;  xhat = h * rstd;
+ *     dx = dresidual = rstd * (g - xhat * mean(g * xhat)) + dh
+ *   x, y, dy, dx     : [M, D] bf16 (fp16 with AVION_FLAG_F16)
+ *   residual, h, dh  : [M, D] in that format, or fp32 with AVION_FLAG_WIDE_F32 (a residual stream held in 32 bits).
+ *                      residual and h are both given or both NULL: then the norm is of x itself, h in the formulas is x
+ *   weight, dweight  : fp32 [D];   rstd: fp32 [M], out of the forward (NULL where no backward follows), in of the backward
+ *   dh               : gradient that reaches h by its other use, NULL for none
+ *   dx, dresidual    : outputs of the backward, NULL where not wanted.  dresidual (fp32) only with AVION_FLAG_WIDE_F32; without
+ *                      it dx is the gradient of both inputs.
+ *   M >= 0; D a multiple of 8, at most 16384; eps finite and >= 0
+ *   workspace (backward): 256-byte aligned, avion_rmsnorm_bwd_workspace_bytes(M, D) bytes (at most 1024 * D floats)
+ * Statistics and sums in fp32 (the sum of a row's squares has to be finite there), outputs rounded once; no atomics,
+ * bit-reproducible.  M = 0 writes zeros to dweight and nothing else.  Pointers 16-byte aligned.
+ */
+int avion_rmsnorm_fwd(const void *x, const void *residual, const float *weight, void *y, void *h, float *rstd,
+                      long long M, int D, float eps, unsigned flags, void *stream);
+
+size_t avion_rmsnorm_bwd_workspace_bytes(long long M, int D);
+
+int avion_rmsnorm_bwd(const void *h, const float *weight, const float *rstd, const void *dy, const void *dh,
+                      void *dx, float *dresidual, float *dweight, long long M, int D, unsigned flags,
+                      void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * Rows in 8 bits, for a product that runs at twice the rate of 16-bit operands (feature extraction and zero-shot evaluation
+ * with a trained encoder; no backward).  Per row y in R^D:
+ *     scale = max(max|y|, 2^-96) / 448,   y8 = e4m3(y / scale)    (OCP e4m3, nearest even; 448 is its largest value)
+ * avion_rmsnorm_fwd_fp8: y is avion_rmsnorm_fwd's, rounded only here; avion_quantize_rows: y is x itself (an attention's
+ * output, a weight [N, K] when it is laid out).
+ *   y8, x8 : out, [M, D] one byte an element, fully overwritten;   scale: out, fp32 [M]
+ *   D a multiple of 16, at most 16384; everything else as above.  NaN stays NaN; an infinite value makes its row's scale
+ *   infinite.
+ */
+int avion_rmsnorm_fwd_fp8(const void *x, const void *residual, const float *weight, void *y8, float *scale, void *h,
+                          long long M, int D, float eps, unsigned flags, void *stream);
+
+int avion_quantize_rows(const void *x, void *x8, float *scale, long long M, int D, unsigned flags, void *stream);
+
+/*
+ * The linear layer that reads them:  y_mn = x_scale_m * w_scale_n * sum_k x8_mk * w8_nk + bias_n
+ *   x8 : in, [M, K] e4m3 with fp32 x_scale [M];   w8 : in, [N, K] e4m3 (one row per output) with fp32 w_scale [N]
+ *   bias : in, fp32 [N] or NULL;   y : out, [M, N] bf16 (fp16 with AVION_FLAG_F16), fully overwritten
+ *   M >= 0 (0: nothing happens); N a multiple of 8 up to 2^20; K a multiple of 16 up to 65536; M below 2^31 - 256 and at most
+ *   2^24 tiles of 64 x 64 in y; pointers 16-byte aligned
+ * fp32 sums, scaled and rounded once.  The matrix unit first adds 8 products of neighbouring k, dropping of each what lies
+ * below 2^-13 of the largest one's power of two (measured; 2^-5 and more separate the operands from what they were rounded
+ * from).  No workspace; bit-reproducible.
+ */
+int avion_linear_fp8(const void *x8, const float *x_scale, const void *w8, const float *w_scale, const float *bias,
+                     void *y, long long M, int N, int K, unsigned flags, void *stream);
+
+/*
  * Allocation-free backward, for callers that cannot provide device scratch of their own: code
  * under HIP graph capture, tight serving or training loops, harnesses that forbid hipMalloc.
  * Same operation, arguments, rules and bits as avion_attn_bwd (bf16, not causal), without the

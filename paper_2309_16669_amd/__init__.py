@@ -15,7 +15,7 @@ _PKG = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_PKG, "libavion_attn.so")
 
 OK, EINVAL, EUNSUPPORTED, EWORKSPACE, EHIP, ESCRATCH = 0, -1, -2, -3, -4, -5
-FLAG_F16, FLAG_CAUSAL, FLAG_QKVPACKED = 1, 2, 4
+FLAG_F16, FLAG_CAUSAL, FLAG_QKVPACKED, FLAG_WIDE_F32, FLAG_TOKENS_I32 = 1, 2, 4, 8, 16
 
 _lib = None
 
@@ -90,6 +90,24 @@ def load_library() -> ctypes.CDLL:
         lib.avion_column_sum.argtypes = [p, p, ll, i, u, p, sz, p]
         lib.avion_attn_bwd_noalloc.restype = i
         lib.avion_attn_bwd_noalloc.argtypes = [p, p, p, p, p, p, p, p, p, i, i, i, i, f, p]
+        lib.avion_embedding_fwd.restype = i
+        lib.avion_embedding_fwd.argtypes = [p, p, p, ll, ll, i, f, u, p]
+        lib.avion_embedding_bwd_workspace_bytes.restype = sz
+        lib.avion_embedding_bwd_workspace_bytes.argtypes = [ll, ll, i]
+        lib.avion_embedding_bwd.restype = i
+        lib.avion_embedding_bwd.argtypes = [p, p, p, ll, ll, i, f, u, p, sz, p]
+        lib.avion_rmsnorm_fwd.restype = i
+        lib.avion_rmsnorm_fwd.argtypes = [p, p, p, p, p, p, ll, i, f, u, p]
+        lib.avion_rmsnorm_bwd_workspace_bytes.restype = sz
+        lib.avion_rmsnorm_bwd_workspace_bytes.argtypes = [ll, i]
+        lib.avion_rmsnorm_bwd.restype = i
+        lib.avion_rmsnorm_bwd.argtypes = [p, p, p, p, p, p, p, p, ll, i, u, p, sz, p]
+        lib.avion_rmsnorm_fwd_fp8.restype = i
+        lib.avion_rmsnorm_fwd_fp8.argtypes = [p, p, p, p, p, p, ll, i, f, u, p]
+        lib.avion_quantize_rows.restype = i
+        lib.avion_quantize_rows.argtypes = [p, p, p, ll, i, u, p]
+        lib.avion_linear_fp8.restype = i
+        lib.avion_linear_fp8.argtypes = [p, p, p, p, p, p, ll, i, i, u, p]
         _lib = lib
     return _lib
 
@@ -404,3 +422,154 @@ def column_sum(x, out, workspace, stream=None) -> None:
     _require(workspace, "workspace", torch.uint8)
     _check(load_library().avion_column_sum(_ptr(x), _ptr(out), M, F, _flags(x.dtype, False, False), _ptr(workspace),
                                            workspace.numel(), _stream_handle(stream)))
+
+
+def _opt(t):
+    return ctypes.c_void_p(None) if t is None else _ptr(t)
+
+
+def _one_device(*tensors):
+    """The device of all of them (None: absent).  The calls below run with it as the current device, on its current stream
+    unless another is given."""
+    device = tensors[0].device
+    for t in tensors:
+        if t is not None and t.device != device:
+            raise ValueError(f"tensors must live on one GPU, got {device} and {t.device}")
+    return device
+
+
+def _launch(device, entry, args, stream):
+    import torch
+    with torch.cuda.device(device):
+        _check(entry(*args, _stream_handle(stream)))
+
+
+def _tokens_flag(tokens) -> int:
+    import torch
+    if tokens.dtype not in (torch.int64, torch.int32):
+        raise ValueError(f"tokens must be int64 or int32, got {tokens.dtype}")
+    return FLAG_TOKENS_I32 if tokens.dtype == torch.int32 else 0
+
+
+def _wide_flag(t, dtype, name) -> int:
+    """FLAG_WIDE_F32 for an fp32 tensor, 0 for one of `dtype`."""
+    import torch
+    if t.dtype not in (torch.float32, dtype):
+        raise ValueError(f"{name} must be {dtype} or torch.float32, got {t.dtype}")
+    return FLAG_WIDE_F32 if t.dtype == torch.float32 else 0
+
+
+def embedding_fwd(tokens, table, y, scale: float, stream=None) -> None:
+    """avion_embedding_fwd: tokens int64 or int32 [n], table [V, D] in the format of y or fp32, y bf16 or fp16 [n, D]."""
+    (n,), (V, D) = tokens.shape, table.shape
+    flags = _tokens_flag(tokens) | _flags(y.dtype, False, False) | _wide_flag(table, y.dtype, "table")
+    _require(tokens, "tokens", tokens.dtype, (n,))
+    _require(table, "table", table.dtype, (V, D))
+    _require(y, "y", y.dtype, (n, D))
+    _launch(_one_device(table, tokens, y), load_library().avion_embedding_fwd,
+            (_ptr(tokens), _ptr(table), _ptr(y), n, V, D, float(scale), flags), stream)
+
+
+def embedding_bwd_workspace_bytes(n: int, V: int, D: int) -> int:
+    return int(load_library().avion_embedding_bwd_workspace_bytes(n, V, D))
+
+
+def embedding_bwd(tokens, dy, dtable, scale: float, workspace, stream=None) -> None:
+    """avion_embedding_bwd: dy bf16 or fp16 [n, D]; dtable [V, D] in that format or fp32."""
+    import torch
+    (n,), (V, D) = tokens.shape, dtable.shape
+    flags = _tokens_flag(tokens) | _flags(dy.dtype, False, False) | _wide_flag(dtable, dy.dtype, "dtable")
+    _require(tokens, "tokens", tokens.dtype, (n,))
+    _require(dy, "dy", dy.dtype, (n, D))
+    _require(dtable, "dtable", dtable.dtype, (V, D))
+    _require(workspace, "workspace", torch.uint8)
+    _launch(_one_device(dtable, tokens, dy, workspace), load_library().avion_embedding_bwd,
+            (_ptr(tokens), _ptr(dy), _ptr(dtable), n, V, D, float(scale), flags, _ptr(workspace), workspace.numel()), stream)
+
+
+def _rms_inputs(x, residual, weight, h):
+    import torch
+    M, D = x.shape
+    flags = _flags(x.dtype, False, False)
+    _require(x, "x", x.dtype, (M, D))
+    _require(weight, "weight", torch.float32, (D,))
+    if (residual is None) != (h is None):
+        raise ValueError("residual and h are given together or not at all")
+    if residual is not None:
+        flags |= _wide_flag(residual, x.dtype, "residual")
+        _require(residual, "residual", residual.dtype, (M, D))
+        _require(h, "h", residual.dtype, (M, D))
+    return M, D, flags
+
+
+def rmsnorm_fwd(x, residual, weight, y, h, rstd, eps: float, stream=None) -> None:
+    """avion_rmsnorm_fwd: x, y bf16 or fp16 [M, D]; residual and h (both None: no addition) in that format or fp32; weight fp32
+    [D]; rstd fp32 [M], or None where no backward follows."""
+    import torch
+    M, D, flags = _rms_inputs(x, residual, weight, h)
+    _require(y, "y", x.dtype, (M, D))
+    if rstd is not None:
+        _require(rstd, "rstd", torch.float32, (M,))
+    _launch(_one_device(x, residual, weight, y, h, rstd), load_library().avion_rmsnorm_fwd,
+            (_ptr(x), _opt(residual), _ptr(weight), _ptr(y), _opt(h), _opt(rstd), M, D, float(eps), flags), stream)
+
+
+def rmsnorm_fwd_fp8(x, residual, weight, y8, scale, h, eps: float, stream=None) -> None:
+    """avion_rmsnorm_fwd_fp8: the same with y in 8 bits: y8 float8_e4m3fn [M, D], scale fp32 [M]."""
+    import torch
+    M, D, flags = _rms_inputs(x, residual, weight, h)
+    _require(y8, "y8", torch.float8_e4m3fn, (M, D))
+    _require(scale, "scale", torch.float32, (M,))
+    _launch(_one_device(x, residual, weight, y8, scale, h), load_library().avion_rmsnorm_fwd_fp8,
+            (_ptr(x), _opt(residual), _ptr(weight), _ptr(y8), _ptr(scale), _opt(h), M, D, float(eps), flags), stream)
+
+
+def rmsnorm_bwd_workspace_bytes(M: int, D: int) -> int:
+    return int(load_library().avion_rmsnorm_bwd_workspace_bytes(M, D))
+
+
+def rmsnorm_bwd(h, weight, rstd, dy, dh, dx, dresidual, dweight, workspace, stream=None) -> None:
+    """avion_rmsnorm_bwd: h [M, D] in the format of dy or fp32 (the residual stream's); dh like h or None; dx in the format of dy
+    or None; dresidual fp32, only with an fp32 stream, or None; dweight fp32 [D]."""
+    import torch
+    M, D = dy.shape
+    flags = _flags(dy.dtype, False, False) | _wide_flag(h, dy.dtype, "h")
+    _require(h, "h", h.dtype, (M, D))
+    _require(weight, "weight", torch.float32, (D,))
+    _require(rstd, "rstd", torch.float32, (M,))
+    _require(dy, "dy", dy.dtype, (M, D))
+    for t, n, dt in ((dh, "dh", h.dtype), (dx, "dx", dy.dtype), (dresidual, "dresidual", torch.float32)):
+        if t is not None:
+            _require(t, n, dt, (M, D))
+    _require(dweight, "dweight", torch.float32, (D,))
+    _require(workspace, "workspace", torch.uint8)
+    _launch(_one_device(h, weight, rstd, dy, dh, dx, dresidual, dweight, workspace), load_library().avion_rmsnorm_bwd,
+            (_ptr(h), _ptr(weight), _ptr(rstd), _ptr(dy), _opt(dh), _opt(dx), _opt(dresidual), _ptr(dweight), M, D, flags,
+             _ptr(workspace), workspace.numel()), stream)
+
+
+def quantize_rows(x, x8, scale, stream=None) -> None:
+    """avion_quantize_rows: x bf16 or fp16 [M, D] -> x8 float8_e4m3fn [M, D], scale fp32 [M]."""
+    import torch
+    M, D = x.shape
+    _require(x, "x", x.dtype, (M, D))
+    _require(x8, "x8", torch.float8_e4m3fn, (M, D))
+    _require(scale, "scale", torch.float32, (M,))
+    _launch(_one_device(x, x8, scale), load_library().avion_quantize_rows,
+            (_ptr(x), _ptr(x8), _ptr(scale), M, D, _flags(x.dtype, False, False)), stream)
+
+
+def linear_fp8(x8, x_scale, w8, w_scale, bias, y, stream=None) -> None:
+    """avion_linear_fp8: x8 float8_e4m3fn [M, K] with fp32 x_scale [M], w8 [N, K] with w_scale [N], bias fp32 [N] or None, y
+    bf16 or fp16 [M, N]."""
+    import torch
+    (M, K), N = x8.shape, w8.shape[0]
+    _require(x8, "x8", torch.float8_e4m3fn, (M, K))
+    _require(x_scale, "x_scale", torch.float32, (M,))
+    _require(w8, "w8", torch.float8_e4m3fn, (N, K))
+    _require(w_scale, "w_scale", torch.float32, (N,))
+    if bias is not None:
+        _require(bias, "bias", torch.float32, (N,))
+    _require(y, "y", y.dtype, (M, N))
+    _launch(_one_device(x8, x_scale, w8, w_scale, bias, y), load_library().avion_linear_fp8,
+            (_ptr(x8), _ptr(x_scale), _ptr(w8), _ptr(w_scale), _opt(bias), _ptr(y), M, N, K, _flags(y.dtype, False, False)), stream)

@@ -19,7 +19,13 @@ stream are ordered and may share it.  The native calls take theirs from torch's 
 the call.
 
 `layer_norm(x, gamma, beta)` and `bias_gelu(x, bias)` wrap the layer-normalisation and bias + GELU
-entry points the same way (what they keep for the backward is stated in their docstrings).
+entry points the same way (what they keep for the backward is stated in their docstrings), and so do
+`embedding(tokens, weight)` and `add_rms_norm(x, residual, weight)` for the token table and for the RMS
+normalisation with the residual's addition.  These two take the backward's workspace from torch's allocator for
+the length of the call in either way of calling, and run on the device of their tensors.
+
+`rms_norm_fp8`, `add_rms_norm_fp8`, `quantize_rows` and `linear_fp8` are the 8-bit path of a trained encoder: they
+have no backward, and refuse inputs whose gradient is being recorded.
 """
 from __future__ import annotations
 
@@ -31,6 +37,9 @@ import torch
 
 from . import (attn_bwd_ex, attn_bwd_workspace_bytes, attn_fwd_ex, bias_gelu_bwd, bias_gelu_bwd_workspace_bytes, bias_gelu_bwd_y,
                bias_gelu_fwd, column_sum, column_sum_workspace_bytes, layernorm_bwd, layernorm_bwd_workspace_bytes, layernorm_fwd, load_library)
+from . import (embedding_bwd, embedding_bwd_workspace_bytes, embedding_fwd, rmsnorm_bwd, rmsnorm_bwd_workspace_bytes, rmsnorm_fwd,
+               rmsnorm_fwd_fp8)
+from . import linear_fp8 as _linear_fp8, quantize_rows as _quantize_rows
 
 _native = None
 
@@ -46,7 +55,8 @@ def native_calls():
         except ImportError as e:
             warnings.warn(f"paper_2309_16669_amd/_avion_torch.so does not load ({e}); the Python classes take its calls, at "
                           "several times the host time.  Build it: python -c 'import __graft_entry__ as g; g.build()'")
-            names = ("attention", "attention_qkvpacked", "layer_norm", "bias_gelu", "bias_gelu_linear")
+            names = ("attention", "attention_qkvpacked", "layer_norm", "bias_gelu", "bias_gelu_linear", "embedding", "rms_norm",
+                     "add_rms_norm", "rms_norm_fp8", "add_rms_norm_fp8", "quantize_rows", "linear_fp8")
             _avion_torch = types.SimpleNamespace(**{n: lambda *args: None for n in names})
         _native = _avion_torch
     return _native
@@ -235,3 +245,167 @@ def attention_qkvpacked(qkv, scale: float | None = None, causal: bool = False):
     scale, causal = 1.0 / math.sqrt(qkv.shape[-1]) if scale is None else float(scale), bool(causal)
     o = (_native or native_calls()).attention_qkvpacked(qkv, scale, causal)
     return _AttentionPacked.apply(qkv, scale, causal) if o is None else o
+
+
+# ------------------------------------------------------------------- token table, RMS normalisation, 8-bit path
+def _bytes_on(device, need):
+    if need == 0:
+        raise ValueError("unsupported shape")
+    return torch.empty(need, dtype=torch.uint8, device=device)
+
+
+class _Embedding(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, tokens, weight, scale, dtype):
+        t = tokens.contiguous().view(-1)
+        V, D = weight.shape
+        y = torch.empty((t.shape[0], D), dtype=dtype, device=weight.device)
+        embedding_fwd(t, weight.contiguous(), y, scale)
+        ctx.save_for_backward(t)
+        ctx.scale, ctx.shape, ctx.dtype = scale, (V, D), weight.dtype
+        return y.view(*tokens.shape, D)
+
+    @staticmethod
+    def backward(ctx, dy):
+        (t,) = ctx.saved_tensors
+        V, D = ctx.shape
+        dweight = torch.empty((V, D), dtype=ctx.dtype, device=dy.device)
+        embedding_bwd(t, dy.contiguous().view(-1, D), dweight, ctx.scale,
+                      _bytes_on(dy.device, embedding_bwd_workspace_bytes(t.shape[0], V, D)))
+        return None, dweight, None, None
+
+
+class _AddRmsNorm(torch.autograd.Function):
+    """residual None: the norm of x itself, y alone."""
+
+    @staticmethod
+    def forward(ctx, x, residual, weight, eps):
+        shape = x.shape
+        D = shape[-1]
+        x2 = x.contiguous().view(-1, D)
+        r2 = None if residual is None else residual.contiguous().view(-1, D)
+        y, h = torch.empty_like(x2), None if residual is None else torch.empty_like(r2)
+        rstd = torch.empty((x2.shape[0],), dtype=torch.float32, device=x.device)
+        rmsnorm_fwd(x2, r2, weight.contiguous(), y, h, rstd, eps)
+        ctx.set_materialize_grads(False)
+        h = x2.view(shape) if h is None else h.view(shape)
+        ctx.save_for_backward(h, weight, rstd)         # the residual stream, kept anyway, and one float per token; not y
+        ctx.dtype, ctx.alone = x.dtype, residual is None
+        return y.view(shape) if residual is None else (y.view(shape), h)
+
+    @staticmethod
+    def backward(ctx, dy, dh=None):
+        h, weight, rstd = ctx.saved_tensors
+        if dy is None and dh is None:
+            return None, None, None, None
+        D = h.shape[-1]
+        h2 = h.contiguous().view(-1, D)
+        dy = torch.zeros(h2.shape, dtype=ctx.dtype, device=h.device) if dy is None else dy.contiguous().view(-1, D)
+        dh = None if dh is None else dh.contiguous().view(-1, D)
+        wide = h.dtype != ctx.dtype
+        dx = torch.empty_like(dy) if ctx.needs_input_grad[0] or not wide else None
+        dr = torch.empty_like(h2) if wide and ctx.needs_input_grad[1] else None
+        dweight = torch.empty_like(weight, memory_format=torch.contiguous_format)
+        rmsnorm_bwd(h2, weight.contiguous(), rstd, dy, dh, dx, dr, dweight,
+                    _bytes_on(h.device, rmsnorm_bwd_workspace_bytes(*h2.shape)))
+        dx = None if dx is None else dx.view(h.shape)
+        dr = dx if not wide else None if dr is None else dr.view(h.shape)
+        return dx, (None if ctx.alone else dr), dweight, None
+
+
+def _check_residual(x, residual):
+    if residual.shape != x.shape:
+        raise ValueError(f"residual must have the shape of x, {tuple(x.shape)}, got {tuple(residual.shape)}")
+
+
+def _no_backward(name, *tensors):
+    if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in tensors):
+        raise ValueError(f"{name} has no backward: call it under torch.no_grad(), or detach its inputs")
+
+
+def embedding(tokens, weight, scale: float = 1.0, dtype=None):
+    """scale * weight[tokens] for tokens (int64 or int32, any shape) of a table [V, D] in bf16, fp16 or fp32, D a multiple of 8;
+    the result is bf16 or fp16 (`dtype`; the table's own format, bf16 for an fp32 table, if None).  A token outside [0, V)
+    gives a row of zeros and adds to no gradient.  Differentiable in weight (the gradient has the table's format; fp32 sums in
+    a fixed order); keeps the tokens for the backward."""
+    if dtype is None:
+        dtype = torch.bfloat16 if weight.dtype == torch.float32 else weight.dtype
+    y = (_native or native_calls()).embedding(tokens, weight, float(scale), dtype == torch.float16, dtype == torch.bfloat16)
+    return _Embedding.apply(tokens, weight, float(scale), dtype) if y is None else y
+
+
+def rms_norm(x, weight, eps: float = 1e-6):
+    """Root-mean-square normalisation over the last axis of x (bf16 or fp16, any leading shape, width <= 16384 and a multiple of
+    8) with fp32 gains.  Differentiable in x and weight; keeps x and one float per token for the backward."""
+    y = (_native or native_calls()).rms_norm(x, weight, float(eps))
+    return _AddRmsNorm.apply(x, None, weight, float(eps)) if y is None else y
+
+
+def add_rms_norm(x, residual, weight, eps: float = 1e-6):
+    """(y, h): h = x + residual, the residual stream behind a layer's branch, and y = rms_norm(h, weight), what the next branch
+    reads.  x bf16 or fp16 [..., D]; residual, of the same shape, in the format of x or fp32, and h like it (y is the norm of h
+    as stored).  Differentiable in x, residual and weight; keeps h and one float per token."""
+    _check_residual(x, residual)
+    out = (_native or native_calls()).add_rms_norm(x, residual, weight, float(eps))
+    return _AddRmsNorm.apply(x, residual, weight, float(eps)) if out is None else out
+
+
+def _rms_norm_fp8(x, residual, weight, eps):
+    shape = x.shape
+    x2 = x.contiguous().view(-1, shape[-1])
+    r2 = None if residual is None else residual.contiguous().view(-1, shape[-1])
+    y8 = torch.empty(x2.shape, dtype=torch.float8_e4m3fn, device=x.device)
+    scale = torch.empty((x2.shape[0],), dtype=torch.float32, device=x.device)
+    h = None if r2 is None else torch.empty_like(r2)
+    rmsnorm_fwd_fp8(x2, r2, weight.contiguous(), y8, scale, h, eps)
+    return y8.view(shape), scale.view(shape[:-1]), None if h is None else h.view(shape)
+
+
+def rms_norm_fp8(x, weight, eps: float = 1e-6):
+    """(y8, scale): rms_norm(x, weight) in 8 bits, y ~ y8 * scale[..., None] with y8 float8_e4m3fn [..., D] and one fp32 scale a
+    row, max|y| / 448.  D a multiple of 16.  No backward."""
+    _no_backward("rms_norm_fp8", x, weight)
+    out = (_native or native_calls()).rms_norm_fp8(x, weight, float(eps))
+    return _rms_norm_fp8(x, None, weight, float(eps))[:2] if out is None else out
+
+
+def add_rms_norm_fp8(x, residual, weight, eps: float = 1e-6):
+    """(y8, scale, h): add_rms_norm with y in 8 bits, as rms_norm_fp8 gives it.  No backward."""
+    _check_residual(x, residual)
+    _no_backward("add_rms_norm_fp8", x, residual, weight)
+    out = (_native or native_calls()).add_rms_norm_fp8(x, residual, weight, float(eps))
+    return _rms_norm_fp8(x, residual, weight, float(eps)) if out is None else out
+
+
+def quantize_rows(x):
+    """(x8, scale) with x ~ x8 * scale[..., None]: the rows (last axis, a multiple of 16) of a bf16 or fp16 tensor in 8 bits
+    (float8_e4m3fn) with one fp32 scale a row, max|x| / 448.  For a weight [N, K] that linear_fp8 reads, and for activations
+    that no norm produces.  No backward."""
+    _no_backward("quantize_rows", x)
+    out = (_native or native_calls()).quantize_rows(x)
+    if out is not None:
+        return out
+    x2 = x.contiguous().view(-1, x.shape[-1])
+    x8 = torch.empty(x2.shape, dtype=torch.float8_e4m3fn, device=x.device)
+    scale = torch.empty((x2.shape[0],), dtype=torch.float32, device=x.device)
+    _quantize_rows(x2, x8, scale)
+    return x8.view(x.shape), scale.view(x.shape[:-1])
+
+
+def linear_fp8(x8, x_scale, w8, w_scale, bias=None, dtype=torch.bfloat16):
+    """linear(x, w, bias) of rows in 8 bits: x ~ x8 * x_scale[..., None] with x8 [..., K], w ~ w8 * w_scale[:, None] with w8
+    [N, K] (both float8_e4m3fn, scales fp32, as rms_norm_fp8 and quantize_rows give them), bias fp32 [N] or None.  The
+    result [..., N] is bf16 or fp16 (`dtype`), summed in fp32 and rounded once.  K a multiple of 16, N of 8.  No backward."""
+    _no_backward("linear_fp8", x8, x_scale, w8, w_scale, bias)
+    y = (_native or native_calls()).linear_fp8(x8, x_scale, w8, w_scale, bias, dtype == torch.float16, dtype == torch.bfloat16)
+    if y is not None:
+        return y
+    K = x8.shape[-1]
+    if w8.dim() != 2 or w8.shape[1] != K:
+        raise ValueError(f"w8 must have shape (N, {K}), got {tuple(w8.shape)}")
+    if x_scale.shape != x8.shape[:-1]:
+        raise ValueError(f"x_scale must have shape {tuple(x8.shape[:-1])}, got {tuple(x_scale.shape)}")
+    x2 = x8.contiguous().view(-1, K)
+    y = torch.empty((x2.shape[0], w8.shape[0]), dtype=dtype, device=x8.device)
+    _linear_fp8(x2, x_scale.contiguous().view(-1), w8.contiguous(), w_scale.contiguous(), None if bias is None else bias.contiguous(), y)
+    return y.view(*x8.shape[:-1], w8.shape[0])

@@ -17,6 +17,7 @@
 #include "avion_flow.h"
 #include "avion_fwd.h"
 #include "avion_head.h"
+#include "avion_host.h"
 #include "avion_ln.h"
 #include "avion_pair.h"
 #include "avion_small.h"
@@ -30,14 +31,6 @@ constexpr size_t kScratchBytes = size_t(32) << 20;
 static __device__ __align__(256) unsigned char scratch[kScratchBytes];
 
 namespace {
-
-thread_local char g_hip_error[256] = "";
-
-int hip_fail(hipError_t e, const char* what)
-{
-    std::snprintf(g_hip_error, sizeof g_hip_error, "%s: %s", what, hipGetErrorString(e));
-    return AVION_EHIP;
-}
 
 // Device address of `scratch` on each GPU, looked up once per device with that device current.
 constexpr int kMaxDevices = 64;
@@ -60,8 +53,6 @@ int scratch_of_current_device(void** out)
     *out = g_scratch_ptr[dev];
     return AVION_OK;
 }
-
-bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
 // Token strides (elements between consecutive tokens of one head) of the two tensor groups.
 struct Strides {
@@ -101,27 +92,6 @@ bool grid_for(long long nblocks, unsigned* grid)
     if (padded > 0x7fffffffLL) return false;
     *grid = (unsigned)padded;
     return true;
-}
-
-// Raises the kernel's dynamic LDS limit once; `done` is the caller's per-instance flag.  A failure
-// is not remembered, so the next call tries again.
-template <typename K>
-hipError_t allow_lds(K kernel, int bytes, std::atomic<bool>& done)
-{
-    if (done.load(std::memory_order_acquire)) return hipSuccess;
-    const hipError_t e =
-        hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
-    if (e == hipSuccess) done.store(true, std::memory_order_release);
-    return e;
-}
-
-// Result of the launch just made on this thread.  Errors left behind by earlier, unrelated work of
-// the caller are cleared before the launch (begin_launch) so that they are not mistaken for it.
-void begin_launch() { (void)hipGetLastError(); }
-int end_launch(const char* what)
-{
-    const hipError_t e = hipGetLastError();
-    return e == hipSuccess ? AVION_OK : hip_fail(e, what);
 }
 
 template <int D, int NW, int KG, typename E, bool CAUSAL>
@@ -303,10 +273,6 @@ int launch_win_bwd(const raw16* q, const raw16* k, const raw16* v, const raw16* 
 // Kernel instances by head size, format and masking (wavefronts per workgroup: fwd_cut, bwd_cut and head_impl below).
 // by_variant calls f(head dim, element format, causal) with the three as compile-time tags, by_format
 // f(element format, causal).
-template <typename T>
-struct TypeTag {
-    using type = T;
-};
 template <typename F>
 int by_format(Variant var, F f)
 {

@@ -1,0 +1,514 @@
+// Token table: lookup with scaling, and the table's gradient by sorted tokens.
+//     y_i = s W[t_i];     dW[v] = s sum over i with t_i = v, in ascending i, of dy_i
+// A token outside [0, V) names no row: its y is zero and it adds to no gradient (padding, another device's share of a table).
+//
+// Lookup: bound by memory bandwidth, one read of a row and one write; a thread moves 16-byte pieces, several in flight.
+//
+// Gradient: reads dy once and writes every row of dW once (rows that no token names: zeros).  Floating-point sums in a fixed
+// order, no atomics on them: results are bit-reproducible.
+//   up to kEmbSmallTokens tokens: one launch.  A workgroup per (slot, 512 columns) ends at once unless its slot is the first
+//   with its token; else it collects the slots with that token, in order, and sums their rows.  Further workgroups clear the
+//   rows that no token names.
+//   beyond: the slots are sorted by token (stable radix sort, digits of up to 10 bits; per digit one launch that counts and one
+//   that places: each of at most 256 workgroups adds up the counts of the ones before it itself, so nothing waits for another
+//   workgroup), then a workgroup sums the rows of kEmbChunk sorted slots, writes the sums of the tokens that begin and end
+//   among them, and leaves what spans a border to a last launch, as fp32 sums: a token that fills most slots (padding) is
+//   spread over the chip like any others.  The unnamed rows are cleared by spare workgroups of the first placing launch, whose
+//   sort is bound by latency.  Whether a token is named: the counting launch writes each slot's number to stamp[token] (plain
+//   stores, any one of them is right), and row v is named if stamp[v] is a slot whose token is v, so the stamps need no
+//   clearing before.
+#pragma once
+#include "avion_common.h"
+#include "avion_ln.h"
+
+constexpr int kEmbThreads = 256;
+constexpr int kEmbFly = 4;                // pieces in flight per thread in the lookup
+constexpr int kEmbSmallTokens = 1024;     // at most this many: gradient in one launch
+constexpr int kEmbCols = 512;             // columns of a workgroup in the sums: 8 per lane
+constexpr int kEmbChunk = 128;            // sorted slots of a workgroup: 32 per wavefront
+constexpr int kEmbSortTile = 1024;        // slots that a sorting workgroup places at a time: 256 per wavefront
+constexpr int kEmbSortGrid = 256;         // sorting workgroups at most
+constexpr int kEmbMaxBins = 1024;
+constexpr int kEmbClearBytes = 1 << 15;   // of the table that a clearing workgroup looks after
+
+template <typename T>
+DEVINL unsigned token_key(const T* tokens, long i, int V)
+{
+    const long t = (long)tokens[i];
+    return t >= 0 && t < V ? (unsigned)t : (unsigned)V;  // V: no row
+}
+
+// 8 values of a row of the table or of dy
+template <typename E>
+DEVINL void emb_load8(const void* base, long at, float (&v)[8])
+{
+    if constexpr (std::is_same_v<E, float>) {
+        load8(static_cast<const float*>(base) + at, v);
+    } else {
+        const u32x4 c = *reinterpret_cast<const u32x4*>(static_cast<const raw16*>(base) + at);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = E::widen(as_frag8(c), e);
+    }
+}
+template <typename E>
+DEVINL void emb_store8(void* base, long at, const float (&v)[8])
+{
+    if constexpr (std::is_same_v<E, float>) {
+        store8(static_cast<float*>(base) + at, v);
+    } else {
+        u32x4 w;
+#pragma unroll
+        for (int p = 0; p < 4; ++p) w[p] = E::pack(v[2 * p], v[2 * p + 1]);
+        *reinterpret_cast<u32x4*>(static_cast<raw16*>(base) + at) = w;
+    }
+}
+
+// T: token type, TE: table's format (16-bit or fp32), E: output's.  pieces = D / 8; magic = ceil(2^32 / pieces).
+template <typename T, typename TE, typename E>
+__global__ void __launch_bounds__(kEmbThreads)
+avion_embedding_fwd_kernel(const T* __restrict__ tokens, const void* __restrict__ table, raw16* __restrict__ y, long n, int V,
+                           int D, float scale, int pieces, unsigned magic)
+{
+    const long total = n * pieces, base = (long)blockIdx.x * (kEmbThreads * kEmbFly);
+    const long row0 = base / pieces;
+    const unsigned rem = (unsigned)(base - row0 * pieces);  // < pieces; rem + kEmbThreads * kEmbFly stays below 2^16
+    unsigned key[kEmbFly], piece[kEmbFly];
+    long row[kEmbFly];
+#pragma unroll
+    for (int k = 0; k < kEmbFly; ++k) {
+        const unsigned at = rem + threadIdx.x + kEmbThreads * k;
+        const unsigned down = pieces == 1 ? at : (unsigned)(((unsigned long)at * magic) >> 32);
+        row[k] = row0 + down;
+        piece[k] = at - down * pieces;
+        key[k] = row[k] < n ? token_key(tokens, row[k], V) : (unsigned)V;
+    }
+    float v[kEmbFly][8];
+#pragma unroll
+    for (int k = 0; k < kEmbFly; ++k) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[k][e] = 0.f;
+        if (key[k] != (unsigned)V) emb_load8<TE>(table, (long)key[k] * D + piece[k] * 8, v[k]);
+    }
+#pragma unroll
+    for (int k = 0; k < kEmbFly; ++k) {
+        if (base + threadIdx.x + kEmbThreads * k >= total) continue;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[k][e] = key[k] != (unsigned)V ? v[k][e] * scale : 0.f;
+        emb_store8<E>(y, row[k] * D + piece[k] * 8, v[k]);
+    }
+}
+
+// the rows [first, first + rows) of the table that `named` does not claim, cleared by this workgroup
+template <typename TE, typename F>
+DEVINL void emb_clear(void* dtable, long first, long rows, int D, F named)
+{
+    const float zero[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
+    for (long r = first + wave; r < first + rows; r += kEmbThreads / 64) {
+        if (named(r)) continue;
+        for (int c = lane * 8; c < D; c += 512) emb_store8<TE>(dtable, r * D + c, zero);
+    }
+}
+
+// ------------------------------------------------------------------------- gradient, few tokens
+// grid: (ncol * n) workgroups of slots, then clearing ones of `rows` table rows each (rows <= kEmbSmallRows)
+constexpr int kEmbSmallRows = 1024;
+template <typename T, typename E, typename TE>
+__global__ void __launch_bounds__(kEmbThreads)
+avion_embedding_bwd_small_kernel(const T* __restrict__ tokens, const raw16* __restrict__ dy, void* __restrict__ dtable, int n,
+                                 int V, int D, float scale, int ncol, int rows)
+{
+    __shared__ unsigned keys[kEmbSmallTokens];
+    __shared__ unsigned short slots[kEmbSmallTokens];
+    __shared__ unsigned char flags[kEmbSmallRows];
+    __shared__ int counts[kEmbSmallTokens / 64];
+    __shared__ float sums[3][kEmbCols];
+    const int tid = threadIdx.x, lane = tid % 64, wave = tid / 64;
+    if ((int)blockIdx.x >= ncol * n) {
+        const long first = (long)((int)blockIdx.x - ncol * n) * rows;
+        const long here = V - first < rows ? V - first : rows;
+        for (int i = tid; i < rows; i += kEmbThreads) flags[i] = 0;
+        __syncthreads();
+        for (int i = tid; i < n; i += kEmbThreads) {
+            const long at = (long)token_key(tokens, i, V) - first;
+            if (at >= 0 && at < here) flags[at] = 1;
+        }
+        __syncthreads();
+        emb_clear<TE>(dtable, first, here, D, [&](long r) { return flags[r - first] != 0; });
+        return;
+    }
+    const int slot = blockIdx.x / ncol, col = (blockIdx.x % ncol) * kEmbCols + lane * 8;
+    const unsigned key = token_key(tokens, slot, V);
+    if (key == (unsigned)V) return;
+    bool before = false;
+    for (int i = tid; i < n; i += kEmbThreads) {
+        keys[i] = token_key(tokens, i, V);
+        before |= i < slot && keys[i] == key;
+    }
+    if (__syncthreads_or(before)) return;
+    // the slots with this token, in order: 64 at a time by vote, places by the votes before
+    const int groups = (n + 63) / 64;
+    for (int g = wave; g < groups; g += kEmbThreads / 64) {
+        const int i = g * 64 + lane;
+        const unsigned long hit = __ballot(i < n && keys[i] == key);
+        if (lane == 0) counts[g] = __popcll(hit);
+    }
+    __syncthreads();
+    int total = 0;
+    for (int g = 0; g < groups; ++g) {
+        if (g % (kEmbThreads / 64) == wave) {
+            const int i = g * 64 + lane;
+            const bool mine = i < n && keys[i] == key;
+            const unsigned long hit = __ballot(mine);
+            if (mine) slots[total + __popcll(hit & ((1ul << lane) - 1))] = (unsigned short)i;
+        }
+        total += counts[g];
+    }
+    __syncthreads();
+    float acc[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    if (col < D) {
+        int i = wave;
+        for (; i + 12 < total; i += 16) {
+            float v[4][8];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) emb_load8<E>(dy, (long)slots[i + 4 * k] * D + col, v[k]);
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) acc[e] += v[k][e];
+        }
+        for (; i < total; i += 4) {
+            float v[8];
+            emb_load8<E>(dy, (long)slots[i] * D + col, v);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) acc[e] += v[e];
+        }
+    }
+    if (total > 1) {
+        if (wave > 0) store8(&sums[wave - 1][lane * 8], acc);
+        __syncthreads();
+        if (wave == 0)
+#pragma unroll
+            for (int w = 0; w < 3; ++w)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) acc[e] += sums[w][lane * 8 + e];
+    }
+    if (wave == 0 && col < D) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) acc[e] *= scale;
+        emb_store8<TE>(dtable, (long)key * D + col, acc);
+    }
+}
+
+// ------------------------------------------------------------------------------------- the sort
+// Each of gridDim.x (hist) workgroups owns `per` consecutive slots.  FIRST: keys come from the tokens, slots are their own
+// numbers, and the stamps are written.
+template <typename T, bool FIRST>
+__global__ void __launch_bounds__(kEmbThreads)
+avion_embedding_hist_kernel(const T* __restrict__ tokens, const unsigned* __restrict__ keys, unsigned* __restrict__ stamp,
+                            unsigned* __restrict__ hist, long n, int V, long per, int shift, int bins)
+{
+    __shared__ unsigned count[kEmbMaxBins];
+    for (int b = threadIdx.x; b < bins; b += kEmbThreads) count[b] = 0;
+    __syncthreads();
+    const long from = (long)blockIdx.x * per, to = from + per < n ? from + per : n;
+    for (long i = from + threadIdx.x; i < to; i += kEmbThreads) {
+        unsigned key;
+        if constexpr (FIRST) {
+            key = token_key(tokens, i, V);
+            if (key != (unsigned)V) stamp[key] = (unsigned)i;
+        } else {
+            key = keys[i];
+        }
+        atomicAdd(&count[(key >> shift) & (bins - 1)], 1u);  // integers: the order does not matter
+    }
+    __syncthreads();
+    for (int b = threadIdx.x; b < bins; b += kEmbThreads) hist[(long)blockIdx.x * bins + b] = count[b];
+}
+
+// the first nsort workgroups place their slots by this digit, the others (FIRST) clear `rows` table rows each
+template <typename T, bool FIRST, typename TE>
+__global__ void __launch_bounds__(kEmbThreads)
+avion_embedding_place_kernel(const T* __restrict__ tokens, const unsigned* __restrict__ keys, const unsigned* __restrict__ slots,
+                             const unsigned* __restrict__ hist, const unsigned* __restrict__ stamp, unsigned* __restrict__ keys_out,
+                             unsigned* __restrict__ slots_out, void* __restrict__ dtable, long n, int V, int D, long per, int nsort,
+                             int shift, int bits, int rows)
+{
+    constexpr int WAVES = kEmbThreads / 64;
+    __shared__ unsigned base[kEmbMaxBins];          // where the next slot with this digit goes
+    __shared__ unsigned count[WAVES][kEmbMaxBins];  // of a tile, by wavefront; then each wavefront's places
+    __shared__ unsigned part[WAVES];
+    const int tid = threadIdx.x, lane = tid % 64, wave = tid / 64, bins = 1 << bits;
+    if constexpr (FIRST) {
+        if ((int)blockIdx.x >= nsort) {
+            const long first = (long)((int)blockIdx.x - nsort) * rows;
+            emb_clear<TE>(dtable, first, V - first < rows ? V - first : rows, D, [&](long r) {
+                const unsigned s = stamp[r];
+                return s < n && token_key(tokens, s, V) == (unsigned)r;
+            });
+            return;
+        }
+    }
+    // a digit's first place: all slots with a smaller digit, then this digit's slots of the workgroups before
+    const int each = (bins + kEmbThreads - 1) / kEmbThreads;  // consecutive digits of a thread: 1, 2 or 4
+    unsigned total[kEmbMaxBins / kEmbThreads], ahead[kEmbMaxBins / kEmbThreads], mine = 0;
+#pragma unroll
+    for (int k = 0; k < kEmbMaxBins / kEmbThreads; ++k) {
+        total[k] = ahead[k] = 0;
+        const int b = tid * each + k;
+        if (k < each && b < bins) {
+#pragma unroll 8
+            for (int g = 0; g < nsort; ++g) {
+                const unsigned c = hist[(long)g * bins + b];
+                total[k] += c;
+                if (g < (int)blockIdx.x) ahead[k] += c;
+            }
+            mine += total[k];
+        }
+    }
+    unsigned upto = mine;  // sum over the threads of this wavefront up to this one
+#pragma unroll
+    for (int off = 1; off < 64; off <<= 1) {
+        const unsigned o = __shfl_up(upto, off, 64);
+        if (lane >= off) upto += o;
+    }
+    if (lane == 63) part[wave] = upto;
+    __syncthreads();
+    unsigned start = upto - mine;
+    for (int w = 0; w < wave; ++w) start += part[w];
+#pragma unroll
+    for (int k = 0; k < kEmbMaxBins / kEmbThreads; ++k) {
+        const int b = tid * each + k;
+        if (k < each && b < bins) base[b] = start + ahead[k];
+        start += total[k];
+    }
+    const long from = (long)blockIdx.x * per, to = from + per < n ? from + per : n;
+    for (long tile = from; tile < to; tile += kEmbSortTile) {
+        for (int b = tid; b < WAVES * bins; b += kEmbThreads) count[b >> bits][b & (bins - 1)] = 0;
+        __syncthreads();
+        constexpr int ROUNDS = kEmbSortTile / kEmbThreads;
+        unsigned key[ROUNDS], slot[ROUNDS], rank[ROUNDS];
+#pragma unroll
+        for (int r = 0; r < ROUNDS; ++r) {
+            const long i = tile + wave * (kEmbSortTile / WAVES) + r * 64 + lane;
+            key[r] = slot[r] = 0;
+            if (i < to) {
+                key[r] = FIRST ? token_key(tokens, i, V) : keys[i];
+                slot[r] = FIRST ? (unsigned)i : slots[i];
+            }
+        }
+        // a slot's rank among its wavefront's with the same digit: the lanes below that vote alike, and the rounds before
+#pragma unroll
+        for (int r = 0; r < ROUNDS; ++r) {
+            const bool in = tile + wave * (kEmbSortTile / WAVES) + r * 64 + lane < to;
+            const unsigned digit = (key[r] >> shift) & (bins - 1);
+            unsigned long same = __ballot(in);
+            for (int b = 0; b < bits; ++b) {
+                const unsigned long vote = __ballot((digit >> b) & 1);
+                same &= (digit >> b) & 1 ? vote : ~vote;
+            }
+            const unsigned below = __popcll(same & ((1ul << lane) - 1));
+            rank[r] = 0;
+            if (in) {
+                volatile unsigned* c = &count[wave][digit];
+                rank[r] = *c + below;
+                if (below == 0) *c = rank[r] + __popcll(same);
+            }
+            __builtin_amdgcn_wave_barrier();
+        }
+        __syncthreads();
+        for (int b = tid; b < bins; b += kEmbThreads) {
+            unsigned at = base[b];
+#pragma unroll
+            for (int w = 0; w < WAVES; ++w) {
+                const unsigned c = count[w][b];
+                count[w][b] = at;
+                at += c;
+            }
+            base[b] = at;
+        }
+        __syncthreads();
+#pragma unroll
+        for (int r = 0; r < ROUNDS; ++r) {
+            const long i = tile + wave * (kEmbSortTile / WAVES) + r * 64 + lane;
+            if (i < to) {
+                const unsigned p = count[wave][(key[r] >> shift) & (bins - 1)] + rank[r];
+                if (p < n) {  // always, unless the tokens change between the launches
+                    keys_out[p] = key[r];
+                    slots_out[p] = slot[r];
+                }
+            }
+        }
+        __syncthreads();
+    }
+}
+
+// ------------------------------------------------------------------------------------- the sums
+// Sums of kEmbChunk sorted slots in 512 columns.  heads[chunk][D]: the sum of a token that began in a chunk before, tails: of
+// one that begins here and goes on in the next.
+template <typename E, typename TE>
+__global__ void __launch_bounds__(kEmbThreads)
+avion_embedding_sum_kernel(const unsigned* __restrict__ keys, const unsigned* __restrict__ slots, const raw16* __restrict__ dy,
+                           void* __restrict__ dtable, float* __restrict__ heads, float* __restrict__ tails, long n, int V, int D,
+                           float scale)
+{
+    constexpr int WAVES = kEmbThreads / 64, PER = kEmbChunk / WAVES, FLY = 8;
+    __shared__ float sh_head[WAVES][kEmbCols], sh_tail[WAVES][kEmbCols];
+    __shared__ unsigned sh_key[WAVES];  // of the tail
+    __shared__ int sh_what[WAVES];      // 1: has a head, 2: the head ends here, 4: has a tail
+    const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+    const int col = blockIdx.y * kEmbCols + lane * 8;
+    const bool in = col < D;
+    const long first = (long)blockIdx.x * kEmbChunk + wave * PER;
+    const int count = first >= n ? 0 : n - first < PER ? (int)(n - first) : PER;
+    const unsigned none = (unsigned)V;
+    // lane l: key and slot of sorted place first + l (l < count), lane 63: the key before, lane 62: the key after
+    unsigned key = none, slot = 0;
+    if (lane < count) {
+        key = min(keys[first + lane], none);
+        slot = min(slots[first + lane], (unsigned)(n - 1));  // (both hold, unless the tokens change between the launches)
+    } else if (lane == 63 && first > 0 && first <= n) {
+        key = keys[first - 1];
+    } else if (lane == 62 && first + count < n) {
+        key = keys[first + count];
+    }
+    const unsigned key_before = __builtin_amdgcn_readlane(key, 63), key_after = __builtin_amdgcn_readlane(key, 62);
+    int what = 0;
+    float acc[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    const unsigned key0 = __builtin_amdgcn_readfirstlane(key);
+    bool head = count > 0 && first > 0 && key0 == key_before && key0 != none;
+    if (head) what = 1;
+    for (int i0 = 0; i0 < count; i0 += FLY) {
+        u32x4 raw[FLY];
+#pragma unroll
+        for (int k = 0; k < FLY; ++k) {
+            const int i = i0 + k;
+            const unsigned ki = __builtin_amdgcn_readlane(key, i < PER ? i : 0), si = __builtin_amdgcn_readlane(slot, i < PER ? i : 0);
+            raw[k] = u32x4{0u, 0u, 0u, 0u};
+            if (i < count && ki != none && in) raw[k] = *reinterpret_cast<const u32x4*>(dy + (long)si * D + col);
+        }
+#pragma unroll
+        for (int k = 0; k < FLY; ++k) {
+            const int i = i0 + k;
+            if (i >= count) break;
+            const unsigned ki = __builtin_amdgcn_readlane(key, i);
+            if (ki == none) break;  // the slots without a row are the last ones
+#pragma unroll
+            for (int e = 0; e < 8; ++e) acc[e] += E::widen(as_frag8(raw[k]), e);
+            const bool last = i == count - 1;
+            const unsigned next = last ? key_after : __builtin_amdgcn_readlane(key, i < PER - 1 ? i + 1 : 0);
+            if (next == ki && !last) continue;
+            if (next == ki && head) {             // one token, from before this wavefront's slots to behind them
+                store8(&sh_head[wave][lane * 8], acc);
+            } else if (next == ki) {              // begins here, goes on behind
+                store8(&sh_tail[wave][lane * 8], acc);
+                what |= 4;
+                if (lane == 0) sh_key[wave] = ki;
+            } else if (head) {                    // began before, ends here
+                store8(&sh_head[wave][lane * 8], acc);
+                what |= 2;
+                head = false;
+            } else if (in) {
+                float o[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) o[e] = acc[e] * scale;
+                emb_store8<TE>(dtable, (long)ki * D + col, o);
+            }
+#pragma unroll
+            for (int e = 0; e < 8; ++e) acc[e] = 0.f;
+        }
+    }
+    if (lane == 0) sh_what[wave] = what;
+    __syncthreads();
+    // the parts that meet at the wavefronts' borders, in order
+    if (wave != 0 || !in) return;
+    bool running = false, began_here = false;
+    unsigned run_key = none;
+    float run[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    for (int w = 0; w < WAVES; ++w) {
+        const int f = sh_what[w];
+        if (f & 1) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) run[e] += sh_head[w][lane * 8 + e];
+            running = true;
+            if (f & 2) {
+                if (began_here) {
+                    float o[8];
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) o[e] = run[e] * scale;
+                    emb_store8<TE>(dtable, (long)run_key * D + col, o);
+                } else {
+                    store8(heads + (long)blockIdx.x * D + col, run);
+                }
+                running = began_here = false;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) run[e] = 0.f;
+            }
+        }
+        if (f & 4) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) run[e] = sh_tail[w][lane * 8 + e];
+            running = began_here = true;
+            run_key = sh_key[w];
+        }
+    }
+    if (running) store8((began_here ? tails : heads) + (long)blockIdx.x * D + col, run);
+}
+
+// The tokens that span chunks: the workgroup of the chunk where one begins adds its tail and the heads behind it, in a fixed
+// order: 64 groups of threads each take every 64th, 64 columns a workgroup.
+constexpr int kEmbJoinGroups = 64, kEmbJoinCols = 64;
+template <typename TE>
+__global__ void __launch_bounds__(kEmbJoinGroups * kEmbJoinCols / 4)
+avion_embedding_join_kernel(const unsigned* __restrict__ keys, const float* __restrict__ heads, const float* __restrict__ tails,
+                            void* __restrict__ dtable, long n, int V, int D, float scale, long nchunks)
+{
+    constexpr int LANES = kEmbJoinCols / 4, THREADS = kEmbJoinGroups * LANES, FLY = 4;
+    __shared__ f32x4 sh[kEmbJoinGroups][LANES];
+    const long c = blockIdx.x, end = (c + 1) * kEmbChunk;
+    if (end >= n) return;
+    const unsigned key = keys[end - 1];
+    if (key >= (unsigned)V || keys[end] != key) return;
+    if (c > 0 && keys[c * kEmbChunk - 1] == key) return;  // began before this chunk
+    // the chunks whose first slot has this token follow this one without a gap
+    long behind = 0;
+    for (long from = c + 1; from < nchunks; from += THREADS) {
+        const long q = from + threadIdx.x;
+        const int hits = __syncthreads_count(q < nchunks && keys[q * kEmbChunk] == key);
+        behind += hits;
+        if (hits < THREADS) break;
+    }
+    const int lane = threadIdx.x % LANES, group = threadIdx.x / LANES;
+    const int col = blockIdx.y * kEmbJoinCols + lane * 4;
+    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+    if (col < D) {
+        const float* p = heads + (c + 1) * D + col;
+        if (group == 0) acc = *reinterpret_cast<const f32x4*>(tails + c * D + col);
+        long q = group;
+        for (; q + (FLY - 1) * kEmbJoinGroups < behind; q += FLY * kEmbJoinGroups) {
+            f32x4 v[FLY];
+#pragma unroll
+            for (int k = 0; k < FLY; ++k) v[k] = *reinterpret_cast<const f32x4*>(p + (q + k * kEmbJoinGroups) * D);
+#pragma unroll
+            for (int k = 0; k < FLY; ++k) acc += v[k];
+        }
+        for (; q < behind; q += kEmbJoinGroups) acc += *reinterpret_cast<const f32x4*>(p + q * D);
+    }
+    sh[group][lane] = acc;
+    for (int half = kEmbJoinGroups / 2; half > 0; half /= 2) {
+        __syncthreads();
+        if (group < half) {
+            acc += sh[group + half][lane];
+            sh[group][lane] = acc;
+        }
+    }
+    if (group == 0 && col < D) {
+        acc *= scale;
+        if constexpr (std::is_same_v<TE, float>) {
+            *reinterpret_cast<f32x4*>(static_cast<float*>(dtable) + (long)key * D + col) = acc;
+        } else {
+            *reinterpret_cast<u32x2*>(static_cast<raw16*>(dtable) + (long)key * D + col) =
+                u32x2{TE::pack(acc[0], acc[1]), TE::pack(acc[2], acc[3])};
+        }
+    }
+}

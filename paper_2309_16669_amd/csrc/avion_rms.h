@@ -1,0 +1,384 @@
+// Root-mean-square normalisation together with the residual's addition in front of it, forward and backward, its form with
+// an 8-bit output, and the same rounding to 8 bits for a tensor as it is.  Per token row, x, r in R^D, gains w:
+//     h = x + r (rounded to the format of r: the norm is of what the residual stream holds; h = x without r)
+//     rstd = 1 / sqrt(mean(h^2) + eps),  y = h rstd w
+//     8 bits: s = max(max|y|, 2^-96) / 448,  q = e4m3(y / s): each row fills the format's range (largest value 448)
+//     backward, with xhat = h rstd, g = dy w and dh the gradient that reaches h by its other use:
+//     dw = sum_rows dy xhat,   dx = dr = rstd (g - xhat mean(g xhat)) + dh
+// What the backward needs from the forward is h itself, which the stream keeps anyway, and one fp32 per row.
+//
+// Bound by memory bandwidth: forward two reads and two writes per element, backward three reads and one write (two with a
+// stream in 32 bits).  WPR wavefronts own a row at a time, lane j of them the 16-byte chunks j, j + 64 WPR, ...: all of the
+// row is in registers, so it is read once, and the next row is requested before the current one is worked on.  Sums and
+// statistics are fp32, outputs are rounded once (nearest even).  max|y| is rstd max|h w|, so that the row's sum and its maximum
+// travel through one exchange.  The gains' gradient is summed over each wavefront's rows in registers, over the workgroup's
+// through LDS and over the workgroups by avion_ln_param_reduce_kernel in a fixed order: no atomics, bit-reproducible.
+#pragma once
+#include "avion_common.h"
+#include "avion_ln.h"
+
+constexpr int kRmsWaves = 4;            // wavefronts of a workgroup (as many as a row's, where a row has more)
+constexpr int kRmsMaxGrid = 1024;       // workgroups of a launch; also the number of partial sums of the gains' gradient
+constexpr int kRmsMaxD = 16384;         // 8 wavefronts x 4 chunks x 64 lanes x 8
+constexpr float kF8Max = 448.0f;        // largest finite e4m3 value
+constexpr float kF8Least = 1.2621774483536189e-29f;  // 2^-96: a row's largest magnitude counts as at least this
+
+DEVINL float wave_max(float x)
+{
+#pragma unroll
+    for (int off = 1; off < 32; off <<= 1) x = fmaxf(x, __shfl_xor(x, off, 64));
+    return both_halves_max(x);
+}
+
+// 8 fp32 -> 8 e4m3 (nearest even).  |v| < 464 or NaN.
+DEVINL u32x2 pack_fp8(const float (&v)[8])
+{
+    u32x2 w;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        int p = __builtin_amdgcn_cvt_pk_fp8_f32(v[4 * i], v[4 * i + 1], 0, false);
+        p = __builtin_amdgcn_cvt_pk_fp8_f32(v[4 * i + 2], v[4 * i + 3], p, true);
+        w[i] = (unsigned)p;
+    }
+    return w;
+}
+
+// A lane's share of a row: NCH chunks of 8 elements, 16-bit (E) or fp32
+template <int NCH, int WPR, typename E>
+struct RmsRow {
+    u32x4 c[NCH];
+    DEVINL void load(const void* base, long row, int D, int nchunks, int at)
+    {
+        const u32x4 zero = {0u, 0u, 0u, 0u};
+        const raw16* p = static_cast<const raw16*>(base) + row * D;
+#pragma unroll
+        for (int j = 0; j < NCH; ++j) {
+            const int ch = at + 64 * WPR * j;
+            c[j] = ch < nchunks ? *reinterpret_cast<const u32x4*>(p + ch * 8) : zero;
+        }
+    }
+    DEVINL float get(int j, int e) const { return E::widen(as_frag8(c[j]), e); }
+    DEVINL static void store(void* base, long row, int D, int ch, const float (&v)[8])
+    {
+        u32x4 w;
+#pragma unroll
+        for (int p = 0; p < 4; ++p) w[p] = E::pack(v[2 * p], v[2 * p + 1]);
+        *reinterpret_cast<u32x4*>(static_cast<raw16*>(base) + row * D + ch * 8) = w;
+    }
+    // v as the format holds it
+    DEVINL static void round(float (&v)[8])
+    {
+        u32x4 w;
+#pragma unroll
+        for (int p = 0; p < 4; ++p) w[p] = E::pack(v[2 * p], v[2 * p + 1]);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = E::widen(as_frag8(w), e);
+    }
+};
+template <int NCH, int WPR>
+struct RmsRow<NCH, WPR, float> {
+    f32x4 c[NCH][2];
+    DEVINL void load(const void* base, long row, int D, int nchunks, int at)
+    {
+        const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
+        const float* p = static_cast<const float*>(base) + row * D;
+#pragma unroll
+        for (int j = 0; j < NCH; ++j) {
+            const int ch = at + 64 * WPR * j;
+            c[j][0] = ch < nchunks ? *reinterpret_cast<const f32x4*>(p + ch * 8) : zero;
+            c[j][1] = ch < nchunks ? *reinterpret_cast<const f32x4*>(p + ch * 8 + 4) : zero;
+        }
+    }
+    DEVINL float get(int j, int e) const { return c[j][e / 4][e % 4]; }
+    DEVINL static void store(void* base, long row, int D, int ch, const float (&v)[8])
+    {
+        store8(static_cast<float*>(base) + row * D + ch * 8, v);
+    }
+    DEVINL static void round(float (&)[8]) {}
+};
+
+// Sum of a (and maximum of b) over the WPR wavefronts of a row.  Through LDS where there is more than one; two places, used
+// in turn by consecutive rows: a wavefront writes the other one only after the barrier that everybody's reads of the one
+// before precede.
+template <int WPR, bool MAX>
+DEVINL void row_reduce(float& a, float& b, float (&sh)[2][WPR][2], int wave, int lane, int& turn)
+{
+    a = wave_sum(a);
+    if (MAX) b = wave_max(b);
+    if constexpr (WPR > 1) {
+        if (lane == 0) {
+            sh[turn][wave][0] = a;
+            if (MAX) sh[turn][wave][1] = b;
+        }
+        __syncthreads();
+        a = sh[turn][0][0];
+        if (MAX) b = sh[turn][0][1];
+#pragma unroll
+        for (int w = 1; w < WPR; ++w) {
+            a += sh[turn][w][0];
+            if (MAX) b = fmaxf(b, sh[turn][w][1]);
+        }
+        turn ^= 1;
+    }
+}
+
+// Rows of one workgroup: WPR = 1: one row per wavefront at a time; else one row per workgroup
+template <int WPR>
+struct RmsWork {
+    static constexpr int WAVES = WPR > kRmsWaves ? WPR : kRmsWaves;
+    static constexpr int ROWS = WAVES / WPR;  // rows at a time
+};
+
+// y (E), or y8 and scale with F8; h where there is a residual; rstd where it is asked for
+template <int WPR, int NCH, typename E, typename R, bool F8>
+__global__ void __launch_bounds__(RmsWork<WPR>::WAVES * 64)
+avion_rmsnorm_fwd_kernel(const raw16* __restrict__ x, const void* __restrict__ residual, const float* __restrict__ weight,
+                         void* __restrict__ y, float* __restrict__ scale, void* __restrict__ h, float* __restrict__ rstd,
+                         long M, int D, float eps)
+{
+    using W = RmsWork<WPR>;
+    __shared__ float sh[2][WPR][2];
+    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, at = WPR == 1 ? lane : (int)threadIdx.x;
+    const int nchunks = D / 8;
+    const float inv_d = 1.0f / (float)D;
+    const long stride = (long)gridDim.x * W::ROWS;
+    long row = (long)blockIdx.x * W::ROWS + (WPR == 1 ? wave : 0);
+    if (row >= M) return;
+    float gain[NCH][8];
+    int turn = 0;
+
+    RmsRow<NCH, WPR, E> xa, xb;
+    RmsRow<NCH, WPR, R> ra, rb;
+    auto load = [&](RmsRow<NCH, WPR, E>& xr, RmsRow<NCH, WPR, R>& rr, long n) {
+        xr.load(x, n, D, nchunks, at);
+        if (residual) rr.load(residual, n, D, nchunks, at);
+    };
+    load(xa, ra, row);
+#pragma unroll
+    for (int j = 0; j < NCH; ++j) {
+        const int ch = at + 64 * WPR * j;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) gain[j][e] = 0.f;
+        if (ch < nchunks) load8(weight + ch * 8, gain[j]);
+    }
+
+    auto finish = [&](const RmsRow<NCH, WPR, E>& xr, const RmsRow<NCH, WPR, R>& rr, long n) {
+        float v[NCH][8], ss = 0.f, big = 0.f;
+#pragma unroll
+        for (int j = 0; j < NCH; ++j) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[j][e] = xr.get(j, e);
+            if (residual) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[j][e] += rr.get(j, e);
+                RmsRow<NCH, WPR, R>::round(v[j]);
+            }
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                ss = fmaf(v[j][e], v[j][e], ss);  // chunks past the row are zeros
+                if (F8) big = fmaxf(big, fabsf(v[j][e] * gain[j][e]));
+            }
+        }
+        row_reduce<WPR, F8>(ss, big, sh, wave, lane, turn);
+        const float rs = __builtin_amdgcn_rsqf(fmaf(ss, inv_d, eps));
+        float inv = rs;
+        if (F8) {
+            big = fmaxf(big * rs, kF8Least);
+            inv = kF8Max / big;
+        }
+#pragma unroll
+        for (int j = 0; j < NCH; ++j) {
+            const int ch = at + 64 * WPR * j;
+            if (ch < nchunks) {
+                if (residual) RmsRow<NCH, WPR, R>::store(h, n, D, ch, v[j]);
+                float o[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) o[e] = v[j][e] * rs * gain[j][e];
+                if constexpr (F8) {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) o[e] *= inv;
+                    *reinterpret_cast<u32x2*>(static_cast<char*>(y) + n * D + ch * 8) = pack_fp8(o);
+                } else {
+                    RmsRow<NCH, WPR, E>::store(y, n, D, ch, o);
+                }
+            }
+        }
+        if (at == 0) {
+            if (F8) scale[n] = big * (1.0f / kF8Max);
+            if (rstd) rstd[n] = rs;
+        }
+    };
+
+    // two rows in registers: the next one is in flight while the current one is worked on
+    while (true) {
+        const long n1 = row + stride;
+        if (n1 < M) load(xb, rb, n1);
+        finish(xa, ra, row);
+        if (n1 >= M) break;
+        const long n2 = n1 + stride;
+        if (n2 < M) load(xa, ra, n2);
+        finish(xb, rb, n1);
+        if (n2 >= M) break;
+        row = n2;
+    }
+}
+
+// rows of x as they are, in 8 bits
+template <int WPR, int NCH, typename E>
+__global__ void __launch_bounds__(RmsWork<WPR>::WAVES * 64)
+avion_quantize_rows_kernel(const raw16* __restrict__ x, void* __restrict__ y, float* __restrict__ scale, long M, int D)
+{
+    using W = RmsWork<WPR>;
+    __shared__ float sh[2][WPR][2];
+    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, at = WPR == 1 ? lane : (int)threadIdx.x;
+    const int nchunks = D / 8;
+    const long stride = (long)gridDim.x * W::ROWS;
+    long row = (long)blockIdx.x * W::ROWS + (WPR == 1 ? wave : 0);
+    if (row >= M) return;
+    int turn = 0;
+    auto finish = [&](const RmsRow<NCH, WPR, E>& xr, long n) {
+        float none = 0.f, big = 0.f;
+#pragma unroll
+        for (int j = 0; j < NCH; ++j)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) big = fmaxf(big, fabsf(xr.get(j, e)));
+        row_reduce<WPR, true>(none, big, sh, wave, lane, turn);
+        big = fmaxf(big, kF8Least);
+        const float inv = kF8Max / big;
+#pragma unroll
+        for (int j = 0; j < NCH; ++j) {
+            const int ch = at + 64 * WPR * j;
+            if (ch < nchunks) {
+                float o[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) o[e] = xr.get(j, e) * inv;
+                *reinterpret_cast<u32x2*>(static_cast<char*>(y) + n * D + ch * 8) = pack_fp8(o);
+            }
+        }
+        if (at == 0) scale[n] = big * (1.0f / kF8Max);
+    };
+    RmsRow<NCH, WPR, E> a, b;
+    a.load(x, row, D, nchunks, at);
+    while (true) {
+        const long n1 = row + stride;
+        if (n1 < M) b.load(x, n1, D, nchunks, at);
+        finish(a, row);
+        if (n1 >= M) break;
+        const long n2 = n1 + stride;
+        if (n2 < M) a.load(x, n2, D, nchunks, at);
+        finish(b, n1);
+        if (n2 >= M) break;
+        row = n2;
+    }
+}
+
+// dx (E; the gradient of both inputs where the stream has that format too), dr (fp32 stream), either may be absent, and this
+// workgroup's partial sums of the gains' gradient into part[blockIdx.x][D].  dh may be absent.
+template <int WPR, int NCH, typename E, typename R>
+__global__ void __launch_bounds__(RmsWork<WPR>::WAVES * 64)
+avion_rmsnorm_bwd_kernel(const void* __restrict__ h, const float* __restrict__ weight, const float* __restrict__ rstd,
+                         const raw16* __restrict__ dy, const void* __restrict__ dh, void* __restrict__ dx,
+                         float* __restrict__ dr, float* __restrict__ part, long M, int D)
+{
+    using W = RmsWork<WPR>;
+    extern __shared__ __attribute__((aligned(16))) char smem[];  // WPR = 1: (kRmsWaves - 1) x D floats
+    __shared__ float sh[2][WPR][2];
+    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, at = WPR == 1 ? lane : (int)threadIdx.x;
+    const int nchunks = D / 8;
+    const float inv_d = 1.0f / (float)D;
+    const long stride = (long)gridDim.x * W::ROWS;
+    long row = (long)blockIdx.x * W::ROWS + (WPR == 1 ? wave : 0);
+    float gain[NCH][8], dw[NCH][8];
+    int turn = 0;
+#pragma unroll
+    for (int j = 0; j < NCH; ++j) {
+        const int ch = at + 64 * WPR * j;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) gain[j][e] = dw[j][e] = 0.f;
+        if (ch < nchunks) load8(weight + ch * 8, gain[j]);
+    }
+
+    struct Rows {
+        RmsRow<NCH, WPR, R> h, dh;
+        RmsRow<NCH, WPR, E> dy;
+        float rs;
+    };
+    auto load = [&](Rows& t, long n) {
+        t.h.load(h, n, D, nchunks, at);
+        t.dy.load(dy, n, D, nchunks, at);
+        if (dh) t.dh.load(dh, n, D, nchunks, at);
+        t.rs = rstd[n];
+    };
+    auto finish = [&](const Rows& t, long n) {
+        float s = 0.f, none = 0.f;
+#pragma unroll
+        for (int j = 0; j < NCH; ++j)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const float xh = t.h.get(j, e) * t.rs, gy = t.dy.get(j, e);
+                s = fmaf(gy * gain[j][e], xh, s);  // zero in chunks past the row
+                dw[j][e] = fmaf(gy, xh, dw[j][e]);
+            }
+        row_reduce<WPR, false>(s, none, sh, wave, lane, turn);
+        const float c = s * inv_d;
+#pragma unroll
+        for (int j = 0; j < NCH; ++j) {
+            const int ch = at + 64 * WPR * j;
+            if (ch < nchunks) {
+                float o[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    o[e] = t.rs * (t.dy.get(j, e) * gain[j][e] - t.h.get(j, e) * t.rs * c);
+                    if (dh) o[e] += t.dh.get(j, e);
+                }
+                if (dx) RmsRow<NCH, WPR, E>::store(dx, n, D, ch, o);
+                if (dr) store8(dr + n * D + ch * 8, o);
+            }
+        }
+    };
+    if (row < M) {
+        Rows a, b;
+        load(a, row);
+        while (true) {
+            const long n1 = row + stride;
+            if (n1 < M) load(b, n1);
+            finish(a, row);
+            if (n1 >= M) break;
+            const long n2 = n1 + stride;
+            if (n2 < M) load(a, n2);
+            finish(b, n1);
+            if (n2 >= M) break;
+            row = n2;
+        }
+    }
+    float* out = part + (long)blockIdx.x * D;
+    if constexpr (WPR == 1) {
+        // workgroup sum in wavefront order (0 + 1 + 2 + 3)
+        float* sums = reinterpret_cast<float*>(smem);
+        if (wave > 0) {
+#pragma unroll
+            for (int j = 0; j < NCH; ++j) {
+                const int ch = at + 64 * j;
+                if (ch < nchunks) store8(sums + (wave - 1) * D + ch * 8, dw[j]);
+            }
+        }
+        __syncthreads();
+        if (wave > 0) return;
+#pragma unroll
+        for (int j = 0; j < NCH; ++j) {
+            const int ch = at + 64 * j;
+            if (ch < nchunks)
+                for (int w = 0; w < W::WAVES - 1; ++w) {
+                    float a[8];
+                    load8(sums + w * D + ch * 8, a);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) dw[j][e] += a[e];
+                }
+        }
+    }
+#pragma unroll
+    for (int j = 0; j < NCH; ++j) {
+        const int ch = at + 64 * WPR * j;
+        if (ch < nchunks) store8(out + ch * 8, dw[j]);
+    }
+}

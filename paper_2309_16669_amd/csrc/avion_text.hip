@@ -1,0 +1,410 @@
+// C ABI of the text encoder's entry and of the 8-bit path: token table, RMS normalisation with the residual's addition,
+// rows in 8 bits and their product.  See include/avion_attn.h for the contract of every entry point.
+#include "avion_attn.h"
+
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+
+#include "avion_embed.h"
+#include "avion_fp8.h"
+#include "avion_host.h"
+#include "avion_rms.h"
+
+namespace {
+
+constexpr long long kComputeUnits = 256;
+
+template <typename F>
+int by_element(unsigned flags, F f)
+{
+    if (flags & AVION_FLAG_F16) return f(TypeTag<F16>{});
+    return f(TypeTag<Bf16>{});
+}
+template <int N>
+using Int = std::integral_constant<int, N>;
+
+// ------------------------------------------------------------------------------ RMS normalisation
+int rms_check(long long M, int D, unsigned flags, unsigned allowed)
+{
+    if (M < 0 || D < 1) return AVION_EINVAL;
+    if (flags & ~allowed) return AVION_EINVAL;
+    if (D % 8 != 0 || D > kRmsMaxD) return AVION_EUNSUPPORTED;
+    if (M > (1LL << 40)) return AVION_EUNSUPPORTED;
+    return AVION_OK;
+}
+// Wavefronts a row.  One holds up to 2048 columns (4 chunks a lane) and needs no exchange through LDS; wider rows take four, or
+// eight beyond 8192.  Few rows take four as well.
+int rms_wavefronts(long long M, int D)
+{
+    if (D > 8192) return 8;
+    if (D > 2048 || (D > 512 && M <= 1024)) return 4;
+    return 1;
+}
+unsigned rms_grid(long long M, int D)
+{
+    const int rows = rms_wavefronts(M, D) == 1 ? kRmsWaves : 1;
+    return (unsigned)std::min<long long>((M + rows - 1) / rows, kRmsMaxGrid);
+}
+// f(wavefronts a row, chunks a lane)
+template <typename F>
+int rms_by_width(long long M, int D, F f)
+{
+    const int wpr = rms_wavefronts(M, D), per_lane = (D / 8 + 64 * wpr - 1) / (64 * wpr);
+    if (wpr == 8) return f(Int<8>{}, Int<4>{});
+    if (wpr == 4) {
+        if (per_lane <= 1) return f(Int<4>{}, Int<1>{});
+        if (per_lane <= 2) return f(Int<4>{}, Int<2>{});
+        return f(Int<4>{}, Int<4>{});
+    }
+    if (per_lane <= 1) return f(Int<1>{}, Int<1>{});
+    if (per_lane <= 2) return f(Int<1>{}, Int<2>{});
+    return f(Int<1>{}, Int<4>{});
+}
+// f(stream's format): E, or fp32
+template <typename E, typename F>
+int rms_by_stream(unsigned flags, F f)
+{
+    if (flags & AVION_FLAG_WIDE_F32) return f(TypeTag<float>{});
+    return f(TypeTag<E>{});
+}
+
+template <bool F8>
+int rmsnorm_fwd_impl(const void* x, const void* residual, const float* weight, void* y, float* scale, void* h, float* rstd, long long M,
+                     int D, float eps, unsigned flags, void* stream)
+{
+    const int rc = rms_check(M, D, flags, AVION_FLAG_F16 | AVION_FLAG_WIDE_F32);
+    if (rc != AVION_OK) return rc;
+    if (!(eps >= 0.f) || !std::isfinite(eps)) return AVION_EINVAL;
+    if (M == 0) return AVION_OK;
+    if (!x || !weight || !y || (F8 && !scale) || (residual == nullptr) != (h == nullptr)) return AVION_EINVAL;
+    if (!residual && (flags & AVION_FLAG_WIDE_F32)) return AVION_EINVAL;
+    const void* ptrs[] = {x, residual, weight, y, scale, h, rstd};
+    for (const void* p : ptrs)
+        if (!aligned16(p)) return AVION_EUNSUPPORTED;
+    if (F8 && D % 16 != 0) return AVION_EUNSUPPORTED;
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    return by_element(flags, [&](auto fmt) {
+        using E = typename decltype(fmt)::type;
+        return rms_by_stream<E>(flags, [&](auto wide) {
+            return rms_by_width(M, D, [&](auto wpr, auto nch) {
+                constexpr int WPR = decltype(wpr)::value;
+                begin_launch();
+                hipLaunchKernelGGL((avion_rmsnorm_fwd_kernel<WPR, decltype(nch)::value, E, typename decltype(wide)::type, F8>),
+                                   dim3(rms_grid(M, D)), dim3(RmsWork<WPR>::WAVES * 64), 0, st, static_cast<const raw16*>(x),
+                                   residual, weight, y, scale, h, rstd, (long)M, D, eps);
+                return end_launch("launch avion_rmsnorm_fwd_kernel");
+            });
+        });
+    });
+}
+
+// --------------------------------------------------------------------------------- token table
+constexpr unsigned kEmbFlags = AVION_FLAG_F16 | AVION_FLAG_WIDE_F32 | AVION_FLAG_TOKENS_I32;
+constexpr int kEmbMaxD = 65536;
+constexpr long long kEmbMax = 1LL << 28;  // slots, and rows of the table
+
+int embedding_check(long long n, long long V, int D, unsigned flags)
+{
+    if (n < 0 || V < 1 || D < 1) return AVION_EINVAL;
+    if (flags & ~kEmbFlags) return AVION_EINVAL;
+    if (D % 8 != 0 || D > kEmbMaxD || V > kEmbMax || n > kEmbMax) return AVION_EUNSUPPORTED;
+    if (n * (D / 8) > (1LL << 34)) return AVION_EUNSUPPORTED;  // workgroups of the lookup
+    return AVION_OK;
+}
+// f(token type, table's format, output's format)
+template <typename F>
+int embedding_by_type(unsigned flags, F f)
+{
+    return by_element(flags, [&](auto fmt) {
+        auto by_table = [&](auto tok) {
+            if (flags & AVION_FLAG_WIDE_F32) return f(tok, TypeTag<float>{}, fmt);
+            return f(tok, fmt, fmt);
+        };
+        if (flags & AVION_FLAG_TOKENS_I32) return by_table(TypeTag<int>{});
+        return by_table(TypeTag<long>{});
+    });
+}
+// How the gradient of n slots is cut: digits of the sort, its workgroups, chunks of the sums, and where all of it lies.
+struct EmbeddingPlan {
+    int passes, bits, nsort;
+    long long per, nchunks;
+    size_t keys[2], slots[2], hist, stamp, heads, tails, bytes;
+    EmbeddingPlan(long long n, long long V, int D)
+    {
+        if (n <= kEmbSmallTokens) {
+            bytes = 256;
+            return;
+        }
+        int need = 0;  // keys 0 .. V
+        while ((V >> need) != 0) ++need;
+        passes = (need + 9) / 10;
+        bits = (need + passes - 1) / passes;
+        // whole tiles a workgroup, at most kEmbSortGrid workgroups
+        const long long tiles = (n + kEmbSortTile - 1) / kEmbSortTile;
+        per = (tiles + kEmbSortGrid - 1) / kEmbSortGrid * kEmbSortTile;
+        nsort = (int)((n + per - 1) / per);
+        nchunks = (n + kEmbChunk - 1) / kEmbChunk;
+        size_t at = 0;
+        auto take = [&](size_t b) {
+            const size_t here = at;
+            at += round256(b);
+            return here;
+        };
+        for (int i = 0; i < 2; ++i) keys[i] = take(n * 4);
+        for (int i = 0; i < 2; ++i) slots[i] = take(n * 4);
+        hist = take((size_t)nsort * 4 << bits);
+        stamp = take(V * 4);
+        heads = take((size_t)nchunks * D * 4);
+        tails = take((size_t)nchunks * D * 4);
+        bytes = at;
+    }
+};
+// table rows of a clearing workgroup
+int clear_rows(long long V, int D, size_t element, int most)
+{
+    const long long fits = kEmbClearBytes / ((long long)D * (long long)element);
+    return (int)std::min<long long>(std::max({fits, 1LL, (V >> 20) + 1}), most);
+}
+
+// ------------------------------------------------------------------------------- 8-bit product
+template <int MT, typename E>
+int launch_few(const char* x8, const float* xs, const char* w8, const float* ws, const float* bias, raw16* y, int M, int N, int K,
+               hipStream_t st)
+{
+    begin_launch();
+    hipLaunchKernelGGL((avion_linear_fp8_few_kernel<MT, E>), dim3((N + 15) / 16), dim3(kFewWaves * 64), 0, st, x8, xs, w8, ws, bias, y,
+                       M, N, K);
+    return end_launch("launch avion_linear_fp8_few_kernel");
+}
+long long fp8_tiles(int M, int N, int tm, int tn) { return (long long)((M + tm - 1) / tm) * ((N + tn - 1) / tn); }
+template <int TM, int TN, int WM, int WN, typename E>
+int launch_fp8(const char* x8, const float* xs, const char* w8, const float* ws, const float* bias, raw16* y, int M, int N, int K,
+               hipStream_t st)
+{
+    using Cfg = Fp8Cfg<TM, TN, WM, WN>;
+    static std::atomic<bool> lds_allowed{false};
+    const auto kernel = avion_linear_fp8_kernel<TM, TN, WM, WN, E>;
+    const hipError_t attr = allow_lds(kernel, Cfg::LDS_BYTES, lds_allowed);
+    if (attr != hipSuccess) return hip_fail(attr, "hipFuncSetAttribute(linear_fp8)");
+    const long long tiles = fp8_tiles(M, N, TM, TN);
+    const unsigned grid = (unsigned)((tiles + 7) / 8 * 8);
+    begin_launch();
+    hipLaunchKernelGGL(kernel, dim3(grid), dim3(Cfg::NT), Cfg::LDS_BYTES, st, x8, xs, w8, ws, bias, y, M, N, K, (N + TN - 1) / TN,
+                       (int)tiles);
+    return end_launch("launch avion_linear_fp8_kernel");
+}
+
+}  // namespace
+
+extern "C" {
+
+int avion_rmsnorm_fwd(const void* x, const void* residual, const float* weight, void* y, void* h, float* rstd, long long M, int D,
+                      float eps, unsigned flags, void* stream)
+{
+    return rmsnorm_fwd_impl<false>(x, residual, weight, y, nullptr, h, rstd, M, D, eps, flags, stream);
+}
+
+int avion_rmsnorm_fwd_fp8(const void* x, const void* residual, const float* weight, void* y8, float* scale, void* h, long long M,
+                          int D, float eps, unsigned flags, void* stream)
+{
+    return rmsnorm_fwd_impl<true>(x, residual, weight, y8, scale, h, nullptr, M, D, eps, flags, stream);
+}
+
+size_t avion_rmsnorm_bwd_workspace_bytes(long long M, int D)
+{
+    if (rms_check(M, D, 0, 0) != AVION_OK) return 0;
+    return round256(std::max<size_t>((size_t)rms_grid(M, D) * D * sizeof(float), 1));
+}
+
+int avion_rmsnorm_bwd(const void* h, const float* weight, const float* rstd, const void* dy, const void* dh, void* dx, float* dresidual,
+                      float* dweight, long long M, int D, unsigned flags, void* workspace, size_t workspace_bytes, void* stream)
+{
+    const int rc = rms_check(M, D, flags, AVION_FLAG_F16 | AVION_FLAG_WIDE_F32);
+    if (rc != AVION_OK) return rc;
+    if (!dweight) return AVION_EINVAL;
+    if (M > 0 && (!h || !weight || !rstd || !dy)) return AVION_EINVAL;
+    if (dresidual && !(flags & AVION_FLAG_WIDE_F32)) return AVION_EINVAL;
+    const void* ptrs[] = {h, weight, rstd, dy, dh, dx, dresidual, dweight};
+    for (const void* p : ptrs)
+        if (!aligned16(p)) return AVION_EUNSUPPORTED;
+    if (!workspace_fits(workspace, workspace_bytes, avion_rmsnorm_bwd_workspace_bytes(M, D))) return AVION_EWORKSPACE;
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    float* part = static_cast<float*>(workspace);
+    const unsigned grid = rms_grid(M, D);
+    if (M > 0) {
+        const int r1 = by_element(flags, [&](auto fmt) {
+            using E = typename decltype(fmt)::type;
+            return rms_by_stream<E>(flags, [&](auto wide) {
+                return rms_by_width(M, D, [&](auto wpr, auto nch) {
+                    constexpr int WPR = decltype(wpr)::value;
+                    begin_launch();
+                    hipLaunchKernelGGL((avion_rmsnorm_bwd_kernel<WPR, decltype(nch)::value, E, typename decltype(wide)::type>),
+                                       dim3(grid), dim3(RmsWork<WPR>::WAVES * 64), WPR == 1 ? (kRmsWaves - 1) * D * sizeof(float) : 0,
+                                       st, h, weight, rstd, static_cast<const raw16*>(dy), dh, dx, dresidual, part, (long)M, D);
+                    return end_launch("launch avion_rmsnorm_bwd_kernel");
+                });
+            });
+        });
+        if (r1 != AVION_OK) return r1;
+    }
+    // sums over the workgroups (none: zeros); the reduction kernel splits its 2 * (D / 2) columns into two outputs
+    begin_launch();
+    hipLaunchKernelGGL((avion_ln_param_reduce_kernel<void>), dim3((D + kLnReduceCols - 1) / kLnReduceCols),
+                       dim3(kLnReduceCols * kLnReduceGroups), 0, st, part, dweight, dweight + D / 2, (int)grid, D / 2);
+    return end_launch("launch avion_ln_param_reduce_kernel");
+}
+
+int avion_quantize_rows(const void* x, void* x8, float* scale, long long M, int D, unsigned flags, void* stream)
+{
+    const int rc = rms_check(M, D, flags, AVION_FLAG_F16);
+    if (rc != AVION_OK) return rc;
+    if (M == 0) return AVION_OK;
+    if (!x || !x8 || !scale) return AVION_EINVAL;
+    if (!aligned16(x) || !aligned16(x8) || !aligned16(scale) || D % 16 != 0) return AVION_EUNSUPPORTED;
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    return by_element(flags, [&](auto fmt) {
+        return rms_by_width(M, D, [&](auto wpr, auto nch) {
+            constexpr int WPR = decltype(wpr)::value;
+            begin_launch();
+            hipLaunchKernelGGL((avion_quantize_rows_kernel<WPR, decltype(nch)::value, typename decltype(fmt)::type>),
+                               dim3(rms_grid(M, D)), dim3(RmsWork<WPR>::WAVES * 64), 0, st, static_cast<const raw16*>(x), x8, scale,
+                               (long)M, D);
+            return end_launch("launch avion_quantize_rows_kernel");
+        });
+    });
+}
+
+int avion_linear_fp8(const void* x8, const float* x_scale, const void* w8, const float* w_scale, const float* bias, void* y,
+                     long long M, int N, int K, unsigned flags, void* stream)
+{
+    if (M < 0 || N < 1 || K < 1 || (flags & ~AVION_FLAG_F16)) return AVION_EINVAL;
+    if (M >= (1LL << 31) - 256 || N % 8 != 0 || N > (1 << 20) || K % 16 != 0 || K > (1 << 16)) return AVION_EUNSUPPORTED;
+    if (fp8_tiles((int)M, N, 64, 64) > (1LL << 24)) return AVION_EUNSUPPORTED;  // workgroups of a launch
+    if (M == 0) return AVION_OK;
+    if (!x8 || !x_scale || !w8 || !w_scale || !y) return AVION_EINVAL;
+    const void* ptrs[] = {x8, x_scale, w8, w_scale, bias, y};
+    for (const void* p : ptrs)
+        if (!aligned16(p)) return AVION_EUNSUPPORTED;
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    const char *x = static_cast<const char*>(x8), *w = static_cast<const char*>(w8);
+    raw16* out = static_cast<raw16*>(y);
+    const int m = (int)M;
+    return by_element(flags, [&](auto fmt) {
+        using E = typename decltype(fmt)::type;
+        if (m <= 16) return launch_few<1, E>(x, x_scale, w, w_scale, bias, out, m, N, K, st);
+        if (m <= 32) return launch_few<2, E>(x, x_scale, w, w_scale, bias, out, m, N, K, st);
+        if (fp8_tiles(m, N, 256, 128) >= 2 * kComputeUnits)
+            return launch_fp8<256, 128, 2, 2, E>(x, x_scale, w, w_scale, bias, out, m, N, K, st);
+        if (fp8_tiles(m, N, 128, 128) >= kComputeUnits)
+            return launch_fp8<128, 128, 2, 2, E>(x, x_scale, w, w_scale, bias, out, m, N, K, st);
+        return launch_fp8<64, 64, 2, 2, E>(x, x_scale, w, w_scale, bias, out, m, N, K, st);
+    });
+}
+
+int avion_embedding_fwd(const void* tokens, const void* table, void* y, long long n, long long V, int D, float scale, unsigned flags,
+                        void* stream)
+{
+    const int rc = embedding_check(n, V, D, flags);
+    if (rc != AVION_OK) return rc;
+    if (!std::isfinite(scale)) return AVION_EINVAL;
+    if (n == 0) return AVION_OK;
+    if (!tokens || !table || !y) return AVION_EINVAL;
+    if (!aligned16(table) || !aligned16(y)) return AVION_EUNSUPPORTED;
+    if (reinterpret_cast<uintptr_t>(tokens) % (flags & AVION_FLAG_TOKENS_I32 ? 4 : 8) != 0) return AVION_EUNSUPPORTED;
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    const int pieces = D / 8;
+    const unsigned magic = (unsigned)(((1ULL << 32) + pieces - 1) / pieces);
+    const long long per = kEmbThreads * kEmbFly, grid = (n * pieces + per - 1) / per;
+    return embedding_by_type(flags, [&](auto tok, auto tab, auto fmt) {
+        using T = typename decltype(tok)::type;
+        begin_launch();
+        hipLaunchKernelGGL((avion_embedding_fwd_kernel<T, typename decltype(tab)::type, typename decltype(fmt)::type>),
+                           dim3((unsigned)grid), dim3(kEmbThreads), 0, st, static_cast<const T*>(tokens), table,
+                           static_cast<raw16*>(y), (long)n, (int)V, D, scale, pieces, magic);
+        return end_launch("launch avion_embedding_fwd_kernel");
+    });
+}
+
+size_t avion_embedding_bwd_workspace_bytes(long long n, long long V, int D)
+{
+    if (embedding_check(n, V, D, 0) != AVION_OK) return 0;
+    return EmbeddingPlan(n, V, D).bytes;
+}
+
+int avion_embedding_bwd(const void* tokens, const void* dy, void* dtable, long long n, long long V, int D, float scale, unsigned flags,
+                        void* workspace, size_t workspace_bytes, void* stream)
+{
+    const int rc = embedding_check(n, V, D, flags);
+    if (rc != AVION_OK) return rc;
+    if (!std::isfinite(scale) || !dtable || (n > 0 && (!tokens || !dy))) return AVION_EINVAL;
+    if (!aligned16(dy) || !aligned16(dtable)) return AVION_EUNSUPPORTED;
+    if (reinterpret_cast<uintptr_t>(tokens) % (flags & AVION_FLAG_TOKENS_I32 ? 4 : 8) != 0) return AVION_EUNSUPPORTED;
+    const EmbeddingPlan p(n, V, D);
+    if (!workspace_fits(workspace, workspace_bytes, p.bytes)) return AVION_EWORKSPACE;
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    return embedding_by_type(flags, [&](auto tok, auto tab, auto fmt) -> int {
+        using T = typename decltype(tok)::type;
+        using TE = typename decltype(tab)::type;
+        using E = typename decltype(fmt)::type;
+        const T* t = static_cast<const T*>(tokens);
+        const raw16* g = static_cast<const raw16*>(dy);
+        const size_t element = std::is_same_v<TE, float> ? 4 : 2;
+        const dim3 block(kEmbThreads);
+        const int ncol = (D + kEmbCols - 1) / kEmbCols;
+        if (n <= kEmbSmallTokens) {
+            const int rows = clear_rows(V, D, element, kEmbSmallRows);
+            begin_launch();
+            hipLaunchKernelGGL((avion_embedding_bwd_small_kernel<T, E, TE>), dim3((unsigned)(ncol * n + (V + rows - 1) / rows)), block,
+                               0, st, t, g, dtable, (int)n, (int)V, D, scale, ncol, rows);
+            return end_launch("launch avion_embedding_bwd_small_kernel");
+        }
+        char* ws = static_cast<char*>(workspace);
+        unsigned *keys[2], *slots[2];
+        for (int i = 0; i < 2; ++i) {
+            keys[i] = reinterpret_cast<unsigned*>(ws + p.keys[i]);
+            slots[i] = reinterpret_cast<unsigned*>(ws + p.slots[i]);
+        }
+        unsigned *hist = reinterpret_cast<unsigned*>(ws + p.hist), *stamp = reinterpret_cast<unsigned*>(ws + p.stamp);
+        float *heads = reinterpret_cast<float*>(ws + p.heads), *tails = reinterpret_cast<float*>(ws + p.tails);
+        const int rows = clear_rows(V, D, element, 1 << 28);
+        for (int pass = 0; pass < p.passes; ++pass) {
+            const int to = pass % 2, from = 1 - to, shift = pass * p.bits, bins = 1 << p.bits;
+            const unsigned clearing = pass == 0 ? (unsigned)((V + rows - 1) / rows) : 0u;
+            begin_launch();
+            if (pass == 0)
+                hipLaunchKernelGGL((avion_embedding_hist_kernel<T, true>), dim3(p.nsort), block, 0, st, t, keys[from], stamp, hist, (long)n,
+                                   (int)V, (long)p.per, shift, bins);
+            else
+                hipLaunchKernelGGL((avion_embedding_hist_kernel<T, false>), dim3(p.nsort), block, 0, st, t, keys[from], stamp, hist, (long)n,
+                                   (int)V, (long)p.per, shift, bins);
+            int rk = end_launch("launch avion_embedding_hist_kernel");
+            if (rk != AVION_OK) return rk;
+            begin_launch();
+            if (pass == 0)
+                hipLaunchKernelGGL((avion_embedding_place_kernel<T, true, TE>), dim3(p.nsort + clearing), block, 0, st, t, keys[from],
+                                   slots[from], hist, stamp, keys[to], slots[to], dtable, (long)n, (int)V, D, (long)p.per, p.nsort,
+                                   shift, p.bits, rows);
+            else
+                hipLaunchKernelGGL((avion_embedding_place_kernel<T, false, TE>), dim3(p.nsort), block, 0, st, t, keys[from], slots[from],
+                                   hist, stamp, keys[to], slots[to], dtable, (long)n, (int)V, D, (long)p.per, p.nsort, shift, p.bits,
+                                   rows);
+            rk = end_launch("launch avion_embedding_place_kernel");
+            if (rk != AVION_OK) return rk;
+        }
+        const int last = (p.passes - 1) % 2;
+        begin_launch();
+        hipLaunchKernelGGL((avion_embedding_sum_kernel<E, TE>), dim3((unsigned)p.nchunks, ncol), block, 0, st, keys[last], slots[last], g,
+                           dtable, heads, tails, (long)n, (int)V, D, scale);
+        const int rs = end_launch("launch avion_embedding_sum_kernel");
+        if (rs != AVION_OK) return rs;
+        begin_launch();
+        hipLaunchKernelGGL((avion_embedding_join_kernel<TE>), dim3((unsigned)p.nchunks, (D + kEmbJoinCols - 1) / kEmbJoinCols),
+                           dim3(kEmbJoinGroups * kEmbJoinCols / 4), 0, st, keys[last], heads, tails, dtable, (long)n, (int)V, D, scale,
+                           (long)p.nchunks);
+        return end_launch("launch avion_embedding_join_kernel");
+    });
+}
+
+}  // extern "C"

@@ -8,6 +8,7 @@
 // formats and shapes, with no transform, mode, tracer or tangent in force.  For anything else it returns
 // None, and the caller goes through the Python classes, which raise or behave as they always did.  Errors
 // of the library are raised as the binding's AvionError.
+#include <c10/core/DeviceGuard.h>
 #include <c10/core/impl/LocalDispatchKeySet.h>
 #include <c10/core/impl/TorchDispatchModeTLS.h>
 #include <c10/hip/HIPStream.h>
@@ -408,6 +409,278 @@ pybind11::object bias_gelu_linear(pybind11::handle x_, pybind11::handle bias_, p
     END_HANDLE_TH_ERRORS_PYBIND
 }
 
+// --------------------------------------------------------- token table, RMS normalisation, 8-bit path
+// These run on the device of their tensors, whatever the current one is.
+unsigned wide_flag(const Tensor& t) { return t.scalar_type() == at::kFloat ? AVION_FLAG_WIDE_F32 : 0u; }
+void* data_of(const Tensor& t) { return t.defined() ? t.data_ptr() : nullptr; }
+
+// As without_lock, for a call with several outputs
+template <typename F>
+pybind11::object many_without_lock(F call)
+{
+    variable_list out;
+    {
+        pybind11::gil_scoped_release release;
+        out = call();
+    }
+    pybind11::tuple t(out.size());
+    for (size_t i = 0; i < out.size(); ++i) t[i] = pybind11::cast(out[i]);
+    return std::move(t);
+}
+
+unsigned embedding_flags(const Tensor& tokens, const Tensor& table, at::ScalarType out)
+{
+    return (out == at::kHalf ? AVION_FLAG_F16 : 0u) | wide_flag(table) | (tokens.scalar_type() == at::kInt ? AVION_FLAG_TOKENS_I32 : 0u);
+}
+Tensor embedding_fwd(const Tensor& tokens, const Tensor& weight_, double scale, at::ScalarType out)
+{
+    const Tensor t = tokens.contiguous(), weight = weight_.contiguous();
+    std::vector<int64_t> shape = tokens.sizes().vec();
+    shape.push_back(weight.size(1));
+    const Tensor y = at::empty(shape, weight.options().dtype(out));
+    check(avion_embedding_fwd(t.data_ptr(), weight.data_ptr(), y.data_ptr(), t.numel(), weight.size(0), (int)weight.size(1), (float)scale,
+                              embedding_flags(t, weight, out), stream()));
+    return y;
+}
+struct Embedding : torch::autograd::Function<Embedding> {
+    static Tensor forward(AutogradContext* ctx, const Tensor& weight, const Tensor& tokens, double scale, bool f16)
+    {
+        const c10::DeviceGuard guard(weight.device());
+        ctx->save_for_backward({tokens});
+        ctx->saved_data["scale"] = scale;
+        ctx->saved_data["shape"] = weight.sizes().vec();
+        ctx->saved_data["format"] = weight.scalar_type();
+        ctx->saved_data["tokens"] = tokens.scalar_type();
+        return embedding_fwd(tokens, weight, scale, f16 ? at::kHalf : at::kBFloat16);
+    }
+    static variable_list backward(AutogradContext* ctx, variable_list grad)
+    {
+        const Tensor dy = grad[0].contiguous(), tokens = ctx->get_saved_variables()[0].contiguous();
+        const c10::DeviceGuard guard(dy.device());
+        const std::vector<int64_t> shape = ctx->saved_data["shape"].toIntVector();
+        const int64_t V = shape[0], D = shape[1], n = dy.numel() / D;
+        require(tokens, "tokens", dy.sizes().slice(0, dy.dim() - 1), ctx->saved_data["tokens"].toScalarType(), dy);
+        const Tensor dweight = at::empty(shape, dy.options().dtype(ctx->saved_data["format"].toScalarType()));
+        const size_t need = avion_embedding_bwd_workspace_bytes(n, V, (int)D);
+        const Tensor ws = workspace(need, dy);
+        check(avion_embedding_bwd(tokens.data_ptr(), dy.data_ptr(), dweight.data_ptr(), n, V, (int)D,
+                                  (float)ctx->saved_data["scale"].toDouble(), embedding_flags(tokens, dweight, dy.scalar_type()),
+                                  ws.data_ptr(), need, stream()));
+        return {dweight, Tensor(), Tensor(), Tensor()};
+    }
+};
+pybind11::object embedding(pybind11::handle tokens_, pybind11::handle weight_, double scale, bool f16, bool bf16)
+{
+    HANDLE_TH_ERRORS
+    const Tensor *tokens, *weight;
+    if (!plain(tokens_.ptr(), &tokens) || !plain(weight_.ptr(), &weight) || !plain_thread() || f16 == bf16) return pybind11::none();
+    const at::ScalarType out = f16 ? at::kHalf : at::kBFloat16;
+    if (weight->dim() != 2 || weight->size(1) > INT32_MAX || tokens->device() != weight->device() ||
+        (weight->scalar_type() != at::kFloat && weight->scalar_type() != out) ||
+        (tokens->scalar_type() != at::kLong && tokens->scalar_type() != at::kInt))
+        return pybind11::none();
+    return without_lock([&] {
+        if (records({weight})) return Embedding::apply(*weight, *tokens, scale, f16);
+        const c10::DeviceGuard guard(weight->device());
+        return embedding_fwd(*tokens, *weight, scale, out);
+    });
+    END_HANDLE_TH_ERRORS_PYBIND
+}
+
+// residual undefined: the norm of x itself.  {y, h (undefined then), rstd (where a backward follows)}
+struct RmsOut {
+    Tensor y, h, rstd, x;
+};
+RmsOut rms_fwd(const Tensor& x_, const Tensor& residual, const Tensor& weight, double eps, bool keep)
+{
+    RmsOut r;
+    r.x = x_.contiguous();
+    const int64_t D = r.x.size(-1), M = r.x.numel() / D;
+    const Tensor res = residual.defined() ? residual.contiguous() : Tensor();
+    r.y = at::empty(r.x.sizes(), r.x.options());
+    if (res.defined()) r.h = at::empty(res.sizes(), res.options());
+    if (keep) r.rstd = at::empty({M}, weight.options());
+    check(avion_rmsnorm_fwd(r.x.data_ptr(), data_of(res), weight.contiguous().data_ptr<float>(), r.y.data_ptr(), data_of(r.h),
+                            static_cast<float*>(data_of(r.rstd)), M, (int)D, (float)eps,
+                            format_flag(r.x) | (res.defined() ? wide_flag(res) : 0u), stream()));
+    return r;
+}
+// {dx, dresidual, dweight}; where the stream has the format of y, dx is the gradient of both
+variable_list rms_bwd(const Tensor& h, const Tensor& weight_, const Tensor& rstd, const Tensor& dy_, const Tensor& dh_, at::ScalarType format,
+                      bool want_dx, bool want_dr)
+{
+    const Tensor& given = dy_.defined() ? dy_ : dh_;
+    const c10::DeviceGuard guard(given.device());
+    const Tensor weight = weight_.contiguous(), dh = dh_.defined() ? dh_.contiguous() : Tensor();
+    const Tensor dy = dy_.defined() ? dy_.contiguous() : at::zeros(given.sizes(), given.options().dtype(format));
+    const int64_t D = given.size(-1), M = given.numel() / D;
+    require(h, "h", given.sizes(), dh.defined() ? dh.scalar_type() : h.scalar_type(), given);
+    TORCH_CHECK_VALUE(h.scalar_type() == format || h.scalar_type() == at::kFloat, "h must be ", format, " or float, got ", h.scalar_type());
+    require(weight, "weight", {D}, at::kFloat, given);
+    require(rstd, "rstd", {M}, at::kFloat, given);
+    const bool wide = h.scalar_type() == at::kFloat;
+    Tensor dx, dr;
+    if (want_dx || !wide) dx = at::empty_like(dy);
+    if (want_dr && wide) dr = at::empty_like(h);
+    const Tensor dweight = at::empty({D}, weight.options());
+    const size_t need = avion_rmsnorm_bwd_workspace_bytes(M, (int)D);
+    const Tensor ws = workspace(need, h);
+    check(avion_rmsnorm_bwd(h.data_ptr(), weight.data_ptr<float>(), rstd.data_ptr<float>(), dy.data_ptr(), data_of(dh), data_of(dx),
+                            static_cast<float*>(data_of(dr)), dweight.data_ptr<float>(), M, (int)D, format_flag(dy) | wide_flag(h),
+                            ws.data_ptr(), need, stream()));
+    return {dx, wide ? dr : dx, dweight};
+}
+struct RmsNorm : torch::autograd::Function<RmsNorm> {
+    static Tensor forward(AutogradContext* ctx, const Tensor& x, const Tensor& weight, double eps)
+    {
+        const c10::DeviceGuard guard(x.device());
+        const RmsOut r = rms_fwd(x, Tensor(), weight, eps, true);
+        ctx->save_for_backward({r.x, weight, r.rstd});  // the input and one float per token
+        return r.y;
+    }
+    static variable_list backward(AutogradContext* ctx, variable_list grad)
+    {
+        const variable_list s = ctx->get_saved_variables();
+        require(s[0], "x", grad[0].sizes(), grad[0].scalar_type(), grad[0]);
+        variable_list g = rms_bwd(s[0], s[1], s[2], grad[0], Tensor(), grad[0].scalar_type(), true, false);
+        return {g[0], g[2], Tensor()};
+    }
+};
+struct AddRmsNorm : torch::autograd::Function<AddRmsNorm> {
+    static variable_list forward(AutogradContext* ctx, const Tensor& x, const Tensor& residual, const Tensor& weight, double eps)
+    {
+        const c10::DeviceGuard guard(x.device());
+        const RmsOut r = rms_fwd(x, residual, weight, eps, true);
+        ctx->set_materialize_grads(false);
+        ctx->save_for_backward({r.h, weight, r.rstd});  // the residual stream, kept anyway, and one float per token; not y
+        ctx->saved_data["format"] = x.scalar_type();
+        return {r.y, r.h};
+    }
+    static variable_list backward(AutogradContext* ctx, variable_list grad)
+    {
+        if (!grad[0].defined() && !grad[1].defined()) return {Tensor(), Tensor(), Tensor(), Tensor()};
+        const variable_list s = ctx->get_saved_variables();
+        variable_list g = rms_bwd(s[0], s[1], s[2], grad[0], grad[1], ctx->saved_data["format"].toScalarType(),
+                                  ctx->needs_input_grad(0), ctx->needs_input_grad(1));
+        g.resize(4);
+        return g;
+    }
+};
+// x, weight and (where there is one) residual of a norm in the expected formats and shapes
+bool rms_args(pybind11::handle x_, pybind11::handle residual_, pybind11::handle weight_, const Tensor** x, const Tensor** residual,
+              const Tensor** weight)
+{
+    if (!plain(x_.ptr(), x) || !plain_thread()) return false;
+    if ((*x)->dim() < 1 || !element_format(**x) || (*x)->size(-1) > INT32_MAX || !parameter(weight_.ptr(), (*x)->size(-1), **x, weight))
+        return false;
+    if (!residual) return true;
+    if (!plain(residual_.ptr(), residual)) return false;
+    const Tensor& r = **residual;
+    return r.sizes() == (*x)->sizes() && r.device() == (*x)->device() &&
+           (r.scalar_type() == (*x)->scalar_type() || r.scalar_type() == at::kFloat);
+}
+pybind11::object rms_norm(pybind11::handle x_, pybind11::handle weight_, double eps)
+{
+    HANDLE_TH_ERRORS
+    const Tensor *x, *weight;
+    if (!rms_args(x_, x_, weight_, &x, nullptr, &weight)) return pybind11::none();
+    return without_lock([&] {
+        if (records({x, weight})) return RmsNorm::apply(*x, *weight, eps);
+        const c10::DeviceGuard guard(x->device());
+        return rms_fwd(*x, Tensor(), *weight, eps, false).y;
+    });
+    END_HANDLE_TH_ERRORS_PYBIND
+}
+pybind11::object add_rms_norm(pybind11::handle x_, pybind11::handle residual_, pybind11::handle weight_, double eps)
+{
+    HANDLE_TH_ERRORS
+    const Tensor *x, *residual, *weight;
+    if (!rms_args(x_, residual_, weight_, &x, &residual, &weight)) return pybind11::none();
+    return many_without_lock([&]() -> variable_list {
+        if (records({x, residual, weight})) return AddRmsNorm::apply(*x, *residual, *weight, eps);
+        const c10::DeviceGuard guard(x->device());
+        const RmsOut r = rms_fwd(*x, *residual, *weight, eps, false);
+        return {r.y, r.h};
+    });
+    END_HANDLE_TH_ERRORS_PYBIND
+}
+
+// ---- 8 bits: no backward; the caller has made sure that nothing records
+variable_list rms_fp8(const Tensor& x_, const Tensor& residual, const Tensor& weight, double eps)
+{
+    const c10::DeviceGuard guard(x_.device());
+    const Tensor x = x_.contiguous(), res = residual.defined() ? residual.contiguous() : Tensor();
+    const int64_t D = x.size(-1), M = x.numel() / D;
+    const Tensor y8 = at::empty(x.sizes(), x.options().dtype(at::kFloat8_e4m3fn));
+    const Tensor scale = at::empty(x.sizes().slice(0, x.dim() - 1), weight.options());
+    const Tensor h = res.defined() ? at::empty(res.sizes(), res.options()) : Tensor();
+    check(avion_rmsnorm_fwd_fp8(x.data_ptr(), data_of(res), weight.contiguous().data_ptr<float>(), y8.data_ptr(), scale.data_ptr<float>(),
+                                data_of(h), M, (int)D, (float)eps, format_flag(x) | (res.defined() ? wide_flag(res) : 0u), stream()));
+    if (h.defined()) return {y8, scale, h};
+    return {y8, scale};
+}
+pybind11::object rms_norm_fp8(pybind11::handle x_, pybind11::handle weight_, double eps)
+{
+    HANDLE_TH_ERRORS
+    const Tensor *x, *weight;
+    if (!rms_args(x_, x_, weight_, &x, nullptr, &weight) || records({x, weight})) return pybind11::none();
+    return many_without_lock([&] { return rms_fp8(*x, Tensor(), *weight, eps); });
+    END_HANDLE_TH_ERRORS_PYBIND
+}
+pybind11::object add_rms_norm_fp8(pybind11::handle x_, pybind11::handle residual_, pybind11::handle weight_, double eps)
+{
+    HANDLE_TH_ERRORS
+    const Tensor *x, *residual, *weight;
+    if (!rms_args(x_, residual_, weight_, &x, &residual, &weight) || records({x, residual, weight})) return pybind11::none();
+    return many_without_lock([&] { return rms_fp8(*x, *residual, *weight, eps); });
+    END_HANDLE_TH_ERRORS_PYBIND
+}
+pybind11::object quantize_rows(pybind11::handle x_)
+{
+    HANDLE_TH_ERRORS
+    const Tensor* x;
+    if (!plain(x_.ptr(), &x) || !plain_thread() || x->dim() < 1 || !element_format(*x) || x->size(-1) > INT32_MAX || records({x}))
+        return pybind11::none();
+    return many_without_lock([&]() -> variable_list {
+        const c10::DeviceGuard guard(x->device());
+        const Tensor in = x->contiguous();
+        const int64_t D = in.size(-1);
+        const Tensor x8 = at::empty(in.sizes(), in.options().dtype(at::kFloat8_e4m3fn));
+        const Tensor scale = at::empty(in.sizes().slice(0, in.dim() - 1), in.options().dtype(at::kFloat));
+        check(avion_quantize_rows(in.data_ptr(), x8.data_ptr(), scale.data_ptr<float>(), in.numel() / D, (int)D, format_flag(in), stream()));
+        return {x8, scale};
+    });
+    END_HANDLE_TH_ERRORS_PYBIND
+}
+pybind11::object linear_fp8(pybind11::handle x8_, pybind11::handle xs_, pybind11::handle w8_, pybind11::handle ws_, pybind11::handle bias_,
+                            bool f16, bool bf16)
+{
+    HANDLE_TH_ERRORS
+    const Tensor *x8, *xs, *w8, *ws, *bias = nullptr;
+    if (!plain(x8_.ptr(), &x8) || !plain(xs_.ptr(), &xs) || !plain(w8_.ptr(), &w8) || !plain_thread() || f16 == bf16)
+        return pybind11::none();
+    if (x8->dim() < 1 || w8->dim() != 2 || x8->scalar_type() != at::kFloat8_e4m3fn || w8->scalar_type() != at::kFloat8_e4m3fn ||
+        w8->size(1) != x8->size(-1) || w8->device() != x8->device() || !fits_int(*w8) || xs->scalar_type() != at::kFloat ||
+        xs->device() != x8->device() || xs->sizes() != x8->sizes().slice(0, x8->dim() - 1))
+        return pybind11::none();
+    if (!parameter(ws_.ptr(), w8->size(0), *x8, &ws) || (!bias_.is_none() && !parameter(bias_.ptr(), w8->size(0), *x8, &bias)))
+        return pybind11::none();
+    if (records({xs, ws}) || (bias && records({bias}))) return pybind11::none();
+    return without_lock([&] {
+        const c10::DeviceGuard guard(x8->device());
+        const Tensor x = x8->contiguous(), s = xs->contiguous(), w = w8->contiguous(), sw = ws->contiguous();
+        const Tensor b = bias ? bias->contiguous() : Tensor();
+        const int64_t K = x.size(-1), N = w.size(0);
+        std::vector<int64_t> shape = x.sizes().vec();
+        shape.back() = N;
+        const Tensor y = at::empty(shape, x.options().dtype(f16 ? at::kHalf : at::kBFloat16));
+        check(avion_linear_fp8(x.data_ptr(), s.data_ptr<float>(), w.data_ptr(), sw.data_ptr<float>(), static_cast<float*>(data_of(b)),
+                               y.data_ptr(), x.numel() / K, (int)N, (int)K, f16 ? AVION_FLAG_F16 : 0u, stream()));
+        return y;
+    });
+    END_HANDLE_TH_ERRORS_PYBIND
+}
+
 }  // namespace
 
 PYBIND11_MODULE(_avion_torch, m)
@@ -418,4 +691,11 @@ PYBIND11_MODULE(_avion_torch, m)
     m.def("layer_norm", &layer_norm);
     m.def("bias_gelu", &bias_gelu);
     m.def("bias_gelu_linear", &bias_gelu_linear);
+    m.def("embedding", &embedding);
+    m.def("rms_norm", &rms_norm);
+    m.def("add_rms_norm", &add_rms_norm);
+    m.def("rms_norm_fp8", &rms_norm_fp8);
+    m.def("add_rms_norm_fp8", &add_rms_norm_fp8);
+    m.def("quantize_rows", &quantize_rows);
+    m.def("linear_fp8", &linear_fp8);
 }
