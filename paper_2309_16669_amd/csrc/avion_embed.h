@@ -11,7 +11,7 @@
 //   rows that no token names.
 //   beyond: the slots are sorted by token (stable radix sort, digits of up to 10 bits; per digit one launch that counts and one
 //   that places: each of at most 256 workgroups adds up the counts of the ones before it itself, so nothing waits for another
-//   workgroup), then a workgroup sums the rows of kEmbChunk sorted slots, writes the sums of the tokens that begin and end
+//   workgroup), then a workgroup sums the rows of a chunk of sorted slots, writes the sums of the tokens that begin and end
 //   among them, and leaves what spans a border to a last launch, as fp32 sums: a token that fills most slots (padding) is
 //   spread over the chip like any others.  The unnamed rows are cleared by spare workgroups of the first placing launch, whose
 //   sort is bound by latency.  Whether a token is named: the counting launch writes each slot's number to stamp[token] (plain
@@ -25,10 +25,13 @@ constexpr int kEmbThreads = 256;
 constexpr int kEmbFly = 4;                // pieces in flight per thread in the lookup
 constexpr int kEmbSmallTokens = 1024;     // at most this many: gradient in one launch
 constexpr int kEmbCols = 512;             // columns of a workgroup in the sums: 8 per lane
-constexpr int kEmbChunk = 128;            // sorted slots of a workgroup: 32 per wavefront
-constexpr int kEmbSortTile = 1024;        // slots that a sorting workgroup places at a time: 256 per wavefront
-constexpr int kEmbSortGrid = 256;         // sorting workgroups at most
-constexpr int kEmbMaxBins = 1024;
+constexpr int kEmbSumWaves = 8;           // of a workgroup in the sums
+constexpr int kEmbSumMost = 32;           // sorted slots of a wavefront there: this many, or
+constexpr int kEmbSumFew = 8;             // where there are fewer than kEmbSumEnough
+constexpr int kEmbSumEnough = 1 << 15;
+constexpr int kEmbSortThreads = 1024;
+constexpr int kEmbSortTile = 2048;        // slots that a sorting workgroup places at a time: 128 per wavefront
+constexpr int kEmbSortGrid = 96;          // sorting workgroups at most
 constexpr int kEmbClearBytes = 1 << 15;   // of the table that a clearing workgroup looks after
 
 template <typename T>
@@ -37,6 +40,25 @@ DEVINL unsigned token_key(const T* tokens, long i, int V)
     const long t = (long)tokens[i];
     return t >= 0 && t < V ? (unsigned)t : (unsigned)V;  // V: no row
 }
+
+// 8 values of a row as they lie in memory
+template <typename E>
+struct EmbPiece {
+    u32x4 c;
+    DEVINL void load(const void* base, long at) { c = *reinterpret_cast<const u32x4*>(static_cast<const raw16*>(base) + at); }
+    DEVINL float get(int e) const { return E::widen(as_frag8(c), e); }
+};
+template <>
+struct EmbPiece<float> {
+    f32x4 c[2];
+    DEVINL void load(const void* base, long at)
+    {
+        const f32x4* p = reinterpret_cast<const f32x4*>(static_cast<const float*>(base) + at);
+        c[0] = p[0];
+        c[1] = p[1];
+    }
+    DEVINL float get(int e) const { return c[e / 4][e % 4]; }
+};
 
 // 8 values of a row of the table or of dy
 template <typename E>
@@ -82,31 +104,36 @@ avion_embedding_fwd_kernel(const T* __restrict__ tokens, const void* __restrict_
         piece[k] = at - down * pieces;
         key[k] = row[k] < n ? token_key(tokens, row[k], V) : (unsigned)V;
     }
-    float v[kEmbFly][8];
+    EmbPiece<TE> v[kEmbFly];
 #pragma unroll
-    for (int k = 0; k < kEmbFly; ++k) {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) v[k][e] = 0.f;
-        if (key[k] != (unsigned)V) emb_load8<TE>(table, (long)key[k] * D + piece[k] * 8, v[k]);
-    }
+    for (int k = 0; k < kEmbFly; ++k)
+        if (key[k] != (unsigned)V) v[k].load(table, (long)key[k] * D + piece[k] * 8);
 #pragma unroll
     for (int k = 0; k < kEmbFly; ++k) {
         if (base + threadIdx.x + kEmbThreads * k >= total) continue;
+        u32x4 w = {0u, 0u, 0u, 0u};
+        if (key[k] != (unsigned)V)
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[k][e] = key[k] != (unsigned)V ? v[k][e] * scale : 0.f;
-        emb_store8<E>(y, row[k] * D + piece[k] * 8, v[k]);
+            for (int p = 0; p < 4; ++p) w[p] = E::pack(v[k].get(2 * p) * scale, v[k].get(2 * p + 1) * scale);
+        __builtin_nontemporal_store(w, reinterpret_cast<u32x4*>(y + row[k] * D + piece[k] * 8));
     }
 }
 
-// the rows [first, first + rows) of the table that `named` does not claim, cleared by this workgroup
-template <typename TE, typename F>
+// The rows [first, first + rows) of the table that `named` does not claim, cleared by this workgroup: a wavefront asks for 64
+// rows at once (one lane each: the answers take two dependent loads).
+template <typename TE, int WAVES, typename F>
 DEVINL void emb_clear(void* dtable, long first, long rows, int D, F named)
 {
     const float zero[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
     const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
-    for (long r = first + wave; r < first + rows; r += kEmbThreads / 64) {
-        if (named(r)) continue;
-        for (int c = lane * 8; c < D; c += 512) emb_store8<TE>(dtable, r * D + c, zero);
+    const long share = (rows + WAVES - 1) / WAVES, from = wave * share, to = from + share < rows ? from + share : rows;
+    for (long r0 = from; r0 < to; r0 += 64) {
+        unsigned long clear = __ballot(r0 + lane < to && !named(first + r0 + lane));
+        while (clear) {
+            const long r = first + r0 + __builtin_ctzl(clear);
+            clear &= clear - 1;
+            for (int c = lane * 8; c < D; c += 512) emb_store8<TE>(dtable, r * D + c, zero);
+        }
     }
 }
 
@@ -134,7 +161,7 @@ avion_embedding_bwd_small_kernel(const T* __restrict__ tokens, const raw16* __re
             if (at >= 0 && at < here) flags[at] = 1;
         }
         __syncthreads();
-        emb_clear<TE>(dtable, first, here, D, [&](long r) { return flags[r - first] != 0; });
+        emb_clear<TE, kEmbThreads / 64>(dtable, first, here, D, [&](long r) { return flags[r - first] != 0; });
         return;
     }
     const int slot = blockIdx.x / ncol, col = (blockIdx.x % ncol) * kEmbCols + lane * 8;
@@ -202,17 +229,19 @@ avion_embedding_bwd_small_kernel(const T* __restrict__ tokens, const raw16* __re
 
 // ------------------------------------------------------------------------------------- the sort
 // Each of gridDim.x (hist) workgroups owns `per` consecutive slots.  FIRST: keys come from the tokens, slots are their own
-// numbers, and the stamps are written.
-template <typename T, bool FIRST>
-__global__ void __launch_bounds__(kEmbThreads)
+// numbers, and the stamps are written.  A digit has BITS bits.
+template <typename T, bool FIRST, int BITS>
+__global__ void __launch_bounds__(kEmbSortThreads)
 avion_embedding_hist_kernel(const T* __restrict__ tokens, const unsigned* __restrict__ keys, unsigned* __restrict__ stamp,
-                            unsigned* __restrict__ hist, long n, int V, long per, int shift, int bins)
+                            unsigned* __restrict__ hist, long n, int V, long per, int shift)
 {
-    __shared__ unsigned count[kEmbMaxBins];
-    for (int b = threadIdx.x; b < bins; b += kEmbThreads) count[b] = 0;
+    constexpr int BINS = 1 << BITS;
+    __shared__ unsigned count[BINS];
+    if (threadIdx.x < BINS) count[threadIdx.x] = 0;
     __syncthreads();
     const long from = (long)blockIdx.x * per, to = from + per < n ? from + per : n;
-    for (long i = from + threadIdx.x; i < to; i += kEmbThreads) {
+#pragma unroll 2
+    for (long i = from + threadIdx.x; i < to; i += kEmbSortThreads) {
         unsigned key;
         if constexpr (FIRST) {
             key = token_key(tokens, i, V);
@@ -220,74 +249,39 @@ avion_embedding_hist_kernel(const T* __restrict__ tokens, const unsigned* __rest
         } else {
             key = keys[i];
         }
-        atomicAdd(&count[(key >> shift) & (bins - 1)], 1u);  // integers: the order does not matter
+        atomicAdd(&count[(key >> shift) & (BINS - 1)], 1u);  // integers: the order does not matter
     }
     __syncthreads();
-    for (int b = threadIdx.x; b < bins; b += kEmbThreads) hist[(long)blockIdx.x * bins + b] = count[b];
+    if (threadIdx.x < BINS) hist[(long)blockIdx.x * BINS + threadIdx.x] = count[threadIdx.x];
 }
 
-// the first nsort workgroups place their slots by this digit, the others (FIRST) clear `rows` table rows each
-template <typename T, bool FIRST, typename TE>
-__global__ void __launch_bounds__(kEmbThreads)
+// The first nsort workgroups place their slots by this digit, the others clear `rows` table rows each, from row clear_from to
+// before clear_to.
+template <typename T, bool FIRST, int BITS, typename TE>
+__global__ void __launch_bounds__(kEmbSortThreads)
 avion_embedding_place_kernel(const T* __restrict__ tokens, const unsigned* __restrict__ keys, const unsigned* __restrict__ slots,
                              const unsigned* __restrict__ hist, const unsigned* __restrict__ stamp, unsigned* __restrict__ keys_out,
                              unsigned* __restrict__ slots_out, void* __restrict__ dtable, long n, int V, int D, long per, int nsort,
-                             int shift, int bits, int rows)
+                             int shift, int rows, long clear_from, long clear_to)
 {
-    constexpr int WAVES = kEmbThreads / 64;
-    __shared__ unsigned base[kEmbMaxBins];          // where the next slot with this digit goes
-    __shared__ unsigned count[WAVES][kEmbMaxBins];  // of a tile, by wavefront; then each wavefront's places
+    constexpr int BINS = 1 << BITS, WAVES = kEmbSortThreads / 64, ROUNDS = kEmbSortTile / kEmbSortThreads, GROUPS = kEmbSortThreads / BINS,
+                  FLY = 32;
+    __shared__ unsigned short count[WAVES][BINS];        // of a tile, by wavefront; then what the wavefronts before have
+    __shared__ unsigned total[GROUPS][BINS], ahead[GROUPS][BINS];
+    __shared__ unsigned base[BINS];                      // where the next slot with this digit goes
     __shared__ unsigned part[WAVES];
-    const int tid = threadIdx.x, lane = tid % 64, wave = tid / 64, bins = 1 << bits;
-    if constexpr (FIRST) {
-        if ((int)blockIdx.x >= nsort) {
-            const long first = (long)((int)blockIdx.x - nsort) * rows;
-            emb_clear<TE>(dtable, first, V - first < rows ? V - first : rows, D, [&](long r) {
-                const unsigned s = stamp[r];
-                return s < n && token_key(tokens, s, V) == (unsigned)r;
-            });
-            return;
-        }
-    }
-    // a digit's first place: all slots with a smaller digit, then this digit's slots of the workgroups before
-    const int each = (bins + kEmbThreads - 1) / kEmbThreads;  // consecutive digits of a thread: 1, 2 or 4
-    unsigned total[kEmbMaxBins / kEmbThreads], ahead[kEmbMaxBins / kEmbThreads], mine = 0;
-#pragma unroll
-    for (int k = 0; k < kEmbMaxBins / kEmbThreads; ++k) {
-        total[k] = ahead[k] = 0;
-        const int b = tid * each + k;
-        if (k < each && b < bins) {
-#pragma unroll 8
-            for (int g = 0; g < nsort; ++g) {
-                const unsigned c = hist[(long)g * bins + b];
-                total[k] += c;
-                if (g < (int)blockIdx.x) ahead[k] += c;
-            }
-            mine += total[k];
-        }
-    }
-    unsigned upto = mine;  // sum over the threads of this wavefront up to this one
-#pragma unroll
-    for (int off = 1; off < 64; off <<= 1) {
-        const unsigned o = __shfl_up(upto, off, 64);
-        if (lane >= off) upto += o;
-    }
-    if (lane == 63) part[wave] = upto;
-    __syncthreads();
-    unsigned start = upto - mine;
-    for (int w = 0; w < wave; ++w) start += part[w];
-#pragma unroll
-    for (int k = 0; k < kEmbMaxBins / kEmbThreads; ++k) {
-        const int b = tid * each + k;
-        if (k < each && b < bins) base[b] = start + ahead[k];
-        start += total[k];
+    const int tid = threadIdx.x, lane = tid % 64, wave = tid / 64;
+    if ((int)blockIdx.x >= nsort) {
+        const long first = clear_from + (long)((int)blockIdx.x - nsort) * rows;
+        emb_clear<TE, WAVES>(dtable, first, clear_to - first < rows ? clear_to - first : rows, D, [&](long r) {
+            const unsigned s = stamp[r];
+            return s < n && token_key(tokens, s, V) == (unsigned)r;
+        });
+        return;
     }
     const long from = (long)blockIdx.x * per, to = from + per < n ? from + per : n;
-    for (long tile = from; tile < to; tile += kEmbSortTile) {
-        for (int b = tid; b < WAVES * bins; b += kEmbThreads) count[b >> bits][b & (bins - 1)] = 0;
-        __syncthreads();
-        constexpr int ROUNDS = kEmbSortTile / kEmbThreads;
-        unsigned key[ROUNDS], slot[ROUNDS], rank[ROUNDS];
+    unsigned key[ROUNDS], slot[ROUNDS], rank[ROUNDS];
+    auto load = [&](long tile) {
 #pragma unroll
         for (int r = 0; r < ROUNDS; ++r) {
             const long i = tile + wave * (kEmbSortTile / WAVES) + r * 64 + lane;
@@ -297,42 +291,93 @@ avion_embedding_place_kernel(const T* __restrict__ tokens, const unsigned* __res
                 slot[r] = FIRST ? (unsigned)i : slots[i];
             }
         }
+    };
+    load(from);
+    // a digit's first place: all slots with a smaller digit, then this digit's slots of the workgroups before.  The workgroups'
+    // counts are read by GROUPS groups of threads, a digit a thread.
+    {
+        const int b = tid % BINS, group = tid / BINS, share = (nsort + GROUPS - 1) / GROUPS;
+        const int g_from = group * share, g_to = min(g_from + share, nsort);
+        unsigned t = 0, a = 0;
+#pragma unroll 1
+        for (int g0 = g_from; g0 < g_to; g0 += FLY) {
+            unsigned c[FLY];
+#pragma unroll
+            for (int g = 0; g < FLY; ++g) c[g] = hist[min(g0 + g, nsort - 1) * BINS + b];
+#pragma unroll
+            for (int g = 0; g < FLY; ++g) {
+                t += g0 + g < g_to ? c[g] : 0u;
+                a += g0 + g < min(g_to, (int)blockIdx.x) ? c[g] : 0u;
+            }
+        }
+        total[group][b] = t;
+        ahead[group][b] = a;
+    }
+    __syncthreads();
+    unsigned mine = 0, before = 0;
+    if (tid < BINS)
+#pragma unroll
+        for (int g = 0; g < GROUPS; ++g) {
+            mine += total[g][tid];
+            before += ahead[g][tid];
+        }
+    unsigned upto = mine;  // sum over the threads of this wavefront up to this one
+#pragma unroll
+    for (int off = 1; off < 64; off <<= 1) {
+        const unsigned o = __shfl_up(upto, off, 64);
+        if (lane >= off) upto += o;
+    }
+    if (lane == 63) part[wave] = upto;
+    __syncthreads();
+    if (tid < BINS) {
+        unsigned start = upto - mine;
+#pragma unroll
+        for (int w = 0; w < BINS / 64; ++w) start += w < wave ? part[w] : 0u;
+        base[tid] = start + before;
+    }
+    for (long tile = from; tile < to; tile += kEmbSortTile) {
+        if (tile > from) load(tile);
+        for (int b = tid; b < WAVES * BINS / 2; b += kEmbSortThreads) reinterpret_cast<unsigned*>(count)[b] = 0;
+        __syncthreads();
         // a slot's rank among its wavefront's with the same digit: the lanes below that vote alike, and the rounds before
+        unsigned long same[ROUNDS];
 #pragma unroll
         for (int r = 0; r < ROUNDS; ++r) {
-            const bool in = tile + wave * (kEmbSortTile / WAVES) + r * 64 + lane < to;
-            const unsigned digit = (key[r] >> shift) & (bins - 1);
-            unsigned long same = __ballot(in);
-            for (int b = 0; b < bits; ++b) {
+            const unsigned digit = (key[r] >> shift) & (BINS - 1);
+            same[r] = __ballot(tile + wave * (kEmbSortTile / WAVES) + r * 64 + lane < to);
+#pragma unroll
+            for (int b = 0; b < BITS; ++b) {
                 const unsigned long vote = __ballot((digit >> b) & 1);
-                same &= (digit >> b) & 1 ? vote : ~vote;
+                same[r] &= (digit >> b) & 1 ? vote : ~vote;
             }
-            const unsigned below = __popcll(same & ((1ul << lane) - 1));
+        }
+#pragma unroll
+        for (int r = 0; r < ROUNDS; ++r) {
+            const unsigned below = __popcll(same[r] & ((1ul << lane) - 1));
             rank[r] = 0;
-            if (in) {
-                volatile unsigned* c = &count[wave][digit];
+            if (tile + wave * (kEmbSortTile / WAVES) + r * 64 + lane < to) {
+                volatile unsigned short* c = &count[wave][(key[r] >> shift) & (BINS - 1)];
                 rank[r] = *c + below;
-                if (below == 0) *c = rank[r] + __popcll(same);
+                if (below == 0) *c = (unsigned short)(rank[r] + __popcll(same[r]));
             }
             __builtin_amdgcn_wave_barrier();
         }
         __syncthreads();
-        for (int b = tid; b < bins; b += kEmbThreads) {
-            unsigned at = base[b];
+        unsigned here = 0;
+        if (tid < BINS) {
 #pragma unroll
             for (int w = 0; w < WAVES; ++w) {
-                const unsigned c = count[w][b];
-                count[w][b] = at;
-                at += c;
+                const unsigned c = count[w][tid];
+                count[w][tid] = (unsigned short)here;
+                here += c;
             }
-            base[b] = at;
         }
         __syncthreads();
 #pragma unroll
         for (int r = 0; r < ROUNDS; ++r) {
             const long i = tile + wave * (kEmbSortTile / WAVES) + r * 64 + lane;
             if (i < to) {
-                const unsigned p = count[wave][(key[r] >> shift) & (bins - 1)] + rank[r];
+                const unsigned d = (key[r] >> shift) & (BINS - 1), p = base[d] + count[wave][d] + rank[r];
                 if (p < n) {  // always, unless the tokens change between the launches
                     keys_out[p] = key[r];
                     slots_out[p] = slot[r];
@@ -340,85 +385,79 @@ avion_embedding_place_kernel(const T* __restrict__ tokens, const unsigned* __res
             }
         }
         __syncthreads();
+        if (tid < BINS) base[tid] += here;
     }
 }
 
 // ------------------------------------------------------------------------------------- the sums
-// Sums of kEmbChunk sorted slots in 512 columns.  heads[chunk][D]: the sum of a token that began in a chunk before, tails: of
+// Sums of kEmbSumWaves * PER sorted slots (a chunk) in 512 columns.  heads[chunk][D]: the sum of a token that began in a chunk before, tails: of
 // one that begins here and goes on in the next.
-template <typename E, typename TE>
-__global__ void __launch_bounds__(kEmbThreads)
+template <int PER, typename E, typename TE>
+__global__ void __launch_bounds__(kEmbSumWaves * 64)
 avion_embedding_sum_kernel(const unsigned* __restrict__ keys, const unsigned* __restrict__ slots, const raw16* __restrict__ dy,
                            void* __restrict__ dtable, float* __restrict__ heads, float* __restrict__ tails, long n, int V, int D,
                            float scale)
 {
-    constexpr int WAVES = kEmbThreads / 64, PER = kEmbChunk / WAVES, FLY = 8;
+    constexpr int WAVES = kEmbSumWaves, FLY = PER < 16 ? PER : 16;
     __shared__ float sh_head[WAVES][kEmbCols], sh_tail[WAVES][kEmbCols];
     __shared__ unsigned sh_key[WAVES];  // of the tail
     __shared__ int sh_what[WAVES];      // 1: has a head, 2: the head ends here, 4: has a tail
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
-    const int col = blockIdx.y * kEmbCols + lane * 8;
+    const int col = blockIdx.y * kEmbCols + lane * 8, read_col = col < D ? col : 0;
     const bool in = col < D;
-    const long first = (long)blockIdx.x * kEmbChunk + wave * PER;
+    const long first = ((long)blockIdx.x * WAVES + wave) * PER;
     const int count = first >= n ? 0 : n - first < PER ? (int)(n - first) : PER;
     const unsigned none = (unsigned)V;
-    // lane l: key and slot of sorted place first + l (l < count), lane 63: the key before, lane 62: the key after
+    // lane l: key and slot of sorted place first + l, lane `count`: the key behind, lane 63: the key before.  (A key is at most
+    // V and a slot below n, unless the tokens change between the launches.)
     unsigned key = none, slot = 0;
-    if (lane < count) {
-        key = min(keys[first + lane], none);
-        slot = min(slots[first + lane], (unsigned)(n - 1));  // (both hold, unless the tokens change between the launches)
-    } else if (lane == 63 && first > 0 && first <= n) {
-        key = keys[first - 1];
-    } else if (lane == 62 && first + count < n) {
-        key = keys[first + count];
+    const long place = lane == 63 ? first - 1 : first + lane;
+    if (place >= 0 && place < n && (lane <= count || lane == 63)) {
+        key = min(keys[place], none);
+        slot = min(slots[place], (unsigned)(n - 1));
     }
-    const unsigned key_before = __builtin_amdgcn_readlane(key, 63), key_after = __builtin_amdgcn_readlane(key, 62);
-    int what = 0;
+    const unsigned behind = __shfl_down(key, 1, 64);
+    const int valid = __popcll(__ballot(lane < count && key != none));  // the slots without a row are the last ones
+    const int last = valid - 1;
+    // after these places a sum is complete, or passed on
+    const unsigned long cuts = __ballot(lane < valid && (lane == last || behind != key));
+    const bool head = valid > 0 && __builtin_amdgcn_readlane(key, 63) == __builtin_amdgcn_readfirstlane(key);
+    const bool on = valid > 0 && __builtin_amdgcn_readlane(behind, last < 0 ? 0 : last) == __builtin_amdgcn_readlane(key, last < 0 ? 0 : last);
+    const int head_cut = head ? __builtin_ctzl(cuts | 1ul << 63) : -1;   // the sum that began before ends or is passed on here
+    const int tail_cut = on && head_cut != last ? last : -1;             // the sum that begins here and goes on
+    if (lane == 0) {
+        sh_what[wave] = (head ? 1 : 0) | (head && !(on && head_cut == last) ? 2 : 0) | (tail_cut >= 0 ? 4 : 0);
+        if (tail_cut >= 0) sh_key[wave] = __builtin_amdgcn_readlane(key, last);
+    }
     float acc[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-    const unsigned key0 = __builtin_amdgcn_readfirstlane(key);
-    bool head = count > 0 && first > 0 && key0 == key_before && key0 != none;
-    if (head) what = 1;
-    for (int i0 = 0; i0 < count; i0 += FLY) {
+    // (a loop: unrolled, the cuts' code is so long that small launches wait for instructions)
+#pragma unroll 1
+    for (int i0 = 0; i0 < valid; i0 += FLY) {
         u32x4 raw[FLY];
 #pragma unroll
-        for (int k = 0; k < FLY; ++k) {
-            const int i = i0 + k;
-            const unsigned ki = __builtin_amdgcn_readlane(key, i < PER ? i : 0), si = __builtin_amdgcn_readlane(slot, i < PER ? i : 0);
-            raw[k] = u32x4{0u, 0u, 0u, 0u};
-            if (i < count && ki != none && in) raw[k] = *reinterpret_cast<const u32x4*>(dy + (long)si * D + col);
+        for (int k = 0; k < FLY; ++k) {  // (places behind the last valid one: any row, their sum goes nowhere)
+            const raw16* row = dy + (long)__builtin_amdgcn_readlane(slot, i0 + k) * D;
+            raw[k] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(row + read_col));
         }
+        const unsigned here = (unsigned)(cuts >> i0);
 #pragma unroll
         for (int k = 0; k < FLY; ++k) {
-            const int i = i0 + k;
-            if (i >= count) break;
-            const unsigned ki = __builtin_amdgcn_readlane(key, i);
-            if (ki == none) break;  // the slots without a row are the last ones
 #pragma unroll
             for (int e = 0; e < 8; ++e) acc[e] += E::widen(as_frag8(raw[k]), e);
-            const bool last = i == count - 1;
-            const unsigned next = last ? key_after : __builtin_amdgcn_readlane(key, i < PER - 1 ? i + 1 : 0);
-            if (next == ki && !last) continue;
-            if (next == ki && head) {             // one token, from before this wavefront's slots to behind them
-                store8(&sh_head[wave][lane * 8], acc);
-            } else if (next == ki) {              // begins here, goes on behind
-                store8(&sh_tail[wave][lane * 8], acc);
-                what |= 4;
-                if (lane == 0) sh_key[wave] = ki;
-            } else if (head) {                    // began before, ends here
-                store8(&sh_head[wave][lane * 8], acc);
-                what |= 2;
-                head = false;
-            } else if (in) {
-                float o[8];
+            if (here >> k & 1) {
+                if (i0 + k == head_cut || i0 + k == tail_cut) {
+                    store8(i0 + k == head_cut ? &sh_head[wave][lane * 8] : &sh_tail[wave][lane * 8], acc);
+                } else if (in) {
+                    float o[8];
 #pragma unroll
-                for (int e = 0; e < 8; ++e) o[e] = acc[e] * scale;
-                emb_store8<TE>(dtable, (long)ki * D + col, o);
+                    for (int e = 0; e < 8; ++e) o[e] = acc[e] * scale;
+                    emb_store8<TE>(dtable, (long)__builtin_amdgcn_readlane(key, i0 + k) * D + col, o);
+                }
+#pragma unroll
+                for (int e = 0; e < 8; ++e) acc[e] = 0.f;
             }
-#pragma unroll
-            for (int e = 0; e < 8; ++e) acc[e] = 0.f;
         }
     }
-    if (lane == 0) sh_what[wave] = what;
     __syncthreads();
     // the parts that meet at the wavefronts' borders, in order
     if (wave != 0 || !in) return;
@@ -456,25 +495,25 @@ avion_embedding_sum_kernel(const unsigned* __restrict__ keys, const unsigned* __
 }
 
 // The tokens that span chunks: the workgroup of the chunk where one begins adds its tail and the heads behind it, in a fixed
-// order: 64 groups of threads each take every 64th, 64 columns a workgroup.
-constexpr int kEmbJoinGroups = 64, kEmbJoinCols = 64;
+// order: 16 groups of threads each take every 16th, 64 columns a workgroup.
+constexpr int kEmbJoinGroups = 16, kEmbJoinCols = 64;
 template <typename TE>
 __global__ void __launch_bounds__(kEmbJoinGroups * kEmbJoinCols / 4)
 avion_embedding_join_kernel(const unsigned* __restrict__ keys, const float* __restrict__ heads, const float* __restrict__ tails,
-                            void* __restrict__ dtable, long n, int V, int D, float scale, long nchunks)
+                            void* __restrict__ dtable, long n, int V, int D, float scale, long nchunks, int chunk)
 {
-    constexpr int LANES = kEmbJoinCols / 4, THREADS = kEmbJoinGroups * LANES, FLY = 4;
+    constexpr int LANES = kEmbJoinCols / 4, THREADS = kEmbJoinGroups * LANES, FLY = 16;
     __shared__ f32x4 sh[kEmbJoinGroups][LANES];
-    const long c = blockIdx.x, end = (c + 1) * kEmbChunk;
+    const long c = blockIdx.x, end = (c + 1) * chunk;
     if (end >= n) return;
     const unsigned key = keys[end - 1];
     if (key >= (unsigned)V || keys[end] != key) return;
-    if (c > 0 && keys[c * kEmbChunk - 1] == key) return;  // began before this chunk
+    if (c > 0 && keys[c * chunk - 1] == key) return;  // began before this chunk
     // the chunks whose first slot has this token follow this one without a gap
     long behind = 0;
     for (long from = c + 1; from < nchunks; from += THREADS) {
         const long q = from + threadIdx.x;
-        const int hits = __syncthreads_count(q < nchunks && keys[q * kEmbChunk] == key);
+        const int hits = __syncthreads_count(q < nchunks && keys[q * chunk] == key);
         behind += hits;
         if (hits < THREADS) break;
     }

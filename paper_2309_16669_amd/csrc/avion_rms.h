@@ -18,7 +18,7 @@
 #include "avion_ln.h"
 
 constexpr int kRmsWaves = 4;            // wavefronts of a workgroup (as many as a row's, where a row has more)
-constexpr int kRmsMaxGrid = 1024;       // workgroups of a launch; also the number of partial sums of the gains' gradient
+constexpr int kRmsMaxGrid = 2048;       // workgroups of a launch; also the number of partial sums of the gains' gradient
 constexpr int kRmsMaxD = 16384;         // 8 wavefronts x 4 chunks x 64 lanes x 8
 constexpr float kF8Max = 448.0f;        // largest finite e4m3 value
 constexpr float kF8Least = 1.2621774483536189e-29f;  // 2^-96: a row's largest magnitude counts as at least this

@@ -128,7 +128,7 @@ int embedding_by_type(unsigned flags, F f)
 }
 // How the gradient of n slots is cut: digits of the sort, its workgroups, chunks of the sums, and where all of it lies.
 struct EmbeddingPlan {
-    int passes, bits, nsort;
+    int passes, bits, nsort, chunk;
     long long per, nchunks;
     size_t keys[2], slots[2], hist, stamp, heads, tails, bytes;
     EmbeddingPlan(long long n, long long V, int D)
@@ -140,12 +140,13 @@ struct EmbeddingPlan {
         int need = 0;  // keys 0 .. V
         while ((V >> need) != 0) ++need;
         passes = (need + 9) / 10;
-        bits = (need + passes - 1) / passes;
+        bits = need <= 8 * passes ? 8 : 10;
         // whole tiles a workgroup, at most kEmbSortGrid workgroups
         const long long tiles = (n + kEmbSortTile - 1) / kEmbSortTile;
         per = (tiles + kEmbSortGrid - 1) / kEmbSortGrid * kEmbSortTile;
         nsort = (int)((n + per - 1) / per);
-        nchunks = (n + kEmbChunk - 1) / kEmbChunk;
+        chunk = kEmbSumWaves * (n < kEmbSumEnough ? kEmbSumFew : kEmbSumMost);
+        nchunks = (n + chunk - 1) / chunk;
         size_t at = 0;
         auto take = [&](size_t b) {
             const size_t here = at;
@@ -369,40 +370,43 @@ int avion_embedding_bwd(const void* tokens, const void* dy, void* dtable, long l
         unsigned *hist = reinterpret_cast<unsigned*>(ws + p.hist), *stamp = reinterpret_cast<unsigned*>(ws + p.stamp);
         float *heads = reinterpret_cast<float*>(ws + p.heads), *tails = reinterpret_cast<float*>(ws + p.tails);
         const int rows = clear_rows(V, D, element, 1 << 28);
+        auto sort = [&](auto first, auto width, int pass) {
+            constexpr bool FIRST = decltype(first)::value;
+            constexpr int BITS = decltype(width)::value;
+            const int to = pass % 2, from = 1 - to, shift = pass * BITS;
+            const dim3 threads(kEmbSortThreads);
+            begin_launch();
+            hipLaunchKernelGGL((avion_embedding_hist_kernel<T, FIRST, BITS>), dim3(p.nsort), threads, 0, st, t, keys[from], stamp, hist,
+                               (long)n, (int)V, (long)p.per, shift);
+            const int rh = end_launch("launch avion_embedding_hist_kernel");
+            if (rh != AVION_OK) return rh;
+            // each placing launch clears its share of the table
+            const long clear_from = (long)(V * pass / p.passes), clear_to = (long)(V * (pass + 1) / p.passes);
+            const unsigned clearing = (unsigned)((clear_to - clear_from + rows - 1) / rows);
+            begin_launch();
+            hipLaunchKernelGGL((avion_embedding_place_kernel<T, FIRST, BITS, TE>), dim3(p.nsort + clearing), threads, 0, st, t, keys[from],
+                               slots[from], hist, stamp, keys[to], slots[to], dtable, (long)n, (int)V, D, (long)p.per, p.nsort, shift, rows,
+                               clear_from, clear_to);
+            return end_launch("launch avion_embedding_place_kernel");
+        };
         for (int pass = 0; pass < p.passes; ++pass) {
-            const int to = pass % 2, from = 1 - to, shift = pass * p.bits, bins = 1 << p.bits;
-            const unsigned clearing = pass == 0 ? (unsigned)((V + rows - 1) / rows) : 0u;
-            begin_launch();
-            if (pass == 0)
-                hipLaunchKernelGGL((avion_embedding_hist_kernel<T, true>), dim3(p.nsort), block, 0, st, t, keys[from], stamp, hist, (long)n,
-                                   (int)V, (long)p.per, shift, bins);
-            else
-                hipLaunchKernelGGL((avion_embedding_hist_kernel<T, false>), dim3(p.nsort), block, 0, st, t, keys[from], stamp, hist, (long)n,
-                                   (int)V, (long)p.per, shift, bins);
-            int rk = end_launch("launch avion_embedding_hist_kernel");
-            if (rk != AVION_OK) return rk;
-            begin_launch();
-            if (pass == 0)
-                hipLaunchKernelGGL((avion_embedding_place_kernel<T, true, TE>), dim3(p.nsort + clearing), block, 0, st, t, keys[from],
-                                   slots[from], hist, stamp, keys[to], slots[to], dtable, (long)n, (int)V, D, (long)p.per, p.nsort,
-                                   shift, p.bits, rows);
-            else
-                hipLaunchKernelGGL((avion_embedding_place_kernel<T, false, TE>), dim3(p.nsort), block, 0, st, t, keys[from], slots[from],
-                                   hist, stamp, keys[to], slots[to], dtable, (long)n, (int)V, D, (long)p.per, p.nsort, shift, p.bits,
-                                   rows);
-            rk = end_launch("launch avion_embedding_place_kernel");
+            const int rk = pass == 0 ? (p.bits == 8 ? sort(std::true_type{}, Int<8>{}, 0) : sort(std::true_type{}, Int<10>{}, 0))
+                                     : (p.bits == 8 ? sort(std::false_type{}, Int<8>{}, pass) : sort(std::false_type{}, Int<10>{}, pass));
             if (rk != AVION_OK) return rk;
         }
         const int last = (p.passes - 1) % 2;
-        begin_launch();
-        hipLaunchKernelGGL((avion_embedding_sum_kernel<E, TE>), dim3((unsigned)p.nchunks, ncol), block, 0, st, keys[last], slots[last], g,
-                           dtable, heads, tails, (long)n, (int)V, D, scale);
-        const int rs = end_launch("launch avion_embedding_sum_kernel");
+        auto sums = [&](auto per) {
+            begin_launch();
+            hipLaunchKernelGGL((avion_embedding_sum_kernel<decltype(per)::value, E, TE>), dim3((unsigned)p.nchunks, ncol),
+                               dim3(kEmbSumWaves * 64), 0, st, keys[last], slots[last], g, dtable, heads, tails, (long)n, (int)V, D, scale);
+            return end_launch("launch avion_embedding_sum_kernel");
+        };
+        const int rs = n < kEmbSumEnough ? sums(Int<kEmbSumFew>{}) : sums(Int<kEmbSumMost>{});
         if (rs != AVION_OK) return rs;
         begin_launch();
         hipLaunchKernelGGL((avion_embedding_join_kernel<TE>), dim3((unsigned)p.nchunks, (D + kEmbJoinCols - 1) / kEmbJoinCols),
                            dim3(kEmbJoinGroups * kEmbJoinCols / 4), 0, st, keys[last], heads, tails, dtable, (long)n, (int)V, D, scale,
-                           (long)p.nchunks);
+                           (long)p.nchunks, p.chunk);
         return end_launch("launch avion_embedding_join_kernel");
     });
 }
