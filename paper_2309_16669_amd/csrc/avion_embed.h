@@ -9,8 +9,8 @@
 //   up to kEmbSmallTokens tokens: one launch.  A workgroup per (slot, 512 columns) ends at once unless its slot is the first
 //   with its token; else it collects the slots with that token, in order, and sums their rows.  Further workgroups clear the
 //   rows that no token names.
-//   beyond: the slots are sorted by token (stable radix sort, digits of up to 10 bits; per digit one launch that counts and one
-//   that places: each of at most 256 workgroups adds up the counts of the ones before it itself, so nothing waits for another
+//   beyond: the slots are sorted by token (few: by counting, in one launch; else a stable radix sort, digits of 8 or 10 bits; per
+//   digit one launch that counts and one that places: each of at most 96 workgroups adds up the counts of the ones before it itself, so nothing waits for another
 //   workgroup), then a workgroup sums the rows of a chunk of sorted slots, writes the sums of the tokens that begin and end
 //   among them, and leaves what spans a border to a last launch, as fp32 sums: a token that fills most slots (padding) is
 //   spread over the chip like any others.  The unnamed rows are cleared by spare workgroups of the first placing launch, whose
@@ -23,7 +23,7 @@
 
 constexpr int kEmbThreads = 256;
 constexpr int kEmbFly = 4;                // pieces in flight per thread in the lookup
-constexpr int kEmbSmallTokens = 1024;     // at most this many: gradient in one launch
+constexpr int kEmbSmallTokens = 512;      // at most this many: gradient in one launch
 constexpr int kEmbCols = 512;             // columns of a workgroup in the sums: 8 per lane
 constexpr int kEmbSumWaves = 8;           // of a workgroup in the sums
 constexpr int kEmbSumMost = 32;           // sorted slots of a wavefront there: this many, or
@@ -60,18 +60,6 @@ struct EmbPiece<float> {
     DEVINL float get(int e) const { return c[e / 4][e % 4]; }
 };
 
-// 8 values of a row of the table or of dy
-template <typename E>
-DEVINL void emb_load8(const void* base, long at, float (&v)[8])
-{
-    if constexpr (std::is_same_v<E, float>) {
-        load8(static_cast<const float*>(base) + at, v);
-    } else {
-        const u32x4 c = *reinterpret_cast<const u32x4*>(static_cast<const raw16*>(base) + at);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = E::widen(as_frag8(c), e);
-    }
-}
 template <typename E>
 DEVINL void emb_store8(void* base, long at, const float (&v)[8])
 {
@@ -139,9 +127,9 @@ DEVINL void emb_clear(void* dtable, long first, long rows, int D, F named)
 
 // ------------------------------------------------------------------------- gradient, few tokens
 // grid: (ncol * n) workgroups of slots, then clearing ones of `rows` table rows each (rows <= kEmbSmallRows)
-constexpr int kEmbSmallRows = 1024;
+constexpr int kEmbSmallRows = 1024, kEmbSmallThreads = 512;
 template <typename T, typename E, typename TE>
-__global__ void __launch_bounds__(kEmbThreads)
+__global__ void __launch_bounds__(kEmbSmallThreads)
 avion_embedding_bwd_small_kernel(const T* __restrict__ tokens, const raw16* __restrict__ dy, void* __restrict__ dtable, int n,
                                  int V, int D, float scale, int ncol, int rows)
 {
@@ -149,33 +137,34 @@ avion_embedding_bwd_small_kernel(const T* __restrict__ tokens, const raw16* __re
     __shared__ unsigned short slots[kEmbSmallTokens];
     __shared__ unsigned char flags[kEmbSmallRows];
     __shared__ int counts[kEmbSmallTokens / 64];
-    __shared__ float sums[3][kEmbCols];
+    constexpr int WAVES = kEmbSmallThreads / 64, FLY = 8;
+    __shared__ float sums[WAVES - 1][kEmbCols];
     const int tid = threadIdx.x, lane = tid % 64, wave = tid / 64;
     if ((int)blockIdx.x >= ncol * n) {
         const long first = (long)((int)blockIdx.x - ncol * n) * rows;
         const long here = V - first < rows ? V - first : rows;
-        for (int i = tid; i < rows; i += kEmbThreads) flags[i] = 0;
+        for (int i = tid; i < rows; i += kEmbSmallThreads) flags[i] = 0;
         __syncthreads();
-        for (int i = tid; i < n; i += kEmbThreads) {
+        for (int i = tid; i < n; i += kEmbSmallThreads) {
             const long at = (long)token_key(tokens, i, V) - first;
             if (at >= 0 && at < here) flags[at] = 1;
         }
         __syncthreads();
-        emb_clear<TE, kEmbThreads / 64>(dtable, first, here, D, [&](long r) { return flags[r - first] != 0; });
+        emb_clear<TE, WAVES>(dtable, first, here, D, [&](long r) { return flags[r - first] != 0; });
         return;
     }
     const int slot = blockIdx.x / ncol, col = (blockIdx.x % ncol) * kEmbCols + lane * 8;
     const unsigned key = token_key(tokens, slot, V);
     if (key == (unsigned)V) return;
     bool before = false;
-    for (int i = tid; i < n; i += kEmbThreads) {
+    for (int i = tid; i < n; i += kEmbSmallThreads) {
         keys[i] = token_key(tokens, i, V);
         before |= i < slot && keys[i] == key;
     }
     if (__syncthreads_or(before)) return;
     // the slots with this token, in order: 64 at a time by vote, places by the votes before
     const int groups = (n + 63) / 64;
-    for (int g = wave; g < groups; g += kEmbThreads / 64) {
+    for (int g = wave; g < groups; g += WAVES) {
         const int i = g * 64 + lane;
         const unsigned long hit = __ballot(i < n && keys[i] == key);
         if (lane == 0) counts[g] = __popcll(hit);
@@ -183,7 +172,7 @@ avion_embedding_bwd_small_kernel(const T* __restrict__ tokens, const raw16* __re
     __syncthreads();
     int total = 0;
     for (int g = 0; g < groups; ++g) {
-        if (g % (kEmbThreads / 64) == wave) {
+        if (g % (WAVES) == wave) {
             const int i = g * 64 + lane;
             const bool mine = i < n && keys[i] == key;
             const unsigned long hit = __ballot(mine);
@@ -195,28 +184,27 @@ avion_embedding_bwd_small_kernel(const T* __restrict__ tokens, const raw16* __re
     float acc[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
     if (col < D) {
         int i = wave;
-        for (; i + 12 < total; i += 16) {
-            float v[4][8];
+        for (; i + (FLY - 1) * WAVES < total; i += FLY * WAVES) {
+            EmbPiece<E> v[FLY];
 #pragma unroll
-            for (int k = 0; k < 4; ++k) emb_load8<E>(dy, (long)slots[i + 4 * k] * D + col, v[k]);
+            for (int k = 0; k < FLY; ++k) v[k].load(dy, (long)slots[i + WAVES * k] * D + col);
 #pragma unroll
-            for (int k = 0; k < 4; ++k)
+            for (int k = 0; k < FLY; ++k)
 #pragma unroll
-                for (int e = 0; e < 8; ++e) acc[e] += v[k][e];
+                for (int e = 0; e < 8; ++e) acc[e] += v[k].get(e);
         }
-        for (; i < total; i += 4) {
-            float v[8];
-            emb_load8<E>(dy, (long)slots[i] * D + col, v);
+        for (; i < total; i += WAVES) {
+            EmbPiece<E> v;
+            v.load(dy, (long)slots[i] * D + col);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) acc[e] += v[e];
+            for (int e = 0; e < 8; ++e) acc[e] += v.get(e);
         }
     }
     if (total > 1) {
         if (wave > 0) store8(&sums[wave - 1][lane * 8], acc);
         __syncthreads();
         if (wave == 0)
-#pragma unroll
-            for (int w = 0; w < 3; ++w)
+            for (int w = 0; w < min(WAVES, total) - 1; ++w)
 #pragma unroll
                 for (int e = 0; e < 8; ++e) acc[e] += sums[w][lane * 8 + e];
     }
@@ -389,6 +377,50 @@ avion_embedding_place_kernel(const T* __restrict__ tokens, const unsigned* __res
     }
 }
 
+// Up to kEmbRankSlots slots: a slot's sorted place is the number of slots before it, counted: those with a smaller token, and
+// those with the same one and a smaller number.  A workgroup places 64 slots; its 16 wavefronts each compare them with a share
+// of the keys.  stamp[token]: the place of one of its slots.
+constexpr int kEmbRankSlots = 8192;
+template <typename T>
+__global__ void __launch_bounds__(kEmbSortThreads)
+avion_embedding_rank_kernel(const T* __restrict__ tokens, unsigned* __restrict__ keys_out, unsigned* __restrict__ slots_out,
+                            unsigned* __restrict__ stamp, int n, int V)
+{
+    constexpr int WAVES = kEmbSortThreads / 64;
+    __shared__ u32x4 keys4[kEmbRankSlots / 4];
+    __shared__ unsigned part[WAVES][64];
+    unsigned* keys = reinterpret_cast<unsigned*>(keys4);
+    const int tid = threadIdx.x, lane = tid % 64, wave = tid / 64, n4 = (n + 3) / 4;
+    for (int i = tid; i < 4 * n4; i += kEmbSortThreads) keys[i] = i < n ? token_key(tokens, i, V) : ~0u;
+    __syncthreads();
+    const int first = blockIdx.x * 64, i = first + lane;
+    const unsigned mine = i < n ? keys[i] : ~0u;
+    unsigned below = 0;
+    // all slots before the workgroup's (equal ones count), its own (equal ones with a smaller number), all behind
+    for (int j = wave; j < first / 4; j += WAVES) {
+        const u32x4 k = keys4[j];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) below += k[e] <= mine ? 1u : 0u;
+    }
+    for (int j = first / 4 + 16 + wave; j < n4; j += WAVES) {
+        const u32x4 k = keys4[j];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) below += k[e] < mine ? 1u : 0u;
+    }
+    for (int j = first + wave; j < min(first + 64, n); j += WAVES) {
+        const unsigned k = keys[j];
+        below += k < mine || (k == mine && j < i) ? 1u : 0u;
+    }
+    part[wave][lane] = below;
+    __syncthreads();
+    if (wave > 0 || i >= n) return;
+#pragma unroll
+    for (int w = 1; w < WAVES; ++w) below += part[w][lane];
+    keys_out[below] = mine;
+    slots_out[below] = (unsigned)i;
+    if (mine != (unsigned)V) stamp[mine] = below;
+}
+
 // ------------------------------------------------------------------------------------- the sums
 // Sums of kEmbSumWaves * PER sorted slots (a chunk) in 512 columns.  heads[chunk][D]: the sum of a token that began in a chunk before, tails: of
 // one that begins here and goes on in the next.
@@ -396,9 +428,18 @@ template <int PER, typename E, typename TE>
 __global__ void __launch_bounds__(kEmbSumWaves * 64)
 avion_embedding_sum_kernel(const unsigned* __restrict__ keys, const unsigned* __restrict__ slots, const raw16* __restrict__ dy,
                            void* __restrict__ dtable, float* __restrict__ heads, float* __restrict__ tails, long n, int V, int D,
-                           float scale)
+                           float scale, int nchunks, const unsigned* __restrict__ stamp, int rows)
 {
     constexpr int WAVES = kEmbSumWaves, FLY = PER < 16 ? PER : 16;
+    if ((int)blockIdx.x >= nchunks) {  // (few slots: the table is cleared here)
+        const long r0 = (long)((int)blockIdx.x - nchunks) * rows;
+        if (blockIdx.y == 0)
+            emb_clear<TE, WAVES>(dtable, r0, V - r0 < rows ? V - r0 : rows, D, [&](long r) {
+                const unsigned s = stamp[r];
+                return s < n && keys[s] == (unsigned)r;
+            });
+        return;
+    }
     __shared__ float sh_head[WAVES][kEmbCols], sh_tail[WAVES][kEmbCols];
     __shared__ unsigned sh_key[WAVES];  // of the tail
     __shared__ int sh_what[WAVES];      // 1: has a head, 2: the head ends here, 4: has a tail
@@ -495,8 +536,8 @@ avion_embedding_sum_kernel(const unsigned* __restrict__ keys, const unsigned* __
 }
 
 // The tokens that span chunks: the workgroup of the chunk where one begins adds its tail and the heads behind it, in a fixed
-// order: 16 groups of threads each take every 16th, 64 columns a workgroup.
-constexpr int kEmbJoinGroups = 16, kEmbJoinCols = 64;
+// order: 16 groups of threads each take every 16th, 128 columns a workgroup.
+constexpr int kEmbJoinGroups = 16, kEmbJoinCols = 128;
 template <typename TE>
 __global__ void __launch_bounds__(kEmbJoinGroups * kEmbJoinCols / 4)
 avion_embedding_join_kernel(const unsigned* __restrict__ keys, const float* __restrict__ heads, const float* __restrict__ tails,

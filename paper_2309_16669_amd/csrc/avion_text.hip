@@ -137,6 +137,7 @@ struct EmbeddingPlan {
             bytes = 256;
             return;
         }
+        const bool radix = n > kEmbRankSlots;
         int need = 0;  // keys 0 .. V
         while ((V >> need) != 0) ++need;
         passes = (need + 9) / 10;
@@ -153,9 +154,14 @@ struct EmbeddingPlan {
             at += round256(b);
             return here;
         };
-        for (int i = 0; i < 2; ++i) keys[i] = take(n * 4);
-        for (int i = 0; i < 2; ++i) slots[i] = take(n * 4);
-        hist = take((size_t)nsort * 4 << bits);
+        for (int i = 0; i < (radix ? 2 : 1); ++i) keys[i] = take(n * 4);
+        for (int i = 0; i < (radix ? 2 : 1); ++i) slots[i] = take(n * 4);
+        if (!radix) {
+            passes = 1;  // the result lies where one pass would leave it
+            keys[1] = keys[0];
+            slots[1] = slots[0];
+        }
+        hist = take(radix ? (size_t)nsort * 4 << bits : 0);
         stamp = take(V * 4);
         heads = take((size_t)nchunks * D * 4);
         tails = take((size_t)nchunks * D * 4);
@@ -352,13 +358,12 @@ int avion_embedding_bwd(const void* tokens, const void* dy, void* dtable, long l
         const T* t = static_cast<const T*>(tokens);
         const raw16* g = static_cast<const raw16*>(dy);
         const size_t element = std::is_same_v<TE, float> ? 4 : 2;
-        const dim3 block(kEmbThreads);
         const int ncol = (D + kEmbCols - 1) / kEmbCols;
         if (n <= kEmbSmallTokens) {
             const int rows = clear_rows(V, D, element, kEmbSmallRows);
             begin_launch();
-            hipLaunchKernelGGL((avion_embedding_bwd_small_kernel<T, E, TE>), dim3((unsigned)(ncol * n + (V + rows - 1) / rows)), block,
-                               0, st, t, g, dtable, (int)n, (int)V, D, scale, ncol, rows);
+            hipLaunchKernelGGL((avion_embedding_bwd_small_kernel<T, E, TE>), dim3((unsigned)(ncol * n + (V + rows - 1) / rows)),
+                               dim3(kEmbSmallThreads), 0, st, t, g, dtable, (int)n, (int)V, D, scale, ncol, rows);
             return end_launch("launch avion_embedding_bwd_small_kernel");
         }
         char* ws = static_cast<char*>(workspace);
@@ -389,16 +394,26 @@ int avion_embedding_bwd(const void* tokens, const void* dy, void* dtable, long l
                                clear_from, clear_to);
             return end_launch("launch avion_embedding_place_kernel");
         };
-        for (int pass = 0; pass < p.passes; ++pass) {
+        const bool ranked = n <= kEmbRankSlots;
+        if (ranked) {
+            begin_launch();
+            hipLaunchKernelGGL((avion_embedding_rank_kernel<T>), dim3((unsigned)((n + 63) / 64)), dim3(kEmbSortThreads), 0, st, t, keys[0],
+                               slots[0], stamp, (int)n, (int)V);
+            const int rr = end_launch("launch avion_embedding_rank_kernel");
+            if (rr != AVION_OK) return rr;
+        }
+        for (int pass = 0; !ranked && pass < p.passes; ++pass) {
             const int rk = pass == 0 ? (p.bits == 8 ? sort(std::true_type{}, Int<8>{}, 0) : sort(std::true_type{}, Int<10>{}, 0))
                                      : (p.bits == 8 ? sort(std::false_type{}, Int<8>{}, pass) : sort(std::false_type{}, Int<10>{}, pass));
             if (rk != AVION_OK) return rk;
         }
         const int last = (p.passes - 1) % 2;
         auto sums = [&](auto per) {
+            const unsigned clearing = ranked ? (unsigned)((V + rows - 1) / rows) : 0u;
             begin_launch();
-            hipLaunchKernelGGL((avion_embedding_sum_kernel<decltype(per)::value, E, TE>), dim3((unsigned)p.nchunks, ncol),
-                               dim3(kEmbSumWaves * 64), 0, st, keys[last], slots[last], g, dtable, heads, tails, (long)n, (int)V, D, scale);
+            hipLaunchKernelGGL((avion_embedding_sum_kernel<decltype(per)::value, E, TE>), dim3((unsigned)p.nchunks + clearing, ncol),
+                               dim3(kEmbSumWaves * 64), 0, st, keys[last], slots[last], g, dtable, heads, tails, (long)n, (int)V, D, scale,
+                               (int)p.nchunks, stamp, rows);
             return end_launch("launch avion_embedding_sum_kernel");
         };
         const int rs = n < kEmbSumEnough ? sums(Int<kEmbSumFew>{}) : sums(Int<kEmbSumMost>{});
