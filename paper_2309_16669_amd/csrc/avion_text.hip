@@ -186,13 +186,13 @@ int launch_few(const char* x8, const float* xs, const char* w8, const float* ws,
     return end_launch("launch avion_linear_fp8_few_kernel");
 }
 long long fp8_tiles(int M, int N, int tm, int tn) { return (long long)((M + tm - 1) / tm) * ((N + tn - 1) / tn); }
-template <int TM, int TN, int WM, int WN, typename E>
+template <int TM, int TN, int WM, int WN, int ST, typename E>
 int launch_fp8(const char* x8, const float* xs, const char* w8, const float* ws, const float* bias, raw16* y, int M, int N, int K,
                hipStream_t st)
 {
-    using Cfg = Fp8Cfg<TM, TN, WM, WN>;
+    using Cfg = Fp8Cfg<TM, TN, WM, WN, ST>;
     static std::atomic<bool> lds_allowed{false};
-    const auto kernel = avion_linear_fp8_kernel<TM, TN, WM, WN, E>;
+    const auto kernel = avion_linear_fp8_kernel<TM, TN, WM, WN, ST, E>;
     const hipError_t attr = allow_lds(kernel, Cfg::LDS_BYTES, lds_allowed);
     if (attr != hipSuccess) return hip_fail(attr, "hipFuncSetAttribute(linear_fp8)");
     const long long tiles = fp8_tiles(M, N, TM, TN);
@@ -201,6 +201,21 @@ int launch_fp8(const char* x8, const float* xs, const char* w8, const float* ws,
     hipLaunchKernelGGL(kernel, dim3(grid), dim3(Cfg::NT), Cfg::LDS_BYTES, st, x8, xs, w8, ws, bias, y, M, N, K, (N + TN - 1) / TN,
                        (int)tiles);
     return end_launch("launch avion_linear_fp8_kernel");
+}
+
+template <typename E>
+int launch_wide(const char* x8, const float* xs, const char* w8, const float* ws, const float* bias, raw16* y, int M, int N, int K,
+                hipStream_t st)
+{
+    static std::atomic<bool> lds_allowed{false};
+    const auto kernel = avion_linear_fp8_wide_kernel<E>;
+    const hipError_t attr = allow_lds(kernel, kWideLds, lds_allowed);
+    if (attr != hipSuccess) return hip_fail(attr, "hipFuncSetAttribute(linear_fp8_wide)");
+    const int ntm = (M + kWideM - 1) / kWideM, ntn = (N + kWideN - 1) / kWideN;
+    const unsigned grid = (unsigned)std::min<long long>(kComputeUnits, ((long long)ntm * ntn + 7) / 8 * 8);
+    begin_launch();
+    hipLaunchKernelGGL(kernel, dim3(grid), dim3(kWideWaves * 64), kWideLds, st, x8, xs, w8, ws, bias, y, M, N, K, ntm, ntn);
+    return end_launch("launch avion_linear_fp8_wide_kernel");
 }
 
 }  // namespace
@@ -302,11 +317,16 @@ int avion_linear_fp8(const void* x8, const float* x_scale, const void* w8, const
         using E = typename decltype(fmt)::type;
         if (m <= 16) return launch_few<1, E>(x, x_scale, w, w_scale, bias, out, m, N, K, st);
         if (m <= 32) return launch_few<2, E>(x, x_scale, w, w_scale, bias, out, m, N, K, st);
+        static const char* v = getenv("FP8V");
+        if (v && v[0] == '4') return launch_wide<E>(x, x_scale, w, w_scale, bias, out, m, N, K, st);
+        if (v && v[0] == '1') return launch_fp8<256, 256, 2, 4, 2, E>(x, x_scale, w, w_scale, bias, out, m, N, K, st);
+        if (v && v[0] == '2') return launch_fp8<128, 128, 2, 2, 2, E>(x, x_scale, w, w_scale, bias, out, m, N, K, st);
+        if (v && v[0] == '3') return launch_fp8<256, 128, 4, 2, 3, E>(x, x_scale, w, w_scale, bias, out, m, N, K, st);
         if (fp8_tiles(m, N, 256, 128) >= 2 * kComputeUnits)
-            return launch_fp8<256, 128, 2, 2, E>(x, x_scale, w, w_scale, bias, out, m, N, K, st);
+            return launch_fp8<256, 128, 2, 2, 3, E>(x, x_scale, w, w_scale, bias, out, m, N, K, st);
         if (fp8_tiles(m, N, 128, 128) >= kComputeUnits)
-            return launch_fp8<128, 128, 2, 2, E>(x, x_scale, w, w_scale, bias, out, m, N, K, st);
-        return launch_fp8<64, 64, 2, 2, E>(x, x_scale, w, w_scale, bias, out, m, N, K, st);
+            return launch_fp8<128, 128, 2, 2, 2, E>(x, x_scale, w, w_scale, bias, out, m, N, K, st);
+        return launch_fp8<64, 64, 2, 2, 3, E>(x, x_scale, w, w_scale, bias, out, m, N, K, st);
     });
 }
 
