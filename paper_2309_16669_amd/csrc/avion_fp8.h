@@ -26,15 +26,16 @@ DEVINL f32x4 mfma8_16(i32x8 a, i32x8 b, f32x4 c) { return __builtin_amdgcn_mfma_
 
 // ------------------------------------------------------------------------------------- few rows
 // Bound by the weights' bytes (one token: N K bytes for 2 N K operations) or by latency.  A workgroup takes 16 rows of w8 and
-// all rows of x8 (MT tiles of 16); its four wavefronts take every fourth 128-byte step of K, four steps in flight, straight
+// all rows of x8 (MT tiles of 16); its four wavefronts take every fourth 128-byte step of K, eight or four steps in flight, straight
 // from memory into the operands, and add their sums through LDS in a fixed order.
-constexpr int kFewWaves = 4, kFewFly = 4;
+constexpr int kFewWaves = 4;
 template <int MT, typename E>
 __global__ void __launch_bounds__(kFewWaves * 64)
 avion_linear_fp8_few_kernel(const char* __restrict__ x8, const float* __restrict__ x_scale, const char* __restrict__ w8,
                             const float* __restrict__ w_scale, const float* __restrict__ bias, raw16* __restrict__ y, int M, int N,
                             int K)
 {
+    constexpr int FLY = MT == 1 ? 8 : 4;
     __shared__ f32x4 sh[kFewWaves - 1][MT][64];
     const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, l16 = lane % 16, G = lane / 16;
     const int n0 = blockIdx.x * 16;
@@ -48,20 +49,20 @@ avion_linear_fp8_few_kernel(const char* __restrict__ x8, const float* __restrict
     for (int t = 0; t < MT; ++t) acc[t] = f32x4{0.f, 0.f, 0.f, 0.f};
     const u32x4 zero = {0u, 0u, 0u, 0u};
     const int steps = (K + 127) / 128;
-    for (int s0 = wave; s0 < steps; s0 += kFewWaves * kFewFly) {
-        i32x8 w[kFewFly], x[kFewFly][MT];
+    for (int s0 = wave; s0 < steps; s0 += kFewWaves * FLY) {
+        i32x8 w[FLY], x[FLY][MT];
 #pragma unroll
-        for (int f = 0; f < kFewFly; ++f) {
-            const int k = (s0 + f * kFewWaves) * 128 + 32 * G;  // K is a multiple of 16
-            const bool a = k < K, b = k + 16 < K;
-            w[f] = join16(a ? *reinterpret_cast<const u32x4*>(wp + k) : zero, b ? *reinterpret_cast<const u32x4*>(wp + k + 16) : zero);
+        for (int f = 0; f < FLY; ++f) {
+            const int k = (s0 + f * kFewWaves) * 128 + 16 * G;  // K is a multiple of 16
+            const bool a = k < K, b = k + 64 < K;
+            w[f] = join16(a ? *reinterpret_cast<const u32x4*>(wp + k) : zero, b ? *reinterpret_cast<const u32x4*>(wp + k + 64) : zero);
 #pragma unroll
             for (int t = 0; t < MT; ++t)
                 x[f][t] = join16(a ? *reinterpret_cast<const u32x4*>(xp[t] + k) : zero,
-                                 b ? *reinterpret_cast<const u32x4*>(xp[t] + k + 16) : zero);
+                                 b ? *reinterpret_cast<const u32x4*>(xp[t] + k + 64) : zero);
         }
 #pragma unroll
-        for (int f = 0; f < kFewFly; ++f)
+        for (int f = 0; f < FLY; ++f)
 #pragma unroll
             for (int t = 0; t < MT; ++t) acc[t] = mfma8_16(w[f], x[f][t], acc[t]);
     }
@@ -366,7 +367,6 @@ avion_linear_fp8_wide_kernel(const char* __restrict__ x8, const float* __restric
                 } else if (q + 1 < total) {
                     if (s == 0 && q > 0) fp8_landed_barrier<kWideStores>();
                     else fp8_landed_barrier<0>();
-                    if (q + 2 < total) fetch();
 #pragma unroll
                     for (int j = 0; j < NI; ++j) a[0][j] = read(a0 + next + j * 32 * kWideK, 0);
                     b_next = read(b0 + next, 0);
@@ -377,6 +377,7 @@ avion_linear_fp8_wide_kernel(const char* __restrict__ x8, const float* __restric
                 __builtin_amdgcn_sched_barrier(0);
                 b = b_next;
             }
+            if (q + 2 < total) fetch();
             buf ^= 1;
         }
 

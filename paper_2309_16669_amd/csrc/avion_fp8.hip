@@ -1,0 +1,105 @@
+// C ABI of the product of rows in 8 bits.  See include/avion_attn.h for its contract.
+#include "avion_attn.h"
+
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+
+#include "avion_fp8.h"
+#include "avion_host.h"
+
+namespace {
+
+constexpr long long kComputeUnits = 256;
+
+// ------------------------------------------------------------------------------- 8-bit product
+template <int MT, typename E>
+int launch_few(const char* x8, const float* xs, const char* w8, const float* ws, const float* bias, raw16* y, int M, int N, int K,
+               hipStream_t st)
+{
+    begin_launch();
+    hipLaunchKernelGGL((avion_linear_fp8_few_kernel<MT, E>), dim3((N + 15) / 16), dim3(kFewWaves * 64), 0, st, x8, xs, w8, ws, bias, y,
+                       M, N, K);
+    return end_launch("launch avion_linear_fp8_few_kernel");
+}
+long long fp8_tiles(int M, int N, int tm, int tn) { return (long long)((M + tm - 1) / tm) * ((N + tn - 1) / tn); }
+template <int TM, int TN, int WM, int WN, int ST, typename E>
+int launch_fp8(const char* x8, const float* xs, const char* w8, const float* ws, const float* bias, raw16* y, int M, int N, int K,
+               hipStream_t st)
+{
+    using Cfg = Fp8Cfg<TM, TN, WM, WN, ST>;
+    static std::atomic<bool> lds_allowed{false};
+    const auto kernel = avion_linear_fp8_kernel<TM, TN, WM, WN, ST, E>;
+    const hipError_t attr = allow_lds(kernel, Cfg::LDS_BYTES, lds_allowed);
+    if (attr != hipSuccess) return hip_fail(attr, "hipFuncSetAttribute(linear_fp8)");
+    const long long tiles = fp8_tiles(M, N, TM, TN);
+    const unsigned grid = (unsigned)((tiles + 7) / 8 * 8);
+    begin_launch();
+    hipLaunchKernelGGL(kernel, dim3(grid), dim3(Cfg::NT), Cfg::LDS_BYTES, st, x8, xs, w8, ws, bias, y, M, N, K, (N + TN - 1) / TN,
+                       (int)tiles);
+    return end_launch("launch avion_linear_fp8_kernel");
+}
+
+// Which kernel (us, kernel alone):
+//   up to 16 rows (32 where K is at most 2048): straight from memory.  16 x 6144 x 4096: 11.2, tiles of 64 x 64 12.9;
+//     32 x 1024 x 1024: 4.1 and 5.3, but 32 x 6144 x 4096: 14.4 and 12.8.
+//   else the smallest tiles that leave no more than one for a compute unit (latency), larger ones beyond (traffic):
+//     64 x 64 and 128 x 64 on 1024 x 1024 x 1024 (256 tiles): 6.0 and 6.9, on 512 x 4096 x 4096 (512): 21.8 and 17.5;
+//     128 x 64 and 128 x 128 on 785 x 2304 x 768 (126 tiles of 128 x 128): 6.8 and 8.7, on 1570 x 3840 x 1280 (390): 19.3 and 16.2
+//   256 x 256: a round of its 256 tiles takes about as long as 820 tiles of 128 x 128 in a long row and less to begin with, so it
+//     needs rounds that are well filled: 12544 x 768 x 768 (147 tiles): 14.8 against 17.4 of 128 x 128, 2048 x 4096 x 4096 (128):
+//     46 against 38, 6272 x 2304 x 768 (225): 16.5 against 20.6, 50176 x 2304 x 768: 109 against 164
+bool fp8_wide(int M, int N)
+{
+    const long long tiles = fp8_tiles(M, N, kWideM, kWideN), rounds = (tiles + kComputeUnits - 1) / kComputeUnits;
+    return 5 * (tiles + 64) >= 4 * kComputeUnits * rounds;
+}
+template <typename E>
+int launch_wide(const char* x8, const float* xs, const char* w8, const float* ws, const float* bias, raw16* y, int M, int N, int K,
+                hipStream_t st)
+{
+    static std::atomic<bool> lds_allowed{false};
+    const auto kernel = avion_linear_fp8_wide_kernel<E>;
+    const hipError_t attr = allow_lds(kernel, kWideLds, lds_allowed);
+    if (attr != hipSuccess) return hip_fail(attr, "hipFuncSetAttribute(linear_fp8_wide)");
+    const int ntm = (M + kWideM - 1) / kWideM, ntn = (N + kWideN - 1) / kWideN;
+    const unsigned grid = (unsigned)std::min<long long>(kComputeUnits, ((long long)ntm * ntn + 7) / 8 * 8);
+    begin_launch();
+    hipLaunchKernelGGL(kernel, dim3(grid), dim3(kWideWaves * 64), kWideLds, st, x8, xs, w8, ws, bias, y, M, N, K, ntm, ntn);
+    return end_launch("launch avion_linear_fp8_wide_kernel");
+}
+
+}  // namespace
+
+extern "C" {
+
+int avion_linear_fp8(const void* x8, const float* x_scale, const void* w8, const float* w_scale, const float* bias, void* y,
+                     long long M, int N, int K, unsigned flags, void* stream)
+{
+    if (M < 0 || N < 1 || K < 1 || (flags & ~AVION_FLAG_F16)) return AVION_EINVAL;
+    if (M >= (1LL << 31) - 256 || N % 8 != 0 || N > (1 << 20) || K % 16 != 0 || K > (1 << 16)) return AVION_EUNSUPPORTED;
+    if (fp8_tiles((int)M, N, 64, 64) > (1LL << 24)) return AVION_EUNSUPPORTED;  // workgroups of a launch
+    if (M == 0) return AVION_OK;
+    if (!x8 || !x_scale || !w8 || !w_scale || !y) return AVION_EINVAL;
+    const void* ptrs[] = {x8, x_scale, w8, w_scale, bias, y};
+    for (const void* p : ptrs)
+        if (!aligned16(p)) return AVION_EUNSUPPORTED;
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    const char *x = static_cast<const char*>(x8), *w = static_cast<const char*>(w8);
+    raw16* out = static_cast<raw16*>(y);
+    const int m = (int)M;
+    return by_element(flags, [&](auto fmt) {
+        using E = typename decltype(fmt)::type;
+        if (m <= 16) return launch_few<1, E>(x, x_scale, w, w_scale, bias, out, m, N, K, st);
+        if (m <= 32 && K <= 2048) return launch_few<2, E>(x, x_scale, w, w_scale, bias, out, m, N, K, st);
+        if (fp8_wide(m, N)) return launch_wide<E>(x, x_scale, w, w_scale, bias, out, m, N, K, st);
+        if (fp8_tiles(m, N, 128, 128) >= kComputeUnits)
+            return launch_fp8<128, 128, 2, 2, 2, E>(x, x_scale, w, w_scale, bias, out, m, N, K, st);
+        if (fp8_tiles(m, N, 64, 64) > kComputeUnits)
+            return launch_fp8<128, 64, 2, 2, 3, E>(x, x_scale, w, w_scale, bias, out, m, N, K, st);
+        return launch_fp8<64, 64, 2, 2, 3, E>(x, x_scale, w, w_scale, bias, out, m, N, K, st);
+    });
+}
+
+}  // extern "C"

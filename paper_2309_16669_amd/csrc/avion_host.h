@@ -7,6 +7,7 @@
 #include <cstdio>
 
 #include "avion_attn.h"
+#include "avion_common.h"
 
 // one text per thread for the whole library (avion_last_hip_error)
 inline thread_local char g_hip_error[256] = "";
@@ -51,5 +52,13 @@ template <typename T>
 struct TypeTag {
     using type = T;
 };
+
+// f(element format) by AVION_FLAG_F16
+template <typename F>
+int by_element(unsigned flags, F f)
+{
+    if (flags & AVION_FLAG_F16) return f(TypeTag<F16>{});
+    return f(TypeTag<Bf16>{});
+}
 
 }  // namespace

@@ -1,5 +1,4 @@
-// C ABI of the text encoder's entry and of the 8-bit path: token table, RMS normalisation with the residual's addition,
-// rows in 8 bits and their product.  See include/avion_attn.h for the contract of every entry point.
+// C ABI of the text encoder's entry: token table, RMS normalisation with the residual's addition, rows in 8 bits.  See include/avion_attn.h for the contract of every entry point.
 #include "avion_attn.h"
 
 #include <hip/hip_runtime.h>
@@ -8,20 +7,11 @@
 #include <cmath>
 
 #include "avion_embed.h"
-#include "avion_fp8.h"
 #include "avion_host.h"
 #include "avion_rms.h"
 
 namespace {
 
-constexpr long long kComputeUnits = 256;
-
-template <typename F>
-int by_element(unsigned flags, F f)
-{
-    if (flags & AVION_FLAG_F16) return f(TypeTag<F16>{});
-    return f(TypeTag<Bf16>{});
-}
 template <int N>
 using Int = std::integral_constant<int, N>;
 
@@ -175,49 +165,6 @@ int clear_rows(long long V, int D, size_t element, int most)
     return (int)std::min<long long>(std::max({fits, 1LL, (V >> 20) + 1}), most);
 }
 
-// ------------------------------------------------------------------------------- 8-bit product
-template <int MT, typename E>
-int launch_few(const char* x8, const float* xs, const char* w8, const float* ws, const float* bias, raw16* y, int M, int N, int K,
-               hipStream_t st)
-{
-    begin_launch();
-    hipLaunchKernelGGL((avion_linear_fp8_few_kernel<MT, E>), dim3((N + 15) / 16), dim3(kFewWaves * 64), 0, st, x8, xs, w8, ws, bias, y,
-                       M, N, K);
-    return end_launch("launch avion_linear_fp8_few_kernel");
-}
-long long fp8_tiles(int M, int N, int tm, int tn) { return (long long)((M + tm - 1) / tm) * ((N + tn - 1) / tn); }
-template <int TM, int TN, int WM, int WN, int ST, typename E>
-int launch_fp8(const char* x8, const float* xs, const char* w8, const float* ws, const float* bias, raw16* y, int M, int N, int K,
-               hipStream_t st)
-{
-    using Cfg = Fp8Cfg<TM, TN, WM, WN, ST>;
-    static std::atomic<bool> lds_allowed{false};
-    const auto kernel = avion_linear_fp8_kernel<TM, TN, WM, WN, ST, E>;
-    const hipError_t attr = allow_lds(kernel, Cfg::LDS_BYTES, lds_allowed);
-    if (attr != hipSuccess) return hip_fail(attr, "hipFuncSetAttribute(linear_fp8)");
-    const long long tiles = fp8_tiles(M, N, TM, TN);
-    const unsigned grid = (unsigned)((tiles + 7) / 8 * 8);
-    begin_launch();
-    hipLaunchKernelGGL(kernel, dim3(grid), dim3(Cfg::NT), Cfg::LDS_BYTES, st, x8, xs, w8, ws, bias, y, M, N, K, (N + TN - 1) / TN,
-                       (int)tiles);
-    return end_launch("launch avion_linear_fp8_kernel");
-}
-
-template <typename E>
-int launch_wide(const char* x8, const float* xs, const char* w8, const float* ws, const float* bias, raw16* y, int M, int N, int K,
-                hipStream_t st)
-{
-    static std::atomic<bool> lds_allowed{false};
-    const auto kernel = avion_linear_fp8_wide_kernel<E>;
-    const hipError_t attr = allow_lds(kernel, kWideLds, lds_allowed);
-    if (attr != hipSuccess) return hip_fail(attr, "hipFuncSetAttribute(linear_fp8_wide)");
-    const int ntm = (M + kWideM - 1) / kWideM, ntn = (N + kWideN - 1) / kWideN;
-    const unsigned grid = (unsigned)std::min<long long>(kComputeUnits, ((long long)ntm * ntn + 7) / 8 * 8);
-    begin_launch();
-    hipLaunchKernelGGL(kernel, dim3(grid), dim3(kWideWaves * 64), kWideLds, st, x8, xs, w8, ws, bias, y, M, N, K, ntm, ntn);
-    return end_launch("launch avion_linear_fp8_wide_kernel");
-}
-
 }  // namespace
 
 extern "C" {
@@ -295,38 +242,6 @@ int avion_quantize_rows(const void* x, void* x8, float* scale, long long M, int 
                                (long)M, D);
             return end_launch("launch avion_quantize_rows_kernel");
         });
-    });
-}
-
-int avion_linear_fp8(const void* x8, const float* x_scale, const void* w8, const float* w_scale, const float* bias, void* y,
-                     long long M, int N, int K, unsigned flags, void* stream)
-{
-    if (M < 0 || N < 1 || K < 1 || (flags & ~AVION_FLAG_F16)) return AVION_EINVAL;
-    if (M >= (1LL << 31) - 256 || N % 8 != 0 || N > (1 << 20) || K % 16 != 0 || K > (1 << 16)) return AVION_EUNSUPPORTED;
-    if (fp8_tiles((int)M, N, 64, 64) > (1LL << 24)) return AVION_EUNSUPPORTED;  // workgroups of a launch
-    if (M == 0) return AVION_OK;
-    if (!x8 || !x_scale || !w8 || !w_scale || !y) return AVION_EINVAL;
-    const void* ptrs[] = {x8, x_scale, w8, w_scale, bias, y};
-    for (const void* p : ptrs)
-        if (!aligned16(p)) return AVION_EUNSUPPORTED;
-    hipStream_t st = static_cast<hipStream_t>(stream);
-    const char *x = static_cast<const char*>(x8), *w = static_cast<const char*>(w8);
-    raw16* out = static_cast<raw16*>(y);
-    const int m = (int)M;
-    return by_element(flags, [&](auto fmt) {
-        using E = typename decltype(fmt)::type;
-        if (m <= 16) return launch_few<1, E>(x, x_scale, w, w_scale, bias, out, m, N, K, st);
-        if (m <= 32) return launch_few<2, E>(x, x_scale, w, w_scale, bias, out, m, N, K, st);
-        static const char* v = getenv("FP8V");
-        if (v && v[0] == '4') return launch_wide<E>(x, x_scale, w, w_scale, bias, out, m, N, K, st);
-        if (v && v[0] == '1') return launch_fp8<256, 256, 2, 4, 2, E>(x, x_scale, w, w_scale, bias, out, m, N, K, st);
-        if (v && v[0] == '2') return launch_fp8<128, 128, 2, 2, 2, E>(x, x_scale, w, w_scale, bias, out, m, N, K, st);
-        if (v && v[0] == '3') return launch_fp8<256, 128, 4, 2, 3, E>(x, x_scale, w, w_scale, bias, out, m, N, K, st);
-        if (fp8_tiles(m, N, 256, 128) >= 2 * kComputeUnits)
-            return launch_fp8<256, 128, 2, 2, 3, E>(x, x_scale, w, w_scale, bias, out, m, N, K, st);
-        if (fp8_tiles(m, N, 128, 128) >= kComputeUnits)
-            return launch_fp8<128, 128, 2, 2, 2, E>(x, x_scale, w, w_scale, bias, out, m, N, K, st);
-        return launch_fp8<64, 64, 2, 2, 3, E>(x, x_scale, w, w_scale, bias, out, m, N, K, st);
     });
 }
 
