@@ -329,7 +329,7 @@ int avion_embedding_bwd(const void *tokens, const void *dy, void *dtable, long l
  *   dx, dresidual    : outputs of the backward, NULL where not wanted.  dresidual (fp32) only with AVION_FLAG_WIDE_F32; without
  *                      it dx is the gradient of both inputs.
  *   M >= 0; D a multiple of 8, at most 16384; eps finite and >= 0
- *   workspace (backward): 256-byte aligned, avion_rmsnorm_bwd_workspace_bytes(M, D) bytes (at most 1024 * D floats)
+ *   workspace (backward): 256-byte aligned, avion_rmsnorm_bwd_workspace_bytes(M, D) bytes (at most 512 * D floats)
  * Statistics and sums in fp32 (the sum of a row's squares has to be finite there), outputs rounded once; no atomics,
  * bit-reproducible.  M = 0 writes zeros to dweight and nothing else.  Pointers 16-byte aligned.
  */

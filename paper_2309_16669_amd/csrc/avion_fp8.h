@@ -28,14 +28,14 @@ DEVINL f32x4 mfma8_16(i32x8 a, i32x8 b, f32x4 c) { return __builtin_amdgcn_mfma_
 // Bound by the weights' bytes (one token: N K bytes for 2 N K operations) or by latency.  A workgroup takes 16 rows of w8 and
 // all rows of x8 (MT tiles of 16); its four wavefronts take every fourth 128-byte step of K, eight or four steps in flight, straight
 // from memory into the operands, and add their sums through LDS in a fixed order.
-constexpr int kFewWaves = 4;
+constexpr int kFewWaves = 8;
 template <int MT, typename E>
 __global__ void __launch_bounds__(kFewWaves * 64)
 avion_linear_fp8_few_kernel(const char* __restrict__ x8, const float* __restrict__ x_scale, const char* __restrict__ w8,
                             const float* __restrict__ w_scale, const float* __restrict__ bias, raw16* __restrict__ y, int M, int N,
                             int K)
 {
-    constexpr int FLY = MT == 1 ? 8 : 4;
+    constexpr int FLY = 4;
     __shared__ f32x4 sh[kFewWaves - 1][MT][64];
     const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, l16 = lane % 16, G = lane / 16;
     const int n0 = blockIdx.x * 16;

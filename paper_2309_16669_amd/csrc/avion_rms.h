@@ -18,16 +18,55 @@
 #include "avion_ln.h"
 
 constexpr int kRmsWaves = 4;            // wavefronts of a workgroup (as many as a row's, where a row has more)
-constexpr int kRmsMaxGrid = 2048;       // workgroups of a launch; also the number of partial sums of the gains' gradient
+constexpr int kRmsMaxGrid = 512;        // workgroups of a launch; also the number of partial sums of the gains' gradient
 constexpr int kRmsMaxD = 16384;         // 8 wavefronts x 4 chunks x 64 lanes x 8
 constexpr float kF8Max = 448.0f;        // largest finite e4m3 value
 constexpr float kF8Least = 1.2621774483536189e-29f;  // 2^-96: a row's largest magnitude counts as at least this
 
-DEVINL float wave_max(float x)
+// Sum and maximum over a wavefront by lane moves of the vector unit alone (a chain of LDS permutes takes about 600 cycles a
+// row): pairs, quads, mirrored eights and sixteens, then the rows of sixteen and the halves exchanged.
+template <int CTRL>
+DEVINL float lane_move(float x)
 {
-#pragma unroll
-    for (int off = 1; off < 32; off <<= 1) x = fmaxf(x, __shfl_xor(x, off, 64));
-    return both_halves_max(x);
+    return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), CTRL, 0xf, 0xf, true));
+}
+DEVINL void sixteens(float x, float& a, float& b)  // as `halves`, for the two rows of sixteen of each half
+{
+    const unsigned u = __builtin_bit_cast(unsigned, x);
+    const auto r = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+    unsigned r0 = r[0], r1 = r[1];
+    asm volatile("" : "+v"(r0), "+v"(r1));
+    a = __builtin_bit_cast(float, r0);
+    b = __builtin_bit_cast(float, r1);
+}
+// of LANES = 16, 32 or 64 neighbours
+template <int LANES>
+DEVINL float lanes_sum(float x)
+{
+    x += lane_move<0xB1>(x);   // lanes 1 0 3 2
+    x += lane_move<0x4E>(x);   // 2 3 0 1
+    x += lane_move<0x141>(x);  // 7 - l of each eight
+    x += lane_move<0x140>(x);  // 15 - l of each sixteen
+    if (LANES > 16) {
+        float a, b;
+        sixteens(x, a, b);
+        x = a + b;
+    }
+    return LANES > 32 ? both_halves_sum(x) : x;
+}
+template <int LANES>
+DEVINL float lanes_max(float x)
+{
+    x = fmaxf(x, lane_move<0xB1>(x));
+    x = fmaxf(x, lane_move<0x4E>(x));
+    x = fmaxf(x, lane_move<0x141>(x));
+    x = fmaxf(x, lane_move<0x140>(x));
+    if (LANES > 16) {
+        float a, b;
+        sixteens(x, a, b);
+        x = fmaxf(a, b);
+    }
+    return LANES > 32 ? both_halves_max(x) : x;
 }
 
 // 8 fp32 -> 8 e4m3 (nearest even).  |v| < 464 or NaN.
@@ -44,17 +83,25 @@ DEVINL u32x2 pack_fp8(const float (&v)[8])
 }
 
 // A lane's share of a row: NCH chunks of 8 elements, 16-bit (E) or fp32
-template <int NCH, int WPR, typename E>
+// LAST: nobody reads it again (all inputs of the backward).  Read past the caches, backward of 157696 x 512 142 -> 112 us; the
+// forward, whose inputs are as dead, takes 101 or 121 then instead of 107, by turns, and reads them as usual.
+template <bool LAST, typename V>
+DEVINL V rms_load(const V* p)
+{
+    return LAST ? __builtin_nontemporal_load(p) : *p;
+}
+template <int NCH, int LANES, typename E>
 struct RmsRow {
     u32x4 c[NCH];
+    template <bool LAST = false>
     DEVINL void load(const void* base, long row, int D, int nchunks, int at)
     {
         const u32x4 zero = {0u, 0u, 0u, 0u};
         const raw16* p = static_cast<const raw16*>(base) + row * D;
 #pragma unroll
         for (int j = 0; j < NCH; ++j) {
-            const int ch = at + 64 * WPR * j;
-            c[j] = ch < nchunks ? *reinterpret_cast<const u32x4*>(p + ch * 8) : zero;
+            const int ch = at + LANES * j;
+            c[j] = ch < nchunks ? rms_load<LAST>(reinterpret_cast<const u32x4*>(p + ch * 8)) : zero;
         }
     }
     DEVINL float get(int j, int e) const { return E::widen(as_frag8(c[j]), e); }
@@ -75,18 +122,19 @@ struct RmsRow {
         for (int e = 0; e < 8; ++e) v[e] = E::widen(as_frag8(w), e);
     }
 };
-template <int NCH, int WPR>
-struct RmsRow<NCH, WPR, float> {
+template <int NCH, int LANES>
+struct RmsRow<NCH, LANES, float> {
     f32x4 c[NCH][2];
+    template <bool LAST = false>
     DEVINL void load(const void* base, long row, int D, int nchunks, int at)
     {
         const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
         const float* p = static_cast<const float*>(base) + row * D;
 #pragma unroll
         for (int j = 0; j < NCH; ++j) {
-            const int ch = at + 64 * WPR * j;
-            c[j][0] = ch < nchunks ? *reinterpret_cast<const f32x4*>(p + ch * 8) : zero;
-            c[j][1] = ch < nchunks ? *reinterpret_cast<const f32x4*>(p + ch * 8 + 4) : zero;
+            const int ch = at + LANES * j;
+            c[j][0] = ch < nchunks ? rms_load<LAST>(reinterpret_cast<const f32x4*>(p + ch * 8)) : zero;
+            c[j][1] = ch < nchunks ? rms_load<LAST>(reinterpret_cast<const f32x4*>(p + ch * 8 + 4)) : zero;
         }
     }
     DEVINL float get(int j, int e) const { return c[j][e / 4][e % 4]; }
@@ -97,14 +145,29 @@ struct RmsRow<NCH, WPR, float> {
     DEVINL static void round(float (&)[8]) {}
 };
 
-// Sum of a (and maximum of b) over the WPR wavefronts of a row.  Through LDS where there is more than one; two places, used
-// in turn by consecutive rows: a wavefront writes the other one only after the barrier that everybody's reads of the one
-// before precede.
-template <int WPR, bool MAX>
-DEVINL void row_reduce(float& a, float& b, float (&sh)[2][WPR][2], int wave, int lane, int& turn)
+// How a row lies over lanes: 16 or 32 neighbours (several rows a wavefront), a wavefront, or 4 or 8 wavefronts of a workgroup.
+template <int LANES>
+struct RmsWork {
+    static constexpr int WPR = LANES / 64 > 1 ? LANES / 64 : 1;              // wavefronts a row
+    static constexpr int SUB = LANES < 64 ? 64 / LANES : 1;                  // rows a wavefront
+    static constexpr int WAVES = WPR > kRmsWaves ? WPR : kRmsWaves;
+    static constexpr int ROWS = LANES <= 64 ? kRmsWaves * SUB : 1;           // rows of a workgroup at a time
+    int lane, wave, at, sub;
+    DEVINL RmsWork() : lane(threadIdx.x % 64), wave(threadIdx.x / 64), at(LANES <= 64 ? lane % LANES : (int)threadIdx.x), sub(LANES < 64 ? lane / LANES : 0) {}
+    // the first of this wavefront's rows (the same in all its lanes); a lane's own is `sub` behind
+    DEVINL long first() const { return (long)blockIdx.x * ROWS + (LANES <= 64 ? wave * SUB : 0); }
+    DEVINL long stride() const { return (long)gridDim.x * ROWS; }
+};
+
+// Sum of a (and maximum of b) over the lanes of a row.  Through LDS where it has more than one wavefront; two places, used in
+// turn by consecutive rows: a wavefront writes the other one only after the barrier that everybody's reads of the one before
+// precede.
+template <int LANES, bool MAX>
+DEVINL void row_reduce(float& a, float& b, float (&sh)[2][RmsWork<LANES>::WPR][2], int wave, int lane, int& turn)
 {
-    a = wave_sum(a);
-    if (MAX) b = wave_max(b);
+    constexpr int WPR = RmsWork<LANES>::WPR, IN = LANES < 64 ? LANES : 64;
+    a = lanes_sum<IN>(a);
+    if (MAX) b = lanes_max<IN>(b);
     if constexpr (WPR > 1) {
         if (lane == 0) {
             sh[turn][wave][0] = a;
@@ -122,47 +185,44 @@ DEVINL void row_reduce(float& a, float& b, float (&sh)[2][WPR][2], int wave, int
     }
 }
 
-// Rows of one workgroup: WPR = 1: one row per wavefront at a time; else one row per workgroup
-template <int WPR>
-struct RmsWork {
-    static constexpr int WAVES = WPR > kRmsWaves ? WPR : kRmsWaves;
-    static constexpr int ROWS = WAVES / WPR;  // rows at a time
-};
-
 // y (E), or y8 and scale with F8; h where there is a residual; rstd where it is asked for
-template <int WPR, int NCH, typename E, typename R, bool F8>
-__global__ void __launch_bounds__(RmsWork<WPR>::WAVES * 64)
+template <int LANES, int NCH, typename E, typename R, bool F8>
+__global__ void __launch_bounds__(RmsWork<LANES>::WAVES * 64)
 avion_rmsnorm_fwd_kernel(const raw16* __restrict__ x, const void* __restrict__ residual, const float* __restrict__ weight,
                          void* __restrict__ y, float* __restrict__ scale, void* __restrict__ h, float* __restrict__ rstd,
                          long M, int D, float eps)
 {
-    using W = RmsWork<WPR>;
-    __shared__ float sh[2][WPR][2];
-    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, at = WPR == 1 ? lane : (int)threadIdx.x;
+    const RmsWork<LANES> rw;
+    __shared__ float sh[2][RmsWork<LANES>::WPR][2];
+    const int lane = rw.lane, wave = rw.wave, at = rw.at;
     const int nchunks = D / 8;
     const float inv_d = 1.0f / (float)D;
-    const long stride = (long)gridDim.x * W::ROWS;
-    long row = (long)blockIdx.x * W::ROWS + (WPR == 1 ? wave : 0);
+    const long stride = rw.stride();
+    long row = rw.first();
     if (row >= M) return;
     float gain[NCH][8];
     int turn = 0;
 
-    RmsRow<NCH, WPR, E> xa, xb;
-    RmsRow<NCH, WPR, R> ra, rb;
-    auto load = [&](RmsRow<NCH, WPR, E>& xr, RmsRow<NCH, WPR, R>& rr, long n) {
-        xr.load(x, n, D, nchunks, at);
-        if (residual) rr.load(residual, n, D, nchunks, at);
+    RmsRow<NCH, LANES, E> xa, xb;
+    RmsRow<NCH, LANES, R> ra, rb;
+    auto load = [&](RmsRow<NCH, LANES, E>& xr, RmsRow<NCH, LANES, R>& rr, long n) {
+        n += rw.sub;
+        const int chunks = n < M ? nchunks : 0;
+        xr.load(x, n, D, chunks, at);
+        if (residual) rr.load(residual, n, D, chunks, at);
     };
     load(xa, ra, row);
 #pragma unroll
     for (int j = 0; j < NCH; ++j) {
-        const int ch = at + 64 * WPR * j;
+        const int ch = at + LANES * j;
 #pragma unroll
         for (int e = 0; e < 8; ++e) gain[j][e] = 0.f;
         if (ch < nchunks) load8(weight + ch * 8, gain[j]);
     }
 
-    auto finish = [&](const RmsRow<NCH, WPR, E>& xr, const RmsRow<NCH, WPR, R>& rr, long n) {
+    auto finish = [&](const RmsRow<NCH, LANES, E>& xr, const RmsRow<NCH, LANES, R>& rr, long n) {
+        n += rw.sub;
+        const int chunks = n < M ? nchunks : 0;
         float v[NCH][8], ss = 0.f, big = 0.f;
 #pragma unroll
         for (int j = 0; j < NCH; ++j) {
@@ -171,7 +231,7 @@ avion_rmsnorm_fwd_kernel(const raw16* __restrict__ x, const void* __restrict__ r
             if (residual) {
 #pragma unroll
                 for (int e = 0; e < 8; ++e) v[j][e] += rr.get(j, e);
-                RmsRow<NCH, WPR, R>::round(v[j]);
+                RmsRow<NCH, LANES, R>::round(v[j]);
             }
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
@@ -179,7 +239,7 @@ avion_rmsnorm_fwd_kernel(const raw16* __restrict__ x, const void* __restrict__ r
                 if (F8) big = fmaxf(big, fabsf(v[j][e] * gain[j][e]));
             }
         }
-        row_reduce<WPR, F8>(ss, big, sh, wave, lane, turn);
+        row_reduce<LANES, F8>(ss, big, sh, wave, lane, turn);
         const float rs = __builtin_amdgcn_rsqf(fmaf(ss, inv_d, eps));
         float inv = rs;
         if (F8) {
@@ -188,9 +248,9 @@ avion_rmsnorm_fwd_kernel(const raw16* __restrict__ x, const void* __restrict__ r
         }
 #pragma unroll
         for (int j = 0; j < NCH; ++j) {
-            const int ch = at + 64 * WPR * j;
-            if (ch < nchunks) {
-                if (residual) RmsRow<NCH, WPR, R>::store(h, n, D, ch, v[j]);
+            const int ch = at + LANES * j;
+            if (ch < chunks) {
+                if (residual) RmsRow<NCH, LANES, R>::store(h, n, D, ch, v[j]);
                 float o[8];
 #pragma unroll
                 for (int e = 0; e < 8; ++e) o[e] = v[j][e] * rs * gain[j][e];
@@ -199,11 +259,11 @@ avion_rmsnorm_fwd_kernel(const raw16* __restrict__ x, const void* __restrict__ r
                     for (int e = 0; e < 8; ++e) o[e] *= inv;
                     *reinterpret_cast<u32x2*>(static_cast<char*>(y) + n * D + ch * 8) = pack_fp8(o);
                 } else {
-                    RmsRow<NCH, WPR, E>::store(y, n, D, ch, o);
+                    RmsRow<NCH, LANES, E>::store(y, n, D, ch, o);
                 }
             }
         }
-        if (at == 0) {
+        if (at == 0 && n < M) {
             if (F8) scale[n] = big * (1.0f / kF8Max);
             if (rstd) rstd[n] = rs;
         }
@@ -224,48 +284,51 @@ avion_rmsnorm_fwd_kernel(const raw16* __restrict__ x, const void* __restrict__ r
 }
 
 // rows of x as they are, in 8 bits
-template <int WPR, int NCH, typename E>
-__global__ void __launch_bounds__(RmsWork<WPR>::WAVES * 64)
+template <int LANES, int NCH, typename E>
+__global__ void __launch_bounds__(RmsWork<LANES>::WAVES * 64)
 avion_quantize_rows_kernel(const raw16* __restrict__ x, void* __restrict__ y, float* __restrict__ scale, long M, int D)
 {
-    using W = RmsWork<WPR>;
-    __shared__ float sh[2][WPR][2];
-    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, at = WPR == 1 ? lane : (int)threadIdx.x;
+    const RmsWork<LANES> rw;
+    __shared__ float sh[2][RmsWork<LANES>::WPR][2];
+    const int lane = rw.lane, wave = rw.wave, at = rw.at;
     const int nchunks = D / 8;
-    const long stride = (long)gridDim.x * W::ROWS;
-    long row = (long)blockIdx.x * W::ROWS + (WPR == 1 ? wave : 0);
+    const long stride = rw.stride();
+    long row = rw.first();
     if (row >= M) return;
     int turn = 0;
-    auto finish = [&](const RmsRow<NCH, WPR, E>& xr, long n) {
+    auto load = [&](RmsRow<NCH, LANES, E>& xr, long n) { xr.load(x, n + rw.sub, D, n + rw.sub < M ? nchunks : 0, at); };
+    auto finish = [&](const RmsRow<NCH, LANES, E>& xr, long n) {
+        n += rw.sub;
+        const int chunks = n < M ? nchunks : 0;
         float none = 0.f, big = 0.f;
 #pragma unroll
         for (int j = 0; j < NCH; ++j)
 #pragma unroll
             for (int e = 0; e < 8; ++e) big = fmaxf(big, fabsf(xr.get(j, e)));
-        row_reduce<WPR, true>(none, big, sh, wave, lane, turn);
+        row_reduce<LANES, true>(none, big, sh, wave, lane, turn);
         big = fmaxf(big, kF8Least);
         const float inv = kF8Max / big;
 #pragma unroll
         for (int j = 0; j < NCH; ++j) {
-            const int ch = at + 64 * WPR * j;
-            if (ch < nchunks) {
+            const int ch = at + LANES * j;
+            if (ch < chunks) {
                 float o[8];
 #pragma unroll
                 for (int e = 0; e < 8; ++e) o[e] = xr.get(j, e) * inv;
                 *reinterpret_cast<u32x2*>(static_cast<char*>(y) + n * D + ch * 8) = pack_fp8(o);
             }
         }
-        if (at == 0) scale[n] = big * (1.0f / kF8Max);
+        if (at == 0 && n < M) scale[n] = big * (1.0f / kF8Max);
     };
-    RmsRow<NCH, WPR, E> a, b;
-    a.load(x, row, D, nchunks, at);
+    RmsRow<NCH, LANES, E> a, b;
+    load(a, row);
     while (true) {
         const long n1 = row + stride;
-        if (n1 < M) b.load(x, n1, D, nchunks, at);
+        if (n1 < M) load(b, n1);
         finish(a, row);
         if (n1 >= M) break;
         const long n2 = n1 + stride;
-        if (n2 < M) a.load(x, n2, D, nchunks, at);
+        if (n2 < M) load(a, n2);
         finish(b, n1);
         if (n2 >= M) break;
         row = n2;
@@ -274,42 +337,46 @@ avion_quantize_rows_kernel(const raw16* __restrict__ x, void* __restrict__ y, fl
 
 // dx (E; the gradient of both inputs where the stream has that format too), dr (fp32 stream), either may be absent, and this
 // workgroup's partial sums of the gains' gradient into part[blockIdx.x][D].  dh may be absent.
-template <int WPR, int NCH, typename E, typename R>
-__global__ void __launch_bounds__(RmsWork<WPR>::WAVES * 64)
+template <int LANES, int NCH, typename E, typename R>
+__global__ void __launch_bounds__(RmsWork<LANES>::WAVES * 64)
 avion_rmsnorm_bwd_kernel(const void* __restrict__ h, const float* __restrict__ weight, const float* __restrict__ rstd,
                          const raw16* __restrict__ dy, const void* __restrict__ dh, void* __restrict__ dx,
                          float* __restrict__ dr, float* __restrict__ part, long M, int D)
 {
-    using W = RmsWork<WPR>;
+    const RmsWork<LANES> rw;
     extern __shared__ __attribute__((aligned(16))) char smem[];  // WPR = 1: (kRmsWaves - 1) x D floats
-    __shared__ float sh[2][WPR][2];
-    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, at = WPR == 1 ? lane : (int)threadIdx.x;
+    __shared__ float sh[2][RmsWork<LANES>::WPR][2];
+    const int lane = rw.lane, wave = rw.wave, at = rw.at;
     const int nchunks = D / 8;
     const float inv_d = 1.0f / (float)D;
-    const long stride = (long)gridDim.x * W::ROWS;
-    long row = (long)blockIdx.x * W::ROWS + (WPR == 1 ? wave : 0);
+    const long stride = rw.stride();
+    long row = rw.first();
     float gain[NCH][8], dw[NCH][8];
     int turn = 0;
 #pragma unroll
     for (int j = 0; j < NCH; ++j) {
-        const int ch = at + 64 * WPR * j;
+        const int ch = at + LANES * j;
 #pragma unroll
         for (int e = 0; e < 8; ++e) gain[j][e] = dw[j][e] = 0.f;
         if (ch < nchunks) load8(weight + ch * 8, gain[j]);
     }
 
     struct Rows {
-        RmsRow<NCH, WPR, R> h, dh;
-        RmsRow<NCH, WPR, E> dy;
+        RmsRow<NCH, LANES, R> h, dh;
+        RmsRow<NCH, LANES, E> dy;
         float rs;
     };
     auto load = [&](Rows& t, long n) {
-        t.h.load(h, n, D, nchunks, at);
-        t.dy.load(dy, n, D, nchunks, at);
-        if (dh) t.dh.load(dh, n, D, nchunks, at);
-        t.rs = rstd[n];
+        n += rw.sub;
+        const int chunks = n < M ? nchunks : 0;
+        t.h.template load<true>(h, n, D, chunks, at);
+        t.dy.template load<true>(dy, n, D, chunks, at);
+        if (dh) t.dh.template load<true>(dh, n, D, chunks, at);
+        t.rs = n < M ? rstd[n] : 0.f;
     };
     auto finish = [&](const Rows& t, long n) {
+        n += rw.sub;
+        const int chunks = n < M ? nchunks : 0;
         float s = 0.f, none = 0.f;
 #pragma unroll
         for (int j = 0; j < NCH; ++j)
@@ -319,24 +386,31 @@ avion_rmsnorm_bwd_kernel(const void* __restrict__ h, const float* __restrict__ w
                 s = fmaf(gy * gain[j][e], xh, s);  // zero in chunks past the row
                 dw[j][e] = fmaf(gy, xh, dw[j][e]);
             }
-        row_reduce<WPR, false>(s, none, sh, wave, lane, turn);
+        row_reduce<LANES, false>(s, none, sh, wave, lane, turn);
         const float c = s * inv_d;
 #pragma unroll
         for (int j = 0; j < NCH; ++j) {
-            const int ch = at + 64 * WPR * j;
-            if (ch < nchunks) {
+            const int ch = at + LANES * j;
+            if (ch < chunks) {
                 float o[8];
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
                     o[e] = t.rs * (t.dy.get(j, e) * gain[j][e] - t.h.get(j, e) * t.rs * c);
                     if (dh) o[e] += t.dh.get(j, e);
                 }
-                if (dx) RmsRow<NCH, WPR, E>::store(dx, n, D, ch, o);
+                if (dx) RmsRow<NCH, LANES, E>::store(dx, n, D, ch, o);
                 if (dr) store8(dr + n * D + ch * 8, o);
             }
         }
     };
-    if (row < M) {
+    if (NCH > 2) {
+        // (two rows in registers would leave one wavefront a SIMD)
+        for (; row < M; row += stride) {
+            Rows a;
+            load(a, row);
+            finish(a, row);
+        }
+    } else if (row < M) {
         Rows a, b;
         load(a, row);
         while (true) {
@@ -352,13 +426,25 @@ avion_rmsnorm_bwd_kernel(const void* __restrict__ h, const float* __restrict__ w
         }
     }
     float* out = part + (long)blockIdx.x * D;
-    if constexpr (WPR == 1) {
-        // workgroup sum in wavefront order (0 + 1 + 2 + 3)
+    if constexpr (LANES <= 64) {
+        // the rows that a wavefront held side by side, then the workgroup's sum in wavefront order (0 + 1 + 2 + 3)
+        if (LANES < 64)
+#pragma unroll
+            for (int j = 0; j < NCH; ++j)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    if (LANES == 16) {
+                        float a, b;
+                        sixteens(dw[j][e], a, b);
+                        dw[j][e] = a + b;
+                    }
+                    dw[j][e] = both_halves_sum(dw[j][e]);
+                }
         float* sums = reinterpret_cast<float*>(smem);
         if (wave > 0) {
 #pragma unroll
             for (int j = 0; j < NCH; ++j) {
-                const int ch = at + 64 * j;
+                const int ch = at + LANES * j;
                 if (ch < nchunks) store8(sums + (wave - 1) * D + ch * 8, dw[j]);
             }
         }
@@ -366,9 +452,9 @@ avion_rmsnorm_bwd_kernel(const void* __restrict__ h, const float* __restrict__ w
         if (wave > 0) return;
 #pragma unroll
         for (int j = 0; j < NCH; ++j) {
-            const int ch = at + 64 * j;
+            const int ch = at + LANES * j;
             if (ch < nchunks)
-                for (int w = 0; w < W::WAVES - 1; ++w) {
+                for (int w = 0; w < kRmsWaves - 1; ++w) {
                     float a[8];
                     load8(sums + w * D + ch * 8, a);
 #pragma unroll
@@ -378,7 +464,7 @@ avion_rmsnorm_bwd_kernel(const void* __restrict__ h, const float* __restrict__ w
     }
 #pragma unroll
     for (int j = 0; j < NCH; ++j) {
-        const int ch = at + 64 * WPR * j;
+        const int ch = at + LANES * j;
         if (ch < nchunks) store8(out + ch * 8, dw[j]);
     }
 }

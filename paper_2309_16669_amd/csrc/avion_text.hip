@@ -24,33 +24,35 @@ int rms_check(long long M, int D, unsigned flags, unsigned allowed)
     if (M > (1LL << 40)) return AVION_EUNSUPPORTED;
     return AVION_OK;
 }
-// Wavefronts a row.  One holds up to 2048 columns (4 chunks a lane) and needs no exchange through LDS; wider rows take four, or
-// eight beyond 8192.  Few rows take four as well.
-int rms_wavefronts(long long M, int D)
+// Lanes a row.  A wavefront holds up to 2048 columns (4 chunks a lane) and needs no exchange through LDS; narrow rows take 16
+// or 32 lanes, wide ones four wavefronts, or eight beyond 8192.  Few rows take four wavefronts as well.
+int rms_lanes(long long M, int D)
 {
-    if (D > 8192) return 8;
-    if (D > 2048 || (D > 512 && M <= 1024)) return 4;
-    return 1;
+    if (D > 8192) return 512;
+    if (D > 2048 || (D > 512 && M <= 1024)) return 256;
+    return D <= 128 ? 16 : D <= 256 ? 32 : 64;
 }
 unsigned rms_grid(long long M, int D)
 {
-    const int rows = rms_wavefronts(M, D) == 1 ? kRmsWaves : 1;
+    const int lanes = rms_lanes(M, D), rows = lanes <= 64 ? kRmsWaves * (64 / lanes) : 1;
     return (unsigned)std::min<long long>((M + rows - 1) / rows, kRmsMaxGrid);
 }
-// f(wavefronts a row, chunks a lane)
+// f(lanes a row, chunks a lane)
 template <typename F>
 int rms_by_width(long long M, int D, F f)
 {
-    const int wpr = rms_wavefronts(M, D), per_lane = (D / 8 + 64 * wpr - 1) / (64 * wpr);
-    if (wpr == 8) return f(Int<8>{}, Int<4>{});
-    if (wpr == 4) {
-        if (per_lane <= 1) return f(Int<4>{}, Int<1>{});
-        if (per_lane <= 2) return f(Int<4>{}, Int<2>{});
-        return f(Int<4>{}, Int<4>{});
+    const int lanes = rms_lanes(M, D), per_lane = (D / 8 + lanes - 1) / lanes;
+    if (lanes == 16) return f(Int<16>{}, Int<1>{});
+    if (lanes == 32) return f(Int<32>{}, Int<1>{});
+    if (lanes == 512) return f(Int<512>{}, Int<4>{});
+    if (lanes == 256) {
+        if (per_lane <= 1) return f(Int<256>{}, Int<1>{});
+        if (per_lane <= 2) return f(Int<256>{}, Int<2>{});
+        return f(Int<256>{}, Int<4>{});
     }
-    if (per_lane <= 1) return f(Int<1>{}, Int<1>{});
-    if (per_lane <= 2) return f(Int<1>{}, Int<2>{});
-    return f(Int<1>{}, Int<4>{});
+    if (per_lane <= 1) return f(Int<64>{}, Int<1>{});
+    if (per_lane <= 2) return f(Int<64>{}, Int<2>{});
+    return f(Int<64>{}, Int<4>{});
 }
 // f(stream's format): E, or fp32
 template <typename E, typename F>
@@ -78,11 +80,11 @@ int rmsnorm_fwd_impl(const void* x, const void* residual, const float* weight, v
     return by_element(flags, [&](auto fmt) {
         using E = typename decltype(fmt)::type;
         return rms_by_stream<E>(flags, [&](auto wide) {
-            return rms_by_width(M, D, [&](auto wpr, auto nch) {
-                constexpr int WPR = decltype(wpr)::value;
+            return rms_by_width(M, D, [&](auto lanes, auto nch) {
+                constexpr int LANES = decltype(lanes)::value;
                 begin_launch();
-                hipLaunchKernelGGL((avion_rmsnorm_fwd_kernel<WPR, decltype(nch)::value, E, typename decltype(wide)::type, F8>),
-                                   dim3(rms_grid(M, D)), dim3(RmsWork<WPR>::WAVES * 64), 0, st, static_cast<const raw16*>(x),
+                hipLaunchKernelGGL((avion_rmsnorm_fwd_kernel<LANES, decltype(nch)::value, E, typename decltype(wide)::type, F8>),
+                                   dim3(rms_grid(M, D)), dim3(RmsWork<LANES>::WAVES * 64), 0, st, static_cast<const raw16*>(x),
                                    residual, weight, y, scale, h, rstd, (long)M, D, eps);
                 return end_launch("launch avion_rmsnorm_fwd_kernel");
             });
@@ -206,11 +208,11 @@ int avion_rmsnorm_bwd(const void* h, const float* weight, const float* rstd, con
         const int r1 = by_element(flags, [&](auto fmt) {
             using E = typename decltype(fmt)::type;
             return rms_by_stream<E>(flags, [&](auto wide) {
-                return rms_by_width(M, D, [&](auto wpr, auto nch) {
-                    constexpr int WPR = decltype(wpr)::value;
+                return rms_by_width(M, D, [&](auto lanes, auto nch) {
+                    constexpr int LANES = decltype(lanes)::value;
                     begin_launch();
-                    hipLaunchKernelGGL((avion_rmsnorm_bwd_kernel<WPR, decltype(nch)::value, E, typename decltype(wide)::type>),
-                                       dim3(grid), dim3(RmsWork<WPR>::WAVES * 64), WPR == 1 ? (kRmsWaves - 1) * D * sizeof(float) : 0,
+                    hipLaunchKernelGGL((avion_rmsnorm_bwd_kernel<LANES, decltype(nch)::value, E, typename decltype(wide)::type>),
+                                       dim3(grid), dim3(RmsWork<LANES>::WAVES * 64), LANES <= 64 ? (kRmsWaves - 1) * D * sizeof(float) : 0,
                                        st, h, weight, rstd, static_cast<const raw16*>(dy), dh, dx, dresidual, part, (long)M, D);
                     return end_launch("launch avion_rmsnorm_bwd_kernel");
                 });
@@ -234,11 +236,11 @@ int avion_quantize_rows(const void* x, void* x8, float* scale, long long M, int 
     if (!aligned16(x) || !aligned16(x8) || !aligned16(scale) || D % 16 != 0) return AVION_EUNSUPPORTED;
     hipStream_t st = static_cast<hipStream_t>(stream);
     return by_element(flags, [&](auto fmt) {
-        return rms_by_width(M, D, [&](auto wpr, auto nch) {
-            constexpr int WPR = decltype(wpr)::value;
+        return rms_by_width(M, D, [&](auto lanes, auto nch) {
+            constexpr int LANES = decltype(lanes)::value;
             begin_launch();
-            hipLaunchKernelGGL((avion_quantize_rows_kernel<WPR, decltype(nch)::value, typename decltype(fmt)::type>),
-                               dim3(rms_grid(M, D)), dim3(RmsWork<WPR>::WAVES * 64), 0, st, static_cast<const raw16*>(x), x8, scale,
+            hipLaunchKernelGGL((avion_quantize_rows_kernel<LANES, decltype(nch)::value, typename decltype(fmt)::type>),
+                               dim3(rms_grid(M, D)), dim3(RmsWork<LANES>::WAVES * 64), 0, st, static_cast<const raw16*>(x), x8, scale,
                                (long)M, D);
             return end_launch("launch avion_quantize_rows_kernel");
         });

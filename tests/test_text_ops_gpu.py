@@ -246,8 +246,8 @@ def _norm_check(M, D, fmt, stream, eps=1e-6, seed=0, mul=1.0, use_dh=True):
     return y, dx, dw
 
 
-NORM_SHAPES = [(1, 8), (1, 64), (3, 72), (5, 512), (33, 520), (130, 768), (1025, 768), (4097, 1288), (257, 2048), (1030, 2048), (2, 2056),
-               (1, 4096), (65, 4104), (1300, 4096), (7, 8192), (3, 8200), (2, 16384), (1100, 8200)]
+NORM_SHAPES = [(1, 8), (1, 64), (3, 72), (4099, 128), (13, 136), (1001, 200), (2048, 256), (5, 512), (33, 520), (130, 768), (1025, 768), (4097, 1288), (257, 2048), (1030, 2048), (2, 2056),
+               (1, 4096), (65, 4104), (1300, 4096), (7, 8192), (3, 8200), (2, 16384), (1100, 8200), (700, 16384)]
 
 
 @pytest.mark.parametrize("M,D", NORM_SHAPES)
@@ -363,7 +363,7 @@ def _rows8_check(y64, q, scale, noise):
     within("q", q.float(), v, ops.e4m3_half_step(v) + 2 * noise * np.abs(v))
 
 
-@pytest.mark.parametrize("M,D", [(1, 16), (1, 4096), (3, 80), (5, 512), (33, 528), (130, 768), (1025, 768), (4097, 1296), (1030, 2048),
+@pytest.mark.parametrize("M,D", [(1, 16), (1, 4096), (3, 80), (2050, 128), (77, 144), (999, 256), (5, 512), (33, 528), (130, 768), (1025, 768), (4097, 1296), (1030, 2048),
                                  (2, 2064), (65, 4112), (1300, 4096), (3, 8208), (2, 16384)])
 @pytest.mark.parametrize("fmt,stream", [(BF, BF), (HF, FP), (BF, None), (HF, HF)])
 def test_rows_in_8_bits(M, D, fmt, stream):
