@@ -90,19 +90,20 @@ avion_linear_fp8_few_kernel(const char* __restrict__ x8, const float* __restrict
 }
 
 // ------------------------------------------------------------------------------------ many rows
-// Tiles of TM rows of x8 by TN rows of w8, 64 bytes of K at a time, moved global -> LDS by LDS-direct loads into one of three
-// buffers: while a step is multiplied, the next one has been asked for and the one after is being asked for.
-// LDS: rows of 64 bytes; the four 16-byte chunks of a row are permuted by a XOR with bits 2..3 of the row number, so that a
+// Tiles of TM rows of x8 by TN rows of w8, 128 bytes of K (whole cache lines) at a time, moved global -> LDS by LDS-direct loads
+// into one of ST buffers: while a step is multiplied, the next ones are on their way.  With KG = 2 two groups of wavefronts
+// take every other step each, for launches whose time is the chain of steps, and add their sums at the end.
+// LDS: rows of 128 bytes; the eight 16-byte chunks of a row are permuted by a XOR with bits 1..3 of the row number, so that a
 // fragment read (16 consecutive lanes: 16 rows, one chunk) meets 16 different places.
-template <int TM, int TN, int WM, int WN, int ST>
+template <int TM, int TN, int WM, int WN, int ST, int KG>
 struct Fp8Cfg {
-    static constexpr int BK = 128, STAGES = ST, NT = WM * WN * 64;
+    static constexpr int BK = 128, STAGES = ST, NT = WM * WN * KG * 64;
     static constexpr int MI = TM / WM / 32, NI = TN / WN / 32;  // 32 x 32 tiles of a wavefront
     static constexpr int BLOCKS = (TM + TN) / 8;                // 1 KB loads of a step
     static constexpr int LOADS = BLOCKS / (WM * WN);            // of a wavefront
     static constexpr int STAGE = (TM + TN) * BK;
-    static constexpr int LDS_BYTES = STAGE * STAGES;
-    static_assert(BLOCKS % (WM * WN) == 0 && TM % 8 == 0, "");
+    static constexpr int LDS_BYTES = STAGE * STAGES * KG;
+    static_assert(BLOCKS % (WM * WN) == 0 && TM % 8 == 0 && ST >= 2 && ST <= 6 && (ST - 1) * LOADS < 64, "");
 };
 
 // Between the lanes of one wavefront: LDS takes its accesses in the order of the program, which the compiler, looking at one
@@ -115,24 +116,25 @@ DEVINL void fp8_landed_barrier()
     asm volatile("s_waitcnt vmcnt(%0)\n\ts_waitcnt lgkmcnt(0)\n\ts_barrier" ::"i"(LOADS) : "memory");
 }
 
-template <int TM, int TN, int WM, int WN, int ST, typename E>
-__global__ void __launch_bounds__(WM* WN * 64, WM * WN == 8 ? 1 : 2)
+template <int TM, int TN, int WM, int WN, int ST, int KG, typename E>
+__global__ void __launch_bounds__(WM* WN* KG * 64, KG > 1 ? 1 : 2)
 avion_linear_fp8_kernel(const char* __restrict__ x8, const float* __restrict__ x_scale, const char* __restrict__ w8,
                         const float* __restrict__ w_scale, const float* __restrict__ bias, raw16* __restrict__ y, int M, int N, int K,
                         int ntn, int ntiles)
 {
-    using Cfg = Fp8Cfg<TM, TN, WM, WN, ST>;
+    using Cfg = Fp8Cfg<TM, TN, WM, WN, ST, KG>;
     extern __shared__ __attribute__((aligned(16))) char smem[];
-    const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), l32 = lane % 32, g = lane / 32;
+    const int lane = threadIdx.x % 64, l32 = lane % 32, g = lane / 32;
+    const int group = __builtin_amdgcn_readfirstlane(threadIdx.x / (WM * WN * 64)), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64) % (WM * WN);
     // consecutive tiles on one XCD (workgroups go round the 8 of them): the tiles of one block of x8 share its L2
     const int per = gridDim.x / 8, tile = (blockIdx.x % 8) * per + blockIdx.x / 8;
     if (tile >= ntiles) return;
     const int m0 = tile / ntn * TM, n0 = tile % ntn * TN;
     const int rows_m = M - m0 < TM ? M - m0 : TM, rows_n = N - n0 < TN ? N - n0 : TN;
     const RawBuffer xb(x8 + (long)m0 * K, (unsigned)rows_m * (unsigned)K), wb(w8 + (long)n0 * K, (unsigned)rows_n * (unsigned)K);
-    const unsigned lds = lds_address(smem);
+    const unsigned lds = lds_address(smem) + group * (Cfg::STAGE * ST);  // each group of wavefronts has its own steps and buffers
 
-    // 1 KB block b of a step: rows 16 b .. 16 b + 15 (x8's, then w8's); lane i brings the chunk that lies at 16 i
+    // 1 KB block b of a step: rows 8 b .. 8 b + 7 (x8's, then w8's); lane i brings the chunk that lies at 16 i
     const unsigned ch = ((lane & 7) ^ (lane >> 4 & 3)) * 16;
     unsigned voff[Cfg::LOADS];
 #pragma unroll
@@ -142,7 +144,7 @@ avion_linear_fp8_kernel(const char* __restrict__ x8, const float* __restrict__ x
         voff[i] = (unsigned)row * (unsigned)K;
     }
     auto fetch = [&](int step, int buf) {
-        const unsigned k = (unsigned)step * Cfg::BK;
+        const unsigned k = (unsigned)(step * KG + group) * Cfg::BK;
 #pragma unroll
         for (int i = 0; i < Cfg::LOADS; ++i) {
             const int b = wave + i * WM * WN;
@@ -163,17 +165,20 @@ avion_linear_fp8_kernel(const char* __restrict__ x8, const float* __restrict__ x
 #pragma unroll
         for (int j = 0; j < Cfg::NI; ++j) acc[i][j] = f32x16_zero();
 
-    const int steps = (K + Cfg::BK - 1) / Cfg::BK;
+    const int steps = (K + Cfg::BK * KG - 1) / (Cfg::BK * KG);
 #pragma unroll
     for (int i = 0; i < ST; ++i)
         if (i < steps) fetch(i, i);
     // `left`: steps behind the awaited one that have been asked for
     auto landed = [&](int left) {
-        if (left >= ST - 1) fp8_landed_barrier<(ST - 1) * Cfg::LOADS>();
-        else if (left == 3) fp8_landed_barrier<(ST > 4 ? 3 : 0) * Cfg::LOADS>();
-        else if (left == 2) fp8_landed_barrier<(ST > 3 ? 2 : 0) * Cfg::LOADS>();
-        else if (left == 1) fp8_landed_barrier<Cfg::LOADS>();
-        else fp8_landed_barrier<0>();
+        switch (min(left, ST - 1)) {
+            case 5: fp8_landed_barrier<5 * Cfg::LOADS>(); break;
+            case 4: fp8_landed_barrier<4 * Cfg::LOADS>(); break;
+            case 3: fp8_landed_barrier<3 * Cfg::LOADS>(); break;
+            case 2: fp8_landed_barrier<2 * Cfg::LOADS>(); break;
+            case 1: fp8_landed_barrier<Cfg::LOADS>(); break;
+            default: fp8_landed_barrier<0>();
+        }
     };
     auto read = [&](unsigned base, unsigned half) { return join16(*(ptr)(base + (c0 ^ half)), *(ptr)(base + (c1 ^ half))); };
     i32x8 a[2][Cfg::NI], b;
@@ -232,6 +237,22 @@ avion_linear_fp8_kernel(const char* __restrict__ x8, const float* __restrict__ x
 #pragma unroll
     for (int i = 0; i < Cfg::MI; ++i) sx[i] = x_scale[min(m_wave + 32 * i + l32, M - 1)];
     __syncthreads();  // everybody has read the last step's buffer
+    if constexpr (KG > 1) {
+        // the groups' sums, in the groups' order
+        static_assert(Cfg::MI * Cfg::NI * WM * WN * 4096 <= Cfg::STAGE * ST && KG == 2, "");
+        f32x16* sums = reinterpret_cast<f32x16*>(smem + Cfg::STAGE * ST) + wave * (Cfg::MI * Cfg::NI * 64) + lane;
+#pragma unroll
+        for (int i = 0; i < Cfg::MI; ++i)
+#pragma unroll
+            for (int j = 0; j < Cfg::NI; ++j)
+                if (group == 1) sums[(i * Cfg::NI + j) * 64] = acc[i][j];
+        __syncthreads();
+        if (group == 1) return;
+#pragma unroll
+        for (int i = 0; i < Cfg::MI; ++i)
+#pragma unroll
+            for (int j = 0; j < Cfg::NI; ++j) acc[i][j] += sums[(i * Cfg::NI + j) * 64];
+    }
     char* out = smem + wave * (32 * ROW);
     const int n = n_wave + lane % LANES * 8;
 #pragma unroll
@@ -272,7 +293,7 @@ constexpr int kWideLds = 2 * kWideStage + 3 * kWideScales + kWideWaves * 16 * kW
 constexpr int kWideStores = 16;
 constexpr int kNontemporal = 2;  // of a buffer access's cache policy
 
-template <typename E>
+template <typename E, bool STREAM>
 __global__ void __launch_bounds__(kWideWaves * 64)
 avion_linear_fp8_wide_kernel(const char* __restrict__ x8, const float* __restrict__ x_scale, const char* __restrict__ w8,
                              const float* __restrict__ w_scale, const float* __restrict__ bias, raw16* __restrict__ y, int M, int N,
@@ -437,7 +458,7 @@ avion_linear_fp8_wide_kernel(const char* __restrict__ x8, const float* __restric
                     const u32x4 v = *reinterpret_cast<const u32x4*>(stage + (r + lane / 8) * kWideRow + lane % 8 * 16);
                     const unsigned row = wm * 128 + 32 * i + 16 * half + r + lane / 8;
                     __builtin_amdgcn_raw_buffer_store_b128(v, out, col_at == kOutOfRangeBase ? kOutOfRangeBase : row * (unsigned)N * 2 + col_at,
-                                                           0, kNontemporal);
+                                                           0, STREAM ? kNontemporal : 0);
                 }
                 own_lds_written();
             }

@@ -24,13 +24,13 @@ int launch_few(const char* x8, const float* xs, const char* w8, const float* ws,
     return end_launch("launch avion_linear_fp8_few_kernel");
 }
 long long fp8_tiles(int M, int N, int tm, int tn) { return (long long)((M + tm - 1) / tm) * ((N + tn - 1) / tn); }
-template <int TM, int TN, int WM, int WN, int ST, typename E>
+template <int TM, int TN, int WM, int WN, int ST, int KG, typename E>
 int launch_fp8(const char* x8, const float* xs, const char* w8, const float* ws, const float* bias, raw16* y, int M, int N, int K,
                hipStream_t st)
 {
-    using Cfg = Fp8Cfg<TM, TN, WM, WN, ST>;
+    using Cfg = Fp8Cfg<TM, TN, WM, WN, ST, KG>;
     static std::atomic<bool> lds_allowed{false};
-    const auto kernel = avion_linear_fp8_kernel<TM, TN, WM, WN, ST, E>;
+    const auto kernel = avion_linear_fp8_kernel<TM, TN, WM, WN, ST, KG, E>;
     const hipError_t attr = allow_lds(kernel, Cfg::LDS_BYTES, lds_allowed);
     if (attr != hipSuccess) return hip_fail(attr, "hipFuncSetAttribute(linear_fp8)");
     const long long tiles = fp8_tiles(M, N, TM, TN);
@@ -46,21 +46,22 @@ int launch_fp8(const char* x8, const float* xs, const char* w8, const float* ws,
 //     32 x 1024 x 1024: 4.1 and 5.3, but 32 x 6144 x 4096: 14.4 and 12.8.
 //   else the smallest tiles that leave no more than one for a compute unit (latency), larger ones beyond (traffic):
 //     64 x 64 and 128 x 64 on 1024 x 1024 x 1024 (256 tiles): 6.0 and 6.9, on 512 x 4096 x 4096 (512): 21.8 and 17.5;
+//     with eight wavefronts, half of K each, where K is long: 64 x 6144 x 4096: 13.3 -> 10.7, 64 x 2304 x 768: 4.8 and 4.8;
 //     128 x 64 and 128 x 128 on 785 x 2304 x 768 (126 tiles of 128 x 128): 6.8 and 8.7, on 1570 x 3840 x 1280 (390): 19.3 and 16.2
 //   256 x 256: a round of its 256 tiles takes about as long as 820 tiles of 128 x 128 in a long row and less to begin with, so it
 //     needs rounds that are well filled: 12544 x 768 x 768 (147 tiles): 14.8 against 17.4 of 128 x 128, 2048 x 4096 x 4096 (128):
-//     46 against 38, 6272 x 2304 x 768 (225): 16.5 against 20.6, 50176 x 2304 x 768: 109 against 164
+//     46 against 38, 6272 x 2304 x 768 (225): 16.5 against 20.6, 50176 x 2304 x 768: 88 against 165
 bool fp8_wide(int M, int N)
 {
     const long long tiles = fp8_tiles(M, N, kWideM, kWideN), rounds = (tiles + kComputeUnits - 1) / kComputeUnits;
     return 5 * (tiles + 64) >= 4 * kComputeUnits * rounds;
 }
-template <typename E>
+template <typename E, bool STREAM>
 int launch_wide(const char* x8, const float* xs, const char* w8, const float* ws, const float* bias, raw16* y, int M, int N, int K,
                 hipStream_t st)
 {
     static std::atomic<bool> lds_allowed{false};
-    const auto kernel = avion_linear_fp8_wide_kernel<E>;
+    const auto kernel = avion_linear_fp8_wide_kernel<E, STREAM>;
     const hipError_t attr = allow_lds(kernel, kWideLds, lds_allowed);
     if (attr != hipSuccess) return hip_fail(attr, "hipFuncSetAttribute(linear_fp8_wide)");
     const int ntm = (M + kWideM - 1) / kWideM, ntn = (N + kWideN - 1) / kWideN;
@@ -93,12 +94,16 @@ int avion_linear_fp8(const void* x8, const float* x_scale, const void* w8, const
         using E = typename decltype(fmt)::type;
         if (m <= 16) return launch_few<1, E>(x, x_scale, w, w_scale, bias, out, m, N, K, st);
         if (m <= 32 && K <= 2048) return launch_few<2, E>(x, x_scale, w, w_scale, bias, out, m, N, K, st);
-        if (fp8_wide(m, N)) return launch_wide<E>(x, x_scale, w, w_scale, bias, out, m, N, K, st);
+        // (stores past the caches only where rows are whole cache lines: 30000 x 1544 x 768 67.6 us with them, 54.8 without,
+        // 50176 x 2304 x 768 88 and 112)
+        if (fp8_wide(m, N) && N % 64 == 0) return launch_wide<E, true>(x, x_scale, w, w_scale, bias, out, m, N, K, st);
+        if (fp8_wide(m, N)) return launch_wide<E, false>(x, x_scale, w, w_scale, bias, out, m, N, K, st);
         if (fp8_tiles(m, N, 128, 128) >= kComputeUnits)
-            return launch_fp8<128, 128, 2, 2, 2, E>(x, x_scale, w, w_scale, bias, out, m, N, K, st);
+            return launch_fp8<128, 128, 2, 2, 2, 1, E>(x, x_scale, w, w_scale, bias, out, m, N, K, st);
         if (fp8_tiles(m, N, 64, 64) > kComputeUnits)
-            return launch_fp8<128, 64, 2, 2, 3, E>(x, x_scale, w, w_scale, bias, out, m, N, K, st);
-        return launch_fp8<64, 64, 2, 2, 3, E>(x, x_scale, w, w_scale, bias, out, m, N, K, st);
+            return launch_fp8<128, 64, 2, 2, 3, 1, E>(x, x_scale, w, w_scale, bias, out, m, N, K, st);
+        if (K >= 1024) return launch_fp8<64, 64, 2, 2, 3, 2, E>(x, x_scale, w, w_scale, bias, out, m, N, K, st);
+        return launch_fp8<64, 64, 2, 2, 3, 1, E>(x, x_scale, w, w_scale, bias, out, m, N, K, st);
     });
 }
 

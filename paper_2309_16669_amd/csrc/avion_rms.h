@@ -8,8 +8,9 @@
 // What the backward needs from the forward is h itself, which the stream keeps anyway, and one fp32 per row.
 //
 // Bound by memory bandwidth: forward two reads and two writes per element, backward three reads and one write (two with a
-// stream in 32 bits).  WPR wavefronts own a row at a time, lane j of them the 16-byte chunks j, j + 64 WPR, ...: all of the
-// row is in registers, so it is read once, and the next row is requested before the current one is worked on.  Sums and
+// stream in 32 bits).  LANES lanes own a row at a time (16 or 32 neighbours, a wavefront, or 4 or 8 wavefronts), lane j of
+// them the 16-byte chunks j, j + LANES, ...: all of the row is in registers, so it is read once, and the next row is requested
+// before the current one is worked on.  Sums and
 // statistics are fp32, outputs are rounded once (nearest even).  max|y| is rstd max|h w|, so that the row's sum and its maximum
 // travel through one exchange.  The gains' gradient is summed over each wavefront's rows in registers, over the workgroup's
 // through LDS and over the workgroups by avion_ln_param_reduce_kernel in a fixed order: no atomics, bit-reproducible.
@@ -336,20 +337,58 @@ avion_quantize_rows_kernel(const raw16* __restrict__ x, void* __restrict__ y, fl
 }
 
 // dx (E; the gradient of both inputs where the stream has that format too), dr (fp32 stream), either may be absent, and this
-// workgroup's partial sums of the gains' gradient into part[blockIdx.x][D].  dh may be absent.
-template <int LANES, int NCH, typename E, typename R>
+// workgroup's partial sums of the gains' gradient into part[blockIdx.x][D].  dh may be absent.  FEW: few rows, in one launch:
+// the workgroups behind the first row_wgs sum 64 columns of the gains' gradient each over all rows, which they read once more
+// (rstd is known, so they need nothing of the others), into dweight.
+constexpr int kRmsFewCols = 64;
+template <int LANES, int NCH, typename E, typename R, bool FEW>
 __global__ void __launch_bounds__(RmsWork<LANES>::WAVES * 64)
 avion_rmsnorm_bwd_kernel(const void* __restrict__ h, const float* __restrict__ weight, const float* __restrict__ rstd,
                          const raw16* __restrict__ dy, const void* __restrict__ dh, void* __restrict__ dx,
-                         float* __restrict__ dr, float* __restrict__ part, long M, int D)
+                         float* __restrict__ dr, float* __restrict__ part, float* __restrict__ dweight, long M, int D, int row_wgs)
 {
     const RmsWork<LANES> rw;
-    extern __shared__ __attribute__((aligned(16))) char smem[];  // WPR = 1: (kRmsWaves - 1) x D floats
+    extern __shared__ __attribute__((aligned(16))) char smem[];  // LANES <= 64: (kRmsWaves - 1) x D floats
     __shared__ float sh[2][RmsWork<LANES>::WPR][2];
+    if constexpr (FEW) {
+        constexpr int LPC = kRmsFewCols / 8, GROUPS = RmsWork<LANES>::WAVES * 64 / LPC, FLY = 4;
+        __shared__ float sums[GROUPS][kRmsFewCols];
+        if ((int)blockIdx.x >= row_wgs) {
+            const int lane = threadIdx.x % LPC, group = threadIdx.x / LPC, ch = ((int)blockIdx.x - row_wgs) * LPC + lane;
+            float acc[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+            for (long r0 = group; r0 < M; r0 += FLY * GROUPS) {
+                RmsRow<1, 64, R> hh[FLY];
+                RmsRow<1, 64, E> dd[FLY];
+                float rs[FLY];
+#pragma unroll
+                for (int k = 0; k < FLY; ++k) {
+                    const long n = r0 + k * GROUPS;
+                    const int chunks = n < M ? D / 8 : 0;
+                    hh[k].load(h, n, D, chunks, ch);
+                    dd[k].load(dy, n, D, chunks, ch);
+                    rs[k] = n < M ? rstd[n] : 0.f;
+                }
+#pragma unroll
+                for (int k = 0; k < FLY; ++k)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) acc[e] = fmaf(dd[k].get(0, e), hh[k].get(0, e) * rs[k], acc[e]);
+            }
+            store8(&sums[group][lane * 8], acc);
+            __syncthreads();
+            const int col = ((int)blockIdx.x - row_wgs) * kRmsFewCols + threadIdx.x;
+            if (threadIdx.x < kRmsFewCols && col < D) {
+                float t = 0.f;
+#pragma unroll
+                for (int g = 0; g < GROUPS; ++g) t += sums[g][threadIdx.x];
+                dweight[col] = t;
+            }
+            return;
+        }
+    }
     const int lane = rw.lane, wave = rw.wave, at = rw.at;
     const int nchunks = D / 8;
     const float inv_d = 1.0f / (float)D;
-    const long stride = rw.stride();
+    const long stride = (long)row_wgs * RmsWork<LANES>::ROWS;
     long row = rw.first();
     float gain[NCH][8], dw[NCH][8];
     int turn = 0;
@@ -369,9 +408,9 @@ avion_rmsnorm_bwd_kernel(const void* __restrict__ h, const float* __restrict__ w
     auto load = [&](Rows& t, long n) {
         n += rw.sub;
         const int chunks = n < M ? nchunks : 0;
-        t.h.template load<true>(h, n, D, chunks, at);
-        t.dy.template load<true>(dy, n, D, chunks, at);
-        if (dh) t.dh.template load<true>(dh, n, D, chunks, at);
+        t.h.template load<!FEW>(h, n, D, chunks, at);
+        t.dy.template load<!FEW>(dy, n, D, chunks, at);
+        if (dh) t.dh.template load<!FEW>(dh, n, D, chunks, at);
         t.rs = n < M ? rstd[n] : 0.f;
     };
     auto finish = [&](const Rows& t, long n) {
@@ -384,7 +423,7 @@ avion_rmsnorm_bwd_kernel(const void* __restrict__ h, const float* __restrict__ w
             for (int e = 0; e < 8; ++e) {
                 const float xh = t.h.get(j, e) * t.rs, gy = t.dy.get(j, e);
                 s = fmaf(gy * gain[j][e], xh, s);  // zero in chunks past the row
-                dw[j][e] = fmaf(gy, xh, dw[j][e]);
+                if (!FEW) dw[j][e] = fmaf(gy, xh, dw[j][e]);
             }
         row_reduce<LANES, false>(s, none, sh, wave, lane, turn);
         const float c = s * inv_d;
@@ -425,6 +464,7 @@ avion_rmsnorm_bwd_kernel(const void* __restrict__ h, const float* __restrict__ w
             row = n2;
         }
     }
+    if constexpr (FEW) return;
     float* out = part + (long)blockIdx.x * D;
     if constexpr (LANES <= 64) {
         // the rows that a wavefront held side by side, then the workgroup's sum in wavefront order (0 + 1 + 2 + 3)
