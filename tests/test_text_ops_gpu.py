@@ -92,9 +92,11 @@ def _embed(tokens, V, D, table, out, scale, token_type="int64", seed=0):
     return y, dw
 
 
-SMALL = [(1, 1, 8), (1, 50000, 512), (7, 3, 64), (64, 64, 520), (77, 1000, 512), (1000, 5, 72), (1024, 3000, 776), (1023, 1, 1032)]
-LARGE = [(1025, 3, 64), (1025, 3000, 512), (5000, 1, 8), (2048, 1023, 776), (2049, 1024, 520), (40000, 300000, 24), (9999, 1100000, 8),
-         (300000, 700, 16)]
+# one launch (up to 512 slots), sorted by counting (up to 8192), by one, two and three digits; sums of 8 and (from 32768) of 32
+# slots a wavefront; narrow, ragged and several blocks of columns
+SMALL = [(1, 1, 8), (1, 50000, 512), (7, 3, 64), (64, 64, 520), (77, 1000, 512), (500, 5, 72), (512, 3000, 776), (511, 1, 1032)]
+LARGE = [(513, 3, 64), (1025, 3000, 512), (5000, 1, 8), (2048, 1023, 776), (8192, 1024, 520), (8193, 200, 64), (9999, 256, 1032), (20000, 40000, 136),
+         (32767, 500, 72), (32768, 500, 72), (40000, 300000, 24), (9999, 1100000, 8), (300000, 700, 16)]
 
 
 @pytest.mark.parametrize("n,V,D", SMALL + LARGE)
@@ -105,14 +107,14 @@ def test_embedding_shapes(n, V, D, table, out):
 
 
 @pytest.mark.parametrize("table,out", [(BF, BF), (HF, HF), (FP, BF), (FP, HF)])
-@pytest.mark.parametrize("n", [900, 20000])
+@pytest.mark.parametrize("n", [400, 4000, 20000, 36000])
 def test_embedding_formats(table, out, n):
     rng = np.random.default_rng(n)
     tokens = rng.integers(0, 333, size=(4, n // 4))
     _embed(tokens, 333, 136, table, out, float(np.sqrt(136.0)), seed=n)
 
 
-@pytest.mark.parametrize("n", [1000, 3000, 70000])
+@pytest.mark.parametrize("n", [400, 3000, 20000, 70000])
 @pytest.mark.parametrize("kind", ["one", "padding", "none", "outside", "ends", "sorted", "reversed"])
 def test_embedding_contents(kind, n):
     # one token everywhere; three quarters padding; no token at all; some slots outside the table on either side; the first and
@@ -136,14 +138,18 @@ def test_embedding_contents(kind, n):
     _embed(t, V, D, BF, BF, -0.25, seed=5)
 
 
-@pytest.mark.parametrize("lengths", [[32] * 40, [128] * 12, [31, 33] * 30, [127, 1, 128, 256, 129, 383, 1, 1, 126, 500], [64, 96] * 12,
-                                     [1] * 1100, [1500], [1, 1499], [96, 128, 32, 256, 160, 700, 4, 60]])
+@pytest.mark.parametrize("lengths", [[8] * 100, [64] * 20, [7, 9] * 60, [63, 1, 64, 128, 65, 191, 1, 1, 62, 500], [16, 48] * 20, [1] * 1100, [1500],
+                                     [1, 1499], [56, 64, 8, 128, 72, 700, 4, 60], [64] * 200, [9000], [32] * 1100, [256] * 140, [31, 33] * 600,
+                                     [255, 1, 256, 512, 257, 767, 1, 1, 254, 5000] * 5, [32, 224] * 140, [36000], [1, 33000, 7],
+                                     [192, 256, 32, 512, 288, 700, 4, 60] * 20],
+                         ids=lambda v: f"{len(v)}_runs_{sum(v)}")
 def test_embedding_runs_that_end_at_the_cuts(lengths):
-    # runs of equal tokens that begin and end at, before and behind the borders of the wavefronts' and workgroups' shares
+    # runs of equal tokens that begin and end at, before and behind the borders of the wavefronts' (8 or 32 slots) and
+    # workgroups' (64 or 256) shares
     t = np.repeat(np.arange(len(lengths)) * 2, lengths)
     rng = np.random.default_rng(len(lengths))
     t = t[rng.permutation(t.size)]
-    _embed(t, 2 * len(lengths) + 1, 520, BF, BF, 1.0, seed=9)
+    _embed(t, 2 * len(lengths) + 1, 520 if t.size < 20000 else 72, BF, BF, 1.0, seed=9)
 
 
 def test_embedding_captions_of_a_contrastive_batch():
@@ -196,7 +202,7 @@ def test_embedding_rows_past_32_bits():
     for i, r in enumerate(rows):
         w[r] = i + 1
     w.requires_grad_()
-    for n in (len(rows), 2000):
+    for n in (len(rows), 2000, 10000):
         t = torch.tensor(rows, device="cuda").repeat(-(-n // len(rows)))[:n]
         y = ag.embedding(t, w, 2.0)
         assert torch.equal(y[:5, ::300].float(), torch.tensor([[2.0, 4, 6, 8, 10]], device="cuda").t().expand(5, 4))
@@ -412,9 +418,13 @@ def _linear_check(M, N, K, fmt, bias, seed=0):
     return y
 
 
+# straight from memory (up to 16 rows, 32 with a short K); tiles of 64 x 64 with one group over K and two (K of 1024 on), of
+# 128 x 64, of 128 x 128, of 256 x 256 (rows of y that are whole cache lines, and others; one and several tiles a workgroup; one
+# step of K); K that ends inside a step
 LINEAR = [(1, 8, 16), (1, 2304, 768), (1, 6144, 4096), (2, 24, 48), (15, 1000, 272), (16, 16, 128), (17, 520, 144), (31, 72, 1040), (32, 64, 64),
-          (33, 64, 80), (63, 136, 112), (64, 64, 4112), (65, 72, 64), (100, 1000, 1280), (785, 768, 768), (1570, 1000, 1280), (2000, 2304, 784),
-          (129, 136, 32), (4096, 2048, 528), (20000, 520, 208), (12001, 1544, 96)]
+          (32, 64, 2064), (33, 64, 80), (63, 136, 112), (64, 64, 4112), (65, 72, 64), (100, 1000, 1280), (40, 72, 1024), (785, 768, 768),
+          (785, 2304, 784), (1570, 1000, 1280), (2000, 2304, 784), (129, 136, 32), (4096, 2048, 528), (20000, 520, 208), (12001, 1544, 96),
+          (40001, 264, 128), (9000, 2304, 400), (36864, 256, 272), (12001, 4096, 112)]
 
 
 @pytest.mark.parametrize("M,N,K", LINEAR)
@@ -423,7 +433,7 @@ def test_linear_shapes(M, N, K, fmt, bias):
     _linear_check(M, N, K, fmt, bias, seed=M + N)
 
 
-@pytest.mark.parametrize("M,N", [(1, 136), (40, 136), (700, 1032), (30000, 264)])
+@pytest.mark.parametrize("M,N", [(1, 136), (40, 136), (700, 1032), (3000, 1032), (30000, 264), (40000, 320), (20000, 832)])
 def test_linear_leaves_what_is_not_its_own(M, N):
     # y lies between guards; the operands' neighbours are NaNs
     import torch
@@ -653,7 +663,7 @@ def test_captured_and_replayed():
         return [y.detach(), s.detach(), *[t.detach() for t in g], o]
     side = torch.cuda.Stream()
     graphs = []
-    for shape in ((4, 40), (30, 77)):      # gradient of few and of many slots
+    for shape in ((4, 40), (30, 77), (120, 77)):      # gradient of few, of more and of many slots
         t, dy = torch.zeros(shape, dtype=torch.int64, device="cuda"), torch.zeros((*shape, 128), dtype=torch.bfloat16, device="cuda")
         side.wait_stream(torch.cuda.current_stream())
         with torch.cuda.stream(side):
