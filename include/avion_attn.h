@@ -296,7 +296,7 @@ int avion_column_sum(const void *x, void *sum, long long M, int F, unsigned flag
  *   table  : in,  [V, D]; dtable: out, same shape and format, fully overwritten (rows that no token names: zeros).  The format
  *            of y, or fp32 with AVION_FLAG_WIDE_F32
  *   y, dy  : [n, D] bf16 (fp16 with AVION_FLAG_F16)
- *   n >= 0; V >= 1; scale finite; D a multiple of 8 up to 65536, n and V up to 2^28, n * D up to 2^37
+ *   n >= 0; V >= 1; scale finite; D a multiple of 8 up to 65536, n and V up to 2^28, n * D up to 2^36
  *   workspace (backward): 256-byte aligned, avion_embedding_bwd_workspace_bytes(n, V, D) bytes, contents ignored and left
  *   unspecified; calls that overlap in time must not share one
  * The gradient sorts the slots by token and sums each token's rows in fp32 in a fixed order, rounded once: no atomics on
@@ -362,7 +362,7 @@ int avion_quantize_rows(const void *x, void *x8, float *scale, long long M, int 
  *   x8 : in, [M, K] e4m3 with fp32 x_scale [M];   w8 : in, [N, K] e4m3 (one row per output) with fp32 w_scale [N]
  *   bias : in, fp32 [N] or NULL;   y : out, [M, N] bf16 (fp16 with AVION_FLAG_F16), fully overwritten
  *   M >= 0 (0: nothing happens); N a multiple of 8 up to 2^20; K a multiple of 16 up to 65536; M below 2^31 - 256 and at most
- *   2^24 tiles of 64 x 64 in y; pointers 16-byte aligned
+ *   2^24 tiles of 64 x 64 in y; pointers 16-byte aligned, x_scale's 4-byte (rows of a larger tensor)
  * fp32 sums, scaled and rounded once.  The matrix unit first adds 8 products of neighbouring k, dropping of each what lies
  * below 2^-13 of the largest one's power of two (measured; 2^-5 and more separate the operands from what they were rounded
  * from).  No workspace; bit-reproducible.

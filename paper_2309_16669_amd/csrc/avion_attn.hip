@@ -711,14 +711,14 @@ struct Planes {
 
 extern "C" {
 
-int avion_version(void) { return 20200; }  // 2.2.0
+int avion_version(void) { return 20300; }  // 2.3.0
 
 const char* avion_strerror(int code)
 {
     switch (code) {
         case AVION_OK: return "ok";
-        case AVION_EINVAL: return "invalid argument (null pointer, B/H/N < 1, or scale not finite or below 2^-60)";
-        case AVION_EUNSUPPORTED: return "unsupported shape or alignment (d must be 64 or 80; pointers 16-byte aligned)";
+        case AVION_EINVAL: return "invalid argument (null pointer, size or flag that does not exist, scale or eps out of range)";
+        case AVION_EUNSUPPORTED: return "unsupported shape or alignment (attention: d must be 64 or 80; pointers 16-byte aligned; limits of the entry point)";
         case AVION_EWORKSPACE: return "workspace missing, misaligned or too small";
         case AVION_EHIP: return "HIP runtime error (see avion_last_hip_error)";
         case AVION_ESCRATCH: return "problem needs more than the 32 MiB built-in scratch of avion_attn_bwd_noalloc";

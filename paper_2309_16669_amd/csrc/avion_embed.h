@@ -428,25 +428,25 @@ template <int PER, typename E, typename TE>
 __global__ void __launch_bounds__(kEmbSumWaves * 64)
 avion_embedding_sum_kernel(const unsigned* __restrict__ keys, const unsigned* __restrict__ slots, const raw16* __restrict__ dy,
                            void* __restrict__ dtable, float* __restrict__ heads, float* __restrict__ tails, long n, int V, int D,
-                           float scale, int nchunks, const unsigned* __restrict__ stamp, int rows)
+                           float scale, int nchunks, int ncol, const unsigned* __restrict__ stamp, int rows)
 {
     constexpr int WAVES = kEmbSumWaves, FLY = PER < 16 ? PER : 16;
-    if ((int)blockIdx.x >= nchunks) {  // (few slots: the table is cleared here)
-        const long r0 = (long)((int)blockIdx.x - nchunks) * rows;
-        if (blockIdx.y == 0)
-            emb_clear<TE, WAVES>(dtable, r0, V - r0 < rows ? V - r0 : rows, D, [&](long r) {
-                const unsigned s = stamp[r];
-                return s < n && keys[s] == (unsigned)r;
-            });
+    const int sums = nchunks * ncol, chunk = blockIdx.x / ncol, block = blockIdx.x - chunk * ncol;
+    if ((int)blockIdx.x >= sums) {  // (few slots: the table is cleared here)
+        const long r0 = (long)((int)blockIdx.x - sums) * rows;
+        emb_clear<TE, WAVES>(dtable, r0, V - r0 < rows ? V - r0 : rows, D, [&](long r) {
+            const unsigned s = stamp[r];
+            return s < n && keys[s] == (unsigned)r;
+        });
         return;
     }
     __shared__ float sh_head[WAVES][kEmbCols], sh_tail[WAVES][kEmbCols];
     __shared__ unsigned sh_key[WAVES];  // of the tail
     __shared__ int sh_what[WAVES];      // 1: has a head, 2: the head ends here, 4: has a tail
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
-    const int col = blockIdx.y * kEmbCols + lane * 8, read_col = col < D ? col : 0;
+    const int col = block * kEmbCols + lane * 8, read_col = col < D ? col : 0;
     const bool in = col < D;
-    const long first = ((long)blockIdx.x * WAVES + wave) * PER;
+    const long first = ((long)chunk * WAVES + wave) * PER;
     const int count = first >= n ? 0 : n - first < PER ? (int)(n - first) : PER;
     const unsigned none = (unsigned)V;
     // lane l: key and slot of sorted place first + l, lane `count`: the key behind, lane 63: the key before.  (A key is at most
@@ -518,7 +518,7 @@ avion_embedding_sum_kernel(const unsigned* __restrict__ keys, const unsigned* __
                     for (int e = 0; e < 8; ++e) o[e] = run[e] * scale;
                     emb_store8<TE>(dtable, (long)run_key * D + col, o);
                 } else {
-                    store8(heads + (long)blockIdx.x * D + col, run);
+                    store8(heads + (long)chunk * D + col, run);
                 }
                 running = began_here = false;
 #pragma unroll
@@ -532,7 +532,7 @@ avion_embedding_sum_kernel(const unsigned* __restrict__ keys, const unsigned* __
             run_key = sh_key[w];
         }
     }
-    if (running) store8((began_here ? tails : heads) + (long)blockIdx.x * D + col, run);
+    if (running) store8((began_here ? tails : heads) + (long)chunk * D + col, run);
 }
 
 // The tokens that span chunks: the workgroup of the chunk where one begins adds its tail and the heads behind it, in a fixed

@@ -29,9 +29,9 @@ int launch_fp8(const char* x8, const float* xs, const char* w8, const float* ws,
                hipStream_t st)
 {
     using Cfg = Fp8Cfg<TM, TN, WM, WN, ST, KG>;
-    static std::atomic<bool> lds_allowed{false};
+    static std::atomic<unsigned long long> lds_allowed{0};
     const auto kernel = avion_linear_fp8_kernel<TM, TN, WM, WN, ST, KG, E>;
-    const hipError_t attr = allow_lds(kernel, Cfg::LDS_BYTES, lds_allowed);
+    const hipError_t attr = allow_lds_here(kernel, Cfg::LDS_BYTES, lds_allowed);
     if (attr != hipSuccess) return hip_fail(attr, "hipFuncSetAttribute(linear_fp8)");
     const long long tiles = fp8_tiles(M, N, TM, TN);
     const unsigned grid = (unsigned)((tiles + 7) / 8 * 8);
@@ -60,9 +60,9 @@ template <typename E, bool STREAM>
 int launch_wide(const char* x8, const float* xs, const char* w8, const float* ws, const float* bias, raw16* y, int M, int N, int K,
                 hipStream_t st)
 {
-    static std::atomic<bool> lds_allowed{false};
+    static std::atomic<unsigned long long> lds_allowed{0};
     const auto kernel = avion_linear_fp8_wide_kernel<E, STREAM>;
-    const hipError_t attr = allow_lds(kernel, kWideLds, lds_allowed);
+    const hipError_t attr = allow_lds_here(kernel, kWideLds, lds_allowed);
     if (attr != hipSuccess) return hip_fail(attr, "hipFuncSetAttribute(linear_fp8_wide)");
     const int ntm = (M + kWideM - 1) / kWideM, ntn = (N + kWideN - 1) / kWideN;
     const unsigned grid = (unsigned)std::min<long long>(kComputeUnits, ((long long)ntm * ntn + 7) / 8 * 8);
@@ -83,9 +83,10 @@ int avion_linear_fp8(const void* x8, const float* x_scale, const void* w8, const
     if (fp8_tiles((int)M, N, 64, 64) > (1LL << 24)) return AVION_EUNSUPPORTED;  // workgroups of a launch
     if (M == 0) return AVION_OK;
     if (!x8 || !x_scale || !w8 || !w_scale || !y) return AVION_EINVAL;
-    const void* ptrs[] = {x8, x_scale, w8, w_scale, bias, y};
+    const void* ptrs[] = {x8, w8, w_scale, bias, y};
     for (const void* p : ptrs)
         if (!aligned16(p)) return AVION_EUNSUPPORTED;
+    if (reinterpret_cast<uintptr_t>(x_scale) % 4 != 0) return AVION_EUNSUPPORTED;
     hipStream_t st = static_cast<hipStream_t>(stream);
     const char *x = static_cast<const char*>(x8), *w = static_cast<const char*>(w8);
     raw16* out = static_cast<raw16*>(y);

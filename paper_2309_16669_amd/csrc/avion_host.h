@@ -39,6 +39,20 @@ hipError_t allow_lds(K kernel, int bytes, std::atomic<bool>& done)
     return e;
 }
 
+// The same, remembered for each GPU (bit = device number; beyond 64 of them each call asks again).
+template <typename K>
+hipError_t allow_lds_here(K kernel, int bytes, std::atomic<unsigned long long>& done)
+{
+    int dev = -1;
+    hipError_t e = hipGetDevice(&dev);
+    if (e != hipSuccess) return e;
+    const unsigned long long bit = dev >= 0 && dev < 64 ? 1ull << dev : 0;
+    if (done.load(std::memory_order_acquire) & bit) return hipSuccess;
+    e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    if (e == hipSuccess) done.fetch_or(bit, std::memory_order_release);
+    return e;
+}
+
 // Result of the launch just made on this thread.  Errors left behind by earlier, unrelated work of
 // the caller are cleared before the launch (begin_launch) so that they are not mistaken for it.
 [[maybe_unused]] void begin_launch() { (void)hipGetLastError(); }

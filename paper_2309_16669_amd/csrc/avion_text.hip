@@ -102,7 +102,7 @@ int embedding_check(long long n, long long V, int D, unsigned flags)
     if (n < 0 || V < 1 || D < 1) return AVION_EINVAL;
     if (flags & ~kEmbFlags) return AVION_EINVAL;
     if (D % 8 != 0 || D > kEmbMaxD || V > kEmbMax || n > kEmbMax) return AVION_EUNSUPPORTED;
-    if (n * (D / 8) > (1LL << 34)) return AVION_EUNSUPPORTED;  // workgroups of the lookup
+    if (n * (D / 8) > (1LL << 33)) return AVION_EUNSUPPORTED;  // threads of the lookup: below 2^32
     return AVION_OK;
 }
 // f(token type, table's format, output's format)
@@ -359,9 +359,9 @@ int avion_embedding_bwd(const void* tokens, const void* dy, void* dtable, long l
         auto sums = [&](auto per) {
             const unsigned clearing = ranked ? (unsigned)((V + rows - 1) / rows) : 0u;
             begin_launch();
-            hipLaunchKernelGGL((avion_embedding_sum_kernel<decltype(per)::value, E, TE>), dim3((unsigned)p.nchunks + clearing, ncol),
+            hipLaunchKernelGGL((avion_embedding_sum_kernel<decltype(per)::value, E, TE>), dim3((unsigned)p.nchunks * ncol + clearing),
                                dim3(kEmbSumWaves * 64), 0, st, keys[last], slots[last], g, dtable, heads, tails, (long)n, (int)V, D, scale,
-                               (int)p.nchunks, stamp, rows);
+                               (int)p.nchunks, ncol, stamp, rows);
             return end_launch("launch avion_embedding_sum_kernel");
         };
         const int rs = n < kEmbSumEnough ? sums(Int<kEmbSumFew>{}) : sums(Int<kEmbSumMost>{});

@@ -44,7 +44,7 @@ CASES = [
                       (dict(V=0), av.EINVAL), (dict(D=0), av.EINVAL), (dict(scale=NAN), av.EINVAL), (dict(scale=INF), av.EINVAL),
                       (dict(flags=2), av.EINVAL), (dict(flags=32), av.EINVAL), (dict(D=60), av.EUNSUPPORTED),
                       (dict(D=65536 + 8), av.EUNSUPPORTED), (dict(V=(1 << 28) + 1), av.EUNSUPPORTED),
-                      (dict(n=(1 << 28) + 1), av.EUNSUPPORTED), (dict(n=1 << 28, D=1032), av.EUNSUPPORTED), (dict(table=P + 8), av.EUNSUPPORTED),
+                      (dict(n=(1 << 28) + 1), av.EUNSUPPORTED), (dict(n=1 << 28, D=264), av.EUNSUPPORTED), (dict(table=P + 8), av.EUNSUPPORTED),
                       (dict(y=P + 2), av.EUNSUPPORTED), (dict(tokens=P + 4), av.EUNSUPPORTED),
                       (dict(tokens=P + 2, flags=av.FLAG_TOKENS_I32), av.EUNSUPPORTED), (dict(n=0, tokens=None, y=None), av.OK)]),
     (_embedding_bwd, [(dict(tokens=None), av.EINVAL), (dict(dy=None), av.EINVAL), (dict(dtable=None), av.EINVAL), (dict(n=-1), av.EINVAL),
@@ -70,7 +70,8 @@ CASES = [
     (_linear, [(dict(x8=None), av.EINVAL), (dict(xs=None), av.EINVAL), (dict(w8=None), av.EINVAL), (dict(ws=None), av.EINVAL),
                (dict(y=None), av.EINVAL), (dict(M=-1), av.EINVAL), (dict(N=0), av.EINVAL), (dict(K=0), av.EINVAL), (dict(flags=2), av.EINVAL),
                (dict(N=60), av.EUNSUPPORTED), (dict(K=24), av.EUNSUPPORTED), (dict(K=65536 + 16), av.EUNSUPPORTED),
-               (dict(N=(1 << 20) + 8), av.EUNSUPPORTED), (dict(M=1 << 31), av.EUNSUPPORTED), (dict(bias=P + 8), av.EUNSUPPORTED), (dict(x8=P + 8), av.EUNSUPPORTED),
+               (dict(N=(1 << 20) + 8), av.EUNSUPPORTED), (dict(M=1 << 31), av.EUNSUPPORTED), (dict(bias=P + 8), av.EUNSUPPORTED), (dict(x8=P + 8), av.EUNSUPPORTED), (dict(xs=P + 2), av.EUNSUPPORTED),
+               (dict(ws=P + 4), av.EUNSUPPORTED),
                (dict(M=0, x8=None, y=None), av.OK)]),
 ]
 

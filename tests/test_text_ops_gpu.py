@@ -165,6 +165,13 @@ def test_embedding_captions_of_a_contrastive_batch():
     assert torch.equal(y, y2) and torch.equal(dw, dw2)
 
 
+def test_embedding_wide_rows():
+    # several blocks of columns beside a table that is mostly cleared, on every way of sorting
+    rng = np.random.default_rng(1)
+    for n in (300, 2000, 9000):
+        _embed(rng.integers(0, 700, size=n), 700, 4104, BF, BF, 1.0, seed=n)
+
+
 def test_embedding_strides_empty_and_tied_gradients():
     import torch
     from paper_2309_16669_amd import autograd as ag
@@ -487,6 +494,11 @@ def test_linear_strides_and_empty():
     y = ag.linear_fp8(x8.transpose(0, 1), xs.t(), w8, ws, b)
     assert torch.equal(y, ag.linear_fp8(x8, xs, w8, ws, b.contiguous()).transpose(0, 1))
     assert ag.linear_fp8(x8[:, :0], xs[:, :0], w8, ws).shape == (4, 0, 24)
+    v8, vs = ag.quantize_rows(randn(4, (40001, 64), BF))    # rows of a larger tensor: scales at any place
+    y = ag.linear_fp8(v8, vs, w8, ws)
+    for rows in (slice(1, 10), slice(3, 90), slice(1, 1000), slice(2, 40001)):
+        assert torch.equal(ag.linear_fp8(v8[rows], vs[rows], w8, ws), y[rows])
+    assert torch.equal(ag.linear_fp8(v8[5], vs[5], w8, ws), y[5])
     assert ag.quantize_rows(x8[:, :0].to(torch.bfloat16))[1].shape == (4, 0)
     y8, s, h = ag.add_rms_norm_fp8(torch.empty((0, 64), dtype=torch.bfloat16, device="cuda"), torch.empty((0, 64), device="cuda"), torch.ones(64, device="cuda"))
     assert y8.shape == (0, 64) and s.shape == (0,) and h.dtype == torch.float32
