@@ -83,6 +83,27 @@ DEVINL u32x2 pack_fp8(const float (&v)[8])
     return w;
 }
 
+// 448 / big as the sum of two fp32 (`lo` corrects the quotient's rounding): a row's values are scaled by it to within half a
+// step of fp32 before they are rounded to 8 bits, so that hardly one lands on the other side of a border than in exact
+// arithmetic.  Not finite: `lo` is left out.
+struct F8Factor {
+    float hi, lo;
+    DEVINL explicit F8Factor(float big)
+    {
+        hi = kF8Max / big;
+        const float l = fmaf(-hi, big, kF8Max) / big;
+        lo = fabsf(l) < hi ? l : 0.f;
+    }
+    DEVINL F8Factor(float h, float l) : hi(h), lo(l) {}
+    DEVINL float times(float v) const { return fmaf(v, hi, v * lo); }
+    // (a * b) times this, the product's rounding corrected too
+    DEVINL float times(float a, float b) const
+    {
+        const float t = a * b, e = fmaf(a, b, -t);
+        return fmaf(t, hi, fmaf(t, lo, e * hi));
+    }
+};
+
 // A lane's share of a row: NCH chunks of 8 elements, 16-bit (E) or fp32
 // LAST: nobody reads it again (all inputs of the backward).  Read past the caches, backward of 157696 x 512 142 -> 112 us; the
 // forward, whose inputs are as dead, takes 101 or 121 then instead of 107, by turns, and reads them as usual.
@@ -242,10 +263,15 @@ avion_rmsnorm_fwd_kernel(const raw16* __restrict__ x, const void* __restrict__ r
         }
         row_reduce<LANES, F8>(ss, big, sh, wave, lane, turn);
         const float rs = __builtin_amdgcn_rsqf(fmaf(ss, inv_d, eps));
-        float inv = rs;
+        // 8 bits: y / scale = h w 448 / max|h w|, in which rstd has gone (unless the row is so small that the least scale holds)
+        F8Factor to8(0.f, 0.f);
         if (F8) {
-            big = fmaxf(big * rs, kF8Least);
-            inv = kF8Max / big;
+            to8 = F8Factor(big);
+            big *= rs;
+            if (!(big >= kF8Least)) {
+                big = kF8Least;
+                to8 = F8Factor(rs * (kF8Max / kF8Least), 0.f);
+            }
         }
 #pragma unroll
         for (int j = 0; j < NCH; ++j) {
@@ -253,13 +279,13 @@ avion_rmsnorm_fwd_kernel(const raw16* __restrict__ x, const void* __restrict__ r
             if (ch < chunks) {
                 if (residual) RmsRow<NCH, LANES, R>::store(h, n, D, ch, v[j]);
                 float o[8];
-#pragma unroll
-                for (int e = 0; e < 8; ++e) o[e] = v[j][e] * rs * gain[j][e];
                 if constexpr (F8) {
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) o[e] *= inv;
+                    for (int e = 0; e < 8; ++e) o[e] = to8.times(v[j][e], gain[j][e]);
                     *reinterpret_cast<u32x2*>(static_cast<char*>(y) + n * D + ch * 8) = pack_fp8(o);
                 } else {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) o[e] = v[j][e] * rs * gain[j][e];
                     RmsRow<NCH, LANES, E>::store(y, n, D, ch, o);
                 }
             }
@@ -308,14 +334,14 @@ avion_quantize_rows_kernel(const raw16* __restrict__ x, void* __restrict__ y, fl
             for (int e = 0; e < 8; ++e) big = fmaxf(big, fabsf(xr.get(j, e)));
         row_reduce<LANES, true>(none, big, sh, wave, lane, turn);
         big = fmaxf(big, kF8Least);
-        const float inv = kF8Max / big;
+        const F8Factor to8(big);
 #pragma unroll
         for (int j = 0; j < NCH; ++j) {
             const int ch = at + LANES * j;
             if (ch < chunks) {
                 float o[8];
 #pragma unroll
-                for (int e = 0; e < 8; ++e) o[e] = xr.get(j, e) * inv;
+                for (int e = 0; e < 8; ++e) o[e] = to8.times(xr.get(j, e));
                 *reinterpret_cast<u32x2*>(static_cast<char*>(y) + n * D + ch * 8) = pack_fp8(o);
             }
         }
