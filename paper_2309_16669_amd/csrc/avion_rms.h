@@ -94,7 +94,6 @@ struct F8Factor {
         const float l = fmaf(-hi, big, kF8Max) / big;
         lo = fabsf(l) < hi ? l : 0.f;
     }
-    DEVINL F8Factor(float h, float l) : hi(h), lo(l) {}
     DEVINL float times(float v) const { return fmaf(v, hi, v * lo); }
     // (a * b) times this, the product's rounding corrected too
     DEVINL float times(float a, float b) const
@@ -263,16 +262,12 @@ avion_rmsnorm_fwd_kernel(const raw16* __restrict__ x, const void* __restrict__ r
         }
         row_reduce<LANES, F8>(ss, big, sh, wave, lane, turn);
         const float rs = __builtin_amdgcn_rsqf(fmaf(ss, inv_d, eps));
-        // 8 bits: y / scale = h w 448 / max|h w|, in which rstd has gone (unless the row is so small that the least scale holds)
-        F8Factor to8(0.f, 0.f);
-        if (F8) {
-            to8 = F8Factor(big);
-            big *= rs;
-            if (!(big >= kF8Least)) {
-                big = kF8Least;
-                to8 = F8Factor(rs * (kF8Max / kF8Least), 0.f);
-            }
-        }
+        // 8 bits: y / scale = h w 448 / max|h w|, in which rstd has gone; it stays where the least scale holds, where max|h w|
+        // is too small to divide by (with an eps below 1e-14), and where something is not finite
+        const float big_y = big * rs;
+        const bool gone = big >= 0x1p-90f && big_y >= kF8Least;
+        const float up = gone ? 1.f : rs;
+        const F8Factor to8(gone ? big : fmaxf(big_y, kF8Least));
 #pragma unroll
         for (int j = 0; j < NCH; ++j) {
             const int ch = at + LANES * j;
@@ -281,7 +276,7 @@ avion_rmsnorm_fwd_kernel(const raw16* __restrict__ x, const void* __restrict__ r
                 float o[8];
                 if constexpr (F8) {
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) o[e] = to8.times(v[j][e], gain[j][e]);
+                    for (int e = 0; e < 8; ++e) o[e] = to8.times(v[j][e] * up, gain[j][e]);
                     *reinterpret_cast<u32x2*>(static_cast<char*>(y) + n * D + ch * 8) = pack_fp8(o);
                 } else {
 #pragma unroll
@@ -291,7 +286,7 @@ avion_rmsnorm_fwd_kernel(const raw16* __restrict__ x, const void* __restrict__ r
             }
         }
         if (at == 0 && n < M) {
-            if (F8) scale[n] = big * (1.0f / kF8Max);
+            if (F8) scale[n] = fmaxf(big_y, kF8Least) * (1.0f / kF8Max);
             if (rstd) rstd[n] = rs;
         }
     };

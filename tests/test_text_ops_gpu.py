@@ -399,6 +399,21 @@ def test_rows_in_8_bits(M, D, fmt, stream):
     _rows8_check(ops.rms_fwd(h, f64(w), 1e-6)[0], q, s, (D / 2 + 20) * E)
 
 
+@pytest.mark.parametrize("D", [64, 4096])
+def test_rows_in_8_bits_small_values_and_small_eps(D):
+    """Values whose products with the gains lie near the least fp32 number, under an eps that leaves the norm of them at 1; and
+    zeros under it, which stay zeros."""
+    import torch
+    from paper_2309_16669_amd import autograd as ag
+    x, r, w = torch.zeros((3, D), dtype=torch.bfloat16, device="cuda"), 1e-16 * randn(1, (3, D), FP), 1e-21 * (1 + 0.1 * randn(2, (D,), FP))
+    q, s, h = ag.add_rms_norm_fp8(x, r, w, 0.0)
+    assert torch.equal(h, r)
+    _rows8_check(ops.rms_fwd(f64(r), f64(w), 0.0)[0], q, s, (D / 2 + 20) * E)
+    for eps in (1e-20, 1e-36):
+        q, s = ag.rms_norm_fp8(x, 1e21 * w, eps)
+        assert not q.float().any() and abs(float(s[0]) - 2.0 ** -96 / 448) <= 2 * E * 2.0 ** -96 / 448
+
+
 def _group_max(t):
     t = np.abs(f64(t.float()))
     t = np.pad(t, ((0, 0), (0, -t.shape[1] % 8)))
