@@ -26,8 +26,9 @@ DEVINL f32x4 mfma8_16(i32x8 a, i32x8 b, f32x4 c) { return __builtin_amdgcn_mfma_
 
 // ------------------------------------------------------------------------------------- few rows
 // Bound by the weights' bytes (one token: N K bytes for 2 N K operations) or by latency.  A workgroup takes 16 rows of w8 and
-// all rows of x8 (MT tiles of 16); its four wavefronts take every fourth 128-byte step of K, eight or four steps in flight, straight
-// from memory into the operands, and add their sums through LDS in a fixed order.
+// all rows of x8 (MT tiles of 16); its eight wavefronts take every eighth 128-byte step of K, four steps in flight each, straight
+// from memory into the operands (nothing is read twice by a workgroup, so LDS has nothing to give), and add their sums through
+// LDS in a fixed order.  1 x 6144 x 4096: 8.0 us, 3.1 TB/s of w8 (25 MB: a launch this short does not reach the copy's 5.2).
 constexpr int kFewWaves = 8;
 template <int MT, typename E>
 __global__ void __launch_bounds__(kFewWaves * 64)
@@ -115,6 +116,9 @@ DEVINL void fp8_landed_barrier()
 {
     asm volatile("s_waitcnt vmcnt(%0)\n\ts_waitcnt lgkmcnt(0)\n\ts_barrier" ::"i"(LOADS) : "memory");
 }
+
+// This wavefront's reads of LDS are done, and so are everybody's.
+DEVINL void read_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 
 template <int TM, int TN, int WM, int WN, int ST, int KG, typename E>
 __global__ void __launch_bounds__(WM* WN* KG * 64, KG > 1 ? 1 : 2)
@@ -287,13 +291,20 @@ avion_linear_fp8_kernel(const char* __restrict__ x8, const float* __restrict__ x
 //   share stays in its L2.
 //   Waits: a step's loads are awaited with everything older; stores of a tile are younger than the loads that the next tile's
 //   first step awaits, so that wait leaves them (kWideStores of them, all issued always) on their way.
+//   AHEAD, for long K: w8's half of a buffer, whose rows are all in registers from the middle of a step on, is filled again from
+//   there, behind a barrier of its own.  50176 x 1024 x 4096 220 -> 202 us, 50176 x 768 x 2304 99 -> 92, 8192 cubed 434 -> 416;
+//   with fewer steps a tile it gives nothing or costs: 25088 x 2048 x 1536 89 and 90, 12544 x 4096 x 1024 65 and 68.
+// Bound by the loads of one step, which is all that two buffers of 64 KB leave in flight: on 50176 x 2304 x 768 (88 to 96 us, 1.9
+// PFLOP/s and 2.9 TB/s of its bytes) the matrix units work 35 % of the cycles and LDS answers reads in 23 %; without loads it
+// takes 80 us, without contractions 69, without stores 7 less.  8192 cubed: 2.64 PFLOP/s.
 constexpr int kWideM = 256, kWideN = 256, kWideK = 128, kWideWaves = 8, kWideGroup = 8;
 constexpr int kWideStage = (kWideM + kWideN) * kWideK, kWideScales = 3 * 1024, kWideRow = 144;
 constexpr int kWideLds = 2 * kWideStage + 3 * kWideScales + kWideWaves * 16 * kWideRow;
 constexpr int kWideStores = 16;
+constexpr int kWideAhead = 2048;  // AHEAD from this K on
 constexpr int kNontemporal = 2;  // of a buffer access's cache policy
 
-template <typename E, bool STREAM>
+template <typename E, bool STREAM, bool AHEAD>
 __global__ void __launch_bounds__(kWideWaves * 64)
 avion_linear_fp8_wide_kernel(const char* __restrict__ x8, const float* __restrict__ x_scale, const char* __restrict__ w8,
                              const float* __restrict__ w_scale, const float* __restrict__ bias, raw16* __restrict__ y, int M, int N,
@@ -323,7 +334,7 @@ avion_linear_fp8_wide_kernel(const char* __restrict__ x8, const float* __restric
     const unsigned ch = ((lane & 7) ^ (lane >> 4 & 3) ^ (wave & 1) * 4) * 16, row_at = (unsigned)(wave * 8 + lane / 8) * (unsigned)K + ch;
     int f_tile = first, f_step = 0, f_buf = 0, f_scales = 0;
     RawBuffer xb(x8, 0), wb(w8, 0);
-    auto fetch = [&] {
+    auto fetch_tile = [&] {  // before a step's loads: the next tile, if this is its first step
         if (f_step == 0) {
             int m0, n0;
             place(f_tile, m0, n0);
@@ -336,10 +347,16 @@ avion_linear_fp8_wide_kernel(const char* __restrict__ x8, const float* __restric
             if (wave == 1) load_to_lds16(RawBuffer(w_scale + n0, rows_n * 4), into + 1024, lane * 16);
             if (wave == 2 && bias) load_to_lds16(RawBuffer(bias + n0, rows_n * 4), into + 2048, lane * 16);
         }
+    };
+    auto fetch_half = [&](const RawBuffer& buffer, unsigned to) {
         const unsigned k = (unsigned)f_step * kWideK, v = k + ch < (unsigned)K ? row_at + k : kOutOfRangeBase;
-        const unsigned down = 8 * kWideWaves * (unsigned)K, to = lds + f_buf * kWideStage + wave * 1024;
-        load_to_lds16_x4<kWideWaves * 1024>(xb, xb, xb, xb, to, v, v + down, v + 2 * down, v + 3 * down);
-        load_to_lds16_x4<kWideWaves * 1024>(wb, wb, wb, wb, to + kWideM * kWideK, v, v + down, v + 2 * down, v + 3 * down);
+        const unsigned down = 8 * kWideWaves * (unsigned)K;
+        load_to_lds16_x4<kWideWaves * 1024>(buffer, buffer, buffer, buffer, lds + f_buf * kWideStage + to + wave * 1024, v, v + down,
+                                            v + 2 * down, v + 3 * down);
+    };
+    auto fetch_w = [&] { fetch_half(wb, kWideM * kWideK); };
+    auto fetch_x = [&] { fetch_half(xb, 0); };
+    auto fetched = [&] {
         f_buf ^= 1;
         if (++f_step == steps) {
             f_step = 0;
@@ -355,6 +372,12 @@ avion_linear_fp8_wide_kernel(const char* __restrict__ x8, const float* __restric
 
     f32x16 acc[MI][NI];
     i32x8 a[2][NI], b;
+    auto fetch = [&] {
+        fetch_tile();
+        fetch_x();
+        fetch_w();
+        fetched();
+    };
     fetch();
     if (total > 1) {
         fetch();
@@ -379,6 +402,11 @@ avion_linear_fp8_wide_kernel(const char* __restrict__ x8, const float* __restric
             for (int gr = 0; gr < 2 * MI; ++gr) {
                 const int i = gr % MI, half = gr / MI;
                 i32x8 b_next = b;
+                if (AHEAD && gr == MI + 1 && q + 2 < total) {
+                    read_barrier();  // w8's rows of this step are in everybody's registers
+                    fetch_tile();
+                    fetch_w();
+                }
                 if (i + 1 < MI) {
                     b_next = read(b0 + at + (i + 1) * 32 * kWideK, half * 64);
                 } else if (half == 0) {
@@ -386,8 +414,14 @@ avion_linear_fp8_wide_kernel(const char* __restrict__ x8, const float* __restric
                     for (int j = 0; j < NI; ++j) a[1][j] = read(a0 + at + j * 32 * kWideK, 64);
                     b_next = read(b0 + at, 64);
                 } else if (q + 1 < total) {
-                    if (s == 0 && q > 0) fp8_landed_barrier<kWideStores>();
-                    else fp8_landed_barrier<0>();
+                    const bool after = s == 0 && q > 0;  // a tile's stores
+                    if (AHEAD && q + 2 < total) {
+                        if (after) fp8_landed_barrier<kWideStores + LOADS / 2>();
+                        else fp8_landed_barrier<LOADS / 2>();
+                    } else {
+                        if (after) fp8_landed_barrier<kWideStores>();
+                        else fp8_landed_barrier<0>();
+                    }
 #pragma unroll
                     for (int j = 0; j < NI; ++j) a[0][j] = read(a0 + next + j * 32 * kWideK, 0);
                     b_next = read(b0 + next, 0);
@@ -398,7 +432,12 @@ avion_linear_fp8_wide_kernel(const char* __restrict__ x8, const float* __restric
                 __builtin_amdgcn_sched_barrier(0);
                 b = b_next;
             }
-            if (q + 2 < total) fetch();
+            if (q + 2 < total) {
+                if (!AHEAD) fetch_tile();
+                fetch_x();
+                if (!AHEAD) fetch_w();
+                fetched();
+            }
             buf ^= 1;
         }
 

@@ -56,12 +56,12 @@ bool fp8_wide(int M, int N)
     const long long tiles = fp8_tiles(M, N, kWideM, kWideN), rounds = (tiles + kComputeUnits - 1) / kComputeUnits;
     return 5 * (tiles + 64) >= 4 * kComputeUnits * rounds;
 }
-template <typename E, bool STREAM>
-int launch_wide(const char* x8, const float* xs, const char* w8, const float* ws, const float* bias, raw16* y, int M, int N, int K,
-                hipStream_t st)
+template <typename E, bool STREAM, bool AHEAD>
+int launch_wide_by(const char* x8, const float* xs, const char* w8, const float* ws, const float* bias, raw16* y, int M, int N, int K,
+                   hipStream_t st)
 {
     static std::atomic<unsigned long long> lds_allowed{0};
-    const auto kernel = avion_linear_fp8_wide_kernel<E, STREAM>;
+    const auto kernel = avion_linear_fp8_wide_kernel<E, STREAM, AHEAD>;
     const hipError_t attr = allow_lds_here(kernel, kWideLds, lds_allowed);
     if (attr != hipSuccess) return hip_fail(attr, "hipFuncSetAttribute(linear_fp8_wide)");
     const int ntm = (M + kWideM - 1) / kWideM, ntn = (N + kWideN - 1) / kWideN;
@@ -69,6 +69,13 @@ int launch_wide(const char* x8, const float* xs, const char* w8, const float* ws
     begin_launch();
     hipLaunchKernelGGL(kernel, dim3(grid), dim3(kWideWaves * 64), kWideLds, st, x8, xs, w8, ws, bias, y, M, N, K, ntm, ntn);
     return end_launch("launch avion_linear_fp8_wide_kernel");
+}
+template <typename E, bool STREAM>
+int launch_wide(const char* x8, const float* xs, const char* w8, const float* ws, const float* bias, raw16* y, int M, int N, int K,
+                hipStream_t st)
+{
+    if (K >= kWideAhead) return launch_wide_by<E, STREAM, true>(x8, xs, w8, ws, bias, y, M, N, K, st);
+    return launch_wide_by<E, STREAM, false>(x8, xs, w8, ws, bias, y, M, N, K, st);
 }
 
 }  // namespace

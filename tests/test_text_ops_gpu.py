@@ -92,7 +92,7 @@ def _embed(tokens, V, D, table, out, scale, token_type="int64", seed=0):
     return y, dw
 
 
-# one launch (up to 512 slots), sorted by counting (up to 8192), by one, two and three digits; sums of 8 and (from 32768) of 32
+# one launch (up to 768 slots), sorted by counting (up to 8192), by one, two and three digits; sums of 8 and (from 32768) of 32
 # slots a wavefront; narrow, ragged and several blocks of columns
 SMALL = [(1, 1, 8), (1, 50000, 512), (7, 3, 64), (64, 64, 520), (77, 1000, 512), (500, 5, 72), (512, 3000, 776), (511, 1, 1032)]
 LARGE = [(513, 3, 64), (1025, 3000, 512), (5000, 1, 8), (2048, 1023, 776), (8192, 1024, 520), (8193, 200, 64), (9999, 256, 1032), (20000, 40000, 136),
@@ -104,6 +104,14 @@ LARGE = [(513, 3, 64), (1025, 3000, 512), (5000, 1, 8), (2048, 1023, 776), (8192
 def test_embedding_shapes(n, V, D, table, out):
     rng = np.random.default_rng(n + V + D)
     _embed(rng.integers(0, V, size=n), V, D, table, out, 1.5, "int32" if n % 2 else "int64", seed=n)
+
+
+@pytest.mark.parametrize("n", [700, 767, 768, 769])
+@pytest.mark.parametrize("V,D", [(1, 520), (5000, 136)])
+def test_embedding_around_one_launch(n, V, D):
+    tokens = np.random.default_rng(n).integers(0, V, size=n)
+    tokens[::3] = 0
+    _embed(tokens, V, D, BF, BF, 0.5, seed=n)
 
 
 @pytest.mark.parametrize("table,out", [(BF, BF), (HF, HF), (FP, BF), (FP, HF)])
@@ -267,6 +275,16 @@ NORM_SHAPES = [(1, 8), (1, 64), (3, 72), (4099, 128), (13, 136), (1001, 200), (2
 @pytest.mark.parametrize("fmt,stream", [(BF, BF), (HF, FP), (BF, None)])
 def test_norm_shapes(M, D, fmt, stream):
     _norm_check(M, D, fmt, stream, seed=M + D)
+
+
+@pytest.mark.parametrize("M", [511, 512, 513])    # a workgroup a row, and several rows
+@pytest.mark.parametrize("D", [520, 1024, 2048])
+def test_norm_around_a_workgroup_a_row(M, D):
+    from paper_2309_16669_amd import autograd as ag
+    _norm_check(M, D, BF, FP, seed=M + D)
+    x = randn(M, (M, D // 16 * 16), BF)
+    q, s = ag.quantize_rows(x)
+    _rows8_check(f64(x), q, s, 4 * E)
 
 
 @pytest.mark.parametrize("fmt,stream", [(BF, FP), (HF, HF), (HF, None)])
@@ -453,6 +471,15 @@ LINEAR = [(1, 8, 16), (1, 2304, 768), (1, 6144, 4096), (2, 24, 48), (15, 1000, 2
 @pytest.mark.parametrize("fmt,bias", [(BF, False), (HF, True)])
 def test_linear_shapes(M, N, K, fmt, bias):
     _linear_check(M, N, K, fmt, bias, seed=M + N)
+
+
+# tiles of 256 x 256 with a long K: one tile a workgroup and several, K that ends inside a step, rows of y that are whole cache
+# lines and others
+@pytest.mark.parametrize("M,N,K,fmt,bias", [(36001, 256, 2064, BF, False), (5900, 3800, 2048, HF, True), (23000, 1024, 2192, HF, False), (23000, 1032, 2304, BF, True)])
+def test_linear_many_rows_and_long_contractions(M, N, K, fmt, bias):
+    y = _linear_check(M, N, K, fmt, bias, seed=K)
+    import torch
+    assert torch.equal(y, _linear_check(M, N, K, fmt, bias, seed=K))
 
 
 @pytest.mark.parametrize("M,N", [(1, 136), (40, 136), (700, 1032), (3000, 1032), (30000, 264), (40000, 320), (20000, 832)])
