@@ -2,28 +2,37 @@
 //     y_i = s W[t_i];     dW[v] = s sum over i with t_i = v, in ascending i, of dy_i
 // A token outside [0, V) names no row: its y is zero and it adds to no gradient (padding, another device's share of a table).
 //
-// Lookup: bound by memory bandwidth, one read of a row and one write; a thread moves 16-byte pieces, several in flight.
+// Lookup: bound by memory bandwidth, one read of a row and one write; a thread moves 16-byte pieces, four in flight, and writes
+// past the caches (y is not read again before the next kernel, the table's rows are): 157696 x 512 from 50000 rows 49 -> 28.6 us,
+// 5.6 TB/s written.
 //
 // Gradient: reads dy once and writes every row of dW once (rows that no token names: zeros).  Floating-point sums in a fixed
 // order, no atomics on them: results are bit-reproducible.
 //   up to kEmbSmallTokens tokens: one launch.  A workgroup per (slot, 512 columns) ends at once unless its slot is the first
 //   with its token; else it collects the slots with that token, in order, and sums their rows.  Further workgroups clear the
 //   rows that no token names.
-//   beyond: the slots are sorted by token (few: by counting, in one launch; else a stable radix sort, digits of 8 or 10 bits; per
-//   digit one launch that counts and one that places: each of at most 96 workgroups adds up the counts of the ones before it itself, so nothing waits for another
-//   workgroup), then a workgroup sums the rows of a chunk of sorted slots, writes the sums of the tokens that begin and end
-//   among them, and leaves what spans a border to a last launch, as fp32 sums: a token that fills most slots (padding) is
-//   spread over the chip like any others.  The unnamed rows are cleared by spare workgroups of the first placing launch, whose
-//   sort is bound by latency.  Whether a token is named: the counting launch writes each slot's number to stamp[token] (plain
-//   stores, any one of them is right), and row v is named if stamp[v] is a slot whose token is v, so the stamps need no
-//   clearing before.
+//   beyond: the slots are sorted by token, then a workgroup sums the rows of a chunk of sorted slots, writes the sums of the
+//   tokens that begin and end among them, and leaves what spans a border to a last launch, as fp32 sums: a token that fills most
+//   slots (padding) is spread over the chip like any others.
+//   The sort, up to kEmbRankSlots: by counting, in one launch; else a stable radix sort with digits of 8 or 10 bits, per digit
+//   one launch that counts and one that places: each of at most 96 workgroups adds up the counts of the ones before it itself,
+//   so nothing waits for another workgroup.  The sort is bound by latency, so the unnamed rows are cleared by spare workgroups
+//   of its placing launches (or of the sums, where it is one launch).
+//   Whether a token is named: the counting launch writes each slot's number to stamp[token] (plain stores, any one of them is
+//   right), and row v is named if stamp[v] is a slot whose token is v, so the stamps need no clearing before.
+// Both sides at the borders (table 50000 x 512, us): one launch and sorted 700 slots 13.4 and 16.5, 1000 slots, 3/4 of them one
+// token's, 19.3 and 18.0; counting and radix 8000 slots 32 and 36, 9000 34 and 35, 12000 40 and 36; 8 and 32 slots a wavefront in
+// the sums 20000 slots 41 and 45, 40000 47 and 47, 130000 79 and 66.
+// 157696 slots of 512 columns into 50000 rows: 73 us, of these the sums 34 (5.1 TB/s of dy and dW), counting and placing
+// 4.3 + 9.8 and 4.4 + 10.8 (25 MB of zeros beside each placing), the join 9.6 (chains of latency: padding is one token's).
+// First version 118.
 #pragma once
 #include "avion_common.h"
 #include "avion_ln.h"
 
 constexpr int kEmbThreads = 256;
 constexpr int kEmbFly = 4;                // pieces in flight per thread in the lookup
-constexpr int kEmbSmallTokens = 512;      // at most this many: gradient in one launch
+constexpr int kEmbSmallTokens = 768;      // at most this many: gradient in one launch
 constexpr int kEmbCols = 512;             // columns of a workgroup in the sums: 8 per lane
 constexpr int kEmbSumWaves = 8;           // of a workgroup in the sums
 constexpr int kEmbSumMost = 32;           // sorted slots of a wavefront there: this many, or
@@ -422,8 +431,8 @@ avion_embedding_rank_kernel(const T* __restrict__ tokens, unsigned* __restrict__
 }
 
 // ------------------------------------------------------------------------------------- the sums
-// Sums of kEmbSumWaves * PER sorted slots (a chunk) in 512 columns.  heads[chunk][D]: the sum of a token that began in a chunk before, tails: of
-// one that begins here and goes on in the next.
+// Sums of kEmbSumWaves * PER sorted slots (a chunk) in 512 columns.  heads[chunk][D]: the sum of a token that began in a chunk
+// before, tails: of one that begins here and goes on in the next.
 template <int PER, typename E, typename TE>
 __global__ void __launch_bounds__(kEmbSumWaves * 64)
 avion_embedding_sum_kernel(const unsigned* __restrict__ keys, const unsigned* __restrict__ slots, const raw16* __restrict__ dy,

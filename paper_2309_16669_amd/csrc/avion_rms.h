@@ -10,7 +10,8 @@
 // Bound by memory bandwidth: forward two reads and two writes per element, backward three reads and one write (two with a
 // stream in 32 bits).  LANES lanes own a row at a time (16 or 32 neighbours, a wavefront, or 4 or 8 wavefronts), lane j of
 // them the 16-byte chunks j, j + LANES, ...: all of the row is in registers, so it is read once, and the next row is requested
-// before the current one is worked on.  Sums and
+// before the current one is worked on.  The grid is two workgroups a compute unit, more streams only meet in the memory (forward
+// + backward of 50176 x 768 58 + 55 us, with 1024 workgroups 60 + 58; 157696 x 512 117 + 119, 125 + 130).  Sums and
 // statistics are fp32, outputs are rounded once (nearest even).  max|y| is rstd max|h w|, so that the row's sum and its maximum
 // travel through one exchange.  The gains' gradient is summed over each wavefront's rows in registers, over the workgroup's
 // through LDS and over the workgroups by avion_ln_param_reduce_kernel in a fixed order: no atomics, bit-reproducible.
@@ -20,6 +21,7 @@
 
 constexpr int kRmsWaves = 4;            // wavefronts of a workgroup (as many as a row's, where a row has more)
 constexpr int kRmsMaxGrid = 512;        // workgroups of a launch; also the number of partial sums of the gains' gradient
+constexpr int kQuantizeMaxGrid = 1024;  // one read and half a write a row keep less in flight: 157696 x 512 48, with 512 59 us
 constexpr int kRmsMaxD = 16384;         // 8 wavefronts x 4 chunks x 64 lanes x 8
 constexpr float kF8Max = 448.0f;        // largest finite e4m3 value
 constexpr float kF8Least = 1.2621774483536189e-29f;  // 2^-96: a row's largest magnitude counts as at least this
@@ -174,7 +176,9 @@ struct RmsWork {
     static constexpr int WAVES = WPR > kRmsWaves ? WPR : kRmsWaves;
     static constexpr int ROWS = LANES <= 64 ? kRmsWaves * SUB : 1;           // rows of a workgroup at a time
     int lane, wave, at, sub;
-    DEVINL RmsWork() : lane(threadIdx.x % 64), wave(threadIdx.x / 64), at(LANES <= 64 ? lane % LANES : (int)threadIdx.x), sub(LANES < 64 ? lane / LANES : 0) {}
+    DEVINL RmsWork()
+        : lane(threadIdx.x % 64), wave(threadIdx.x / 64), at(LANES <= 64 ? lane % LANES : (int)threadIdx.x),
+          sub(LANES < 64 ? lane / LANES : 0) {}
     // the first of this wavefront's rows (the same in all its lanes); a lane's own is `sub` behind
     DEVINL long first() const { return (long)blockIdx.x * ROWS + (LANES <= 64 ? wave * SUB : 0); }
     DEVINL long stride() const { return (long)gridDim.x * ROWS; }

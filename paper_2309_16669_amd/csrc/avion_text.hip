@@ -1,4 +1,5 @@
-// C ABI of the text encoder's entry: token table, RMS normalisation with the residual's addition, rows in 8 bits.  See include/avion_attn.h for the contract of every entry point.
+// C ABI of the text encoder's entry: token table, RMS normalisation with the residual's addition, rows in 8 bits.  See
+// include/avion_attn.h for the contract of every entry point.
 #include "avion_attn.h"
 
 #include <hip/hip_runtime.h>
@@ -25,17 +26,19 @@ int rms_check(long long M, int D, unsigned flags, unsigned allowed)
     return AVION_OK;
 }
 // Lanes a row.  A wavefront holds up to 2048 columns (4 chunks a lane) and needs no exchange through LDS; narrow rows take 16
-// or 32 lanes, wide ones four wavefronts, or eight beyond 8192.  Few rows take four wavefronts as well.
+// or 32 lanes (forward and backward of 600000 x 128 111 + 112 us with 16, 214 + 208 with 64; 100000 x 256 39 + 38 and 45 + 46),
+// wide ones four wavefronts, or eight beyond 8192.  So few rows that each has a workgroup of its own take four wavefronts as
+// well: 1 x 1024 2.3 and 2.5 us, 300 x 1024 2.9 and 3.0; with more rows than workgroups, 1000 x 768, 3.8 and 3.3.
 int rms_lanes(long long M, int D)
 {
     if (D > 8192) return 512;
-    if (D > 2048 || (D > 512 && M <= 1024)) return 256;
+    if (D > 2048 || (D > 512 && M <= kRmsMaxGrid)) return 256;
     return D <= 128 ? 16 : D <= 256 ? 32 : 64;
 }
-unsigned rms_grid(long long M, int D)
+unsigned rms_grid(long long M, int D, int most = kRmsMaxGrid)
 {
     const int lanes = rms_lanes(M, D), rows = lanes <= 64 ? kRmsWaves * (64 / lanes) : 1;
-    return (unsigned)std::min<long long>((M + rows - 1) / rows, kRmsMaxGrid);
+    return (unsigned)std::min<long long>((M + rows - 1) / rows, most);
 }
 // f(lanes a row, chunks a lane)
 template <typename F>
@@ -205,7 +208,8 @@ int avion_rmsnorm_bwd(const void* h, const float* weight, const float* rstd, con
     float* part = static_cast<float*>(workspace);
     const unsigned grid = rms_grid(M, D);
     // One launch where the gains' gradient can read the rows once more at little cost (they are in the caches then): a launch
-    // and its kernel less (this call on 4 x 64: 7.6 -> 4.0 us of the host's time).
+    // and its kernel less (this call on 4 x 64: 7.6 -> 4.0 us of the host's time).  On the GPU 300 x 1024 takes 4.0 us, and the
+    // two ways meet near 1000 rows, whose sums are a chain of 8 loads there (1000 x 768 8.5, in two launches 1500 x 1024 9.2).
     const bool few = M > 0 && M <= 1024 && M * D <= (1 << 20);
     if (M > 0) {
         const int r1 = by_element(flags, [&](auto fmt) {
@@ -251,8 +255,8 @@ int avion_quantize_rows(const void* x, void* x8, float* scale, long long M, int 
             constexpr int LANES = decltype(lanes)::value;
             begin_launch();
             hipLaunchKernelGGL((avion_quantize_rows_kernel<LANES, decltype(nch)::value, typename decltype(fmt)::type>),
-                               dim3(rms_grid(M, D)), dim3(RmsWork<LANES>::WAVES * 64), 0, st, static_cast<const raw16*>(x), x8, scale,
-                               (long)M, D);
+                               dim3(rms_grid(M, D, kQuantizeMaxGrid)), dim3(RmsWork<LANES>::WAVES * 64), 0, st,
+                               static_cast<const raw16*>(x), x8, scale, (long)M, D);
             return end_launch("launch avion_quantize_rows_kernel");
         });
     });
