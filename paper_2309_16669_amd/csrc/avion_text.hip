@@ -255,7 +255,7 @@ int avion_quantize_rows(const void* x, void* x8, float* scale, long long M, int 
             constexpr int LANES = decltype(lanes)::value;
             begin_launch();
             hipLaunchKernelGGL((avion_quantize_rows_kernel<LANES, decltype(nch)::value, typename decltype(fmt)::type>),
-                               dim3(rms_grid(M, D, kQuantizeMaxGrid)), dim3(RmsWork<LANES>::WAVES * 64), 0, st,
+                               dim3(rms_grid(M, D, D <= kQuantizeMaxGridD ? kQuantizeMaxGrid : kRmsMaxGrid)), dim3(RmsWork<LANES>::WAVES * 64), 0, st,
                                static_cast<const raw16*>(x), x8, scale, (long)M, D);
             return end_launch("launch avion_quantize_rows_kernel");
         });
