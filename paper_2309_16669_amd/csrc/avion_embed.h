@@ -24,7 +24,7 @@
 // token's, 19.3 and 18.0; counting and radix 8000 slots 32 and 36, 9000 34 and 35, 12000 40 and 36; 8 and 32 slots a wavefront in
 // the sums 20000 slots 41 and 45, 40000 47 and 47, 130000 79 and 66.
 // 157696 slots of 512 columns into 50000 rows: 73 us, of these the sums 34 (5.1 TB/s of dy and dW), counting and placing
-// 4.3 + 9.8 and 4.4 + 10.8 (25 MB of zeros beside each placing), the join 9.6 (chains of latency: padding is one token's).
+// 4.3 + 9.8 and 4.4 + 10.8 (half of the unnamed rows cleared beside each placing), the join 9.6 (chains of latency: padding is one token's).
 // First version 118.
 #pragma once
 #include "avion_common.h"
