@@ -440,6 +440,9 @@ def _one_device(*tensors):
 
 def _launch(device, entry, args, stream):
     import torch
+    for a, kind in zip(args, entry.argtypes):
+        if kind is ctypes.c_int and not -(1 << 31) <= a < 1 << 31:   # (ctypes would take it modulo 2^32)
+            raise ValueError(f"{a} does not fit 32 bits")
     with torch.cuda.device(device):
         _check(entry(*args, _stream_handle(stream)))
 

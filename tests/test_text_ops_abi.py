@@ -118,3 +118,9 @@ def test_the_front_end_refuses():
                  lambda: ag.quantize_rows(x.clone().requires_grad_()), lambda: ag.linear_fp8(x8, s, w8, ws, ws.clone().requires_grad_())):
         with pytest.raises(ValueError, match="no backward"):
             call()
+
+
+def test_sizes_past_32_bits_are_not_cut():
+    # D is an int of the C interface
+    with pytest.raises(ValueError, match="32 bits"):
+        av._launch(0, av.load_library().avion_quantize_rows, (P, P, P, 1, (1 << 32) + 64, 0), None)
