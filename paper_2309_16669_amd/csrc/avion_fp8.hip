@@ -47,6 +47,8 @@ int launch_fp8(const char* x8, const float* xs, const char* w8, const float* ws,
 //   else the smallest tiles that leave no more than one for a compute unit (latency), larger ones beyond (traffic):
 //     64 x 64 and 128 x 64 on 1024 x 1024 x 1024 (256 tiles): 6.0 and 6.9, on 512 x 4096 x 4096 (512): 21.8 and 17.5;
 //     with eight wavefronts, half of K each, where K is long: 64 x 6144 x 4096: 13.3 -> 10.7, 64 x 2304 x 768: 4.8 and 4.8;
+//     128 x 64 in this way, where there is one for a compute unit at most: 2048 x 1024 x 4096 16.6 -> 15.0, 3000 x 640 x 8192
+//     29 -> 25, but 1570 x 1000 x 1280 7.7 -> 8.1 (1024 x 2048 x 2048 as long either way);
 //     128 x 64 and 128 x 128 on 785 x 2304 x 768 (126 tiles of 128 x 128): 6.8 and 8.7, on 1570 x 3840 x 1280 (390): 19.3 and 16.2
 //   256 x 256: a round of its 256 tiles takes about as long as 820 tiles of 128 x 128 in a long row and less to begin with, so it
 //     needs rounds that are well filled: 12544 x 768 x 768 (147 tiles): 14.8 against 17.4 of 128 x 128, 2048 x 4096 x 4096 (128):
@@ -108,6 +110,8 @@ int avion_linear_fp8(const void* x8, const float* x_scale, const void* w8, const
         if (fp8_wide(m, N)) return launch_wide<E, false>(x, x_scale, w, w_scale, bias, out, m, N, K, st);
         if (fp8_tiles(m, N, 128, 128) >= kComputeUnits)
             return launch_fp8<128, 128, 2, 2, 2, 1, E>(x, x_scale, w, w_scale, bias, out, m, N, K, st);
+        if (fp8_tiles(m, N, 64, 64) > kComputeUnits && fp8_tiles(m, N, 128, 64) <= kComputeUnits && K >= 4096)
+            return launch_fp8<128, 64, 2, 2, 3, 2, E>(x, x_scale, w, w_scale, bias, out, m, N, K, st);
         if (fp8_tiles(m, N, 64, 64) > kComputeUnits)
             return launch_fp8<128, 64, 2, 2, 3, 1, E>(x, x_scale, w, w_scale, bias, out, m, N, K, st);
         if (K >= 1024) return launch_fp8<64, 64, 2, 2, 3, 2, E>(x, x_scale, w, w_scale, bias, out, m, N, K, st);

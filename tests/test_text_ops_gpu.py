@@ -473,6 +473,13 @@ def test_linear_shapes(M, N, K, fmt, bias):
     _linear_check(M, N, K, fmt, bias, seed=M + N)
 
 
+# tiles of 128 x 64 with two groups over K (from 4096 on), and around
+@pytest.mark.parametrize("M,N,K", [(1570, 1000, 4096), (300, 6144, 4112), (1030, 520, 4352), (1025, 1032, 4080), (2048, 1024, 4224)])
+@pytest.mark.parametrize("fmt,bias", [(BF, True), (HF, False)])
+def test_linear_two_groups_over_k(M, N, K, fmt, bias):
+    _linear_check(M, N, K, fmt, bias, seed=M + K)
+
+
 # tiles of 256 x 256 with a long K: one tile a workgroup and several, K that ends inside a step, rows of y that are whole cache
 # lines and others
 @pytest.mark.parametrize("M,N,K,fmt,bias", [(36001, 256, 2064, BF, False), (5900, 3800, 2048, HF, True), (23000, 1024, 2192, HF, False), (23000, 1032, 2304, BF, True)])
