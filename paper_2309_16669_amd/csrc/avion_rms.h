@@ -86,25 +86,39 @@ DEVINL u32x2 pack_fp8(const float (&v)[8])
     return w;
 }
 
-// 448 / big as the sum of two fp32 (`lo` corrects the quotient's rounding): a row's values are scaled by it to within half a
-// step of fp32 before they are rounded to 8 bits, so that hardly one lands on the other side of a border than in exact
-// arithmetic.  Not finite: `lo` is left out.
+// Whether v lies within 5 steps of fp32 of the middle between two (normal) 8-bit values: then its roundings so far, 4 steps at
+// most, decide on the side.
+DEVINL bool near_middle(float v) { return ((__builtin_bit_cast(unsigned, v) - (0x80000u - 5u)) & 0xfffffu) <= 10u; }
+
+// 448 / (big + rest), rest < half a step of big, as the sum of two fp32: what a row's values are scaled by, without a rounding
+// that shows before the last one, to 8 bits.
 struct F8Factor {
     float hi, lo;
-    DEVINL explicit F8Factor(float big)
+    DEVINL explicit F8Factor(float big, float rest = 0.f)
     {
         hi = kF8Max / big;
-        const float l = fmaf(-hi, big, kF8Max) / big;
-        lo = fabsf(l) < hi ? l : 0.f;
+        const float l = fmaf(-hi, rest, fmaf(-hi, big, kF8Max)) / big;
+        lo = fabsf(l) < hi ? l : 0.f;  // (not finite: left out)
     }
     DEVINL float times(float v) const { return fmaf(v, hi, v * lo); }
-    // (a * b) times this, the product's rounding corrected too
+    // (a * b) times this.  Rounded to fp32; where that is a middle and the exact value (to 2^-40) is not, moved off to its side.
     DEVINL float times(float a, float b) const
     {
-        const float t = a * b, e = fmaf(a, b, -t);
-        return fmaf(t, hi, fmaf(t, lo, e * hi));
+        const float t = a * b, e = fmaf(a, b, -t), c = fmaf(t, lo, e * hi), q = fmaf(t, hi, c), rest = fmaf(t, hi, -q) + c;
+        if (__builtin_bit_cast(unsigned, q) << 12 != 0x80000000u || !(fabsf(rest) > fabsf(q) * 0x1p-40f)) return q;
+        return __builtin_bit_cast(float, __builtin_bit_cast(int, q) + ((rest < 0.f) == (q < 0.f) ? 1 : -1));
     }
 };
+
+// Products of these values are formed anew behind this (kept from before, they take a wide row's kernel from 187 to 278 registers).
+template <int NCH>
+DEVINL void apart(float (&v)[NCH][8])
+{
+#pragma unroll
+    for (int j = 0; j < NCH; ++j)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) asm volatile("" : "+v"(v[j][e]));
+}
 
 // A lane's share of a row: NCH chunks of 8 elements, 16-bit (E) or fp32
 // LAST: nobody reads it again (all inputs of the backward).  Read past the caches, backward of 157696 x 512 142 -> 112 us; the
@@ -212,8 +226,9 @@ DEVINL void row_reduce(float& a, float& b, float (&sh)[2][RmsWork<LANES>::WPR][2
 }
 
 // y (E), or y8 and scale with F8; h where there is a residual; rstd where it is asked for
+// (two wavefronts a SIMD at least: 8 bits and an fp32 stream would take 262 registers at 4 chunks a lane)
 template <int LANES, int NCH, typename E, typename R, bool F8>
-__global__ void __launch_bounds__(RmsWork<LANES>::WAVES * 64)
+__global__ void __launch_bounds__(RmsWork<LANES>::WAVES * 64, 2)
 avion_rmsnorm_fwd_kernel(const raw16* __restrict__ x, const void* __restrict__ residual, const float* __restrict__ weight,
                          void* __restrict__ y, float* __restrict__ scale, void* __restrict__ h, float* __restrict__ rstd,
                          long M, int D, float eps)
@@ -270,20 +285,55 @@ avion_rmsnorm_fwd_kernel(const raw16* __restrict__ x, const void* __restrict__ r
         // 8 bits: y / scale = h w 448 / max|h w|, in which rstd has gone; it stays where the least scale holds, where max|h w|
         // is too small to divide by (with an eps below 1e-14), and where something is not finite
         const float big_y = big * rs;
-        const bool gone = big >= 0x1p-90f && big_y >= kF8Least;
-        const float up = gone ? 1.f : rs;
-        const F8Factor to8(gone ? big : fmaxf(big_y, kF8Least));
+        u32x2 in8[NCH];
+        if constexpr (F8) {
+            const bool gone = big >= 0x1p-90f && big_y >= kF8Least;
+            const float by = kF8Max / big;
+            bool again = !gone;
+            apart(v);
+#pragma unroll
+            for (int j = 0; j < NCH; ++j) {
+                float o[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    o[e] = v[j][e] * gain[j][e] * by;
+                    again |= near_middle(o[e]);
+                }
+                in8[j] = pack_fp8(o);
+            }
+            // A row with a value whose side is open (one row of 120 of 768 columns), or one that keeps rstd: once more, exactly.
+            // (Quotients rounded to fp32 first put some twenty of 50176 x 768 values on the other side of a middle, this one at
+            // most; 52.9 -> 53.9 us, 4096 x 1024 8.6 -> 9.2, 3000 x 8192, whose wavefronts have to agree, 36 -> 39.  The first pass
+            // closer, which opens fewer sides: 55.1, 9.4 and 39.)
+            if (LANES > 64 ? __syncthreads_or(again) : __any(again)) {
+                float none = 0.f, rest = -big;  // of the largest product: what its rounding took
+                apart(v);
+#pragma unroll
+                for (int j = 0; j < NCH; ++j)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e)
+                        if (fabsf(v[j][e] * gain[j][e]) == big) rest = fmaxf(rest, fmaf(fabsf(v[j][e]), fabsf(gain[j][e]), -big));
+                row_reduce<LANES, true>(none, rest, sh, wave, lane, turn);
+                const F8Factor to8(gone ? big : fmaxf(big_y, kF8Least), gone ? rest : 0.f);
+                const float up = gone ? 1.f : rs;
+#pragma unroll
+                for (int j = 0; j < NCH; ++j) {
+                    float o[8];
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) o[e] = to8.times(v[j][e] * up, gain[j][e]);
+                    in8[j] = pack_fp8(o);
+                }
+            }
+        }
 #pragma unroll
         for (int j = 0; j < NCH; ++j) {
             const int ch = at + LANES * j;
             if (ch < chunks) {
                 if (residual) RmsRow<NCH, LANES, R>::store(h, n, D, ch, v[j]);
-                float o[8];
                 if constexpr (F8) {
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) o[e] = to8.times(v[j][e] * up, gain[j][e]);
-                    *reinterpret_cast<u32x2*>(static_cast<char*>(y) + n * D + ch * 8) = pack_fp8(o);
+                    *reinterpret_cast<u32x2*>(static_cast<char*>(y) + n * D + ch * 8) = in8[j];
                 } else {
+                    float o[8];
 #pragma unroll
                     for (int e = 0; e < 8; ++e) o[e] = v[j][e] * rs * gain[j][e];
                     RmsRow<NCH, LANES, E>::store(y, n, D, ch, o);

@@ -417,6 +417,30 @@ def test_rows_in_8_bits(M, D, fmt, stream):
     _rows8_check(ops.rms_fwd(h, f64(w), 1e-6)[0], q, s, (D / 2 + 20) * E)
 
 
+@pytest.mark.parametrize("M,D", [(6000, 128), (4000, 240), (5000, 768), (1000, 2000), (400, 768), (700, 4096), (200, 8208)])
+@pytest.mark.parametrize("fmt,stream", [(BF, BF), (HF, FP), (BF, None)])
+def test_norm_in_8_bits_is_the_nearest_value(M, D, fmt, stream):
+    """Of a normal value the nearest, unless it lies within 2^-38 of the middle between two: the quotient is held in two fp32, a few
+    roundings of 2^-48 each, and what is then left is compared with 2^-40."""
+    import torch
+    from paper_2309_16669_amd import autograd as ag
+    x, w = randn(M + D, (M, D), fmt), 1 + 0.1 * randn(2, (D,), FP)
+    w[::7] = 1.0      # products without a rounding, and the exact middles among their quotients
+    if stream is None:
+        q, s = ag.rms_norm_fp8(x, w)
+        h = x
+    else:
+        q, s, h = ag.add_rms_norm_fp8(x, randn(3, (M, D), stream, 2.0), w)
+    p = h.double() * w.double()
+    v = (p / p.abs().amax(1, keepdim=True) * 448.0).abs()
+    e = torch.floor(torch.log2(v.clamp_min(2.0 ** -6)))
+    steps = v * torch.exp2(3 - e)
+    open_side = (steps - torch.floor(steps) - 0.5).abs() <= steps * 2.0 ** -38
+    near = torch.round(steps) * torch.exp2(e - 3)
+    off = (q.double().abs() != near) & ~open_side & (v >= 2.0 ** -6)
+    assert not off.any(), (int(off.sum()), v[off][:4], q.double().abs()[off][:4])
+
+
 @pytest.mark.parametrize("D", [64, 4096])
 def test_rows_in_8_bits_small_values_and_small_eps(D):
     """Values whose products with the gains lie near the least fp32 number, under an eps that leaves the norm of them at 1; and
