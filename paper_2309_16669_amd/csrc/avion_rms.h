@@ -21,8 +21,7 @@
 
 constexpr int kRmsWaves = 4;            // wavefronts of a workgroup (as many as a row's, where a row has more)
 constexpr int kRmsMaxGrid = 512;        // workgroups of a launch; also the number of partial sums of the gains' gradient
-constexpr int kQuantizeMaxGrid = 1024;  // of avion_quantize_rows_kernel up to kQuantizeMaxGridD columns
-constexpr int kQuantizeMaxGridD = 1024;
+constexpr int kQuantizeMaxGrid = 1024;  // of avion_quantize_rows_kernel, for narrow rows
 constexpr int kRmsMaxD = 16384;         // 8 wavefronts x 4 chunks x 64 lanes x 8
 constexpr float kF8Max = 448.0f;        // largest finite e4m3 value
 constexpr float kF8Least = 1.2621774483536189e-29f;  // 2^-96: a row's largest magnitude counts as at least this
@@ -361,8 +360,9 @@ avion_rmsnorm_fwd_kernel(const raw16* __restrict__ x, const void* __restrict__ r
 }
 
 // Rows of x as they are, in 8 bits.  One read and half a write an element: with two workgroups a compute unit, narrow rows keep too
-// little in flight.  512 and 1024 workgroups: 157696 x 512 59 and 48 us, 12544 x 512 6.8 and 6.5, 50176 x 768 26 and 23,
-// 25088 x 1024 14.9 and 13.8, 12544 x 1024 8.8 and 9.2, but 50176 x 1280 38.1 and 38.6, 6272 x 2048 8.8 and 9.4.
+// little in flight; up to 1024 columns (two chunks a lane) that shows where x is read from memory.  512 and 1024 workgroups:
+// 157696 x 512 59 and 48 us, 12544 x 512 6.8 and 6.5, 50176 x 768 26 and 23, 25088 x 1024 14.9 and 13.8, but 12544 x 1024 8.8 and
+// 9.2, 8192 x 1024 6.9 and 7.2, 50176 x 1280 38.1 and 38.6.
 template <int LANES, int NCH, typename E>
 __global__ void __launch_bounds__(RmsWork<LANES>::WAVES * 64)
 avion_quantize_rows_kernel(const raw16* __restrict__ x, void* __restrict__ y, float* __restrict__ scale, long M, int D)

@@ -250,12 +250,13 @@ int avion_quantize_rows(const void* x, void* x8, float* scale, long long M, int 
     if (!x || !x8 || !scale) return AVION_EINVAL;
     if (!aligned16(x) || !aligned16(x8) || !aligned16(scale) || D % 16 != 0) return AVION_EUNSUPPORTED;
     hipStream_t st = static_cast<hipStream_t>(stream);
+    const int grid = D <= 512 || (D <= 1024 && M * D >= (1 << 24)) ? kQuantizeMaxGrid : kRmsMaxGrid;
     return by_element(flags, [&](auto fmt) {
         return rms_by_width(M, D, [&](auto lanes, auto nch) {
             constexpr int LANES = decltype(lanes)::value;
             begin_launch();
             hipLaunchKernelGGL((avion_quantize_rows_kernel<LANES, decltype(nch)::value, typename decltype(fmt)::type>),
-                               dim3(rms_grid(M, D, D <= kQuantizeMaxGridD ? kQuantizeMaxGrid : kRmsMaxGrid)), dim3(RmsWork<LANES>::WAVES * 64), 0, st,
+                               dim3(rms_grid(M, D, grid)), dim3(RmsWork<LANES>::WAVES * 64), 0, st,
                                static_cast<const raw16*>(x), x8, scale, (long)M, D);
             return end_launch("launch avion_quantize_rows_kernel");
         });
