@@ -282,11 +282,12 @@ avion_rmsnorm_fwd_kernel(const raw16* __restrict__ x, const void* __restrict__ r
         row_reduce<LANES, F8>(ss, big, sh, wave, lane, turn);
         const float rs = __builtin_amdgcn_rsqf(fmaf(ss, inv_d, eps));
         // 8 bits: y / scale = h w 448 / max|h w|, in which rstd has gone; it stays where the least scale holds, where max|h w|
-        // is too small to divide by (with an eps below 1e-14), and where something is not finite
-        const float big_y = big * rs;
+        // is too small to divide by (with an eps below 1e-14), and where that maximum or something else is not finite (gains of
+        // 1e30 on a stream of 1e10): max|y| is then taken of the products with rstd
+        float big_y = big * rs;
         u32x2 in8[NCH];
         if constexpr (F8) {
-            const bool gone = big >= 0x1p-90f && big_y >= kF8Least;
+            const bool gone = big >= 0x1p-90f && big < __builtin_inff() && big_y >= kF8Least;
             const float by = kF8Max / big;
             bool again = !gone;
             apart(v);
@@ -305,16 +306,20 @@ avion_rmsnorm_fwd_kernel(const raw16* __restrict__ x, const void* __restrict__ r
             // most; 52.9 -> 53.9 us, 4096 x 1024 8.6 -> 9.2, 3000 x 8192, whose wavefronts have to agree, 36 -> 39.  The first pass
             // closer, which opens fewer sides: 55.1, 9.4 and 39.)
             if (LANES > 64 ? __syncthreads_or(again) : __any(again)) {
-                float none = 0.f, rest = -big;  // of the largest product: what its rounding took
+                // of the largest product: what its rounding took; or the largest product with rstd
+                const float up = gone ? 1.f : rs;
+                float none = 0.f, rest = gone ? -big : 0.f;
                 apart(v);
 #pragma unroll
                 for (int j = 0; j < NCH; ++j)
 #pragma unroll
-                    for (int e = 0; e < 8; ++e)
-                        if (fabsf(v[j][e] * gain[j][e]) == big) rest = fmaxf(rest, fmaf(fabsf(v[j][e]), fabsf(gain[j][e]), -big));
+                    for (int e = 0; e < 8; ++e) {
+                        const float a = fabsf(v[j][e] * up), b = fabsf(gain[j][e]);
+                        if (!gone || a * b == big) rest = fmaxf(rest, gone ? fmaf(a, b, -big) : a * b);
+                    }
                 row_reduce<LANES, true>(none, rest, sh, wave, lane, turn);
+                if (!gone) big_y = rest;
                 const F8Factor to8(gone ? big : fmaxf(big_y, kF8Least), gone ? rest : 0.f);
-                const float up = gone ? 1.f : rs;
 #pragma unroll
                 for (int j = 0; j < NCH; ++j) {
                     float o[8];
