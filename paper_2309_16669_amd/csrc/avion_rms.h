@@ -85,10 +85,6 @@ DEVINL u32x2 pack_fp8(const float (&v)[8])
     return w;
 }
 
-// Whether v lies within 5 steps of fp32 of the middle between two (normal) 8-bit values: then its roundings so far, 4 steps at
-// most, decide on the side.
-DEVINL bool near_middle(float v) { return ((__builtin_bit_cast(unsigned, v) - (0x80000u - 5u)) & 0xfffffu) <= 10u; }
-
 // 448 / (big + rest), rest < half a step of big, as the sum of two fp32: what a row's values are scaled by, without a rounding
 // that shows before the last one, to 8 bits.
 struct F8Factor {
@@ -100,16 +96,17 @@ struct F8Factor {
         lo = fabsf(l) < hi ? l : 0.f;  // (not finite: left out)
     }
     DEVINL float times(float v) const { return fmaf(v, hi, v * lo); }
-    // (a * b) times this.  Rounded to fp32; where that is a middle and the exact value (to 2^-40) is not, moved off to its side.
+    // (a * b) times this, in fp32 rounded to odd: towards zero, the last bit set where something (to 2^-40) is left.  What is rounded
+    // once more from there, to the 8-bit values of whatever size, goes to the side that the exact value would.
     DEVINL float times(float a, float b) const
     {
         const float t = a * b, e = fmaf(a, b, -t), c = fmaf(t, lo, e * hi), q = fmaf(t, hi, c), rest = fmaf(t, hi, -q) + c;
-        if (__builtin_bit_cast(unsigned, q) << 12 != 0x80000000u || !(fabsf(rest) > fabsf(q) * 0x1p-40f)) return q;
-        return __builtin_bit_cast(float, __builtin_bit_cast(int, q) + ((rest < 0.f) == (q < 0.f) ? 1 : -1));
+        const int below = (rest < 0.f) != (q < 0.f) ? 1 : 0, odd = (__builtin_bit_cast(int, q) - below) | 1;
+        return fabsf(rest) > fabsf(q) * 0x1p-40f ? __builtin_bit_cast(float, odd) : q;
     }
 };
 
-// Products of these values are formed anew behind this (kept from before, they take a wide row's kernel from 187 to 278 registers).
+// Products of these values are formed anew behind this (kept from before, they take a wide row's kernel from 202 to 220 registers).
 template <int NCH>
 DEVINL void apart(float (&v)[NCH][8])
 {
@@ -288,23 +285,27 @@ avion_rmsnorm_fwd_kernel(const raw16* __restrict__ x, const void* __restrict__ r
         u32x2 in8[NCH];
         if constexpr (F8) {
             const bool gone = big >= 0x1p-90f && big < __builtin_inff() && big_y >= kF8Least;
-            const float by = kF8Max / big;
+            // five roundings at most lie between these and the exact quotients: where both ends of eight round alike, so do those
+            const float by = kF8Max / big, by_more = by * (1.f + 0x1p-21f), by_less = by * (1.f - 0x1p-21f);
             bool again = !gone;
             apart(v);
 #pragma unroll
             for (int j = 0; j < NCH; ++j) {
-                float o[8];
+                float more[8], less[8];
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
-                    o[e] = v[j][e] * gain[j][e] * by;
-                    again |= near_middle(o[e]);
+                    const float p = v[j][e] * gain[j][e];
+                    more[e] = p * by_more;
+                    less[e] = p * by_less;
                 }
-                in8[j] = pack_fp8(o);
+                in8[j] = pack_fp8(more);
+                const u32x2 other = pack_fp8(less);
+                again |= in8[j][0] != other[0] || in8[j][1] != other[1];
             }
-            // A row with a value whose side is open (one row of 120 of 768 columns), or one that keeps rstd: once more, exactly.
-            // (Quotients rounded to fp32 first put some twenty of 50176 x 768 values on the other side of a middle, this one at
-            // most; 52.9 -> 53.9 us, 4096 x 1024 8.6 -> 9.2, 3000 x 8192, whose wavefronts have to agree, 36 -> 39.  The first pass
-            // closer, which opens fewer sides: 55.1, 9.4 and 39.)
+            // A row with a value whose ends part (one row of 120 of 768 columns), or one that keeps rstd: once more, exactly.
+            // (Against quotients rounded to fp32 before, some twenty of 50176 x 768 of which lie on the wrong side of a middle:
+            // 54.1 us and 53 there, 4096 x 1024 9.2 and 8.6, 3000 x 8192, whose wavefronts have to agree, 39.6 and 36.  Finding the
+            // rows by the bits of one quotient took 54.5, 9.4 and 39.6, spilled at 4 chunks a lane, and knew no middles below 2^-6.)
             if (LANES > 64 ? __syncthreads_or(again) : __any(again)) {
                 // of the largest product: what its rounding took; or the largest product with rstd
                 const float up = gone ? 1.f : rs;

@@ -1,10 +1,12 @@
 """GPU tests of the text operators at the ends of their ranges.
 
 Bounds as in test_text_ops_gpu.py: E = 2^-24 for each fp32 operation, u half a step of a result's format."""
+from fractions import Fraction
+
 import pytest
 
 from oracle import text_ops as ops
-from tests.test_text_ops_gpu import E, FP, _rows8_check, f64, randn
+from tests.test_text_ops_gpu import BF, E, FP, HF, _rows8_check, f64, randn
 
 pytestmark = pytest.mark.gpu
 
@@ -30,3 +32,63 @@ def test_rows_in_8_bits_products_past_fp32(h_size, w_size, M, D):
         _rows8_check(ops.rms_fwd(f64(r.to(torch.bfloat16)), f64(w), 1e-20)[0], q, s, (D / 2 + 20) * E)
     q, s, h = ag.add_rms_norm_fp8(x, r, w / w_size, 1e-20)
     _rows8_check(ops.rms_fwd(f64(r), f64(w / w_size), 1e-20)[0], q, s, (D / 2 + 20) * E)
+
+
+def _small_ties():
+    """(big, value) of 8-bit significands, value / big * 448 exactly in the middle of two of the least 8-bit values (steps of
+    2^-9), and the even one of the two."""
+    out = []
+    for m in range(128, 256):
+        for a in range(128, 256):
+            for e in range(-22, -12):
+                v = Fraction(a, m) * 448 * Fraction(2) ** e * 1024      # in half steps
+                if v.denominator == 1 and v.numerator % 2 and v < 16:
+                    k = (v.numerator - 1) // 2
+                    out.append((m / 64.0, a * 2.0 ** (e - 6), (k + k % 2) * 2.0 ** -9))
+    return out
+
+
+@pytest.mark.parametrize("D", [16, 256, 768, 4096, 8208])
+def test_norm_in_8_bits_exact_middles_of_the_least_values(D):
+    import torch
+    from paper_2309_16669_amd import autograd as ag
+    ties = _small_ties()
+    assert len(ties) > 10 and any(abs(b - 2.109375) < 1e-9 for b, _, _ in ties)
+    x = torch.zeros((len(ties), D), dtype=torch.float64)
+    want = torch.zeros((len(ties), D))
+    for i, (big, value, q) in enumerate(ties):
+        at = 1 + (7 * i) % (D - 1)
+        x[i, 0], x[i, at] = big, -value if i % 2 else value
+        want[i, 0], want[i, at] = 448.0, -q if i % 2 else q
+    xb = x.to(torch.bfloat16)
+    assert torch.equal(xb.double(), x)
+    q, _ = ag.rms_norm_fp8(xb.cuda(), torch.ones(D, device="cuda"))
+    assert torch.equal(q.float().cpu(), want)
+    q, _ = ag.quantize_rows(xb.cuda())
+    assert torch.equal(q.float().cpu(), want)
+
+
+@pytest.mark.parametrize("M,D", [(6000, 128), (4000, 240), (5000, 768), (400, 768), (700, 4096), (200, 8208)])
+@pytest.mark.parametrize("fmt,stream", [(BF, BF), (HF, FP), (BF, None)])
+def test_norm_in_8_bits_is_the_nearest_of_the_least_values(M, D, fmt, stream):
+    """Of all values, those below 2^-6 among them (all but one of a row here), the nearest 8-bit one, unless the quotient lies within
+    2^-38 of the middle between two."""
+    import torch
+    from paper_2309_16669_amd import autograd as ag
+    x, w = randn(M + D, (M, D), fmt, 2.0 ** -11), 1 + 0.1 * randn(2, (D,), FP)
+    w[::7] = 1.0
+    x[:, 3] = 64.0 * (1 + torch.rand(M, device="cuda")).to(x.dtype)
+    if stream is None:
+        q, s = ag.rms_norm_fp8(x, w)
+        h = x
+    else:
+        q, s, h = ag.add_rms_norm_fp8(x, randn(3, (M, D), stream, 2.0 ** -11), w)
+    p = h.double() * w.double()
+    v = (p / p.abs().amax(1, keepdim=True) * 448.0).abs()
+    assert float((v < 2.0 ** -6).double().mean()) > 0.5
+    e = torch.floor(torch.log2(v.clamp_min(2.0 ** -6)))
+    steps = v * torch.exp2(3 - e)
+    open_side = (steps - torch.floor(steps) - 0.5).abs() <= steps * 2.0 ** -38
+    near = torch.round(steps) * torch.exp2(e - 3)
+    off = (q.double().abs() != near) & ~open_side
+    assert not off.any(), (int(off.sum()), v[off][:4], q.double().abs()[off][:4])
