@@ -72,6 +72,14 @@ DEVINL float lanes_max(float x)
     return LANES > 32 ? both_halves_max(x) : x;
 }
 
+// 1 / sqrt(x), also of x below 2^-126, which the unit takes for zero
+DEVINL float rsqrt_of(float x)
+{
+    const bool least = x < 0x1p-126f;
+    const float r = __builtin_amdgcn_rsqf(least ? x * 0x1p64f : x);
+    return least ? r * 0x1p32f : r;
+}
+
 // 8 fp32 -> 8 e4m3 (nearest even).  |v| < 464 or NaN.
 DEVINL u32x2 pack_fp8(const float (&v)[8])
 {
@@ -277,7 +285,7 @@ avion_rmsnorm_fwd_kernel(const raw16* __restrict__ x, const void* __restrict__ r
             }
         }
         row_reduce<LANES, F8>(ss, big, sh, wave, lane, turn);
-        const float rs = __builtin_amdgcn_rsqf(fmaf(ss, inv_d, eps));
+        const float rs = rsqrt_of(fmaf(ss, inv_d, eps));
         // 8 bits: y / scale = h w 448 / max|h w|, in which rstd has gone; it stays where the least scale holds, where max|h w|
         // is too small to divide by (with an eps below 1e-14), and where that maximum or something else is not finite (gains of
         // 1e30 on a stream of 1e10): max|y| is then taken of the products with rstd

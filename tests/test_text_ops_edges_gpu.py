@@ -3,10 +3,11 @@
 Bounds as in test_text_ops_gpu.py: E = 2^-24 for each fp32 operation, u half a step of a result's format."""
 from fractions import Fraction
 
+import numpy as np
 import pytest
 
 from oracle import text_ops as ops
-from tests.test_text_ops_gpu import BF, E, FP, HF, _rows8_check, f64, randn
+from tests.test_text_ops_gpu import BF, E, FP, HF, U, _rows8_check, f64, randn, within
 
 pytestmark = pytest.mark.gpu
 
@@ -92,3 +93,30 @@ def test_norm_in_8_bits_is_the_nearest_of_the_least_values(M, D, fmt, stream):
     near = torch.round(steps) * torch.exp2(e - 3)
     off = (q.double().abs() != near) & ~open_side
     assert not off.any(), (int(off.sum()), v[off][:4], q.double().abs()[off][:4])
+
+
+# --------------------------------------------------------------------------------------------- RMS normalisation
+def test_norm_of_rows_near_the_least_numbers():
+    """A mean of squares (with eps) below fp32's least normal number, 2^-126: rows of zeros under such an eps stay zeros, and rows
+    whose squares fp32 holds as multiples of 2^-149 have a norm of size 1."""
+    import torch
+    from paper_2309_16669_amd import autograd as ag
+    for D in (64, 256, 768, 4096):
+        w = 1 + 0.1 * randn(1, (D,), FP)
+        zeros = torch.zeros((5, D), dtype=torch.bfloat16, device="cuda")
+        for eps in (1e-38, 1e-40, 1e-44):
+            assert not ag.rms_norm(zeros, w, eps).any()
+            q, s = ag.rms_norm_fp8(zeros, w, eps)
+            assert not q.float().any() and abs(float(s[0]) - 2.0 ** -96 / 448) <= 2 * E * 2.0 ** -96 / 448
+            x = zeros.clone().requires_grad_()
+            (dx,) = torch.autograd.grad(ag.rms_norm(x, w, eps), x, torch.zeros_like(x))
+            assert not dx.any()
+        r = 1e-20 * randn(2, (5, D), FP)
+        y, h = ag.add_rms_norm(zeros, r, w, 0.0)
+        ref, rstd = ops.rms_fwd(f64(r), f64(w), 0.0)
+        # each addition to the sum, and the mean, is off by half of 2^-149 at most; half of that relative error is rstd's
+        lost = (D + D) * 2.0 ** -150 / (2 * D) * rstd[:, None] ** 2
+        assert lost.max() < 1e-4
+        within("y", y, ref, (U[BF] + (D / 2 + 12) * E + lost) * np.abs(ref))
+        q, s, h = ag.add_rms_norm_fp8(zeros, r, w, 0.0)
+        _rows8_check(ref, q, s, (D / 2 + 20) * E + float(lost.max()))
