@@ -22,7 +22,8 @@ the call.
 entry points the same way (what they keep for the backward is stated in their docstrings), and so do
 `embedding(tokens, weight)` and `add_rms_norm(x, residual, weight)` for the token table and for the RMS
 normalisation with the residual's addition.  These two take the backward's workspace from torch's allocator for
-the length of the call in either way of calling, and run on the device of their tensors.
+the length of the call in either way of calling, and run on the device of their tensors.  These and the calls below take
+tensors, and gradients, of any strides and at any address (what is not contiguous at a multiple of 16 bytes is copied first).
 
 `rms_norm_fp8`, `add_rms_norm_fp8`, `quantize_rows` and `linear_fp8` are the 8-bit path of a trained encoder: they
 have no backward, and refuse inputs whose gradient is being recorded.
@@ -254,13 +255,20 @@ def _bytes_on(device, need):
     return torch.empty(need, dtype=torch.uint8, device=device)
 
 
+def _dense(t):
+    """Contiguous and at a multiple of 16 bytes, as the C entries ask: a piece of a larger tensor (a gradient that comes out of a
+    concatenation) may begin at any element, and its place is not the caller's to choose."""
+    t = t.contiguous()
+    return t if t.data_ptr() % 16 == 0 else t.clone()
+
+
 class _Embedding(torch.autograd.Function):
     @staticmethod
     def forward(ctx, tokens, weight, scale, dtype):
         t = tokens.contiguous().view(-1)
         V, D = weight.shape
         y = torch.empty((t.shape[0], D), dtype=dtype, device=weight.device)
-        embedding_fwd(t, weight.contiguous(), y, scale)
+        embedding_fwd(t, _dense(weight), y, scale)
         ctx.save_for_backward(t)
         ctx.scale, ctx.shape, ctx.dtype = scale, (V, D), weight.dtype
         return y.view(*tokens.shape, D)
@@ -270,7 +278,7 @@ class _Embedding(torch.autograd.Function):
         (t,) = ctx.saved_tensors
         V, D = ctx.shape
         dweight = torch.empty((V, D), dtype=ctx.dtype, device=dy.device)
-        embedding_bwd(t, dy.contiguous().view(-1, D), dweight, ctx.scale,
+        embedding_bwd(t, _dense(dy).view(-1, D), dweight, ctx.scale,
                       _bytes_on(dy.device, embedding_bwd_workspace_bytes(t.shape[0], V, D)))
         return None, dweight, None, None
 
@@ -282,11 +290,11 @@ class _AddRmsNorm(torch.autograd.Function):
     def forward(ctx, x, residual, weight, eps):
         shape = x.shape
         D = shape[-1]
-        x2 = x.contiguous().view(-1, D)
-        r2 = None if residual is None else residual.contiguous().view(-1, D)
+        x2 = _dense(x).view(-1, D)
+        r2 = None if residual is None else _dense(residual).view(-1, D)
         y, h = torch.empty_like(x2), None if residual is None else torch.empty_like(r2)
         rstd = torch.empty((x2.shape[0],), dtype=torch.float32, device=x.device)
-        rmsnorm_fwd(x2, r2, weight.contiguous(), y, h, rstd, eps)
+        rmsnorm_fwd(x2, r2, _dense(weight), y, h, rstd, eps)
         ctx.set_materialize_grads(False)
         h = x2.view(shape) if h is None else h.view(shape)
         ctx.save_for_backward(h, weight, rstd)         # the residual stream, kept anyway, and one float per token; not y
@@ -299,14 +307,14 @@ class _AddRmsNorm(torch.autograd.Function):
         if dy is None and dh is None:
             return None, None, None, None
         D = h.shape[-1]
-        h2 = h.contiguous().view(-1, D)
-        dy = torch.zeros(h2.shape, dtype=ctx.dtype, device=h.device) if dy is None else dy.contiguous().view(-1, D)
-        dh = None if dh is None else dh.contiguous().view(-1, D)
+        h2 = _dense(h).view(-1, D)
+        dy = torch.zeros(h2.shape, dtype=ctx.dtype, device=h.device) if dy is None else _dense(dy).view(-1, D)
+        dh = None if dh is None else _dense(dh).view(-1, D)
         wide = h.dtype != ctx.dtype
         dx = torch.empty_like(dy) if ctx.needs_input_grad[0] or not wide else None
         dr = torch.empty_like(h2) if wide and ctx.needs_input_grad[1] else None
         dweight = torch.empty_like(weight, memory_format=torch.contiguous_format)
-        rmsnorm_bwd(h2, weight.contiguous(), rstd, dy, dh, dx, dr, dweight,
+        rmsnorm_bwd(h2, _dense(weight), rstd, dy, dh, dx, dr, dweight,
                     _bytes_on(h.device, rmsnorm_bwd_workspace_bytes(*h2.shape)))
         dx = None if dx is None else dx.view(h.shape)
         dr = dx if not wide else None if dr is None else dr.view(h.shape)
@@ -352,12 +360,12 @@ def add_rms_norm(x, residual, weight, eps: float = 1e-6):
 
 def _rms_norm_fp8(x, residual, weight, eps):
     shape = x.shape
-    x2 = x.contiguous().view(-1, shape[-1])
-    r2 = None if residual is None else residual.contiguous().view(-1, shape[-1])
+    x2 = _dense(x).view(-1, shape[-1])
+    r2 = None if residual is None else _dense(residual).view(-1, shape[-1])
     y8 = torch.empty(x2.shape, dtype=torch.float8_e4m3fn, device=x.device)
     scale = torch.empty((x2.shape[0],), dtype=torch.float32, device=x.device)
     h = None if r2 is None else torch.empty_like(r2)
-    rmsnorm_fwd_fp8(x2, r2, weight.contiguous(), y8, scale, h, eps)
+    rmsnorm_fwd_fp8(x2, r2, _dense(weight), y8, scale, h, eps)
     return y8.view(shape), scale.view(shape[:-1]), None if h is None else h.view(shape)
 
 
@@ -385,7 +393,7 @@ def quantize_rows(x):
     out = (_native or native_calls()).quantize_rows(x)
     if out is not None:
         return out
-    x2 = x.contiguous().view(-1, x.shape[-1])
+    x2 = _dense(x).view(-1, x.shape[-1])
     x8 = torch.empty(x2.shape, dtype=torch.float8_e4m3fn, device=x.device)
     scale = torch.empty((x2.shape[0],), dtype=torch.float32, device=x.device)
     _quantize_rows(x2, x8, scale)
@@ -405,7 +413,7 @@ def linear_fp8(x8, x_scale, w8, w_scale, bias=None, dtype=torch.bfloat16):
         raise ValueError(f"w8 must have shape (N, {K}), got {tuple(w8.shape)}")
     if x_scale.shape != x8.shape[:-1]:
         raise ValueError(f"x_scale must have shape {tuple(x8.shape[:-1])}, got {tuple(x_scale.shape)}")
-    x2 = x8.contiguous().view(-1, K)
+    x2 = _dense(x8).view(-1, K)
     y = torch.empty((x2.shape[0], w8.shape[0]), dtype=dtype, device=x8.device)
-    _linear_fp8(x2, x_scale.contiguous().view(-1), w8.contiguous(), w_scale.contiguous(), None if bias is None else bias.contiguous(), y)
+    _linear_fp8(x2, x_scale.contiguous().view(-1), _dense(w8), _dense(w_scale), None if bias is None else _dense(bias), y)
     return y.view(*x8.shape[:-1], w8.shape[0])

@@ -413,6 +413,13 @@ pybind11::object bias_gelu_linear(pybind11::handle x_, pybind11::handle bias_, p
 // These run on the device of their tensors, whatever the current one is.
 unsigned wide_flag(const Tensor& t) { return t.scalar_type() == at::kFloat ? AVION_FLAG_WIDE_F32 : 0u; }
 void* data_of(const Tensor& t) { return t.defined() ? t.data_ptr() : nullptr; }
+// Contiguous and at a multiple of 16 bytes, as the C entries ask: a piece of a larger tensor (a gradient that comes out of a
+// concatenation) may begin at any element, and its place is not the caller's to choose.
+Tensor dense(const Tensor& t)
+{
+    const Tensor c = t.contiguous();
+    return reinterpret_cast<uintptr_t>(c.data_ptr()) % 16 == 0 ? c : c.clone();
+}
 
 // As without_lock, for a call with several outputs
 template <typename F>
@@ -434,7 +441,7 @@ unsigned embedding_flags(const Tensor& tokens, const Tensor& table, at::ScalarTy
 }
 Tensor embedding_fwd(const Tensor& tokens, const Tensor& weight_, double scale, at::ScalarType out)
 {
-    const Tensor t = tokens.contiguous(), weight = weight_.contiguous();
+    const Tensor t = tokens.contiguous(), weight = dense(weight_);
     std::vector<int64_t> shape = tokens.sizes().vec();
     shape.push_back(weight.size(1));
     const Tensor y = at::empty(shape, weight.options().dtype(out));
@@ -455,8 +462,8 @@ struct Embedding : torch::autograd::Function<Embedding> {
     }
     static variable_list backward(AutogradContext* ctx, variable_list grad)
     {
-        const Tensor dy = grad[0].contiguous(), tokens = ctx->get_saved_variables()[0].contiguous();
-        const c10::DeviceGuard guard(dy.device());
+        const c10::DeviceGuard guard(grad[0].device());
+        const Tensor dy = dense(grad[0]), tokens = ctx->get_saved_variables()[0].contiguous();
         const std::vector<int64_t> shape = ctx->saved_data["shape"].toIntVector();
         const int64_t V = shape[0], D = shape[1], n = dy.numel() / D;
         require(tokens, "tokens", dy.sizes().slice(0, dy.dim() - 1), ctx->saved_data["tokens"].toScalarType(), dy);
@@ -494,27 +501,28 @@ struct RmsOut {
 RmsOut rms_fwd(const Tensor& x_, const Tensor& residual, const Tensor& weight, double eps, bool keep)
 {
     RmsOut r;
-    r.x = x_.contiguous();
+    r.x = dense(x_);
     const int64_t D = r.x.size(-1), M = r.x.numel() / D;
-    const Tensor res = residual.defined() ? residual.contiguous() : Tensor();
+    const Tensor res = residual.defined() ? dense(residual) : Tensor();
     r.y = at::empty(r.x.sizes(), r.x.options());
     if (res.defined()) r.h = at::empty(res.sizes(), res.options());
     if (keep) r.rstd = at::empty({M}, weight.options());
-    check(avion_rmsnorm_fwd(r.x.data_ptr(), data_of(res), weight.contiguous().data_ptr<float>(), r.y.data_ptr(), data_of(r.h),
+    check(avion_rmsnorm_fwd(r.x.data_ptr(), data_of(res), dense(weight).data_ptr<float>(), r.y.data_ptr(), data_of(r.h),
                             static_cast<float*>(data_of(r.rstd)), M, (int)D, (float)eps,
                             format_flag(r.x) | (res.defined() ? wide_flag(res) : 0u), stream()));
     return r;
 }
 // {dx, dresidual, dweight}; where the stream has the format of y, dx is the gradient of both
-variable_list rms_bwd(const Tensor& h, const Tensor& weight_, const Tensor& rstd, const Tensor& dy_, const Tensor& dh_, at::ScalarType format,
+variable_list rms_bwd(const Tensor& h_, const Tensor& weight_, const Tensor& rstd, const Tensor& dy_, const Tensor& dh_, at::ScalarType format,
                       bool want_dx, bool want_dr)
 {
     const Tensor& given = dy_.defined() ? dy_ : dh_;
     const c10::DeviceGuard guard(given.device());
-    const Tensor weight = weight_.contiguous(), dh = dh_.defined() ? dh_.contiguous() : Tensor();
-    const Tensor dy = dy_.defined() ? dy_.contiguous() : at::zeros(given.sizes(), given.options().dtype(format));
+    const Tensor dh = dh_.defined() ? dense(dh_) : Tensor();
+    const Tensor dy = dy_.defined() ? dense(dy_) : at::zeros(given.sizes(), given.options().dtype(format));
     const int64_t D = given.size(-1), M = given.numel() / D;
-    require(h, "h", given.sizes(), dh.defined() ? dh.scalar_type() : h.scalar_type(), given);
+    require(h_, "h", given.sizes(), dh.defined() ? dh.scalar_type() : h_.scalar_type(), given);
+    const Tensor h = dense(h_), weight = dense(weight_);
     TORCH_CHECK_VALUE(h.scalar_type() == format || h.scalar_type() == at::kFloat, "h must be ", format, " or float, got ", h.scalar_type());
     require(weight, "weight", {D}, at::kFloat, given);
     require(rstd, "rstd", {M}, at::kFloat, given);
@@ -585,7 +593,7 @@ pybind11::object rms_norm(pybind11::handle x_, pybind11::handle weight_, double 
     const Tensor *x, *weight;
     if (!rms_args(x_, x_, weight_, &x, nullptr, &weight)) return pybind11::none();
     return without_lock([&] {
-        if (records({x, weight})) return RmsNorm::apply(*x, *weight, eps);
+        if (records({x, weight})) return RmsNorm::apply(dense(*x), *weight, eps);
         const c10::DeviceGuard guard(x->device());
         return rms_fwd(*x, Tensor(), *weight, eps, false).y;
     });
@@ -609,12 +617,12 @@ pybind11::object add_rms_norm(pybind11::handle x_, pybind11::handle residual_, p
 variable_list rms_fp8(const Tensor& x_, const Tensor& residual, const Tensor& weight, double eps)
 {
     const c10::DeviceGuard guard(x_.device());
-    const Tensor x = x_.contiguous(), res = residual.defined() ? residual.contiguous() : Tensor();
+    const Tensor x = dense(x_), res = residual.defined() ? dense(residual) : Tensor();
     const int64_t D = x.size(-1), M = x.numel() / D;
     const Tensor y8 = at::empty(x.sizes(), x.options().dtype(at::kFloat8_e4m3fn));
     const Tensor scale = at::empty(x.sizes().slice(0, x.dim() - 1), weight.options());
     const Tensor h = res.defined() ? at::empty(res.sizes(), res.options()) : Tensor();
-    check(avion_rmsnorm_fwd_fp8(x.data_ptr(), data_of(res), weight.contiguous().data_ptr<float>(), y8.data_ptr(), scale.data_ptr<float>(),
+    check(avion_rmsnorm_fwd_fp8(x.data_ptr(), data_of(res), dense(weight).data_ptr<float>(), y8.data_ptr(), scale.data_ptr<float>(),
                                 data_of(h), M, (int)D, (float)eps, format_flag(x) | (res.defined() ? wide_flag(res) : 0u), stream()));
     if (h.defined()) return {y8, scale, h};
     return {y8, scale};
@@ -643,7 +651,7 @@ pybind11::object quantize_rows(pybind11::handle x_)
         return pybind11::none();
     return many_without_lock([&]() -> variable_list {
         const c10::DeviceGuard guard(x->device());
-        const Tensor in = x->contiguous();
+        const Tensor in = dense(*x);
         const int64_t D = in.size(-1);
         const Tensor x8 = at::empty(in.sizes(), in.options().dtype(at::kFloat8_e4m3fn));
         const Tensor scale = at::empty(in.sizes().slice(0, in.dim() - 1), in.options().dtype(at::kFloat));
@@ -668,8 +676,8 @@ pybind11::object linear_fp8(pybind11::handle x8_, pybind11::handle xs_, pybind11
     if (records({xs, ws}) || (bias && records({bias}))) return pybind11::none();
     return without_lock([&] {
         const c10::DeviceGuard guard(x8->device());
-        const Tensor x = x8->contiguous(), s = xs->contiguous(), w = w8->contiguous(), sw = ws->contiguous();
-        const Tensor b = bias ? bias->contiguous() : Tensor();
+        const Tensor x = dense(*x8), s = xs->contiguous(), w = dense(*w8), sw = dense(*ws);
+        const Tensor b = bias ? dense(*bias) : Tensor();
         const int64_t K = x.size(-1), N = w.size(0);
         std::vector<int64_t> shape = x.sizes().vec();
         shape.back() = N;

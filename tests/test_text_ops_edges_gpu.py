@@ -1,4 +1,4 @@
-"""GPU tests of the text operators at the ends of their ranges.
+"""GPU tests of the text operators at the ends of their ranges, and with tensors at any address.
 
 Bounds as in test_text_ops_gpu.py: E = 2^-24 for each fp32 operation, u half a step of a result's format."""
 from fractions import Fraction
@@ -120,3 +120,72 @@ def test_norm_of_rows_near_the_least_numbers():
         within("y", y, ref, (U[BF] + (D / 2 + 12) * E + lost) * np.abs(ref))
         q, s, h = ag.add_rms_norm_fp8(zeros, r, w, 0.0)
         _rows8_check(ref, q, s, (D / 2 + 20) * E + float(lost.max()))
+
+
+# ---------------------------------------------------------------------------------------------------- addresses
+def odd(t):
+    """The same values in memory whose address is a multiple of the element's size only."""
+    import torch
+    room = torch.empty(t.numel() + 1, dtype=t.dtype, device=t.device)
+    out = room[1:].view(t.shape)
+    out.copy_(t.detach())
+    assert out.is_contiguous() and out.data_ptr() % 16 != 0
+    return out
+
+
+def _both_ways(monkeypatch):
+    """The native calls, then the classes."""
+    from types import SimpleNamespace
+    from paper_2309_16669_amd import autograd as ag
+    names = ("embedding", "rms_norm", "add_rms_norm", "rms_norm_fp8", "add_rms_norm_fp8", "quantize_rows", "linear_fp8")
+    ag.native_calls()
+    yield "native"
+    with monkeypatch.context() as m:
+        m.setattr(ag, "_native", SimpleNamespace(**{n: lambda *args: None for n in names}))
+        yield "classes"
+
+
+def test_tensors_at_any_address(monkeypatch):
+    import torch
+    from paper_2309_16669_amd import autograd as ag
+    M, D = 37, 144
+    t = torch.arange(2 * M, device="cuda").view(2, M) % 50
+    table, x, r, w = randn(1, (50, D), BF), randn(2, (M, D), BF), randn(3, (M, D), FP), 1 + 0.1 * randn(4, (D,), FP)
+    dy2, dy, dh = randn(5, (2, M, D), BF), randn(6, (M, D), BF), randn(7, (M, D), FP)
+    calls = [(lambda a: ag.embedding(t, a, 2.0), [table], [dy2]), (ag.rms_norm, [x, w], [dy]), (ag.add_rms_norm, [x, r, w], [dy, dh]),
+             (ag.add_rms_norm, [x, r.bfloat16(), w], [dy, dh.bfloat16()])]
+    x8, xs = ag.quantize_rows(x)
+    w8, ws = ag.quantize_rows(randn(8, (64, D), BF))
+    b = randn(9, (64,), FP)
+    plain = [(ag.rms_norm_fp8, [x, w]), (ag.add_rms_norm_fp8, [x, r, w]), (ag.quantize_rows, [x]), (ag.linear_fp8, [x8, xs, w8, ws, b])]
+    for way in _both_ways(monkeypatch):
+        for call, args, grads in calls:
+            got = []
+            for place_args, place_grads in ((torch.clone, torch.clone), (odd, torch.clone), (torch.clone, odd), (odd, odd)):
+                leaves = [place_args(a).requires_grad_() for a in args]
+                out = call(*leaves)
+                out = out if isinstance(out, tuple) else (out,)
+                g = torch.autograd.grad(out, leaves, [place_grads(d) for d in grads])
+                got.append([*out, *g])
+            for other in got[1:]:
+                assert all(torch.equal(a, c) for a, c in zip(got[0], other)), way
+        for call, args in plain:
+            with torch.no_grad():
+                a, c = call(*args), call(*[odd(v) for v in args])
+            for u, v in zip(a if isinstance(a, tuple) else (a,), c if isinstance(c, tuple) else (c,)):
+                assert torch.equal(u.float(), v.float()), way
+
+
+def test_gradients_from_behind_an_odd_part(monkeypatch):
+    # what a concatenation hands back: a contiguous piece that begins at an odd element
+    import torch
+    from paper_2309_16669_amd import autograd as ag
+    x, w = randn(1, (9, 64), BF), 1 + 0.1 * randn(2, (64,), FP)
+    t, table, a = torch.arange(9, device="cuda"), randn(3, (9, 64), BF), randn(4, (3,), BF)
+    for way in _both_ways(monkeypatch):
+        for call, leaf in ((lambda v: ag.rms_norm(v, w), x), (lambda v: ag.add_rms_norm(v, x, w)[0], x),
+                           (lambda v: ag.add_rms_norm(x, v, w)[1], x), (lambda v: ag.embedding(t, v), table)):
+            p, q = leaf.clone().requires_grad_(), leaf.clone().requires_grad_()
+            torch.cat([a, call(p).flatten()]).float().square().sum().backward()
+            call(q).float().square().sum().backward()
+            assert torch.equal(p.grad, q.grad), way
