@@ -24,6 +24,7 @@ entry points the same way (what they keep for the backward is stated in their do
 normalisation with the residual's addition.  These two take the backward's workspace from torch's allocator for
 the length of the call in either way of calling, and run on the device of their tensors.  These and the calls below take
 tensors, and gradients, of any strides and at any address (what is not contiguous at a multiple of 16 bytes is copied first).
+Their gradients are not differentiable: under create_graph they carry a node that raises.
 
 `rms_norm_fp8`, `add_rms_norm_fp8`, `quantize_rows` and `linear_fp8` are the 8-bit path of a trained encoder: they
 have no backward, and refuse inputs whose gradient is being recorded.
@@ -262,6 +263,28 @@ def _dense(t):
     return t if t.data_ptr() % 16 == 0 else t.clone()
 
 
+class _NoSecondDerivative(torch.autograd.Function):
+    """The node of a gradient that a kernel has written: it leads to the tensors that the gradient depends on, and says that the
+    way back through it does not exist.  Without it a second derivative would silently miss this operator's part."""
+
+    @staticmethod
+    def forward(ctx, what, gradient, *inputs):
+        ctx.what = what
+        return gradient[0]
+
+    @staticmethod
+    def backward(ctx, _):
+        raise RuntimeError(f"{ctx.what} has no second derivative")
+
+
+def _depends_on(gradient, what, *inputs):
+    """`gradient` with that node, where the backward itself is recorded (create_graph)."""
+    inputs = [t for t in inputs if t is not None and t.requires_grad]
+    if gradient is None or not inputs or not torch.is_grad_enabled():
+        return gradient
+    return _NoSecondDerivative.apply(what, (gradient,), *inputs)
+
+
 class _Embedding(torch.autograd.Function):
     @staticmethod
     def forward(ctx, tokens, weight, scale, dtype):
@@ -280,7 +303,7 @@ class _Embedding(torch.autograd.Function):
         dweight = torch.empty((V, D), dtype=ctx.dtype, device=dy.device)
         embedding_bwd(t, _dense(dy).view(-1, D), dweight, ctx.scale,
                       _bytes_on(dy.device, embedding_bwd_workspace_bytes(t.shape[0], V, D)))
-        return None, dweight, None, None
+        return None, _depends_on(dweight, "embedding", dy), None, None
 
 
 class _AddRmsNorm(torch.autograd.Function):
@@ -290,15 +313,16 @@ class _AddRmsNorm(torch.autograd.Function):
     def forward(ctx, x, residual, weight, eps):
         shape = x.shape
         D = shape[-1]
-        x2 = _dense(x).view(-1, D)
+        x = _dense(x)
+        x2 = x.view(-1, D)
         r2 = None if residual is None else _dense(residual).view(-1, D)
         y, h = torch.empty_like(x2), None if residual is None else torch.empty_like(r2)
         rstd = torch.empty((x2.shape[0],), dtype=torch.float32, device=x.device)
         rmsnorm_fwd(x2, r2, _dense(weight), y, h, rstd, eps)
         ctx.set_materialize_grads(False)
-        h = x2.view(shape) if h is None else h.view(shape)
+        h = x if h is None else h.view(shape)
         ctx.save_for_backward(h, weight, rstd)         # the residual stream, kept anyway, and one float per token; not y
-        ctx.dtype, ctx.alone = x.dtype, residual is None
+        ctx.dtype, ctx.alone, ctx.vary = x.dtype, residual is None, any(ctx.needs_input_grad[:2])
         return y.view(shape) if residual is None else (y.view(shape), h)
 
     @staticmethod
@@ -307,6 +331,7 @@ class _AddRmsNorm(torch.autograd.Function):
         if dy is None and dh is None:
             return None, None, None, None
         D = h.shape[-1]
+        given = dy, dh
         h2 = _dense(h).view(-1, D)
         dy = torch.zeros(h2.shape, dtype=ctx.dtype, device=h.device) if dy is None else _dense(dy).view(-1, D)
         dh = None if dh is None else _dense(dh).view(-1, D)
@@ -316,8 +341,10 @@ class _AddRmsNorm(torch.autograd.Function):
         dweight = torch.empty_like(weight, memory_format=torch.contiguous_format)
         rmsnorm_bwd(h2, _dense(weight), rstd, dy, dh, dx, dr, dweight,
                     _bytes_on(h.device, rmsnorm_bwd_workspace_bytes(*h2.shape)))
-        dx = None if dx is None else dx.view(h.shape)
-        dr = dx if not wide else None if dr is None else dr.view(h.shape)
+        what = "rms_norm" if ctx.alone else "add_rms_norm"
+        dx = None if dx is None else _depends_on(dx.view(h.shape), what, *given, h, weight)
+        dr = dx if not wide else None if dr is None else _depends_on(dr.view(h.shape), what, *given, h, weight)
+        dweight = _depends_on(dweight, what, given[0], h if ctx.vary else None)
         return dx, (None if ctx.alone else dr), dweight, None
 
 
@@ -334,7 +361,7 @@ def _no_backward(name, *tensors):
 def embedding(tokens, weight, scale: float = 1.0, dtype=None):
     """scale * weight[tokens] for tokens (int64 or int32, any shape) of a table [V, D] in bf16, fp16 or fp32, D a multiple of 8;
     the result is bf16 or fp16 (`dtype`; the table's own format, bf16 for an fp32 table, if None).  A token outside [0, V)
-    gives a row of zeros and adds to no gradient.  Differentiable in weight (the gradient has the table's format; fp32 sums in
+    gives a row of zeros and adds to no gradient.  Differentiable once in weight (the gradient has the table's format; fp32 sums in
     a fixed order); keeps the tokens for the backward."""
     if dtype is None:
         dtype = torch.bfloat16 if weight.dtype == torch.float32 else weight.dtype
@@ -344,15 +371,15 @@ def embedding(tokens, weight, scale: float = 1.0, dtype=None):
 
 def rms_norm(x, weight, eps: float = 1e-6):
     """Root-mean-square normalisation over the last axis of x (bf16 or fp16, any leading shape, width <= 16384 and a multiple of
-    8) with fp32 gains.  Differentiable in x and weight; keeps x and one float per token for the backward."""
+    8) with fp32 gains.  Differentiable once in x and weight; keeps x and one float per token for the backward."""
     y = (_native or native_calls()).rms_norm(x, weight, float(eps))
-    return _AddRmsNorm.apply(x, None, weight, float(eps)) if y is None else y
+    return _AddRmsNorm.apply(_dense(x), None, weight, float(eps)) if y is None else y
 
 
 def add_rms_norm(x, residual, weight, eps: float = 1e-6):
     """(y, h): h = x + residual, the residual stream behind a layer's branch, and y = rms_norm(h, weight), what the next branch
     reads.  x bf16 or fp16 [..., D]; residual, of the same shape, in the format of x or fp32, and h like it (y is the norm of h
-    as stored).  Differentiable in x, residual and weight; keeps h and one float per token."""
+    as stored).  Differentiable once in x, residual and weight; keeps h and one float per token."""
     _check_residual(x, residual)
     out = (_native or native_calls()).add_rms_norm(x, residual, weight, float(eps))
     return _AddRmsNorm.apply(x, residual, weight, float(eps)) if out is None else out

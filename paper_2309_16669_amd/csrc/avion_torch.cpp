@@ -14,6 +14,7 @@
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/custom_function.h>
+#include <torch/csrc/autograd/functions/utils.h>
 #include <torch/csrc/autograd/python_variable.h>
 #include <torch/csrc/jit/frontend/tracer.h>
 #include <torch/csrc/utils/pybind.h>
@@ -435,6 +436,26 @@ pybind11::object many_without_lock(F call)
     return std::move(t);
 }
 
+// The node of a gradient that a kernel has written: it leads to the tensors that the gradient depends on, and says that the way
+// back through it does not exist.  Without it a second derivative would silently miss this operator's part.
+struct NoSecondDerivative : torch::autograd::Node {
+    const char* what;
+    explicit NoSecondDerivative(const char* operation) : what(operation) {}
+    variable_list apply(variable_list&&) override { TORCH_CHECK(false, what, " has no second derivative"); }
+};
+// where the backward itself is recorded (create_graph)
+void depends_on(const Tensor& gradient, const char* what, std::initializer_list<Tensor> inputs)
+{
+    if (!gradient.defined() || !at::GradMode::is_enabled()) return;
+    std::shared_ptr<NoSecondDerivative> node;
+    for (const Tensor& t : inputs) {
+        if (!t.defined() || !t.requires_grad()) continue;
+        if (!node) node = std::shared_ptr<NoSecondDerivative>(new NoSecondDerivative(what), torch::autograd::deleteNode);
+        node->add_next_edge(torch::autograd::impl::gradient_edge(t));
+    }
+    if (node) torch::autograd::set_history(gradient, node);
+}
+
 unsigned embedding_flags(const Tensor& tokens, const Tensor& table, at::ScalarType out)
 {
     return (out == at::kHalf ? AVION_FLAG_F16 : 0u) | wide_flag(table) | (tokens.scalar_type() == at::kInt ? AVION_FLAG_TOKENS_I32 : 0u);
@@ -473,6 +494,7 @@ struct Embedding : torch::autograd::Function<Embedding> {
         check(avion_embedding_bwd(tokens.data_ptr(), dy.data_ptr(), dweight.data_ptr(), n, V, (int)D,
                                   (float)ctx->saved_data["scale"].toDouble(), embedding_flags(tokens, dweight, dy.scalar_type()),
                                   ws.data_ptr(), need, stream()));
+        depends_on(dweight, "embedding", {grad[0]});
         return {dweight, Tensor(), Tensor(), Tensor()};
     }
 };
@@ -512,9 +534,10 @@ RmsOut rms_fwd(const Tensor& x_, const Tensor& residual, const Tensor& weight, d
                             format_flag(r.x) | (res.defined() ? wide_flag(res) : 0u), stream()));
     return r;
 }
-// {dx, dresidual, dweight}; where the stream has the format of y, dx is the gradient of both
+// {dx, dresidual, dweight}; where the stream has the format of y, dx is the gradient of both.  vary: h depends on what is
+// differentiated
 variable_list rms_bwd(const Tensor& h_, const Tensor& weight_, const Tensor& rstd, const Tensor& dy_, const Tensor& dh_, at::ScalarType format,
-                      bool want_dx, bool want_dr)
+                      bool want_dx, bool want_dr, const char* what, bool vary)
 {
     const Tensor& given = dy_.defined() ? dy_ : dh_;
     const c10::DeviceGuard guard(given.device());
@@ -536,6 +559,9 @@ variable_list rms_bwd(const Tensor& h_, const Tensor& weight_, const Tensor& rst
     check(avion_rmsnorm_bwd(h.data_ptr(), weight.data_ptr<float>(), rstd.data_ptr<float>(), dy.data_ptr(), data_of(dh), data_of(dx),
                             static_cast<float*>(data_of(dr)), dweight.data_ptr<float>(), M, (int)D, format_flag(dy) | wide_flag(h),
                             ws.data_ptr(), need, stream()));
+    depends_on(dx, what, {dy_, dh_, h_, weight_});
+    if (wide) depends_on(dr, what, {dy_, dh_, h_, weight_});
+    depends_on(dweight, what, {dy_, vary ? h_ : Tensor()});
     return {dx, wide ? dr : dx, dweight};
 }
 struct RmsNorm : torch::autograd::Function<RmsNorm> {
@@ -550,7 +576,7 @@ struct RmsNorm : torch::autograd::Function<RmsNorm> {
     {
         const variable_list s = ctx->get_saved_variables();
         require(s[0], "x", grad[0].sizes(), grad[0].scalar_type(), grad[0]);
-        variable_list g = rms_bwd(s[0], s[1], s[2], grad[0], Tensor(), grad[0].scalar_type(), true, false);
+        variable_list g = rms_bwd(s[0], s[1], s[2], grad[0], Tensor(), grad[0].scalar_type(), true, false, "rms_norm", true);
         return {g[0], g[2], Tensor()};
     }
 };
@@ -562,6 +588,7 @@ struct AddRmsNorm : torch::autograd::Function<AddRmsNorm> {
         ctx->set_materialize_grads(false);
         ctx->save_for_backward({r.h, weight, r.rstd});  // the residual stream, kept anyway, and one float per token; not y
         ctx->saved_data["format"] = x.scalar_type();
+        ctx->saved_data["vary"] = x.requires_grad() || residual.requires_grad();
         return {r.y, r.h};
     }
     static variable_list backward(AutogradContext* ctx, variable_list grad)
@@ -569,7 +596,7 @@ struct AddRmsNorm : torch::autograd::Function<AddRmsNorm> {
         if (!grad[0].defined() && !grad[1].defined()) return {Tensor(), Tensor(), Tensor(), Tensor()};
         const variable_list s = ctx->get_saved_variables();
         variable_list g = rms_bwd(s[0], s[1], s[2], grad[0], grad[1], ctx->saved_data["format"].toScalarType(),
-                                  ctx->needs_input_grad(0), ctx->needs_input_grad(1));
+                                  ctx->needs_input_grad(0), ctx->needs_input_grad(1), "add_rms_norm", ctx->saved_data["vary"].toBool());
         g.resize(4);
         return g;
     }

@@ -1,4 +1,5 @@
-"""GPU tests of the text operators at the ends of their ranges, and with tensors at any address.
+"""GPU tests of the text operators at the ends of their ranges: gains and streams near fp32's largest and least numbers, quotients
+among the least 8-bit values, tensors at any address, and gradients that are differentiated again.
 
 Bounds as in test_text_ops_gpu.py: E = 2^-24 for each fp32 operation, u half a step of a result's format."""
 from fractions import Fraction
@@ -189,3 +190,45 @@ def test_gradients_from_behind_an_odd_part(monkeypatch):
             torch.cat([a, call(p).flatten()]).float().square().sum().backward()
             call(q).float().square().sum().backward()
             assert torch.equal(p.grad, q.grad), way
+
+
+# ---------------------------------------------------------------------------------------------- differentiated again
+def test_second_derivatives_raise(monkeypatch):
+    import torch
+    from paper_2309_16669_amd import autograd as ag
+    t, table, w = torch.arange(9, device="cuda") % 4, randn(1, (5, 64), BF), 1 + 0.1 * randn(2, (64,), FP)
+    x, r = randn(3, (9, 64), BF), randn(4, (9, 64), FP)
+    columns = randn(5, (64, 9), BF).t()
+    square = lambda y: y.float().square().sum()
+    cases = [(lambda a: square(ag.embedding(t, a)), [table]),
+             (lambda a, b: ag.rms_norm(a, b).float().sum(), [x, w]),          # dy depends on nothing: the norm's own curvature
+             (lambda a: ag.rms_norm(a, w).float().sum(), [columns]),          # an input that is laid out anew
+             (lambda b: square(ag.rms_norm(x, b)), [w]),
+             (lambda a, b, c: ag.add_rms_norm(a, b, c)[0].float().sum(), [x, r, w]),
+             (lambda a: ag.add_rms_norm(a, r, w)[0].float().sum(), [x]),
+             (lambda b: ag.add_rms_norm(x, b, w)[0].float().sum(), [r]),
+             (lambda a, b: ag.add_rms_norm(a, b, w)[0].float().sum(), [x, x]),
+             (lambda a: square(ag.add_rms_norm(a, r, w)[1]), [x])]
+    for way in _both_ways(monkeypatch):
+        for f, args in cases:
+            leaves = [a.clone(memory_format=torch.preserve_format).requires_grad_() for a in args]
+            first = torch.autograd.grad(f(*leaves), leaves)
+            g = torch.autograd.grad(f(*leaves), leaves, create_graph=True)
+            assert all(torch.equal(a, b) for a, b in zip(first, g)), way    # the first derivative alone is served
+            penalty = sum(square(v) for v in g) + sum(v.float().sum() for v in leaves)
+            with pytest.raises(RuntimeError, match="second derivative"):
+                torch.autograd.grad(penalty, leaves, retain_graph=True)
+            with pytest.raises(RuntimeError, match="second derivative"):
+                penalty.backward()
+
+
+def test_gradients_that_depend_on_nothing_carry_no_node(monkeypatch):
+    import torch
+    from paper_2309_16669_amd import autograd as ag
+    t, table, w = torch.arange(9, device="cuda") % 4, randn(1, (5, 64), BF).requires_grad_(), (1 + 0.1 * randn(2, (64,), FP)).requires_grad_()
+    x = randn(3, (9, 64), BF)
+    for way in _both_ways(monkeypatch):
+        # linear in the table, and in the gains
+        for y, leaf in ((ag.embedding(t, table), table), (ag.rms_norm(x, w), w), (ag.add_rms_norm(x, x, w)[0], w)):
+            (g,) = torch.autograd.grad(y, leaf, torch.ones_like(y), create_graph=True)
+            assert not g.requires_grad, way
