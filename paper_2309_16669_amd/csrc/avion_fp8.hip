@@ -50,11 +50,17 @@ int launch_fp8(const char* x8, const float* xs, const char* w8, const float* ws,
 //     128 x 64 in this way, where there is one for a compute unit at most: 2048 x 1024 x 4096 16.6 -> 15.0, 3000 x 640 x 8192
 //     29 -> 25, but 1570 x 1000 x 1280 7.7 -> 8.1 (1024 x 2048 x 2048 as long either way);
 //     128 x 64 and 128 x 128 on 785 x 2304 x 768 (126 tiles of 128 x 128): 6.8 and 8.7, on 1570 x 3840 x 1280 (390): 19.3 and 16.2
+//     and 128 x 128 only where y has more than 64 columns: 36864 x 64 x 1024 11.4 and 12.5, 36864 x 72 x 1024 13.5 and 12.6
 //   256 x 256: a round of its 256 tiles takes about as long as 820 tiles of 128 x 128 in a long row and less to begin with, so it
-//     needs rounds that are well filled: 12544 x 768 x 768 (147 tiles): 14.8 against 17.4 of 128 x 128, 2048 x 4096 x 4096 (128):
-//     46 against 38, 6272 x 2304 x 768 (225): 16.5 against 20.6, 50176 x 2304 x 768: 88 against 165
+//     needs rounds that are well filled, at any K (these tiles, then those of 128 x 128): 12544 x 768 (147 tiles) 13.5 and 15.6 with K = 768, 43 and 53
+//     with 4096; 2048 x 4096 x 4096 (128): 46 and 38; 8448 x 2048 (264, a second round that is nearly empty) 26.1 and 22.8, 93 and 82;
+//     11008 x 2048 (344) 26.5 and 26.3, 94.3 and 93.7; 12800 x 1792 (350) 26.6 and 26.3, 93 and 97; 25088 x 1024 (392) 26 and 30,
+//     102 and 131
+//     and tiles that are more than half inside y both ways: 65536 x 128 x 1024 18.9 and 16.5, 65536 x 136 x 1024 20.8 and 22.5;
+//     128 x 50000 x 768 15.8 and 12.3, 160 x 50000 x 768 16.3 and 22.1
 bool fp8_wide(int M, int N)
 {
+    if (M <= kWideM / 2 || N <= kWideN / 2) return false;
     const long long tiles = fp8_tiles(M, N, kWideM, kWideN), rounds = (tiles + kComputeUnits - 1) / kComputeUnits;
     return 5 * (tiles + 64) >= 4 * kComputeUnits * rounds;
 }
@@ -108,7 +114,7 @@ int avion_linear_fp8(const void* x8, const float* x_scale, const void* w8, const
         // 50176 x 2304 x 768 88 and 112)
         if (fp8_wide(m, N) && N % 64 == 0) return launch_wide<E, true>(x, x_scale, w, w_scale, bias, out, m, N, K, st);
         if (fp8_wide(m, N)) return launch_wide<E, false>(x, x_scale, w, w_scale, bias, out, m, N, K, st);
-        if (fp8_tiles(m, N, 128, 128) >= kComputeUnits)
+        if (N > 64 && fp8_tiles(m, N, 128, 128) >= kComputeUnits)
             return launch_fp8<128, 128, 2, 2, 2, 1, E>(x, x_scale, w, w_scale, bias, out, m, N, K, st);
         if (fp8_tiles(m, N, 64, 64) > kComputeUnits && fp8_tiles(m, N, 128, 64) <= kComputeUnits && K >= 4096)
             return launch_fp8<128, 64, 2, 2, 3, 2, E>(x, x_scale, w, w_scale, bias, out, m, N, K, st);

@@ -8,7 +8,7 @@ import numpy as np
 import pytest
 
 from oracle import text_ops as ops
-from tests.test_text_ops_gpu import BF, E, FP, HF, U, _rows8_check, f64, randn, within
+from tests.test_text_ops_gpu import BF, E, FP, HF, U, _linear_check, _rows8_check, f64, randn, within
 
 pytestmark = pytest.mark.gpu
 
@@ -94,6 +94,13 @@ def test_norm_in_8_bits_is_the_nearest_of_the_least_values(M, D, fmt, stream):
     near = torch.round(steps) * torch.exp2(e - 3)
     off = (q.double().abs() != near) & ~open_side
     assert not off.any(), (int(off.sum()), v[off][:4], q.double().abs()[off][:4])
+
+
+# narrow and short y with many tiles: half a tile of 256 x 256 and less, 64 columns
+@pytest.mark.parametrize("M,N,K", [(36001, 64, 80), (36865, 72, 144), (40001, 128, 96), (40001, 136, 48), (33, 40000, 64), (128, 40000, 80), (129, 40000, 48)])
+@pytest.mark.parametrize("fmt,bias", [(BF, True), (HF, False)])
+def test_linear_narrow_and_short(M, N, K, fmt, bias):
+    _linear_check(M, N, K, fmt, bias, seed=M + N)
 
 
 # --------------------------------------------------------------------------------------------- RMS normalisation
