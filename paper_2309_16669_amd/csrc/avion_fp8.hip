@@ -42,8 +42,10 @@ int launch_fp8(const char* x8, const float* xs, const char* w8, const float* ws,
 }
 
 // Which kernel (us, kernel alone):
-//   up to 16 rows (32 where K is at most 2048): straight from memory.  16 x 6144 x 4096: 11.2, tiles of 64 x 64 12.9;
-//     32 x 1024 x 1024: 4.1 and 5.3, but 32 x 6144 x 4096: 14.4 and 12.8.
+//   up to 16 rows, and up to 32 where each compute unit has one workgroup at most (N up to 4096): straight from memory.  K = 1024
+//     and 4096, then tiles of 64 x 64: 32 x 4096 3.9, 8.7 and 4.6, 9.9; 32 x 4608 5.2, 13.8 and 4.7, 9.9; 17 x 4608 4.5, 11.2 and
+//     4.6, 9.9; 16 x 4608 4.0, 10.1 and 4.5, 9.8; 8 x 8192 4.0, 9.1 and 4.9, 10.0.  (Up to 16 rows and N past 8192 either may be
+//     faster: 1 x 12288 6.0, 13.0 and 5.6, 10.4; 1 x 50000 14.7, 40 and 13.4, 53.)
 //   else the smallest tiles that leave no more than one for a compute unit (latency), larger ones beyond (traffic):
 //     64 x 64 and 128 x 64 on 1024 x 1024 x 1024 (256 tiles): 6.0 and 6.9, on 512 x 4096 x 4096 (512): 21.8 and 17.5;
 //     with eight wavefronts, half of K each, where K is long: 64 x 6144 x 4096: 13.3 -> 10.7, 64 x 2304 x 768: 4.8 and 4.8;
@@ -109,7 +111,7 @@ int avion_linear_fp8(const void* x8, const float* x_scale, const void* w8, const
     return by_element(flags, [&](auto fmt) {
         using E = typename decltype(fmt)::type;
         if (m <= 16) return launch_few<1, E>(x, x_scale, w, w_scale, bias, out, m, N, K, st);
-        if (m <= 32 && K <= 2048) return launch_few<2, E>(x, x_scale, w, w_scale, bias, out, m, N, K, st);
+        if (m <= 32 && N <= 16 * kComputeUnits) return launch_few<2, E>(x, x_scale, w, w_scale, bias, out, m, N, K, st);
         // (stores past the caches only where rows are whole cache lines: 30000 x 1544 x 768 67.6 us with them, 54.8 without,
         // 50176 x 2304 x 768 88 and 112)
         if (fp8_wide(m, N) && N % 64 == 0) return launch_wide<E, true>(x, x_scale, w, w_scale, bias, out, m, N, K, st);

@@ -103,6 +103,13 @@ def test_linear_narrow_and_short(M, N, K, fmt, bias):
     _linear_check(M, N, K, fmt, bias, seed=M + N)
 
 
+# up to 32 rows, around the width from which tiles take them
+@pytest.mark.parametrize("M,N,K", [(17, 4096, 2064), (32, 4096, 4096), (32, 4104, 2048), (17, 4104, 272), (24, 6144, 1040), (32, 33000, 48)])
+@pytest.mark.parametrize("fmt,bias", [(BF, True), (HF, False)])
+def test_linear_few_rows(M, N, K, fmt, bias):
+    _linear_check(M, N, K, fmt, bias, seed=M + K)
+
+
 # --------------------------------------------------------------------------------------------- RMS normalisation
 def test_norm_of_rows_near_the_least_numbers():
     """A mean of squares (with eps) below fp32's least normal number, 2^-126: rows of zeros under such an eps stay zeros, and rows
