@@ -432,7 +432,7 @@ avion_quantize_rows_kernel(const raw16* __restrict__ x, void* __restrict__ y, fl
 // workgroup's partial sums of the gains' gradient into part[blockIdx.x][D].  dh may be absent.  FEW: few rows, in one launch:
 // the workgroups behind the first row_wgs sum 64 columns of the gains' gradient each over all rows, which they read once more
 // (rstd is known, so they need nothing of the others), into dweight.
-constexpr int kRmsFewCols = 64;
+constexpr int kRmsFewCols = 64, kRmsFewRows = 640;
 template <int LANES, int NCH, typename E, typename R, bool FEW>
 __global__ void __launch_bounds__(RmsWork<LANES>::WAVES * 64)
 avion_rmsnorm_bwd_kernel(const void* __restrict__ h, const float* __restrict__ weight, const float* __restrict__ rstd,

@@ -208,9 +208,10 @@ int avion_rmsnorm_bwd(const void* h, const float* weight, const float* rstd, con
     float* part = static_cast<float*>(workspace);
     const unsigned grid = rms_grid(M, D);
     // One launch where the gains' gradient can read the rows once more at little cost (they are in the caches then): a launch
-    // and its kernel less (this call on 4 x 64: 7.6 -> 4.0 us of the host's time).  On the GPU 300 x 1024 takes 4.0 us, and the
-    // two ways meet near 1000 rows, whose sums are a chain of 8 loads there (1000 x 768 8.5, in two launches 1500 x 1024 9.2).
-    const bool few = M > 0 && M <= 1024 && M * D <= (1 << 20);
+    // and its kernel less (this call on 4 x 64: 7.6 -> 4.0 us of the host's time).  On the GPU, one launch and two: 300 x 1024 4.0
+    // and 6.6, 640 x 64 5.1 and 5.0, x 768 5.4 and 6.2, x 2048 7.9 and 8.8, x 16384 22.4 and 34.9; 704 x 64 5.8 and 5.0, x 768 6.0
+    // and 6.6, x 1536 8.1 and 8.0; 800 x 768 7.2 and 6.7; 1024 x 64 7.1 and 5.0, x 768 9.4 and 7.0 (a chain of 8 loads).
+    const bool few = M > 0 && M <= kRmsFewRows;
     if (M > 0) {
         const int r1 = by_element(flags, [&](auto fmt) {
             using E = typename decltype(fmt)::type;

@@ -8,7 +8,7 @@ import numpy as np
 import pytest
 
 from oracle import text_ops as ops
-from tests.test_text_ops_gpu import BF, E, FP, HF, U, _linear_check, _rows8_check, f64, randn, within
+from tests.test_text_ops_gpu import BF, E, FP, HF, U, _linear_check, _norm_check, _rows8_check, f64, randn, within
 
 pytestmark = pytest.mark.gpu
 
@@ -135,6 +135,17 @@ def test_norm_of_rows_near_the_least_numbers():
         within("y", y, ref, (U[BF] + (D / 2 + 12) * E + lost) * np.abs(ref))
         q, s, h = ag.add_rms_norm_fp8(zeros, r, w, 0.0)
         _rows8_check(ref, q, s, (D / 2 + 20) * E + float(lost.max()))
+
+
+# the gains' gradient in the same launch, and in one of its own
+@pytest.mark.parametrize("M", [639, 640, 641])
+@pytest.mark.parametrize("D", [64, 136, 768, 2056, 8200])
+def test_norm_around_one_launch(M, D):
+    _norm_check(M, D, BF, FP, seed=M + D)
+
+
+def test_norm_of_the_widest_rows_in_one_launch():
+    _norm_check(600, 16384, HF, HF, seed=5)
 
 
 # ---------------------------------------------------------------------------------------------------- addresses
