@@ -300,7 +300,8 @@ int avion_column_sum(const void *x, void *sum, long long M, int F, unsigned flag
  *   workspace (backward): 256-byte aligned, avion_embedding_bwd_workspace_bytes(n, V, D) bytes, contents ignored and left
  *   unspecified; calls that overlap in time must not share one
  * The gradient sorts the slots by token and sums each token's rows in fp32 in a fixed order, rounded once: no atomics on
- * floating-point values, bit-reproducible, whatever share of the slots one token fills.  The tokens must not change
+ * floating-point values, whatever share of the slots one token fills.  The same n and tokens give the same bits; the order
+ * depends on both, so slots that are added elsewhere may change a row's last bits.  The tokens must not change
  * while the call runs.  n = 0: y is not touched, dtable becomes zeros.
  */
 #define AVION_FLAG_WIDE_F32 8u
@@ -330,8 +331,10 @@ int avion_embedding_bwd(const void *tokens, const void *dy, void *dtable, long l
  *                      it dx is the gradient of both inputs.
  *   M >= 0; D a multiple of 8, at most 16384; eps finite and >= 0
  *   workspace (backward): 256-byte aligned, avion_rmsnorm_bwd_workspace_bytes(M, D) bytes (at most 512 * D floats)
- * Statistics and sums in fp32 (the sum of a row's squares has to be finite there), outputs rounded once; no atomics,
- * bit-reproducible.  M = 0 writes zeros to dweight and nothing else.  Pointers 16-byte aligned.
+ * Statistics and sums in fp32 (the sum of a row's squares and, in the backward, dy * weight have to be finite there; squares
+ * below 2^-149 vanish, and a row whose squares and eps all do is not finite), outputs rounded once.  No atomics: the same sizes
+ * give the same bits (M decides how a row is summed, so a row's last bits may differ between calls of different M).
+ * M = 0 writes zeros to dweight and nothing else.  Pointers 16-byte aligned.
  */
 int avion_rmsnorm_fwd(const void *x, const void *residual, const float *weight, void *y, void *h, float *rstd,
                       long long M, int D, float eps, unsigned flags, void *stream);
@@ -363,9 +366,9 @@ int avion_quantize_rows(const void *x, void *x8, float *scale, long long M, int 
  *   bias : in, fp32 [N] or NULL;   y : out, [M, N] bf16 (fp16 with AVION_FLAG_F16), fully overwritten
  *   M >= 0 (0: nothing happens); N a multiple of 8 up to 2^20; K a multiple of 16 up to 65536; M below 2^31 - 256 and at most
  *   2^24 tiles of 64 x 64 in y; pointers 16-byte aligned, x_scale's 4-byte (rows of a larger tensor)
- * fp32 sums, scaled and rounded once.  The matrix unit first adds 8 products of neighbouring k, dropping of each what lies
+ * fp32 sums, times x_scale (finite), times w_scale, in fp32, rounded once.  The matrix unit first adds 8 products of neighbouring k, dropping of each what lies
  * below 2^-13 of the largest one's power of two (measured; 2^-5 and more separate the operands from what they were rounded
- * from).  No workspace; bit-reproducible.
+ * from).  No workspace; the same sizes give the same bits (M, N and K decide how K is cut).
  */
 int avion_linear_fp8(const void *x8, const float *x_scale, const void *w8, const float *w_scale, const float *bias,
                      void *y, long long M, int N, int K, unsigned flags, void *stream);

@@ -1,13 +1,15 @@
 // Token table: lookup with scaling, and the table's gradient by sorted tokens.
-//     y_i = s W[t_i];     dW[v] = s sum over i with t_i = v, in ascending i, of dy_i
+//     y_i = s W[t_i];     dW[v] = s sum over i with t_i = v of dy_i, in an order that n and the tokens fix
 // A token outside [0, V) names no row: its y is zero and it adds to no gradient (padding, another device's share of a table).
 //
 // Lookup: bound by memory bandwidth, one read of a row and one write; a thread moves 16-byte pieces, four in flight, and writes
-// past the caches (y is not read again before the next kernel, the table's rows are): 157696 x 512 from 50000 rows 49 -> 28.6 us,
-// 5.6 TB/s written.
+// past the caches (y is not read again before the next kernel, the table's rows are).  Captions of 512 columns from 50000 rows, us, past
+// the caches and through them: 157696 slots 29.7 (5.4 TB/s written) and 41.8, 78848 16.4 and 18.6, 4928 3.7 and 3.7; together with
+// the norm that reads y next 103 and 108, 54.5 and 49.3, 9.3 and 8.8: what y leaves in the caches is worth more than the lookup
+// gains up to about 80 MB of it.
 //
 // Gradient: reads dy once and writes every row of dW once (rows that no token names: zeros).  Floating-point sums in a fixed
-// order, no atomics on them: results are bit-reproducible.
+// order, no atomics on them: the same n and tokens give the same bits.
 //   up to kEmbSmallTokens tokens: one launch.  A workgroup per (slot, 512 columns) ends at once unless its slot is the first
 //   with its token; else it collects the slots with that token, in order, and sums their rows.  Further workgroups clear the
 //   rows that no token names.
@@ -23,8 +25,8 @@
 // Both sides at the borders (table 50000 x 512, us): one launch and sorted 700 slots 13.4 and 16.5, 1000 slots, 3/4 of them one
 // token's, 19.3 and 18.0; counting and radix 8000 slots 32 and 36, 9000 34 and 35, 12000 40 and 36; 8 and 32 slots a wavefront in
 // the sums 20000 slots 41 and 45, 40000 47 and 47, 130000 79 and 66.
-// 157696 slots of 512 columns into 50000 rows: 73 us, of these the sums 34 (5.1 TB/s of dy and dW), counting and placing
-// 4.3 + 9.8 and 4.4 + 10.8 (half of the unnamed rows cleared beside each placing), the join 9.6 (chains of latency: padding is one token's).
+// 157696 slots of 512 columns into 50000 rows: 71 us, of these the sums 34 (5.1 TB/s of dy and dW), counting and placing
+// 4.2 + 9.8 and 4.1 + 10.2 (half of the unnamed rows cleared beside each placing), the join 9.0 (chains of latency: padding is one token's).
 // First version 118.
 #pragma once
 #include "avion_common.h"

@@ -294,9 +294,12 @@ avion_linear_fp8_kernel(const char* __restrict__ x8, const float* __restrict__ x
 //   AHEAD, for long K: w8's half of a buffer, whose rows are all in registers from the middle of a step on, is filled again from
 //   there, behind a barrier of its own.  50176 x 1024 x 4096 220 -> 202 us, 50176 x 768 x 2304 99 -> 92, 8192 cubed 434 -> 416;
 //   with fewer steps a tile it gives nothing or costs: 25088 x 2048 x 1536 89 and 90, 12544 x 4096 x 1024 65 and 68.
-// Bound by the loads of one step, which is all that two buffers of 64 KB leave in flight: on 50176 x 2304 x 768 (88 to 96 us, 1.9
-// PFLOP/s and 2.9 TB/s of its bytes) the matrix units work 35 % of the cycles and LDS answers reads in 23 %; without loads it
-// takes 80 us, without contractions 69, without stores 7 less.  8192 cubed: 2.64 PFLOP/s.
+// Bound by two things in turn.  50176 x 2304 x K, back to back and without AHEAD, takes 65, 82, 102, 122 and 166 us at K = 256, 512,
+// 768, 1024 and 1536: 9.6 us a step of K and 46 that do not depend on it.  A step of a tile is 1.4 us, 0.85 of them contractions; the rest
+// waits for its loads, all that two buffers of 64 KB leave in flight.  The 46, 6.6 us for each of a workgroup's seven tiles, are the
+// scaling, exchange and stores of y (44 at the copy's rate), beside which nobody contracts.  No part alone is the bound: at K = 768
+// it takes 80 us without loads, 69 without contractions, 7 less without stores.  That case: 93 (in the profiler) to 102 us, 1.9 to
+// 1.7 PFLOP/s, matrix units 35 % of the cycles, LDS reads 24 %.  8192 cubed: 2.64 PFLOP/s.
 constexpr int kWideM = 256, kWideN = 256, kWideK = 128, kWideWaves = 8, kWideGroup = 8;
 constexpr int kWideStage = (kWideM + kWideN) * kWideK, kWideScales = 3 * 1024, kWideRow = 144;
 constexpr int kWideLds = 2 * kWideStage + 3 * kWideScales + kWideWaves * 16 * kWideRow;

@@ -48,9 +48,10 @@ int launch_fp8(const char* x8, const float* xs, const char* w8, const float* ws,
 //     faster: 1 x 12288 6.0, 13.0 and 5.6, 10.4; 1 x 50000 14.7, 40 and 13.4, 53.)
 //   else the smallest tiles that leave no more than one for a compute unit (latency), larger ones beyond (traffic):
 //     64 x 64 and 128 x 64 on 1024 x 1024 x 1024 (256 tiles): 6.0 and 6.9, on 512 x 4096 x 4096 (512): 21.8 and 17.5;
-//     with eight wavefronts, half of K each, where K is long: 64 x 6144 x 4096: 13.3 -> 10.7, 64 x 2304 x 768: 4.8 and 4.8;
-//     128 x 64 in this way, where there is one for a compute unit at most: 2048 x 1024 x 4096 16.6 -> 15.0, 3000 x 640 x 8192
-//     29 -> 25, but 1570 x 1000 x 1280 7.7 -> 8.1 (1024 x 2048 x 2048 as long either way);
+//     with eight wavefronts, half of K each, where K is long: 64 x 2304 with K = 512 3.8 and 3.8, 768 4.4 and 4.2, 1024 5.0 and 4.6,
+//     4096 12.7 and 9.9, 1024 x 1024 with K = 512 4.1 and 4.2, 1024 5.7 and 5.4;
+//     128 x 64 in this way, where there is one for a compute unit at most: 2048 x 1024 with K = 1280 7.7 and 8.2, 2048 9.8 and 9.9,
+//     3584 14.7 and 13.9, 4096 16.2 and 14.8; 1024 x 2048 with 3584 14.7 and 14.5; 3000 x 640 x 8192 28.6 and 24.9;
 //     128 x 64 and 128 x 128 on 785 x 2304 x 768 (126 tiles of 128 x 128): 6.8 and 8.7, on 1570 x 3840 x 1280 (390): 19.3 and 16.2
 //     and 128 x 128 only where y has more than 64 columns: 36864 x 64 x 1024 11.4 and 12.5, 36864 x 72 x 1024 13.5 and 12.6
 //   256 x 256: a round of its 256 tiles takes about as long as 820 tiles of 128 x 128 in a long row and less to begin with, so it
@@ -112,8 +113,8 @@ int avion_linear_fp8(const void* x8, const float* x_scale, const void* w8, const
         using E = typename decltype(fmt)::type;
         if (m <= 16) return launch_few<1, E>(x, x_scale, w, w_scale, bias, out, m, N, K, st);
         if (m <= 32 && N <= 16 * kComputeUnits) return launch_few<2, E>(x, x_scale, w, w_scale, bias, out, m, N, K, st);
-        // (stores past the caches only where rows are whole cache lines: 30000 x 1544 x 768 67.6 us with them, 54.8 without,
-        // 50176 x 2304 x 768 88 and 112)
+        // (stores past the caches only where rows are whole cache lines: 30000 x 1544 x 768 65.9 us with them, 55.4 without,
+        // 50176 x 2304 x 768 106 and 116, 50176 x 2304 x 2304 244 and 243, 12544 x 4096 x 1024 65.6 and 64.4)
         if (fp8_wide(m, N) && N % 64 == 0) return launch_wide<E, true>(x, x_scale, w, w_scale, bias, out, m, N, K, st);
         if (fp8_wide(m, N)) return launch_wide<E, false>(x, x_scale, w, w_scale, bias, out, m, N, K, st);
         if (N > 64 && fp8_tiles(m, N, 128, 128) >= kComputeUnits)
