@@ -374,6 +374,67 @@ int avion_linear_fp8(const void *x8, const float *x_scale, const void *w8, const
                      void *y, long long M, int N, int K, unsigned flags, void *stream);
 
 /*
+ * Rotary positions: pairs of a head's channels turned by the angle of their token's position, on one to four axes (time, height
+ * and width of a video's tokens; one for text).  Pair j of the first 2 * pairs channels belongs to axis a(j): the first sections[0]
+ * pairs to axis 0, the next sections[1] to axis 1, ...
+ *     theta = positions[a(j)][t mod P] * freqs[j];  y1 = x1 cos theta - x2 sin theta;  y2 = x2 cos theta + x1 sin theta
+ *   q, yq     : [T, Hq, d] bf16 (fp16 with AVION_FLAG_F16); k, yk: [T, Hk, d], Hk = 0 for none.  Token rows of q and k are rs_q and
+ *               rs_k elements apart (slices of a joint projection), heads d apart; yq and yk are contiguous.  yq may be q, and yk k,
+ *               where that is contiguous too; else outputs must not overlap inputs
+ *   positions : [axes, P] int64 (int32 with AVION_FLAG_TOKENS_I32, fp32 with AVION_FLAG_POSITIONS_F32: places between frames); token
+ *               t has the positions of t mod P (a batch of clips of P tokens each); P divides T
+ *   freqs     : fp32 [pairs], radians a step;   sections: `axes` numbers on the HOST, their sum is `pairs`
+ *   Pairs are channels j and pairs + j, or with AVION_FLAG_INTERLEAVED 2 j and 2 j + 1.  Channels from 2 * pairs on are copied.
+ *   AVION_FLAG_INVERSE: -theta, the backward (the gradient of q is the inverse turn of the gradient of yq).
+ *   d a multiple of 8 up to 4096; pairs a multiple of 8 up to 512, 2 * pairs <= d; axes <= 4; T < 2^31 - 8; rs a multiple of 8
+ * Angles are formed in 64 bits and reduced to one turn before they are rounded, so far positions lose nothing; one rounding of the
+ * result.  T = 0: nothing happens.  Pointers 16-byte aligned (positions and freqs naturally).
+ */
+#define AVION_FLAG_INTERLEAVED 32u
+#define AVION_FLAG_INVERSE 64u
+#define AVION_FLAG_POSITIONS_F32 128u
+
+int avion_rotary(const void *q, const void *k, const void *positions, const float *freqs, void *yq, void *yk,
+                 long long T, long long P, int Hq, int Hk, int d, int pairs, const int *sections, int axes,
+                 long long rs_q, long long rs_k, unsigned flags, void *stream);
+
+/*
+ * Attention over S sequences of different lengths that lie one after the other, without padding between them: the captions or the
+ * videos of a batch, prompts, single tokens behind a cache.  Query head h reads key head h / (Hq / Hk).
+ *   q, o, dO, dq : [Tq, Hq, d];  k, v, dk, dv : [Tk, Hk, d]; bf16 (fp16 with AVION_FLAG_F16).  Hk divides Hq; d = 64, 80 or 128.
+ *                  Token rows of q, k and v are rs_q, rs_k, rs_v elements apart (multiples of 8), heads d apart; the others are
+ *                  contiguous.  Outputs must not overlap inputs or each other
+ *   offsets_q    : [S + 1] int32 on the device, non-decreasing: sequence s has queries offsets_q[s] .. offsets_q[s+1] - 1
+ *   offsets_k    : the same of the keys (may be the same array).  Lengths may be 0 on either side
+ *   lse          : fp32 [Hq, Tq]
+ *   AVION_FLAG_CAUSAL: query i of nq sees the keys up to i + nk - nq (the last query stands beside the last key)
+ * A query that sees no key has o = 0 and lse = -inf and gets no gradient.  Rows that belong to no sequence (before the first
+ * offset, from the last one on) have o = 0 and lse = -inf, and gradients 0.  What a sequence holds reaches no other one.  Within a
+ * sequence infinities and NaN are not checked and propagate, past a mask too.  Offsets are not checked: values outside 0 .. T are
+ * taken as the nearest of these, and decreasing ones give rows without a defined value, never an access outside the tensors.
+ *   Tq, Tk up to 2^28, S up to 2^20, Tq * Hq / Hk up to 2^30; scale as for avion_attn_fwd
+ *   workspace: 256-byte aligned, avion_ragged_fwd_workspace_bytes / _bwd_workspace_bytes bytes of these sizes (0: unsupported),
+ *   contents ignored and left unspecified; calls that overlap in time must not share one.  The forward's may be NULL where every
+ *   sequence has as many queries as keys.
+ * Arithmetic as avion_attn_fwd and _bwd (sums, statistics and LSE in fp32; weights and dS rounded to the format before a product),
+ * with a running maximum; no atomics: the same sizes and offsets give the same bits.
+ */
+size_t avion_ragged_fwd_workspace_bytes(long long Tq, long long Tk, long long S, int Hq, int Hk, int d);
+
+int avion_ragged_fwd(const void *q, const void *k, const void *v, const int *offsets_q, const int *offsets_k,
+                     void *o, float *lse, long long Tq, long long Tk, long long S, int Hq, int Hk, int d,
+                     long long rs_q, long long rs_k, long long rs_v, float scale, unsigned flags,
+                     void *workspace, size_t workspace_bytes, void *stream);
+
+size_t avion_ragged_bwd_workspace_bytes(long long Tq, long long Tk, long long S, int Hq, int Hk, int d);
+
+int avion_ragged_bwd(const void *q, const void *k, const void *v, const int *offsets_q, const int *offsets_k,
+                     const void *o, const float *lse, const void *dO, void *dq, void *dk, void *dv,
+                     long long Tq, long long Tk, long long S, int Hq, int Hk, int d,
+                     long long rs_q, long long rs_k, long long rs_v, float scale, unsigned flags,
+                     void *workspace, size_t workspace_bytes, void *stream);
+
+/*
  * Allocation-free backward, for callers that cannot provide device scratch of their own: code
  * under HIP graph capture, tight serving or training loops, harnesses that forbid hipMalloc.
  * Same operation, arguments, rules and bits as avion_attn_bwd (bf16, not causal), without the

@@ -16,6 +16,7 @@ LIB_PATH = os.path.join(_PKG, "libavion_attn.so")
 
 OK, EINVAL, EUNSUPPORTED, EWORKSPACE, EHIP, ESCRATCH = 0, -1, -2, -3, -4, -5
 FLAG_F16, FLAG_CAUSAL, FLAG_QKVPACKED, FLAG_WIDE_F32, FLAG_TOKENS_I32 = 1, 2, 4, 8, 16
+FLAG_INTERLEAVED, FLAG_INVERSE, FLAG_POSITIONS_F32 = 32, 64, 128
 
 _lib = None
 
@@ -108,6 +109,15 @@ def load_library() -> ctypes.CDLL:
         lib.avion_quantize_rows.argtypes = [p, p, p, ll, i, u, p]
         lib.avion_linear_fp8.restype = i
         lib.avion_linear_fp8.argtypes = [p, p, p, p, p, p, ll, i, i, u, p]
+        lib.avion_rotary.restype = i
+        lib.avion_rotary.argtypes = [p, p, p, p, p, p, ll, ll, i, i, i, i, p, i, ll, ll, u, p]
+        for entry in (lib.avion_ragged_fwd_workspace_bytes, lib.avion_ragged_bwd_workspace_bytes):
+            entry.restype = sz
+            entry.argtypes = [ll, ll, ll, i, i, i]
+        lib.avion_ragged_fwd.restype = i
+        lib.avion_ragged_fwd.argtypes = [p, p, p, p, p, p, p, ll, ll, ll, i, i, i, ll, ll, ll, f, u, p, sz, p]
+        lib.avion_ragged_bwd.restype = i
+        lib.avion_ragged_bwd.argtypes = [p, p, p, p, p, p, p, p, p, p, p, ll, ll, ll, i, i, i, ll, ll, ll, f, u, p, sz, p]
         _lib = lib
     return _lib
 
@@ -576,3 +586,95 @@ def linear_fp8(x8, x_scale, w8, w_scale, bias, y, stream=None) -> None:
     _require(y, "y", y.dtype, (M, N))
     _launch(_one_device(x8, x_scale, w8, w_scale, bias, y), load_library().avion_linear_fp8,
             (_ptr(x8), _ptr(x_scale), _ptr(w8), _ptr(w_scale), _opt(bias), _ptr(y), M, N, K, _flags(y.dtype, False, False)), stream)
+
+
+def _heads(t, name, dtype, rows=None, H=None, d=None):
+    """Token rows [T, H, d] whose heads are contiguous: the elements between two rows."""
+    if not t.is_cuda:
+        raise ValueError(f"{name} must live on the GPU")
+    if t.dtype != dtype:
+        raise ValueError(f"{name} must be {dtype}, got {t.dtype}")
+    if t.dim() != 3 or any(want is not None and have != want for have, want in zip(t.shape, (rows, H, d))):
+        want = tuple("any" if n is None else n for n in (rows, H, d))
+        raise ValueError(f"{name} must have shape {want}, got {tuple(t.shape)}")
+    if t.shape[2] > 1 and t.stride(2) != 1 or t.shape[1] > 1 and t.stride(1) != t.shape[2]:
+        raise ValueError(f"{name}: the channels and heads of a token must be contiguous")
+    return t.stride(0) if t.shape[0] > 1 else t.shape[1] * t.shape[2]
+
+
+def _positions_flag(positions) -> int:
+    import torch
+    flags = {torch.int64: 0, torch.int32: FLAG_TOKENS_I32, torch.float32: FLAG_POSITIONS_F32}
+    if positions.dtype not in flags:
+        raise ValueError(f"positions must be int64, int32 or float32, got {positions.dtype}")
+    return flags[positions.dtype]
+
+
+def rotary(q, k, positions, freqs, sections, yq, yk, interleaved: bool = False, inverse: bool = False, stream=None) -> None:
+    """avion_rotary: q [T, Hq, d] and k [T, Hk, d] (or None) bf16 or fp16, heads contiguous, token rows of any stride; positions int64,
+    int32 or fp32 [axes, P] with P dividing T; freqs fp32 [pairs]; sections: the pairs of each axis; yq, yk [T, H, d] contiguous."""
+    import torch
+    T, Hq, d = q.shape
+    rs_q = _heads(q, "q", q.dtype)
+    rs_k = 0 if k is None else _heads(k, "k", q.dtype, T, None, d)
+    flags = _flags(q.dtype, False, False) | _positions_flag(positions)
+    sections = tuple(int(n) for n in sections)
+    _require(positions, "positions", positions.dtype, (len(sections), positions.shape[-1]))
+    _require(freqs, "freqs", torch.float32, (sum(sections),))
+    _require(yq, "yq", q.dtype, (T, Hq, d))
+    if (k is None) != (yk is None):
+        raise ValueError("k and yk are given together or not at all")
+    if k is not None:
+        _require(yk, "yk", q.dtype, tuple(k.shape))
+    _launch(_one_device(q, k, positions, freqs, yq, yk), load_library().avion_rotary,
+            (_ptr(q), _opt(k), _ptr(positions), _ptr(freqs), _ptr(yq), _opt(yk), T, positions.shape[1], Hq, 0 if k is None else k.shape[1], d,
+             sum(sections), (ctypes.c_int * max(1, len(sections)))(*sections), len(sections), rs_q, rs_k,
+             flags | (FLAG_INTERLEAVED if interleaved else 0) | (FLAG_INVERSE if inverse else 0)), stream)
+
+
+def _ragged_inputs(q, k, v, offsets_q, offsets_k):
+    import torch
+    (Tq, Hq, d), (Tk, Hk, _) = q.shape, k.shape
+    strides = _heads(q, "q", q.dtype), _heads(k, "k", q.dtype, None, None, d), _heads(v, "v", q.dtype, Tk, Hk, d)
+    (n,) = offsets_q.shape
+    if n < 1:
+        raise ValueError("offsets_q must hold at least one number")
+    _require(offsets_q, "offsets_q", torch.int32, (n,))
+    _require(offsets_k, "offsets_k", torch.int32, (n,))
+    return (Tq, Tk, n - 1, Hq, Hk, d), strides
+
+
+def ragged_fwd_workspace_bytes(Tq: int, Tk: int, S: int, Hq: int, Hk: int, d: int) -> int:
+    return int(load_library().avion_ragged_fwd_workspace_bytes(Tq, Tk, S, Hq, Hk, d))
+
+
+def ragged_bwd_workspace_bytes(Tq: int, Tk: int, S: int, Hq: int, Hk: int, d: int) -> int:
+    return int(load_library().avion_ragged_bwd_workspace_bytes(Tq, Tk, S, Hq, Hk, d))
+
+
+def ragged_fwd(q, k, v, offsets_q, offsets_k, o, lse, scale: float, workspace, causal: bool = False, stream=None) -> None:
+    """avion_ragged_fwd: q [Tq, Hq, d], k and v [Tk, Hk, d] bf16 or fp16, heads contiguous, token rows of any stride; offsets int32
+    [S + 1]; o [Tq, Hq, d]; lse fp32 [Hq, Tq]."""
+    import torch
+    sizes, strides = _ragged_inputs(q, k, v, offsets_q, offsets_k)
+    _require(o, "o", q.dtype, tuple(q.shape))
+    _require(lse, "lse", torch.float32, (q.shape[1], q.shape[0]))
+    _require(workspace, "workspace", torch.uint8)
+    _launch(_one_device(q, k, v, offsets_q, offsets_k, o, lse, workspace), load_library().avion_ragged_fwd,
+            (_ptr(q), _ptr(k), _ptr(v), _ptr(offsets_q), _ptr(offsets_k), _ptr(o), _ptr(lse), *sizes, *strides, float(scale),
+             _flags(q.dtype, causal, False), _ptr(workspace), workspace.numel()), stream)
+
+
+def ragged_bwd(q, k, v, offsets_q, offsets_k, o, lse, dO, dq, dk, dv, scale: float, workspace, causal: bool = False, stream=None) -> None:
+    """avion_ragged_bwd: inputs, o and lse as ragged_fwd had and wrote them; dO and dq like o, dk and dv [Tk, Hk, d] contiguous."""
+    import torch
+    sizes, strides = _ragged_inputs(q, k, v, offsets_q, offsets_k)
+    for t, n in ((o, "o"), (dO, "dO"), (dq, "dq")):
+        _require(t, n, q.dtype, tuple(q.shape))
+    for t, n in ((dk, "dk"), (dv, "dv")):
+        _require(t, n, q.dtype, tuple(k.shape))
+    _require(lse, "lse", torch.float32, (q.shape[1], q.shape[0]))
+    _require(workspace, "workspace", torch.uint8)
+    _launch(_one_device(q, k, v, offsets_q, offsets_k, o, lse, dO, dq, dk, dv, workspace), load_library().avion_ragged_bwd,
+            (_ptr(q), _ptr(k), _ptr(v), _ptr(offsets_q), _ptr(offsets_k), _ptr(o), _ptr(lse), _ptr(dO), _ptr(dq), _ptr(dk), _ptr(dv),
+             *sizes, *strides, float(scale), _flags(q.dtype, causal, False), _ptr(workspace), workspace.numel()), stream)

@@ -41,7 +41,8 @@ from . import (attn_bwd_ex, attn_bwd_workspace_bytes, attn_fwd_ex, bias_gelu_bwd
                bias_gelu_fwd, column_sum, column_sum_workspace_bytes, layernorm_bwd, layernorm_bwd_workspace_bytes, layernorm_fwd, load_library)
 from . import (embedding_bwd, embedding_bwd_workspace_bytes, embedding_fwd, rmsnorm_bwd, rmsnorm_bwd_workspace_bytes, rmsnorm_fwd,
                rmsnorm_fwd_fp8)
-from . import linear_fp8 as _linear_fp8, quantize_rows as _quantize_rows
+from . import linear_fp8 as _linear_fp8, quantize_rows as _quantize_rows, rotary as _rotary
+from . import ragged_bwd, ragged_bwd_workspace_bytes, ragged_fwd, ragged_fwd_workspace_bytes
 
 _native = None
 
@@ -58,7 +59,8 @@ def native_calls():
             warnings.warn(f"paper_2309_16669_amd/_avion_torch.so does not load ({e}); the Python classes take its calls, at "
                           "several times the host time.  Build it: python -c 'import __graft_entry__ as g; g.build()'")
             names = ("attention", "attention_qkvpacked", "layer_norm", "bias_gelu", "bias_gelu_linear", "embedding", "rms_norm",
-                     "add_rms_norm", "rms_norm_fp8", "add_rms_norm_fp8", "quantize_rows", "linear_fp8")
+                     "add_rms_norm", "rms_norm_fp8", "add_rms_norm_fp8", "quantize_rows", "linear_fp8", "rotary", "attention_ragged",
+                     "linear_cross_entropy")
             _avion_torch = types.SimpleNamespace(**{n: lambda *args: None for n in names})
         _native = _avion_torch
     return _native
@@ -444,3 +446,123 @@ def linear_fp8(x8, x_scale, w8, w_scale, bias=None, dtype=torch.bfloat16):
     y = torch.empty((x2.shape[0], w8.shape[0]), dtype=dtype, device=x8.device)
     _linear_fp8(x2, x_scale.contiguous().view(-1), _dense(w8), _dense(w_scale), None if bias is None else _dense(bias), y)
     return y.view(*x8.shape[:-1], w8.shape[0])
+
+
+# --------------------------------------------------- rotary positions, sequences of different lengths, the loss
+def _rows(t):
+    """t as token rows whose heads and channels are contiguous and which begin at multiples of 16 bytes: itself where it is such
+    (a slice of a joint projection), else a copy."""
+    T, H, d = t.shape
+    plain = (d == 1 or t.stride(2) == 1) and (H == 1 or t.stride(1) == d) and (T < 2 or H * d <= t.stride(0) <= 1 << 23 and t.stride(0) % 8 == 0)
+    return t if plain and t.data_ptr() % 16 == 0 else _dense(t)
+
+
+def _turn_rows(q, k, positions, freqs, sections, interleaved, inverse):
+    def rows(t):
+        return None if t is None else _rows(t.reshape(-1, *t.shape[-2:]))
+
+    def out(t):
+        return None if t is None else torch.empty(t.shape, dtype=t.dtype, device=t.device)
+
+    yq, yk = out(q), out(k)
+    _rotary(rows(q), rows(k), positions, freqs, sections, yq.view(-1, *q.shape[-2:]), None if yk is None else yk.view(-1, *k.shape[-2:]),
+            interleaved, inverse)
+    return yq, yk
+
+
+class _Rotary(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, q, k, positions, freqs, sections, interleaved):
+        ctx.save_for_backward(positions, freqs)        # not q, not k
+        ctx.sections, ctx.interleaved = sections, interleaved
+        ctx.set_materialize_grads(False)
+        yq, yk = _turn_rows(q, k, positions, freqs, sections, interleaved, False)
+        return yq if k is None else (yq, yk)
+
+    @staticmethod
+    def backward(ctx, dq, dk=None):
+        positions, freqs = ctx.saved_tensors
+        first, second = (dk, None) if dq is None else (dq, dk)
+        if first is None:
+            return None, None, None, None, None, None
+        a, b = _turn_rows(first, second, positions, freqs, ctx.sections, ctx.interleaved, True)
+        a, b = _depends_on(a, "rotary", first), _depends_on(b, "rotary", second)
+        return (None, a, None, None, None, None) if dq is None else (a, b, None, None, None, None)
+
+
+def rotary_frequencies(pairs, base: float = 10000.0, device=None):
+    """freqs of `rotary`: for each axis of `pairs` (a number, or one a axis) the spectrum base ** (-j / n), j = 0 .. n - 1."""
+    sections = (pairs,) if isinstance(pairs, int) else tuple(pairs)
+    freqs = [float(base) ** (-j / n) for n in sections for j in range(n)]
+    return torch.tensor(freqs, dtype=torch.float32, device=device)
+
+
+def rotary(q, k, positions, freqs, sections=None, interleaved: bool = False):
+    """Queries and keys (bf16 or fp16 [..., H, d], the same leading shape; k may be None) turned by their tokens' positions: pair j of
+    a head's first 2 * len(freqs) channels by positions[axis of j] * freqs[j] radians; the other channels stay.  positions (int64,
+    int32 or float32): one axis, with the leading shape or its last part (then shared over what stands before it: the clips of a
+    batch); with `sections`, the pairs of up to four axes (time, height, width), such a tensor for each axis, stacked.  Pairs are
+    channels j and len(freqs) + j, or neighbours if `interleaved`.  len(freqs) and d are multiples of 8.  Returns (q, k), or q where
+    k is None.  Differentiable once in q and k; keeps neither."""
+    sections = (freqs.shape[0],) if sections is None else tuple(int(n) for n in sections)
+    lead, place = tuple(q.shape[:-2]), tuple(positions.shape)
+    if q.dim() < 3 or (k is not None and tuple(k.shape[:-2]) != lead):
+        raise ValueError(f"q and k must have shape [..., H, d] with the same leading shape, got {tuple(q.shape)} and "
+                         f"{None if k is None else tuple(k.shape)}")
+    if len(sections) > 1 and (not place or place[0] != len(sections)):
+        raise ValueError(f"positions must hold {len(sections)} axes, got shape {place}")
+    own = place[1:] if len(sections) > 1 else place
+    if not own or lead[len(lead) - len(own):] != own:
+        raise ValueError(f"positions of shape {place} do not fit tokens of shape {lead}")
+    if positions.device != q.device or freqs.device != q.device:
+        raise ValueError("tensors must live on one GPU")
+    out = (_native or native_calls()).rotary(q, k, positions, freqs, sections, bool(interleaved))
+    if out is not None:
+        return out
+    if q.numel() == 0:
+        return q.clone() if k is None else (q.clone(), k.clone())
+    return _Rotary.apply(q, k, positions.contiguous().view(len(sections), -1), freqs.contiguous(), sections, bool(interleaved))
+
+
+class _AttentionRagged(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, q, k, v, offsets, offsets_k, scale, causal):
+        q, k, v = _rows(q), _rows(k), _rows(v)
+        (Tq, Hq, d), (Tk, Hk, _) = q.shape, k.shape
+        o = torch.empty((Tq, Hq, d), dtype=q.dtype, device=q.device)
+        lse = torch.empty((Hq, Tq), dtype=torch.float32, device=q.device)
+        ragged_fwd(q, k, v, offsets, offsets_k, o, lse, scale,
+                   _bytes_on(q.device, ragged_fwd_workspace_bytes(Tq, Tk, offsets.shape[0] - 1, Hq, Hk, d)), causal)
+        ctx.save_for_backward(q, k, v, offsets, offsets_k, o, lse)
+        ctx.scale, ctx.causal = scale, causal
+        return o
+
+    @staticmethod
+    def backward(ctx, given):
+        q, k, v, offsets, offsets_k, o, lse = ctx.saved_tensors
+        q, k, v, dO = _rows(q), _rows(k), _rows(v), _dense(given)
+        (Tq, Hq, d), (Tk, Hk, _) = q.shape, k.shape
+        dq, dk, dv = (torch.empty(t.shape, dtype=t.dtype, device=t.device) for t in (q, k, v))
+        ragged_bwd(q, k, v, offsets, offsets_k, o, lse, dO, dq, dk, dv, ctx.scale,
+                   _bytes_on(q.device, ragged_bwd_workspace_bytes(Tq, Tk, offsets.shape[0] - 1, Hq, Hk, d)), ctx.causal)
+        dq, dk, dv = (_depends_on(t, "attention_ragged", given, q, k, v) for t in (dq, dk, dv))
+        return dq, dk, dv, None, None, None, None
+
+
+def attention_ragged(q, k, v, offsets, offsets_k=None, scale: float | None = None, causal: bool = False):
+    """Attention over sequences of different lengths that lie one after the other (captions or videos without padding, prompts, single
+    tokens behind a cache): q [Tq, Hq, d], k and v [Tk, Hk, d], bf16 or fp16, d in {64, 80, 128}, query head h reading key head
+    h // (Hq // Hk).  Sequence s has queries offsets[s] .. offsets[s + 1] - 1 and keys offsets_k[s] .. offsets_k[s + 1] - 1 (offsets_k
+    None: the same); both int32 [S + 1] on the GPU, lengths may be 0.  `causal`: the last query stands beside the last key, query i
+    of n sees the keys up to i + len(keys) - n.  A query that sees none, and a row of no sequence, gives zeros.  scale defaults to
+    1/sqrt(d).  Slices of a joint projection are read where they lie.  Differentiable once in q, k and v."""
+    scale, causal = 1.0 / math.sqrt(q.shape[-1]) if scale is None else float(scale), bool(causal)
+    offsets_k = offsets if offsets_k is None else offsets_k
+    for t, n in ((q, "q"), (k, "k"), (v, "v")):
+        if t.dim() != 3:
+            raise ValueError(f"{n} must have shape [T, H, d], got {tuple(t.shape)}")
+    for t, n in ((offsets, "offsets"), (offsets_k, "offsets_k")):
+        if t.dim() != 1 or t.dtype != torch.int32 or t.device != q.device or t.shape != offsets.shape:
+            raise ValueError(f"{n} must be int32 of shape [S + 1] on the GPU of q, got {t.dtype} {tuple(t.shape)}")
+    o = (_native or native_calls()).attention_ragged(q, k, v, offsets, offsets_k, scale, causal)
+    return _AttentionRagged.apply(q, k, v, offsets.contiguous(), offsets_k.contiguous(), scale, causal) if o is None else o

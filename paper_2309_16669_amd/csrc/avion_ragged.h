@@ -1,0 +1,781 @@
+// Attention over sequences of different lengths that lie one after the other, with query heads that share key heads.
+//
+//   q [Tq, Hq, d], k and v [Tk, Hk, d], G = Hq / Hk query heads a key head; sequence s owns queries bq[s] .. bq[s+1]-1 and keys
+//   bk[s] .. bk[s+1]-1 (nq and nk of them).  Per sequence and head O = softmax(scale Q K^T) V; under a causal mask query i sees the
+//   keys up to i + nk - nq: the last query stands beside the last key, whether the queries are a whole prompt, its end, or one
+//   token behind a cache.  A query that sees no key has O = 0 and LSE = -inf, and no gradient.
+//
+// Rows.  For one key head all G heads of a query read the same keys, so the kernels' rows are (query, head) pairs, row r = query
+// r / G, head r % G: one token of 8 heads is a tile of 8 rows that reads the cache once, and a prompt's tile of 32 rows is 8
+// queries of 4 heads, which all end at nearly the same key.
+//
+// Slots.  How many blocks of BM rows a sequence has is known on the device only.  A launch has floor(T / BM) + S + 2 slots a head,
+// of which sequence s owns those from floor(begin_s / BM) + s on: at least as many as it has blocks.  A workgroup finds its
+// sequence with one 64-way search over the offsets (one wavefront probes 64 of them at a time) and leaves if its block is past the
+// end.  The rows before the first and behind the last offset are two more "sequences", whose outputs become zeros.  Offsets are
+// read as they come: each border is held inside the tensor, so that no content of them leads out of it.
+//
+// Masks.  All keys of a tile beyond the sequence arrive as zero rows; scores that a query must not see become -inf by selection (a
+// NaN among them too) in the units that need it.  Nothing of a sequence is ever multiplied with another's rows, so what one holds
+// (infinities, NaN, an unused slot) cannot reach the next.  Within a sequence a masked key's weight is 0, which NaN and infinity
+// in its value survive, as in avion_attn_fwd.
+#pragma once
+#include "avion_common.h"
+
+struct RaggedArgs {
+    const raw16 *q, *k, *v;
+    const int *off_q, *off_k;
+    long rs_q, rs_k, rs_v;  // token rows of q, k, v, elements apart; of o and the gradients Hq d and Hk d
+    int S, Tq, Tk, Hq, Hk, G;
+    int slots;
+    int causal;
+    float cs, scale;        // scale * log2 e, scale
+};
+
+// border i of 0 .. S + 2: 0, the offsets, T
+DEVINL int ragged_border(const int* off, int S, int T, int i)
+{
+    if (i <= 0) return 0;
+    if (i > S + 1) return T;
+    return min(max(off[i - 1], 0), T);
+}
+struct RaggedPlace {
+    int i;        // interval of the borders (0 and S + 1: rows of no sequence)
+    int begin, n; // its tokens
+    long block;   // of BM rows
+};
+// The interval that owns `slot`, for blocks of 2^SHIFT rows and `mul` rows a token.  Wavefront-uniform.
+template <int SHIFT>
+DEVINL RaggedPlace ragged_place(const int* off, int S, int T, int mul, long slot, int lane)
+{
+    int lo = 0, n = S + 2;
+    while (n > 1) {
+        const int step = (n + 63) / 64, at = lane * step;
+        const bool begun = at < n && (((long)ragged_border(off, S, T, lo + at) * mul) >> SHIFT) + lo + at <= slot;
+        const int c = max((int)__popcll(__ballot(begun)), 1) - 1;
+        lo += c * step;
+        n = min(step, n - c * step);
+    }
+    RaggedPlace p;
+    p.i = __builtin_amdgcn_readfirstlane(lo);
+    p.begin = __builtin_amdgcn_readfirstlane(ragged_border(off, S, T, p.i));
+    p.n = max(__builtin_amdgcn_readfirstlane(ragged_border(off, S, T, p.i + 1)) - p.begin, 0);
+    p.block = slot - (((long)p.begin * mul) >> SHIFT) - p.i;
+    return p;
+}
+
+// Two buffers in LDS of an A and a B tile of 64 token rows each (and, with SCALARS, 64 + 64 floats), filled by LDS-direct loads
+// as TileRing's.  The descriptors begin at the tile's own first row, so that no length of a sequence and no row stride takes a
+// byte offset past 32 bits; rows past the end arrive as zeros.
+template <int D, int NW, bool SCALARS>
+struct RaggedRing {
+    static constexpr int ROWS = 64, STRIDE = tile_stride<D>(), TILE_BYTES = ROWS * STRIDE;
+    static_assert(TILE_BYTES % 1024 == 0, "");
+    static constexpr int NTI = TILE_BYTES / 1024, NBLK = 2 * NTI, NPW = (NBLK + NW - 1) / NW;
+    static constexpr int OFF_B = TILE_BYTES, OFF_SCALARS = 2 * TILE_BYTES;
+    static constexpr int BUF_BYTES = NBLK * 1024 + (SCALARS ? 1024 : 0);
+    static constexpr int LDS_BYTES = 2 * BUF_BYTES + (D % 32 != 0 ? 64 : 0);
+
+    const raw16 *a, *b;
+    const float* scalars;
+    long rs_a, rs_b;
+    int n, wave;
+    unsigned smem_addr, npad_bytes, scalar_voff;
+    unsigned voff[NPW];
+
+    // a, b: first rows, rs_a and rs_b elements apart, n of them; scalars: two arrays npad floats apart
+    DEVINL RaggedRing(const raw16* a_, long rs_a_, const raw16* b_, long rs_b_, const float* scalars_, int npad, int n_, char* smem,
+                      int wave_, int lane)
+        : a(a_), b(b_), scalars(scalars_), rs_a(rs_a_), rs_b(rs_b_), n(n_), wave(wave_), smem_addr(lds_address(smem)),
+          npad_bytes((unsigned)npad * 4)
+    {
+#pragma unroll
+        for (int j = 0; j < NPW; ++j) {
+            const int blk = wave + NW * j;
+            const bool first = blk < NTI;
+            voff[j] = padded_block_voff<D>(first ? blk : blk - NTI, lane, (unsigned)((first ? rs_a : rs_b) * 2));
+        }
+        if constexpr (SCALARS)
+            scalar_voff = lane < 16 ? (unsigned)lane * 16 : lane < 32 ? npad_bytes + (lane - 16) * 16 : kOutOfRangeBase;
+    }
+    // this wavefront's share of the loads of the tile that begins at row r0, into buffer `to`
+    DEVINL void fetch(int r0, int to) const
+    {
+        const int left = min(n - r0, ROWS);
+        const RawBuffer ab(a + (long)r0 * rs_a, left > 0 ? slice_bytes(rs_a, left, D) : 0);
+        const RawBuffer bb(b + (long)r0 * rs_b, left > 0 ? slice_bytes(rs_b, left, D) : 0);
+        const unsigned base = smem_addr + to * BUF_BYTES + wave * 1024;
+#pragma unroll
+        for (int j = 0; j < NPW; ++j) {
+            const int blk = wave + NW * j;
+            if (NBLK % NW != 0 && blk >= NBLK) continue;
+            load_to_lds16(pick(blk < NTI, ab, bb), base + NW * j * 1024, voff[j]);
+        }
+        if constexpr (SCALARS)
+            // (the arrays go on to the next multiple of 64 rows)
+            if (wave == NW - 1) load_to_lds16(RawBuffer(scalars + r0, npad_bytes + 256), smem_addr + to * BUF_BYTES + OFF_SCALARS, scalar_voff);
+    }
+    DEVINL char* at(char* smem, int to) const { return smem + to * BUF_BYTES; }
+    DEVINL static void landed_barrier()
+    {
+        asm volatile("s_waitcnt vmcnt(0)\n\ts_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    }
+};
+
+// Where a lane's row lies: token and head, and how many keys it sees.  Rows past the end stand for the last one.
+struct RaggedRow {
+    int token, head, keys;
+    DEVINL RaggedRow(const RaggedArgs& a, int hk, int row, int rows, int nq, int nk)
+    {
+        const int r = min(row, rows - 1), i = r / a.G;
+        token = i;
+        head = hk * a.G + r - i * a.G;
+        keys = a.causal ? min(max(i + 1 + nk - nq, 0), nk) : nk;
+    }
+};
+
+// 32 result rows (transposed accumulators, lane = row) to their places in a [T, Hq, D] tensor
+template <int D, typename E>
+struct RaggedStore {
+    static constexpr int CT = (D + 31) / 32, STRIDE = D * 2 + 16, BYTES = 32 * STRIDE, CH = D / 8;
+    DEVINL static void run(char* region, const f32x16 (&acc)[CT], float mul, raw16* out, const RaggedArgs& a, int hk, int begin, int row0,
+                           int rows, int lane)
+    {
+        const int l32 = lane % 32, g = lane / 32;
+#pragma unroll
+        for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const int c0 = 32 * ct + 8 * q + 4 * g;
+                if (c0 < D)
+                    *reinterpret_cast<u32x2*>(region + l32 * STRIDE + c0 * 2) =
+                        u32x2{E::pack(acc[ct][4 * q] * mul, acc[ct][4 * q + 1] * mul), E::pack(acc[ct][4 * q + 2] * mul, acc[ct][4 * q + 3] * mul)};
+            }
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+#pragma unroll
+        for (int x = 0; x < (32 * CH + 63) / 64; ++x) {
+            const int idx = lane + 64 * x, row = idx / CH, ch = idx % CH, r = row0 + row;
+            if (idx < 32 * CH && r < rows) {
+                const int i = r / a.G;
+                *reinterpret_cast<u32x4*>(out + ((long)(begin + i) * a.Hq + hk * a.G + r - i * a.G) * D + ch * 8) =
+                    *reinterpret_cast<const u32x4*>(region + row * STRIDE + ch * 16);
+            }
+        }
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+    }
+};
+
+// Rows of no sequence: zeros in [T, H, D] for `count` heads from h0 on, tokens begin + t0 .. (n of them), by the workgroup
+template <int D>
+DEVINL void ragged_zero(raw16* out, int H, int h0, int heads, long token0, int n)
+{
+    constexpr int CH = D / 8;
+    const u32x4 zero = {0u, 0u, 0u, 0u};
+    for (long x = threadIdx.x; x < (long)n * heads * CH; x += blockDim.x) {
+        const long t = x / (heads * CH);
+        const int in = (int)(x - t * (heads * CH));
+        *reinterpret_cast<u32x4*>(out + ((token0 + t) * H + h0 + in / CH) * D + in % CH * 8) = zero;
+    }
+}
+
+// ------------------------------------------------------------------------------------------- forward
+// One wavefront owns 32 rows, the workgroup's NW share (K | V) tiles of 64 keys; work in units of 32 keys as in avion_fwd_kernel,
+// but with the running maximum: the accumulators are rescaled only where a row's maximum has grown by more than 2^8 (weights then
+// stay below 2^8, which either format holds), a branch that after the first units is hardly ever taken.
+constexpr float kRaggedLazy = 8.f;
+constexpr float kRaggedNone = -3.0e38f;  // reference of a row that has seen nothing: finite, so that -inf - it is -inf
+
+template <int D, int NW>
+struct RaggedFwdCfg {
+    using Ring = RaggedRing<D, NW, false>;
+    static constexpr int NT = NW * 64, BM = 32 * NW, SHIFT = NW == 4 ? 7 : NW == 2 ? 6 : 5;
+    static constexpr int LDS_BYTES = Ring::LDS_BYTES;
+    static constexpr int WAVES_PER_SIMD = D == 64 ? (NW == 4 ? 4 : 1) : D == 80 ? (NW == 4 ? 3 : 1) : NW == 4 ? 2 : 1;
+};
+template <int CT>
+struct RaggedSums {
+    f32x16 o[CT];
+    f32x4 rs4;          // sums of the rounded weights, which multiplied V (four equal values)
+    float m, l;         // reference, sum of the weights
+    DEVINL RaggedSums()
+    {
+        acc_zero(o);
+        rs4 = f32x4{0.f, 0.f, 0.f, 0.f};
+        m = kRaggedNone;
+        l = 0.f;
+    }
+};
+
+// The tiles t0 .. t1 - 1 of one sequence's keys for the wavefront's rows row0 .. row0 + 31
+template <int D, int NW, typename E>
+DEVINL void ragged_fwd_walk(char* smem, const RaggedArgs& a, int hk, int begin_q, int nq, int begin_k, int nk, int row0, int rows, int t0,
+                            int t1, RaggedSums<(D + 31) / 32>& sums, int wave, int lane)
+{
+    using Ring = typename RaggedFwdCfg<D, NW>::Ring;
+    constexpr int KS = D / 16, CT = (D + 31) / 32, STRIDE = Ring::STRIDE;
+    const int l32 = lane % 32, g = lane / 32, tr_off = tr_lane_offset(lane, STRIDE);
+    const Ring ring(a.k + (long)begin_k * a.rs_k + hk * D, a.rs_k, a.v + (long)begin_k * a.rs_v + hk * D, a.rs_v, nullptr, 0, nk, smem,
+                    wave, lane);
+    if (t0 < t1) ring.fetch(t0 * 64, t0 & 1);
+    const bool active = row0 < rows;
+    const RaggedRow row(a, hk, row0 + l32, rows, nq, nk);
+    const int seen_by_all = RaggedRow(a, hk, row0, rows, nq, nk).keys, seen_by_any = RaggedRow(a, hk, row0 + 31, rows, nq, nk).keys;
+    frag8 qf[KS];
+    const raw16* q = a.q + (long)(begin_q + row.token) * a.rs_q + row.head * D + g * 8;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) qf[ks] = *reinterpret_cast<const frag8*>(q + ks * 16);
+    hold(qf);
+    Ring::landed_barrier();
+
+    const float cs = a.cs;
+    auto unit = [&](auto masked, const char* kt, const char* vt, int hk32, int key_base) {
+        f32x16 s;
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) s = E::mfma(nat_frag(kt, STRIDE, 32 * hk32 + l32, ks, g), qf[ks], ks == 0 ? f32x16_zero() : s);
+        if constexpr (decltype(masked)::value) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) s[i] = key_base + 8 * (i / 4) + 4 * g + i % 4 < row.keys ? s[i] : -INFINITY;
+        }
+        frag8 vf[2][CT];
+        if constexpr (D <= 96) {
+#pragma unroll
+            for (int half = 0; half < 2; ++half)
+#pragma unroll
+                for (int ct = 0; ct < CT; ++ct) vf[half][ct] = tr_frag(vt, STRIDE, tr_off, ct, 2 * hk32 + half);
+        }
+        const float top = both_halves_max(max16(s)) * cs;
+        if (__any(top > sums.m + kRaggedLazy)) {
+            const float m = fmaxf(sums.m, top), shrink = fast_exp2(sums.m - m);
+            sums.m = m;
+            sums.l *= shrink;
+            sums.rs4 *= shrink;
+#pragma unroll
+            for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) sums.o[ct][i] *= shrink;
+        }
+        u32x4 pf[2];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const float p = fast_exp2(fmaf(s[i], cs, -sums.m));
+            s[i] = p;
+            sums.l += p;
+            if (i % 2 == 1) pf[i / 8][(i / 2) % 4] = E::pack(s[i - 1], p);
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) sums.rs4 = E::add_four(u32x2{pf[i / 2][2 * (i % 2)], pf[i / 2][2 * (i % 2) + 1]}, sums.rs4);
+#pragma unroll
+        for (int half = 0; half < 2; ++half)
+#pragma unroll
+            for (int ct = 0; ct < CT; ++ct) {
+                if constexpr (D > 96) vf[half][ct] = tr_frag(vt, STRIDE, tr_off, ct, 2 * hk32 + half);
+                sums.o[ct] = E::mfma(vf[half][ct], as_frag8(pf[half]), sums.o[ct]);
+            }
+    };
+    for (int t = t0; t < t1; ++t) {
+        if (t + 1 < t1) ring.fetch((t + 1) * 64, (t + 1) & 1);
+        if (active) {
+            const char* kt = ring.at(smem, t & 1);
+#pragma unroll
+            for (int hk32 = 0; hk32 < 2; ++hk32) {
+                const int key_base = t * 64 + 32 * hk32;
+                if (key_base >= seen_by_any) continue;
+                if (key_base + 32 > seen_by_all) unit(std::true_type{}, kt, kt + Ring::OFF_B, hk32, key_base);
+                else unit(std::false_type{}, kt, kt + Ring::OFF_B, hk32, key_base);
+            }
+        }
+        Ring::landed_barrier();
+    }
+}
+
+// What the sums come to: O's rows and LSE
+template <int D, typename E>
+DEVINL void ragged_fwd_store(char* region, const RaggedArgs& a, raw16* o, float* lse, int hk, int begin_q, int row0, int rows,
+                             RaggedSums<(D + 31) / 32>& sums, int lane)
+{
+    const float l = both_halves_sum(sums.l), r = both_halves_sum(sums.rs4[0]);
+    RaggedStore<D, E>::run(region, sums.o, r == 0.f ? 0.f : 1.f / r, o, a, hk, begin_q, row0, rows, lane);
+    const int row = row0 + lane;
+    if (lane < 32 && row < rows) {
+        const int i = row / a.G;
+        lse[(long)(hk * a.G + row - i * a.G) * a.Tq + begin_q + i] = l == 0.f ? -INFINITY : (sums.m + __builtin_amdgcn_logf(l)) * kLn2;
+    }
+}
+// Rows of no sequence
+template <int D>
+DEVINL void ragged_fwd_none(const RaggedArgs& a, raw16* o, float* lse, int hk, int token0, int n)
+{
+    ragged_zero<D>(o, a.Hq, hk * a.G, a.G, token0, n);
+    for (int x = threadIdx.x; x < n * a.G; x += blockDim.x) lse[(long)(hk * a.G + x / n) * a.Tq + token0 + x % n] = -INFINITY;
+}
+// the tokens whose (token, head) rows a block of BM rows begins: each token belongs to one block
+DEVINL int ragged_first_token(long row, int G) { return (int)((row + G - 1) / G); }
+
+template <int D, int NW, typename E>
+__global__ void __launch_bounds__(NW * 64, (RaggedFwdCfg<D, NW>::WAVES_PER_SIMD))
+avion_ragged_fwd_kernel(RaggedArgs a, raw16* __restrict__ o, float* __restrict__ lse)
+{
+    using Cfg = RaggedFwdCfg<D, NW>;
+    extern __shared__ __attribute__((aligned(16))) char smem[];
+    const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+    // the key heads go round the XCDs; the last blocks, which see the most keys, begin first
+    const int hk = blockIdx.x % a.Hk, slot = a.slots - 1 - blockIdx.x / a.Hk;
+    const RaggedPlace p = ragged_place<Cfg::SHIFT>(a.off_q, a.S, a.Tq, a.G, slot, lane);
+    const int rows = p.n * a.G;
+    if (p.block < 0 || p.block * Cfg::BM >= rows) return;
+    const int block0 = (int)p.block * Cfg::BM;
+    if (p.i == 0 || p.i == a.S + 1) {
+        const int from = ragged_first_token(block0, a.G), to = min(ragged_first_token(block0 + Cfg::BM, a.G), p.n);
+        ragged_fwd_none<D>(a, o, lse, hk, p.begin + from, to - from);
+        return;
+    }
+    const int begin_k = ragged_border(a.off_k, a.S, a.Tk, p.i), nk = max(ragged_border(a.off_k, a.S, a.Tk, p.i + 1) - begin_k, 0);
+    const int last_seen = RaggedRow(a, hk, block0 + Cfg::BM - 1, rows, p.n, nk).keys;
+    RaggedSums<(D + 31) / 32> sums;
+    const int row0 = block0 + wave * 32;
+    ragged_fwd_walk<D, NW, E>(smem, a, hk, p.begin, p.n, begin_k, nk, row0, rows, 0, (last_seen + 63) / 64, sums, wave, lane);
+    if (row0 >= rows) return;
+    ragged_fwd_store<D, E>(smem + wave * RaggedStore<D, E>::BYTES, a, o, lse, hk, p.begin, row0, rows, sums, lane);
+}
+
+// ------------------------------------------------------------------------------ few rows, many keys
+// Single tokens behind long caches: bound by the keys' bytes, which must come from all of memory at once.  Slots are chunks of
+// 2^SHIFT keys (found as above, in the keys' offsets): a wavefront takes the first 32 rows of a sequence through one chunk and
+// leaves its sums; a second launch joins them.  A sequence with one chunk is finished here; rows past the first 32, where there are
+// any, take all keys in the wavefront of the first chunk.
+template <int D>
+struct RaggedPart {
+    static constexpr int FLOATS = 32 * D + 3 * 32;  // O, then reference, sum, sum of the rounded weights
+};
+template <int D, typename E>
+__global__ void __launch_bounds__(64, 1)
+avion_ragged_few_kernel(RaggedArgs a, raw16* __restrict__ o, float* __restrict__ lse, float* __restrict__ parts, int shift)
+{
+    constexpr int CT = (D + 31) / 32;
+    extern __shared__ __attribute__((aligned(16))) char smem[];
+    const int lane = threadIdx.x, hk = blockIdx.x % a.Hk, slot = blockIdx.x / a.Hk;
+    // (blocks of 2^6 tokens, `shift` of them to a chunk: the search knows shifts at compile time)
+    RaggedPlace p;
+    switch (shift) {
+        case 8: p = ragged_place<8>(a.off_k, a.S, a.Tk, 1, slot, lane); break;
+        case 9: p = ragged_place<9>(a.off_k, a.S, a.Tk, 1, slot, lane); break;
+        case 10: p = ragged_place<10>(a.off_k, a.S, a.Tk, 1, slot, lane); break;
+        default: p = ragged_place<11>(a.off_k, a.S, a.Tk, 1, slot, lane); break;
+    }
+    const int chunk = 1 << shift;
+    if (p.i == 0 || p.i == a.S + 1 || p.block < 0 || (p.block > 0 && p.block * chunk >= p.n)) return;
+    const int begin_q = ragged_border(a.off_q, a.S, a.Tq, p.i), nq = max(ragged_border(a.off_q, a.S, a.Tq, p.i + 1) - begin_q, 0);
+    const int rows = nq * a.G, chunks = max((p.n + chunk - 1) >> shift, 1), tiles = (p.n + 63) / 64;
+    for (int row0 = 0; row0 < rows; row0 += 32) {
+        const bool part = row0 == 0 && chunks > 1;
+        if (!part && p.block > 0) return;
+        const int t0 = part ? (int)p.block * (chunk / 64) : 0, t1 = part ? min(t0 + chunk / 64, tiles) : tiles;
+        RaggedSums<CT> sums;
+        ragged_fwd_walk<D, 1, E>(smem, a, hk, begin_q, nq, p.begin, p.n, row0, rows, t0, t1, sums, 0, lane);
+        if (!part) {
+            ragged_fwd_store<D, E>(smem, a, o, lse, hk, begin_q, row0, rows, sums, lane);
+            RaggedFwdCfg<D, 1>::Ring::landed_barrier();
+            continue;
+        }
+        const int l32 = lane % 32, g = lane / 32;
+        float* out = parts + ((long)slot * a.Hk + hk) * RaggedPart<D>::FLOATS;
+        if (l32 < rows) {
+#pragma unroll
+            for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+                for (int q = 0; q < 4; ++q)
+                    if (32 * ct + 8 * q + 4 * g < D)
+                        *reinterpret_cast<f32x4*>(out + l32 * D + 32 * ct + 8 * q + 4 * g) =
+                            f32x4{sums.o[ct][4 * q], sums.o[ct][4 * q + 1], sums.o[ct][4 * q + 2], sums.o[ct][4 * q + 3]};
+        }
+        const float l = both_halves_sum(sums.l), r = both_halves_sum(sums.rs4[0]);
+        if (g == 0) {
+            out[32 * D + l32] = sums.m;
+            out[32 * D + 32 + l32] = l;
+            out[32 * D + 64 + l32] = r;
+        }
+        RaggedFwdCfg<D, 1>::Ring::landed_barrier();
+    }
+}
+
+// Joins them: a wavefront a row; chunk after chunk in order.  Also the rows of no sequence.
+template <int D, typename E>
+__global__ void __launch_bounds__(256)
+avion_ragged_join_kernel(RaggedArgs a, raw16* __restrict__ o, float* __restrict__ lse, const float* __restrict__ parts, int shift)
+{
+    const int hk = blockIdx.x % a.Hk, i = blockIdx.x / a.Hk;  // interval of the borders
+    const int begin_q = ragged_border(a.off_q, a.S, a.Tq, i), nq = max(ragged_border(a.off_q, a.S, a.Tq, i + 1) - begin_q, 0);
+    if (i == 0 || i == a.S + 1) {
+        ragged_fwd_none<D>(a, o, lse, hk, begin_q, nq);
+        return;
+    }
+    const int begin_k = ragged_border(a.off_k, a.S, a.Tk, i), nk = max(ragged_border(a.off_k, a.S, a.Tk, i + 1) - begin_k, 0);
+    const int chunks = (nk + (1 << shift) - 1) >> shift, rows = min(nq * a.G, 32);
+    if (chunks < 2) return;
+    const long slot = (begin_k >> shift) + i;
+    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
+    for (int row = wave; row < rows; row += 4) {
+        const float* at = parts + (slot * a.Hk + hk) * RaggedPart<D>::FLOATS;
+        const long step = (long)a.Hk * RaggedPart<D>::FLOATS;
+        float m = kRaggedNone;
+        for (int c = lane; c < chunks; c += 64) m = fmaxf(m, at[c * step + 32 * D + row]);
+#pragma unroll
+        for (int x = 1; x < 64; x *= 2) m = fmaxf(m, __shfl_xor(m, x));
+        float acc[(D + 63) / 64] = {}, l = 0.f, r = 0.f;
+        for (int c = 0; c < chunks; ++c) {
+            const float* part = at + c * step;
+            const float w = fast_exp2(part[32 * D + row] - m);
+            l += w * part[32 * D + 32 + row];
+            r += w * part[32 * D + 64 + row];
+#pragma unroll
+            for (int x = 0; x < (D + 63) / 64; ++x)
+                if (lane + 64 * x < D) acc[x] += w * part[row * D + lane + 64 * x];
+        }
+        const int q = row / a.G, head = hk * a.G + row - q * a.G;
+        const float inv = r == 0.f ? 0.f : 1.f / r;
+#pragma unroll
+        for (int x = 0; x < (D + 63) / 64; ++x)
+            if (lane + 64 * x < D) o[((long)(begin_q + q) * a.Hq + head) * D + lane + 64 * x] = (raw16)(E::pack(acc[x] * inv, 0.f) & 0xffffu);
+        if (lane == 0) lse[(long)head * a.Tq + begin_q + q] = l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * kLn2;
+    }
+}
+
+// ------------------------------------------------------------------------------------------------ dQ
+// As avion_dq_kernel, on the rows above.  delta = rowsum(dO o O) from the O that the forward rounded is off by 2^-9 |dO| |O|, which
+// counts where a row sees few keys; a workgroup whose keys fit two tiles has all of them in LDS and forms delta = sum_j P_j dP_j
+// from them first (up to 128 keys, the rows that need it, and the ones that are not bound by contractions).
+// Leaves lse * log2 e (+inf where a row sees nothing, so that its weights are 0; fp16: less kRaggedShift) and -delta for the second
+// kernel: [Hq][2][npad], sequence s at (floor(begin / 64) + s) * 64.
+//
+// fp16 weights below 2^-14 lose bits: over thousands of keys most are.  The second kernel holds them 2^8 times larger where they
+// are rounded for dV; in dS they stand beside dP, which is as large as the loss is scaled.
+template <typename E>
+constexpr float kRaggedShift = std::is_same<E, F16>::value ? 8.f : 0.f;
+
+template <int D, int NW>
+struct RaggedDqCfg {
+    using Ring = RaggedRing<D, NW, false>;
+    static constexpr int NT = NW * 64, BM = 32 * NW, SHIFT = NW == 4 ? 7 : NW == 2 ? 6 : 5, LDS_BYTES = Ring::LDS_BYTES;
+    static constexpr int WAVES_PER_SIMD = NW < 4 ? 1 : D == 64 ? 3 : 2;
+};
+DEVINL long ragged_scalar_at(int begin, int i) { return ((long)(begin >> 6) + i) * 64; }
+
+template <int D, int NW, typename E>
+__global__ void __launch_bounds__(NW * 64, (RaggedDqCfg<D, NW>::WAVES_PER_SIMD))
+avion_ragged_dq_kernel(RaggedArgs a, const raw16* __restrict__ o, const raw16* __restrict__ dO, const float* __restrict__ lse,
+                       raw16* __restrict__ dq, float* __restrict__ rowsc, int npad)
+{
+    using Cfg = RaggedDqCfg<D, NW>;
+    using Ring = typename Cfg::Ring;
+    constexpr int KS = D / 16, CT = (D + 31) / 32, STRIDE = Ring::STRIDE;
+    extern __shared__ __attribute__((aligned(16))) char smem[];
+    const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), l32 = lane % 32, g = lane / 32;
+    const int hk = blockIdx.x % a.Hk, slot = a.slots - 1 - blockIdx.x / a.Hk;
+    const RaggedPlace p = ragged_place<Cfg::SHIFT>(a.off_q, a.S, a.Tq, a.G, slot, lane);
+    const int rows = p.n * a.G, nq = p.n;
+    if (p.block < 0 || p.block * Cfg::BM >= rows) return;
+    const int block0 = (int)p.block * Cfg::BM;
+    if (p.i == 0 || p.i == a.S + 1) {
+        const int from = ragged_first_token(block0, a.G), to = min(ragged_first_token(block0 + Cfg::BM, a.G), p.n);
+        ragged_zero<D>(dq, a.Hq, hk * a.G, a.G, p.begin + from, to - from);
+        return;
+    }
+    const int begin_k = ragged_border(a.off_k, a.S, a.Tk, p.i), nk = max(ragged_border(a.off_k, a.S, a.Tk, p.i + 1) - begin_k, 0);
+    const int ntiles = (RaggedRow(a, hk, block0 + Cfg::BM - 1, rows, nq, nk).keys + 63) / 64;
+    const bool whole = ntiles <= 2;
+    const Ring ring(a.k + (long)begin_k * a.rs_k + hk * D, a.rs_k, a.v + (long)begin_k * a.rs_v + hk * D, a.rs_v, nullptr, 0, nk, smem,
+                    wave, lane);
+    if (ntiles > 0) ring.fetch(0, 0);
+    if (ntiles == 2) ring.fetch(64, 1);
+    const int row0 = block0 + wave * 32, tr_off = tr_lane_offset(lane, STRIDE);
+    const bool active = row0 < rows;
+    const RaggedRow row(a, hk, row0 + l32, rows, nq, nk);
+    const int seen_by_all = RaggedRow(a, hk, row0, rows, nq, nk).keys, seen_by_any = RaggedRow(a, hk, row0 + 31, rows, nq, nk).keys;
+    frag8 qf[KS], gf[KS];
+    float dl;
+    {
+        const raw16* q = a.q + (long)(p.begin + row.token) * a.rs_q + row.head * D + g * 8;
+        const long at = ((long)(p.begin + row.token) * a.Hq + row.head) * D + g * 8;
+        float part = 0.f;
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) {
+            qf[ks] = *reinterpret_cast<const frag8*>(q + ks * 16);
+            gf[ks] = *reinterpret_cast<const frag8*>(dO + at + ks * 16);
+            const frag8 of = *reinterpret_cast<const frag8*>(o + at + ks * 16);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) part = fmaf(E::widen(of, e), E::widen(gf[ks], e), part);
+        }
+        dl = both_halves_sum(part);
+    }
+    const float saved = lse[(long)row.head * a.Tq + p.begin + row.token];
+    const float lc = saved == -INFINITY ? INFINITY : saved * kLog2e, cs = a.cs;
+    hold(qf);
+    hold(gf);
+    Ring::landed_barrier();
+
+    // P and dP of one unit (masked: 0 where the row does not see the key, whatever lies there)
+    auto weights = [&](auto masked, const char* kt, int hk32, int key_base, f32x16& pe, f32x16& dp) {
+        const char* vt = kt + Ring::OFF_B;
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) {
+            const frag8 ak = nat_frag(kt, STRIDE, 32 * hk32 + l32, ks, g), av = nat_frag(vt, STRIDE, 32 * hk32 + l32, ks, g);
+            pe = E::mfma(ak, qf[ks], ks == 0 ? f32x16_zero() : pe);
+            dp = E::mfma(av, gf[ks], ks == 0 ? f32x16_zero() : dp);
+        }
+        if constexpr (decltype(masked)::value) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const bool sees = key_base + 8 * (i / 4) + 4 * g + i % 4 < row.keys;
+                pe[i] = sees ? pe[i] : -INFINITY;
+                dp[i] = sees ? dp[i] : 0.f;
+            }
+        }
+    };
+    if (whole && active) {
+        float sum = 0.f;
+        for (int key_base = 0; key_base < seen_by_any; key_base += 32) {
+            f32x16 pe, dp;
+            weights(std::true_type{}, ring.at(smem, key_base / 64), key_base / 32 % 2, key_base, pe, dp);
+#pragma unroll
+            for (int i = 0; i < 16; ++i) sum = fmaf(fast_exp2(fmaf(pe[i], cs, -lc)), dp[i], sum);
+        }
+        dl = both_halves_sum(sum);
+    }
+    if (active && g == 0 && row0 + l32 < rows) {
+        float* ws = rowsc + (long)row.head * 2 * npad + ragged_scalar_at(p.begin, p.i) + row.token;
+        ws[0] = lc - kRaggedShift<E>;
+        ws[npad] = -dl;
+    }
+    f32x16 acc[CT];
+    acc_zero(acc);
+    auto unit = [&](auto masked, const char* kt, int hk32, int key_base) {
+        f32x16 s, dp;
+        weights(masked, kt, hk32, key_base, s, dp);
+        frag8 kf[2][CT];
+        if constexpr (D <= 96) {
+#pragma unroll
+            for (int half = 0; half < 2; ++half)
+#pragma unroll
+                for (int ct = 0; ct < CT; ++ct) kf[half][ct] = tr_frag(kt, STRIDE, tr_off, ct, 2 * hk32 + half);
+        }
+        u32x4 df[2];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            s[i] = fast_exp2(fmaf(s[i], cs, -lc)) * (dp[i] - dl);
+            if (i % 2 == 1) df[i / 8][(i / 2) % 4] = E::pack(s[i - 1], s[i]);
+        }
+#pragma unroll
+        for (int half = 0; half < 2; ++half)
+#pragma unroll
+            for (int ct = 0; ct < CT; ++ct) {
+                if constexpr (D > 96) kf[half][ct] = tr_frag(kt, STRIDE, tr_off, ct, 2 * hk32 + half);
+                acc[ct] = E::mfma(kf[half][ct], as_frag8(df[half]), acc[ct]);
+            }
+    };
+    for (int t = 0; t < ntiles; ++t) {
+        if (!whole && t + 1 < ntiles) ring.fetch((t + 1) * 64, (t + 1) & 1);
+        if (active) {
+            const char* kt = ring.at(smem, t & 1);
+#pragma unroll
+            for (int hk32 = 0; hk32 < 2; ++hk32) {
+                const int key_base = t * 64 + 32 * hk32;
+                if (key_base >= seen_by_any) continue;
+                if (key_base + 32 > seen_by_all) unit(std::true_type{}, kt, hk32, key_base);
+                else unit(std::false_type{}, kt, hk32, key_base);
+            }
+        }
+        Ring::landed_barrier();
+    }
+    if (!active) return;
+    RaggedStore<D, E>::run(smem + wave * RaggedStore<D, E>::BYTES, acc, a.scale, dq, a, hk, p.begin, row0, rows, lane_from_exec());
+}
+
+// -------------------------------------------------------------------------------------------- dK, dV
+// As avion_dkdv_kernel: a wavefront owns 32 keys of one key head; the tiles of 64 queries of its query heads come one after the
+// other.  With `parts` > 1 the query heads are dealt to that many workgroups, whose sums meet in fp32 (avion_ragged_sum_kernel).
+template <int D, int NW>
+struct RaggedDkvCfg {
+    using Ring = RaggedRing<D, NW, true>;
+    static constexpr int NT = NW * 64, BN = 32 * NW, SHIFT = NW == 4 ? 7 : NW == 2 ? 6 : 5, LDS_BYTES = Ring::LDS_BYTES;
+    static constexpr int WAVES_PER_SIMD = NW < 4 ? 1 : D == 64 ? 3 : D == 80 ? 2 : 1;
+};
+// 32 rows of fp32 sums, lane = row
+template <int D>
+DEVINL void ragged_store_part(const f32x16 (&acc)[(D + 31) / 32], float* out, long stride, int rows, int lane)
+{
+    const int l32 = lane % 32, g = lane / 32;
+    if (l32 >= rows) return;
+#pragma unroll
+    for (int ct = 0; ct < (D + 31) / 32; ++ct)
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+            if (32 * ct + 8 * q + 4 * g < D)
+                *reinterpret_cast<f32x4*>(out + l32 * stride + 32 * ct + 8 * q + 4 * g) =
+                    f32x4{acc[ct][4 * q], acc[ct][4 * q + 1], acc[ct][4 * q + 2], acc[ct][4 * q + 3]};
+}
+
+template <int D, int NW, typename E>
+__global__ void __launch_bounds__(NW * 64, (RaggedDkvCfg<D, NW>::WAVES_PER_SIMD))
+avion_ragged_dkdv_kernel(RaggedArgs a, const raw16* __restrict__ dO, const float* __restrict__ rowsc, int npad, raw16* __restrict__ dk,
+                         raw16* __restrict__ dv, float* __restrict__ sums, int parts)
+{
+    using Cfg = RaggedDkvCfg<D, NW>;
+    using Ring = typename Cfg::Ring;
+    constexpr int KS = D / 16, CT = (D + 31) / 32, STRIDE = Ring::STRIDE, OFF_G = Ring::OFF_B;
+    extern __shared__ __attribute__((aligned(16))) char smem[];
+    const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), l32 = lane % 32, g = lane / 32;
+    const int hk = blockIdx.x % a.Hk, part = blockIdx.x / a.Hk % parts, slot = blockIdx.x / (a.Hk * parts);
+    const RaggedPlace p = ragged_place<Cfg::SHIFT>(a.off_k, a.S, a.Tk, 1, slot, lane);
+    const int nk = p.n;
+    if (p.block < 0 || p.block * Cfg::BN >= nk) return;
+    const int block0 = (int)p.block * Cfg::BN, k0 = block0 + wave * 32;
+    const int begin_q = ragged_border(a.off_q, a.S, a.Tq, p.i);
+    const int nq = p.i == 0 || p.i == a.S + 1 ? 0 : max(ragged_border(a.off_q, a.S, a.Tq, p.i + 1) - begin_q, 0);
+    const bool active = k0 < nk;
+    // first query that sees a key: this lane's, the wavefront's first and last, the workgroup's first
+    auto first_query = [&](int key) { return a.causal ? max(min(key, nk - 1) - nk + nq, 0) : 0; };
+    const int key = min(k0 + l32, nk - 1), from = first_query(k0 + l32), from_all = first_query(k0 + 31), from_any = first_query(k0);
+    const int tile0 = first_query(block0) / 64, tiles = nq == 0 ? 0 : (nq + 63) / 64 - tile0;
+    const int heads = a.G / parts, h0 = hk * a.G + part * heads;
+
+    const long q_at = (long)begin_q * a.rs_q, o_at = (long)begin_q * a.Hq * D;
+    Ring ring(a.q + q_at, a.rs_q, dO + o_at, (long)a.Hq * D, rowsc + ragged_scalar_at(begin_q, p.i), npad, nq, smem, wave, lane);
+    int f_head = 0, f_tile = 0;  // next to fetch
+    auto fetch = [&](int to) {
+        Ring r = ring;
+        r.a += (h0 + f_head) * D;
+        r.b += (h0 + f_head) * D;
+        r.scalars += (long)(h0 + f_head) * 2 * npad;
+        r.fetch((tile0 + f_tile) * 64, to);
+        if (++f_tile == tiles) {
+            f_tile = 0;
+            ++f_head;
+        }
+    };
+    const int total = heads * tiles;
+    if (total > 0) fetch(0);
+    frag8 kf[KS], vf[KS];
+    {
+        const raw16 *k = a.k + (long)(p.begin + key) * a.rs_k + hk * D + g * 8, *v = a.v + (long)(p.begin + key) * a.rs_v + hk * D + g * 8;
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) {
+            kf[ks] = *reinterpret_cast<const frag8*>(k + ks * 16);
+            vf[ks] = *reinterpret_cast<const frag8*>(v + ks * 16);
+        }
+    }
+    f32x16 dka[CT], dva[CT];
+    acc_zero(dka);
+    acc_zero(dva);
+    hold(kf);
+    hold(vf);
+    Ring::landed_barrier();
+    const float cs = a.cs;
+    const int tr_off = tr_lane_offset(lane, STRIDE);
+
+    auto unit = [&](auto masked, const char* buf, int hq, int query_base) {
+        const float* rowv = reinterpret_cast<const float*>(buf + Ring::OFF_SCALARS) + 32 * hq + 4 * g;
+        f32x16 s, dp;
+#pragma unroll
+        for (int a4 = 0; a4 < 4; ++a4) {
+            const f32x4 d4 = *reinterpret_cast<const f32x4*>(rowv + 64 + 8 * a4);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) dp[4 * a4 + e] = d4[e];
+        }
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) {
+            const frag8 aq = nat_frag(buf, STRIDE, 32 * hq + l32, ks, g), ag = nat_frag(buf + OFF_G, STRIDE, 32 * hq + l32, ks, g);
+            s = E::mfma(aq, kf[ks], ks == 0 ? f32x16_zero() : s);
+            dp = E::mfma(ag, vf[ks], dp);
+        }
+        f32x4 l4[4];
+#pragma unroll
+        for (int a4 = 0; a4 < 4; ++a4) l4[a4] = *reinterpret_cast<const f32x4*>(rowv + 8 * a4);
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+            frag8 tg[CT], tq[CT];
+            if constexpr (D <= 96) {
+#pragma unroll
+                for (int ct = 0; ct < CT; ++ct) {
+                    tg[ct] = tr_frag(buf + OFF_G, STRIDE, tr_off, ct, 2 * hq + half);
+                    tq[ct] = tr_frag(buf, STRIDE, tr_off, ct, 2 * hq + half);
+                }
+            }
+            u32x4 pf, df;
+#pragma unroll
+            for (int e = 8 * half; e < 8 * half + 8; ++e) {
+                float pe = fast_exp2(fmaf(s[e], cs, -l4[e / 4][e % 4]));
+                float ds = (std::is_same<E, F16>::value ? pe * (1.f / 256.f) : pe) * dp[e];
+                if constexpr (decltype(masked)::value) {
+                    const int query = query_base + 8 * (e / 4) + 4 * g + e % 4;
+                    const bool sees = query >= from && query < nq;
+                    pe = sees ? pe : 0.f;
+                    ds = sees ? ds : 0.f;
+                }
+                s[e] = pe;
+                dp[e] = ds;
+                if (e % 2 == 1) {
+                    pf[(e / 2) % 4] = E::pack(s[e - 1], s[e]);
+                    df[(e / 2) % 4] = E::pack(dp[e - 1], dp[e]);
+                }
+            }
+#pragma unroll
+            for (int ct = 0; ct < CT; ++ct) {
+                if constexpr (D > 96) {
+                    tg[ct] = tr_frag(buf + OFF_G, STRIDE, tr_off, ct, 2 * hq + half);
+                    tq[ct] = tr_frag(buf, STRIDE, tr_off, ct, 2 * hq + half);
+                }
+                dva[ct] = E::mfma(tg[ct], as_frag8(pf), dva[ct]);
+                dka[ct] = E::mfma(tq[ct], as_frag8(df), dka[ct]);
+            }
+        }
+    };
+    int tile = 0;
+    for (int n = 0; n < total; ++n) {
+        if (n + 1 < total) fetch((n + 1) & 1);
+        if (active) {
+            const char* buf = ring.at(smem, n & 1);
+#pragma unroll
+            for (int hq = 0; hq < 2; ++hq) {
+                const int query_base = (tile0 + tile) * 64 + 32 * hq;
+                if (query_base >= nq || query_base + 32 <= from_any) continue;
+                if (query_base < from_all || query_base + 32 > nq) unit(std::true_type{}, buf, hq, query_base);
+                else unit(std::false_type{}, buf, hq, query_base);
+            }
+        }
+        if (++tile == tiles) tile = 0;
+        Ring::landed_barrier();
+    }
+    if (!active) return;
+    const int lane_now = lane_from_exec();
+    const float dv_mul = std::is_same<E, F16>::value ? 1.f / 256.f : 1.f;
+    const long rs = (long)a.Hk * D, at = (long)(p.begin + k0) * rs + hk * D;
+    if (parts > 1) {
+        const long whole = (long)a.Tk * rs;
+        float* out = sums + part * 2 * whole + at;
+        ragged_store_part<D>(dka, out, rs, nk - k0, lane_now);
+        ragged_store_part<D>(dva, out + whole, rs, nk - k0, lane_now);
+        return;
+    }
+    char* region = smem + wave * RowStore<D, E>::BYTES;
+    RowStore<D, E>::run(region, dka, a.scale, dk + at, rs, nk - k0, lane_now);
+    RowStore<D, E>::run(region, dva, dv_mul, dv + at, rs, nk - k0, lane_now);
+}
+
+// dK and dV from the parts' sums, part after part
+template <typename E>
+__global__ void __launch_bounds__(256)
+avion_ragged_sum_kernel(const float* __restrict__ sums, int parts, long n, raw16* __restrict__ dk, raw16* __restrict__ dv, float dk_mul, float dv_mul)
+{
+    const long chunks = n / 4;
+    for (long x = blockIdx.x * 256L + threadIdx.x; x < 2 * chunks; x += gridDim.x * 256L) {
+        const bool second = x >= chunks;
+        const long i = (second ? x - chunks : x) * 4;
+        f32x4 t = {0.f, 0.f, 0.f, 0.f};
+        for (int p = 0; p < parts; ++p) t += *reinterpret_cast<const f32x4*>(sums + (2L * p + second) * n + i);
+        t *= second ? dv_mul : dk_mul;
+        *reinterpret_cast<u32x2*>((second ? dv : dk) + i) = u32x2{E::pack(t[0], t[1]), E::pack(t[2], t[3])};
+    }
+}

@@ -1,0 +1,243 @@
+// C ABI of the attention over sequences of different lengths.  See include/avion_attn.h for its contract.
+#include "avion_attn.h"
+
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+
+#include "avion_host.h"
+#include "avion_ragged.h"
+
+namespace {
+
+template <int N>
+using Int = std::integral_constant<int, N>;
+
+constexpr float kMinScale = 8.673617379884035e-19f;  // 2^-60, as avion_attn_fwd
+constexpr long long kComputeUnits = 256, kMostTokens = 1 << 28, kMostSequences = 1 << 20, kMostStride = 1 << 23;
+
+struct RaggedShape {
+    long long Tq, Tk, S;
+    int Hq, Hk, d;
+};
+int ragged_check(const RaggedShape& s)
+{
+    if (s.Tq < 0 || s.Tk < 0 || s.S < 0 || s.Hq < 1 || s.Hk < 1 || s.d < 1 || s.Hq % s.Hk != 0) return AVION_EINVAL;
+    if ((s.d != 64 && s.d != 80 && s.d != 128) || s.Tq > kMostTokens || s.Tk > kMostTokens || s.S > kMostSequences) return AVION_EUNSUPPORTED;
+    const long long G = s.Hq / s.Hk;
+    if (s.Hq > (1 << 16) || s.Tq * G > (1LL << 30) || (s.Tq * G / 32 + s.Tk / 32 + s.S + 2) * s.Hq > 0x7fffffffLL) return AVION_EUNSUPPORTED;
+    if ((long long)s.Hq * s.d > kMostStride) return AVION_EUNSUPPORTED;
+    return AVION_OK;
+}
+bool stride_ok(long long rs, int H, int d) { return rs >= (long long)H * d; }
+
+// Few rows a sequence and many keys: a wavefront per chunk of keys.  2^shift keys a chunk, 0: not this way.
+int few_shift(const RaggedShape& s)
+{
+    const long long G = s.Hq / s.Hk;
+    if (s.S < 1 || s.Tq * G > 32 * s.S || s.Tk < 256 * s.S) return 0;
+    int shift = 8;
+    while (shift < 11 && (s.Tk >> shift) * s.Hk > 8 * kComputeUnits) ++shift;
+    return shift;
+}
+long long few_slots(const RaggedShape& s, int shift) { return (s.Tk >> shift) + s.S + 2; }
+size_t few_bytes(const RaggedShape& s)
+{
+    const int shift = few_shift(s);
+    return shift == 0 ? 0 : round256((size_t)few_slots(s, shift) * s.Hk * (32 * s.d + 96) * 4);
+}
+
+// wavefronts a workgroup: whole blocks of 128 rows, or of 32 where sequences are short
+int ragged_waves(long long rows, long long S) { return rows >= 64 * S ? 4 : 1; }
+
+int dkdv_parts(const RaggedShape& s)
+{
+    const int G = s.Hq / s.Hk, nw = ragged_waves(s.Tk, s.S);
+    const long long blocks = (s.Tk / (32 * nw) + s.S) * s.Hk;
+    int parts = 1;
+    for (int p = 2; p <= G && p <= 8; ++p)
+        if (G % p == 0 && blocks * parts < 2 * kComputeUnits) parts = p;
+    return parts;
+}
+long long ragged_npad(const RaggedShape& s) { return (s.Tq / 64 + s.S + 2) * 64; }
+size_t scalar_bytes(const RaggedShape& s) { return round256((size_t)s.Hq * 2 * ragged_npad(s) * 4); }
+size_t parts_bytes(const RaggedShape& s)
+{
+    const int parts = dkdv_parts(s);
+    return parts == 1 ? 0 : round256((size_t)parts * 2 * s.Tk * s.Hk * s.d * 4);
+}
+
+// f(head channels, element format)
+template <typename F>
+int by_head(int d, unsigned flags, F f)
+{
+    return by_element(flags, [&](auto fmt) {
+        if (d == 64) return f(Int<64>{}, fmt);
+        if (d == 80) return f(Int<80>{}, fmt);
+        return f(Int<128>{}, fmt);
+    });
+}
+template <typename F>
+int by_waves(int nw, F f)
+{
+    return nw == 4 ? f(Int<4>{}) : f(Int<1>{});
+}
+
+RaggedArgs ragged_args(const RaggedShape& s, const void* q, const void* k, const void* v, const int* off_q, const int* off_k, long long rs_q,
+                       long long rs_k, long long rs_v, float scale, unsigned flags)
+{
+    RaggedArgs a{};
+    a.q = static_cast<const raw16*>(q);
+    a.k = static_cast<const raw16*>(k);
+    a.v = static_cast<const raw16*>(v);
+    a.off_q = off_q;
+    a.off_k = off_k;
+    a.rs_q = rs_q;
+    a.rs_k = rs_k;
+    a.rs_v = rs_v;
+    a.S = (int)s.S;
+    a.Tq = (int)s.Tq;
+    a.Tk = (int)s.Tk;
+    a.Hq = s.Hq;
+    a.Hk = s.Hk;
+    a.G = s.Hq / s.Hk;
+    a.causal = flags & AVION_FLAG_CAUSAL ? 1 : 0;
+    a.cs = scale * kLog2e;
+    a.scale = scale;
+    return a;
+}
+
+template <typename K, typename... Args>
+int launch(K kernel, int lds, std::atomic<unsigned long long>& allowed, long long grid, int threads, hipStream_t st, const char* what, Args... args)
+{
+    const hipError_t attr = lds ? allow_lds_here(kernel, lds, allowed) : hipSuccess;
+    if (attr != hipSuccess) return hip_fail(attr, "hipFuncSetAttribute(ragged attention)");
+    begin_launch();
+    hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(threads), lds, st, args...);
+    return end_launch(what);
+}
+
+int ragged_inputs(const RaggedShape& s, const void* q, const void* k, const void* v, const int* off_q, const int* off_k, long long rs_q,
+                  long long rs_k, long long rs_v, float scale, unsigned flags)
+{
+    if (flags & ~(AVION_FLAG_F16 | AVION_FLAG_CAUSAL)) return AVION_EINVAL;
+    if (!(scale >= kMinScale) || !std::isfinite(scale)) return AVION_EINVAL;
+    const int rc = ragged_check(s);
+    if (rc != AVION_OK) return rc;
+    if (!stride_ok(rs_q, s.Hq, s.d) || !stride_ok(rs_k, s.Hk, s.d) || !stride_ok(rs_v, s.Hk, s.d)) return AVION_EINVAL;
+    for (const long long rs : {rs_q, rs_k, rs_v})
+        if (rs > kMostStride || rs % 8 != 0) return AVION_EUNSUPPORTED;
+    if (!off_q || !off_k || (s.Tq > 0 && !q) || (s.Tk > 0 && (!k || !v))) return AVION_EINVAL;
+    if (!aligned16(q) || !aligned16(k) || !aligned16(v)) return AVION_EUNSUPPORTED;
+    if (reinterpret_cast<uintptr_t>(off_q) % 4 != 0 || reinterpret_cast<uintptr_t>(off_k) % 4 != 0) return AVION_EUNSUPPORTED;
+    return AVION_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t avion_ragged_fwd_workspace_bytes(long long Tq, long long Tk, long long S, int Hq, int Hk, int d)
+{
+    const RaggedShape s{Tq, Tk, S, Hq, Hk, d};
+    return ragged_check(s) == AVION_OK ? std::max<size_t>(256, few_bytes(s)) : 0;
+}
+
+int avion_ragged_fwd(const void* q, const void* k, const void* v, const int* offsets_q, const int* offsets_k, void* o, float* lse,
+                     long long Tq, long long Tk, long long S, int Hq, int Hk, int d, long long rs_q, long long rs_k, long long rs_v,
+                     float scale, unsigned flags, void* workspace, size_t workspace_bytes, void* stream)
+{
+    const RaggedShape s{Tq, Tk, S, Hq, Hk, d};
+    const int rc = ragged_inputs(s, q, k, v, offsets_q, offsets_k, rs_q, rs_k, rs_v, scale, flags);
+    if (rc != AVION_OK) return rc;
+    if (Tq > 0 && (!o || !lse)) return AVION_EINVAL;
+    if (!aligned16(o) || reinterpret_cast<uintptr_t>(lse) % 4 != 0) return AVION_EUNSUPPORTED;
+    const size_t need = few_bytes(s);
+    if (need && !workspace_fits(workspace, workspace_bytes, need)) return AVION_EWORKSPACE;
+    if (Tq == 0) return AVION_OK;
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    RaggedArgs a = ragged_args(s, q, k, v, offsets_q, offsets_k, rs_q, rs_k, rs_v, scale, flags);
+    raw16* out = static_cast<raw16*>(o);
+    return by_head(d, flags, [&](auto dim, auto fmt) {
+        constexpr int D = decltype(dim)::value;
+        using E = typename decltype(fmt)::type;
+        if (const int shift = few_shift(s)) {
+            static std::atomic<unsigned long long> allowed{0}, none{0};
+            float* parts = static_cast<float*>(workspace);
+            const int first = launch(avion_ragged_few_kernel<D, E>, RaggedFwdCfg<D, 1>::LDS_BYTES, allowed, few_slots(s, shift) * Hk, 64, st,
+                                     "launch avion_ragged_few_kernel", a, out, lse, parts, shift);
+            if (first != AVION_OK) return first;
+            return launch(avion_ragged_join_kernel<D, E>, 0, none, (S + 2) * Hk, 256, st, "launch avion_ragged_join_kernel", a, out, lse,
+                          (const float*)parts, shift);
+        }
+        return by_waves(ragged_waves(Tq * a.G, S), [&](auto nw) {
+            constexpr int NW = decltype(nw)::value;
+            using Cfg = RaggedFwdCfg<D, NW>;
+            static std::atomic<unsigned long long> allowed{0};
+            a.slots = (int)(Tq * a.G / Cfg::BM + S + 2);
+            return launch(avion_ragged_fwd_kernel<D, NW, E>, Cfg::LDS_BYTES, allowed, (long long)a.slots * Hk, Cfg::NT, st,
+                          "launch avion_ragged_fwd_kernel", a, out, lse);
+        });
+    });
+}
+
+size_t avion_ragged_bwd_workspace_bytes(long long Tq, long long Tk, long long S, int Hq, int Hk, int d)
+{
+    const RaggedShape s{Tq, Tk, S, Hq, Hk, d};
+    return ragged_check(s) == AVION_OK ? scalar_bytes(s) + parts_bytes(s) : 0;
+}
+
+int avion_ragged_bwd(const void* q, const void* k, const void* v, const int* offsets_q, const int* offsets_k, const void* o,
+                     const float* lse, const void* dO, void* dq, void* dk, void* dv, long long Tq, long long Tk, long long S, int Hq,
+                     int Hk, int d, long long rs_q, long long rs_k, long long rs_v, float scale, unsigned flags, void* workspace,
+                     size_t workspace_bytes, void* stream)
+{
+    const RaggedShape s{Tq, Tk, S, Hq, Hk, d};
+    const int rc = ragged_inputs(s, q, k, v, offsets_q, offsets_k, rs_q, rs_k, rs_v, scale, flags);
+    if (rc != AVION_OK) return rc;
+    if ((Tq > 0 && (!o || !lse || !dO || !dq)) || (Tk > 0 && (!dk || !dv))) return AVION_EINVAL;
+    for (const void* p : {o, dO, (const void*)dq, (const void*)dk, (const void*)dv})
+        if (!aligned16(p)) return AVION_EUNSUPPORTED;
+    if (reinterpret_cast<uintptr_t>(lse) % 4 != 0) return AVION_EUNSUPPORTED;
+    if (!workspace_fits(workspace, workspace_bytes, avion_ragged_bwd_workspace_bytes(Tq, Tk, S, Hq, Hk, d))) return AVION_EWORKSPACE;
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    RaggedArgs a = ragged_args(s, q, k, v, offsets_q, offsets_k, rs_q, rs_k, rs_v, scale, flags);
+    float* rowsc = static_cast<float*>(workspace);
+    float* sums = reinterpret_cast<float*>(static_cast<char*>(workspace) + scalar_bytes(s));
+    const int npad = (int)ragged_npad(s), parts = dkdv_parts(s);
+    return by_head(d, flags, [&](auto dim, auto fmt) {
+        constexpr int D = decltype(dim)::value;
+        using E = typename decltype(fmt)::type;
+        if (Tq > 0) {
+            const int first = by_waves(ragged_waves(Tq * a.G, S), [&](auto nw) {
+                constexpr int NW = decltype(nw)::value;
+                using Cfg = RaggedDqCfg<D, NW>;
+                static std::atomic<unsigned long long> allowed{0};
+                a.slots = (int)(Tq * a.G / Cfg::BM + S + 2);
+                return launch(avion_ragged_dq_kernel<D, NW, E>, Cfg::LDS_BYTES, allowed, (long long)a.slots * Hk, Cfg::NT, st,
+                              "launch avion_ragged_dq_kernel", a, static_cast<const raw16*>(o), static_cast<const raw16*>(dO), lse,
+                              static_cast<raw16*>(dq), rowsc, npad);
+            });
+            if (first != AVION_OK) return first;
+        }
+        if (Tk == 0) return AVION_OK;
+        const int second = by_waves(ragged_waves(Tk, S), [&](auto nw) {
+            constexpr int NW = decltype(nw)::value;
+            using Cfg = RaggedDkvCfg<D, NW>;
+            static std::atomic<unsigned long long> allowed{0};
+            a.slots = (int)(Tk / Cfg::BN + S + 2);
+            return launch(avion_ragged_dkdv_kernel<D, NW, E>, Cfg::LDS_BYTES, allowed, (long long)a.slots * Hk * parts, Cfg::NT, st,
+                          "launch avion_ragged_dkdv_kernel", a, static_cast<const raw16*>(dO), (const float*)rowsc, npad,
+                          static_cast<raw16*>(dk), static_cast<raw16*>(dv), sums, parts);
+        });
+        if (second != AVION_OK || parts == 1) return second;
+        static std::atomic<unsigned long long> none{0};
+        const long long n = Tk * Hk * D;
+        return launch(avion_ragged_sum_kernel<E>, 0, none, std::min<long long>(2048, (n / 2 + 255) / 256), 256, st,
+                      "launch avion_ragged_sum_kernel", (const float*)sums, parts, (long)n, static_cast<raw16*>(dk), static_cast<raw16*>(dv),
+                      scale, std::is_same<E, F16>::value ? 1.f / 256.f : 1.f);
+    });
+}
+
+}  // extern "C"

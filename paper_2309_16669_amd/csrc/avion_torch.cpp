@@ -18,6 +18,7 @@
 #include <torch/csrc/autograd/python_variable.h>
 #include <torch/csrc/jit/frontend/tracer.h>
 #include <torch/csrc/utils/pybind.h>
+#include <pybind11/stl.h>
 #include <ATen/ATen.h>
 #include <ATen/PythonTorchFunctionTLS.h>
 
@@ -716,6 +717,231 @@ pybind11::object linear_fp8(pybind11::handle x8_, pybind11::handle xs_, pybind11
     END_HANDLE_TH_ERRORS_PYBIND
 }
 
+// ------------------------------------------- rotary positions, sequences of different lengths
+// Token rows [T, H, d] whose heads and channels are contiguous, at a multiple of 16 bytes: t itself where it is such (a slice of a
+// joint projection), else a copy
+Tensor rows(const Tensor& t)
+{
+    const int64_t T = t.size(0), H = t.size(1), d = t.size(2), rs = t.stride(0);
+    const bool plain = (d == 1 || t.stride(2) == 1) && (H == 1 || t.stride(1) == d) &&
+                       (T < 2 || (rs >= H * d && rs <= (1 << 23) && rs % 8 == 0));
+    return plain && reinterpret_cast<uintptr_t>(t.data_ptr()) % 16 == 0 ? t : dense(t);
+}
+int64_t row_stride(const Tensor& t) { return t.size(0) > 1 ? t.stride(0) : t.size(1) * t.size(2); }
+
+struct Turn {
+    std::vector<int64_t> sections;
+    bool interleaved;
+};
+// {q, k (undefined where there is none)} turned
+variable_list turned(const Tensor& q, const Tensor& k, const Tensor& positions, const Tensor& freqs, const Turn& turn, bool inverse)
+{
+    const Tensor q3 = rows(q.reshape({-1, q.size(-2), q.size(-1)}));
+    const Tensor k3 = k.defined() ? rows(k.reshape({-1, k.size(-2), k.size(-1)})) : Tensor();
+    variable_list y{at::empty(q.sizes(), q.options()), k.defined() ? at::empty(k.sizes(), k.options()) : Tensor()};
+    std::vector<int> sections(turn.sections.begin(), turn.sections.end());
+    const unsigned flags = format_flag(q) | (positions.scalar_type() == at::kInt     ? AVION_FLAG_TOKENS_I32
+                                             : positions.scalar_type() == at::kFloat ? AVION_FLAG_POSITIONS_F32
+                                                                                     : 0u) |
+                           (turn.interleaved ? AVION_FLAG_INTERLEAVED : 0u) | (inverse ? AVION_FLAG_INVERSE : 0u);
+    check(avion_rotary(q3.data_ptr(), data_of(k3), positions.data_ptr(), freqs.data_ptr<float>(), y[0].data_ptr(), data_of(y[1]), q3.size(0),
+                       positions.numel() / (int64_t)sections.size(), (int)q3.size(1), k3.defined() ? (int)k3.size(1) : 0, (int)q3.size(2),
+                       (int)freqs.numel(), sections.data(), (int)sections.size(), row_stride(q3), k3.defined() ? row_stride(k3) : 0, flags,
+                       stream()));
+    return y;
+}
+// what either node below keeps: positions and freqs, not q, not k
+void keep_turn(AutogradContext* ctx, const Tensor& positions, const Tensor& freqs, const std::vector<int64_t>& sections, bool interleaved)
+{
+    ctx->save_for_backward({positions, freqs});
+    ctx->saved_data["sections"] = sections;
+    ctx->saved_data["interleaved"] = interleaved;
+    ctx->saved_data["positions"] = positions.scalar_type();
+    ctx->saved_data["shape"] = positions.sizes().vec();
+    ctx->set_materialize_grads(false);
+}
+// the gradients a and b (b undefined: none) turned back
+variable_list turn_back(AutogradContext* ctx, const Tensor& a, const Tensor& b)
+{
+    const c10::DeviceGuard guard(a.device());
+    const variable_list s = ctx->get_saved_variables();
+    const std::vector<int64_t> sections = ctx->saved_data["sections"].toIntVector();
+    int64_t pairs = 0;
+    for (int64_t n : sections) pairs += n;
+    require(s[0], "positions", ctx->saved_data["shape"].toIntVector(), ctx->saved_data["positions"].toScalarType(), a);
+    require(s[1], "freqs", {pairs}, at::kFloat, a);
+    variable_list g = turned(a, b, s[0], s[1], {sections, ctx->saved_data["interleaved"].toBool()}, true);
+    depends_on(g[0], "rotary", {a});
+    depends_on(g[1], "rotary", {b});
+    return g;
+}
+struct RotaryOne : torch::autograd::Function<RotaryOne> {
+    static Tensor forward(AutogradContext* ctx, const Tensor& q, const Tensor& positions, const Tensor& freqs,
+                          const std::vector<int64_t>& sections, bool interleaved)
+    {
+        const c10::DeviceGuard guard(q.device());
+        keep_turn(ctx, positions, freqs, sections, interleaved);
+        return turned(q, Tensor(), positions, freqs, {sections, interleaved}, false)[0];
+    }
+    static variable_list backward(AutogradContext* ctx, variable_list grad)
+    {
+        variable_list out(5);
+        if (grad[0].defined()) out[0] = turn_back(ctx, grad[0], Tensor())[0];
+        return out;
+    }
+};
+struct Rotary : torch::autograd::Function<Rotary> {
+    static variable_list forward(AutogradContext* ctx, const Tensor& q, const Tensor& k, const Tensor& positions, const Tensor& freqs,
+                                 const std::vector<int64_t>& sections, bool interleaved)
+    {
+        const c10::DeviceGuard guard(q.device());
+        keep_turn(ctx, positions, freqs, sections, interleaved);
+        return turned(q, k, positions, freqs, {sections, interleaved}, false);
+    }
+    static variable_list backward(AutogradContext* ctx, variable_list grad)
+    {
+        variable_list out(6);
+        if (grad[0].defined() && grad[1].defined()) {
+            const variable_list g = turn_back(ctx, grad[0], grad[1]);
+            out[0] = g[0];
+            out[1] = g[1];
+        } else if (grad[0].defined() || grad[1].defined()) {
+            const int which = grad[0].defined() ? 0 : 1;
+            out[which] = turn_back(ctx, grad[which], Tensor())[0];
+        }
+        return out;
+    }
+};
+pybind11::object rotary(pybind11::handle q_, pybind11::handle k_, pybind11::handle positions_, pybind11::handle freqs_,
+                        const std::vector<int64_t>& sections, bool interleaved)
+{
+    HANDLE_TH_ERRORS
+    const Tensor *q, *k = nullptr, *positions, *freqs;
+    if (!plain(q_.ptr(), &q) || (!k_.is_none() && !plain(k_.ptr(), &k)) || !plain(positions_.ptr(), &positions) ||
+        !plain(freqs_.ptr(), &freqs) || !plain_thread())
+        return pybind11::none();
+    if (!element_format(*q) || q->dim() < 3 || !fits_int(*q) || freqs->scalar_type() != at::kFloat || freqs->dim() != 1 ||
+        positions->device() != q->device() || freqs->device() != q->device() || sections.empty() ||
+        positions->numel() % (int64_t)sections.size() != 0 ||
+        (positions->scalar_type() != at::kLong && positions->scalar_type() != at::kInt && positions->scalar_type() != at::kFloat))
+        return pybind11::none();
+    if (k && (k->scalar_type() != q->scalar_type() || k->device() != q->device() || k->dim() != q->dim() || k->size(-1) != q->size(-1) ||
+              !fits_int(*k) || k->sizes().slice(0, k->dim() - 2) != q->sizes().slice(0, q->dim() - 2)))
+        return pybind11::none();
+    int64_t pairs = 0;
+    for (int64_t n : sections) {
+        if (n < 0 || n > INT32_MAX) return pybind11::none();
+        pairs += n;
+    }
+    if (pairs != freqs->numel()) return pybind11::none();
+    const auto call = [&]() -> variable_list {
+        const Tensor kk = k ? *k : Tensor(), p = positions->contiguous(), f = freqs->contiguous();
+        if (k && records({q, k})) return Rotary::apply(*q, kk, p, f, sections, interleaved);
+        if (!k && records({q})) return {RotaryOne::apply(*q, p, f, sections, interleaved)};
+        const c10::DeviceGuard guard(q->device());
+        return turned(*q, kk, p, f, {sections, interleaved}, false);
+    };
+    if (!k) return without_lock([&] { return call()[0]; });
+    return many_without_lock(call);
+    END_HANDLE_TH_ERRORS_PYBIND
+}
+
+// the sizes of one call, in the C interface's order
+struct RaggedSizes {
+    int64_t Tq, Tk, S;
+    int Hq, Hk, d;
+    RaggedSizes(const Tensor& q, const Tensor& k, const Tensor& offsets)
+        : Tq(q.size(0)), Tk(k.size(0)), S(offsets.size(0) - 1), Hq((int)q.size(1)), Hk((int)k.size(1)), d((int)q.size(2))
+    {
+    }
+};
+struct RaggedOut {
+    Tensor q, k, v, o, lse;
+};
+RaggedOut ragged_fwd(const Tensor& q_, const Tensor& k_, const Tensor& v_, const Tensor& offsets, const Tensor& offsets_k, double scale, bool causal)
+{
+    RaggedOut r{rows(q_), rows(k_), rows(v_), Tensor(), Tensor()};
+    const RaggedSizes s(r.q, r.k, offsets);
+    r.o = at::empty({s.Tq, s.Hq, s.d}, r.q.options());
+    r.lse = at::empty({s.Hq, s.Tq}, r.q.options().dtype(at::kFloat));
+    const size_t need = avion_ragged_fwd_workspace_bytes(s.Tq, s.Tk, s.S, s.Hq, s.Hk, s.d);
+    const Tensor ws = need > 256 ? workspace(need, r.q) : Tensor();
+    check(avion_ragged_fwd(r.q.data_ptr(), r.k.data_ptr(), r.v.data_ptr(), offsets.data_ptr<int>(), offsets_k.data_ptr<int>(), r.o.data_ptr(),
+                           r.lse.data_ptr<float>(), s.Tq, s.Tk, s.S, s.Hq, s.Hk, s.d, row_stride(r.q), row_stride(r.k), row_stride(r.v),
+                           (float)scale, format_flag(r.q) | (causal ? AVION_FLAG_CAUSAL : 0u), data_of(ws), need, stream()));
+    return r;
+}
+struct AttentionRagged : torch::autograd::Function<AttentionRagged> {
+    static Tensor forward(AutogradContext* ctx, const Tensor& q, const Tensor& k, const Tensor& v, const Tensor& offsets, const Tensor& offsets_k,
+                          double scale, bool causal)
+    {
+        const c10::DeviceGuard guard(q.device());
+        const RaggedOut r = ragged_fwd(q, k, v, offsets, offsets_k, scale, causal);
+        ctx->save_for_backward({r.q, r.k, r.v, offsets, offsets_k, r.o, r.lse});
+        ctx->saved_data["scale"] = scale;
+        ctx->saved_data["causal"] = causal;
+        ctx->saved_data["keys"] = r.k.sizes().vec();
+        ctx->saved_data["borders"] = offsets.size(0);
+        return r.o;
+    }
+    static variable_list backward(AutogradContext* ctx, variable_list grad)
+    {
+        const c10::DeviceGuard guard(grad[0].device());
+        const variable_list saved = ctx->get_saved_variables();
+        const Tensor dO = dense(grad[0]);
+        const at::ScalarType dt = dO.scalar_type();
+        const std::vector<int64_t> keys = ctx->saved_data["keys"].toIntVector();
+        const int64_t borders = ctx->saved_data["borders"].toInt();
+        // (rows() of what came back: an unpacked tensor may have other strides)
+        const Tensor q = saved[0].dim() == 3 ? rows(saved[0]) : saved[0], k = saved[1].dim() == 3 ? rows(saved[1]) : saved[1],
+                     v = saved[2].dim() == 3 ? rows(saved[2]) : saved[2];
+        const auto same = [&](const Tensor& t, const char* name, at::IntArrayRef shape) {
+            TORCH_CHECK_VALUE(t.is_cuda() && t.device() == dO.device() && t.scalar_type() == dt && t.sizes() == shape, name,
+                              " must live on the GPU of the gradient, be ", dt, " and have shape ", shape);
+        };
+        same(q, "q", dO.sizes());
+        same(k, "k", keys);
+        same(v, "v", keys);
+        require(saved[3], "offsets", {borders}, at::kInt, dO);
+        require(saved[4], "offsets_k", {borders}, at::kInt, dO);
+        require(saved[5], "o", dO.sizes(), dt, dO);
+        require(saved[6], "lse", {dO.size(1), dO.size(0)}, at::kFloat, dO);
+        const RaggedSizes s(q, k, saved[3]);
+        const Tensor dq = at::empty(q.sizes(), q.options()), dk = at::empty(k.sizes(), k.options()), dv = at::empty(v.sizes(), v.options());
+        const size_t need = avion_ragged_bwd_workspace_bytes(s.Tq, s.Tk, s.S, s.Hq, s.Hk, s.d);
+        const Tensor ws = workspace(need, q);
+        check(avion_ragged_bwd(q.data_ptr(), k.data_ptr(), v.data_ptr(), saved[3].data_ptr<int>(), saved[4].data_ptr<int>(), saved[5].data_ptr(),
+                               saved[6].data_ptr<float>(), dO.data_ptr(), dq.data_ptr(), dk.data_ptr(), dv.data_ptr(), s.Tq, s.Tk, s.S, s.Hq,
+                               s.Hk, s.d, row_stride(q), row_stride(k), row_stride(v), (float)ctx->saved_data["scale"].toDouble(),
+                               format_flag(q) | (ctx->saved_data["causal"].toBool() ? AVION_FLAG_CAUSAL : 0u), ws.data_ptr(), need, stream()));
+        for (const Tensor& t : {dq, dk, dv}) depends_on(t, "attention_ragged", {grad[0], saved[0], saved[1], saved[2]});
+        return {dq, dk, dv, Tensor(), Tensor(), Tensor(), Tensor()};
+    }
+};
+pybind11::object attention_ragged(pybind11::handle q_, pybind11::handle k_, pybind11::handle v_, pybind11::handle offsets_,
+                                  pybind11::handle offsets_k_, double scale, bool causal)
+{
+    HANDLE_TH_ERRORS
+    const Tensor *q, *k, *v, *offsets, *offsets_k;
+    if (!plain(q_.ptr(), &q) || !plain(k_.ptr(), &k) || !plain(v_.ptr(), &v) || !plain(offsets_.ptr(), &offsets) ||
+        !plain(offsets_k_.ptr(), &offsets_k) || !plain_thread())
+        return pybind11::none();
+    if (q->dim() != 3 || !element_format(*q) || !fits_int(*q) || !fits_int(*k) || k->dim() != 3 || k->size(2) != q->size(2) ||
+        v->sizes() != k->sizes() || offsets->dim() != 1 || offsets_k->sizes() != offsets->sizes())
+        return pybind11::none();
+    for (const Tensor* t : {k, v})
+        if (t->scalar_type() != q->scalar_type() || t->device() != q->device()) return pybind11::none();
+    for (const Tensor* t : {offsets, offsets_k})
+        if (t->scalar_type() != at::kInt || t->device() != q->device()) return pybind11::none();
+    return without_lock([&] {
+        const Tensor a = offsets->contiguous(), b = offsets_k->contiguous();
+        if (records({q, k, v})) return AttentionRagged::apply(*q, *k, *v, a, b, scale, causal);
+        const c10::DeviceGuard guard(q->device());
+        return ragged_fwd(*q, *k, *v, a, b, scale, causal).o;
+    });
+    END_HANDLE_TH_ERRORS_PYBIND
+}
+
 }  // namespace
 
 PYBIND11_MODULE(_avion_torch, m)
@@ -733,4 +959,6 @@ PYBIND11_MODULE(_avion_torch, m)
     m.def("add_rms_norm_fp8", &add_rms_norm_fp8);
     m.def("quantize_rows", &quantize_rows);
     m.def("linear_fp8", &linear_fp8);
+    m.def("rotary", &rotary);
+    m.def("attention_ragged", &attention_ragged);
 }
