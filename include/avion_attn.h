@@ -435,6 +435,42 @@ int avion_ragged_bwd(const void *q, const void *k, const void *v, const int *off
                      void *workspace, size_t workspace_bytes, void *stream);
 
 /*
+ * Softmax cross entropy of a linear layer's outputs that are never kept: the words of a text decoder over its vocabulary, or a
+ * contrastive batch (row i of x belongs to row i of w).  With z = scale * x w^T:
+ *     lse_m = ln sum_v exp z_mv;  loss_m = lse_m - z_{m,t_m};  dz = (softmax(z) - onehot(t)) * dloss_m;  dx = scale dz w;  dw = scale dz^T x
+ *   x, dx   : [T, D], w, dw : [V, D]; bf16 (fp16 with AVION_FLAG_F16).  Rows of x and w are rs_x and rs_w elements apart (multiples
+ *             of 8); dx and dw are contiguous
+ *   targets : [T] int64 (int32 with AVION_FLAG_TOKENS_I32).  A target outside [0, V), or equal to ignore_index, is none: that row's loss
+ *             is 0, and its dz zeros (dw takes zero times what the row of x holds: infinities and NaN in it do propagate there)
+ *   loss, lse : out, fp32 [T]; loss may be NULL where total is given.   total : out, fp32 [2], or NULL: the sum of the losses (their
+ *             mean over the rows with a target, 0 if there is none, with AVION_FLAG_MEAN) and the number of rows with a target
+ *   dloss   : in, fp32 [T], or with AVION_FLAG_ONE_GRADIENT one number, the gradient of total[0]; then with AVION_FLAG_MEAN it is divided
+ *             by total[1]
+ *   dx, dw  : out, fully overwritten; either may be NULL (not both)
+ *   scale > 0 and finite; D a multiple of 8 up to 65536; T, V up to 2^28; rs up to 2^20
+ *   workspace: 256-byte aligned, avion_linear_ce_fwd_workspace_bytes / _bwd_workspace_bytes bytes (0: unsupported), contents ignored and
+ *   left unspecified; calls that overlap in time must not share one.  The backward takes the vocabulary in pieces: dz of one piece
+ *   (at most 1 GB, or 256 columns) and, where there are several, dx in fp32 lie in it
+ * Logits, statistics and sums in fp32, dz rounded to the format before its products (fp16: scaled by the largest |dloss| and 2^14,
+ * so that small probabilities keep their bits), results rounded once.  No atomics: the same sizes give the same bits.
+ * T = 0: total and dw become zeros.  Pointers 16-byte aligned (fp32 ones and targets naturally).
+ */
+#define AVION_FLAG_MEAN 256u
+#define AVION_FLAG_ONE_GRADIENT 512u
+
+size_t avion_linear_ce_fwd_workspace_bytes(long long T, long long V, int D);
+
+int avion_linear_ce_fwd(const void *x, const void *w, const void *targets, float *loss, float *lse, float *total,
+                        long long T, long long V, int D, long long rs_x, long long rs_w, float scale, long long ignore_index,
+                        unsigned flags, void *workspace, size_t workspace_bytes, void *stream);
+
+size_t avion_linear_ce_bwd_workspace_bytes(long long T, long long V, int D);
+
+int avion_linear_ce_bwd(const void *x, const void *w, const void *targets, const float *lse, const float *dloss, const float *total,
+                        void *dx, void *dw, long long T, long long V, int D, long long rs_x, long long rs_w, float scale,
+                        long long ignore_index, unsigned flags, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
  * Allocation-free backward, for callers that cannot provide device scratch of their own: code
  * under HIP graph capture, tight serving or training loops, harnesses that forbid hipMalloc.
  * Same operation, arguments, rules and bits as avion_attn_bwd (bf16, not causal), without the

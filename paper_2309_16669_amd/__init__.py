@@ -16,7 +16,7 @@ LIB_PATH = os.path.join(_PKG, "libavion_attn.so")
 
 OK, EINVAL, EUNSUPPORTED, EWORKSPACE, EHIP, ESCRATCH = 0, -1, -2, -3, -4, -5
 FLAG_F16, FLAG_CAUSAL, FLAG_QKVPACKED, FLAG_WIDE_F32, FLAG_TOKENS_I32 = 1, 2, 4, 8, 16
-FLAG_INTERLEAVED, FLAG_INVERSE, FLAG_POSITIONS_F32 = 32, 64, 128
+FLAG_INTERLEAVED, FLAG_INVERSE, FLAG_POSITIONS_F32, FLAG_MEAN, FLAG_ONE_GRADIENT = 32, 64, 128, 256, 512
 
 _lib = None
 
@@ -118,6 +118,13 @@ def load_library() -> ctypes.CDLL:
         lib.avion_ragged_fwd.argtypes = [p, p, p, p, p, p, p, ll, ll, ll, i, i, i, ll, ll, ll, f, u, p, sz, p]
         lib.avion_ragged_bwd.restype = i
         lib.avion_ragged_bwd.argtypes = [p, p, p, p, p, p, p, p, p, p, p, ll, ll, ll, i, i, i, ll, ll, ll, f, u, p, sz, p]
+        for entry in (lib.avion_linear_ce_fwd_workspace_bytes, lib.avion_linear_ce_bwd_workspace_bytes):
+            entry.restype = sz
+            entry.argtypes = [ll, ll, i]
+        lib.avion_linear_ce_fwd.restype = i
+        lib.avion_linear_ce_fwd.argtypes = [p, p, p, p, p, p, ll, ll, i, ll, ll, f, ll, u, p, sz, p]
+        lib.avion_linear_ce_bwd.restype = i
+        lib.avion_linear_ce_bwd.argtypes = [p, p, p, p, p, p, p, p, ll, ll, i, ll, ll, f, ll, u, p, sz, p]
         _lib = lib
     return _lib
 
@@ -678,3 +685,61 @@ def ragged_bwd(q, k, v, offsets_q, offsets_k, o, lse, dO, dq, dk, dv, scale: flo
     _launch(_one_device(q, k, v, offsets_q, offsets_k, o, lse, dO, dq, dk, dv, workspace), load_library().avion_ragged_bwd,
             (_ptr(q), _ptr(k), _ptr(v), _ptr(offsets_q), _ptr(offsets_k), _ptr(o), _ptr(lse), _ptr(dO), _ptr(dq), _ptr(dk), _ptr(dv),
              *sizes, *strides, float(scale), _flags(q.dtype, causal, False), _ptr(workspace), workspace.numel()), stream)
+
+
+def _matrix(t, name, dtype, cols=None):
+    """Rows [n, D] with contiguous columns: the elements between two rows."""
+    if not t.is_cuda:
+        raise ValueError(f"{name} must live on the GPU")
+    if t.dtype != dtype:
+        raise ValueError(f"{name} must be {dtype}, got {t.dtype}")
+    if t.dim() != 2 or (cols is not None and t.shape[1] != cols):
+        raise ValueError(f"{name} must have shape {('any', 'any' if cols is None else cols)}, got {tuple(t.shape)}")
+    if t.shape[1] > 1 and t.stride(1) != 1:
+        raise ValueError(f"{name}: rows must be contiguous")
+    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
+
+
+def linear_ce_fwd_workspace_bytes(T: int, V: int, D: int) -> int:
+    return int(load_library().avion_linear_ce_fwd_workspace_bytes(T, V, D))
+
+
+def linear_ce_bwd_workspace_bytes(T: int, V: int, D: int) -> int:
+    return int(load_library().avion_linear_ce_bwd_workspace_bytes(T, V, D))
+
+
+def linear_ce_fwd(x, w, targets, loss, lse, total, scale: float, ignore_index: int, workspace, mean: bool = False, stream=None) -> None:
+    """avion_linear_ce_fwd: x [T, D] and w [V, D] bf16 or fp16, rows of any stride; targets int64 or int32 [T]; loss (or None) and lse
+    fp32 [T]; total fp32 [2] (or None): sum, or mean, of the losses and the number of targets."""
+    import torch
+    (T, D), V = x.shape, w.shape[0]
+    strides = _matrix(x, "x", x.dtype), _matrix(w, "w", x.dtype, D)
+    flags = _flags(x.dtype, False, False) | _tokens_flag(targets) | (FLAG_MEAN if mean else 0)
+    _require(targets, "targets", targets.dtype, (T,))
+    for t, n, shape in ((loss, "loss", (T,)), (lse, "lse", (T,)), (total, "total", (2,))):
+        if t is not None:
+            _require(t, n, torch.float32, shape)
+    _require(workspace, "workspace", torch.uint8)
+    _launch(_one_device(x, w, targets, loss, lse, total, workspace), load_library().avion_linear_ce_fwd,
+            (_ptr(x), _ptr(w), _ptr(targets), _opt(loss), _opt(lse), _opt(total), T, V, D, *strides, float(scale), int(ignore_index), flags,
+             _ptr(workspace), workspace.numel()), stream)
+
+
+def linear_ce_bwd(x, w, targets, lse, dloss, total, dx, dw, scale: float, ignore_index: int, workspace, mean: bool = False, stream=None) -> None:
+    """avion_linear_ce_bwd: dloss fp32 [T] (a gradient for each row) or of one element (of the sum, or with `mean` of the mean; total
+    as the forward wrote it); dx [T, D] and dw [V, D] contiguous, either may be None."""
+    import torch
+    (T, D), V = x.shape, w.shape[0]
+    strides = _matrix(x, "x", x.dtype), _matrix(w, "w", x.dtype, D)
+    one = dloss.dim() == 0 or mean
+    flags = _flags(x.dtype, False, False) | _tokens_flag(targets) | (FLAG_MEAN if mean else 0) | (FLAG_ONE_GRADIENT if one else 0)
+    _require(targets, "targets", targets.dtype, (T,))
+    _require(lse, "lse", torch.float32, (T,))
+    _require(dloss, "dloss", torch.float32, () if one else (T,))
+    for t, n, dt, shape in ((total, "total", torch.float32, (2,)), (dx, "dx", x.dtype, (T, D)), (dw, "dw", x.dtype, (V, D))):
+        if t is not None:
+            _require(t, n, dt, shape)
+    _require(workspace, "workspace", torch.uint8)
+    _launch(_one_device(x, w, targets, lse, dloss, total, dx, dw, workspace), load_library().avion_linear_ce_bwd,
+            (_ptr(x), _ptr(w), _ptr(targets), _ptr(lse), _ptr(dloss), _opt(total), _opt(dx), _opt(dw), T, V, D, *strides, float(scale),
+             int(ignore_index), flags, _ptr(workspace), workspace.numel()), stream)

@@ -42,6 +42,7 @@ from . import (attn_bwd_ex, attn_bwd_workspace_bytes, attn_fwd_ex, bias_gelu_bwd
 from . import (embedding_bwd, embedding_bwd_workspace_bytes, embedding_fwd, rmsnorm_bwd, rmsnorm_bwd_workspace_bytes, rmsnorm_fwd,
                rmsnorm_fwd_fp8)
 from . import linear_fp8 as _linear_fp8, quantize_rows as _quantize_rows, rotary as _rotary
+from . import linear_ce_bwd, linear_ce_bwd_workspace_bytes, linear_ce_fwd, linear_ce_fwd_workspace_bytes
 from . import ragged_bwd, ragged_bwd_workspace_bytes, ragged_fwd, ragged_fwd_workspace_bytes
 
 _native = None
@@ -566,3 +567,58 @@ def attention_ragged(q, k, v, offsets, offsets_k=None, scale: float | None = Non
             raise ValueError(f"{n} must be int32 of shape [S + 1] on the GPU of q, got {t.dtype} {tuple(t.shape)}")
     o = (_native or native_calls()).attention_ragged(q, k, v, offsets, offsets_k, scale, causal)
     return _AttentionRagged.apply(q, k, v, offsets.contiguous(), offsets_k.contiguous(), scale, causal) if o is None else o
+
+
+def _columns(t):
+    """t [n, D] with contiguous rows at multiples of 16 bytes: itself where it is such, else a copy."""
+    n, D = t.shape
+    plain = (D == 1 or t.stride(1) == 1) and (n < 2 or D <= t.stride(0) <= 1 << 20 and t.stride(0) % 8 == 0)
+    return t if plain and t.data_ptr() % 16 == 0 else _dense(t)
+
+
+class _LinearCrossEntropy(torch.autograd.Function):
+    """reduction: 0 none, 1 mean, 2 sum.  Keeps x, weight, the targets and one float a row; no logits."""
+
+    @staticmethod
+    def forward(ctx, x, weight, targets, scale, ignore_index, reduction):
+        x2, w = _columns(x.reshape(-1, x.shape[-1])), _columns(weight)
+        T, (V, D) = x2.shape[0], w.shape
+        t = targets.contiguous().view(-1)
+        lse = torch.empty((T,), dtype=torch.float32, device=x.device)
+        loss = torch.empty((T,), dtype=torch.float32, device=x.device) if reduction == 0 else None
+        total = None if reduction == 0 else torch.empty((2,), dtype=torch.float32, device=x.device)
+        linear_ce_fwd(x2, w, t, loss, lse, total, scale, ignore_index, _bytes_on(x.device, linear_ce_fwd_workspace_bytes(T, V, D)),
+                      reduction == 1)
+        ctx.save_for_backward(x2, w, t, lse, *(() if total is None else (total,)))
+        ctx.args, ctx.shape = (scale, ignore_index, reduction), x.shape
+        return loss.view(targets.shape) if reduction == 0 else total[0].clone()
+
+    @staticmethod
+    def backward(ctx, given):
+        x2, w, t, lse, *total = ctx.saved_tensors
+        scale, ignore_index, reduction = ctx.args
+        x2, w = _columns(x2), _columns(w)
+        dx = torch.empty(x2.shape, dtype=x2.dtype, device=x2.device) if ctx.needs_input_grad[0] else None
+        dw = torch.empty(w.shape, dtype=w.dtype, device=w.device) if ctx.needs_input_grad[1] else None
+        dloss = given.contiguous().view(-1 if reduction == 0 else ())
+        linear_ce_bwd(x2, w, t, lse, dloss, total[0] if total else None, dx, dw, scale, ignore_index,
+                      _bytes_on(w.device, linear_ce_bwd_workspace_bytes(x2.shape[0], *w.shape)), reduction == 1)
+        dx = None if dx is None else _depends_on(dx.view(ctx.shape), "linear_cross_entropy", given, x2, w)
+        return dx, _depends_on(dw, "linear_cross_entropy", given, x2, w), None, None, None, None
+
+
+def linear_cross_entropy(x, weight, targets, scale: float = 1.0, ignore_index: int = -100, reduction: str = "mean"):
+    """Softmax cross entropy of the logits scale * x weight^T, which are never kept: x [..., D] and weight [V, D] in bf16 or fp16, D a
+    multiple of 8, targets (int64 or int32) of the shape [...].  weight may be a token table (the words of a text decoder) or the
+    other side of a contrastive batch, with targets 0, 1, 2, ....  A target outside [0, V), or equal to ignore_index, is none: its
+    row's loss is 0.  reduction "mean" (over the rows with a target; 0 where there is none), "sum" or "none" (one loss a row, in
+    fp32).  Differentiable once in x and weight; keeps one float a row."""
+    kinds = {"none": 0, "mean": 1, "sum": 2}
+    if reduction not in kinds:
+        raise ValueError(f"reduction must be 'mean', 'sum' or 'none', got {reduction!r}")
+    if weight.dim() != 2 or x.dim() < 1 or x.shape[-1] != weight.shape[1]:
+        raise ValueError(f"weight must have shape (V, {x.shape[-1] if x.dim() else '?'}), got {tuple(weight.shape)}")
+    if targets.shape != x.shape[:-1]:
+        raise ValueError(f"targets must have shape {tuple(x.shape[:-1])}, got {tuple(targets.shape)}")
+    loss = (_native or native_calls()).linear_cross_entropy(x, weight, targets, float(scale), int(ignore_index), kinds[reduction])
+    return _LinearCrossEntropy.apply(x, weight, targets, float(scale), int(ignore_index), kinds[reduction]) if loss is None else loss

@@ -1,0 +1,530 @@
+// Softmax cross entropy of a linear layer's outputs that are never kept: rows x [T, D] against a table w [V, D] (the vocabulary of a
+// text decoder, or the other side of a contrastive batch), z = s x w^T:
+//     lse_m = ln sum_v exp z_mv,   loss_m = lse_m - z_{m, t_m}
+//     dz = (softmax(z) - onehot(t)) dloss_m,   dx = s dz w,   dw = s dz^T x
+// T V numbers do not fit what T D and V D do, so the forward forms z tile by tile and keeps a running maximum and sum a row; the
+// backward forms it again, one piece of the vocabulary after the other, rounds dz of that piece to the operands' format (workspace,
+// bounded) and multiplies it with w and with x.  2 T V D operations forward, 6 backward; all four products are bound by the matrix
+// units, the forward of few rows by w's bytes.
+//
+// The product.  C [b, a] = sum_k B[b, k] A[a, k], tiles of TB x TA, 64 deep steps; an operand lies in memory either with k contiguous
+// (rows x or w) or with its own index contiguous (its rows are k: dz and x in dw, w in dx).
+//   Either comes to LDS by LDS-direct loads, 128 bytes of k a row or whole rows of the tile's width, and leaves it as fragments
+//   of 8 consecutive k: rows of 128 bytes with ds_read_b128, their eight 16-byte chunks permuted by a XOR with bits 1..3 of the row
+//   number; rows of k with two transposing ds_read_b64_tr_b16 (4 k each), their 64-byte units permuted by a XOR with the row
+//   number mod 4.  Both meet distinct banks.
+//   Two buffers of a step; fragments of 16 k are read while the 16 before are multiplied; before a step's last ones the next step
+//   is awaited, and this one's buffer, which everybody then holds in registers, is filled again.  Steps of a workgroup's tiles
+//   form one stream, so that the next tile's first steps are on their way during the end of a tile.
+//   A is the contiguous index of the result: a lane's accumulators are 4 consecutive a of one row b.
+#pragma once
+#include "avion_common.h"
+
+enum class Along { kK, kIndex };  // what is contiguous in memory
+
+struct LossOperand {
+    const raw16* p;
+    long ld;      // elements between rows
+    int extent;   // of its own index
+    int rows;     // kIndex: rows of k that there are (the others count as zeros)
+};
+
+constexpr int kLossStep = 64;  // k of a step
+
+// One operand's tile in a buffer: how this wavefront brings it there and how a lane reads it
+template <Along ALONG, int W, int WAVES>
+struct LossTile {
+    static constexpr int BYTES = W * 128, BLOCKS = W / 8, PER = (BLOCKS + WAVES - 1) / WAVES;
+    static constexpr int CPR = ALONG == Along::kK ? 8 : W / 8, RPB = 64 / CPR, ROW = CPR * 16;  // chunks a row, rows a 1 KB block
+    static_assert(ALONG == Along::kK || (W >= 128 && W <= 512), "a row of k holds whole groups of four 64-byte units");
+    static_assert(WAVES % 2 == 0 || ALONG == Along::kIndex, "a wavefront's blocks are all even or all odd");
+    LossOperand op;
+    int K, wave;
+    unsigned row_at, chunk;  // this lane's part of a load: byte offset of its row in block `wave`, byte offset in the row
+    unsigned read_at;        // of a fragment
+    unsigned turn;
+    u32x4 desc;
+
+    DEVINL LossTile(const LossOperand& op_, int K_, int wave_, int lane) : op(op_), K(K_), wave(wave_)
+    {
+        const unsigned row = (unsigned)(wave * RPB + lane / CPR);
+        row_at = row * (unsigned)(op.ld * 2);
+        if constexpr (ALONG == Along::kK) chunk = ((lane & 7) ^ (lane >> 4 & 3) ^ (wave & 1) * 4) * 16;
+        else chunk = (((unsigned)lane % CPR) ^ (row & 3) * 4) * 16;
+        const int l32 = lane % 32, g = lane / 32, G = lane >> 4, j = lane & 15;
+        if constexpr (ALONG == Along::kK) {
+            read_at = (unsigned)l32 * 128;
+            turn = (g ^ (l32 >> 1 & 7)) * 16;
+        } else {
+            read_at = (unsigned)(8 * g + (j >> 2)) * ROW + (G & 1) * 32 + (j & 3) * 8;
+            turn = (j >> 2) * 64;
+        }
+        desc = RawBuffer(op.p, 0).words;
+    }
+    // the tile begins at index i0
+    DEVINL void tile(int i0)
+    {
+        if constexpr (ALONG == Along::kK) {
+            const int rows = min(op.extent - i0, W);
+            desc = RawBuffer(op.p + (long)i0 * op.ld, (unsigned)(((long)(rows - 1) * op.ld + K) * 2)).words;
+        }
+    }
+    // its step from k0 on, to LDS address `to`
+    DEVINL void fetch(int i0, int k0, unsigned to) const
+    {
+        u32x4 d = desc;
+        unsigned v = row_at + chunk;
+        if constexpr (ALONG == Along::kK) {
+            v = (unsigned)k0 * 2 + chunk < (unsigned)K * 2 ? v + (unsigned)k0 * 2 : kOutOfRangeBase;
+        } else {
+            const int rows = min(op.rows - k0, kLossStep);
+            d = RawBuffer(op.p + (long)k0 * op.ld + i0, rows > 0 ? (unsigned)(((long)(rows - 1) * op.ld + (op.extent - i0)) * 2) : 0).words;
+        }
+        const unsigned down = (unsigned)(WAVES * RPB) * (unsigned)(op.ld * 2);
+        const RawBuffer b(d);
+        const unsigned at = to + wave * 1024;
+        if constexpr (PER % 4 == 0 && BLOCKS % WAVES == 0) {
+#pragma unroll
+            for (int i = 0; i < PER; i += 4)
+                load_to_lds16_x4<WAVES * 1024>(b, b, b, b, at + i * WAVES * 1024, v + i * down, v + (i + 1) * down, v + (i + 2) * down, v + (i + 3) * down);
+        } else {
+#pragma unroll
+            for (int i = 0; i < PER; ++i)
+                if (BLOCKS % WAVES == 0 || wave + i * WAVES < BLOCKS) load_to_lds16(b, at + i * WAVES * 1024, v + i * down);
+        }
+    }
+    // fragment of the 32 indexes from 32 * t on, k 16 * ks .. (the wavefront's lanes: index l % 32, 8 k of half l / 32)
+    DEVINL frag8 read(unsigned from, int t, int ks) const
+    {
+        if constexpr (ALONG == Along::kK) {
+            typedef const __attribute__((address_space(3))) frag8* ptr;
+            return *(ptr)(from + read_at + (turn ^ (ks * 32)) + t * 4096);
+        } else {
+            const unsigned at = from + read_at + (((unsigned)t * 64) ^ turn) + ks * 16 * ROW;
+            const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)at);
+            const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(at + 4 * ROW));
+            const u32x2 l2 = __builtin_bit_cast(u32x2, lo), h2 = __builtin_bit_cast(u32x2, hi);
+            return as_frag8(u32x4{l2[0], l2[1], h2[0], h2[1]});
+        }
+    }
+};
+
+template <Along AA, Along AB, int TA_, int TB_, int WA_, int WB_>
+struct LossCfg {
+    static constexpr int TA = TA_, TB = TB_, WA = WA_, WB = WB_;
+    static constexpr int WAVES = WA * WB, NT = WAVES * 64;
+    static constexpr int NI = TA / WA / 32, MI = TB / WB / 32;  // 32 x 32 tiles of a wavefront
+    using TileA = LossTile<AA, TA, WAVES>;
+    using TileB = LossTile<AB, TB, WAVES>;
+    static constexpr int STAGE = TileA::BYTES + TileB::BYTES;
+    static constexpr int OUT_ROW = NI * 64 + 16, OUT_BYTES = 32 * OUT_ROW;  // a wavefront's rows on their way out, in a free buffer's place
+    static constexpr int LDS_BYTES = 2 * STAGE + WAVES * (NI == 2 ? 16 : 32) * OUT_ROW;
+    // one workgroup of eight wavefronts a compute unit, or as many of four as LDS takes, two at least
+    static constexpr int WAVES_PER_SIMD = 2;
+    static_assert(LDS_BYTES <= 160 * 1024, "");
+};
+
+DEVINL void loss_landed_barrier() { asm volatile("s_waitcnt vmcnt(0)\n\ts_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+
+// The tiles place(0) .. place(count - 1) -- each sets (a0, b0) -- of one workgroup, over all of K; done(a0, b0, acc) takes a tile's sums.
+template <typename Cfg, typename E, typename Place, typename Done>
+DEVINL void loss_product(char* smem, const LossOperand& opa, const LossOperand& opb, int K, int count, int wave, int lane, Place place, Done done)
+{
+    constexpr int MI = Cfg::MI, NI = Cfg::NI;
+    if (count <= 0) return;
+    const int wa = wave % Cfg::WA, wb = wave / Cfg::WA;
+    typename Cfg::TileA ta(opa, K, wave, lane);
+    typename Cfg::TileB tb(opb, K, wave, lane);
+    const unsigned lds = lds_address(smem);
+    const int steps = (K + kLossStep - 1) / kLossStep, total = count * steps;
+    int f_n = 0, f_step = 0, f_a0 = 0, f_b0 = 0;  // next step to fetch
+    auto fetch = [&](int buf) {
+        if (f_step == 0) {
+            place(f_n, f_a0, f_b0);
+            ta.tile(f_a0);
+            tb.tile(f_b0);
+        }
+        const unsigned to = lds + buf * Cfg::STAGE;
+        ta.fetch(f_a0, f_step * kLossStep, to);
+        tb.fetch(f_b0, f_step * kLossStep, to + Cfg::TileA::BYTES);
+        if (++f_step == steps) {
+            f_step = 0;
+            ++f_n;
+        }
+    };
+    fetch(0);
+    loss_landed_barrier();
+    if (total > 1) fetch(1);
+    frag8 fa[NI], fb[MI];
+    auto read = [&](int buf, int ks) {
+        const unsigned from = lds + buf * Cfg::STAGE;
+#pragma unroll
+        for (int j = 0; j < NI; ++j) fa[j] = ta.read(from, wa * NI + j, ks);
+#pragma unroll
+        for (int i = 0; i < MI; ++i) fb[i] = tb.read(from + Cfg::TileA::BYTES, wb * MI + i, ks);
+    };
+    read(0, 0);
+    int q = 0, buf = 0;
+    f32x16 acc[MI][NI];
+    for (int n = 0; n < count; ++n) {
+#pragma unroll
+        for (int i = 0; i < MI; ++i)
+#pragma unroll
+            for (int j = 0; j < NI; ++j) acc[i][j] = f32x16_zero();
+        for (int s = 0; s < steps; ++s, ++q) {
+#pragma unroll
+            for (int ks = 0; ks < 4; ++ks) {
+                frag8 ca[NI], cb[MI];
+#pragma unroll
+                for (int j = 0; j < NI; ++j) ca[j] = fa[j];
+#pragma unroll
+                for (int i = 0; i < MI; ++i) cb[i] = fb[i];
+                if (ks < 3) {
+                    read(buf, ks + 1);
+                } else if (q + 1 < total) {
+                    loss_landed_barrier();  // the next step is there, and this one in everybody's registers
+                    if (q + 2 < total) fetch(buf);
+                    read(buf ^ 1, 0);
+                }
+                __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                for (int i = 0; i < MI; ++i)
+#pragma unroll
+                    for (int j = 0; j < NI; ++j) acc[i][j] = E::mfma(ca[j], cb[i], acc[i][j]);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            buf ^= 1;
+        }
+        int a0, b0;
+        place(n, a0, b0);
+        done(a0, b0, acc);
+    }
+}
+
+// A wavefront's 32 x (32 NI) part of a result with contiguous a, rounded, to rows of `out` (ld elements apart): through LDS, so that
+// the stores write whole rows of it.  value(j, e): register e of tile j.  Columns from `cols` on and rows from `rows` on are not stored.
+template <int NI, typename E, typename Value>
+DEVINL void loss_store(char* stage, raw16* out, long ld, int rows, int cols, int lane, Value value)
+{
+    constexpr int ROW = NI * 64 + 16, LANES = NI * 4, STEP = 64 / LANES, BATCH = NI == 2 ? 16 : 32;
+    const int l32 = lane % 32, g = lane / 32;
+#pragma unroll
+    for (int half = 0; half < 32 / BATCH; ++half) {
+        if (l32 / BATCH == half) {
+#pragma unroll
+            for (int j = 0; j < NI; ++j)
+#pragma unroll
+                for (int c = 0; c < 4; ++c)
+                    *reinterpret_cast<u32x2*>(stage + l32 % BATCH * ROW + 64 * j + 16 * c + 8 * g) =
+                        u32x2{E::pack(value(j, 4 * c), value(j, 4 * c + 1)), E::pack(value(j, 4 * c + 2), value(j, 4 * c + 3))};
+        }
+        asm volatile("" ::: "memory");  // (LDS takes a wavefront's accesses in the order of the program)
+#pragma unroll
+        for (int r = 0; r < BATCH; r += STEP) {
+            const int row = half * BATCH + r + lane / LANES, col = lane % LANES * 8;
+            if (row < rows && col < cols)
+                *reinterpret_cast<u32x4*>(out + (long)row * ld + col) = *reinterpret_cast<const u32x4*>(stage + (r + lane / LANES) * ROW + col * 2);
+        }
+        asm volatile("" ::: "memory");
+    }
+}
+
+// ------------------------------------------------------------------------------------------- forward
+struct LossArgs {
+    const raw16 *x, *w;
+    const void* targets;
+    long rs_x, rs_w;
+    int T, V, D;
+    int wide;          // targets are int64
+    long long ignore;
+    float cs;          // scale * log2 e
+    float scale;
+};
+// the target of row m, -1 where it has none
+DEVINL int loss_target(const LossArgs& a, int m)
+{
+    if (m >= a.T) return -1;
+    const long t = a.wide ? static_cast<const long*>(a.targets)[m] : (long)static_cast<const int*>(a.targets)[m];
+    return t >= 0 && t < a.V && t != a.ignore ? (int)t : -1;
+}
+
+constexpr float kLossNone = -3.0e38f;
+
+// A workgroup takes TB rows through one of `slabs` runs of vocabulary tiles.  A lane holds, for each of its MI rows, the maximum and sum
+// (base 2, scaled) over the columns that its registers hold; they meet once, at the end: parts [slabs][T] of (maximum, sum).  The lane
+// that holds a row's target leaves its logit.
+template <int TA, int TB, int WA, int WB, typename E>
+__global__ void __launch_bounds__(WA* WB * 64, 2)
+avion_loss_fwd_kernel(LossArgs a, float2* __restrict__ parts, float* __restrict__ hit, int slabs)
+{
+    using Cfg = LossCfg<Along::kK, Along::kK, TA, TB, WA, WB>;
+    constexpr int MI = Cfg::MI, NI = Cfg::NI;
+    extern __shared__ __attribute__((aligned(16))) char smem[];
+    __shared__ float2 meet[WA][TB];
+    const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), l32 = lane % 32, g = lane / 32;
+    const int wa = wave % WA, wb = wave / WA;
+    // the workgroups of an XCD (they go round) take neighbouring runs, of the same rows first
+    const int block = blockIdx.x / slabs, slab = blockIdx.x % slabs;
+    const int b0 = block * TB, ntiles = (a.V + TA - 1) / TA;
+    const int first = (int)((long)ntiles * slab / slabs), last = (int)((long)ntiles * (slab + 1) / slabs);
+    float m[MI], l[MI];
+    int target[MI];
+#pragma unroll
+    for (int i = 0; i < MI; ++i) {
+        m[i] = kLossNone;
+        l[i] = 0.f;
+        target[i] = loss_target(a, b0 + (wb * MI + i) * 32 + l32);
+    }
+    const LossOperand opa{a.w, a.rs_w, a.V, 0}, opb{a.x, a.rs_x, a.T, 0};
+    loss_product<Cfg, E>(
+        smem, opa, opb, a.D, last - first, wave, lane,
+        [&](int n, int& a0, int& bb) {
+            a0 = (first + n) * TA;
+            bb = b0;
+        },
+        [&](int a0, int, f32x16(&acc)[MI][NI]) {
+            const int from = a0 + wa * NI * 32;
+            const bool ragged = from + NI * 32 > a.V;
+#pragma unroll
+            for (int i = 0; i < MI; ++i) {
+                // the target's logit: register e of tile j holds column from + 32 j + 8 (e / 4) + 4 g + e % 4
+                const int at = target[i] - from;
+                if (__any(target[i] >= 0 && at >= 0 && at < NI * 32)) {
+                    float z = 0.f;
+#pragma unroll
+                    for (int j = 0; j < NI; ++j)
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) z = at == 32 * j + 8 * (e / 4) + 4 * g + e % 4 ? acc[i][j][e] : z;
+                    if (target[i] >= 0 && at >= 0 && at < NI * 32 && (at / 4) % 2 == g) hit[b0 + (wb * MI + i) * 32 + l32] = z * a.scale;
+                }
+                if (ragged) {
+#pragma unroll
+                    for (int j = 0; j < NI; ++j)
+#pragma unroll
+                        for (int e = 0; e < 16; ++e)
+                            if (from + 32 * j + 8 * (e / 4) + 4 * g + e % 4 >= a.V) acc[i][j][e] = -INFINITY;
+                }
+                float top = max16(acc[i][0]);
+#pragma unroll
+                for (int j = 1; j < NI; ++j) top = fmaxf(top, max16(acc[i][j]));
+                const float mn = fmaxf(m[i], top * a.cs);
+                l[i] *= fast_exp2(m[i] - mn);
+                m[i] = mn;
+                float sum = 0.f;
+#pragma unroll
+                for (int j = 0; j < NI; ++j)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) sum += fast_exp2(fmaf(acc[i][j][e], a.cs, -mn));
+                l[i] += sum;
+            }
+        });
+#pragma unroll
+    for (int i = 0; i < MI; ++i) {
+        const float mn = both_halves_max(m[i]), sum = both_halves_sum(l[i] * fast_exp2(m[i] - mn));
+        if (g == 0) meet[wa][(wb * MI + i) * 32 + l32] = float2{mn, sum};
+    }
+    __syncthreads();
+    for (int r = threadIdx.x; r < TB; r += Cfg::NT) {
+        if (b0 + r >= a.T) continue;
+        float mn = kLossNone, sum = 0.f;
+#pragma unroll
+        for (int x = 0; x < WA; ++x) mn = fmaxf(mn, meet[x][r].x);
+#pragma unroll
+        for (int x = 0; x < WA; ++x) sum += meet[x][r].y * fast_exp2(meet[x][r].x - mn);
+        parts[(long)slab * a.T + b0 + r] = float2{mn, sum};
+    }
+}
+
+// Rows joined over the runs: lse, loss; and, for a mean or sum, the losses of 256 rows and how many of them have a target.
+__global__ void __launch_bounds__(256)
+avion_loss_join_kernel(LossArgs a, const float2* __restrict__ parts, const float* __restrict__ hit, int slabs, float* __restrict__ loss,
+                       float* __restrict__ lse, double2* __restrict__ sums)
+{
+    const int m = blockIdx.x * 256 + threadIdx.x;
+    double sum = 0., count = 0.;
+    if (m < a.T) {
+        float top = kLossNone, total = 0.f;
+        for (int s = 0; s < slabs; ++s) top = fmaxf(top, parts[(long)s * a.T + m].x);
+        for (int s = 0; s < slabs; ++s) {
+            const float2 p = parts[(long)s * a.T + m];
+            total += p.y * fast_exp2(p.x - top);
+        }
+        const float all = (top + __builtin_amdgcn_logf(total)) * kLn2;
+        lse[m] = all;
+        const bool has = loss_target(a, m) >= 0;
+        const float of = has ? all - hit[m] : 0.f;
+        if (loss) loss[m] = of;
+        sum = of;
+        count = has ? 1. : 0.;
+    }
+    if (!sums) return;
+    __shared__ double2 meet[4];
+#pragma unroll
+    for (int x = 1; x < 64; x *= 2) {
+        sum += __shfl_xor(sum, x);
+        count += __shfl_xor(count, x);
+    }
+    if (threadIdx.x % 64 == 0) meet[threadIdx.x / 64] = double2{sum, count};
+    __syncthreads();
+    if (threadIdx.x == 0)
+        sums[blockIdx.x] = double2{meet[0].x + meet[1].x + meet[2].x + meet[3].x, meet[0].y + meet[1].y + meet[2].y + meet[3].y};
+}
+// total[0]: the mean over the rows with a target (0 where there is none) or the sum, total[1]: how many
+__global__ void __launch_bounds__(256)
+avion_loss_total_kernel(const double2* __restrict__ sums, int n, bool mean, float* __restrict__ total)
+{
+    __shared__ double2 meet[256];
+    double2 t{0., 0.};
+    for (int i = threadIdx.x; i < n; i += 256) {
+        t.x += sums[i].x;
+        t.y += sums[i].y;
+    }
+    meet[threadIdx.x] = t;
+    __syncthreads();
+    for (int half = 128; half > 0; half /= 2) {
+        if ((int)threadIdx.x < half) {
+            meet[threadIdx.x].x += meet[threadIdx.x + half].x;
+            meet[threadIdx.x].y += meet[threadIdx.x + half].y;
+        }
+        __syncthreads();
+    }
+    if (threadIdx.x == 0) {
+        total[0] = (float)(mean ? meet[0].y > 0. ? meet[0].x / meet[0].y : 0. : meet[0].x);
+        total[1] = (float)meet[0].y;
+    }
+}
+
+// ------------------------------------------------------------------------------------------ backward
+// dz is held as (softmax - onehot) r_m S with r_m = dloss_m / max |dloss|, S = 1 for bf16 and 2^14 for fp16 (a softmax over many
+// columns has values below fp16's normal numbers; |dz| stays below 2^14), and the products are scaled back in fp32 by
+// factors[0] = scale max|dloss| / S; factors[1] = 1 / max|dloss|.
+template <typename E>
+constexpr float kLossHeld = std::is_same<E, F16>::value ? 16384.f : 1.f;
+
+__global__ void __launch_bounds__(1024)
+avion_loss_factors_kernel(LossArgs a, const float* __restrict__ dloss, const float* __restrict__ total, bool each, bool mean, float held,
+                          float* __restrict__ factors)
+{
+    if (!each) {  // one gradient for all rows
+        if (threadIdx.x == 0) {
+            float d = dloss[0];
+            if (mean) d = total[1] > 0.f ? d / total[1] : 0.f;
+            factors[0] = d * a.scale / held;
+            factors[1] = 1.f;
+        }
+        return;
+    }
+    __shared__ float meet[16];
+    float top = 0.f;
+    bool nan = false;
+    for (int m = threadIdx.x; m < a.T; m += 1024)
+        if (loss_target(a, m) >= 0) {
+            const float d = fabsf(dloss[m]);
+            nan = nan || !(d <= 3.4028235e38f);
+            top = fmaxf(top, d);
+        }
+    if (nan) top = __builtin_nanf("");
+#pragma unroll
+    for (int x = 1; x < 64; x *= 2) {
+        const float o = __shfl_xor(top, x);
+        top = top != top || o != o ? __builtin_nanf("") : fmaxf(top, o);
+    }
+    if (threadIdx.x % 64 == 0) meet[threadIdx.x / 64] = top;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        for (int i = 1; i < 16; ++i) top = top != top || meet[i] != meet[i] ? __builtin_nanf("") : fmaxf(top, meet[i]);
+        factors[0] = top * a.scale / held;
+        factors[1] = top == 0.f ? 0.f : 1.f / top;
+    }
+}
+
+// dz of the vocabulary's columns v0 .. v0 + n - 1, [T, ld]; columns from n to the next multiple of 8 are zeros
+template <int TA, int TB, int WA, int WB, typename E>
+__global__ void __launch_bounds__(WA* WB * 64, 2)
+avion_loss_dz_kernel(LossArgs a, const float* __restrict__ lse, const float* __restrict__ dloss, const float* __restrict__ factors, bool each,
+                     int v0, int n, raw16* __restrict__ dz, long ld)
+{
+    using Cfg = LossCfg<Along::kK, Along::kK, TA, TB, WA, WB>;
+    constexpr int MI = Cfg::MI, NI = Cfg::NI;
+    extern __shared__ __attribute__((aligned(16))) char smem[];
+    const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), l32 = lane % 32, g = lane / 32;
+    const int wa = wave % WA, wb = wave / WA;
+    const int na = (n + TA - 1) / TA, ntiles = na * ((a.T + TB - 1) / TB), per = (ntiles + 7) / 8, together = gridDim.x / 8;
+    const int first = blockIdx.x % 8 * per + blockIdx.x / 8, end = min(ntiles, (blockIdx.x % 8 + 1) * per);
+    char* stage = smem + 2 * Cfg::STAGE + wave * ((NI == 2 ? 16 : 32) * Cfg::OUT_ROW);
+    const LossOperand opa{a.w + (long)v0 * a.rs_w, a.rs_w, n, 0}, opb{a.x, a.rs_x, a.T, 0};
+    const float inv = factors[1];
+    loss_product<Cfg, E>(
+        smem, opa, opb, a.D, first < end ? (end - first + together - 1) / together : 0, wave, lane,
+        [&](int t, int& a0, int& b0) {
+            const int tile = first + t * together;
+            a0 = tile % na * TA;
+            b0 = tile / na * TB;
+        },
+        [&](int a0, int b0, f32x16(&acc)[MI][NI]) {
+            const int from = a0 + wa * NI * 32;
+#pragma unroll
+            for (int i = 0; i < MI; ++i) {
+                const int m0 = b0 + (wb * MI + i) * 32, row = m0 + l32, target = loss_target(a, row);
+                const float lc = target >= 0 ? lse[row] * kLog2e : INFINITY;
+                const float r = target >= 0 ? (each ? dloss[row] * inv : inv) * kLossHeld<E> : 0.f;
+                const int at = target >= 0 ? target - v0 - from : -1;
+                loss_store<NI, E>(stage, dz + (long)m0 * ld + from, ld, a.T - m0, (int)min(ld - from, (long)NI * 32), lane, [&](int j, int e) {
+                    const int col = 32 * j + 8 * (e / 4) + 4 * g + e % 4;
+                    float p = fast_exp2(fmaf(acc[i][j][e], a.cs, -lc)) - (col == at ? 1.f : 0.f);
+                    p = from + col < n ? p : 0.f;
+                    return target >= 0 ? p * r : 0.f;
+                });
+            }
+        });
+}
+
+// dx (+)= dz w and dw = dz^T x: C [b, a] over K, its first `rows` b, times factors[0] where it is rounded.  sum: fp32 [rows, cols], what earlier pieces left
+// (add) or this one leaves; out: the rounded result, where this is the last.
+template <Along AB, int TA, int TB, int WA, int WB, typename E>
+__global__ void __launch_bounds__(WA* WB * 64, 2)
+avion_loss_grad_kernel(LossOperand opa, LossOperand opb, int rows, int K, const float* __restrict__ factors, float* __restrict__ sum, bool add,
+                       raw16* __restrict__ out)
+{
+    using Cfg = LossCfg<Along::kIndex, AB, TA, TB, WA, WB>;
+    constexpr int MI = Cfg::MI, NI = Cfg::NI;
+    extern __shared__ __attribute__((aligned(16))) char smem[];
+    const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), l32 = lane % 32, g = lane / 32;
+    const int wa = wave % WA, wb = wave / WA, cols = opa.extent;
+    const int na = (cols + TA - 1) / TA, ntiles = na * ((rows + TB - 1) / TB), per = (ntiles + 7) / 8, together = gridDim.x / 8;
+    const int first = blockIdx.x % 8 * per + blockIdx.x / 8, end = min(ntiles, (blockIdx.x % 8 + 1) * per);
+    char* stage = smem + 2 * Cfg::STAGE + wave * ((NI == 2 ? 16 : 32) * Cfg::OUT_ROW);
+    const float mul = factors[0];
+    loss_product<Cfg, E>(
+        smem, opa, opb, K, first < end ? (end - first + together - 1) / together : 0, wave, lane,
+        [&](int t, int& a0, int& b0) {
+            const int tile = first + t * together;
+            a0 = tile % na * TA;
+            b0 = tile / na * TB;
+        },
+        [&](int a0, int b0, f32x16(&acc)[MI][NI]) {
+            const int from = a0 + wa * NI * 32;
+#pragma unroll
+            for (int i = 0; i < MI; ++i) {
+                const int m0 = b0 + (wb * MI + i) * 32, row = m0 + l32;
+                if (sum && row < rows) {
+#pragma unroll
+                    for (int j = 0; j < NI; ++j)
+#pragma unroll
+                        for (int c = 0; c < 4; ++c) {
+                            const int col = from + 32 * j + 8 * c + 4 * g;
+                            if (col >= cols) continue;
+                            f32x4* at = reinterpret_cast<f32x4*>(sum + (long)row * cols + col);
+                            f32x4 v = {acc[i][j][4 * c], acc[i][j][4 * c + 1], acc[i][j][4 * c + 2], acc[i][j][4 * c + 3]};
+                            if (add) v += *at;
+                            if (!out) *at = v;
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) acc[i][j][4 * c + e] = v[e];
+                        }
+                }
+                if (out)
+                    loss_store<NI, E>(stage, out + (long)m0 * cols + from, cols, rows - m0, min(cols - from, NI * 32), lane,
+                                      [&](int j, int e) { return acc[i][j][e] * mul; });
+            }
+        });
+}

@@ -1,0 +1,254 @@
+// C ABI of the loss over a vocabulary.  See include/avion_attn.h for its contract.
+#include "avion_attn.h"
+
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+
+#include "avion_host.h"
+#include "avion_loss.h"
+
+namespace {
+
+constexpr long long kComputeUnits = 256;
+
+struct LossShape {
+    long long T, V;
+    int D;
+};
+int loss_check(const LossShape& s)
+{
+    if (s.T < 0 || s.V < 1 || s.D < 1) return AVION_EINVAL;
+    if (s.D % 8 != 0 || s.D > (1 << 16) || s.T > (1 << 28) || s.V > (1 << 28)) return AVION_EUNSUPPORTED;
+    return AVION_OK;
+}
+long long ceil_div(long long a, long long b) { return (a + b - 1) / b; }
+
+enum class LossTiles { kFew, kSmall, kLarge };  // 32 rows x 128 columns, 128 x 128, 256 x 256
+LossTiles loss_tiles(long long rows, long long cols)
+{
+    if (rows <= 32) return LossTiles::kFew;
+    return ceil_div(rows, 256) * ceil_div(cols, 256) < kComputeUnits ? LossTiles::kSmall : LossTiles::kLarge;
+}
+template <typename F>
+int by_tiles(LossTiles t, F f)
+{
+    if (t == LossTiles::kFew) return f(std::integral_constant<int, 32>{});
+    if (t == LossTiles::kSmall) return f(std::integral_constant<int, 128>{});
+    return f(std::integral_constant<int, 256>{});
+}
+// tile heights and wavefronts of a size: TB, then TA, WA, WB
+template <int TB>
+struct Tile {
+    static constexpr int TA = TB == 256 ? 256 : 128, WA = TB == 32 ? 4 : TB == 128 ? 2 : 4, WB = TB == 32 ? 1 : 2;
+};
+
+// runs of vocabulary tiles in the forward: enough workgroups for the chip, whole rounds of them where there are many
+int loss_slabs(const LossShape& s)
+{
+    const LossTiles t = loss_tiles(s.T, s.V);
+    const long long tb = t == LossTiles::kFew ? 32 : t == LossTiles::kSmall ? 128 : 256, ta = t == LossTiles::kLarge ? 256 : 128;
+    const long long blocks = std::max<long long>(1, ceil_div(s.T, tb)), tiles = ceil_div(s.V, ta), at_once = t == LossTiles::kLarge ? kComputeUnits : 2 * kComputeUnits;
+    return (int)std::max<long long>(1, std::min<long long>(tiles, at_once / blocks));
+}
+struct LossForward {  // offsets of its workspace
+    size_t hit, sums, bytes;
+    LossForward(const LossShape& s)
+    {
+        hit = round256((size_t)loss_slabs(s) * s.T * sizeof(float2));
+        sums = hit + round256((size_t)s.T * 4);
+        bytes = std::max<size_t>(256, sums + round256((size_t)ceil_div(s.T, 256) * sizeof(double2)));
+    }
+};
+
+// A piece of the vocabulary in the backward: dz of it is at most kLossPiece bytes (or 256 columns), in pieces of equal size
+constexpr long long kLossPiece = 1LL << 30;
+long long loss_piece(const LossShape& s)
+{
+    const long long most = std::max<long long>(256, kLossPiece / (2 * std::max<long long>(1, s.T)) / 256 * 256);
+    const long long pieces = ceil_div(s.V, most);
+    return std::min<long long>(most, ceil_div(ceil_div(s.V, pieces), 256) * 256);
+}
+long long loss_ld(const LossShape& s) { return std::min(loss_piece(s), ceil_div(s.V, 64) * 64); }
+struct LossBackward {
+    size_t dz, sum, bytes;
+    LossBackward(const LossShape& s)
+    {
+        dz = 256;
+        sum = dz + round256((size_t)s.T * loss_ld(s) * 2);
+        bytes = sum + (loss_piece(s) >= s.V ? 0 : round256((size_t)s.T * s.D * 4));
+    }
+};
+
+template <typename K, typename... Args>
+int launch(K kernel, int lds, std::atomic<unsigned long long>& allowed, long long grid, int threads, hipStream_t st, const char* what, Args... args)
+{
+    const hipError_t attr = lds > 32 * 1024 ? allow_lds_here(kernel, lds, allowed) : hipSuccess;
+    if (attr != hipSuccess) return hip_fail(attr, "hipFuncSetAttribute(loss)");
+    begin_launch();
+    hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(threads), lds, st, args...);
+    return end_launch(what);
+}
+long long persistent(long long tiles, int tb) { return ceil_div(std::min(tiles, tb == 256 ? kComputeUnits : 2 * kComputeUnits), 8) * 8; }
+
+int loss_inputs(const LossShape& s, const void* x, const void* w, const void* targets, long long rs_x, long long rs_w, float scale,
+                unsigned flags, unsigned allowed)
+{
+    if (flags & ~allowed) return AVION_EINVAL;
+    if (!std::isfinite(scale) || !(scale > 0.f)) return AVION_EINVAL;
+    const int rc = loss_check(s);
+    if (rc != AVION_OK) return rc;
+    if (rs_x < s.D || rs_w < s.D) return AVION_EINVAL;
+    if (rs_x % 8 != 0 || rs_w % 8 != 0 || rs_x > (1 << 20) || rs_w > (1 << 20)) return AVION_EUNSUPPORTED;
+    if (!w || (s.T > 0 && (!x || !targets))) return AVION_EINVAL;
+    if (!aligned16(x) || !aligned16(w) || reinterpret_cast<uintptr_t>(targets) % (flags & AVION_FLAG_TOKENS_I32 ? 4 : 8) != 0)
+        return AVION_EUNSUPPORTED;
+    return AVION_OK;
+}
+LossArgs loss_args(const LossShape& s, const void* x, const void* w, const void* targets, long long rs_x, long long rs_w, long long ignore,
+                   float scale, unsigned flags)
+{
+    LossArgs a{};
+    a.x = static_cast<const raw16*>(x);
+    a.w = static_cast<const raw16*>(w);
+    a.targets = targets;
+    a.rs_x = rs_x;
+    a.rs_w = rs_w;
+    a.T = (int)s.T;
+    a.V = (int)s.V;
+    a.D = s.D;
+    a.wide = flags & AVION_FLAG_TOKENS_I32 ? 0 : 1;
+    a.ignore = ignore;
+    a.cs = scale * kLog2e;
+    a.scale = scale;
+    return a;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t avion_linear_ce_fwd_workspace_bytes(long long T, long long V, int D)
+{
+    const LossShape s{T, V, D};
+    return loss_check(s) == AVION_OK ? LossForward(s).bytes : 0;
+}
+
+int avion_linear_ce_fwd(const void* x, const void* w, const void* targets, float* loss, float* lse, float* total, long long T, long long V,
+                        int D, long long rs_x, long long rs_w, float scale, long long ignore_index, unsigned flags, void* workspace,
+                        size_t workspace_bytes, void* stream)
+{
+    const LossShape s{T, V, D};
+    const int rc = loss_inputs(s, x, w, targets, rs_x, rs_w, scale, flags, AVION_FLAG_F16 | AVION_FLAG_TOKENS_I32 | AVION_FLAG_MEAN);
+    if (rc != AVION_OK) return rc;
+    if ((T > 0 && !lse) || (!loss && !total)) return AVION_EINVAL;
+    for (const void* p : {(const void*)loss, (const void*)lse, (const void*)total})
+        if (reinterpret_cast<uintptr_t>(p) % 4 != 0) return AVION_EUNSUPPORTED;
+    const LossForward at(s);
+    if (!workspace_fits(workspace, workspace_bytes, at.bytes)) return AVION_EWORKSPACE;
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    const LossArgs a = loss_args(s, x, w, targets, rs_x, rs_w, ignore_index, scale, flags);
+    char* ws = static_cast<char*>(workspace);
+    float2* parts = reinterpret_cast<float2*>(ws);
+    float* hit = reinterpret_cast<float*>(ws + at.hit);
+    double2* sums = total ? reinterpret_cast<double2*>(ws + at.sums) : nullptr;
+    static std::atomic<unsigned long long> none{0};
+    if (T > 0) {
+        const int slabs = loss_slabs(s);
+        const int first = by_element(flags, [&](auto fmt) {
+            using E = typename decltype(fmt)::type;
+            return by_tiles(loss_tiles(T, V), [&](auto tb) {
+                constexpr int TB = decltype(tb)::value;
+                using X = Tile<TB>;
+                static std::atomic<unsigned long long> allowed{0};
+                return launch(avion_loss_fwd_kernel<X::TA, TB, X::WA, X::WB, E>, 2 * LossCfg<Along::kK, Along::kK, X::TA, TB, X::WA, X::WB>::STAGE,
+                              allowed, ceil_div(T, TB) * slabs, X::WA * X::WB * 64, st, "launch avion_loss_fwd_kernel", a, parts, hit, slabs);
+            });
+        });
+        if (first != AVION_OK) return first;
+        const int second = launch(avion_loss_join_kernel, 0, none, ceil_div(T, 256), 256, st, "launch avion_loss_join_kernel", a,
+                                  (const float2*)parts, (const float*)hit, slabs, loss, lse, sums);
+        if (second != AVION_OK) return second;
+    }
+    if (!total) return AVION_OK;
+    return launch(avion_loss_total_kernel, 0, none, 1, 256, st, "launch avion_loss_total_kernel", (const double2*)sums, (int)ceil_div(T, 256),
+                  (flags & AVION_FLAG_MEAN) != 0, total);
+}
+
+size_t avion_linear_ce_bwd_workspace_bytes(long long T, long long V, int D)
+{
+    const LossShape s{T, V, D};
+    return loss_check(s) == AVION_OK ? LossBackward(s).bytes : 0;
+}
+
+int avion_linear_ce_bwd(const void* x, const void* w, const void* targets, const float* lse, const float* dloss, const float* total, void* dx,
+                        void* dw, long long T, long long V, int D, long long rs_x, long long rs_w, float scale, long long ignore_index,
+                        unsigned flags, void* workspace, size_t workspace_bytes, void* stream)
+{
+    const LossShape s{T, V, D};
+    const int rc = loss_inputs(s, x, w, targets, rs_x, rs_w, scale, flags,
+                               AVION_FLAG_F16 | AVION_FLAG_TOKENS_I32 | AVION_FLAG_MEAN | AVION_FLAG_ONE_GRADIENT);
+    if (rc != AVION_OK) return rc;
+    const bool each = !(flags & AVION_FLAG_ONE_GRADIENT), mean = (flags & AVION_FLAG_MEAN) != 0;
+    if (!dloss || (!dx && !dw) || (T > 0 && !lse) || (mean && (each || !total))) return AVION_EINVAL;
+    if (!aligned16(dx) || !aligned16(dw)) return AVION_EUNSUPPORTED;
+    for (const void* p : {(const void*)lse, (const void*)dloss, (const void*)total})
+        if (reinterpret_cast<uintptr_t>(p) % 4 != 0) return AVION_EUNSUPPORTED;
+    const LossBackward at(s);
+    if (!workspace_fits(workspace, workspace_bytes, at.bytes)) return AVION_EWORKSPACE;
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    const LossArgs a = loss_args(s, x, w, targets, rs_x, rs_w, ignore_index, scale, flags);
+    char* ws = static_cast<char*>(workspace);
+    float* factors = reinterpret_cast<float*>(ws);
+    raw16* dz = reinterpret_cast<raw16*>(ws + at.dz);
+    float* sum = reinterpret_cast<float*>(ws + at.sum);
+    const long long piece = loss_piece(s), ld = loss_ld(s);
+    return by_element(flags, [&](auto fmt) {
+        using E = typename decltype(fmt)::type;
+        static std::atomic<unsigned long long> none{0};
+        int rc2 = launch(avion_loss_factors_kernel, 0, none, 1, 1024, st, "launch avion_loss_factors_kernel", a, dloss, total, each, mean,
+                         kLossHeld<E>, factors);
+        for (long long v0 = 0; v0 < V && rc2 == AVION_OK; v0 += piece) {
+            const long long n = std::min(piece, V - v0), held = std::min(ld, ceil_div(n, 8) * 8);
+            if (T > 0)
+                rc2 = by_tiles(loss_tiles(T, n), [&](auto tb) {
+                    constexpr int TB = decltype(tb)::value;
+                    using X = Tile<TB>;
+                    using Cfg = LossCfg<Along::kK, Along::kK, X::TA, TB, X::WA, X::WB>;
+                    static std::atomic<unsigned long long> allowed{0};
+                    return launch(avion_loss_dz_kernel<X::TA, TB, X::WA, X::WB, E>, Cfg::LDS_BYTES, allowed,
+                                  persistent(ceil_div(T, TB) * ceil_div(n, X::TA), TB), Cfg::NT, st, "launch avion_loss_dz_kernel", a, lse, dloss,
+                                  (const float*)factors, each, (int)v0, (int)n, dz, (long)ld);
+                });
+            if (rc2 == AVION_OK && dx && T > 0)
+                rc2 = by_tiles(loss_tiles(T, D), [&](auto tb) {
+                    constexpr int TB = decltype(tb)::value;
+                    using X = Tile<TB>;
+                    using Cfg = LossCfg<Along::kIndex, Along::kK, X::TA, TB, X::WA, X::WB>;
+                    static std::atomic<unsigned long long> allowed{0};
+                    const LossOperand opa{a.w + v0 * rs_w, (long)rs_w, D, (int)n}, opb{dz, (long)ld, (int)T, 0};
+                    const bool last = v0 + n >= V;
+                    return launch(avion_loss_grad_kernel<Along::kK, X::TA, TB, X::WA, X::WB, E>, Cfg::LDS_BYTES, allowed,
+                                  persistent(ceil_div(T, TB) * ceil_div(D, X::TA), TB), Cfg::NT, st, "launch avion_loss_grad_kernel (dx)", opa, opb,
+                                  (int)T, (int)held, (const float*)factors, piece >= V ? (float*)nullptr : sum, v0 > 0,
+                                  last ? static_cast<raw16*>(dx) : (raw16*)nullptr);
+                });
+            if (rc2 == AVION_OK && dw)
+                rc2 = by_tiles(std::max(LossTiles::kSmall, loss_tiles(n, D)), [&](auto tb) {
+                    constexpr int TB = decltype(tb)::value < 128 ? 128 : decltype(tb)::value;
+                    using X = Tile<TB>;
+                    using Cfg = LossCfg<Along::kIndex, Along::kIndex, X::TA, TB, X::WA, X::WB>;
+                    static std::atomic<unsigned long long> allowed{0};
+                    const LossOperand opa{a.x, (long)rs_x, D, (int)T}, opb{dz, (long)ld, (int)held, (int)T};
+                    return launch(avion_loss_grad_kernel<Along::kIndex, X::TA, TB, X::WA, X::WB, E>, Cfg::LDS_BYTES, allowed,
+                                  persistent(ceil_div(n, TB) * ceil_div(D, X::TA), TB), Cfg::NT, st, "launch avion_loss_grad_kernel (dw)", opa, opb,
+                                  (int)n, (int)std::max<long long>(1, T), (const float*)factors, (float*)nullptr, false,
+                                  static_cast<raw16*>(dw) + v0 * D);
+                });
+        }
+        return rc2;
+    });
+}
+
+}  // extern "C"

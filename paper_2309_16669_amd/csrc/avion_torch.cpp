@@ -942,6 +942,112 @@ pybind11::object attention_ragged(pybind11::handle q_, pybind11::handle k_, pybi
     END_HANDLE_TH_ERRORS_PYBIND
 }
 
+// ------------------------------------------------------------------------ loss over a vocabulary
+// [n, D] with contiguous rows at multiples of 16 bytes: t itself where it is such, else a copy
+Tensor columns(const Tensor& t)
+{
+    const int64_t n = t.size(0), D = t.size(1), rs = t.stride(0);
+    const bool plain = (D == 1 || t.stride(1) == 1) && (n < 2 || (rs >= D && rs <= (1 << 20) && rs % 8 == 0));
+    return plain && reinterpret_cast<uintptr_t>(t.data_ptr()) % 16 == 0 ? t : dense(t);
+}
+int64_t column_stride(const Tensor& t) { return t.size(0) > 1 ? t.stride(0) : t.size(1); }
+enum { kNone = 0, kMean = 1, kSum = 2 };
+unsigned loss_flags(const Tensor& x, const Tensor& targets, int64_t reduction)
+{
+    return format_flag(x) | (targets.scalar_type() == at::kInt ? AVION_FLAG_TOKENS_I32 : 0u) | (reduction == kMean ? AVION_FLAG_MEAN : 0u);
+}
+struct LossOut {
+    Tensor x, w, targets, lse, total, loss;
+};
+LossOut loss_fwd(const Tensor& x, const Tensor& w, const Tensor& targets, double scale, int64_t ignore, int64_t reduction)
+{
+    LossOut r;
+    r.x = columns(x.reshape({-1, x.size(-1)}));
+    r.w = columns(w);
+    r.targets = targets.contiguous();
+    const int64_t T = r.x.size(0), V = r.w.size(0), D = r.w.size(1);
+    const auto f32 = x.options().dtype(at::kFloat);
+    r.lse = at::empty({T}, f32);
+    if (reduction == kNone) r.loss = at::empty(targets.sizes(), f32);
+    else r.total = at::empty({2}, f32);
+    const size_t need = avion_linear_ce_fwd_workspace_bytes(T, V, (int)D);
+    const Tensor ws = workspace(need, x);
+    check(avion_linear_ce_fwd(r.x.data_ptr(), r.w.data_ptr(), r.targets.data_ptr(), static_cast<float*>(data_of(r.loss)), r.lse.data_ptr<float>(),
+                              static_cast<float*>(data_of(r.total)), T, V, (int)D, column_stride(r.x), column_stride(r.w), (float)scale, ignore,
+                              loss_flags(r.x, r.targets, reduction), ws.data_ptr(), need, stream()));
+    // (the number of targets behind it stays the backward's; the caller gets a number of its own)
+    if (reduction != kNone) r.loss = r.total.select(0, 0);
+    return r;
+}
+struct LinearCrossEntropy : torch::autograd::Function<LinearCrossEntropy> {
+    static Tensor forward(AutogradContext* ctx, const Tensor& x, const Tensor& w, const Tensor& targets, double scale, int64_t ignore,
+                          int64_t reduction)
+    {
+        const c10::DeviceGuard guard(x.device());
+        const LossOut r = loss_fwd(x, w, targets, scale, ignore, reduction);
+        ctx->save_for_backward({r.x, r.w, r.targets, r.lse, reduction == kNone ? r.lse : r.total});
+        ctx->saved_data["shape"] = x.sizes().vec();
+        ctx->saved_data["table"] = w.sizes().vec();
+        ctx->saved_data["format"] = x.scalar_type();
+        ctx->saved_data["targets"] = targets.scalar_type();
+        ctx->saved_data["scale"] = scale;
+        ctx->saved_data["ignore"] = ignore;
+        ctx->saved_data["reduction"] = reduction;
+        return reduction == kNone ? r.loss : r.loss.clone();
+    }
+    static variable_list backward(AutogradContext* ctx, variable_list grad)
+    {
+        const c10::DeviceGuard guard(grad[0].device());
+        const variable_list s = ctx->get_saved_variables();
+        const Tensor g = grad[0].contiguous();
+        const std::vector<int64_t> shape = ctx->saved_data["shape"].toIntVector(), table = ctx->saved_data["table"].toIntVector();
+        const int64_t reduction = ctx->saved_data["reduction"].toInt(), V = table[0], D = table[1];
+        int64_t T = 1;
+        for (size_t i = 0; i + 1 < shape.size(); ++i) T *= shape[i];
+        const at::ScalarType dt = ctx->saved_data["format"].toScalarType();
+        const auto same = [&](const Tensor& t, const char* name, at::IntArrayRef sizes) {
+            TORCH_CHECK_VALUE(t.is_cuda() && t.device() == g.device() && t.scalar_type() == dt && t.sizes() == sizes, name,
+                              " must live on the GPU of the gradient, be ", dt, " and have shape ", sizes);
+            return columns(t);
+        };
+        const Tensor x = same(s[0], "x", {T, D}), w = same(s[1], "weight", table);
+        require(s[2], "targets", at::IntArrayRef(shape).slice(0, shape.size() - 1), ctx->saved_data["targets"].toScalarType(), g);
+        require(s[3], "lse", {T}, at::kFloat, g);
+        if (reduction != kNone) require(s[4], "total", {2}, at::kFloat, g);
+        const Tensor dx = ctx->needs_input_grad(0) ? at::empty(shape, x.options()) : Tensor();
+        const Tensor dw = ctx->needs_input_grad(1) ? at::empty(table, w.options()) : Tensor();
+        const size_t need = avion_linear_ce_bwd_workspace_bytes(T, V, (int)D);
+        const Tensor ws = workspace(need, x);
+        check(avion_linear_ce_bwd(x.data_ptr(), w.data_ptr(), s[2].data_ptr(), s[3].data_ptr<float>(), g.data_ptr<float>(),
+                                  reduction == kNone ? nullptr : s[4].data_ptr<float>(), data_of(dx), data_of(dw), T, V, (int)D,
+                                  column_stride(x), column_stride(w), (float)ctx->saved_data["scale"].toDouble(),
+                                  ctx->saved_data["ignore"].toInt(),
+                                  loss_flags(x, s[2], reduction) | (reduction == kNone ? 0u : AVION_FLAG_ONE_GRADIENT), ws.data_ptr(), need,
+                                  stream()));
+        depends_on(dx, "linear_cross_entropy", {grad[0], s[0], s[1]});
+        depends_on(dw, "linear_cross_entropy", {grad[0], s[0], s[1]});
+        return {dx, dw, Tensor(), Tensor(), Tensor(), Tensor()};
+    }
+};
+pybind11::object linear_cross_entropy(pybind11::handle x_, pybind11::handle w_, pybind11::handle targets_, double scale, int64_t ignore,
+                                      int64_t reduction)
+{
+    HANDLE_TH_ERRORS
+    const Tensor *x, *w, *targets;
+    if (!plain(x_.ptr(), &x) || !plain(w_.ptr(), &w) || !plain(targets_.ptr(), &targets) || !plain_thread()) return pybind11::none();
+    if (!element_format(*x) || x->dim() < 1 || w->dim() != 2 || w->scalar_type() != x->scalar_type() || w->size(1) != x->size(-1) ||
+        w->size(1) > INT32_MAX || w->device() != x->device() || targets->device() != x->device() ||
+        targets->sizes() != x->sizes().slice(0, x->dim() - 1) ||
+        (targets->scalar_type() != at::kLong && targets->scalar_type() != at::kInt))
+        return pybind11::none();
+    return without_lock([&] {
+        if (records({x, w})) return LinearCrossEntropy::apply(*x, *w, *targets, scale, ignore, reduction);
+        const c10::DeviceGuard guard(x->device());
+        return loss_fwd(*x, *w, *targets, scale, ignore, reduction).loss;
+    });
+    END_HANDLE_TH_ERRORS_PYBIND
+}
+
 }  // namespace
 
 PYBIND11_MODULE(_avion_torch, m)
@@ -961,4 +1067,5 @@ PYBIND11_MODULE(_avion_torch, m)
     m.def("linear_fp8", &linear_fp8);
     m.def("rotary", &rotary);
     m.def("attention_ragged", &attention_ragged);
+    m.def("linear_cross_entropy", &linear_cross_entropy);
 }
