@@ -58,7 +58,7 @@ struct LossForward {  // offsets of its workspace
     {
         hit = round256((size_t)loss_slabs(s) * s.T * sizeof(float2));
         sums = hit + round256((size_t)s.T * 4);
-        bytes = std::max<size_t>(256, sums + round256((size_t)ceil_div(s.T, 256) * sizeof(double2)));
+        bytes = std::max<size_t>(256, sums + round256((size_t)ceil_div(s.T, kLossJoin) * sizeof(double2)));
     }
 };
 
@@ -167,12 +167,12 @@ int avion_linear_ce_fwd(const void* x, const void* w, const void* targets, float
             });
         });
         if (first != AVION_OK) return first;
-        const int second = launch(avion_loss_join_kernel, 0, none, ceil_div(T, 256), 256, st, "launch avion_loss_join_kernel", a,
+        const int second = launch(avion_loss_join_kernel, 0, none, ceil_div(T, kLossJoin), 256, st, "launch avion_loss_join_kernel", a,
                                   (const float2*)parts, (const float*)hit, slabs, loss, lse, sums);
         if (second != AVION_OK) return second;
     }
     if (!total) return AVION_OK;
-    return launch(avion_loss_total_kernel, 0, none, 1, 256, st, "launch avion_loss_total_kernel", (const double2*)sums, (int)ceil_div(T, 256),
+    return launch(avion_loss_total_kernel, 0, none, 1, 256, st, "launch avion_loss_total_kernel", (const double2*)sums, (int)ceil_div(T, kLossJoin),
                   (flags & AVION_FLAG_MEAN) != 0, total);
 }
 

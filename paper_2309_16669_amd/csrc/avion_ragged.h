@@ -15,8 +15,8 @@
 // end.  The rows before the first and behind the last offset are two more "sequences", whose outputs become zeros.  Offsets are
 // read as they come: each border is held inside the tensor, so that no content of them leads out of it.
 //
-// Masks.  All keys of a tile beyond the sequence arrive as zero rows; scores that a query must not see become -inf by selection (a
-// NaN among them too) in the units that need it.  Nothing of a sequence is ever multiplied with another's rows, so what one holds
+// Masks.  All keys of a tile beyond the sequence arrive as zero rows; the scores that a query must not see start from -1e30 as in the
+// other kernels, in the units that need it.  Nothing of a sequence is ever multiplied with another's rows, so what one holds
 // (infinities, NaN, an unused slot) cannot reach the next.  Within a sequence a masked key's weight is 0, which NaN and infinity
 // in its value survive, as in avion_attn_fwd.
 #pragma once
@@ -231,14 +231,11 @@ DEVINL void ragged_fwd_walk(char* smem, const RaggedArgs& a, int hk, int begin_q
     Ring::landed_barrier();
 
     const float cs = a.cs;
-    auto unit = [&](auto masked, const char* kt, const char* vt, int hk32, int key_base) {
-        f32x16 s;
+    // (one copy of the unit: with a copy for masked and one for whole units the accumulators took 20 registers' worth of spills)
+    auto unit = [&](const char* kt, const char* vt, int hk32, int key_base) {
+        f32x16 s = key_base + 32 > seen_by_all ? key_mask_block(key_base, g, row.keys) : f32x16_zero();
 #pragma unroll
-        for (int ks = 0; ks < KS; ++ks) s = E::mfma(nat_frag(kt, STRIDE, 32 * hk32 + l32, ks, g), qf[ks], ks == 0 ? f32x16_zero() : s);
-        if constexpr (decltype(masked)::value) {
-#pragma unroll
-            for (int i = 0; i < 16; ++i) s[i] = key_base + 8 * (i / 4) + 4 * g + i % 4 < row.keys ? s[i] : -INFINITY;
-        }
+        for (int ks = 0; ks < KS; ++ks) s = E::mfma(nat_frag(kt, STRIDE, 32 * hk32 + l32, ks, g), qf[ks], s);
         frag8 vf[2][CT];
         if constexpr (D <= 96) {
 #pragma unroll
@@ -283,12 +280,13 @@ DEVINL void ragged_fwd_walk(char* smem, const RaggedArgs& a, int hk, int begin_q
             for (int hk32 = 0; hk32 < 2; ++hk32) {
                 const int key_base = t * 64 + 32 * hk32;
                 if (key_base >= seen_by_any) continue;
-                if (key_base + 32 > seen_by_all) unit(std::true_type{}, kt, kt + Ring::OFF_B, hk32, key_base);
-                else unit(std::false_type{}, kt, kt + Ring::OFF_B, hk32, key_base);
+                unit(kt, kt + Ring::OFF_B, hk32, key_base);
             }
         }
         Ring::landed_barrier();
     }
+    // a row that none of these keys is for has met their masks only
+    if (row.keys <= t0 * 64) sums = RaggedSums<CT>();
 }
 
 // What the sums come to: O's rows and LSE
@@ -516,29 +514,22 @@ avion_ragged_dq_kernel(RaggedArgs a, const raw16* __restrict__ o, const raw16* _
     hold(gf);
     Ring::landed_barrier();
 
-    // P and dP of one unit (masked: 0 where the row does not see the key, whatever lies there)
-    auto weights = [&](auto masked, const char* kt, int hk32, int key_base, f32x16& pe, f32x16& dp) {
+    // scores (far below all others where the row does not see the key) and dP of one unit
+    auto products = [&](const char* kt, int hk32, int key_base, f32x16& sc, f32x16& dp) {
         const char* vt = kt + Ring::OFF_B;
+        sc = key_base + 32 > seen_by_all ? key_mask_block(key_base, g, row.keys) : f32x16_zero();
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) {
             const frag8 ak = nat_frag(kt, STRIDE, 32 * hk32 + l32, ks, g), av = nat_frag(vt, STRIDE, 32 * hk32 + l32, ks, g);
-            pe = E::mfma(ak, qf[ks], ks == 0 ? f32x16_zero() : pe);
+            sc = E::mfma(ak, qf[ks], sc);
             dp = E::mfma(av, gf[ks], ks == 0 ? f32x16_zero() : dp);
-        }
-        if constexpr (decltype(masked)::value) {
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                const bool sees = key_base + 8 * (i / 4) + 4 * g + i % 4 < row.keys;
-                pe[i] = sees ? pe[i] : -INFINITY;
-                dp[i] = sees ? dp[i] : 0.f;
-            }
         }
     };
     if (whole && active) {
         float sum = 0.f;
         for (int key_base = 0; key_base < seen_by_any; key_base += 32) {
             f32x16 pe, dp;
-            weights(std::true_type{}, ring.at(smem, key_base / 64), key_base / 32 % 2, key_base, pe, dp);
+            products(ring.at(smem, key_base / 64), key_base / 32 % 2, key_base, pe, dp);
 #pragma unroll
             for (int i = 0; i < 16; ++i) sum = fmaf(fast_exp2(fmaf(pe[i], cs, -lc)), dp[i], sum);
         }
@@ -549,11 +540,18 @@ avion_ragged_dq_kernel(RaggedArgs a, const raw16* __restrict__ o, const raw16* _
         ws[0] = lc - kRaggedShift<E>;
         ws[npad] = -dl;
     }
+    // the rows up to the next multiple of 64: weight 0
+    if (block0 + Cfg::BM >= rows)
+        for (int x = threadIdx.x; x < (-nq & 63) * a.G; x += Cfg::NT) {
+            float* ws = rowsc + (long)(hk * a.G + x % a.G) * 2 * npad + ragged_scalar_at(p.begin, p.i) + nq + x / a.G;
+            ws[0] = INFINITY;
+            ws[npad] = 0.f;
+        }
     f32x16 acc[CT];
     acc_zero(acc);
-    auto unit = [&](auto masked, const char* kt, int hk32, int key_base) {
+    auto unit = [&](const char* kt, int hk32, int key_base) {
         f32x16 s, dp;
-        weights(masked, kt, hk32, key_base, s, dp);
+        products(kt, hk32, key_base, s, dp);
         frag8 kf[2][CT];
         if constexpr (D <= 96) {
 #pragma unroll
@@ -583,8 +581,7 @@ avion_ragged_dq_kernel(RaggedArgs a, const raw16* __restrict__ o, const raw16* _
             for (int hk32 = 0; hk32 < 2; ++hk32) {
                 const int key_base = t * 64 + 32 * hk32;
                 if (key_base >= seen_by_any) continue;
-                if (key_base + 32 > seen_by_all) unit(std::true_type{}, kt, hk32, key_base);
-                else unit(std::false_type{}, kt, hk32, key_base);
+                unit(kt, hk32, key_base);
             }
         }
         Ring::landed_barrier();
@@ -675,9 +672,9 @@ avion_ragged_dkdv_kernel(RaggedArgs a, const raw16* __restrict__ dO, const float
     const float cs = a.cs;
     const int tr_off = tr_lane_offset(lane, STRIDE);
 
-    auto unit = [&](auto masked, const char* buf, int hq, int query_base) {
+    auto unit = [&](const char* buf, int hq, int query_base) {
         const float* rowv = reinterpret_cast<const float*>(buf + Ring::OFF_SCALARS) + 32 * hq + 4 * g;
-        f32x16 s, dp;
+        f32x16 dp, s = query_base < from_all ? query_mask_block(query_base, g, from) : f32x16_zero();
 #pragma unroll
         for (int a4 = 0; a4 < 4; ++a4) {
             const f32x4 d4 = *reinterpret_cast<const f32x4*>(rowv + 64 + 8 * a4);
@@ -687,7 +684,7 @@ avion_ragged_dkdv_kernel(RaggedArgs a, const raw16* __restrict__ dO, const float
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) {
             const frag8 aq = nat_frag(buf, STRIDE, 32 * hq + l32, ks, g), ag = nat_frag(buf + OFF_G, STRIDE, 32 * hq + l32, ks, g);
-            s = E::mfma(aq, kf[ks], ks == 0 ? f32x16_zero() : s);
+            s = E::mfma(aq, kf[ks], s);
             dp = E::mfma(ag, vf[ks], dp);
         }
         f32x4 l4[4];
@@ -706,14 +703,8 @@ avion_ragged_dkdv_kernel(RaggedArgs a, const raw16* __restrict__ dO, const float
             u32x4 pf, df;
 #pragma unroll
             for (int e = 8 * half; e < 8 * half + 8; ++e) {
-                float pe = fast_exp2(fmaf(s[e], cs, -l4[e / 4][e % 4]));
-                float ds = (std::is_same<E, F16>::value ? pe * (1.f / 256.f) : pe) * dp[e];
-                if constexpr (decltype(masked)::value) {
-                    const int query = query_base + 8 * (e / 4) + 4 * g + e % 4;
-                    const bool sees = query >= from && query < nq;
-                    pe = sees ? pe : 0.f;
-                    ds = sees ? ds : 0.f;
-                }
+                const float pe = fast_exp2(fmaf(s[e], cs, -l4[e / 4][e % 4]));
+                const float ds = (std::is_same<E, F16>::value ? pe * (1.f / 256.f) : pe) * dp[e];
                 s[e] = pe;
                 dp[e] = ds;
                 if (e % 2 == 1) {
@@ -741,8 +732,7 @@ avion_ragged_dkdv_kernel(RaggedArgs a, const raw16* __restrict__ dO, const float
             for (int hq = 0; hq < 2; ++hq) {
                 const int query_base = (tile0 + tile) * 64 + 32 * hq;
                 if (query_base >= nq || query_base + 32 <= from_any) continue;
-                if (query_base < from_all || query_base + 32 > nq) unit(std::true_type{}, buf, hq, query_base);
-                else unit(std::false_type{}, buf, hq, query_base);
+                unit(buf, hq, query_base);
             }
         }
         if (++tile == tiles) tile = 0;
