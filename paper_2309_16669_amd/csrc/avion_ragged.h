@@ -64,17 +64,17 @@ DEVINL RaggedPlace ragged_place(const int* off, int S, int T, int mul, long slot
     return p;
 }
 
-// Two buffers in LDS of an A and a B tile of 64 token rows each (and, with SCALARS, 64 + 64 floats), filled by LDS-direct loads
+// NBUF buffers in LDS of an A and a B tile of ROWS token rows each (and, with SCALARS, ROWS + ROWS floats), filled by LDS-direct loads
 // as TileRing's.  The descriptors begin at the tile's own first row, so that no length of a sequence and no row stride takes a
 // byte offset past 32 bits; rows past the end arrive as zeros.
-template <int D, int NW, bool SCALARS>
+template <int D, int NW, int ROWS_, int NBUF_, bool SCALARS>
 struct RaggedRing {
-    static constexpr int ROWS = 64, STRIDE = tile_stride<D>(), TILE_BYTES = ROWS * STRIDE;
-    static_assert(TILE_BYTES % 1024 == 0, "");
-    static constexpr int NTI = TILE_BYTES / 1024, NBLK = 2 * NTI, NPW = (NBLK + NW - 1) / NW;
-    static constexpr int OFF_B = TILE_BYTES, OFF_SCALARS = 2 * TILE_BYTES;
+    static constexpr int ROWS = ROWS_, NBUF = NBUF_, STRIDE = tile_stride<D>();
+    // 1 KB blocks of a tile (the last one's rows past the tile, where there are any, are not read)
+    static constexpr int NTI = (ROWS * STRIDE + 1023) / 1024, NBLK = 2 * NTI, NPW = (NBLK + NW - 1) / NW;
+    static constexpr int OFF_B = NTI * 1024, OFF_SCALARS = 2 * NTI * 1024;
     static constexpr int BUF_BYTES = NBLK * 1024 + (SCALARS ? 1024 : 0);
-    static constexpr int LDS_BYTES = 2 * BUF_BYTES + (D % 32 != 0 ? 64 : 0);
+    static constexpr int LDS_BYTES = NBUF * BUF_BYTES + (D % 32 != 0 ? 64 : 0);
 
     const raw16 *a, *b;
     const float* scalars;
@@ -96,12 +96,13 @@ struct RaggedRing {
             voff[j] = padded_block_voff<D>(first ? blk : blk - NTI, lane, (unsigned)((first ? rs_a : rs_b) * 2));
         }
         if constexpr (SCALARS)
-            scalar_voff = lane < 16 ? (unsigned)lane * 16 : lane < 32 ? npad_bytes + (lane - 16) * 16 : kOutOfRangeBase;
+            scalar_voff = lane < ROWS / 4 ? (unsigned)lane * 16 : lane < ROWS / 2 ? npad_bytes + (lane - ROWS / 4) * 16 : kOutOfRangeBase;
     }
-    // this wavefront's share of the loads of the tile that begins at row r0, into buffer `to`
-    DEVINL void fetch(int r0, int to) const
+    // this wavefront's share of the loads of tile t, into buffer `to` (t % NBUF)
+    DEVINL void fetch(int t) const { fetch(t, t & (NBUF - 1)); }
+    DEVINL void fetch(int t, int to) const
     {
-        const int left = min(n - r0, ROWS);
+        const int r0 = t * ROWS, left = min(n - r0, ROWS);
         const RawBuffer ab(a + (long)r0 * rs_a, left > 0 ? slice_bytes(rs_a, left, D) : 0);
         const RawBuffer bb(b + (long)r0 * rs_b, left > 0 ? slice_bytes(rs_b, left, D) : 0);
         const unsigned base = smem_addr + to * BUF_BYTES + wave * 1024;
@@ -113,12 +114,24 @@ struct RaggedRing {
         }
         if constexpr (SCALARS)
             // (the arrays go on to the next multiple of 64 rows)
-            if (wave == NW - 1) load_to_lds16(RawBuffer(scalars + r0, npad_bytes + 256), smem_addr + to * BUF_BYTES + OFF_SCALARS, scalar_voff);
+            if (wave == NW - 1) load_to_lds16(RawBuffer(scalars + r0, npad_bytes + ROWS * 4), smem_addr + to * BUF_BYTES + OFF_SCALARS, scalar_voff);
     }
-    DEVINL char* at(char* smem, int to) const { return smem + to * BUF_BYTES; }
+    DEVINL char* at(char* smem, int t) const { return smem + (t & (NBUF - 1)) * BUF_BYTES; }
+    // what was asked for is in LDS, and nobody reads any more what was read (one wavefront has nobody to wait for)
     DEVINL static void landed_barrier()
     {
-        asm volatile("s_waitcnt vmcnt(0)\n\ts_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        if constexpr (NW > 1) asm volatile("s_waitcnt vmcnt(0)\n\ts_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        else asm volatile("s_waitcnt vmcnt(0)\n\ts_waitcnt lgkmcnt(0)" ::: "memory");
+    }
+    // before tile t is computed on, from t0 on: with two buffers the next one is asked for, with one this one
+    DEVINL void before(int t, int t0, int t1) const
+    {
+        if constexpr (NBUF == 2) {
+            if (t + 1 < t1) fetch(t + 1);
+        } else if (t > t0) {
+            fetch(t);
+            landed_barrier();
+        }
     }
 };
 
@@ -188,13 +201,18 @@ DEVINL void ragged_zero(raw16* out, int H, int h0, int heads, long token0, int n
 constexpr float kRaggedLazy = 8.f;
 constexpr float kRaggedNone = -3.0e38f;  // reference of a row that has seen nothing: finite, so that -inf - it is -inf
 
-template <int D, int NW>
+template <int D, int NW, int ROWS, int NBUF>
 struct RaggedFwdCfg {
-    using Ring = RaggedRing<D, NW, false>;
-    static constexpr int NT = NW * 64, BM = 32 * NW, SHIFT = NW == 4 ? 7 : NW == 2 ? 6 : 5;
+    using Ring = RaggedRing<D, NW, ROWS, NBUF, false>;
+    static constexpr int NT = NW * 64, BM = 32 * NW, SHIFT = NW == 4 ? 7 : 5;
     static constexpr int LDS_BYTES = Ring::LDS_BYTES;
-    static constexpr int WAVES_PER_SIMD = D == 64 ? (NW == 4 ? 4 : 1) : D == 80 ? (NW == 4 ? 3 : 1) : NW == 4 ? 2 : 1;
+    static constexpr int WAVES_PER_SIMD = NBUF == 2 && NW == 1 ? 1 : D == 64 ? 4 : D == 80 ? 3 : 2;
 };
+// Short sequences: one wavefront, one buffer of 32 rows, so that 16 workgroups of a compute unit wait for their loads at once
+template <int NW>
+constexpr int kRaggedRows = NW == 1 ? 32 : 64;
+template <int NW>
+constexpr int kRaggedBuffers = NW == 1 ? 1 : 2;
 template <int CT>
 struct RaggedSums {
     f32x16 o[CT];
@@ -210,16 +228,16 @@ struct RaggedSums {
 };
 
 // The tiles t0 .. t1 - 1 of one sequence's keys for the wavefront's rows row0 .. row0 + 31
-template <int D, int NW, typename E>
+template <int D, int NW, int ROWS, int NBUF, typename E>
 DEVINL void ragged_fwd_walk(char* smem, const RaggedArgs& a, int hk, int begin_q, int nq, int begin_k, int nk, int row0, int rows, int t0,
                             int t1, RaggedSums<(D + 31) / 32>& sums, int wave, int lane)
 {
-    using Ring = typename RaggedFwdCfg<D, NW>::Ring;
+    using Ring = typename RaggedFwdCfg<D, NW, ROWS, NBUF>::Ring;
     constexpr int KS = D / 16, CT = (D + 31) / 32, STRIDE = Ring::STRIDE;
     const int l32 = lane % 32, g = lane / 32, tr_off = tr_lane_offset(lane, STRIDE);
     const Ring ring(a.k + (long)begin_k * a.rs_k + hk * D, a.rs_k, a.v + (long)begin_k * a.rs_v + hk * D, a.rs_v, nullptr, 0, nk, smem,
                     wave, lane);
-    if (t0 < t1) ring.fetch(t0 * 64, t0 & 1);
+    if (t0 < t1) ring.fetch(t0);
     const bool active = row0 < rows;
     const RaggedRow row(a, hk, row0 + l32, rows, nq, nk);
     const int seen_by_all = RaggedRow(a, hk, row0, rows, nq, nk).keys, seen_by_any = RaggedRow(a, hk, row0 + 31, rows, nq, nk).keys;
@@ -273,12 +291,12 @@ DEVINL void ragged_fwd_walk(char* smem, const RaggedArgs& a, int hk, int begin_q
             }
     };
     for (int t = t0; t < t1; ++t) {
-        if (t + 1 < t1) ring.fetch((t + 1) * 64, (t + 1) & 1);
+        ring.before(t, t0, t1);
         if (active) {
-            const char* kt = ring.at(smem, t & 1);
+            const char* kt = ring.at(smem, t);
 #pragma unroll
-            for (int hk32 = 0; hk32 < 2; ++hk32) {
-                const int key_base = t * 64 + 32 * hk32;
+            for (int hk32 = 0; hk32 < ROWS / 32; ++hk32) {
+                const int key_base = t * ROWS + 32 * hk32;
                 if (key_base >= seen_by_any) continue;
                 unit(kt, kt + Ring::OFF_B, hk32, key_base);
             }
@@ -286,7 +304,7 @@ DEVINL void ragged_fwd_walk(char* smem, const RaggedArgs& a, int hk, int begin_q
         Ring::landed_barrier();
     }
     // a row that none of these keys is for has met their masks only
-    if (row.keys <= t0 * 64) sums = RaggedSums<CT>();
+    if (row.keys <= t0 * ROWS) sums = RaggedSums<CT>();
 }
 
 // What the sums come to: O's rows and LSE
@@ -313,10 +331,11 @@ DEVINL void ragged_fwd_none(const RaggedArgs& a, raw16* o, float* lse, int hk, i
 DEVINL int ragged_first_token(long row, int G) { return (int)((row + G - 1) / G); }
 
 template <int D, int NW, typename E>
-__global__ void __launch_bounds__(NW * 64, (RaggedFwdCfg<D, NW>::WAVES_PER_SIMD))
+__global__ void __launch_bounds__(NW * 64, (RaggedFwdCfg<D, NW, kRaggedRows<NW>, kRaggedBuffers<NW>>::WAVES_PER_SIMD))
 avion_ragged_fwd_kernel(RaggedArgs a, raw16* __restrict__ o, float* __restrict__ lse)
 {
-    using Cfg = RaggedFwdCfg<D, NW>;
+    constexpr int ROWS = kRaggedRows<NW>, NBUF = kRaggedBuffers<NW>;
+    using Cfg = RaggedFwdCfg<D, NW, ROWS, NBUF>;
     extern __shared__ __attribute__((aligned(16))) char smem[];
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     // the key heads go round the XCDs; the last blocks, which see the most keys, begin first
@@ -334,7 +353,7 @@ avion_ragged_fwd_kernel(RaggedArgs a, raw16* __restrict__ o, float* __restrict__
     const int last_seen = RaggedRow(a, hk, block0 + Cfg::BM - 1, rows, p.n, nk).keys;
     RaggedSums<(D + 31) / 32> sums;
     const int row0 = block0 + wave * 32;
-    ragged_fwd_walk<D, NW, E>(smem, a, hk, p.begin, p.n, begin_k, nk, row0, rows, 0, (last_seen + 63) / 64, sums, wave, lane);
+    ragged_fwd_walk<D, NW, ROWS, NBUF, E>(smem, a, hk, p.begin, p.n, begin_k, nk, row0, rows, 0, (last_seen + ROWS - 1) / ROWS, sums, wave, lane);
     if (row0 >= rows) return;
     ragged_fwd_store<D, E>(smem + wave * RaggedStore<D, E>::BYTES, a, o, lse, hk, p.begin, row0, rows, sums, lane);
 }
@@ -372,10 +391,10 @@ avion_ragged_few_kernel(RaggedArgs a, raw16* __restrict__ o, float* __restrict__
         if (!part && p.block > 0) return;
         const int t0 = part ? (int)p.block * (chunk / 64) : 0, t1 = part ? min(t0 + chunk / 64, tiles) : tiles;
         RaggedSums<CT> sums;
-        ragged_fwd_walk<D, 1, E>(smem, a, hk, begin_q, nq, p.begin, p.n, row0, rows, t0, t1, sums, 0, lane);
+        ragged_fwd_walk<D, 1, 64, 2, E>(smem, a, hk, begin_q, nq, p.begin, p.n, row0, rows, t0, t1, sums, 0, lane);
         if (!part) {
             ragged_fwd_store<D, E>(smem, a, o, lse, hk, begin_q, row0, rows, sums, lane);
-            RaggedFwdCfg<D, 1>::Ring::landed_barrier();
+            RaggedFwdCfg<D, 1, 64, 2>::Ring::landed_barrier();
             continue;
         }
         const int l32 = lane % 32, g = lane / 32;
@@ -395,15 +414,17 @@ avion_ragged_few_kernel(RaggedArgs a, raw16* __restrict__ o, float* __restrict__
             out[32 * D + 32 + l32] = l;
             out[32 * D + 64 + l32] = r;
         }
-        RaggedFwdCfg<D, 1>::Ring::landed_barrier();
+        RaggedFwdCfg<D, 1, 64, 2>::Ring::landed_barrier();
     }
 }
 
-// Joins them: a wavefront a row; chunk after chunk in order.  Also the rows of no sequence.
+// Joins them: a wavefront a row, D / 4 lanes a chunk and as many chunks at a time as that leaves; groups in a fixed order.  Also the
+// rows of no sequence.
 template <int D, typename E>
 __global__ void __launch_bounds__(256)
 avion_ragged_join_kernel(RaggedArgs a, raw16* __restrict__ o, float* __restrict__ lse, const float* __restrict__ parts, int shift)
 {
+    constexpr int LANES = D / 4, GROUPS = 64 / LANES;
     const int hk = blockIdx.x % a.Hk, i = blockIdx.x / a.Hk;  // interval of the borders
     const int begin_q = ragged_border(a.off_q, a.S, a.Tq, i), nq = max(ragged_border(a.off_q, a.S, a.Tq, i + 1) - begin_q, 0);
     if (i == 0 || i == a.S + 1) {
@@ -413,38 +434,49 @@ avion_ragged_join_kernel(RaggedArgs a, raw16* __restrict__ o, float* __restrict_
     const int begin_k = ragged_border(a.off_k, a.S, a.Tk, i), nk = max(ragged_border(a.off_k, a.S, a.Tk, i + 1) - begin_k, 0);
     const int chunks = (nk + (1 << shift) - 1) >> shift, rows = min(nq * a.G, 32);
     if (chunks < 2) return;
-    const long slot = (begin_k >> shift) + i;
-    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
+    const long slot = (begin_k >> shift) + i, step = (long)a.Hk * RaggedPart<D>::FLOATS;
+    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, group = lane / LANES, col = lane % LANES * 4;
     for (int row = wave; row < rows; row += 4) {
         const float* at = parts + (slot * a.Hk + hk) * RaggedPart<D>::FLOATS;
-        const long step = (long)a.Hk * RaggedPart<D>::FLOATS;
         float m = kRaggedNone;
         for (int c = lane; c < chunks; c += 64) m = fmaxf(m, at[c * step + 32 * D + row]);
 #pragma unroll
         for (int x = 1; x < 64; x *= 2) m = fmaxf(m, __shfl_xor(m, x));
-        float acc[(D + 63) / 64] = {}, l = 0.f, r = 0.f;
-        for (int c = 0; c < chunks; ++c) {
-            const float* part = at + c * step;
-            const float w = fast_exp2(part[32 * D + row] - m);
-            l += w * part[32 * D + 32 + row];
-            r += w * part[32 * D + 64 + row];
+        f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+        float l = 0.f, r = 0.f;
+        if (group < GROUPS) {
+#pragma unroll 4
+            for (int c = group; c < chunks; c += GROUPS) {
+                const float* part = at + c * step;
+                const float w = fast_exp2(part[32 * D + row] - m);
+                l += w * part[32 * D + 32 + row];
+                r += w * part[32 * D + 64 + row];
+                acc += w * *reinterpret_cast<const f32x4*>(part + row * D + col);
+            }
+        }
+        // the groups' sums, one after the other
+        f32x4 sum = acc;
+        float ls = l, rs = r;
 #pragma unroll
-            for (int x = 0; x < (D + 63) / 64; ++x)
-                if (lane + 64 * x < D) acc[x] += w * part[row * D + lane + 64 * x];
+        for (int x = 1; x < GROUPS; ++x) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) sum[e] += __shfl(acc[e], lane % LANES + x * LANES);
+            ls += __shfl(l, lane % LANES + x * LANES);
+            rs += __shfl(r, lane % LANES + x * LANES);
         }
         const int q = row / a.G, head = hk * a.G + row - q * a.G;
-        const float inv = r == 0.f ? 0.f : 1.f / r;
-#pragma unroll
-        for (int x = 0; x < (D + 63) / 64; ++x)
-            if (lane + 64 * x < D) o[((long)(begin_q + q) * a.Hq + head) * D + lane + 64 * x] = (raw16)(E::pack(acc[x] * inv, 0.f) & 0xffffu);
-        if (lane == 0) lse[(long)head * a.Tq + begin_q + q] = l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * kLn2;
+        const float inv = rs == 0.f ? 0.f : 1.f / rs;
+        if (group == 0)
+            *reinterpret_cast<u32x2*>(o + ((long)(begin_q + q) * a.Hq + head) * D + col) =
+                u32x2{E::pack(sum[0] * inv, sum[1] * inv), E::pack(sum[2] * inv, sum[3] * inv)};
+        if (lane == 0) lse[(long)head * a.Tq + begin_q + q] = ls == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(ls)) * kLn2;
     }
 }
 
 // ------------------------------------------------------------------------------------------------ dQ
 // As avion_dq_kernel, on the rows above.  delta = rowsum(dO o O) from the O that the forward rounded is off by 2^-9 |dO| |O|, which
-// counts where a row sees few keys; a workgroup whose keys fit two tiles has all of them in LDS and forms delta = sum_j P_j dP_j
-// from them first (up to 128 keys, the rows that need it, and the ones that are not bound by contractions).
+// counts where a row sees few keys; a workgroup with up to 128 keys (all of them in LDS, or in the caches) forms delta = sum_j P_j dP_j
+// from them first: the rows that need it, and the ones that are not bound by contractions.
 // Leaves lse * log2 e (+inf where a row sees nothing, so that its weights are 0; fp16: less kRaggedShift) and -delta for the second
 // kernel: [Hq][2][npad], sequence s at (floor(begin / 64) + s) * 64.
 //
@@ -455,9 +487,9 @@ constexpr float kRaggedShift = std::is_same<E, F16>::value ? 8.f : 0.f;
 
 template <int D, int NW>
 struct RaggedDqCfg {
-    using Ring = RaggedRing<D, NW, false>;
-    static constexpr int NT = NW * 64, BM = 32 * NW, SHIFT = NW == 4 ? 7 : NW == 2 ? 6 : 5, LDS_BYTES = Ring::LDS_BYTES;
-    static constexpr int WAVES_PER_SIMD = NW < 4 ? 1 : D == 64 ? 3 : 2;
+    using Ring = RaggedRing<D, NW, kRaggedRows<NW>, kRaggedBuffers<NW>, false>;
+    static constexpr int NT = NW * 64, BM = 32 * NW, SHIFT = NW == 4 ? 7 : 5, LDS_BYTES = Ring::LDS_BYTES;
+    static constexpr int WAVES_PER_SIMD = D == 64 ? 3 : 2;
 };
 DEVINL long ragged_scalar_at(int begin, int i) { return ((long)(begin >> 6) + i) * 64; }
 
@@ -482,12 +514,13 @@ avion_ragged_dq_kernel(RaggedArgs a, const raw16* __restrict__ o, const raw16* _
         return;
     }
     const int begin_k = ragged_border(a.off_k, a.S, a.Tk, p.i), nk = max(ragged_border(a.off_k, a.S, a.Tk, p.i + 1) - begin_k, 0);
-    const int ntiles = (RaggedRow(a, hk, block0 + Cfg::BM - 1, rows, nq, nk).keys + 63) / 64;
-    const bool whole = ntiles <= 2;
+    constexpr int ROWS = Ring::ROWS;
+    const int ntiles = (RaggedRow(a, hk, block0 + Cfg::BM - 1, rows, nq, nk).keys + ROWS - 1) / ROWS;
+    const bool whole = ntiles * ROWS <= 128;
     const Ring ring(a.k + (long)begin_k * a.rs_k + hk * D, a.rs_k, a.v + (long)begin_k * a.rs_v + hk * D, a.rs_v, nullptr, 0, nk, smem,
                     wave, lane);
-    if (ntiles > 0) ring.fetch(0, 0);
-    if (ntiles == 2) ring.fetch(64, 1);
+    if (ntiles > 0) ring.fetch(0);
+    if (Ring::NBUF == 2 && ntiles == 2) ring.fetch(1);
     const int row0 = block0 + wave * 32, tr_off = tr_lane_offset(lane, STRIDE);
     const bool active = row0 < rows;
     const RaggedRow row(a, hk, row0 + l32, rows, nq, nk);
@@ -529,11 +562,17 @@ avion_ragged_dq_kernel(RaggedArgs a, const raw16* __restrict__ o, const raw16* _
         float sum = 0.f;
         for (int key_base = 0; key_base < seen_by_any; key_base += 32) {
             f32x16 pe, dp;
-            products(ring.at(smem, key_base / 64), key_base / 32 % 2, key_base, pe, dp);
+            if (Ring::NBUF == 1) ring.before(key_base / ROWS, 0, 0);
+            products(ring.at(smem, key_base / ROWS), key_base % ROWS / 32, key_base, pe, dp);
+            if (Ring::NBUF == 1) Ring::landed_barrier();
 #pragma unroll
             for (int i = 0; i < 16; ++i) sum = fmaf(fast_exp2(fmaf(pe[i], cs, -lc)), dp[i], sum);
         }
         dl = both_halves_sum(sum);
+        if (Ring::NBUF == 1 && seen_by_any > ROWS) {
+            ring.fetch(0);
+            Ring::landed_barrier();
+        }
     }
     if (active && g == 0 && row0 + l32 < rows) {
         float* ws = rowsc + (long)row.head * 2 * npad + ragged_scalar_at(p.begin, p.i) + row.token;
@@ -574,12 +613,12 @@ avion_ragged_dq_kernel(RaggedArgs a, const raw16* __restrict__ o, const raw16* _
             }
     };
     for (int t = 0; t < ntiles; ++t) {
-        if (!whole && t + 1 < ntiles) ring.fetch((t + 1) * 64, (t + 1) & 1);
+        if (Ring::NBUF == 1 || !whole) ring.before(t, 0, ntiles);
         if (active) {
-            const char* kt = ring.at(smem, t & 1);
+            const char* kt = ring.at(smem, t);
 #pragma unroll
-            for (int hk32 = 0; hk32 < 2; ++hk32) {
-                const int key_base = t * 64 + 32 * hk32;
+            for (int hk32 = 0; hk32 < ROWS / 32; ++hk32) {
+                const int key_base = t * ROWS + 32 * hk32;
                 if (key_base >= seen_by_any) continue;
                 unit(kt, hk32, key_base);
             }
@@ -595,9 +634,9 @@ avion_ragged_dq_kernel(RaggedArgs a, const raw16* __restrict__ o, const raw16* _
 // other.  With `parts` > 1 the query heads are dealt to that many workgroups, whose sums meet in fp32 (avion_ragged_sum_kernel).
 template <int D, int NW>
 struct RaggedDkvCfg {
-    using Ring = RaggedRing<D, NW, true>;
-    static constexpr int NT = NW * 64, BN = 32 * NW, SHIFT = NW == 4 ? 7 : NW == 2 ? 6 : 5, LDS_BYTES = Ring::LDS_BYTES;
-    static constexpr int WAVES_PER_SIMD = NW < 4 ? 1 : D == 64 ? 3 : D == 80 ? 2 : 1;
+    using Ring = RaggedRing<D, NW, kRaggedRows<NW>, kRaggedBuffers<NW>, true>;
+    static constexpr int NT = NW * 64, BN = 32 * NW, SHIFT = NW == 4 ? 7 : 5, LDS_BYTES = Ring::LDS_BYTES;
+    static constexpr int WAVES_PER_SIMD = D == 64 ? 3 : D == 80 ? 2 : 1;
 };
 // 32 rows of fp32 sums, lane = row
 template <int D>
@@ -621,7 +660,7 @@ avion_ragged_dkdv_kernel(RaggedArgs a, const raw16* __restrict__ dO, const float
 {
     using Cfg = RaggedDkvCfg<D, NW>;
     using Ring = typename Cfg::Ring;
-    constexpr int KS = D / 16, CT = (D + 31) / 32, STRIDE = Ring::STRIDE, OFF_G = Ring::OFF_B;
+    constexpr int KS = D / 16, CT = (D + 31) / 32, STRIDE = Ring::STRIDE, OFF_G = Ring::OFF_B, ROWS = Ring::ROWS;
     extern __shared__ __attribute__((aligned(16))) char smem[];
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), l32 = lane % 32, g = lane / 32;
     const int hk = blockIdx.x % a.Hk, part = blockIdx.x / a.Hk % parts, slot = blockIdx.x / (a.Hk * parts);
@@ -635,18 +674,18 @@ avion_ragged_dkdv_kernel(RaggedArgs a, const raw16* __restrict__ dO, const float
     // first query that sees a key: this lane's, the wavefront's first and last, the workgroup's first
     auto first_query = [&](int key) { return a.causal ? max(min(key, nk - 1) - nk + nq, 0) : 0; };
     const int key = min(k0 + l32, nk - 1), from = first_query(k0 + l32), from_all = first_query(k0 + 31), from_any = first_query(k0);
-    const int tile0 = first_query(block0) / 64, tiles = nq == 0 ? 0 : (nq + 63) / 64 - tile0;
+    const int tile0 = first_query(block0) / ROWS, tiles = nq == 0 ? 0 : (nq + ROWS - 1) / ROWS - tile0;
     const int heads = a.G / parts, h0 = hk * a.G + part * heads;
 
     const long q_at = (long)begin_q * a.rs_q, o_at = (long)begin_q * a.Hq * D;
     Ring ring(a.q + q_at, a.rs_q, dO + o_at, (long)a.Hq * D, rowsc + ragged_scalar_at(begin_q, p.i), npad, nq, smem, wave, lane);
     int f_head = 0, f_tile = 0;  // next to fetch
-    auto fetch = [&](int to) {
+    auto fetch = [&](int n) {
         Ring r = ring;
         r.a += (h0 + f_head) * D;
         r.b += (h0 + f_head) * D;
         r.scalars += (long)(h0 + f_head) * 2 * npad;
-        r.fetch((tile0 + f_tile) * 64, to);
+        r.fetch(tile0 + f_tile, n & (Ring::NBUF - 1));
         if (++f_tile == tiles) {
             f_tile = 0;
             ++f_head;
@@ -677,7 +716,7 @@ avion_ragged_dkdv_kernel(RaggedArgs a, const raw16* __restrict__ dO, const float
         f32x16 dp, s = query_base < from_all ? query_mask_block(query_base, g, from) : f32x16_zero();
 #pragma unroll
         for (int a4 = 0; a4 < 4; ++a4) {
-            const f32x4 d4 = *reinterpret_cast<const f32x4*>(rowv + 64 + 8 * a4);
+            const f32x4 d4 = *reinterpret_cast<const f32x4*>(rowv + ROWS + 8 * a4);
 #pragma unroll
             for (int e = 0; e < 4; ++e) dp[4 * a4 + e] = d4[e];
         }
@@ -725,12 +764,17 @@ avion_ragged_dkdv_kernel(RaggedArgs a, const raw16* __restrict__ dO, const float
     };
     int tile = 0;
     for (int n = 0; n < total; ++n) {
-        if (n + 1 < total) fetch((n + 1) & 1);
+        if constexpr (Ring::NBUF == 2) {
+            if (n + 1 < total) fetch(n + 1);
+        } else if (n > 0) {
+            fetch(n);
+            Ring::landed_barrier();
+        }
         if (active) {
-            const char* buf = ring.at(smem, n & 1);
+            const char* buf = ring.at(smem, n);
 #pragma unroll
-            for (int hq = 0; hq < 2; ++hq) {
-                const int query_base = (tile0 + tile) * 64 + 32 * hq;
+            for (int hq = 0; hq < ROWS / 32; ++hq) {
+                const int query_base = (tile0 + tile) * ROWS + 32 * hq;
                 if (query_base >= nq || query_base + 32 <= from_any) continue;
                 unit(buf, hq, query_base);
             }

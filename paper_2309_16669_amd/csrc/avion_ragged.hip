@@ -165,7 +165,7 @@ int avion_ragged_fwd(const void* q, const void* k, const void* v, const int* off
         if (const int shift = few_shift(s)) {
             static std::atomic<unsigned long long> allowed{0}, none{0};
             float* parts = static_cast<float*>(workspace);
-            const int first = launch(avion_ragged_few_kernel<D, E>, RaggedFwdCfg<D, 1>::LDS_BYTES, allowed, few_slots(s, shift) * Hk, 64, st,
+            const int first = launch(avion_ragged_few_kernel<D, E>, RaggedFwdCfg<D, 1, 64, 2>::LDS_BYTES, allowed, few_slots(s, shift) * Hk, 64, st,
                                      "launch avion_ragged_few_kernel", a, out, lse, parts, shift);
             if (first != AVION_OK) return first;
             return launch(avion_ragged_join_kernel<D, E>, 0, none, (S + 2) * Hk, 256, st, "launch avion_ragged_join_kernel", a, out, lse,
@@ -173,7 +173,7 @@ int avion_ragged_fwd(const void* q, const void* k, const void* v, const int* off
         }
         return by_waves(ragged_waves(Tq * a.G, S), [&](auto nw) {
             constexpr int NW = decltype(nw)::value;
-            using Cfg = RaggedFwdCfg<D, NW>;
+            using Cfg = RaggedFwdCfg<D, NW, kRaggedRows<NW>, kRaggedBuffers<NW>>;
             static std::atomic<unsigned long long> allowed{0};
             a.slots = (int)(Tq * a.G / Cfg::BM + S + 2);
             return launch(avion_ragged_fwd_kernel<D, NW, E>, Cfg::LDS_BYTES, allowed, (long long)a.slots * Hk, Cfg::NT, st,
