@@ -135,6 +135,36 @@ struct RaggedRing {
     }
 };
 
+// Short sequences: one wavefront, one buffer of 32 rows, so that 16 of a compute unit wait for their loads
+// at once; four of them, which know nothing of each other, to a workgroup (kRaggedJobs)
+template <int NW>
+constexpr int kRaggedJobs = NW == 1 ? 4 : 1;
+template <int NW>
+constexpr int kRaggedRows = NW == 1 ? 32 : 64;
+template <int NW>
+constexpr int kRaggedBuffers = NW == 1 ? 1 : 2;
+// The work of a workgroup, or, where a wavefront works alone, of each of its wavefronts
+template <int NW>
+struct RaggedJob {
+    int id, wave, tid;
+    char* smem;
+    DEVINL RaggedJob(char* shared, int lds_bytes)
+    {
+        const int w = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+        if constexpr (NW == 1) {
+            id = blockIdx.x * kRaggedJobs<1> + w;
+            wave = 0;
+            tid = threadIdx.x % 64;
+            smem = shared + w * lds_bytes;
+        } else {
+            id = blockIdx.x;
+            wave = w;
+            tid = threadIdx.x;
+            smem = shared;
+        }
+    }
+};
+
 // Where a lane's row lies: token and head, and how many keys it sees.  Rows past the end stand for the last one.
 struct RaggedRow {
     int token, head, keys;
@@ -181,13 +211,13 @@ struct RaggedStore {
     }
 };
 
-// Rows of no sequence: zeros in [T, H, D] for `count` heads from h0 on, tokens begin + t0 .. (n of them), by the workgroup
+// Rows of no sequence: zeros in [T, H, D] for `count` heads from h0 on, tokens begin + t0 .. (n of them), by `threads` threads
 template <int D>
-DEVINL void ragged_zero(raw16* out, int H, int h0, int heads, long token0, int n)
+DEVINL void ragged_zero(raw16* out, int H, int h0, int heads, long token0, int n, int tid, int threads)
 {
     constexpr int CH = D / 8;
     const u32x4 zero = {0u, 0u, 0u, 0u};
-    for (long x = threadIdx.x; x < (long)n * heads * CH; x += blockDim.x) {
+    for (long x = tid; x < (long)n * heads * CH; x += threads) {
         const long t = x / (heads * CH);
         const int in = (int)(x - t * (heads * CH));
         *reinterpret_cast<u32x4*>(out + ((token0 + t) * H + h0 + in / CH) * D + in % CH * 8) = zero;
@@ -208,11 +238,6 @@ struct RaggedFwdCfg {
     static constexpr int LDS_BYTES = Ring::LDS_BYTES;
     static constexpr int WAVES_PER_SIMD = NBUF == 2 && NW == 1 ? 1 : D == 64 ? 4 : D == 80 ? 3 : 2;
 };
-// Short sequences: one wavefront, one buffer of 32 rows, so that 16 workgroups of a compute unit wait for their loads at once
-template <int NW>
-constexpr int kRaggedRows = NW == 1 ? 32 : 64;
-template <int NW>
-constexpr int kRaggedBuffers = NW == 1 ? 1 : 2;
 template <int CT>
 struct RaggedSums {
     f32x16 o[CT];
@@ -322,31 +347,35 @@ DEVINL void ragged_fwd_store(char* region, const RaggedArgs& a, raw16* o, float*
 }
 // Rows of no sequence
 template <int D>
-DEVINL void ragged_fwd_none(const RaggedArgs& a, raw16* o, float* lse, int hk, int token0, int n)
+DEVINL void ragged_fwd_none(const RaggedArgs& a, raw16* o, float* lse, int hk, int token0, int n, int tid, int threads)
 {
-    ragged_zero<D>(o, a.Hq, hk * a.G, a.G, token0, n);
-    for (int x = threadIdx.x; x < n * a.G; x += blockDim.x) lse[(long)(hk * a.G + x / n) * a.Tq + token0 + x % n] = -INFINITY;
+    ragged_zero<D>(o, a.Hq, hk * a.G, a.G, token0, n, tid, threads);
+    for (long x = tid; x < (long)n * a.G; x += threads) lse[(long)(hk * a.G + x / n) * a.Tq + token0 + x % n] = -INFINITY;
 }
 // the tokens whose (token, head) rows a block of BM rows begins: each token belongs to one block
 DEVINL int ragged_first_token(long row, int G) { return (int)((row + G - 1) / G); }
 
 template <int D, int NW, typename E>
-__global__ void __launch_bounds__(NW * 64, (RaggedFwdCfg<D, NW, kRaggedRows<NW>, kRaggedBuffers<NW>>::WAVES_PER_SIMD))
+__global__ void __launch_bounds__(NW * kRaggedJobs<NW> * 64, (RaggedFwdCfg<D, NW, kRaggedRows<NW>, kRaggedBuffers<NW>>::WAVES_PER_SIMD))
 avion_ragged_fwd_kernel(RaggedArgs a, raw16* __restrict__ o, float* __restrict__ lse)
 {
     constexpr int ROWS = kRaggedRows<NW>, NBUF = kRaggedBuffers<NW>;
     using Cfg = RaggedFwdCfg<D, NW, ROWS, NBUF>;
-    extern __shared__ __attribute__((aligned(16))) char smem[];
-    const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+    extern __shared__ __attribute__((aligned(16))) char shared[];
+    const int lane = threadIdx.x % 64;
+    const RaggedJob<NW> job(shared, Cfg::LDS_BYTES);
+    const int wave = job.wave;
+    char* smem = job.smem;
     // the key heads go round the XCDs; the last blocks, which see the most keys, begin first
-    const int hk = blockIdx.x % a.Hk, slot = a.slots - 1 - blockIdx.x / a.Hk;
+    const int hk = job.id % a.Hk, slot = a.slots - 1 - job.id / a.Hk;
+    if (slot < 0) return;
     const RaggedPlace p = ragged_place<Cfg::SHIFT>(a.off_q, a.S, a.Tq, a.G, slot, lane);
     const int rows = p.n * a.G;
     if (p.block < 0 || p.block * Cfg::BM >= rows) return;
     const int block0 = (int)p.block * Cfg::BM;
     if (p.i == 0 || p.i == a.S + 1) {
         const int from = ragged_first_token(block0, a.G), to = min(ragged_first_token(block0 + Cfg::BM, a.G), p.n);
-        ragged_fwd_none<D>(a, o, lse, hk, p.begin + from, to - from);
+        ragged_fwd_none<D>(a, o, lse, hk, p.begin + from, to - from, job.tid, Cfg::NT);
         return;
     }
     const int begin_k = ragged_border(a.off_k, a.S, a.Tk, p.i), nk = max(ragged_border(a.off_k, a.S, a.Tk, p.i + 1) - begin_k, 0);
@@ -428,7 +457,7 @@ avion_ragged_join_kernel(RaggedArgs a, raw16* __restrict__ o, float* __restrict_
     const int hk = blockIdx.x % a.Hk, i = blockIdx.x / a.Hk;  // interval of the borders
     const int begin_q = ragged_border(a.off_q, a.S, a.Tq, i), nq = max(ragged_border(a.off_q, a.S, a.Tq, i + 1) - begin_q, 0);
     if (i == 0 || i == a.S + 1) {
-        ragged_fwd_none<D>(a, o, lse, hk, begin_q, nq);
+        ragged_fwd_none<D>(a, o, lse, hk, begin_q, nq, threadIdx.x, 256);
         return;
     }
     const int begin_k = ragged_border(a.off_k, a.S, a.Tk, i), nk = max(ragged_border(a.off_k, a.S, a.Tk, i + 1) - begin_k, 0);
@@ -494,23 +523,27 @@ struct RaggedDqCfg {
 DEVINL long ragged_scalar_at(int begin, int i) { return ((long)(begin >> 6) + i) * 64; }
 
 template <int D, int NW, typename E>
-__global__ void __launch_bounds__(NW * 64, (RaggedDqCfg<D, NW>::WAVES_PER_SIMD))
+__global__ void __launch_bounds__(NW * kRaggedJobs<NW> * 64, (RaggedDqCfg<D, NW>::WAVES_PER_SIMD))
 avion_ragged_dq_kernel(RaggedArgs a, const raw16* __restrict__ o, const raw16* __restrict__ dO, const float* __restrict__ lse,
                        raw16* __restrict__ dq, float* __restrict__ rowsc, int npad)
 {
     using Cfg = RaggedDqCfg<D, NW>;
     using Ring = typename Cfg::Ring;
     constexpr int KS = D / 16, CT = (D + 31) / 32, STRIDE = Ring::STRIDE;
-    extern __shared__ __attribute__((aligned(16))) char smem[];
-    const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), l32 = lane % 32, g = lane / 32;
-    const int hk = blockIdx.x % a.Hk, slot = a.slots - 1 - blockIdx.x / a.Hk;
+    extern __shared__ __attribute__((aligned(16))) char shared[];
+    const int lane = threadIdx.x % 64, l32 = lane % 32, g = lane / 32;
+    const RaggedJob<NW> job(shared, Cfg::LDS_BYTES);
+    const int wave = job.wave;
+    char* smem = job.smem;
+    const int hk = job.id % a.Hk, slot = a.slots - 1 - job.id / a.Hk;
+    if (slot < 0) return;
     const RaggedPlace p = ragged_place<Cfg::SHIFT>(a.off_q, a.S, a.Tq, a.G, slot, lane);
     const int rows = p.n * a.G, nq = p.n;
     if (p.block < 0 || p.block * Cfg::BM >= rows) return;
     const int block0 = (int)p.block * Cfg::BM;
     if (p.i == 0 || p.i == a.S + 1) {
         const int from = ragged_first_token(block0, a.G), to = min(ragged_first_token(block0 + Cfg::BM, a.G), p.n);
-        ragged_zero<D>(dq, a.Hq, hk * a.G, a.G, p.begin + from, to - from);
+        ragged_zero<D>(dq, a.Hq, hk * a.G, a.G, p.begin + from, to - from, job.tid, Cfg::NT);
         return;
     }
     const int begin_k = ragged_border(a.off_k, a.S, a.Tk, p.i), nk = max(ragged_border(a.off_k, a.S, a.Tk, p.i + 1) - begin_k, 0);
@@ -581,7 +614,7 @@ avion_ragged_dq_kernel(RaggedArgs a, const raw16* __restrict__ o, const raw16* _
     }
     // the rows up to the next multiple of 64: weight 0
     if (block0 + Cfg::BM >= rows)
-        for (int x = threadIdx.x; x < (-nq & 63) * a.G; x += Cfg::NT) {
+        for (int x = job.tid; x < (-nq & 63) * a.G; x += Cfg::NT) {
             float* ws = rowsc + (long)(hk * a.G + x % a.G) * 2 * npad + ragged_scalar_at(p.begin, p.i) + nq + x / a.G;
             ws[0] = INFINITY;
             ws[npad] = 0.f;
@@ -654,16 +687,20 @@ DEVINL void ragged_store_part(const f32x16 (&acc)[(D + 31) / 32], float* out, lo
 }
 
 template <int D, int NW, typename E>
-__global__ void __launch_bounds__(NW * 64, (RaggedDkvCfg<D, NW>::WAVES_PER_SIMD))
+__global__ void __launch_bounds__(NW * kRaggedJobs<NW> * 64, (RaggedDkvCfg<D, NW>::WAVES_PER_SIMD))
 avion_ragged_dkdv_kernel(RaggedArgs a, const raw16* __restrict__ dO, const float* __restrict__ rowsc, int npad, raw16* __restrict__ dk,
                          raw16* __restrict__ dv, float* __restrict__ sums, int parts)
 {
     using Cfg = RaggedDkvCfg<D, NW>;
     using Ring = typename Cfg::Ring;
     constexpr int KS = D / 16, CT = (D + 31) / 32, STRIDE = Ring::STRIDE, OFF_G = Ring::OFF_B, ROWS = Ring::ROWS;
-    extern __shared__ __attribute__((aligned(16))) char smem[];
-    const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), l32 = lane % 32, g = lane / 32;
-    const int hk = blockIdx.x % a.Hk, part = blockIdx.x / a.Hk % parts, slot = blockIdx.x / (a.Hk * parts);
+    extern __shared__ __attribute__((aligned(16))) char shared[];
+    const int lane = threadIdx.x % 64, l32 = lane % 32, g = lane / 32;
+    const RaggedJob<NW> job(shared, Cfg::LDS_BYTES);
+    const int wave = job.wave;
+    char* smem = job.smem;
+    const int hk = job.id % a.Hk, part = job.id / a.Hk % parts, slot = job.id / (a.Hk * parts);
+    if (slot >= a.slots) return;
     const RaggedPlace p = ragged_place<Cfg::SHIFT>(a.off_k, a.S, a.Tk, 1, slot, lane);
     const int nk = p.n;
     if (p.block < 0 || p.block * Cfg::BN >= nk) return;

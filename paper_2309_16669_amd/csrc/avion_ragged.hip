@@ -118,6 +118,12 @@ int launch(K kernel, int lds, std::atomic<unsigned long long>& allowed, long lon
     return end_launch(what);
 }
 
+template <int NW>
+long long jobs(long long n)
+{
+    return (n + kRaggedJobs<NW> - 1) / kRaggedJobs<NW>;
+}
+
 int ragged_inputs(const RaggedShape& s, const void* q, const void* k, const void* v, const int* off_q, const int* off_k, long long rs_q,
                   long long rs_k, long long rs_v, float scale, unsigned flags)
 {
@@ -176,7 +182,8 @@ int avion_ragged_fwd(const void* q, const void* k, const void* v, const int* off
             using Cfg = RaggedFwdCfg<D, NW, kRaggedRows<NW>, kRaggedBuffers<NW>>;
             static std::atomic<unsigned long long> allowed{0};
             a.slots = (int)(Tq * a.G / Cfg::BM + S + 2);
-            return launch(avion_ragged_fwd_kernel<D, NW, E>, Cfg::LDS_BYTES, allowed, (long long)a.slots * Hk, Cfg::NT, st,
+            return launch(avion_ragged_fwd_kernel<D, NW, E>, Cfg::LDS_BYTES * kRaggedJobs<NW>, allowed, jobs<NW>((long long)a.slots * Hk),
+                          Cfg::NT * kRaggedJobs<NW>, st,
                           "launch avion_ragged_fwd_kernel", a, out, lse);
         });
     });
@@ -215,7 +222,8 @@ int avion_ragged_bwd(const void* q, const void* k, const void* v, const int* off
                 using Cfg = RaggedDqCfg<D, NW>;
                 static std::atomic<unsigned long long> allowed{0};
                 a.slots = (int)(Tq * a.G / Cfg::BM + S + 2);
-                return launch(avion_ragged_dq_kernel<D, NW, E>, Cfg::LDS_BYTES, allowed, (long long)a.slots * Hk, Cfg::NT, st,
+                return launch(avion_ragged_dq_kernel<D, NW, E>, Cfg::LDS_BYTES * kRaggedJobs<NW>, allowed, jobs<NW>((long long)a.slots * Hk),
+                          Cfg::NT * kRaggedJobs<NW>, st,
                               "launch avion_ragged_dq_kernel", a, static_cast<const raw16*>(o), static_cast<const raw16*>(dO), lse,
                               static_cast<raw16*>(dq), rowsc, npad);
             });
@@ -227,7 +235,8 @@ int avion_ragged_bwd(const void* q, const void* k, const void* v, const int* off
             using Cfg = RaggedDkvCfg<D, NW>;
             static std::atomic<unsigned long long> allowed{0};
             a.slots = (int)(Tk / Cfg::BN + S + 2);
-            return launch(avion_ragged_dkdv_kernel<D, NW, E>, Cfg::LDS_BYTES, allowed, (long long)a.slots * Hk * parts, Cfg::NT, st,
+            return launch(avion_ragged_dkdv_kernel<D, NW, E>, Cfg::LDS_BYTES * kRaggedJobs<NW>, allowed, jobs<NW>((long long)a.slots * Hk * parts),
+                          Cfg::NT * kRaggedJobs<NW>, st,
                           "launch avion_ragged_dkdv_kernel", a, static_cast<const raw16*>(dO), (const float*)rowsc, npad,
                           static_cast<raw16*>(dk), static_cast<raw16*>(dv), sums, parts);
         });
