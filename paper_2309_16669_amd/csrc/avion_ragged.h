@@ -11,7 +11,7 @@
 //
 // Slots.  How many blocks of BM rows a sequence has is known on the device only.  A launch has floor(T / BM) + S + 2 slots a head,
 // of which sequence s owns those from floor(begin_s / BM) + s on: at least as many as it has blocks.  A workgroup finds its
-// sequence with one 64-way search over the offsets (one wavefront probes 64 of them at a time) and leaves if its block is past the
+// sequence by a search over the offsets of which a wavefront probes 63 at a time, and leaves if its block is past the
 // end.  The rows before the first and behind the last offset are two more "sequences", whose outputs become zeros.  Offsets are
 // read as they come: each border is held inside the tensor, so that no content of them leads out of it.
 //
@@ -48,20 +48,27 @@ struct RaggedPlace {
 template <int SHIFT>
 DEVINL RaggedPlace ragged_place(const int* off, int S, int T, int mul, long slot, int lane)
 {
-    int lo = 0, n = S + 2;
-    while (n > 1) {
-        const int step = (n + 63) / 64, at = lane * step;
-        const bool begun = at < n && (((long)ragged_border(off, S, T, lo + at) * mul) >> SHIFT) + lo + at <= slot;
-        const int c = max((int)__popcll(__ballot(begun)), 1) - 1;
+    int lo = 0, n = S + 2, c = 0, border = 0;
+    do {  // the last step's lanes hold every border that is left, and the one behind them
+        const int step = (n + 62) / 63, at = lane * step;
+        border = ragged_border(off, S, T, lo + at);
+        const bool begun = at < n && (((long)border * mul) >> SHIFT) + lo + at <= slot;
+        c = max((int)__popcll(__ballot(begun)), 1) - 1;
         lo += c * step;
         n = min(step, n - c * step);
-    }
+    } while (n > 1);
     RaggedPlace p;
-    p.i = __builtin_amdgcn_readfirstlane(lo);
-    p.begin = __builtin_amdgcn_readfirstlane(ragged_border(off, S, T, p.i));
-    p.n = max(__builtin_amdgcn_readfirstlane(ragged_border(off, S, T, p.i + 1)) - p.begin, 0);
+    p.i = lo;
+    p.begin = __builtin_amdgcn_readlane(border, c);
+    p.n = max(__builtin_amdgcn_readlane(border, c + 1) - p.begin, 0);
     p.block = slot - (((long)p.begin * mul) >> SHIFT) - p.i;
     return p;
+}
+// The other side's tokens of the interval: begin and number
+DEVINL int2 ragged_tokens(const int* off, int S, int T, int i)
+{
+    const int begin = ragged_border(off, S, T, i);
+    return int2{begin, max(ragged_border(off, S, T, i + 1) - begin, 0)};
 }
 
 // NBUF buffers in LDS of an A and a B tile of ROWS token rows each (and, with SCALARS, ROWS + ROWS floats), filled by LDS-direct loads
@@ -378,7 +385,9 @@ avion_ragged_fwd_kernel(RaggedArgs a, raw16* __restrict__ o, float* __restrict__
         ragged_fwd_none<D>(a, o, lse, hk, p.begin + from, to - from, job.tid, Cfg::NT);
         return;
     }
-    const int begin_k = ragged_border(a.off_k, a.S, a.Tk, p.i), nk = max(ragged_border(a.off_k, a.S, a.Tk, p.i + 1) - begin_k, 0);
+    // (offsets that serve both sides are here already)
+    const int2 keys = a.off_k == a.off_q && a.Tk == a.Tq ? int2{p.begin, p.n} : ragged_tokens(a.off_k, a.S, a.Tk, p.i);
+    const int begin_k = keys.x, nk = keys.y;
     const int last_seen = RaggedRow(a, hk, block0 + Cfg::BM - 1, rows, p.n, nk).keys;
     RaggedSums<(D + 31) / 32> sums;
     const int row0 = block0 + wave * 32;
@@ -546,7 +555,9 @@ avion_ragged_dq_kernel(RaggedArgs a, const raw16* __restrict__ o, const raw16* _
         ragged_zero<D>(dq, a.Hq, hk * a.G, a.G, p.begin + from, to - from, job.tid, Cfg::NT);
         return;
     }
-    const int begin_k = ragged_border(a.off_k, a.S, a.Tk, p.i), nk = max(ragged_border(a.off_k, a.S, a.Tk, p.i + 1) - begin_k, 0);
+    // (offsets that serve both sides are here already)
+    const int2 keys = a.off_k == a.off_q && a.Tk == a.Tq ? int2{p.begin, p.n} : ragged_tokens(a.off_k, a.S, a.Tk, p.i);
+    const int begin_k = keys.x, nk = keys.y;
     constexpr int ROWS = Ring::ROWS;
     const int ntiles = (RaggedRow(a, hk, block0 + Cfg::BM - 1, rows, nq, nk).keys + ROWS - 1) / ROWS;
     const bool whole = ntiles * ROWS <= 128;
@@ -705,8 +716,8 @@ avion_ragged_dkdv_kernel(RaggedArgs a, const raw16* __restrict__ dO, const float
     const int nk = p.n;
     if (p.block < 0 || p.block * Cfg::BN >= nk) return;
     const int block0 = (int)p.block * Cfg::BN, k0 = block0 + wave * 32;
-    const int begin_q = ragged_border(a.off_q, a.S, a.Tq, p.i);
-    const int nq = p.i == 0 || p.i == a.S + 1 ? 0 : max(ragged_border(a.off_q, a.S, a.Tq, p.i + 1) - begin_q, 0);
+    const int2 queries = a.off_k == a.off_q && a.Tk == a.Tq ? int2{p.begin, p.n} : ragged_tokens(a.off_q, a.S, a.Tq, p.i);
+    const int begin_q = queries.x, nq = p.i == 0 || p.i == a.S + 1 ? 0 : queries.y;
     const bool active = k0 < nk;
     // first query that sees a key: this lane's, the wavefront's first and last, the workgroup's first
     auto first_query = [&](int key) { return a.causal ? max(min(key, nk - 1) - nk + nq, 0) : 0; };
