@@ -27,9 +27,13 @@ struct RaggedArgs {
     const int *off_q, *off_k;
     long rs_q, rs_k, rs_v;  // token rows of q, k, v, elements apart; of o and the gradients Hq d and Hk d
     int S, Tq, Tk, Hq, Hk, G;
+    unsigned g_mul, g_shift;  // of over_heads()
     int slots;
     int causal;
     float cs, scale;        // scale * log2 e, scale
+    // r / G for 0 <= r < 2^31: multiplication by 2^(32 + shift) / G, whose 33rd bit is the addition (a division by a number known at run
+    // time is some 25 instructions, of which a wavefront with one short sequence would spend more than on the softmax)
+    DEVINL int over_heads(int r) const { return (int)((__umulhi(g_mul, (unsigned)r) + (unsigned)r) >> g_shift); }
 };
 
 // border i of 0 .. S + 2: 0, the offsets, T
@@ -74,11 +78,15 @@ DEVINL int2 ragged_tokens(const int* off, int S, int T, int i)
 // NBUF buffers in LDS of an A and a B tile of ROWS token rows each (and, with SCALARS, ROWS + ROWS floats), filled by LDS-direct loads
 // as TileRing's.  The descriptors begin at the tile's own first row, so that no length of a sequence and no row stride takes a
 // byte offset past 32 bits; rows past the end arrive as zeros.
+// Layout of a tile: at 64 channels quad_at's (no bank conflicts, and two addresses a lane for the loads of both tensors instead of one
+// for each load: where registers are scarce, in dK/dV, that is what keeps the accumulators out of scratch), else padded rows.
 template <int D, int NW, int ROWS_, int NBUF_, bool SCALARS>
 struct RaggedRing {
     static constexpr int ROWS = ROWS_, NBUF = NBUF_, STRIDE = tile_stride<D>();
+    static constexpr bool QUAD = D == 64;
     // 1 KB blocks of a tile (the last one's rows past the tile, where there are any, are not read)
-    static constexpr int NTI = (ROWS * STRIDE + 1023) / 1024, NBLK = 2 * NTI, NPW = (NBLK + NW - 1) / NW;
+    static constexpr int NTI = QUAD ? ROWS / 8 : (ROWS * STRIDE + 1023) / 1024, NBLK = 2 * NTI, NPW = (NBLK + NW - 1) / NW;
+    static_assert(!QUAD || (NTI % NW == 0 && (NW == 1 || NW % 2 == 0)), "a load's blocks belong to one tensor, a wavefront's are all even or all odd");
     static constexpr int OFF_B = NTI * 1024, OFF_SCALARS = 2 * NTI * 1024;
     static constexpr int BUF_BYTES = NBLK * 1024 + (SCALARS ? 1024 : 0);
     static constexpr int LDS_BYTES = NBUF * BUF_BYTES + (D % 32 != 0 ? 64 : 0);
@@ -88,7 +96,7 @@ struct RaggedRing {
     long rs_a, rs_b;
     int n, wave;
     unsigned smem_addr, npad_bytes, scalar_voff;
-    unsigned voff[NPW];
+    unsigned place[QUAD ? 3 : NPW];  // of this lane: rows of a and b, and the chunk; or each load's byte offset
 
     // a, b: first rows, rs_a and rs_b elements apart, n of them; scalars: two arrays npad floats apart
     DEVINL RaggedRing(const raw16* a_, long rs_a_, const raw16* b_, long rs_b_, const float* scalars_, int npad, int n_, char* smem,
@@ -96,14 +104,32 @@ struct RaggedRing {
         : a(a_), b(b_), scalars(scalars_), rs_a(rs_a_), rs_b(rs_b_), n(n_), wave(wave_), smem_addr(lds_address(smem)),
           npad_bytes((unsigned)npad * 4)
     {
+        if constexpr (QUAD) {
+            const unsigned row = 8 * wave + lane / 32 * 4 + lane / 4 % 4;
+            place[0] = row * (unsigned)(rs_a * 2);
+            place[1] = row * (unsigned)(rs_b * 2);
+            place[2] = (lane / 16 % 2 * 4 + ((lane ^ (row >> 2)) & 3)) * 16;
+        } else {
 #pragma unroll
-        for (int j = 0; j < NPW; ++j) {
-            const int blk = wave + NW * j;
-            const bool first = blk < NTI;
-            voff[j] = padded_block_voff<D>(first ? blk : blk - NTI, lane, (unsigned)((first ? rs_a : rs_b) * 2));
+            for (int j = 0; j < NPW; ++j) {
+                const int blk = wave + NW * j;
+                const bool first = blk < NTI;
+                place[j] = padded_block_voff<D>(first ? blk : blk - NTI, lane, (unsigned)((first ? rs_a : rs_b) * 2));
+            }
         }
         if constexpr (SCALARS)
             scalar_voff = lane < ROWS / 4 ? (unsigned)lane * 16 : lane < ROWS / 2 ? npad_bytes + (lane - ROWS / 4) * 16 : kOutOfRangeBase;
+    }
+    // this lane's byte offset in load j
+    DEVINL unsigned voff(int j) const
+    {
+        if constexpr (QUAD) {
+            const bool first = NW * j < NTI;
+            const unsigned down = (unsigned)(8 * (NW * j - (first ? 0 : NTI))) * (unsigned)((first ? rs_a : rs_b) * 2);
+            return place[first ? 0 : 1] + down + (NW == 1 ? place[2] ^ (32 * (j & 1)) : place[2]);
+        } else {
+            return place[j];
+        }
     }
     // this wavefront's share of the loads of tile t, into buffer `to` (t % NBUF)
     DEVINL void fetch(int t) const { fetch(t, t & (NBUF - 1)); }
@@ -113,12 +139,18 @@ struct RaggedRing {
         const RawBuffer ab(a + (long)r0 * rs_a, left > 0 ? slice_bytes(rs_a, left, D) : 0);
         const RawBuffer bb(b + (long)r0 * rs_b, left > 0 ? slice_bytes(rs_b, left, D) : 0);
         const unsigned base = smem_addr + to * BUF_BYTES + wave * 1024;
+        // load j's descriptor: known from j where all wavefronts' blocks of it belong to one tensor
+        auto desc = [&](int j) { return NW * j + NW - 1 < NTI ? ab : NW * j >= NTI ? bb : pick(wave + NW * j < NTI, ab, bb); };
+        constexpr int WHOLE = NBLK / NW, FOURS = WHOLE / 4 * 4;  // loads that every wavefront has
 #pragma unroll
-        for (int j = 0; j < NPW; ++j) {
-            const int blk = wave + NW * j;
-            if (NBLK % NW != 0 && blk >= NBLK) continue;
-            load_to_lds16(pick(blk < NTI, ab, bb), base + NW * j * 1024, voff[j]);
-        }
+        for (int j = 0; j < FOURS; j += 4)
+            load_to_lds16_x4<NW * 1024>(desc(j), desc(j + 1), desc(j + 2), desc(j + 3), base + NW * j * 1024, voff(j), voff(j + 1), voff(j + 2),
+                                        voff(j + 3));
+        if constexpr (WHOLE - FOURS >= 2)
+            load_to_lds16_x2<NW * 1024>(desc(FOURS), desc(FOURS + 1), base + NW * FOURS * 1024, voff(FOURS), voff(FOURS + 1));
+#pragma unroll
+        for (int j = FOURS + (WHOLE - FOURS) / 2 * 2; j < NPW; ++j)
+            if (j < WHOLE || wave + NW * j < NBLK) load_to_lds16(desc(j), base + NW * j * 1024, voff(j));
         if constexpr (SCALARS)
             // (the arrays go on to the next multiple of 64 rows)
             if (wave == NW - 1) load_to_lds16(RawBuffer(scalars + r0, npad_bytes + ROWS * 4), smem_addr + to * BUF_BYTES + OFF_SCALARS, scalar_voff);
@@ -139,6 +171,37 @@ struct RaggedRing {
             fetch(t);
             landed_barrier();
         }
+    }
+};
+
+// A lane's fragments of a tile: rows 32 * hk .. of it (natural) and 16 tokens of step `step` (transposed)
+template <int D>
+struct RaggedLane {
+    unsigned nat, tr;
+    DEVINL explicit RaggedLane(int lane)
+        : nat((unsigned)(lane % 32 * tile_stride<D>() + lane / 32 * 16)), tr((unsigned)tr_lane_offset(lane, tile_stride<D>()))
+    {
+    }
+    DEVINL frag8 natural(const char* tile, int hk, int ks) const
+    {
+        return *reinterpret_cast<const frag8*>(tile + nat + 32 * hk * tile_stride<D>() + ks * 32);
+    }
+    DEVINL frag8 transposed(const char* tile, int ct, int step) const { return tr_frag(tile, tile_stride<D>(), (int)tr, ct, step); }
+};
+template <>
+struct RaggedLane<64> : QuadLane {
+    DEVINL explicit RaggedLane(int lane) : QuadLane(lane, 0) {}
+    DEVINL frag8 natural(const char* tile, int hk, int ks) const
+    {
+        return *reinterpret_cast<const frag8*>(tile + nat[ks & 1] + hk * 4096 + (ks >> 1) * 256);
+    }
+    DEVINL frag8 transposed(const char* tile, int ct, int step) const
+    {
+        const lds_char* p = (const lds_char*)tile + step * 2048 + ct * 256;
+        const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(p + tr[0]));
+        const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(p + tr[1]));
+        const u32x2 l2 = __builtin_bit_cast(u32x2, lo), h2 = __builtin_bit_cast(u32x2, hi);
+        return as_frag8(u32x4{l2[0], l2[1], h2[0], h2[1]});
     }
 };
 
@@ -177,7 +240,7 @@ struct RaggedRow {
     int token, head, keys;
     DEVINL RaggedRow(const RaggedArgs& a, int hk, int row, int rows, int nq, int nk)
     {
-        const int r = min(row, rows - 1), i = r / a.G;
+        const int r = min(row, rows - 1), i = a.over_heads(r);
         token = i;
         head = hk * a.G + r - i * a.G;
         keys = a.causal ? min(max(i + 1 + nk - nq, 0), nk) : nk;
@@ -208,7 +271,7 @@ struct RaggedStore {
         for (int x = 0; x < (32 * CH + 63) / 64; ++x) {
             const int idx = lane + 64 * x, row = idx / CH, ch = idx % CH, r = row0 + row;
             if (idx < 32 * CH && r < rows) {
-                const int i = r / a.G;
+                const int i = a.over_heads(r);
                 *reinterpret_cast<u32x4*>(out + ((long)(begin + i) * a.Hq + hk * a.G + r - i * a.G) * D + ch * 8) =
                     *reinterpret_cast<const u32x4*>(region + row * STRIDE + ch * 16);
             }
@@ -265,8 +328,9 @@ DEVINL void ragged_fwd_walk(char* smem, const RaggedArgs& a, int hk, int begin_q
                             int t1, RaggedSums<(D + 31) / 32>& sums, int wave, int lane)
 {
     using Ring = typename RaggedFwdCfg<D, NW, ROWS, NBUF>::Ring;
-    constexpr int KS = D / 16, CT = (D + 31) / 32, STRIDE = Ring::STRIDE;
-    const int l32 = lane % 32, g = lane / 32, tr_off = tr_lane_offset(lane, STRIDE);
+    constexpr int KS = D / 16, CT = (D + 31) / 32;
+    const int l32 = lane % 32, g = lane / 32;
+    const RaggedLane<D> at(lane);
     const Ring ring(a.k + (long)begin_k * a.rs_k + hk * D, a.rs_k, a.v + (long)begin_k * a.rs_v + hk * D, a.rs_v, nullptr, 0, nk, smem,
                     wave, lane);
     if (t0 < t1) ring.fetch(t0);
@@ -285,24 +349,26 @@ DEVINL void ragged_fwd_walk(char* smem, const RaggedArgs& a, int hk, int begin_q
     auto unit = [&](const char* kt, const char* vt, int hk32, int key_base) {
         f32x16 s = key_base + 32 > seen_by_all ? key_mask_block(key_base, g, row.keys) : f32x16_zero();
 #pragma unroll
-        for (int ks = 0; ks < KS; ++ks) s = E::mfma(nat_frag(kt, STRIDE, 32 * hk32 + l32, ks, g), qf[ks], s);
+        for (int ks = 0; ks < KS; ++ks) s = E::mfma(at.natural(kt, hk32, ks), qf[ks], s);
         frag8 vf[2][CT];
         if constexpr (D <= 96) {
 #pragma unroll
             for (int half = 0; half < 2; ++half)
 #pragma unroll
-                for (int ct = 0; ct < CT; ++ct) vf[half][ct] = tr_frag(vt, STRIDE, tr_off, ct, 2 * hk32 + half);
+                for (int ct = 0; ct < CT; ++ct) vf[half][ct] = at.transposed(vt, ct, 2 * hk32 + half);
         }
         const float top = both_halves_max(max16(s)) * cs;
         if (__any(top > sums.m + kRaggedLazy)) {
             const float m = fmaxf(sums.m, top), shrink = fast_exp2(sums.m - m);
             sums.m = m;
-            sums.l *= shrink;
-            sums.rs4 *= shrink;
+            if (key_base > t0 * ROWS) {  // (the first unit finds zeros)
+                sums.l *= shrink;
+                sums.rs4 *= shrink;
 #pragma unroll
-            for (int ct = 0; ct < CT; ++ct)
+                for (int ct = 0; ct < CT; ++ct)
 #pragma unroll
-                for (int i = 0; i < 16; ++i) sums.o[ct][i] *= shrink;
+                    for (int i = 0; i < 16; ++i) sums.o[ct][i] *= shrink;
+            }
         }
         u32x4 pf[2];
 #pragma unroll
@@ -318,7 +384,7 @@ DEVINL void ragged_fwd_walk(char* smem, const RaggedArgs& a, int hk, int begin_q
         for (int half = 0; half < 2; ++half)
 #pragma unroll
             for (int ct = 0; ct < CT; ++ct) {
-                if constexpr (D > 96) vf[half][ct] = tr_frag(vt, STRIDE, tr_off, ct, 2 * hk32 + half);
+                if constexpr (D > 96) vf[half][ct] = at.transposed(vt, ct, 2 * hk32 + half);
                 sums.o[ct] = E::mfma(vf[half][ct], as_frag8(pf[half]), sums.o[ct]);
             }
     };
@@ -348,7 +414,7 @@ DEVINL void ragged_fwd_store(char* region, const RaggedArgs& a, raw16* o, float*
     RaggedStore<D, E>::run(region, sums.o, r == 0.f ? 0.f : 1.f / r, o, a, hk, begin_q, row0, rows, lane);
     const int row = row0 + lane;
     if (lane < 32 && row < rows) {
-        const int i = row / a.G;
+        const int i = a.over_heads(row);
         lse[(long)(hk * a.G + row - i * a.G) * a.Tq + begin_q + i] = l == 0.f ? -INFINITY : (sums.m + __builtin_amdgcn_logf(l)) * kLn2;
     }
 }
@@ -502,7 +568,7 @@ avion_ragged_join_kernel(RaggedArgs a, raw16* __restrict__ o, float* __restrict_
             ls += __shfl(l, lane % LANES + x * LANES);
             rs += __shfl(r, lane % LANES + x * LANES);
         }
-        const int q = row / a.G, head = hk * a.G + row - q * a.G;
+        const int q = a.over_heads(row), head = hk * a.G + row - q * a.G;
         const float inv = rs == 0.f ? 0.f : 1.f / rs;
         if (group == 0)
             *reinterpret_cast<u32x2*>(o + ((long)(begin_q + q) * a.Hq + head) * D + col) =
@@ -527,7 +593,7 @@ template <int D, int NW>
 struct RaggedDqCfg {
     using Ring = RaggedRing<D, NW, kRaggedRows<NW>, kRaggedBuffers<NW>, false>;
     static constexpr int NT = NW * 64, BM = 32 * NW, SHIFT = NW == 4 ? 7 : 5, LDS_BYTES = Ring::LDS_BYTES;
-    static constexpr int WAVES_PER_SIMD = D == 64 ? 3 : 2;
+    static constexpr int WAVES_PER_SIMD = D == 64 ? 4 : 2;
 };
 DEVINL long ragged_scalar_at(int begin, int i) { return ((long)(begin >> 6) + i) * 64; }
 
@@ -538,7 +604,7 @@ avion_ragged_dq_kernel(RaggedArgs a, const raw16* __restrict__ o, const raw16* _
 {
     using Cfg = RaggedDqCfg<D, NW>;
     using Ring = typename Cfg::Ring;
-    constexpr int KS = D / 16, CT = (D + 31) / 32, STRIDE = Ring::STRIDE;
+    constexpr int KS = D / 16, CT = (D + 31) / 32;
     extern __shared__ __attribute__((aligned(16))) char shared[];
     const int lane = threadIdx.x % 64, l32 = lane % 32, g = lane / 32;
     const RaggedJob<NW> job(shared, Cfg::LDS_BYTES);
@@ -565,7 +631,8 @@ avion_ragged_dq_kernel(RaggedArgs a, const raw16* __restrict__ o, const raw16* _
                     wave, lane);
     if (ntiles > 0) ring.fetch(0);
     if (Ring::NBUF == 2 && ntiles == 2) ring.fetch(1);
-    const int row0 = block0 + wave * 32, tr_off = tr_lane_offset(lane, STRIDE);
+    const int row0 = block0 + wave * 32;
+    const RaggedLane<D> at(lane);
     const bool active = row0 < rows;
     const RaggedRow row(a, hk, row0 + l32, rows, nq, nk);
     const int seen_by_all = RaggedRow(a, hk, row0, rows, nq, nk).keys, seen_by_any = RaggedRow(a, hk, row0 + 31, rows, nq, nk).keys;
@@ -573,13 +640,13 @@ avion_ragged_dq_kernel(RaggedArgs a, const raw16* __restrict__ o, const raw16* _
     float dl;
     {
         const raw16* q = a.q + (long)(p.begin + row.token) * a.rs_q + row.head * D + g * 8;
-        const long at = ((long)(p.begin + row.token) * a.Hq + row.head) * D + g * 8;
+        const long out_at = ((long)(p.begin + row.token) * a.Hq + row.head) * D + g * 8;
         float part = 0.f;
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) {
             qf[ks] = *reinterpret_cast<const frag8*>(q + ks * 16);
-            gf[ks] = *reinterpret_cast<const frag8*>(dO + at + ks * 16);
-            const frag8 of = *reinterpret_cast<const frag8*>(o + at + ks * 16);
+            gf[ks] = *reinterpret_cast<const frag8*>(dO + out_at + ks * 16);
+            const frag8 of = *reinterpret_cast<const frag8*>(o + out_at + ks * 16);
 #pragma unroll
             for (int e = 0; e < 8; ++e) part = fmaf(E::widen(of, e), E::widen(gf[ks], e), part);
         }
@@ -597,7 +664,7 @@ avion_ragged_dq_kernel(RaggedArgs a, const raw16* __restrict__ o, const raw16* _
         sc = key_base + 32 > seen_by_all ? key_mask_block(key_base, g, row.keys) : f32x16_zero();
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) {
-            const frag8 ak = nat_frag(kt, STRIDE, 32 * hk32 + l32, ks, g), av = nat_frag(vt, STRIDE, 32 * hk32 + l32, ks, g);
+            const frag8 ak = at.natural(kt, hk32, ks), av = at.natural(vt, hk32, ks);
             sc = E::mfma(ak, qf[ks], sc);
             dp = E::mfma(av, gf[ks], ks == 0 ? f32x16_zero() : dp);
         }
@@ -626,7 +693,8 @@ avion_ragged_dq_kernel(RaggedArgs a, const raw16* __restrict__ o, const raw16* _
     // the rows up to the next multiple of 64: weight 0
     if (block0 + Cfg::BM >= rows)
         for (int x = job.tid; x < (-nq & 63) * a.G; x += Cfg::NT) {
-            float* ws = rowsc + (long)(hk * a.G + x % a.G) * 2 * npad + ragged_scalar_at(p.begin, p.i) + nq + x / a.G;
+            const int i = a.over_heads(x);
+            float* ws = rowsc + (long)(hk * a.G + x - i * a.G) * 2 * npad + ragged_scalar_at(p.begin, p.i) + nq + i;
             ws[0] = INFINITY;
             ws[npad] = 0.f;
         }
@@ -640,7 +708,7 @@ avion_ragged_dq_kernel(RaggedArgs a, const raw16* __restrict__ o, const raw16* _
 #pragma unroll
             for (int half = 0; half < 2; ++half)
 #pragma unroll
-                for (int ct = 0; ct < CT; ++ct) kf[half][ct] = tr_frag(kt, STRIDE, tr_off, ct, 2 * hk32 + half);
+                for (int ct = 0; ct < CT; ++ct) kf[half][ct] = at.transposed(kt, ct, 2 * hk32 + half);
         }
         u32x4 df[2];
 #pragma unroll
@@ -652,7 +720,7 @@ avion_ragged_dq_kernel(RaggedArgs a, const raw16* __restrict__ o, const raw16* _
         for (int half = 0; half < 2; ++half)
 #pragma unroll
             for (int ct = 0; ct < CT; ++ct) {
-                if constexpr (D > 96) kf[half][ct] = tr_frag(kt, STRIDE, tr_off, ct, 2 * hk32 + half);
+                if constexpr (D > 96) kf[half][ct] = at.transposed(kt, ct, 2 * hk32 + half);
                 acc[ct] = E::mfma(kf[half][ct], as_frag8(df[half]), acc[ct]);
             }
     };
@@ -704,7 +772,7 @@ avion_ragged_dkdv_kernel(RaggedArgs a, const raw16* __restrict__ dO, const float
 {
     using Cfg = RaggedDkvCfg<D, NW>;
     using Ring = typename Cfg::Ring;
-    constexpr int KS = D / 16, CT = (D + 31) / 32, STRIDE = Ring::STRIDE, OFF_G = Ring::OFF_B, ROWS = Ring::ROWS;
+    constexpr int KS = D / 16, CT = (D + 31) / 32, OFF_G = Ring::OFF_B, ROWS = Ring::ROWS;
     extern __shared__ __attribute__((aligned(16))) char shared[];
     const int lane = threadIdx.x % 64, l32 = lane % 32, g = lane / 32;
     const RaggedJob<NW> job(shared, Cfg::LDS_BYTES);
@@ -757,7 +825,7 @@ avion_ragged_dkdv_kernel(RaggedArgs a, const raw16* __restrict__ dO, const float
     hold(vf);
     Ring::landed_barrier();
     const float cs = a.cs;
-    const int tr_off = tr_lane_offset(lane, STRIDE);
+    const RaggedLane<D> at(lane);
 
     auto unit = [&](const char* buf, int hq, int query_base) {
         const float* rowv = reinterpret_cast<const float*>(buf + Ring::OFF_SCALARS) + 32 * hq + 4 * g;
@@ -770,7 +838,7 @@ avion_ragged_dkdv_kernel(RaggedArgs a, const raw16* __restrict__ dO, const float
         }
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) {
-            const frag8 aq = nat_frag(buf, STRIDE, 32 * hq + l32, ks, g), ag = nat_frag(buf + OFF_G, STRIDE, 32 * hq + l32, ks, g);
+            const frag8 aq = at.natural(buf, hq, ks), ag = at.natural(buf + OFF_G, hq, ks);
             s = E::mfma(aq, kf[ks], s);
             dp = E::mfma(ag, vf[ks], dp);
         }
@@ -783,8 +851,8 @@ avion_ragged_dkdv_kernel(RaggedArgs a, const raw16* __restrict__ dO, const float
             if constexpr (D <= 96) {
 #pragma unroll
                 for (int ct = 0; ct < CT; ++ct) {
-                    tg[ct] = tr_frag(buf + OFF_G, STRIDE, tr_off, ct, 2 * hq + half);
-                    tq[ct] = tr_frag(buf, STRIDE, tr_off, ct, 2 * hq + half);
+                    tg[ct] = at.transposed(buf + OFF_G, ct, 2 * hq + half);
+                    tq[ct] = at.transposed(buf, ct, 2 * hq + half);
                 }
             }
             u32x4 pf, df;
@@ -802,8 +870,8 @@ avion_ragged_dkdv_kernel(RaggedArgs a, const raw16* __restrict__ dO, const float
 #pragma unroll
             for (int ct = 0; ct < CT; ++ct) {
                 if constexpr (D > 96) {
-                    tg[ct] = tr_frag(buf + OFF_G, STRIDE, tr_off, ct, 2 * hq + half);
-                    tq[ct] = tr_frag(buf, STRIDE, tr_off, ct, 2 * hq + half);
+                    tg[ct] = at.transposed(buf + OFF_G, ct, 2 * hq + half);
+                    tq[ct] = at.transposed(buf, ct, 2 * hq + half);
                 }
                 dva[ct] = E::mfma(tg[ct], as_frag8(pf), dva[ct]);
                 dka[ct] = E::mfma(tq[ct], as_frag8(df), dka[ct]);
@@ -833,17 +901,17 @@ avion_ragged_dkdv_kernel(RaggedArgs a, const raw16* __restrict__ dO, const float
     if (!active) return;
     const int lane_now = lane_from_exec();
     const float dv_mul = std::is_same<E, F16>::value ? 1.f / 256.f : 1.f;
-    const long rs = (long)a.Hk * D, at = (long)(p.begin + k0) * rs + hk * D;
+    const long rs = (long)a.Hk * D, out_at = (long)(p.begin + k0) * rs + hk * D;
     if (parts > 1) {
         const long whole = (long)a.Tk * rs;
-        float* out = sums + part * 2 * whole + at;
+        float* out = sums + part * 2 * whole + out_at;
         ragged_store_part<D>(dka, out, rs, nk - k0, lane_now);
         ragged_store_part<D>(dva, out + whole, rs, nk - k0, lane_now);
         return;
     }
     char* region = smem + wave * RowStore<D, E>::BYTES;
-    RowStore<D, E>::run(region, dka, a.scale, dk + at, rs, nk - k0, lane_now);
-    RowStore<D, E>::run(region, dva, dv_mul, dv + at, rs, nk - k0, lane_now);
+    RowStore<D, E>::run(region, dka, a.scale, dk + out_at, rs, nk - k0, lane_now);
+    RowStore<D, E>::run(region, dva, dv_mul, dv + out_at, rs, nk - k0, lane_now);
 }
 
 // dK and dV from the parts' sums, part after part

@@ -102,6 +102,8 @@ RaggedArgs ragged_args(const RaggedShape& s, const void* q, const void* k, const
     a.Hq = s.Hq;
     a.Hk = s.Hk;
     a.G = s.Hq / s.Hk;
+    while ((1LL << a.g_shift) < a.G) ++a.g_shift;
+    a.g_mul = (unsigned)((1ULL << 32) * ((1ULL << a.g_shift) - a.G) / a.G + 1);
     a.causal = flags & AVION_FLAG_CAUSAL ? 1 : 0;
     a.cs = scale * kLog2e;
     a.scale = scale;
