@@ -126,6 +126,15 @@ struct LossCfg {
 
 DEVINL void loss_landed_barrier() { asm volatile("s_waitcnt vmcnt(0)\n\ts_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 
+// Tile number -> its places: 8 blocks of b, then the next a.  What an XCD's workgroups hold at a time, neighbouring numbers, is then 8
+// blocks of b by a few of a, whose operands fit its L2.
+DEVINL void loss_place(int tile, int na, int nb, int& a, int& b)
+{
+    const int group = tile / (8 * na), in = tile - group * 8 * na, blocks = min(8, nb - group * 8);
+    a = in / blocks;
+    b = group * 8 + in - a * blocks;
+}
+
 // The tiles place(0) .. place(count - 1) -- each sets (a0, b0) -- of one workgroup, over all of K; done(a0, b0, acc) takes a tile's sums.
 template <typename Cfg, typename E, typename Place, typename Done>
 DEVINL void loss_product(char* smem, const LossOperand& opa, const LossOperand& opb, int K, int count, int wave, int lane, Place place, Done done)
@@ -263,8 +272,10 @@ avion_loss_fwd_kernel(LossArgs a, float2* __restrict__ parts, float* __restrict_
     __shared__ float2 meet[WA][TB];
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), l32 = lane % 32, g = lane / 32;
     const int wa = wave % WA, wb = wave / WA;
-    // the workgroups of an XCD (they go round) take neighbouring runs, of the same rows first
-    const int block = blockIdx.x / slabs, slab = blockIdx.x % slabs;
+    const int blocks = (a.T + TB - 1) / TB, logical = xcd_local_id(blockIdx.x, blocks * slabs);
+    if (logical < 0) return;
+    int slab, block;
+    loss_place(logical, slabs, blocks, slab, block);
     const int b0 = block * TB, ntiles = (a.V + TA - 1) / TA;
     const int first = (int)((long)ntiles * slab / slabs), last = (int)((long)ntiles * (slab + 1) / slabs);
     float m[MI], l[MI];
@@ -460,7 +471,7 @@ avion_loss_dz_kernel(LossArgs a, const float* __restrict__ lse, const float* __r
     extern __shared__ __attribute__((aligned(16))) char smem[];
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), l32 = lane % 32, g = lane / 32;
     const int wa = wave % WA, wb = wave / WA;
-    const int na = (n + TA - 1) / TA, ntiles = na * ((a.T + TB - 1) / TB), per = (ntiles + 7) / 8, together = gridDim.x / 8;
+    const int na = (n + TA - 1) / TA, nb = (a.T + TB - 1) / TB, ntiles = na * nb, per = (ntiles + 7) / 8, together = gridDim.x / 8;
     const int first = blockIdx.x % 8 * per + blockIdx.x / 8, end = min(ntiles, (blockIdx.x % 8 + 1) * per);
     char* stage = smem + 2 * Cfg::STAGE + wave * ((NI == 2 ? 16 : 32) * Cfg::OUT_ROW);
     const LossOperand opa{a.w + (long)v0 * a.rs_w, a.rs_w, n, 0}, opb{a.x, a.rs_x, a.T, 0};
@@ -468,9 +479,9 @@ avion_loss_dz_kernel(LossArgs a, const float* __restrict__ lse, const float* __r
     loss_product<Cfg, E>(
         smem, opa, opb, a.D, first < end ? (end - first + together - 1) / together : 0, wave, lane,
         [&](int t, int& a0, int& b0) {
-            const int tile = first + t * together;
-            a0 = tile % na * TA;
-            b0 = tile / na * TB;
+            loss_place(first + t * together, na, nb, a0, b0);
+            a0 *= TA;
+            b0 *= TB;
         },
         [&](int a0, int b0, f32x16(&acc)[MI][NI]) {
             const int from = a0 + wa * NI * 32;
@@ -502,16 +513,16 @@ avion_loss_grad_kernel(LossOperand opa, LossOperand opb, int rows, int K, const 
     extern __shared__ __attribute__((aligned(16))) char smem[];
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), l32 = lane % 32, g = lane / 32;
     const int wa = wave % WA, wb = wave / WA, cols = opa.extent;
-    const int na = (cols + TA - 1) / TA, ntiles = na * ((rows + TB - 1) / TB), per = (ntiles + 7) / 8, together = gridDim.x / 8;
+    const int na = (cols + TA - 1) / TA, nb = (rows + TB - 1) / TB, ntiles = na * nb, per = (ntiles + 7) / 8, together = gridDim.x / 8;
     const int first = blockIdx.x % 8 * per + blockIdx.x / 8, end = min(ntiles, (blockIdx.x % 8 + 1) * per);
     char* stage = smem + 2 * Cfg::STAGE + wave * ((NI == 2 ? 16 : 32) * Cfg::OUT_ROW);
     const float mul = factors[0];
     loss_product<Cfg, E>(
         smem, opa, opb, K, first < end ? (end - first + together - 1) / together : 0, wave, lane,
         [&](int t, int& a0, int& b0) {
-            const int tile = first + t * together;
-            a0 = tile % na * TA;
-            b0 = tile / na * TB;
+            loss_place(first + t * together, na, nb, a0, b0);
+            a0 *= TA;
+            b0 *= TB;
         },
         [&](int a0, int b0, f32x16(&acc)[MI][NI]) {
             const int from = a0 + wa * NI * 32;

@@ -163,7 +163,7 @@ int avion_linear_ce_fwd(const void* x, const void* w, const void* targets, float
                 using X = Tile<TB>;
                 static std::atomic<unsigned long long> allowed{0};
                 return launch(avion_loss_fwd_kernel<X::TA, TB, X::WA, X::WB, E>, 2 * LossCfg<Along::kK, Along::kK, X::TA, TB, X::WA, X::WB>::STAGE,
-                              allowed, ceil_div(T, TB) * slabs, X::WA * X::WB * 64, st, "launch avion_loss_fwd_kernel", a, parts, hit, slabs);
+                              allowed, ceil_div(ceil_div(T, TB) * slabs, 8) * 8, X::WA * X::WB * 64, st, "launch avion_loss_fwd_kernel", a, parts, hit, slabs);
             });
         });
         if (first != AVION_OK) return first;
