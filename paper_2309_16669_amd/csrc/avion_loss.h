@@ -135,7 +135,11 @@ DEVINL void loss_place(int tile, int na, int nb, int& a, int& b)
     b = group * 8 + in - a * blocks;
 }
 
-// The tiles place(0) .. place(count - 1) -- each sets (a0, b0) -- of one workgroup, over all of K; done(a0, b0, acc) takes a tile's sums.
+// The tiles place(0) .. place(count - 1) of one workgroup, each an (a0, b0) and steps k0 .. k1 - 1 (k1 > k0); done(n, a0, b0, acc) takes
+// the sums of tile n.
+struct LossPlace {
+    int a0, b0, k0, k1;
+};
 template <typename Cfg, typename E, typename Place, typename Done>
 DEVINL void loss_product(char* smem, const LossOperand& opa, const LossOperand& opb, int K, int count, int wave, int lane, Place place, Done done)
 {
@@ -145,25 +149,26 @@ DEVINL void loss_product(char* smem, const LossOperand& opa, const LossOperand& 
     typename Cfg::TileA ta(opa, K, wave, lane);
     typename Cfg::TileB tb(opb, K, wave, lane);
     const unsigned lds = lds_address(smem);
-    const int steps = (K + kLossStep - 1) / kLossStep, total = count * steps;
-    int f_n = 0, f_step = 0, f_a0 = 0, f_b0 = 0;  // next step to fetch
+    // the next step to fetch
+    int f_n = 0;
+    LossPlace f = place(0);
+    int f_k = f.k0;
+    ta.tile(f.a0);
+    tb.tile(f.b0);
     auto fetch = [&](int buf) {
-        if (f_step == 0) {
-            place(f_n, f_a0, f_b0);
-            ta.tile(f_a0);
-            tb.tile(f_b0);
-        }
         const unsigned to = lds + buf * Cfg::STAGE;
-        ta.fetch(f_a0, f_step * kLossStep, to);
-        tb.fetch(f_b0, f_step * kLossStep, to + Cfg::TileA::BYTES);
-        if (++f_step == steps) {
-            f_step = 0;
-            ++f_n;
+        ta.fetch(f.a0, f_k * kLossStep, to);
+        tb.fetch(f.b0, f_k * kLossStep, to + Cfg::TileA::BYTES);
+        if (++f_k == f.k1 && ++f_n < count) {
+            f = place(f_n);
+            f_k = f.k0;
+            ta.tile(f.a0);
+            tb.tile(f.b0);
         }
     };
     fetch(0);
     loss_landed_barrier();
-    if (total > 1) fetch(1);
+    if (f_n < count) fetch(1);
     frag8 fa[NI], fb[MI];
     auto read = [&](int buf, int ks) {
         const unsigned from = lds + buf * Cfg::STAGE;
@@ -173,14 +178,15 @@ DEVINL void loss_product(char* smem, const LossOperand& opa, const LossOperand& 
         for (int i = 0; i < MI; ++i) fb[i] = tb.read(from + Cfg::TileA::BYTES, wb * MI + i, ks);
     };
     read(0, 0);
-    int q = 0, buf = 0;
+    int buf = 0;
     f32x16 acc[MI][NI];
     for (int n = 0; n < count; ++n) {
+        const LossPlace p = place(n);
 #pragma unroll
         for (int i = 0; i < MI; ++i)
 #pragma unroll
             for (int j = 0; j < NI; ++j) acc[i][j] = f32x16_zero();
-        for (int s = 0; s < steps; ++s, ++q) {
+        for (int k = p.k0; k < p.k1; ++k) {
 #pragma unroll
             for (int ks = 0; ks < 4; ++ks) {
                 frag8 ca[NI], cb[MI];
@@ -190,9 +196,9 @@ DEVINL void loss_product(char* smem, const LossOperand& opa, const LossOperand& 
                 for (int i = 0; i < MI; ++i) cb[i] = fb[i];
                 if (ks < 3) {
                     read(buf, ks + 1);
-                } else if (q + 1 < total) {
+                } else if (k + 1 < p.k1 || n + 1 < count) {
                     loss_landed_barrier();  // the next step is there, and this one in everybody's registers
-                    if (q + 2 < total) fetch(buf);
+                    if (f_n < count) fetch(buf);
                     read(buf ^ 1, 0);
                 }
                 __builtin_amdgcn_sched_barrier(0);
@@ -204,10 +210,9 @@ DEVINL void loss_product(char* smem, const LossOperand& opa, const LossOperand& 
             }
             buf ^= 1;
         }
-        int a0, b0;
-        place(n, a0, b0);
-        done(a0, b0, acc);
+        done(n, p.a0, p.b0, acc);
     }
+    __syncthreads();  // (a second product may begin in the same buffers)
 }
 
 // A wavefront's 32 x (32 NI) part of a result with contiguous a, rounded, to rows of `out` (ld elements apart): through LDS, so that
@@ -289,11 +294,8 @@ avion_loss_fwd_kernel(LossArgs a, float2* __restrict__ parts, float* __restrict_
     const LossOperand opa{a.w, a.rs_w, a.V, 0}, opb{a.x, a.rs_x, a.T, 0};
     loss_product<Cfg, E>(
         smem, opa, opb, a.D, last - first, wave, lane,
-        [&](int n, int& a0, int& bb) {
-            a0 = (first + n) * TA;
-            bb = b0;
-        },
-        [&](int a0, int, f32x16(&acc)[MI][NI]) {
+        [&](int n) { return LossPlace{(first + n) * TA, b0, 0, (a.D + kLossStep - 1) / kLossStep}; },
+        [&](int, int a0, int, f32x16(&acc)[MI][NI]) {
             const int from = a0 + wa * NI * 32;
             const bool ragged = from + NI * 32 > a.V;
 #pragma unroll
@@ -478,12 +480,14 @@ avion_loss_dz_kernel(LossArgs a, const float* __restrict__ lse, const float* __r
     const float inv = factors[1];
     loss_product<Cfg, E>(
         smem, opa, opb, a.D, first < end ? (end - first + together - 1) / together : 0, wave, lane,
-        [&](int t, int& a0, int& b0) {
-            loss_place(first + t * together, na, nb, a0, b0);
-            a0 *= TA;
-            b0 *= TB;
+        [&](int t) {
+            LossPlace p{0, 0, 0, (a.D + kLossStep - 1) / kLossStep};
+            loss_place(first + t * together, na, nb, p.a0, p.b0);
+            p.a0 *= TA;
+            p.b0 *= TB;
+            return p;
         },
-        [&](int a0, int b0, f32x16(&acc)[MI][NI]) {
+        [&](int, int a0, int b0, f32x16(&acc)[MI][NI]) {
             const int from = a0 + wa * NI * 32;
 #pragma unroll
             for (int i = 0; i < MI; ++i) {
@@ -501,52 +505,85 @@ avion_loss_dz_kernel(LossArgs a, const float* __restrict__ lse, const float* __r
         });
 }
 
-// dx (+)= dz w and dw = dz^T x: C [b, a] over K, its first `rows` b, times factors[0] where it is rounded.  sum: fp32 [rows, cols], what earlier pieces left
-// (add) or this one leaves; out: the rounded result, where this is the last.
-template <Along AB, int TA, int TB, int WA, int WB, typename E>
-__global__ void __launch_bounds__(WA* WB * 64, 2)
-avion_loss_grad_kernel(LossOperand opa, LossOperand opb, int rows, int K, const float* __restrict__ factors, float* __restrict__ sum, bool add,
-                       raw16* __restrict__ out)
+// dx (+)= dz w and dw = dz^T x, one launch for both, so that the rounds of their tiles fill each other up (16384 x 25000 x 768: 192 tiles
+// of 392 steps and 294 of 256 on 256 compute units).  C [b, a], its first `rows` b; each tile is cut into `splits` ranges of K.  One
+// range and one piece of the vocabulary: the result, times factors[0], goes to `out`; else to planes of fp32 [splits][rows][cols]
+// (added to what earlier pieces left), of which avion_loss_sum_kernel makes it.
+struct LossGrad {
+    LossOperand a, b;
+    int rows, K, splits;
+    float* sum;
+    int add;
+    raw16* out;
+};
+template <typename Cfg, typename E>
+DEVINL void loss_grad(char* smem, const LossGrad& p, float mul, int first, int step, int wave, int lane)
 {
-    using Cfg = LossCfg<Along::kIndex, AB, TA, TB, WA, WB>;
     constexpr int MI = Cfg::MI, NI = Cfg::NI;
-    extern __shared__ __attribute__((aligned(16))) char smem[];
-    const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), l32 = lane % 32, g = lane / 32;
-    const int wa = wave % WA, wb = wave / WA, cols = opa.extent;
-    const int na = (cols + TA - 1) / TA, nb = (rows + TB - 1) / TB, ntiles = na * nb, per = (ntiles + 7) / 8, together = gridDim.x / 8;
-    const int first = blockIdx.x % 8 * per + blockIdx.x / 8, end = min(ntiles, (blockIdx.x % 8 + 1) * per);
+    const int l32 = lane % 32, g = lane / 32, wa = wave % Cfg::WA, wb = wave / Cfg::WA, cols = p.a.extent;
+    const int na = (cols + Cfg::TA - 1) / Cfg::TA, nb = (p.rows + Cfg::TB - 1) / Cfg::TB, items = na * nb * p.splits;
+    const int steps = (p.K + kLossStep - 1) / kLossStep;
     char* stage = smem + 2 * Cfg::STAGE + wave * ((NI == 2 ? 16 : 32) * Cfg::OUT_ROW);
-    const float mul = factors[0];
     loss_product<Cfg, E>(
-        smem, opa, opb, K, first < end ? (end - first + together - 1) / together : 0, wave, lane,
-        [&](int t, int& a0, int& b0) {
-            loss_place(first + t * together, na, nb, a0, b0);
-            a0 *= TA;
-            b0 *= TB;
+        smem, p.a, p.b, p.K, first < items ? (items - first + step - 1) / step : 0, wave, lane,
+        [&](int n) {
+            const int item = first + n * step, split = item / (na * nb);
+            LossPlace at{0, 0, (int)((long)steps * split / p.splits), (int)((long)steps * (split + 1) / p.splits)};
+            loss_place(item - split * na * nb, na, nb, at.a0, at.b0);
+            at.a0 *= Cfg::TA;
+            at.b0 *= Cfg::TB;
+            return at;
         },
-        [&](int a0, int b0, f32x16(&acc)[MI][NI]) {
-            const int from = a0 + wa * NI * 32;
+        [&](int n, int a0, int b0, f32x16(&acc)[MI][NI]) {
+            const int from = a0 + wa * NI * 32, split = (first + n * step) / (na * nb);
 #pragma unroll
             for (int i = 0; i < MI; ++i) {
                 const int m0 = b0 + (wb * MI + i) * 32, row = m0 + l32;
-                if (sum && row < rows) {
+                if (!p.out) {
+                    if (row < p.rows) {
 #pragma unroll
-                    for (int j = 0; j < NI; ++j)
+                        for (int j = 0; j < NI; ++j)
 #pragma unroll
-                        for (int c = 0; c < 4; ++c) {
-                            const int col = from + 32 * j + 8 * c + 4 * g;
-                            if (col >= cols) continue;
-                            f32x4* at = reinterpret_cast<f32x4*>(sum + (long)row * cols + col);
-                            f32x4 v = {acc[i][j][4 * c], acc[i][j][4 * c + 1], acc[i][j][4 * c + 2], acc[i][j][4 * c + 3]};
-                            if (add) v += *at;
-                            if (!out) *at = v;
-#pragma unroll
-                            for (int e = 0; e < 4; ++e) acc[i][j][4 * c + e] = v[e];
-                        }
-                }
-                if (out)
-                    loss_store<NI, E>(stage, out + (long)m0 * cols + from, cols, rows - m0, min(cols - from, NI * 32), lane,
+                            for (int c = 0; c < 4; ++c) {
+                                const int col = from + 32 * j + 8 * c + 4 * g;
+                                if (col >= cols) continue;
+                                f32x4* at = reinterpret_cast<f32x4*>(p.sum + ((long)split * p.rows + row) * cols + col);
+                                f32x4 v = {acc[i][j][4 * c], acc[i][j][4 * c + 1], acc[i][j][4 * c + 2], acc[i][j][4 * c + 3]};
+                                if (p.add) v += *at;
+                                *at = v;
+                            }
+                    }
+                } else {
+                    loss_store<NI, E>(stage, p.out + (long)m0 * cols + from, cols, p.rows - m0, min(cols - from, NI * 32), lane,
                                       [&](int j, int e) { return acc[i][j][e] * mul; });
+                }
             }
         });
+}
+template <int TA, int TB, int WA, int WB, typename E>
+__global__ void __launch_bounds__(WA* WB * 64, 2)
+avion_loss_grad_kernel(LossGrad dx, LossGrad dw, const float* __restrict__ factors, int items_x)
+{
+    extern __shared__ __attribute__((aligned(16))) char smem[];
+    const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), groups = gridDim.x;
+    // an XCD's workgroups (they go round) take neighbouring tiles
+    const int id = groups % 8 == 0 ? (int)(blockIdx.x % 8) * (groups / 8) + blockIdx.x / 8 : blockIdx.x;
+    const float mul = factors[0];
+    loss_grad<LossCfg<Along::kIndex, Along::kK, TA, TB, WA, WB>, E>(smem, dx, mul, id < items_x ? id : items_x, groups, wave, lane);
+    // dw's tiles follow dx's in the same round
+    const int taken = items_x % groups, start = id >= taken ? id - taken : id - taken + groups;
+    loss_grad<LossCfg<Along::kIndex, Along::kIndex, TA, TB, WA, WB>, E>(smem, dw, mul, start, groups, wave, lane);
+}
+
+// The planes' sum, in their order, times factors[0]
+template <typename E>
+__global__ void __launch_bounds__(256)
+avion_loss_sum_kernel(const float* __restrict__ sum, int planes, long n, const float* __restrict__ factors, raw16* __restrict__ out)
+{
+    const float mul = factors[0];
+    for (long i = (blockIdx.x * 256L + threadIdx.x) * 4; i < n; i += gridDim.x * 1024L) {
+        f32x4 t = *reinterpret_cast<const f32x4*>(sum + i);
+        for (int p = 1; p < planes; ++p) t += *reinterpret_cast<const f32x4*>(sum + p * n + i);
+        *reinterpret_cast<u32x2*>(out + i) = u32x2{E::pack(t[0] * mul, t[1] * mul), E::pack(t[2] * mul, t[3] * mul)};
+    }
 }

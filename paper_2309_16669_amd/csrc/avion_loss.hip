@@ -71,13 +71,31 @@ long long loss_piece(const LossShape& s)
     return std::min<long long>(most, ceil_div(ceil_div(s.V, pieces), 256) * 256);
 }
 long long loss_ld(const LossShape& s) { return std::min(loss_piece(s), ceil_div(s.V, 64) * 64); }
+// The two gradients' tiles: 256 x 256 where both together have one for each compute unit, else 128 x 128 cut along K until they fill
+// the chip twice over (at least 4 steps a range).
+bool grads_large(const LossShape& s, long long n)
+{
+    return (ceil_div(s.T, 256) + ceil_div(n, 256)) * ceil_div(s.D, 256) >= kComputeUnits;
+}
+int grad_splits(const LossShape& s, long long n, bool dw)
+{
+    if (grads_large(s, n)) return 1;
+    const long long tiles = ceil_div(dw ? n : s.T, 128) * ceil_div(s.D, 128), steps = ceil_div(dw ? s.T : n, kLossStep);
+    return (int)std::max<long long>(1, std::min<long long>(2 * kComputeUnits / std::max<long long>(1, tiles), steps / 4));
+}
 struct LossBackward {
-    size_t dz, sum, bytes;
+    size_t dz, sum_x, sum_w, bytes;
+    bool planes_x, planes_w;
     LossBackward(const LossShape& s)
     {
+        const long long n = loss_piece(s);
+        const int sx = grad_splits(s, n, false), sw = grad_splits(s, n, true);
+        planes_x = n < s.V || sx > 1;
+        planes_w = sw > 1;
         dz = 256;
-        sum = dz + round256((size_t)s.T * loss_ld(s) * 2);
-        bytes = sum + (loss_piece(s) >= s.V ? 0 : round256((size_t)s.T * s.D * 4));
+        sum_x = dz + round256((size_t)s.T * loss_ld(s) * 2);
+        sum_w = sum_x + (planes_x ? round256((size_t)sx * s.T * s.D * 4) : 0);
+        bytes = sum_w + (planes_w ? round256((size_t)sw * std::min(n, s.V) * s.D * 4) : 0);
     }
 };
 
@@ -202,7 +220,6 @@ int avion_linear_ce_bwd(const void* x, const void* w, const void* targets, const
     char* ws = static_cast<char*>(workspace);
     float* factors = reinterpret_cast<float*>(ws);
     raw16* dz = reinterpret_cast<raw16*>(ws + at.dz);
-    float* sum = reinterpret_cast<float*>(ws + at.sum);
     const long long piece = loss_piece(s), ld = loss_ld(s);
     return by_element(flags, [&](auto fmt) {
         using E = typename decltype(fmt)::type;
@@ -221,31 +238,37 @@ int avion_linear_ce_bwd(const void* x, const void* w, const void* targets, const
                                   persistent(ceil_div(T, TB) * ceil_div(n, X::TA), TB), Cfg::NT, st, "launch avion_loss_dz_kernel", a, lse, dloss,
                                   (const float*)factors, each, (int)v0, (int)n, dz, (long)ld);
                 });
-            if (rc2 == AVION_OK && dx && T > 0)
-                rc2 = by_tiles(loss_tiles(T, D), [&](auto tb) {
-                    constexpr int TB = decltype(tb)::value;
-                    using X = Tile<TB>;
-                    using Cfg = LossCfg<Along::kIndex, Along::kK, X::TA, TB, X::WA, X::WB>;
-                    static std::atomic<unsigned long long> allowed{0};
-                    const LossOperand opa{a.w + v0 * rs_w, (long)rs_w, D, (int)n}, opb{dz, (long)ld, (int)T, 0};
-                    const bool last = v0 + n >= V;
-                    return launch(avion_loss_grad_kernel<Along::kK, X::TA, TB, X::WA, X::WB, E>, Cfg::LDS_BYTES, allowed,
-                                  persistent(ceil_div(T, TB) * ceil_div(D, X::TA), TB), Cfg::NT, st, "launch avion_loss_grad_kernel (dx)", opa, opb,
-                                  (int)T, (int)held, (const float*)factors, piece >= V ? (float*)nullptr : sum, v0 > 0,
-                                  last ? static_cast<raw16*>(dx) : (raw16*)nullptr);
-                });
-            if (rc2 == AVION_OK && dw)
-                rc2 = by_tiles(std::max(LossTiles::kSmall, loss_tiles(n, D)), [&](auto tb) {
-                    constexpr int TB = decltype(tb)::value < 128 ? 128 : decltype(tb)::value;
-                    using X = Tile<TB>;
-                    using Cfg = LossCfg<Along::kIndex, Along::kIndex, X::TA, TB, X::WA, X::WB>;
-                    static std::atomic<unsigned long long> allowed{0};
-                    const LossOperand opa{a.x, (long)rs_x, D, (int)T}, opb{dz, (long)ld, (int)held, (int)T};
-                    return launch(avion_loss_grad_kernel<Along::kIndex, X::TA, TB, X::WA, X::WB, E>, Cfg::LDS_BYTES, allowed,
-                                  persistent(ceil_div(n, TB) * ceil_div(D, X::TA), TB), Cfg::NT, st, "launch avion_loss_grad_kernel (dw)", opa, opb,
-                                  (int)n, (int)std::max<long long>(1, T), (const float*)factors, (float*)nullptr, false,
-                                  static_cast<raw16*>(dw) + v0 * D);
-                });
+            if (rc2 != AVION_OK) break;
+            // (the last piece may be smaller; all use the first one's way)
+            const bool last = v0 + n >= V;
+            LossGrad gx{{a.w + v0 * rs_w, (long)rs_w, D, (int)n}, {dz, (long)ld, (int)T, 0}, (int)T, (int)held, grad_splits(s, piece, false),
+                        reinterpret_cast<float*>(ws + at.sum_x), v0 > 0, at.planes_x ? nullptr : static_cast<raw16*>(dx)};
+            LossGrad gw{{a.x, (long)rs_x, D, (int)T}, {dz, (long)ld, (int)held, (int)T}, (int)n, (int)std::max<long long>(1, T),
+                        grad_splits(s, piece, true), reinterpret_cast<float*>(ws + at.sum_w), 0,
+                        at.planes_w ? nullptr : static_cast<raw16*>(dw) + v0 * D};
+            // (a smaller last piece may have fewer steps than planes: the others keep what they have)
+            gx.splits = (int)std::min<long long>(gx.splits, ceil_div(held, kLossStep));
+            if (!dx || T == 0) gx.rows = 0;
+            if (!dw) gw.rows = 0;
+            const auto run = [&](auto tb) {
+                constexpr int TB = decltype(tb)::value;
+                using X = Tile<TB>;
+                using Cfg = LossCfg<Along::kIndex, Along::kIndex, X::TA, TB, X::WA, X::WB>;
+                static std::atomic<unsigned long long> allowed{0};
+                const long long items_x = ceil_div(gx.rows, TB) * ceil_div(D, X::TA) * gx.splits;
+                const long long items_w = ceil_div(gw.rows, TB) * ceil_div(D, X::TA) * gw.splits;
+                return launch(avion_loss_grad_kernel<X::TA, TB, X::WA, X::WB, E>, Cfg::LDS_BYTES, allowed, persistent(items_x + items_w, TB),
+                              Cfg::NT, st, "launch avion_loss_grad_kernel", gx, gw, (const float*)factors, (int)items_x);
+            };
+            if (gx.rows > 0 || gw.rows > 0)
+                rc2 = grads_large(s, piece) ? run(std::integral_constant<int, 256>{}) : run(std::integral_constant<int, 128>{});
+            const auto finish = [&](const LossGrad& g, int planes, void* to) {
+                const long long count = (long long)g.rows * D;
+                return launch(avion_loss_sum_kernel<E>, 0, none, std::min<long long>(2048, ceil_div(count, 1024)), 256, st,
+                              "launch avion_loss_sum_kernel", (const float*)g.sum, planes, (long)count, (const float*)factors, static_cast<raw16*>(to));
+            };
+            if (rc2 == AVION_OK && at.planes_x && last && gx.rows > 0) rc2 = finish(gx, grad_splits(s, piece, false), dx);
+            if (rc2 == AVION_OK && at.planes_w && gw.rows > 0) rc2 = finish(gw, gw.splits, static_cast<raw16*>(dw) + v0 * D);
         }
         return rc2;
     });
