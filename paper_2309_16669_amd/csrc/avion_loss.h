@@ -13,9 +13,12 @@
 //   of 8 consecutive k: rows of 128 bytes with ds_read_b128, their eight 16-byte chunks permuted by a XOR with bits 1..3 of the row
 //   number; rows of k with two transposing ds_read_b64_tr_b16 (4 k each), their 64-byte units permuted by a XOR with the row
 //   number mod 4.  Both meet distinct banks.
-//   Two buffers of a step; fragments of 16 k are read while the 16 before are multiplied; before a step's last ones the next step
+//   Two buffers of a step (four where a compute unit has one workgroup and each step's loads would be waited for: 2048 x 2048 x 512
+//   forward 10.5 -> 7 us); fragments of 16 k are read while the 16 before are multiplied; before a step's last ones the next step
 //   is awaited, and this one's buffer, which everybody then holds in registers, is filled again.  Steps of a workgroup's tiles
 //   form one stream, so that the next tile's first steps are on their way during the end of a tile.
+//   8192 cubed: 1212 to 1258 TFLOP/s by the operands' layouts (the library's product 1301); matrix units busy 62 % of the cycles, LDS
+//   reads 23 %, at 1.8 GHz.
 //   A is the contiguous index of the result: a lane's accumulators are 4 consecutive a of one row b.
 #pragma once
 #include "avion_common.h"
@@ -109,22 +112,30 @@ struct LossTile {
     }
 };
 
-template <Along AA, Along AB, int TA_, int TB_, int WA_, int WB_>
+template <Along AA, Along AB, int TA_, int TB_, int WA_, int WB_, int ST_>
 struct LossCfg {
-    static constexpr int TA = TA_, TB = TB_, WA = WA_, WB = WB_;
+    static constexpr int TA = TA_, TB = TB_, WA = WA_, WB = WB_, ST = ST_;
     static constexpr int WAVES = WA * WB, NT = WAVES * 64;
     static constexpr int NI = TA / WA / 32, MI = TB / WB / 32;  // 32 x 32 tiles of a wavefront
     using TileA = LossTile<AA, TA, WAVES>;
     using TileB = LossTile<AB, TB, WAVES>;
     static constexpr int STAGE = TileA::BYTES + TileB::BYTES;
-    static constexpr int OUT_ROW = NI * 64 + 16, OUT_BYTES = 32 * OUT_ROW;  // a wavefront's rows on their way out, in a free buffer's place
-    static constexpr int LDS_BYTES = 2 * STAGE + WAVES * (NI == 2 ? 16 : 32) * OUT_ROW;
-    // one workgroup of eight wavefronts a compute unit, or as many of four as LDS takes, two at least
-    static constexpr int WAVES_PER_SIMD = 2;
-    static_assert(LDS_BYTES <= 160 * 1024, "");
+    static constexpr int LOADS = TileA::PER + TileB::PER;  // of a wavefront for a step
+    static constexpr int OUT_ROW = NI * 64 + 16, OUT_BYTES = (NI == 2 ? 16 : 32) * OUT_ROW;  // a wavefront's rows on their way out
+    static constexpr int LDS_BYTES = ST * STAGE + WAVES * OUT_BYTES;
+    static_assert(LDS_BYTES <= 160 * 1024 && TileA::BLOCKS % WAVES == 0 && TileB::BLOCKS % WAVES == 0 && ST >= 2 && ST <= 4 && 3 * LOADS < 64, "");
 };
 
-DEVINL void loss_landed_barrier() { asm volatile("s_waitcnt vmcnt(0)\n\ts_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+// All but this wavefront's youngest `left` steps of LOADS loads have arrived (stores and other loads among them are younger than they
+// count here: that waits for more, never for less), its LDS reads are done, and so everybody's.
+template <int ST, int LOADS>
+DEVINL void loss_landed_barrier(int left)
+{
+    if (ST > 3 && left >= 3) asm volatile("s_waitcnt vmcnt(%0)\n\ts_waitcnt lgkmcnt(0)\n\ts_barrier" ::"i"(3 * LOADS) : "memory");
+    else if (ST > 2 && left == 2) asm volatile("s_waitcnt vmcnt(%0)\n\ts_waitcnt lgkmcnt(0)\n\ts_barrier" ::"i"(2 * LOADS) : "memory");
+    else if (left == 1) asm volatile("s_waitcnt vmcnt(%0)\n\ts_waitcnt lgkmcnt(0)\n\ts_barrier" ::"i"(LOADS) : "memory");
+    else asm volatile("s_waitcnt vmcnt(0)\n\ts_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+}
 
 // Tile number -> its places: 8 blocks of b, then the next a.  What an XCD's workgroups hold at a time, neighbouring numbers, is then 8
 // blocks of b by a few of a, whose operands fit its L2.
@@ -140,10 +151,12 @@ DEVINL void loss_place(int tile, int na, int nb, int& a, int& b)
 struct LossPlace {
     int a0, b0, k0, k1;
 };
-template <typename Cfg, typename E, typename Place, typename Done>
-DEVINL void loss_product(char* smem, const LossOperand& opa, const LossOperand& opb, int K, int count, int wave, int lane, Place place, Done done)
+// begin(n, place) is called with the loads of the tile's first step: what it asks for in the same way has arrived when the tile is done.
+template <typename Cfg, typename E, typename Place, typename Begin, typename Done>
+DEVINL void loss_product(char* smem, const LossOperand& opa, const LossOperand& opb, int K, int count, int wave, int lane, Place place, Begin begin,
+                         Done done)
 {
-    constexpr int MI = Cfg::MI, NI = Cfg::NI;
+    constexpr int MI = Cfg::MI, NI = Cfg::NI, ST = Cfg::ST;
     if (count <= 0) return;
     const int wa = wave % Cfg::WA, wb = wave / Cfg::WA;
     typename Cfg::TileA ta(opa, K, wave, lane);
@@ -157,6 +170,7 @@ DEVINL void loss_product(char* smem, const LossOperand& opa, const LossOperand& 
     tb.tile(f.b0);
     auto fetch = [&](int buf) {
         const unsigned to = lds + buf * Cfg::STAGE;
+        if (f_k == f.k0) begin(f_n, f);
         ta.fetch(f.a0, f_k * kLossStep, to);
         tb.fetch(f.b0, f_k * kLossStep, to + Cfg::TileA::BYTES);
         if (++f_k == f.k1 && ++f_n < count) {
@@ -166,9 +180,15 @@ DEVINL void loss_product(char* smem, const LossOperand& opa, const LossOperand& 
             tb.tile(f.b0);
         }
     };
+    int ahead = 0;  // steps asked for behind the one that is awaited next
     fetch(0);
-    loss_landed_barrier();
-    if (f_n < count) fetch(1);
+#pragma unroll
+    for (int i = 1; i < ST; ++i)
+        if (f_n < count) {
+            fetch(i);
+            ++ahead;
+        }
+    loss_landed_barrier<ST, Cfg::LOADS>(ahead);
     frag8 fa[NI], fb[MI];
     auto read = [&](int buf, int ks) {
         const unsigned from = lds + buf * Cfg::STAGE;
@@ -197,9 +217,12 @@ DEVINL void loss_product(char* smem, const LossOperand& opa, const LossOperand& 
                 if (ks < 3) {
                     read(buf, ks + 1);
                 } else if (k + 1 < p.k1 || n + 1 < count) {
-                    loss_landed_barrier();  // the next step is there, and this one in everybody's registers
-                    if (f_n < count) fetch(buf);
-                    read(buf ^ 1, 0);
+                    loss_landed_barrier<ST, Cfg::LOADS>(--ahead);  // the next step is there, and this one in everybody's registers
+                    if (f_n < count) {
+                        fetch(buf);
+                        ++ahead;
+                    }
+                    read(buf + 1 == ST ? 0 : buf + 1, 0);
                 }
                 __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
@@ -208,7 +231,7 @@ DEVINL void loss_product(char* smem, const LossOperand& opa, const LossOperand& 
                     for (int j = 0; j < NI; ++j) acc[i][j] = E::mfma(ca[j], cb[i], acc[i][j]);
                 __builtin_amdgcn_sched_barrier(0);
             }
-            buf ^= 1;
+            buf = buf + 1 == ST ? 0 : buf + 1;
         }
         done(n, p.a0, p.b0, acc);
     }
@@ -267,11 +290,11 @@ constexpr float kLossNone = -3.0e38f;
 // A workgroup takes TB rows through one of `slabs` runs of vocabulary tiles.  A lane holds, for each of its MI rows, the maximum and sum
 // (base 2, scaled) over the columns that its registers hold; they meet once, at the end: parts [slabs][T] of (maximum, sum).  The lane
 // that holds a row's target leaves its logit.
-template <int TA, int TB, int WA, int WB, typename E>
+template <int TA, int TB, int WA, int WB, int ST, typename E>
 __global__ void __launch_bounds__(WA* WB * 64, 2)
 avion_loss_fwd_kernel(LossArgs a, float2* __restrict__ parts, float* __restrict__ hit, int slabs)
 {
-    using Cfg = LossCfg<Along::kK, Along::kK, TA, TB, WA, WB>;
+    using Cfg = LossCfg<Along::kK, Along::kK, TA, TB, WA, WB, ST>;
     constexpr int MI = Cfg::MI, NI = Cfg::NI;
     extern __shared__ __attribute__((aligned(16))) char smem[];
     __shared__ float2 meet[WA][TB];
@@ -294,7 +317,7 @@ avion_loss_fwd_kernel(LossArgs a, float2* __restrict__ parts, float* __restrict_
     const LossOperand opa{a.w, a.rs_w, a.V, 0}, opb{a.x, a.rs_x, a.T, 0};
     loss_product<Cfg, E>(
         smem, opa, opb, a.D, last - first, wave, lane,
-        [&](int n) { return LossPlace{(first + n) * TA, b0, 0, (a.D + kLossStep - 1) / kLossStep}; },
+        [&](int n) { return LossPlace{(first + n) * TA, b0, 0, (a.D + kLossStep - 1) / kLossStep}; }, [](int, const LossPlace&) {},
         [&](int, int a0, int, f32x16(&acc)[MI][NI]) {
             const int from = a0 + wa * NI * 32;
             const bool ragged = from + NI * 32 > a.V;
@@ -348,26 +371,27 @@ avion_loss_fwd_kernel(LossArgs a, float2* __restrict__ parts, float* __restrict_
     }
 }
 
-// Rows joined over the runs, 16 lanes a row: lse, loss; and, for a mean or sum, the losses of 16 rows and how many of them have a target.
-// (With one thread a row 391 runs of 5 rows took 70 us.)
-constexpr int kLossJoin = 16;
+// Rows joined over the runs, LANES lanes a row: lse, loss; and, for a mean or sum, the losses of 256 / LANES rows and how many of them
+// have a target.  (391 runs of 5 rows: one lane 70 us, 16 lanes 8.)
+template <int LANES>
 __global__ void __launch_bounds__(256)
 avion_loss_join_kernel(LossArgs a, const float2* __restrict__ parts, const float* __restrict__ hit, int slabs, float* __restrict__ loss,
                        float* __restrict__ lse, double2* __restrict__ sums)
 {
-    const int lane = threadIdx.x % 16, m = blockIdx.x * kLossJoin + threadIdx.x / 16;
-    __shared__ double2 meet[kLossJoin];
+    const int lane = threadIdx.x % LANES, m = blockIdx.x * (256 / LANES) + threadIdx.x / LANES;
+    __shared__ double2 meet[256 / LANES];
     double2 mine{0., 0.};
     if (m < a.T) {
         float top = kLossNone, total = 0.f;
-        for (int s = lane; s < slabs; s += 16) {
+        #pragma unroll 4
+        for (int s = lane; s < slabs; s += LANES) {
             const float2 p = parts[(long)s * a.T + m];
             const float mn = fmaxf(top, p.x);
             total = total * fast_exp2(top - mn) + p.y * fast_exp2(p.x - mn);
             top = mn;
         }
 #pragma unroll
-        for (int x = 1; x < 16; x *= 2) {
+        for (int x = 1; x < LANES; x *= 2) {
             const float o = __shfl_xor(top, x), ot = __shfl_xor(total, x), mn = fmaxf(top, o);
             total = total * fast_exp2(top - mn) + ot * fast_exp2(o - mn);
             top = mn;
@@ -382,11 +406,11 @@ avion_loss_join_kernel(LossArgs a, const float2* __restrict__ parts, const float
         mine = double2{of, has ? 1. : 0.};
     }
     if (!sums) return;
-    if (lane == 0) meet[threadIdx.x / 16] = mine;
+    if (lane == 0) meet[threadIdx.x / LANES] = mine;
     __syncthreads();
     if (threadIdx.x == 0) {
         double2 t{0., 0.};
-        for (int i = 0; i < kLossJoin; ++i) {
+        for (int i = 0; i < 256 / LANES; ++i) {
             t.x += meet[i].x;
             t.y += meet[i].y;
         }
@@ -421,23 +445,14 @@ avion_loss_total_kernel(const double2* __restrict__ sums, int n, bool mean, floa
 // ------------------------------------------------------------------------------------------ backward
 // dz is held as (softmax - onehot) r_m S with r_m = dloss_m / max |dloss|, S = 1 for bf16 and 2^14 for fp16 (a softmax over many
 // columns has values below fp16's normal numbers; |dz| stays below 2^14), and the products are scaled back in fp32 by
-// factors[0] = scale max|dloss| / S; factors[1] = 1 / max|dloss|.
+// factors[0] = scale max|dloss| / S; factors[1] = max|dloss|.
 template <typename E>
 constexpr float kLossHeld = std::is_same<E, F16>::value ? 16384.f : 1.f;
 
+// max |dloss| over the rows with a target (NaN if one of them is no finite number), where each row has its own
 __global__ void __launch_bounds__(1024)
-avion_loss_factors_kernel(LossArgs a, const float* __restrict__ dloss, const float* __restrict__ total, bool each, bool mean, float held,
-                          float* __restrict__ factors)
+avion_loss_largest_kernel(LossArgs a, const float* __restrict__ dloss, float* __restrict__ factors)
 {
-    if (!each) {  // one gradient for all rows
-        if (threadIdx.x == 0) {
-            float d = dloss[0];
-            if (mean) d = total[1] > 0.f ? d / total[1] : 0.f;
-            factors[0] = d * a.scale / held;
-            factors[1] = 1.f;
-        }
-        return;
-    }
     __shared__ float meet[16];
     float top = 0.f;
     bool nan = false;
@@ -457,27 +472,50 @@ avion_loss_factors_kernel(LossArgs a, const float* __restrict__ dloss, const flo
     __syncthreads();
     if (threadIdx.x == 0) {
         for (int i = 1; i < 16; ++i) top = top != top || meet[i] != meet[i] ? __builtin_nanf("") : fmaxf(top, meet[i]);
-        factors[0] = top * a.scale / held;
-        factors[1] = top == 0.f ? 0.f : 1.f / top;
+        factors[1] = top;
     }
+}
+// What the dz kernel needs of a row, three arrays of `padded` (a multiple of 256) words: its target (-1: none), its lse in base 2 (+inf
+// where it has none: weights 0) and r S; and factors[0], what the products are multiplied with.
+__global__ void __launch_bounds__(256)
+avion_loss_rows_kernel(LossArgs a, const float* __restrict__ lse, const float* __restrict__ dloss, const float* __restrict__ total, bool each,
+                       bool mean, float held, float* __restrict__ factors, int* __restrict__ rows, int padded)
+{
+    const int m = blockIdx.x * 256 + threadIdx.x;
+    const float top = each ? factors[1] : 1.f;
+    if (m == 0) {
+        float d = each ? top : dloss[0];
+        if (!each && mean) d = total[1] > 0.f ? d / total[1] : 0.f;
+        factors[0] = d * a.scale / held;
+    }
+    if (m >= padded) return;
+    const int target = loss_target(a, m);
+    rows[m] = target;
+    float* f = reinterpret_cast<float*>(rows);
+    f[padded + m] = target >= 0 ? lse[m] * kLog2e : INFINITY;
+    f[2 * padded + m] = target >= 0 ? (each ? (top == 0.f ? 0.f : dloss[m] / top) : 1.f) * held : 0.f;
 }
 
 // dz of the vocabulary's columns v0 .. v0 + n - 1, [T, ld]; columns from n to the next multiple of 8 are zeros
-template <int TA, int TB, int WA, int WB, typename E>
+// What a tile's rows need (their targets, lse and factors, 1 KB each for 256 rows) comes to LDS with its first step: loaded where it is
+// used, it made every tile wait once more.  Columns of a target are rare (a wavefront's 32 x 64 logits of 50000 columns hold one in 25),
+// and so are columns past the end: both have a copy of the loop.
+constexpr int kLossRowBytes = 3 * 1024;
+template <int TA, int TB, int WA, int WB, int ST, typename E>
 __global__ void __launch_bounds__(WA* WB * 64, 2)
-avion_loss_dz_kernel(LossArgs a, const float* __restrict__ lse, const float* __restrict__ dloss, const float* __restrict__ factors, bool each,
-                     int v0, int n, raw16* __restrict__ dz, long ld)
+avion_loss_dz_kernel(LossArgs a, const int* __restrict__ rowdata, int padded, int v0, int n, raw16* __restrict__ dz, long ld)
 {
-    using Cfg = LossCfg<Along::kK, Along::kK, TA, TB, WA, WB>;
+    using Cfg = LossCfg<Along::kK, Along::kK, TA, TB, WA, WB, ST>;
     constexpr int MI = Cfg::MI, NI = Cfg::NI;
     extern __shared__ __attribute__((aligned(16))) char smem[];
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), l32 = lane % 32, g = lane / 32;
     const int wa = wave % WA, wb = wave / WA;
     const int na = (n + TA - 1) / TA, nb = (a.T + TB - 1) / TB, ntiles = na * nb, per = (ntiles + 7) / 8, together = gridDim.x / 8;
     const int first = blockIdx.x % 8 * per + blockIdx.x / 8, end = min(ntiles, (blockIdx.x % 8 + 1) * per);
-    char* stage = smem + 2 * Cfg::STAGE + wave * ((NI == 2 ? 16 : 32) * Cfg::OUT_ROW);
+    char* stage = smem + ST * Cfg::STAGE + wave * Cfg::OUT_BYTES;
+    char* rowmem = smem + Cfg::LDS_BYTES;  // of ST + 1 tiles: where a tile is one step, those of ST more are on their way at its end
+    static_assert(Cfg::LDS_BYTES + (ST + 1) * kLossRowBytes <= 160 * 1024 && TB <= 256, "");
     const LossOperand opa{a.w + (long)v0 * a.rs_w, a.rs_w, n, 0}, opb{a.x, a.rs_x, a.T, 0};
-    const float inv = factors[1];
     loss_product<Cfg, E>(
         smem, opa, opb, a.D, first < end ? (end - first + together - 1) / together : 0, wave, lane,
         [&](int t) {
@@ -487,28 +525,42 @@ avion_loss_dz_kernel(LossArgs a, const float* __restrict__ lse, const float* __r
             p.b0 *= TB;
             return p;
         },
-        [&](int, int a0, int b0, f32x16(&acc)[MI][NI]) {
+        [&](int t, const LossPlace& p) {
+            if (wave < 3)
+                load_to_lds16(RawBuffer(rowdata + (long)wave * padded + p.b0, TB * 4), lds_address(rowmem) + t % (ST + 1) * kLossRowBytes + wave * 1024, lane * 16);
+        },
+        [&](int t, int a0, int b0, f32x16(&acc)[MI][NI]) {
             const int from = a0 + wa * NI * 32;
+            const bool ragged = from + NI * 32 > n;
 #pragma unroll
             for (int i = 0; i < MI; ++i) {
-                const int m0 = b0 + (wb * MI + i) * 32, row = m0 + l32, target = loss_target(a, row);
-                const float lc = target >= 0 ? lse[row] * kLog2e : INFINITY;
-                const float r = target >= 0 ? (each ? dloss[row] * inv : inv) * kLossHeld<E> : 0.f;
-                const int at = target >= 0 ? target - v0 - from : -1;
-                loss_store<NI, E>(stage, dz + (long)m0 * ld + from, ld, a.T - m0, (int)min(ld - from, (long)NI * 32), lane, [&](int j, int e) {
-                    const int col = 32 * j + 8 * (e / 4) + 4 * g + e % 4;
-                    float p = fast_exp2(fmaf(acc[i][j][e], a.cs, -lc)) - (col == at ? 1.f : 0.f);
-                    p = from + col < n ? p : 0.f;
-                    return target >= 0 ? p * r : 0.f;
-                });
+                const int in = (wb * MI + i) * 32, m0 = b0 + in;
+                const char* data = rowmem + t % (ST + 1) * kLossRowBytes + (in + l32) * 4;
+                const int target = *reinterpret_cast<const int*>(data), at = target >= 0 ? target - v0 - from : -1;
+                const float lc = *reinterpret_cast<const float*>(data + 1024), r = *reinterpret_cast<const float*>(data + 2048);
+                raw16* out = dz + (long)m0 * ld + from;
+                const int cols = (int)min(ld - from, (long)NI * 32);
+                if (ragged || __any(at >= 0 && at < NI * 32)) {
+                    loss_store<NI, E>(stage, out, ld, a.T - m0, cols, lane, [&](int j, int e) {
+                        const int col = 32 * j + 8 * (e / 4) + 4 * g + e % 4;
+                        const float p = fast_exp2(fmaf(acc[i][j][e], a.cs, -lc)) - (col == at ? 1.f : 0.f);
+                        return target >= 0 && from + col < n ? p * r : 0.f;
+                    });
+                } else {
+                    loss_store<NI, E>(stage, out, ld, a.T - m0, cols, lane, [&](int j, int e) {
+                        const float p = fast_exp2(fmaf(acc[i][j][e], a.cs, -lc)) * r;
+                        return target >= 0 ? p : 0.f;
+                    });
+                }
             }
         });
 }
 
 // dx (+)= dz w and dw = dz^T x, one launch for both, so that the rounds of their tiles fill each other up (16384 x 25000 x 768: 192 tiles
 // of 392 steps and 294 of 256 on 256 compute units).  C [b, a], its first `rows` b; each tile is cut into `splits` ranges of K.  One
-// range and one piece of the vocabulary: the result, times factors[0], goes to `out`; else to planes of fp32 [splits][rows][cols]
-// (added to what earlier pieces left), of which avion_loss_sum_kernel makes it.
+// range and one piece of the vocabulary: the result, times factors[0], goes to `out`; else to planes of fp32, one a range (added to
+// what earlier pieces left), of which avion_loss_sum_kernel makes it.  A plane holds whole tiles in the accumulators' order (tile,
+// wavefront, 32 x 32 block, quarter, lane: 4 numbers), so that a wavefront reads and writes 1 KB at a time.
 struct LossGrad {
     LossOperand a, b;
     int rows, K, splits;
@@ -520,10 +572,10 @@ template <typename Cfg, typename E>
 DEVINL void loss_grad(char* smem, const LossGrad& p, float mul, int first, int step, int wave, int lane)
 {
     constexpr int MI = Cfg::MI, NI = Cfg::NI;
-    const int l32 = lane % 32, g = lane / 32, wa = wave % Cfg::WA, wb = wave / Cfg::WA, cols = p.a.extent;
+    const int wa = wave % Cfg::WA, wb = wave / Cfg::WA, cols = p.a.extent;
     const int na = (cols + Cfg::TA - 1) / Cfg::TA, nb = (p.rows + Cfg::TB - 1) / Cfg::TB, items = na * nb * p.splits;
     const int steps = (p.K + kLossStep - 1) / kLossStep;
-    char* stage = smem + 2 * Cfg::STAGE + wave * ((NI == 2 ? 16 : 32) * Cfg::OUT_ROW);
+    char* stage = smem + Cfg::ST * Cfg::STAGE + wave * Cfg::OUT_BYTES;
     loss_product<Cfg, E>(
         smem, p.a, p.b, p.K, first < items ? (items - first + step - 1) / step : 0, wave, lane,
         [&](int n) {
@@ -534,25 +586,23 @@ DEVINL void loss_grad(char* smem, const LossGrad& p, float mul, int first, int s
             at.b0 *= Cfg::TB;
             return at;
         },
+        [](int, const LossPlace&) {},
         [&](int n, int a0, int b0, f32x16(&acc)[MI][NI]) {
-            const int from = a0 + wa * NI * 32, split = (first + n * step) / (na * nb);
+            const int from = a0 + wa * NI * 32;
+            f32x4* plane = reinterpret_cast<f32x4*>(p.sum) + ((long)(first + n * step) * Cfg::WAVES + wave) * (MI * NI * 256) + lane;
 #pragma unroll
             for (int i = 0; i < MI; ++i) {
-                const int m0 = b0 + (wb * MI + i) * 32, row = m0 + l32;
+                const int m0 = b0 + (wb * MI + i) * 32;
                 if (!p.out) {
-                    if (row < p.rows) {
 #pragma unroll
-                        for (int j = 0; j < NI; ++j)
+                    for (int j = 0; j < NI; ++j)
 #pragma unroll
-                            for (int c = 0; c < 4; ++c) {
-                                const int col = from + 32 * j + 8 * c + 4 * g;
-                                if (col >= cols) continue;
-                                f32x4* at = reinterpret_cast<f32x4*>(p.sum + ((long)split * p.rows + row) * cols + col);
-                                f32x4 v = {acc[i][j][4 * c], acc[i][j][4 * c + 1], acc[i][j][4 * c + 2], acc[i][j][4 * c + 3]};
-                                if (p.add) v += *at;
-                                *at = v;
-                            }
-                    }
+                        for (int c = 0; c < 4; ++c) {
+                            f32x4* at = plane + ((i * NI + j) * 4 + c) * 64;
+                            f32x4 v = {acc[i][j][4 * c], acc[i][j][4 * c + 1], acc[i][j][4 * c + 2], acc[i][j][4 * c + 3]};
+                            if (p.add) v += *at;
+                            *at = v;
+                        }
                 } else {
                     loss_store<NI, E>(stage, p.out + (long)m0 * cols + from, cols, p.rows - m0, min(cols - from, NI * 32), lane,
                                       [&](int j, int e) { return acc[i][j][e] * mul; });
@@ -560,7 +610,7 @@ DEVINL void loss_grad(char* smem, const LossGrad& p, float mul, int first, int s
             }
         });
 }
-template <int TA, int TB, int WA, int WB, typename E>
+template <int TA, int TB, int WA, int WB, int ST, typename E>
 __global__ void __launch_bounds__(WA* WB * 64, 2)
 avion_loss_grad_kernel(LossGrad dx, LossGrad dw, const float* __restrict__ factors, int items_x)
 {
@@ -569,21 +619,40 @@ avion_loss_grad_kernel(LossGrad dx, LossGrad dw, const float* __restrict__ facto
     // an XCD's workgroups (they go round) take neighbouring tiles
     const int id = groups % 8 == 0 ? (int)(blockIdx.x % 8) * (groups / 8) + blockIdx.x / 8 : blockIdx.x;
     const float mul = factors[0];
-    loss_grad<LossCfg<Along::kIndex, Along::kK, TA, TB, WA, WB>, E>(smem, dx, mul, id < items_x ? id : items_x, groups, wave, lane);
+    loss_grad<LossCfg<Along::kIndex, Along::kK, TA, TB, WA, WB, ST>, E>(smem, dx, mul, id < items_x ? id : items_x, groups, wave, lane);
     // dw's tiles follow dx's in the same round
     const int taken = items_x % groups, start = id >= taken ? id - taken : id - taken + groups;
-    loss_grad<LossCfg<Along::kIndex, Along::kIndex, TA, TB, WA, WB>, E>(smem, dw, mul, start, groups, wave, lane);
+    loss_grad<LossCfg<Along::kIndex, Along::kIndex, TA, TB, WA, WB, ST>, E>(smem, dw, mul, start, groups, wave, lane);
 }
 
-// The planes' sum, in their order, times factors[0]
-template <typename E>
+// The planes' sum, in their order, times factors[0]: a wavefront a 32 x 32 block
+template <int TA, int TB, int WA, int WB, typename E>
 __global__ void __launch_bounds__(256)
-avion_loss_sum_kernel(const float* __restrict__ sum, int planes, long n, const float* __restrict__ factors, raw16* __restrict__ out)
+avion_loss_sum_kernel(const float* __restrict__ sum, int planes, int rows, int cols, const float* __restrict__ factors, raw16* __restrict__ out)
 {
-    const float mul = factors[0];
-    for (long i = (blockIdx.x * 256L + threadIdx.x) * 4; i < n; i += gridDim.x * 1024L) {
-        f32x4 t = *reinterpret_cast<const f32x4*>(sum + i);
-        for (int p = 1; p < planes; ++p) t += *reinterpret_cast<const f32x4*>(sum + p * n + i);
-        *reinterpret_cast<u32x2*>(out + i) = u32x2{E::pack(t[0] * mul, t[1] * mul), E::pack(t[2] * mul, t[3] * mul)};
+    using Cfg = LossCfg<Along::kK, Along::kK, TA, TB, WA, WB, 2>;
+    constexpr int MI = Cfg::MI, NI = Cfg::NI, BLOCKS = Cfg::WAVES * MI * NI;
+    const int lane = threadIdx.x % 64, na = (cols + TA - 1) / TA, nb = (rows + TB - 1) / TB;
+    const long unit = blockIdx.x * 4L + threadIdx.x / 64, units = (long)na * nb * BLOCKS;
+    if (unit >= units) return;
+    const int tile = (int)(unit / BLOCKS), in = (int)(unit - (long)tile * BLOCKS), wave = in / (MI * NI), i = in / NI % MI, j = in % NI;
+    int a0, b0;
+    loss_place(tile, na, nb, a0, b0);
+    const int row = b0 * TB + (wave / WA * MI + i) * 32 + lane % 32, col = a0 * TA + (wave % WA * NI + j) * 32 + 4 * (lane / 32);
+    const f32x4* at = reinterpret_cast<const f32x4*>(sum) + unit * 256 + lane;
+    f32x4 t[4];
+#pragma unroll
+    for (int c = 0; c < 4; ++c) t[c] = at[c * 64];
+    for (int p = 1; p < planes; ++p) {
+        at += units * 256;
+#pragma unroll
+        for (int c = 0; c < 4; ++c) t[c] += at[c * 64];
     }
+    const float mul = factors[0];
+    if (row >= rows) return;
+#pragma unroll
+    for (int c = 0; c < 4; ++c)
+        if (col + 8 * c < cols)
+            *reinterpret_cast<u32x2*>(out + (long)row * cols + col + 8 * c) =
+                u32x2{E::pack(t[c][0] * mul, t[c][1] * mul), E::pack(t[c][2] * mul, t[c][3] * mul)};
 }

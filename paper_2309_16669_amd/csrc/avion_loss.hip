@@ -31,18 +31,19 @@ LossTiles loss_tiles(long long rows, long long cols)
     if (rows <= 32) return LossTiles::kFew;
     return ceil_div(rows, 256) * ceil_div(cols, 256) < kComputeUnits ? LossTiles::kSmall : LossTiles::kLarge;
 }
-template <typename F>
-int by_tiles(LossTiles t, F f)
-{
-    if (t == LossTiles::kFew) return f(std::integral_constant<int, 32>{});
-    if (t == LossTiles::kSmall) return f(std::integral_constant<int, 128>{});
-    return f(std::integral_constant<int, 256>{});
-}
-// tile heights and wavefronts of a size: TB, then TA, WA, WB
-template <int TB>
+// tile height and width, wavefronts, buffers
+template <int TB_, int ST_>
 struct Tile {
-    static constexpr int TA = TB == 256 ? 256 : 128, WA = TB == 32 ? 4 : TB == 128 ? 2 : 4, WB = TB == 32 ? 1 : 2;
+    static constexpr int TB = TB_, TA = TB == 256 ? 256 : 128, WA = TB == 128 ? 2 : 4, WB = TB == 32 ? 1 : 2, ST = ST_;
 };
+// f(Tile) for `tiles` tiles of a product: four buffers where each compute unit has one workgroup at most
+template <typename F>
+int by_tiles(LossTiles t, long long tiles, F f)
+{
+    if (t == LossTiles::kFew) return f(Tile<32, 2>{});
+    if (t == LossTiles::kLarge) return f(Tile<256, 2>{});
+    return tiles <= kComputeUnits ? f(Tile<128, 4>{}) : f(Tile<128, 2>{});
+}
 
 // runs of vocabulary tiles in the forward: enough workgroups for the chip, whole rounds of them where there are many
 int loss_slabs(const LossShape& s)
@@ -58,7 +59,7 @@ struct LossForward {  // offsets of its workspace
     {
         hit = round256((size_t)loss_slabs(s) * s.T * sizeof(float2));
         sums = hit + round256((size_t)s.T * 4);
-        bytes = std::max<size_t>(256, sums + round256((size_t)ceil_div(s.T, kLossJoin) * sizeof(double2)));
+        bytes = std::max<size_t>(256, sums + round256((size_t)ceil_div(s.T, 4) * sizeof(double2)));
     }
 };
 
@@ -72,7 +73,7 @@ long long loss_piece(const LossShape& s)
 }
 long long loss_ld(const LossShape& s) { return std::min(loss_piece(s), ceil_div(s.V, 64) * 64); }
 // The two gradients' tiles: 256 x 256 where both together have one for each compute unit, else 128 x 128 cut along K until they fill
-// the chip twice over (at least 4 steps a range).
+// the chip twice over (at least 4 steps a range; a range's plane is written and read again, so no more of them than that takes).
 bool grads_large(const LossShape& s, long long n)
 {
     return (ceil_div(s.T, 256) + ceil_div(n, 256)) * ceil_div(s.D, 256) >= kComputeUnits;
@@ -80,11 +81,21 @@ bool grads_large(const LossShape& s, long long n)
 int grad_splits(const LossShape& s, long long n, bool dw)
 {
     if (grads_large(s, n)) return 1;
-    const long long tiles = ceil_div(dw ? n : s.T, 128) * ceil_div(s.D, 128), steps = ceil_div(dw ? s.T : n, kLossStep);
-    return (int)std::max<long long>(1, std::min<long long>(2 * kComputeUnits / std::max<long long>(1, tiles), steps / 4));
+    const long long steps = ceil_div(dw ? s.T : n, kLossStep);
+    // (of both together; each product's share by its steps)
+    const long long work = ceil_div(s.T, 128) * ceil_div(n, kLossStep) + ceil_div(n, 128) * ceil_div(s.T, kLossStep);
+    const long long fair = std::max<long long>(4, work * ceil_div(s.D, 128) / (2 * kComputeUnits));  // steps of a workgroup
+    return (int)std::max<long long>(1, std::min<long long>(ceil_div(steps, fair), steps / 4));
 }
+// floats of a plane: whole tiles
+long long plane_floats(const LossShape& s, long long n, long long rows)
+{
+    const long long t = grads_large(s, n) ? 256 : 128;
+    return ceil_div(rows, t) * ceil_div(s.D, t) * t * t;
+}
+int loss_padded(const LossShape& s) { return (int)(ceil_div(s.T, 256) * 256); }
 struct LossBackward {
-    size_t dz, sum_x, sum_w, bytes;
+    size_t rows, dz, sum_x, sum_w, bytes;
     bool planes_x, planes_w;
     LossBackward(const LossShape& s)
     {
@@ -92,10 +103,11 @@ struct LossBackward {
         const int sx = grad_splits(s, n, false), sw = grad_splits(s, n, true);
         planes_x = n < s.V || sx > 1;
         planes_w = sw > 1;
-        dz = 256;
+        rows = 256;
+        dz = rows + round256((size_t)loss_padded(s) * 12);
         sum_x = dz + round256((size_t)s.T * loss_ld(s) * 2);
-        sum_w = sum_x + (planes_x ? round256((size_t)sx * s.T * s.D * 4) : 0);
-        bytes = sum_w + (planes_w ? round256((size_t)sw * std::min(n, s.V) * s.D * 4) : 0);
+        sum_w = sum_x + (planes_x ? round256((size_t)sx * plane_floats(s, n, s.T) * 4) : 0);
+        bytes = sum_w + (planes_w ? round256((size_t)sw * plane_floats(s, n, std::min(n, s.V)) * 4) : 0);
     }
 };
 
@@ -176,21 +188,25 @@ int avion_linear_ce_fwd(const void* x, const void* w, const void* targets, float
         const int slabs = loss_slabs(s);
         const int first = by_element(flags, [&](auto fmt) {
             using E = typename decltype(fmt)::type;
-            return by_tiles(loss_tiles(T, V), [&](auto tb) {
-                constexpr int TB = decltype(tb)::value;
-                using X = Tile<TB>;
+            const LossTiles t = loss_tiles(T, V);
+            return by_tiles(t, t == LossTiles::kSmall ? ceil_div(T, 128) * slabs : 0, [&](auto tile) {
+                using X = decltype(tile);
+                using Cfg = LossCfg<Along::kK, Along::kK, X::TA, X::TB, X::WA, X::WB, X::ST>;
                 static std::atomic<unsigned long long> allowed{0};
-                return launch(avion_loss_fwd_kernel<X::TA, TB, X::WA, X::WB, E>, 2 * LossCfg<Along::kK, Along::kK, X::TA, TB, X::WA, X::WB>::STAGE,
-                              allowed, ceil_div(ceil_div(T, TB) * slabs, 8) * 8, X::WA * X::WB * 64, st, "launch avion_loss_fwd_kernel", a, parts, hit, slabs);
+                return launch(avion_loss_fwd_kernel<X::TA, X::TB, X::WA, X::WB, X::ST, E>, X::ST * Cfg::STAGE, allowed,
+                              ceil_div(ceil_div(T, X::TB) * slabs, 8) * 8, Cfg::NT, st, "launch avion_loss_fwd_kernel", a, parts, hit, slabs);
             });
         });
         if (first != AVION_OK) return first;
-        const int second = launch(avion_loss_join_kernel, 0, none, ceil_div(T, kLossJoin), 256, st, "launch avion_loss_join_kernel", a,
-                                  (const float2*)parts, (const float*)hit, slabs, loss, lse, sums);
+        const int second =
+            slabs > 32 ? launch(avion_loss_join_kernel<64>, 0, none, ceil_div(T, 4), 256, st, "launch avion_loss_join_kernel", a, (const float2*)parts,
+                                (const float*)hit, slabs, loss, lse, sums)
+                       : launch(avion_loss_join_kernel<16>, 0, none, ceil_div(T, 16), 256, st, "launch avion_loss_join_kernel", a, (const float2*)parts,
+                                (const float*)hit, slabs, loss, lse, sums);
         if (second != AVION_OK) return second;
     }
     if (!total) return AVION_OK;
-    return launch(avion_loss_total_kernel, 0, none, 1, 256, st, "launch avion_loss_total_kernel", (const double2*)sums, (int)ceil_div(T, kLossJoin),
+    return launch(avion_loss_total_kernel, 0, none, 1, 256, st, "launch avion_loss_total_kernel", (const double2*)sums, (int)ceil_div(T, T > 0 && loss_slabs(s) > 32 ? 4 : 16),
                   (flags & AVION_FLAG_MEAN) != 0, total);
 }
 
@@ -224,19 +240,23 @@ int avion_linear_ce_bwd(const void* x, const void* w, const void* targets, const
     return by_element(flags, [&](auto fmt) {
         using E = typename decltype(fmt)::type;
         static std::atomic<unsigned long long> none{0};
-        int rc2 = launch(avion_loss_factors_kernel, 0, none, 1, 1024, st, "launch avion_loss_factors_kernel", a, dloss, total, each, mean,
-                         kLossHeld<E>, factors);
+        int rc2 = AVION_OK;
+        if (each) rc2 = launch(avion_loss_largest_kernel, 0, none, 1, 1024, st, "launch avion_loss_largest_kernel", a, dloss, factors);
+        int* rows = reinterpret_cast<int*>(ws + at.rows);
+        const int padded = loss_padded(s);
+        if (rc2 == AVION_OK)
+            rc2 = launch(avion_loss_rows_kernel, 0, none, std::max(1, padded / 256), 256, st, "launch avion_loss_rows_kernel", a, lse, dloss, total,
+                         each, mean, kLossHeld<E>, factors, rows, padded);
         for (long long v0 = 0; v0 < V && rc2 == AVION_OK; v0 += piece) {
             const long long n = std::min(piece, V - v0), held = std::min(ld, ceil_div(n, 8) * 8);
             if (T > 0)
-                rc2 = by_tiles(loss_tiles(T, n), [&](auto tb) {
-                    constexpr int TB = decltype(tb)::value;
-                    using X = Tile<TB>;
-                    using Cfg = LossCfg<Along::kK, Along::kK, X::TA, TB, X::WA, X::WB>;
+                rc2 = by_tiles(loss_tiles(T, n), ceil_div(T, 128) * ceil_div(n, 128), [&](auto tile) {
+                    using X = decltype(tile);
+                    using Cfg = LossCfg<Along::kK, Along::kK, X::TA, X::TB, X::WA, X::WB, X::ST>;
                     static std::atomic<unsigned long long> allowed{0};
-                    return launch(avion_loss_dz_kernel<X::TA, TB, X::WA, X::WB, E>, Cfg::LDS_BYTES, allowed,
-                                  persistent(ceil_div(T, TB) * ceil_div(n, X::TA), TB), Cfg::NT, st, "launch avion_loss_dz_kernel", a, lse, dloss,
-                                  (const float*)factors, each, (int)v0, (int)n, dz, (long)ld);
+                    return launch(avion_loss_dz_kernel<X::TA, X::TB, X::WA, X::WB, X::ST, E>, Cfg::LDS_BYTES + (X::ST + 1) * kLossRowBytes, allowed,
+                                  persistent(ceil_div(T, X::TB) * ceil_div(n, X::TA), X::TB), Cfg::NT, st, "launch avion_loss_dz_kernel", a,
+                                  (const int*)rows, padded, (int)v0, (int)n, dz, (long)ld);
                 });
             if (rc2 != AVION_OK) break;
             // (the last piece may be smaller; all use the first one's way)
@@ -250,22 +270,30 @@ int avion_linear_ce_bwd(const void* x, const void* w, const void* targets, const
             gx.splits = (int)std::min<long long>(gx.splits, ceil_div(held, kLossStep));
             if (!dx || T == 0) gx.rows = 0;
             if (!dw) gw.rows = 0;
-            const auto run = [&](auto tb) {
-                constexpr int TB = decltype(tb)::value;
-                using X = Tile<TB>;
-                using Cfg = LossCfg<Along::kIndex, Along::kIndex, X::TA, TB, X::WA, X::WB>;
-                static std::atomic<unsigned long long> allowed{0};
-                const long long items_x = ceil_div(gx.rows, TB) * ceil_div(D, X::TA) * gx.splits;
-                const long long items_w = ceil_div(gw.rows, TB) * ceil_div(D, X::TA) * gw.splits;
-                return launch(avion_loss_grad_kernel<X::TA, TB, X::WA, X::WB, E>, Cfg::LDS_BYTES, allowed, persistent(items_x + items_w, TB),
-                              Cfg::NT, st, "launch avion_loss_grad_kernel", gx, gw, (const float*)factors, (int)items_x);
+            const auto by_grads = [&](auto f) {
+                if (grads_large(s, piece)) return f(Tile<256, 2>{});
+                const long long items = ceil_div(gx.rows, 128) * ceil_div(D, 128) * gx.splits + ceil_div(gw.rows, 128) * ceil_div(D, 128) * gw.splits;
+                return items <= kComputeUnits ? f(Tile<128, 4>{}) : f(Tile<128, 2>{});
             };
             if (gx.rows > 0 || gw.rows > 0)
-                rc2 = grads_large(s, piece) ? run(std::integral_constant<int, 256>{}) : run(std::integral_constant<int, 128>{});
+                rc2 = by_grads([&](auto tile) {
+                    using X = decltype(tile);
+                    using Cfg = LossCfg<Along::kIndex, Along::kIndex, X::TA, X::TB, X::WA, X::WB, X::ST>;
+                    static std::atomic<unsigned long long> allowed{0};
+                    const long long items_x = ceil_div(gx.rows, X::TB) * ceil_div(D, X::TA) * gx.splits;
+                    const long long items_w = ceil_div(gw.rows, X::TB) * ceil_div(D, X::TA) * gw.splits;
+                    return launch(avion_loss_grad_kernel<X::TA, X::TB, X::WA, X::WB, X::ST, E>, Cfg::LDS_BYTES, allowed,
+                                  persistent(items_x + items_w, X::TB), Cfg::NT, st, "launch avion_loss_grad_kernel", gx, gw,
+                                  (const float*)factors, (int)items_x);
+                });
             const auto finish = [&](const LossGrad& g, int planes, void* to) {
-                const long long count = (long long)g.rows * D;
-                return launch(avion_loss_sum_kernel<E>, 0, none, std::min<long long>(2048, ceil_div(count, 1024)), 256, st,
-                              "launch avion_loss_sum_kernel", (const float*)g.sum, planes, (long)count, (const float*)factors, static_cast<raw16*>(to));
+                return by_grads([&](auto tile) {
+                    using X = decltype(tile);
+                    const long long blocks = ceil_div(g.rows, X::TB) * ceil_div(D, X::TA) * (X::TA / 32) * (X::TB / 32);
+                    return launch(avion_loss_sum_kernel<X::TA, X::TB, X::WA, X::WB, E>, 0, none, ceil_div(blocks, 4), 256, st,
+                                  "launch avion_loss_sum_kernel", (const float*)g.sum, planes, g.rows, D, (const float*)factors,
+                                  static_cast<raw16*>(to));
+                });
             };
             if (rc2 == AVION_OK && at.planes_x && last && gx.rows > 0) rc2 = finish(gx, grad_splits(s, piece, false), dx);
             if (rc2 == AVION_OK && at.planes_w && gw.rows > 0) rc2 = finish(gw, gw.splits, static_cast<raw16*>(dw) + v0 * D);
