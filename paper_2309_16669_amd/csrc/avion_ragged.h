@@ -641,14 +641,19 @@ avion_ragged_dq_kernel(RaggedArgs a, const raw16* __restrict__ o, const raw16* _
     {
         const raw16* q = a.q + (long)(p.begin + row.token) * a.rs_q + row.head * D + g * 8;
         const long out_at = ((long)(p.begin + row.token) * a.Hq + row.head) * D + g * 8;
-        float part = 0.f;
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) {
             qf[ks] = *reinterpret_cast<const frag8*>(q + ks * 16);
             gf[ks] = *reinterpret_cast<const frag8*>(dO + out_at + ks * 16);
-            const frag8 of = *reinterpret_cast<const frag8*>(o + out_at + ks * 16);
+        }
+        float part = 0.f;
+        if (!whole) {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) part = fmaf(E::widen(of, e), E::widen(gf[ks], e), part);
+            for (int ks = 0; ks < KS; ++ks) {
+                const frag8 of = *reinterpret_cast<const frag8*>(o + out_at + ks * 16);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) part = fmaf(E::widen(of, e), E::widen(gf[ks], e), part);
+            }
         }
         dl = both_halves_sum(part);
     }
@@ -669,15 +674,22 @@ avion_ragged_dq_kernel(RaggedArgs a, const raw16* __restrict__ o, const raw16* _
             dp = E::mfma(av, gf[ks], ks == 0 ? f32x16_zero() : dp);
         }
     };
+    // weights in place of the scores
+    auto weigh = [&](f32x16& sc) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) sc[i] = fast_exp2(fmaf(sc[i], cs, -lc));
+    };
+    f32x16 s, dp;
+    const bool single = ROWS == 32 && ntiles == 1;  // one unit: its products serve twice
     if (whole && active) {
         float sum = 0.f;
         for (int key_base = 0; key_base < seen_by_any; key_base += 32) {
-            f32x16 pe, dp;
             if (Ring::NBUF == 1) ring.before(key_base / ROWS, 0, 0);
-            products(ring.at(smem, key_base / ROWS), key_base % ROWS / 32, key_base, pe, dp);
+            products(ring.at(smem, key_base / ROWS), key_base % ROWS / 32, key_base, s, dp);
             if (Ring::NBUF == 1) Ring::landed_barrier();
+            weigh(s);
 #pragma unroll
-            for (int i = 0; i < 16; ++i) sum = fmaf(fast_exp2(fmaf(pe[i], cs, -lc)), dp[i], sum);
+            for (int i = 0; i < 16; ++i) sum = fmaf(s[i], dp[i], sum);
         }
         dl = both_halves_sum(sum);
         if (Ring::NBUF == 1 && seen_by_any > ROWS) {
@@ -701,8 +713,10 @@ avion_ragged_dq_kernel(RaggedArgs a, const raw16* __restrict__ o, const raw16* _
     f32x16 acc[CT];
     acc_zero(acc);
     auto unit = [&](const char* kt, int hk32, int key_base) {
-        f32x16 s, dp;
-        products(kt, hk32, key_base, s, dp);
+        if (!single) {
+            products(kt, hk32, key_base, s, dp);
+            weigh(s);
+        }
         frag8 kf[2][CT];
         if constexpr (D <= 96) {
 #pragma unroll
@@ -713,7 +727,7 @@ avion_ragged_dq_kernel(RaggedArgs a, const raw16* __restrict__ o, const raw16* _
         u32x4 df[2];
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
-            s[i] = fast_exp2(fmaf(s[i], cs, -lc)) * (dp[i] - dl);
+            s[i] *= dp[i] - dl;
             if (i % 2 == 1) df[i / 8][(i / 2) % 4] = E::pack(s[i - 1], s[i]);
         }
 #pragma unroll

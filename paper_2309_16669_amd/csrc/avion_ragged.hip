@@ -57,7 +57,7 @@ int dkdv_parts(const RaggedShape& s)
     const long long blocks = (s.Tk / (32 * nw) + s.S) * s.Hk;
     int parts = 1;
     for (int p = 2; p <= G && p <= 8; ++p)
-        if (G % p == 0 && blocks * parts < 2 * kComputeUnits) parts = p;
+        if (G % p == 0 && blocks * parts < 4 * kComputeUnits) parts = p;
     return parts;
 }
 long long ragged_npad(const RaggedShape& s) { return (s.Tq / 64 + s.S + 2) * 64; }
