@@ -72,19 +72,19 @@ long long loss_piece(const LossShape& s)
     return std::min<long long>(most, ceil_div(ceil_div(s.V, pieces), 256) * 256);
 }
 long long loss_ld(const LossShape& s) { return std::min(loss_piece(s), ceil_div(s.V, 64) * 64); }
-// The two gradients' tiles: 256 x 256 where both together have one for each compute unit, else 128 x 128 cut along K until they fill
-// the chip twice over (at least 4 steps a range; a range's plane is written and read again, so no more of them than that takes).
+// The two gradients' tiles: 256 x 256 where both together have one for each compute unit and no side is narrower than one, else 128 x
+// 128.  Either way a product whose steps are more than a workgroup's fair share of all (few tiles, long K) is cut along K, at
+// least 4 steps a range: 213 x 112000 x 72, dx of which is two tiles of 1750 steps, 2540 us without.  A range's plane is written and
+// read again, so there are no more of them than that.
 bool grads_large(const LossShape& s, long long n)
 {
-    return (ceil_div(s.T, 256) + ceil_div(n, 256)) * ceil_div(s.D, 256) >= kComputeUnits;
+    return s.T >= 256 && n >= 256 && s.D > 128 && (ceil_div(s.T, 256) + ceil_div(n, 256)) * ceil_div(s.D, 256) >= kComputeUnits;
 }
 int grad_splits(const LossShape& s, long long n, bool dw)
 {
-    if (grads_large(s, n)) return 1;
-    const long long steps = ceil_div(dw ? s.T : n, kLossStep);
-    // (of both together; each product's share by its steps)
-    const long long work = ceil_div(s.T, 128) * ceil_div(n, kLossStep) + ceil_div(n, 128) * ceil_div(s.T, kLossStep);
-    const long long fair = std::max<long long>(4, work * ceil_div(s.D, 128) / (2 * kComputeUnits));  // steps of a workgroup
+    const long long t = grads_large(s, n) ? 256 : 128, at_once = t == 256 ? kComputeUnits : 2 * kComputeUnits;
+    const long long of_x = ceil_div(n, kLossStep), of_w = ceil_div(s.T, kLossStep), steps = dw ? of_w : of_x;
+    const long long all = (ceil_div(s.T, t) * of_x + ceil_div(n, t) * of_w) * ceil_div(s.D, t), fair = std::max<long long>(4, ceil_div(all, at_once));
     return (int)std::max<long long>(1, std::min<long long>(ceil_div(steps, fair), steps / 4));
 }
 // floats of a plane: whole tiles

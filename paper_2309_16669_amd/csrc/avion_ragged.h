@@ -20,6 +20,7 @@
 // (infinities, NaN, an unused slot) cannot reach the next.  Within a sequence a masked key's weight is 0, which NaN and infinity
 // in its value survive, as in avion_attn_fwd.
 #pragma once
+#include "avion_bwd.h"
 #include "avion_common.h"
 
 struct RaggedArgs {
@@ -75,14 +76,34 @@ DEVINL int2 ragged_tokens(const int* off, int S, int T, int i)
     return int2{begin, max(ragged_border(off, S, T, i + 1) - begin, 0)};
 }
 
+// How a kernel cuts its work.  A workgroup: NW wavefronts of 32 rows (keys in dK/dV) each, in KG groups that walk over a share of the
+// other side's tiles through buffers of their own and add their sums up at the end; tiles of ROWS tokens in NBUF buffers.
+//   RaggedWide   the usual one
+//   RaggedSplit, RaggedSplit4   where such workgroups would leave compute units without work, or with one of two: shorter walks of fewer
+//                rows
+//   RaggedShort  sequences of less than two wavefronts' rows: one wavefront with one buffer of 32 rows, so that 16 of a compute unit
+//                wait for their loads at once; four of them, which know nothing of each other, to a workgroup (JOBS)
+//   RaggedLone   single tokens behind long caches
+template <int NW_, int KG_, int ROWS_, int NBUF_, int JOBS_>
+struct RaggedCut {
+    static constexpr int NW = NW_, KG = KG_, ROWS = ROWS_, NBUF = NBUF_, JOBS = JOBS_;
+    static constexpr int BLOCK = 32 * NW, SHIFT = NW == 4 ? 7 : NW == 2 ? 6 : 5, NT = NW * KG * 64;  // rows, their logarithm, threads of a job
+    static_assert(NBUF == 2 || NW * KG == 1, "");
+};
+using RaggedWide = RaggedCut<4, 1, 64, 2, 1>;
+using RaggedSplit = RaggedCut<2, 2, 64, 2, 1>;
+using RaggedSplit4 = RaggedCut<1, 4, 32, 2, 1>;
+using RaggedShort = RaggedCut<1, 1, 32, 1, 4>;
+using RaggedLone = RaggedCut<1, 1, 64, 2, 1>;
+
 // NBUF buffers in LDS of an A and a B tile of ROWS token rows each (and, with SCALARS, ROWS + ROWS floats), filled by LDS-direct loads
 // as TileRing's.  The descriptors begin at the tile's own first row, so that no length of a sequence and no row stride takes a
 // byte offset past 32 bits; rows past the end arrive as zeros.
 // Layout of a tile: at 64 channels quad_at's (no bank conflicts, and two addresses a lane for the loads of both tensors instead of one
 // for each load: where registers are scarce, in dK/dV, that is what keeps the accumulators out of scratch), else padded rows.
-template <int D, int NW, int ROWS_, int NBUF_, bool SCALARS>
+template <int D, typename Cut, bool SCALARS>
 struct RaggedRing {
-    static constexpr int ROWS = ROWS_, NBUF = NBUF_, STRIDE = tile_stride<D>();
+    static constexpr int NW = Cut::NW, ROWS = Cut::ROWS, NBUF = Cut::NBUF, STRIDE = tile_stride<D>();
     static constexpr bool QUAD = D == 64;
     // 1 KB blocks of a tile (the last one's rows past the tile, where there are any, are not read)
     static constexpr int NTI = QUAD ? ROWS / 8 : (ROWS * STRIDE + 1023) / 1024, NBLK = 2 * NTI, NPW = (NBLK + NW - 1) / NW;
@@ -159,7 +180,7 @@ struct RaggedRing {
     // what was asked for is in LDS, and nobody reads any more what was read (one wavefront has nobody to wait for)
     DEVINL static void landed_barrier()
     {
-        if constexpr (NW > 1) asm volatile("s_waitcnt vmcnt(0)\n\ts_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        if constexpr (NW * Cut::KG > 1) asm volatile("s_waitcnt vmcnt(0)\n\ts_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
         else asm volatile("s_waitcnt vmcnt(0)\n\ts_waitcnt lgkmcnt(0)" ::: "memory");
     }
     // before tile t is computed on, from t0 on: with two buffers the next one is asked for, with one this one
@@ -205,33 +226,37 @@ struct RaggedLane<64> : QuadLane {
     }
 };
 
-// Short sequences: one wavefront, one buffer of 32 rows, so that 16 of a compute unit wait for their loads
-// at once; four of them, which know nothing of each other, to a workgroup (kRaggedJobs)
-template <int NW>
-constexpr int kRaggedJobs = NW == 1 ? 4 : 1;
-template <int NW>
-constexpr int kRaggedRows = NW == 1 ? 32 : 64;
-template <int NW>
-constexpr int kRaggedBuffers = NW == 1 ? 1 : 2;
-// The work of a workgroup, or, where a wavefront works alone, of each of its wavefronts
-template <int NW>
+// The work of a workgroup, or, with several jobs, of each of its wavefronts
+template <typename Cut>
 struct RaggedJob {
-    int id, wave, tid;
-    char* smem;
-    DEVINL RaggedJob(char* shared, int lds_bytes)
+    int id, wave, group, tid;
+    char *all, *smem;  // the job's LDS, the group's
+    DEVINL RaggedJob(char* shared, int ring_bytes)
     {
         const int w = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
-        if constexpr (NW == 1) {
-            id = blockIdx.x * kRaggedJobs<1> + w;
-            wave = 0;
+        if constexpr (Cut::JOBS > 1) {
+            id = blockIdx.x * Cut::JOBS + w;
+            wave = group = 0;
             tid = threadIdx.x % 64;
-            smem = shared + w * lds_bytes;
+            all = smem = shared + w * ring_bytes;
         } else {
             id = blockIdx.x;
-            wave = w;
+            wave = w % Cut::NW;
+            group = Cut::KG == 1 ? 0 : w / Cut::NW;
             tid = threadIdx.x;
-            smem = shared;
+            all = shared;
+            smem = shared + group * ring_bytes;
         }
+    }
+};
+// A group's share of the tiles 0 .. n - 1: all groups pass `per` of them
+struct RaggedShare {
+    int t0, t1, per;
+    DEVINL RaggedShare(int n, int groups, int group)
+    {
+        per = (n + groups - 1) / groups;
+        t0 = min(group * per, n);
+        t1 = min(t0 + per, n);
     }
 };
 
@@ -301,12 +326,12 @@ DEVINL void ragged_zero(raw16* out, int H, int h0, int heads, long token0, int n
 constexpr float kRaggedLazy = 8.f;
 constexpr float kRaggedNone = -3.0e38f;  // reference of a row that has seen nothing: finite, so that -inf - it is -inf
 
-template <int D, int NW, int ROWS, int NBUF>
+template <int D, typename Cut>
 struct RaggedFwdCfg {
-    using Ring = RaggedRing<D, NW, ROWS, NBUF, false>;
-    static constexpr int NT = NW * 64, BM = 32 * NW, SHIFT = NW == 4 ? 7 : 5;
-    static constexpr int LDS_BYTES = Ring::LDS_BYTES;
-    static constexpr int WAVES_PER_SIMD = NBUF == 2 && NW == 1 ? 1 : D == 64 ? 4 : D == 80 ? 3 : 2;
+    using Ring = RaggedRing<D, Cut, false>;
+    static constexpr int LDS_BYTES = Ring::LDS_BYTES * Cut::KG * Cut::JOBS;
+    static_assert(LDS_BYTES <= 160 * 1024, "");
+    static constexpr int WAVES_PER_SIMD = Cut::KG > 1 || std::is_same<Cut, RaggedLone>::value ? 1 : D == 64 ? 4 : D == 80 ? 3 : 2;
 };
 template <int CT>
 struct RaggedSums {
@@ -322,13 +347,13 @@ struct RaggedSums {
     }
 };
 
-// The tiles t0 .. t1 - 1 of one sequence's keys for the wavefront's rows row0 .. row0 + 31
-template <int D, int NW, int ROWS, int NBUF, typename E>
+// The tiles t0 .. t1 - 1 (and as many barriers as `per` tiles take) of one sequence's keys for the wavefront's rows row0 .. row0 + 31
+template <int D, typename Cut, typename E>
 DEVINL void ragged_fwd_walk(char* smem, const RaggedArgs& a, int hk, int begin_q, int nq, int begin_k, int nk, int row0, int rows, int t0,
-                            int t1, RaggedSums<(D + 31) / 32>& sums, int wave, int lane)
+                            int t1, int per, RaggedSums<(D + 31) / 32>& sums, int wave, int lane)
 {
-    using Ring = typename RaggedFwdCfg<D, NW, ROWS, NBUF>::Ring;
-    constexpr int KS = D / 16, CT = (D + 31) / 32;
+    using Ring = typename RaggedFwdCfg<D, Cut>::Ring;
+    constexpr int KS = D / 16, CT = (D + 31) / 32, ROWS = Cut::ROWS;
     const int l32 = lane % 32, g = lane / 32;
     const RaggedLane<D> at(lane);
     const Ring ring(a.k + (long)begin_k * a.rs_k + hk * D, a.rs_k, a.v + (long)begin_k * a.rs_v + hk * D, a.rs_v, nullptr, 0, nk, smem,
@@ -388,9 +413,9 @@ DEVINL void ragged_fwd_walk(char* smem, const RaggedArgs& a, int hk, int begin_q
                 sums.o[ct] = E::mfma(vf[half][ct], as_frag8(pf[half]), sums.o[ct]);
             }
     };
-    for (int t = t0; t < t1; ++t) {
+    for (int t = t0; t < t0 + per; ++t) {
         ring.before(t, t0, t1);
-        if (active) {
+        if (active && (Cut::KG == 1 || t < t1)) {
             const char* kt = ring.at(smem, t);
 #pragma unroll
             for (int hk32 = 0; hk32 < ROWS / 32; ++hk32) {
@@ -428,38 +453,73 @@ DEVINL void ragged_fwd_none(const RaggedArgs& a, raw16* o, float* lse, int hk, i
 // the tokens whose (token, head) rows a block of BM rows begins: each token belongs to one block
 DEVINL int ragged_first_token(long row, int G) { return (int)((row + G - 1) / G); }
 
-template <int D, int NW, typename E>
-__global__ void __launch_bounds__(NW * kRaggedJobs<NW> * 64, (RaggedFwdCfg<D, NW, kRaggedRows<NW>, kRaggedBuffers<NW>>::WAVES_PER_SIMD))
+// The groups' sums of the same rows, in group order, each scaled to the larger reference: into group 0's
+template <int CT, typename Cut>
+DEVINL void ragged_fwd_join(char* area, RaggedSums<CT>& sums, int group, int wave, int lane)
+{
+    constexpr int VALS = CT * 16 + 3;
+    if (group > 0) {
+        float* mine = reinterpret_cast<float*>(area) + ((group - 1) * Cut::NW + wave) * VALS * 64 + lane;
+#pragma unroll
+        for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) mine[(ct * 16 + i) * 64] = sums.o[ct][i];
+        mine[(VALS - 3) * 64] = sums.l;
+        mine[(VALS - 2) * 64] = sums.rs4[0];
+        mine[(VALS - 1) * 64] = sums.m;
+    }
+    __syncthreads();
+    if (group > 0) return;
+#pragma unroll
+    for (int og = 0; og < Cut::KG - 1; ++og) {
+        const float* other = reinterpret_cast<const float*>(area) + (og * Cut::NW + wave) * VALS * 64 + lane;
+        const float m = fmaxf(sums.m, other[(VALS - 1) * 64]), x = fast_exp2(sums.m - m), y = fast_exp2(other[(VALS - 1) * 64] - m);
+        sums.l = sums.l * x + other[(VALS - 3) * 64] * y;
+        sums.rs4[0] = sums.rs4[0] * x + other[(VALS - 2) * 64] * y;
+        sums.m = m;
+#pragma unroll
+        for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) sums.o[ct][i] = sums.o[ct][i] * x + other[(ct * 16 + i) * 64] * y;
+    }
+}
+
+template <int D, typename Cut, typename E>
+__global__ void __launch_bounds__(Cut::NT * Cut::JOBS, (RaggedFwdCfg<D, Cut>::WAVES_PER_SIMD))
 avion_ragged_fwd_kernel(RaggedArgs a, raw16* __restrict__ o, float* __restrict__ lse)
 {
-    constexpr int ROWS = kRaggedRows<NW>, NBUF = kRaggedBuffers<NW>;
-    using Cfg = RaggedFwdCfg<D, NW, ROWS, NBUF>;
+    using Cfg = RaggedFwdCfg<D, Cut>;
+    constexpr int CT = (D + 31) / 32, STORE = Cut::NW * RaggedStore<D, E>::BYTES;
     extern __shared__ __attribute__((aligned(16))) char shared[];
     const int lane = threadIdx.x % 64;
-    const RaggedJob<NW> job(shared, Cfg::LDS_BYTES);
-    const int wave = job.wave;
-    char* smem = job.smem;
+    const RaggedJob<Cut> job(shared, Cfg::Ring::LDS_BYTES);
     // the key heads go round the XCDs; the last blocks, which see the most keys, begin first
     const int hk = job.id % a.Hk, slot = a.slots - 1 - job.id / a.Hk;
     if (slot < 0) return;
-    const RaggedPlace p = ragged_place<Cfg::SHIFT>(a.off_q, a.S, a.Tq, a.G, slot, lane);
+    const RaggedPlace p = ragged_place<Cut::SHIFT>(a.off_q, a.S, a.Tq, a.G, slot, lane);
     const int rows = p.n * a.G;
-    if (p.block < 0 || p.block * Cfg::BM >= rows) return;
-    const int block0 = (int)p.block * Cfg::BM;
+    if (p.block < 0 || p.block * Cut::BLOCK >= rows) return;
+    const int block0 = (int)p.block * Cut::BLOCK;
     if (p.i == 0 || p.i == a.S + 1) {
-        const int from = ragged_first_token(block0, a.G), to = min(ragged_first_token(block0 + Cfg::BM, a.G), p.n);
-        ragged_fwd_none<D>(a, o, lse, hk, p.begin + from, to - from, job.tid, Cfg::NT);
+        const int from = ragged_first_token(block0, a.G), to = min(ragged_first_token(block0 + Cut::BLOCK, a.G), p.n);
+        ragged_fwd_none<D>(a, o, lse, hk, p.begin + from, to - from, job.tid, Cut::NT);
         return;
     }
     // (offsets that serve both sides are here already)
     const int2 keys = a.off_k == a.off_q && a.Tk == a.Tq ? int2{p.begin, p.n} : ragged_tokens(a.off_k, a.S, a.Tk, p.i);
     const int begin_k = keys.x, nk = keys.y;
-    const int last_seen = RaggedRow(a, hk, block0 + Cfg::BM - 1, rows, p.n, nk).keys;
-    RaggedSums<(D + 31) / 32> sums;
-    const int row0 = block0 + wave * 32;
-    ragged_fwd_walk<D, NW, ROWS, NBUF, E>(smem, a, hk, p.begin, p.n, begin_k, nk, row0, rows, 0, (last_seen + ROWS - 1) / ROWS, sums, wave, lane);
+    const int last_seen = RaggedRow(a, hk, block0 + Cut::BLOCK - 1, rows, p.n, nk).keys;
+    const RaggedShare share((last_seen + Cut::ROWS - 1) / Cut::ROWS, Cut::KG, job.group);
+    RaggedSums<CT> sums;
+    const int row0 = block0 + job.wave * 32;
+    ragged_fwd_walk<D, Cut, E>(job.smem, a, hk, p.begin, p.n, begin_k, nk, row0, rows, share.t0, share.t1, share.per, sums, job.wave, lane);
+    if constexpr (Cut::KG > 1) {
+        static_assert(STORE + (Cut::KG - 1) * Cut::NW * (CT * 16 + 3) * 256 <= Cfg::LDS_BYTES, "exchange area");
+        ragged_fwd_join<CT, Cut>(job.all + STORE, sums, job.group, job.wave, lane);
+        if (job.group > 0) return;
+    }
     if (row0 >= rows) return;
-    ragged_fwd_store<D, E>(smem + wave * RaggedStore<D, E>::BYTES, a, o, lse, hk, p.begin, row0, rows, sums, lane);
+    ragged_fwd_store<D, E>(job.all + job.wave * RaggedStore<D, E>::BYTES, a, o, lse, hk, p.begin, row0, rows, sums, lane);
 }
 
 // ------------------------------------------------------------------------------ few rows, many keys
@@ -495,10 +555,10 @@ avion_ragged_few_kernel(RaggedArgs a, raw16* __restrict__ o, float* __restrict__
         if (!part && p.block > 0) return;
         const int t0 = part ? (int)p.block * (chunk / 64) : 0, t1 = part ? min(t0 + chunk / 64, tiles) : tiles;
         RaggedSums<CT> sums;
-        ragged_fwd_walk<D, 1, 64, 2, E>(smem, a, hk, begin_q, nq, p.begin, p.n, row0, rows, t0, t1, sums, 0, lane);
+        ragged_fwd_walk<D, RaggedLone, E>(smem, a, hk, begin_q, nq, p.begin, p.n, row0, rows, t0, t1, t1 - t0, sums, 0, lane);
         if (!part) {
             ragged_fwd_store<D, E>(smem, a, o, lse, hk, begin_q, row0, rows, sums, lane);
-            RaggedFwdCfg<D, 1, 64, 2>::Ring::landed_barrier();
+            RaggedFwdCfg<D, RaggedLone>::Ring::landed_barrier();
             continue;
         }
         const int l32 = lane % 32, g = lane / 32;
@@ -518,7 +578,7 @@ avion_ragged_few_kernel(RaggedArgs a, raw16* __restrict__ o, float* __restrict__
             out[32 * D + 32 + l32] = l;
             out[32 * D + 64 + l32] = r;
         }
-        RaggedFwdCfg<D, 1, 64, 2>::Ring::landed_barrier();
+        RaggedFwdCfg<D, RaggedLone>::Ring::landed_barrier();
     }
 }
 
@@ -589,51 +649,54 @@ avion_ragged_join_kernel(RaggedArgs a, raw16* __restrict__ o, float* __restrict_
 template <typename E>
 constexpr float kRaggedShift = std::is_same<E, F16>::value ? 8.f : 0.f;
 
-template <int D, int NW>
+template <int D, typename Cut>
 struct RaggedDqCfg {
-    using Ring = RaggedRing<D, NW, kRaggedRows<NW>, kRaggedBuffers<NW>, false>;
-    static constexpr int NT = NW * 64, BM = 32 * NW, SHIFT = NW == 4 ? 7 : 5, LDS_BYTES = Ring::LDS_BYTES;
-    static constexpr int WAVES_PER_SIMD = D == 64 ? 4 : 2;
+    using Ring = RaggedRing<D, Cut, false>;
+    static constexpr int LDS_BYTES = Ring::LDS_BYTES * Cut::KG * Cut::JOBS;
+    static_assert(LDS_BYTES <= 160 * 1024, "");
+    static constexpr int WAVES_PER_SIMD = Cut::KG > 1 ? 1 : D == 64 ? 4 : 2;
 };
 DEVINL long ragged_scalar_at(int begin, int i) { return ((long)(begin >> 6) + i) * 64; }
 
-template <int D, int NW, typename E>
-__global__ void __launch_bounds__(NW * kRaggedJobs<NW> * 64, (RaggedDqCfg<D, NW>::WAVES_PER_SIMD))
+template <int D, typename Cut, typename E>
+__global__ void __launch_bounds__(Cut::NT * Cut::JOBS, (RaggedDqCfg<D, Cut>::WAVES_PER_SIMD))
 avion_ragged_dq_kernel(RaggedArgs a, const raw16* __restrict__ o, const raw16* __restrict__ dO, const float* __restrict__ lse,
                        raw16* __restrict__ dq, float* __restrict__ rowsc, int npad)
 {
-    using Cfg = RaggedDqCfg<D, NW>;
+    using Cfg = RaggedDqCfg<D, Cut>;
     using Ring = typename Cfg::Ring;
     constexpr int KS = D / 16, CT = (D + 31) / 32;
     extern __shared__ __attribute__((aligned(16))) char shared[];
     const int lane = threadIdx.x % 64, l32 = lane % 32, g = lane / 32;
-    const RaggedJob<NW> job(shared, Cfg::LDS_BYTES);
+    const RaggedJob<Cut> job(shared, Ring::LDS_BYTES);
     const int wave = job.wave;
     char* smem = job.smem;
     const int hk = job.id % a.Hk, slot = a.slots - 1 - job.id / a.Hk;
     if (slot < 0) return;
-    const RaggedPlace p = ragged_place<Cfg::SHIFT>(a.off_q, a.S, a.Tq, a.G, slot, lane);
+    const RaggedPlace p = ragged_place<Cut::SHIFT>(a.off_q, a.S, a.Tq, a.G, slot, lane);
     const int rows = p.n * a.G, nq = p.n;
-    if (p.block < 0 || p.block * Cfg::BM >= rows) return;
-    const int block0 = (int)p.block * Cfg::BM;
+    if (p.block < 0 || p.block * Cut::BLOCK >= rows) return;
+    const int block0 = (int)p.block * Cut::BLOCK;
     if (p.i == 0 || p.i == a.S + 1) {
-        const int from = ragged_first_token(block0, a.G), to = min(ragged_first_token(block0 + Cfg::BM, a.G), p.n);
-        ragged_zero<D>(dq, a.Hq, hk * a.G, a.G, p.begin + from, to - from, job.tid, Cfg::NT);
+        const int from = ragged_first_token(block0, a.G), to = min(ragged_first_token(block0 + Cut::BLOCK, a.G), p.n);
+        ragged_zero<D>(dq, a.Hq, hk * a.G, a.G, p.begin + from, to - from, job.tid, Cut::NT);
         return;
     }
     // (offsets that serve both sides are here already)
     const int2 keys = a.off_k == a.off_q && a.Tk == a.Tq ? int2{p.begin, p.n} : ragged_tokens(a.off_k, a.S, a.Tk, p.i);
     const int begin_k = keys.x, nk = keys.y;
     constexpr int ROWS = Ring::ROWS;
-    const int ntiles = (RaggedRow(a, hk, block0 + Cfg::BM - 1, rows, nq, nk).keys + ROWS - 1) / ROWS;
-    const bool whole = ntiles * ROWS <= 128;
+    const int ntiles = (RaggedRow(a, hk, block0 + Cut::BLOCK - 1, rows, nq, nk).keys + ROWS - 1) / ROWS;
+    const bool whole = Ring::NBUF == 1 ? ntiles * ROWS <= 128 : ntiles <= 2;  // (the first group's work then)
+    const RaggedShare share(ntiles, Cut::KG == 1 || whole ? 1 : Cut::KG, job.group);
+    const int t0 = share.t0, t1 = share.t1;
     const Ring ring(a.k + (long)begin_k * a.rs_k + hk * D, a.rs_k, a.v + (long)begin_k * a.rs_v + hk * D, a.rs_v, nullptr, 0, nk, smem,
                     wave, lane);
-    if (ntiles > 0) ring.fetch(0);
-    if (Ring::NBUF == 2 && ntiles == 2) ring.fetch(1);
+    if (t0 < t1) ring.fetch(t0);
+    if (Ring::NBUF == 2 && whole && t1 == 2) ring.fetch(1);
     const int row0 = block0 + wave * 32;
     const RaggedLane<D> at(lane);
-    const bool active = row0 < rows;
+    const bool active = row0 < rows, first = job.group == 0;
     const RaggedRow row(a, hk, row0 + l32, rows, nq, nk);
     const int seen_by_all = RaggedRow(a, hk, row0, rows, nq, nk).keys, seen_by_any = RaggedRow(a, hk, row0 + 31, rows, nq, nk).keys;
     frag8 qf[KS], gf[KS];
@@ -680,8 +743,8 @@ avion_ragged_dq_kernel(RaggedArgs a, const raw16* __restrict__ o, const raw16* _
         for (int i = 0; i < 16; ++i) sc[i] = fast_exp2(fmaf(sc[i], cs, -lc));
     };
     f32x16 s, dp;
-    const bool single = ROWS == 32 && ntiles == 1;  // one unit: its products serve twice
-    if (whole && active) {
+    const bool single = Ring::NBUF == 1 && ntiles == 1;  // one unit: its products serve twice
+    if (whole && active && first) {
         float sum = 0.f;
         for (int key_base = 0; key_base < seen_by_any; key_base += 32) {
             if (Ring::NBUF == 1) ring.before(key_base / ROWS, 0, 0);
@@ -697,14 +760,14 @@ avion_ragged_dq_kernel(RaggedArgs a, const raw16* __restrict__ o, const raw16* _
             Ring::landed_barrier();
         }
     }
-    if (active && g == 0 && row0 + l32 < rows) {
+    if (active && first && g == 0 && row0 + l32 < rows) {
         float* ws = rowsc + (long)row.head * 2 * npad + ragged_scalar_at(p.begin, p.i) + row.token;
         ws[0] = lc - kRaggedShift<E>;
         ws[npad] = -dl;
     }
     // the rows up to the next multiple of 64: weight 0
-    if (block0 + Cfg::BM >= rows)
-        for (int x = job.tid; x < (-nq & 63) * a.G; x += Cfg::NT) {
+    if (block0 + Cut::BLOCK >= rows)
+        for (int x = job.tid; x < (-nq & 63) * a.G; x += Cut::NT) {
             const int i = a.over_heads(x);
             float* ws = rowsc + (long)(hk * a.G + x - i * a.G) * 2 * npad + ragged_scalar_at(p.begin, p.i) + nq + i;
             ws[0] = INFINITY;
@@ -738,9 +801,9 @@ avion_ragged_dq_kernel(RaggedArgs a, const raw16* __restrict__ o, const raw16* _
                 acc[ct] = E::mfma(kf[half][ct], as_frag8(df[half]), acc[ct]);
             }
     };
-    for (int t = 0; t < ntiles; ++t) {
-        if (Ring::NBUF == 1 || !whole) ring.before(t, 0, ntiles);
-        if (active) {
+    for (int t = t0; t < t0 + share.per; ++t) {
+        if (Ring::NBUF == 1 || !whole) ring.before(t, t0, t1);
+        if (active && (Cut::KG == 1 || t < t1)) {
             const char* kt = ring.at(smem, t);
 #pragma unroll
             for (int hk32 = 0; hk32 < ROWS / 32; ++hk32) {
@@ -751,18 +814,25 @@ avion_ragged_dq_kernel(RaggedArgs a, const raw16* __restrict__ o, const raw16* _
         }
         Ring::landed_barrier();
     }
+    if constexpr (Cut::KG > 1) {
+        constexpr int STORE = Cut::NW * RaggedStore<D, E>::BYTES;
+        static_assert(STORE + (Cut::KG - 1) * Cut::NW * (int)sizeof(acc) * 64 <= Cfg::LDS_BYTES, "exchange area");
+        add_groups<Cut::NW, Cut::KG>(job.all + STORE, acc, job.group, wave, lane, active);
+        if (!first) return;
+    }
     if (!active) return;
-    RaggedStore<D, E>::run(smem + wave * RaggedStore<D, E>::BYTES, acc, a.scale, dq, a, hk, p.begin, row0, rows, lane_from_exec());
+    RaggedStore<D, E>::run(job.all + wave * RaggedStore<D, E>::BYTES, acc, a.scale, dq, a, hk, p.begin, row0, rows, lane_from_exec());
 }
 
 // -------------------------------------------------------------------------------------------- dK, dV
 // As avion_dkdv_kernel: a wavefront owns 32 keys of one key head; the tiles of 64 queries of its query heads come one after the
 // other.  With `parts` > 1 the query heads are dealt to that many workgroups, whose sums meet in fp32 (avion_ragged_sum_kernel).
-template <int D, int NW>
+template <int D, typename Cut>
 struct RaggedDkvCfg {
-    using Ring = RaggedRing<D, NW, kRaggedRows<NW>, kRaggedBuffers<NW>, true>;
-    static constexpr int NT = NW * 64, BN = 32 * NW, SHIFT = NW == 4 ? 7 : 5, LDS_BYTES = Ring::LDS_BYTES;
-    static constexpr int WAVES_PER_SIMD = D == 64 ? 3 : D == 80 ? 2 : 1;
+    using Ring = RaggedRing<D, Cut, true>;
+    static constexpr int LDS_BYTES = Ring::LDS_BYTES * Cut::KG * Cut::JOBS;
+    static_assert(LDS_BYTES <= 160 * 1024, "");
+    static constexpr int WAVES_PER_SIMD = Cut::KG > 1 ? 1 : D == 64 ? 3 : D == 80 ? 2 : 1;
 };
 // 32 rows of fp32 sums, lane = row
 template <int D>
@@ -779,25 +849,25 @@ DEVINL void ragged_store_part(const f32x16 (&acc)[(D + 31) / 32], float* out, lo
                     f32x4{acc[ct][4 * q], acc[ct][4 * q + 1], acc[ct][4 * q + 2], acc[ct][4 * q + 3]};
 }
 
-template <int D, int NW, typename E>
-__global__ void __launch_bounds__(NW * kRaggedJobs<NW> * 64, (RaggedDkvCfg<D, NW>::WAVES_PER_SIMD))
+template <int D, typename Cut, typename E>
+__global__ void __launch_bounds__(Cut::NT * Cut::JOBS, (RaggedDkvCfg<D, Cut>::WAVES_PER_SIMD))
 avion_ragged_dkdv_kernel(RaggedArgs a, const raw16* __restrict__ dO, const float* __restrict__ rowsc, int npad, raw16* __restrict__ dk,
                          raw16* __restrict__ dv, float* __restrict__ sums, int parts)
 {
-    using Cfg = RaggedDkvCfg<D, NW>;
+    using Cfg = RaggedDkvCfg<D, Cut>;
     using Ring = typename Cfg::Ring;
     constexpr int KS = D / 16, CT = (D + 31) / 32, OFF_G = Ring::OFF_B, ROWS = Ring::ROWS;
     extern __shared__ __attribute__((aligned(16))) char shared[];
     const int lane = threadIdx.x % 64, l32 = lane % 32, g = lane / 32;
-    const RaggedJob<NW> job(shared, Cfg::LDS_BYTES);
+    const RaggedJob<Cut> job(shared, Ring::LDS_BYTES);
     const int wave = job.wave;
     char* smem = job.smem;
     const int hk = job.id % a.Hk, part = job.id / a.Hk % parts, slot = job.id / (a.Hk * parts);
     if (slot >= a.slots) return;
-    const RaggedPlace p = ragged_place<Cfg::SHIFT>(a.off_k, a.S, a.Tk, 1, slot, lane);
+    const RaggedPlace p = ragged_place<Cut::SHIFT>(a.off_k, a.S, a.Tk, 1, slot, lane);
     const int nk = p.n;
-    if (p.block < 0 || p.block * Cfg::BN >= nk) return;
-    const int block0 = (int)p.block * Cfg::BN, k0 = block0 + wave * 32;
+    if (p.block < 0 || p.block * Cut::BLOCK >= nk) return;
+    const int block0 = (int)p.block * Cut::BLOCK, k0 = block0 + wave * 32;
     const int2 queries = a.off_k == a.off_q && a.Tk == a.Tq ? int2{p.begin, p.n} : ragged_tokens(a.off_q, a.S, a.Tq, p.i);
     const int begin_q = queries.x, nq = p.i == 0 || p.i == a.S + 1 ? 0 : queries.y;
     const bool active = k0 < nk;
@@ -809,7 +879,11 @@ avion_ragged_dkdv_kernel(RaggedArgs a, const raw16* __restrict__ dO, const float
 
     const long q_at = (long)begin_q * a.rs_q, o_at = (long)begin_q * a.Hq * D;
     Ring ring(a.q + q_at, a.rs_q, dO + o_at, (long)a.Hq * D, rowsc + ragged_scalar_at(begin_q, p.i), npad, nq, smem, wave, lane);
-    int f_head = 0, f_tile = 0;  // next to fetch
+    // the tiles of all heads, one after the other: this group's share
+    const RaggedShare share(heads * tiles, Cut::KG, job.group);
+    const int total = share.t1 - share.t0;
+    int f_head = tiles > 0 ? share.t0 / tiles : 0, f_tile = share.t0 - f_head * tiles;  // next to fetch
+    int tile = f_tile;
     auto fetch = [&](int n) {
         Ring r = ring;
         r.a += (h0 + f_head) * D;
@@ -821,7 +895,6 @@ avion_ragged_dkdv_kernel(RaggedArgs a, const raw16* __restrict__ dO, const float
             ++f_head;
         }
     };
-    const int total = heads * tiles;
     if (total > 0) fetch(0);
     frag8 kf[KS], vf[KS];
     {
@@ -892,15 +965,14 @@ avion_ragged_dkdv_kernel(RaggedArgs a, const raw16* __restrict__ dO, const float
             }
         }
     };
-    int tile = 0;
-    for (int n = 0; n < total; ++n) {
+    for (int n = 0; n < (Cut::KG == 1 ? total : share.per); ++n) {
         if constexpr (Ring::NBUF == 2) {
             if (n + 1 < total) fetch(n + 1);
         } else if (n > 0) {
             fetch(n);
             Ring::landed_barrier();
         }
-        if (active) {
+        if (active && (Cut::KG == 1 || n < total)) {
             const char* buf = ring.at(smem, n);
 #pragma unroll
             for (int hq = 0; hq < ROWS / 32; ++hq) {
@@ -911,6 +983,14 @@ avion_ragged_dkdv_kernel(RaggedArgs a, const raw16* __restrict__ dO, const float
         }
         if (++tile == tiles) tile = 0;
         Ring::landed_barrier();
+    }
+    if constexpr (Cut::KG > 1) {
+        constexpr int STORE = Cut::NW * RowStore<D, E>::BYTES;
+        static_assert(STORE + (Cut::KG - 1) * Cut::NW * CT * 4096 <= Cfg::LDS_BYTES, "exchange area");
+        add_groups<Cut::NW, Cut::KG>(job.all + STORE, dka, job.group, wave, lane, active);
+        __syncthreads();
+        add_groups<Cut::NW, Cut::KG>(job.all + STORE, dva, job.group, wave, lane, active);
+        if (job.group > 0) return;
     }
     if (!active) return;
     const int lane_now = lane_from_exec();
@@ -923,7 +1003,7 @@ avion_ragged_dkdv_kernel(RaggedArgs a, const raw16* __restrict__ dO, const float
         ragged_store_part<D>(dva, out + whole, rs, nk - k0, lane_now);
         return;
     }
-    char* region = smem + wave * RowStore<D, E>::BYTES;
+    char* region = job.all + wave * RowStore<D, E>::BYTES;
     RowStore<D, E>::run(region, dka, a.scale, dk + out_at, rs, nk - k0, lane_now);
     RowStore<D, E>::run(region, dva, dv_mul, dv + out_at, rs, nk - k0, lane_now);
 }

@@ -48,13 +48,36 @@ size_t few_bytes(const RaggedShape& s)
     return shift == 0 ? 0 : round256((size_t)few_slots(s, shift) * s.Hk * (32 * s.d + 96) * 4);
 }
 
-// wavefronts a workgroup: whole blocks of 128 rows, or of 32 where sequences are short
-int ragged_waves(long long rows, long long S) { return rows >= 64 * S ? 4 : 1; }
+enum class RaggedWay { kShort, kWide, kSplit, kSplit4 };
+// rows: of one head, over S sequences; heads: that are worked on apart.  By how many whole blocks there are (wide, split, split4; forward
+// and backward, us):
+//   from two for a compute unit on the wide cut: 1092 blocks (17 x 500 tokens, 16 heads on 4, causal) 25 + 89, 37 + 113, 59 + 163; 616
+//   (4000 and 5700, 8 heads) 159 + 436, 191 + 465, 258 + 563; 424 (300, 2000, 900, 16 heads, causal) 38 + 95, 29 + 73, 40 + 103; 410
+//   (1000 to 5000, 4 on 2 of 128 channels, causal) 136 + 397, 149 + 396, 199 + 489; 160 (2000 and 500, 8 of 128) 54 + 149, 37 + 99, 45 + 120;
+//   split4 below 96: 125 (1000, 16 heads) 21 + 53, 15 + 53, 17 + 53; 63 (700 and 1200, 4 of 80) 26 + 66, 18 + 54, 16 + 55; 39 (5000, one
+//   head) 81 + 190, 47 + 113, 37 + 86
+// and sequences of less than 64 rows on average by lone wavefronts: 2048 of 6 to 77 tokens (28 on average), 8 heads, forward 54, wide 130.
+RaggedWay ragged_way(long long rows, long long S, long long heads)
+{
+    if (rows < 64 * S) return RaggedWay::kShort;
+    const long long blocks = (rows / 128 + S / 2) * heads;
+    return blocks >= 2 * kComputeUnits ? RaggedWay::kWide : blocks >= 96 ? RaggedWay::kSplit : RaggedWay::kSplit4;
+}
+template <typename F>
+int by_way(RaggedWay way, F f)
+{
+    switch (way) {
+        case RaggedWay::kShort: return f(RaggedShort{});
+        case RaggedWay::kWide: return f(RaggedWide{});
+        case RaggedWay::kSplit: return f(RaggedSplit{});
+        default: return f(RaggedSplit4{});
+    }
+}
 
 int dkdv_parts(const RaggedShape& s)
 {
-    const int G = s.Hq / s.Hk, nw = ragged_waves(s.Tk, s.S);
-    const long long blocks = (s.Tk / (32 * nw) + s.S) * s.Hk;
+    const int G = s.Hq / s.Hk;
+    const long long blocks = (s.Tk / (s.Tk < 64 * s.S ? 32 : 128) + s.S) * s.Hk;
     int parts = 1;
     for (int p = 2; p <= G && p <= 8; ++p)
         if (G % p == 0 && blocks * parts < 4 * kComputeUnits) parts = p;
@@ -78,12 +101,6 @@ int by_head(int d, unsigned flags, F f)
         return f(Int<128>{}, fmt);
     });
 }
-template <typename F>
-int by_waves(int nw, F f)
-{
-    return nw == 4 ? f(Int<4>{}) : f(Int<1>{});
-}
-
 RaggedArgs ragged_args(const RaggedShape& s, const void* q, const void* k, const void* v, const int* off_q, const int* off_k, long long rs_q,
                        long long rs_k, long long rs_v, float scale, unsigned flags)
 {
@@ -120,10 +137,10 @@ int launch(K kernel, int lds, std::atomic<unsigned long long>& allowed, long lon
     return end_launch(what);
 }
 
-template <int NW>
-long long jobs(long long n)
+template <typename Cut>
+long long workgroups(long long jobs)
 {
-    return (n + kRaggedJobs<NW> - 1) / kRaggedJobs<NW>;
+    return (jobs + Cut::JOBS - 1) / Cut::JOBS;
 }
 
 int ragged_inputs(const RaggedShape& s, const void* q, const void* k, const void* v, const int* off_q, const int* off_k, long long rs_q,
@@ -173,19 +190,19 @@ int avion_ragged_fwd(const void* q, const void* k, const void* v, const int* off
         if (const int shift = few_shift(s)) {
             static std::atomic<unsigned long long> allowed{0}, none{0};
             float* parts = static_cast<float*>(workspace);
-            const int first = launch(avion_ragged_few_kernel<D, E>, RaggedFwdCfg<D, 1, 64, 2>::LDS_BYTES, allowed, few_slots(s, shift) * Hk, 64, st,
+            const int first = launch(avion_ragged_few_kernel<D, E>, RaggedFwdCfg<D, RaggedLone>::LDS_BYTES, allowed, few_slots(s, shift) * Hk, 64, st,
                                      "launch avion_ragged_few_kernel", a, out, lse, parts, shift);
             if (first != AVION_OK) return first;
             return launch(avion_ragged_join_kernel<D, E>, 0, none, (S + 2) * Hk, 256, st, "launch avion_ragged_join_kernel", a, out, lse,
                           (const float*)parts, shift);
         }
-        return by_waves(ragged_waves(Tq * a.G, S), [&](auto nw) {
-            constexpr int NW = decltype(nw)::value;
-            using Cfg = RaggedFwdCfg<D, NW, kRaggedRows<NW>, kRaggedBuffers<NW>>;
+        return by_way(ragged_way(Tq * a.G, S, Hk), [&](auto cut) {
+            using Cut = decltype(cut);
+            using Cfg = RaggedFwdCfg<D, Cut>;
             static std::atomic<unsigned long long> allowed{0};
-            a.slots = (int)(Tq * a.G / Cfg::BM + S + 2);
-            return launch(avion_ragged_fwd_kernel<D, NW, E>, Cfg::LDS_BYTES * kRaggedJobs<NW>, allowed, jobs<NW>((long long)a.slots * Hk),
-                          Cfg::NT * kRaggedJobs<NW>, st,
+            a.slots = (int)(Tq * a.G / Cut::BLOCK + S + 2);
+            return launch(avion_ragged_fwd_kernel<D, Cut, E>, Cfg::LDS_BYTES, allowed, workgroups<Cut>((long long)a.slots * Hk),
+                          Cut::NT * Cut::JOBS, st,
                           "launch avion_ragged_fwd_kernel", a, out, lse);
         });
     });
@@ -219,26 +236,26 @@ int avion_ragged_bwd(const void* q, const void* k, const void* v, const int* off
         constexpr int D = decltype(dim)::value;
         using E = typename decltype(fmt)::type;
         if (Tq > 0) {
-            const int first = by_waves(ragged_waves(Tq * a.G, S), [&](auto nw) {
-                constexpr int NW = decltype(nw)::value;
-                using Cfg = RaggedDqCfg<D, NW>;
+            const int first = by_way(ragged_way(Tq * a.G, S, Hk), [&](auto cut) {
+                using Cut = decltype(cut);
+                using Cfg = RaggedDqCfg<D, Cut>;
                 static std::atomic<unsigned long long> allowed{0};
-                a.slots = (int)(Tq * a.G / Cfg::BM + S + 2);
-                return launch(avion_ragged_dq_kernel<D, NW, E>, Cfg::LDS_BYTES * kRaggedJobs<NW>, allowed, jobs<NW>((long long)a.slots * Hk),
-                          Cfg::NT * kRaggedJobs<NW>, st,
+                a.slots = (int)(Tq * a.G / Cut::BLOCK + S + 2);
+                return launch(avion_ragged_dq_kernel<D, Cut, E>, Cfg::LDS_BYTES, allowed, workgroups<Cut>((long long)a.slots * Hk),
+                          Cut::NT * Cut::JOBS, st,
                               "launch avion_ragged_dq_kernel", a, static_cast<const raw16*>(o), static_cast<const raw16*>(dO), lse,
                               static_cast<raw16*>(dq), rowsc, npad);
             });
             if (first != AVION_OK) return first;
         }
         if (Tk == 0) return AVION_OK;
-        const int second = by_waves(ragged_waves(Tk, S), [&](auto nw) {
-            constexpr int NW = decltype(nw)::value;
-            using Cfg = RaggedDkvCfg<D, NW>;
+        const int second = by_way(ragged_way(Tk, S, (long long)Hk * parts), [&](auto cut) {
+            using Cut = decltype(cut);
+            using Cfg = RaggedDkvCfg<D, Cut>;
             static std::atomic<unsigned long long> allowed{0};
-            a.slots = (int)(Tk / Cfg::BN + S + 2);
-            return launch(avion_ragged_dkdv_kernel<D, NW, E>, Cfg::LDS_BYTES * kRaggedJobs<NW>, allowed, jobs<NW>((long long)a.slots * Hk * parts),
-                          Cfg::NT * kRaggedJobs<NW>, st,
+            a.slots = (int)(Tk / Cut::BLOCK + S + 2);
+            return launch(avion_ragged_dkdv_kernel<D, Cut, E>, Cfg::LDS_BYTES, allowed, workgroups<Cut>((long long)a.slots * Hk * parts),
+                          Cut::NT * Cut::JOBS, st,
                           "launch avion_ragged_dkdv_kernel", a, static_cast<const raw16*>(dO), (const float*)rowsc, npad,
                           static_cast<raw16*>(dk), static_cast<raw16*>(dv), sums, parts);
         });
