@@ -27,11 +27,12 @@ def _inputs(T, V, D, dtype, seed=0, none=0.2):
     return x, w, t.cuda()
 
 
-def _reference(x, w, t, scale, dloss, ignore=-100):
-    """Losses, dx, dw for the gradients dloss of the rows' losses, and their bounds; on the host in 64 bits."""
+def _reference(x, w, t, scale, dloss, ignore=-100, where="cpu"):
+    """Losses, dx, dw for the gradients dloss of the rows' losses, and their bounds, in 64 bits; on the host, or where it takes too long
+    there."""
     u, f32 = torch.finfo(x.dtype).eps / 2, 2.0 ** -24
     least = 2.0 ** -39 if x.dtype == F16 else 0.0
-    xd, wd, t = x.detach().cpu().double(), w.detach().cpu().double(), t.cpu().long()
+    xd, wd, t = x.detach().to(where).double(), w.detach().to(where).double(), t.to(where).long()
     T, D = xd.shape
     V = wd.shape[0]
     has = (t >= 0) & (t < V) & (t != ignore)
@@ -39,12 +40,13 @@ def _reference(x, w, t, scale, dloss, ignore=-100):
     z = scale * xd @ wd.t()
     e = scale * (D + 2) * f32 * (xd.abs() @ wd.abs().t()).amax(1) + 4 * f32 * (z.abs().amax(1) + 1)
     lse = torch.logsumexp(z, 1)
-    loss = torch.where(has, lse - z[torch.arange(T), at], torch.zeros(T).double())
-    loss_tol = torch.where(has, 2 * e + 8 * f32 * (lse.abs() + loss.abs() + 1), torch.zeros(T).double())
+    none, rows = torch.zeros(T, device=where).double(), torch.arange(T, device=where)
+    loss = torch.where(has, lse - z[rows, at], none)
+    loss_tol = torch.where(has, 2 * e + 8 * f32 * (lse.abs() + loss.abs() + 1), none)
     one = torch.zeros_like(z)
-    one[torch.arange(T), at] = 1
+    one[rows, at] = 1
     p = torch.exp(z - lse[:, None])
-    d = torch.where(has, dloss.cpu().double(), torch.zeros(T).double())[:, None]
+    d = torch.where(has, dloss.to(where).double(), none)[:, None]
     dz, size = (p - one) * d, d.abs() * (p + one)
     edz = u * dz.abs() + (3 * e[:, None] + 4 * f32) * size + least * d.abs().max()
     dx, dw = scale * dz @ wd, scale * dz.t() @ xd
@@ -52,7 +54,7 @@ def _reference(x, w, t, scale, dloss, ignore=-100):
     dw_tol = u * dw.abs() + scale * (edz + 4 * f32 * dz.abs()).t() @ xd.abs() + least
     if x.dtype == F16:      # results below its normal numbers
         dx_tol, dw_tol = dx_tol + 2.0 ** -25, dw_tol + 2.0 ** -25
-    return (loss, dx, dw), (loss_tol, 1.01 * dx_tol, 1.01 * dw_tol), int(has.sum())
+    return tuple(a.cpu() for a in (loss, dx, dw)), tuple(a.cpu() for a in (loss_tol, 1.01 * dx_tol, 1.01 * dw_tol)), int(has.sum())
 
 
 def _close(got, want, tol, name):
@@ -60,7 +62,7 @@ def _close(got, want, tol, name):
     assert (err <= tol).all(), (name, float((err / tol.clamp_min(1e-300)).max()), (err > tol).nonzero()[0].tolist())
 
 
-def _check(x, w, t, scale=1.0, reduction="mean", dloss=None):
+def _check(x, w, t, scale=1.0, reduction="mean", dloss=None, where="cpu"):
     T = x.shape[0]
     x.requires_grad_(True)
     w.requires_grad_(True)
@@ -75,7 +77,7 @@ def _check(x, w, t, scale=1.0, reduction="mean", dloss=None):
         given = torch.tensor(3.0, device="cuda")
         rows = torch.full((T,), 3.0 / max(1, has) if reduction == "mean" else 3.0)
     dx, dw = torch.autograd.grad(out, (x, w), given)
-    (loss, rx, rw), (loss_tol, tx, tw), n = _reference(x, w, t, scale, rows)
+    (loss, rx, rw), (loss_tol, tx, tw), n = _reference(x, w, t, scale, rows, where=where)
     assert n == has
     if reduction == "none":
         _close(out, loss, loss_tol, "loss")
@@ -98,6 +100,13 @@ def test_sizes(T, V, D, reduction, dtype):
 @pytest.mark.parametrize("dtype", [BF, F16], ids=["bf16", "f16"])
 def test_large_tiles(dtype):
     _check(*_inputs(4100, 4099, 72, dtype))
+
+
+@pytest.mark.parametrize("T,V,D,dtype", [(4000, 4200, 2056, BF), (300, 60000, 1104, F16), (3000, 270, 4104, BF), (213, 30000, 72, BF),
+                                         (20000, 100, 136, F16)], ids=str)
+def test_gradients_of_large_tiles_and_ranges(T, V, D, dtype):
+    """256 x 256 tiles in the gradients, whole and cut along K on either side; 128 x 128 ones cut many times."""
+    _check(*_inputs(T, V, D, dtype), where="cuda")
 
 
 @pytest.mark.parametrize("dtype", [BF, F16], ids=["bf16", "f16"])

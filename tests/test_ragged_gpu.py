@@ -128,6 +128,16 @@ def test_single_tokens_in_chunks(d, dtype):
     _check([1, 2, 1, 0, 1, 20], nk, 4, 1, d, dtype, False)
 
 
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("Hq,Hk,d,dtype,nq,nk", [
+    (32, 32, 64, BF, [300, 129, 64, 1, 200] * 4, None), (32, 16, 128, F16, [260, 130, 7], [300, 130, 90]), (64, 32, 80, BF, [150] * 10, None),
+    (12, 12, 64, F16, [300, 129, 64, 1, 600], None), (8, 8, 128, BF, [500, 700, 130], None), (20, 10, 80, F16, [513, 200, 140], [300, 900, 140]),
+    (1, 1, 64, BF, [1100, 77], None), (4, 2, 128, F16, [700], [1000])], ids=str)
+def test_every_cut(Hq, Hk, d, dtype, nq, nk, causal):
+    """Whole blocks of 128 rows (from 512 of them), two groups of wavefronts (from 96) and four."""
+    _check(nq, nq if nk is None else nk, Hq, Hk, d, dtype, causal)
+
+
 def test_many_sequences():
     g = torch.Generator().manual_seed(3)
     nq = torch.randint(0, 9, (5000,), generator=g).tolist()   # three steps of the search
