@@ -30,6 +30,8 @@ struct RaggedArgs {
     int S, Tq, Tk, Hq, Hk, G;
     unsigned g_mul, g_shift;  // of over_heads()
     int slots;
+    int done;               // backward: sequences of at most so many queries and keys are avion_ragged_whole_kernel's (0: none)
+    int* more;              // and whether there are others, as that kernel has found
     int causal;
     float cs, scale;        // scale * log2 e, scale
     // r / G for 0 <= r < 2^31: multiplication by 2^(32 + shift) / G, whose 33rd bit is the addition (a division by a number known at run
@@ -88,7 +90,7 @@ template <int NW_, int KG_, int ROWS_, int NBUF_, int JOBS_>
 struct RaggedCut {
     static constexpr int NW = NW_, KG = KG_, ROWS = ROWS_, NBUF = NBUF_, JOBS = JOBS_;
     static constexpr int BLOCK = 32 * NW, SHIFT = NW == 4 ? 7 : NW == 2 ? 6 : 5, NT = NW * KG * 64;  // rows, their logarithm, threads of a job
-    static_assert(NBUF == 2 || NW * KG == 1, "");
+    static_assert(NBUF == 2 || KG == 1, "");
 };
 using RaggedWide = RaggedCut<4, 1, 64, 2, 1>;
 using RaggedSplit = RaggedCut<2, 2, 64, 2, 1>;
@@ -672,7 +674,7 @@ avion_ragged_dq_kernel(RaggedArgs a, const raw16* __restrict__ o, const raw16* _
     const int wave = job.wave;
     char* smem = job.smem;
     const int hk = job.id % a.Hk, slot = a.slots - 1 - job.id / a.Hk;
-    if (slot < 0) return;
+    if (slot < 0 || (a.done && !*a.more)) return;
     const RaggedPlace p = ragged_place<Cut::SHIFT>(a.off_q, a.S, a.Tq, a.G, slot, lane);
     const int rows = p.n * a.G, nq = p.n;
     if (p.block < 0 || p.block * Cut::BLOCK >= rows) return;
@@ -685,6 +687,7 @@ avion_ragged_dq_kernel(RaggedArgs a, const raw16* __restrict__ o, const raw16* _
     // (offsets that serve both sides are here already)
     const int2 keys = a.off_k == a.off_q && a.Tk == a.Tq ? int2{p.begin, p.n} : ragged_tokens(a.off_k, a.S, a.Tk, p.i);
     const int begin_k = keys.x, nk = keys.y;
+    if (max(nq, nk) <= a.done) return;
     constexpr int ROWS = Ring::ROWS;
     const int ntiles = (RaggedRow(a, hk, block0 + Cut::BLOCK - 1, rows, nq, nk).keys + ROWS - 1) / ROWS;
     const bool whole = Ring::NBUF == 1 ? ntiles * ROWS <= 128 : ntiles <= 2;  // (the first group's work then)
@@ -849,6 +852,65 @@ DEVINL void ragged_store_part(const f32x16 (&acc)[(D + 31) / 32], float* out, lo
                     f32x4{acc[ct][4 * q], acc[ct][4 * q + 1], acc[ct][4 * q + 2], acc[ct][4 * q + 3]};
 }
 
+// One unit: queries 32 * hq .. of the tiles qt (Q) and gt (dO), whose scalars (lse as avion_ragged_dq_kernel leaves it, then, `rows` further,
+// -delta) stand at `scalars`; `from`: the first query that sees this lane's key, from_all: all keys of the wavefront
+template <int D, typename E>
+DEVINL void ragged_dkdv_unit(const RaggedLane<D>& at, const char* qt, const char* gt, const float* scalars, int rows, int hq, int query_base,
+                             int from, int from_all, float cs, int g, const frag8 (&kf)[D / 16], const frag8 (&vf)[D / 16],
+                             f32x16 (&dka)[(D + 31) / 32], f32x16 (&dva)[(D + 31) / 32])
+{
+    constexpr int KS = D / 16, CT = (D + 31) / 32;
+    const float* rowv = scalars + 32 * hq + 4 * g;
+            f32x16 dp, s = query_base < from_all ? query_mask_block(query_base, g, from) : f32x16_zero();
+#pragma unroll
+            for (int a4 = 0; a4 < 4; ++a4) {
+                const f32x4 d4 = *reinterpret_cast<const f32x4*>(rowv + rows + 8 * a4);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) dp[4 * a4 + e] = d4[e];
+            }
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks) {
+                const frag8 aq = at.natural(qt, hq, ks), ag = at.natural(gt, hq, ks);
+                s = E::mfma(aq, kf[ks], s);
+                dp = E::mfma(ag, vf[ks], dp);
+            }
+            f32x4 l4[4];
+#pragma unroll
+            for (int a4 = 0; a4 < 4; ++a4) l4[a4] = *reinterpret_cast<const f32x4*>(rowv + 8 * a4);
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+                frag8 tg[CT], tq[CT];
+                if constexpr (D <= 96) {
+#pragma unroll
+                    for (int ct = 0; ct < CT; ++ct) {
+                        tg[ct] = at.transposed(gt, ct, 2 * hq + half);
+                        tq[ct] = at.transposed(qt, ct, 2 * hq + half);
+                    }
+                }
+                u32x4 pf, df;
+#pragma unroll
+                for (int e = 8 * half; e < 8 * half + 8; ++e) {
+                    const float pe = fast_exp2(fmaf(s[e], cs, -l4[e / 4][e % 4]));
+                    const float ds = (std::is_same<E, F16>::value ? pe * (1.f / 256.f) : pe) * dp[e];
+                    s[e] = pe;
+                    dp[e] = ds;
+                    if (e % 2 == 1) {
+                        pf[(e / 2) % 4] = E::pack(s[e - 1], s[e]);
+                        df[(e / 2) % 4] = E::pack(dp[e - 1], dp[e]);
+                    }
+                }
+#pragma unroll
+                for (int ct = 0; ct < CT; ++ct) {
+                    if constexpr (D > 96) {
+                        tg[ct] = at.transposed(gt, ct, 2 * hq + half);
+                        tq[ct] = at.transposed(qt, ct, 2 * hq + half);
+                    }
+                    dva[ct] = E::mfma(tg[ct], as_frag8(pf), dva[ct]);
+                    dka[ct] = E::mfma(tq[ct], as_frag8(df), dka[ct]);
+                }
+            }
+}
+
 template <int D, typename Cut, typename E>
 __global__ void __launch_bounds__(Cut::NT * Cut::JOBS, (RaggedDkvCfg<D, Cut>::WAVES_PER_SIMD))
 avion_ragged_dkdv_kernel(RaggedArgs a, const raw16* __restrict__ dO, const float* __restrict__ rowsc, int npad, raw16* __restrict__ dk,
@@ -863,13 +925,14 @@ avion_ragged_dkdv_kernel(RaggedArgs a, const raw16* __restrict__ dO, const float
     const int wave = job.wave;
     char* smem = job.smem;
     const int hk = job.id % a.Hk, part = job.id / a.Hk % parts, slot = job.id / (a.Hk * parts);
-    if (slot >= a.slots) return;
+    if (slot >= a.slots || (a.done && !*a.more)) return;
     const RaggedPlace p = ragged_place<Cut::SHIFT>(a.off_k, a.S, a.Tk, 1, slot, lane);
     const int nk = p.n;
     if (p.block < 0 || p.block * Cut::BLOCK >= nk) return;
     const int block0 = (int)p.block * Cut::BLOCK, k0 = block0 + wave * 32;
     const int2 queries = a.off_k == a.off_q && a.Tk == a.Tq ? int2{p.begin, p.n} : ragged_tokens(a.off_q, a.S, a.Tq, p.i);
     const int begin_q = queries.x, nq = p.i == 0 || p.i == a.S + 1 ? 0 : queries.y;
+    if (max(nq, nk) <= a.done && p.i > 0 && p.i <= a.S) return;
     const bool active = k0 < nk;
     // first query that sees a key: this lane's, the wavefront's first and last, the workgroup's first
     auto first_query = [&](int key) { return a.causal ? max(min(key, nk - 1) - nk + nq, 0) : 0; };
@@ -914,57 +977,6 @@ avion_ragged_dkdv_kernel(RaggedArgs a, const raw16* __restrict__ dO, const float
     const float cs = a.cs;
     const RaggedLane<D> at(lane);
 
-    auto unit = [&](const char* buf, int hq, int query_base) {
-        const float* rowv = reinterpret_cast<const float*>(buf + Ring::OFF_SCALARS) + 32 * hq + 4 * g;
-        f32x16 dp, s = query_base < from_all ? query_mask_block(query_base, g, from) : f32x16_zero();
-#pragma unroll
-        for (int a4 = 0; a4 < 4; ++a4) {
-            const f32x4 d4 = *reinterpret_cast<const f32x4*>(rowv + ROWS + 8 * a4);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) dp[4 * a4 + e] = d4[e];
-        }
-#pragma unroll
-        for (int ks = 0; ks < KS; ++ks) {
-            const frag8 aq = at.natural(buf, hq, ks), ag = at.natural(buf + OFF_G, hq, ks);
-            s = E::mfma(aq, kf[ks], s);
-            dp = E::mfma(ag, vf[ks], dp);
-        }
-        f32x4 l4[4];
-#pragma unroll
-        for (int a4 = 0; a4 < 4; ++a4) l4[a4] = *reinterpret_cast<const f32x4*>(rowv + 8 * a4);
-#pragma unroll
-        for (int half = 0; half < 2; ++half) {
-            frag8 tg[CT], tq[CT];
-            if constexpr (D <= 96) {
-#pragma unroll
-                for (int ct = 0; ct < CT; ++ct) {
-                    tg[ct] = at.transposed(buf + OFF_G, ct, 2 * hq + half);
-                    tq[ct] = at.transposed(buf, ct, 2 * hq + half);
-                }
-            }
-            u32x4 pf, df;
-#pragma unroll
-            for (int e = 8 * half; e < 8 * half + 8; ++e) {
-                const float pe = fast_exp2(fmaf(s[e], cs, -l4[e / 4][e % 4]));
-                const float ds = (std::is_same<E, F16>::value ? pe * (1.f / 256.f) : pe) * dp[e];
-                s[e] = pe;
-                dp[e] = ds;
-                if (e % 2 == 1) {
-                    pf[(e / 2) % 4] = E::pack(s[e - 1], s[e]);
-                    df[(e / 2) % 4] = E::pack(dp[e - 1], dp[e]);
-                }
-            }
-#pragma unroll
-            for (int ct = 0; ct < CT; ++ct) {
-                if constexpr (D > 96) {
-                    tg[ct] = at.transposed(buf + OFF_G, ct, 2 * hq + half);
-                    tq[ct] = at.transposed(buf, ct, 2 * hq + half);
-                }
-                dva[ct] = E::mfma(tg[ct], as_frag8(pf), dva[ct]);
-                dka[ct] = E::mfma(tq[ct], as_frag8(df), dka[ct]);
-            }
-        }
-    };
     for (int n = 0; n < (Cut::KG == 1 ? total : share.per); ++n) {
         if constexpr (Ring::NBUF == 2) {
             if (n + 1 < total) fetch(n + 1);
@@ -978,7 +990,8 @@ avion_ragged_dkdv_kernel(RaggedArgs a, const raw16* __restrict__ dO, const float
             for (int hq = 0; hq < ROWS / 32; ++hq) {
                 const int query_base = (tile0 + tile) * ROWS + 32 * hq;
                 if (query_base >= nq || query_base + 32 <= from_any) continue;
-                unit(buf, hq, query_base);
+                ragged_dkdv_unit<D, E>(at, buf, buf + OFF_G, reinterpret_cast<const float*>(buf + Ring::OFF_SCALARS), ROWS, hq, query_base, from, from_all, cs, g, kf, vf,
+                                       dka, dva);
             }
         }
         if (++tile == tiles) tile = 0;
@@ -1022,4 +1035,187 @@ avion_ragged_sum_kernel(const float* __restrict__ sums, int parts, long n, raw16
         t *= second ? dv_mul : dk_mul;
         *reinterpret_cast<u32x2*>((second ? dv : dk) + i) = u32x2{E::pack(t[0], t[1]), E::pack(t[2], t[3])};
     }
+}
+
+// ------------------------------------------------------------------------------- whole short sequences
+// The backward of a sequence of at most 32 W queries and keys (and more than 16 W), heads not shared, in one pass: W wavefronts hold Q, dO,
+// K and V of one head in LDS, each first does 32 queries (dQ, and lse and delta for the others, as avion_ragged_dq_kernel), then 32
+// keys (dK, dV).  Every tensor is read once and O not at all.
+// A workgroup for each (sequence, head), which ends at once where the sequence is another launch's; but with four wavefronts and 65 KB of
+// LDS, of which a compute unit ends two at a time, a grid that fills the chip once, whose workgroups look at the lengths of 512 sequences
+// at a time and take the pairs number b, b + grid, ... of those that fit.  2048 captions of 6 to 77 tokens, 8 heads, 64 channels, in one and
+// in the other way: W = 1 36 and 52 us, 2 52 and 62, 4 (145 of them) 50 and 38; in two passes 171 for all.
+// The first launch clears `more`, the last one sets it where a sequence (or a row of none) is left for the two passes, which
+// else end at once.
+template <int D, int W>
+struct RaggedWholeCfg {
+    using Cut = RaggedCut<W, 1, 32 * W, 1, 1>;
+    using Ring = RaggedRing<D, Cut, false>;
+    static constexpr int SCALARS = 2 * Ring::BUF_BYTES, ROWS = 32 * W, SECOND = Ring::BUF_BYTES;
+    static constexpr int LDS_BYTES = SCALARS + ROWS * 8 + (D % 32 != 0 ? 64 : 0);
+    static_assert(W * RowStore<D, Bf16>::BYTES <= SCALARS, "");
+};
+// Head h of sequence i
+template <int D, int W, typename E>
+DEVINL void ragged_whole(char* smem, const RaggedArgs& a, const raw16* __restrict__ dO, const float* __restrict__ lse, raw16* __restrict__ dq,
+                         raw16* __restrict__ dk, raw16* __restrict__ dv, int i, int h, int wave, int lane)
+{
+    using Cfg = RaggedWholeCfg<D, W>;
+    using Ring = typename Cfg::Ring;
+    constexpr int KS = D / 16, CT = (D + 31) / 32;
+    // (opaque: what is made of it is not kept over the caller's loop, where it took up to 80 registers)
+    asm volatile("" : "+v"(lane));
+    const int l32 = lane % 32, g = lane / 32;
+    const int2 queries = ragged_tokens(a.off_q, a.S, a.Tq, i);
+    const int2 keys = a.off_k == a.off_q && a.Tk == a.Tq ? queries : ragged_tokens(a.off_k, a.S, a.Tk, i);
+    const int nq = queries.y, nk = keys.y;
+    const long o_at = (long)queries.x * a.Hq * D + h * D, k_at = (long)keys.x * a.Hq * D + h * D, rs = (long)a.Hq * D;
+    const Ring first(a.q + (long)queries.x * a.rs_q + h * D, a.rs_q, dO + o_at, rs, nullptr, 0, nq, smem, wave, lane);
+    const Ring second(a.k + (long)keys.x * a.rs_k + h * D, a.rs_k, a.v + (long)keys.x * a.rs_v + h * D, a.rs_v, nullptr, 0, nk,
+                      smem + Cfg::SECOND, wave, lane);
+    first.fetch(0);
+    second.fetch(0);
+    const char *qt = smem, *gt = smem + Ring::OFF_B, *kt = smem + Cfg::SECOND, *vt = kt + Ring::OFF_B;
+    float* scalars = reinterpret_cast<float*>(smem + Cfg::SCALARS);
+    const RaggedLane<D> at(lane);
+    const int row0 = 32 * wave, row = row0 + l32;
+    const bool active = row0 < nq, in = row < nq;
+    const float saved = in ? lse[(long)h * a.Tq + queries.x + row] : -INFINITY;
+    const float lc = saved == -INFINITY ? INFINITY : saved * kLog2e, cs = a.cs;
+    auto seen = [&](int r) { return a.causal ? min(max(min(r, nq - 1) + 1 + nk - nq, 0), nk) : nk; };
+    const int sees = seen(row), seen_by_all = seen(row0), seen_by_any = seen(row0 + 31);
+    f32x16 acc[CT];
+    acc_zero(acc);
+    Ring::landed_barrier();
+    if (active) {
+        frag8 qf[KS], gf[KS];
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) {
+            qf[ks] = at.natural(qt, wave, ks);
+            gf[ks] = at.natural(gt, wave, ks);
+        }
+        f32x16 s[W], dp[W];
+        float sum = 0.f;
+#pragma unroll
+        for (int u = 0; u < W; ++u) {
+            if (32 * u >= seen_by_any) continue;
+            s[u] = 32 * u + 32 > seen_by_all ? key_mask_block(32 * u, g, sees) : f32x16_zero();
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks) {
+                const frag8 ak = at.natural(kt, u, ks), av = at.natural(vt, u, ks);
+                s[u] = E::mfma(ak, qf[ks], s[u]);
+                dp[u] = E::mfma(av, gf[ks], ks == 0 ? f32x16_zero() : dp[u]);
+            }
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                s[u][e] = fast_exp2(fmaf(s[u][e], cs, -lc));
+                sum = fmaf(s[u][e], dp[u][e], sum);
+            }
+        }
+        const float dl = both_halves_sum(sum);
+        if (g == 0) {
+            scalars[row] = in ? lc - kRaggedShift<E> : INFINITY;
+            scalars[Cfg::ROWS + row] = in ? -dl : 0.f;
+        }
+#pragma unroll
+        for (int u = 0; u < W; ++u) {
+            if (32 * u >= seen_by_any) continue;
+            u32x4 df[2];
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                s[u][e] *= dp[u][e] - dl;
+                if (e % 2 == 1) df[e / 8][(e / 2) % 4] = E::pack(s[u][e - 1], s[u][e]);
+            }
+#pragma unroll
+            for (int half = 0; half < 2; ++half)
+#pragma unroll
+                for (int ct = 0; ct < CT; ++ct) acc[ct] = E::mfma(at.transposed(kt, ct, 2 * u + half), as_frag8(df[half]), acc[ct]);
+        }
+    }
+    __syncthreads();
+    const bool owns = row0 < nk;
+    f32x16 dka[CT], dva[CT];
+    acc_zero(dka);
+    acc_zero(dva);
+    if (owns) {
+        auto first_query = [&](int key) { return a.causal ? max(min(key, nk - 1) - nk + nq, 0) : 0; };
+        const int from = first_query(row), from_all = first_query(row0 + 31), from_any = first_query(row0);
+        frag8 kf[KS], vf[KS];
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) {
+            kf[ks] = at.natural(kt, wave, ks);
+            vf[ks] = at.natural(vt, wave, ks);
+        }
+#pragma unroll
+        for (int hq = 0; hq < W; ++hq)
+            if (32 * hq < nq && 32 * hq + 32 > from_any)
+                ragged_dkdv_unit<D, E>(at, qt, gt, scalars, Cfg::ROWS, hq, 32 * hq, from, from_all, cs, g, kf, vf, dka, dva);
+    }
+    __syncthreads();  // the tiles are read: rows on their way out take their place
+    char* region = smem + wave * RowStore<D, E>::BYTES;
+    if (active) RowStore<D, E>::run(region, acc, a.scale, dq + o_at + row0 * rs, rs, nq - row0, lane);
+    if (!owns) return;
+    RowStore<D, E>::run(region, dka, a.scale, dk + k_at + row0 * rs, rs, nk - row0, lane);
+    RowStore<D, E>::run(region, dva, std::is_same<E, F16>::value ? 1.f / 256.f : 1.f, dv + k_at + row0 * rs, rs, nk - row0, lane);
+}
+template <int D, int W, typename E>
+__global__ void __launch_bounds__(W * 64, D == 128 ? 1 : 2)
+avion_ragged_whole_kernel(RaggedArgs a, const raw16* __restrict__ dO, const float* __restrict__ lse, raw16* __restrict__ dq,
+                          raw16* __restrict__ dk, raw16* __restrict__ dv)
+{
+    using Cfg = RaggedWholeCfg<D, W>;
+    constexpr int LEAST = W == 1 ? -1 : 16 * W;
+    extern __shared__ __attribute__((aligned(16))) char smem[];
+    const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+    const bool same = a.off_k == a.off_q && a.Tk == a.Tq;
+    if (W == 1 && blockIdx.x == 0 && threadIdx.x == 0) *a.more = 0;
+    bool left = false;
+    // rows before the first sequence and behind the last one
+    if (Cfg::ROWS == a.done && blockIdx.x == 0)
+        left = ragged_border(a.off_q, a.S, a.Tq, 1) > 0 || ragged_border(a.off_k, a.S, a.Tk, 1) > 0 ||
+               ragged_border(a.off_q, a.S, a.Tq, a.S + 1) < a.Tq || ragged_border(a.off_k, a.S, a.Tk, a.S + 1) < a.Tk;
+    if constexpr (W < 4) {
+        const int i = blockIdx.x / a.Hq + 1, h = blockIdx.x % a.Hq;
+        int longer = ragged_tokens(a.off_q, a.S, a.Tq, i).y;
+        if (!same) longer = max(longer, ragged_tokens(a.off_k, a.S, a.Tk, i).y);
+        if (Cfg::ROWS == a.done && h == 0 && threadIdx.x == 0 && (left || longer > Cfg::ROWS)) *a.more = 1;
+        if (longer > LEAST && longer <= Cfg::ROWS) ragged_whole<D, W, E>(smem, a, dO, lse, dq, dk, dv, i, h, wave, lane);
+        return;
+    }
+    int before = 0, job = blockIdx.x;
+    for (int base = 1; base <= a.S; base += 512) {
+        unsigned long long mine[8];
+        int found = 0;
+#pragma unroll
+        for (int x = 0; x < 8; ++x) {
+            const int i = base + 64 * x + lane;
+            int longer = -1;
+            if (i <= a.S) {
+                longer = ragged_tokens(a.off_q, a.S, a.Tq, i).y;
+                if (!same) longer = max(longer, ragged_tokens(a.off_k, a.S, a.Tk, i).y);
+            }
+            mine[x] = __ballot(longer > LEAST && longer <= Cfg::ROWS);
+            found += __popcll(mine[x]);
+            left = left || longer > Cfg::ROWS;
+        }
+        for (; job < (before + found) * a.Hq; job += gridDim.x) {
+            int rank = job / a.Hq - before, i = base;
+            unsigned long long m = mine[0];
+#pragma unroll
+            for (int x = 0; x < 7; ++x) {  // the word of it
+                const int n = __popcll(m);
+                if (rank >= n && i == base + 64 * x) {
+                    rank -= n;
+                    i += 64;
+                    m = mine[x + 1];
+                }
+            }
+            for (; rank > 0; --rank) m &= m - 1;
+            i = __builtin_amdgcn_readfirstlane(i + __ffsll(m) - 1);
+            ragged_whole<D, W, E>(smem, a, dO, lse, dq, dk, dv, i, job % a.Hq, wave, lane);
+            __syncthreads();  // before the next one's tiles
+        }
+        before += found;
+    }
+    if (Cfg::ROWS == a.done && blockIdx.x == 0 && __any(left) && threadIdx.x == 0) *a.more = 1;
 }

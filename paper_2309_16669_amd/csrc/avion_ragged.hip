@@ -56,10 +56,11 @@ enum class RaggedWay { kShort, kWide, kSplit, kSplit4 };
 //   (1000 to 5000, 4 on 2 of 128 channels, causal) 136 + 397, 149 + 396, 199 + 489; 160 (2000 and 500, 8 of 128) 54 + 149, 37 + 99, 45 + 120;
 //   split4 below 96: 125 (1000, 16 heads) 21 + 53, 15 + 53, 17 + 53; 63 (700 and 1200, 4 of 80) 26 + 66, 18 + 54, 16 + 55; 39 (5000, one
 //   head) 81 + 190, 47 + 113, 37 + 86
-// and sequences of less than 64 rows on average by lone wavefronts: 2048 of 6 to 77 tokens (28 on average), 8 heads, forward 54, wide 130.
+// and sequences of less than 80 rows on average by lone wavefronts: 2048 of 6 to 77 tokens (28 on average), 8 heads, forward 54, wide 130;
+// 131000 tokens in sequences of 40, 64, 77, 96, 128: 120, 115, 129, 181, 137, wide 164, 134, 160, 126, 172.
 RaggedWay ragged_way(long long rows, long long S, long long heads)
 {
-    if (rows < 64 * S) return RaggedWay::kShort;
+    if (rows < 80 * S) return RaggedWay::kShort;
     const long long blocks = (rows / 128 + S / 2) * heads;
     return blocks >= 2 * kComputeUnits ? RaggedWay::kWide : blocks >= 96 ? RaggedWay::kSplit : RaggedWay::kSplit4;
 }
@@ -77,7 +78,7 @@ int by_way(RaggedWay way, F f)
 int dkdv_parts(const RaggedShape& s)
 {
     const int G = s.Hq / s.Hk;
-    const long long blocks = (s.Tk / (s.Tk < 64 * s.S ? 32 : 128) + s.S) * s.Hk;
+    const long long blocks = (s.Tk / (s.Tk < 80 * s.S ? 32 : 128) + s.S) * s.Hk;
     int parts = 1;
     for (int p = 2; p <= G && p <= 8; ++p)
         if (G % p == 0 && blocks * parts < 4 * kComputeUnits) parts = p;
@@ -211,7 +212,7 @@ int avion_ragged_fwd(const void* q, const void* k, const void* v, const int* off
 size_t avion_ragged_bwd_workspace_bytes(long long Tq, long long Tk, long long S, int Hq, int Hk, int d)
 {
     const RaggedShape s{Tq, Tk, S, Hq, Hk, d};
-    return ragged_check(s) == AVION_OK ? scalar_bytes(s) + parts_bytes(s) : 0;
+    return ragged_check(s) == AVION_OK ? scalar_bytes(s) + parts_bytes(s) + 256 : 0;
 }
 
 int avion_ragged_bwd(const void* q, const void* k, const void* v, const int* offsets_q, const int* offsets_k, const void* o,
@@ -235,6 +236,26 @@ int avion_ragged_bwd(const void* q, const void* k, const void* v, const int* off
     return by_head(d, flags, [&](auto dim, auto fmt) {
         constexpr int D = decltype(dim)::value;
         using E = typename decltype(fmt)::type;
+        // short sequences whose heads are their own: whole, up to 64 tokens (of 128 channels) or 128; the two passes below take the others
+        if (a.G == 1 && S > 0 && std::max(Tq, Tk) <= 128 * S) {
+            a.done = D == 128 ? 64 : 128;
+            a.more = reinterpret_cast<int*>(static_cast<char*>(workspace) + scalar_bytes(s) + parts_bytes(s));
+            int rc3 = AVION_OK;
+            const auto whole = [&](auto w) {
+                constexpr int W = decltype(w)::value;
+                static std::atomic<unsigned long long> allowed{0};
+                if (rc3 == AVION_OK)
+                    rc3 = launch(avion_ragged_whole_kernel<D, W, E>, RaggedWholeCfg<D, W>::LDS_BYTES, allowed,
+                                 W < 4 ? S * Hq : std::min<long long>(S * Hq, kComputeUnits * (160 * 1024 / RaggedWholeCfg<D, W>::LDS_BYTES)),
+                                 W * 64, st,
+                                 "launch avion_ragged_whole_kernel", a, static_cast<const raw16*>(dO), lse, static_cast<raw16*>(dq),
+                                 static_cast<raw16*>(dk), static_cast<raw16*>(dv));
+            };
+            whole(Int<1>{});
+            whole(Int<2>{});
+            if constexpr (D < 128) whole(Int<4>{});
+            if (rc3 != AVION_OK) return rc3;
+        }
         if (Tq > 0) {
             const int first = by_way(ragged_way(Tq * a.G, S, Hk), [&](auto cut) {
                 using Cut = decltype(cut);

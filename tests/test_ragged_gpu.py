@@ -138,6 +138,15 @@ def test_every_cut(Hq, Hk, d, dtype, nq, nk, causal):
     _check(nq, nq if nk is None else nk, Hq, Hk, d, dtype, causal)
 
 
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("d,dtype", [(64, BF), (64, F16), (80, BF), (128, F16)], ids=str)
+@pytest.mark.parametrize("nq,nk", [([1, 31, 32, 33, 63, 64, 65, 0, 5, 96], None), ([5, 40, 64, 1, 0, 33, 2], [9, 20, 64, 33, 12, 0, 70])], ids=str)
+def test_short_sequences_whole(nq, nk, d, dtype, causal):
+    """Up to 32, to 64 and above, mixed; fewer keys than queries, none on either side."""
+    pad = [3] * 20          # short on average
+    _check(nq + pad, (nq if nk is None else nk) + pad, 2, 2, d, dtype, causal)
+
+
 def test_many_sequences():
     g = torch.Generator().manual_seed(3)
     nq = torch.randint(0, 9, (5000,), generator=g).tolist()   # three steps of the search
