@@ -1055,20 +1055,17 @@ struct RaggedWholeCfg {
     static constexpr int LDS_BYTES = SCALARS + ROWS * 8 + (D % 32 != 0 ? 64 : 0);
     static_assert(W * RowStore<D, Bf16>::BYTES <= SCALARS, "");
 };
-// Head h of sequence i
+// Head h of one sequence: its queries and keys, (begin, number)
 template <int D, int W, typename E>
 DEVINL void ragged_whole(char* smem, const RaggedArgs& a, const raw16* __restrict__ dO, const float* __restrict__ lse, raw16* __restrict__ dq,
-                         raw16* __restrict__ dk, raw16* __restrict__ dv, int i, int h, int wave, int lane)
+                         raw16* __restrict__ dk, raw16* __restrict__ dv, int2 queries, int2 keys, int h, int wave, int lane)
 {
     using Cfg = RaggedWholeCfg<D, W>;
     using Ring = typename Cfg::Ring;
     constexpr int KS = D / 16, CT = (D + 31) / 32;
     // (opaque: what is made of it is not kept over the caller's loop, where it took up to 80 registers)
-    asm volatile("" : "+v"(lane));
-    const int l32 = lane % 32, g = lane / 32;
-    const int2 queries = ragged_tokens(a.off_q, a.S, a.Tq, i);
-    const int2 keys = a.off_k == a.off_q && a.Tk == a.Tq ? queries : ragged_tokens(a.off_k, a.S, a.Tk, i);
-    const int nq = queries.y, nk = keys.y;
+    if constexpr (W == 4) asm volatile("" : "+v"(lane));
+    const int l32 = lane % 32, g = lane / 32, nq = queries.y, nk = keys.y;
     const long o_at = (long)queries.x * a.Hq * D + h * D, k_at = (long)keys.x * a.Hq * D + h * D, rs = (long)a.Hq * D;
     const Ring first(a.q + (long)queries.x * a.rs_q + h * D, a.rs_q, dO + o_at, rs, nullptr, 0, nq, smem, wave, lane);
     const Ring second(a.k + (long)keys.x * a.rs_k + h * D, a.rs_k, a.v + (long)keys.x * a.rs_v + h * D, a.rs_v, nullptr, 0, nk,
@@ -1176,10 +1173,10 @@ avion_ragged_whole_kernel(RaggedArgs a, const raw16* __restrict__ dO, const floa
                ragged_border(a.off_q, a.S, a.Tq, a.S + 1) < a.Tq || ragged_border(a.off_k, a.S, a.Tk, a.S + 1) < a.Tk;
     if constexpr (W < 4) {
         const int i = blockIdx.x / a.Hq + 1, h = blockIdx.x % a.Hq;
-        int longer = ragged_tokens(a.off_q, a.S, a.Tq, i).y;
-        if (!same) longer = max(longer, ragged_tokens(a.off_k, a.S, a.Tk, i).y);
+        const int2 queries = ragged_tokens(a.off_q, a.S, a.Tq, i), keys = same ? queries : ragged_tokens(a.off_k, a.S, a.Tk, i);
+        const int longer = max(queries.y, keys.y);
         if (Cfg::ROWS == a.done && h == 0 && threadIdx.x == 0 && (left || longer > Cfg::ROWS)) *a.more = 1;
-        if (longer > LEAST && longer <= Cfg::ROWS) ragged_whole<D, W, E>(smem, a, dO, lse, dq, dk, dv, i, h, wave, lane);
+        if (longer > LEAST && longer <= Cfg::ROWS) ragged_whole<D, W, E>(smem, a, dO, lse, dq, dk, dv, queries, keys, h, wave, lane);
         return;
     }
     int before = 0, job = blockIdx.x;
@@ -1212,7 +1209,8 @@ avion_ragged_whole_kernel(RaggedArgs a, const raw16* __restrict__ dO, const floa
             }
             for (; rank > 0; --rank) m &= m - 1;
             i = __builtin_amdgcn_readfirstlane(i + __ffsll(m) - 1);
-            ragged_whole<D, W, E>(smem, a, dO, lse, dq, dk, dv, i, job % a.Hq, wave, lane);
+            const int2 queries = ragged_tokens(a.off_q, a.S, a.Tq, i), keys = same ? queries : ragged_tokens(a.off_k, a.S, a.Tk, i);
+            ragged_whole<D, W, E>(smem, a, dO, lse, dq, dk, dv, queries, keys, job % a.Hq, wave, lane);
             __syncthreads();  // before the next one's tiles
         }
         before += found;
