@@ -13,10 +13,10 @@
 //   of 8 consecutive k: rows of 128 bytes with ds_read_b128, their eight 16-byte chunks permuted by a XOR with bits 1..3 of the row
 //   number; rows of k with two transposing ds_read_b64_tr_b16 (4 k each), their 64-byte units permuted by a XOR with the row
 //   number mod 4.  Both meet distinct banks.
-//   Two buffers of a step (four where a compute unit has one workgroup and each step's loads would be waited for: 2048 x 2048 x 512
-//   forward 10.5 -> 7 us); fragments of 16 k are read while the 16 before are multiplied; before a step's last ones the next step
-//   is awaited, and this one's buffer, which everybody then holds in registers, is filled again.  Steps of a workgroup's tiles
-//   form one stream, so that the next tile's first steps are on their way during the end of a tile.
+//   Two buffers of a step (four in tiles of 128 gained nothing where a compute unit has one workgroup: 2048 x 2048 x 512 forward 10.4 and
+//   11.6 us); fragments of 16 k are read while the 16 before are multiplied; before a step's last ones the next step is awaited, and
+//   this one's buffer, which everybody then holds in registers, is filled again.  Steps of a workgroup's tiles form one stream, so that
+//   the next tile's first steps are on their way during the end of a tile.
 //   8192 cubed: 1212 to 1258 TFLOP/s by the operands' layouts (the library's product 1301); matrix units busy 62 % of the cycles, LDS
 //   reads 23 %, at 1.8 GHz.
 //   A is the contiguous index of the result: a lane's accumulators are 4 consecutive a of one row b.
@@ -112,9 +112,9 @@ struct LossTile {
     }
 };
 
-template <Along AA, Along AB, int TA_, int TB_, int WA_, int WB_, int ST_>
+template <Along AA, Along AB, int TA_, int TB_, int WA_, int WB_>
 struct LossCfg {
-    static constexpr int TA = TA_, TB = TB_, WA = WA_, WB = WB_, ST = ST_;
+    static constexpr int TA = TA_, TB = TB_, WA = WA_, WB = WB_;
     static constexpr int WAVES = WA * WB, NT = WAVES * 64;
     static constexpr int NI = TA / WA / 32, MI = TB / WB / 32;  // 32 x 32 tiles of a wavefront
     using TileA = LossTile<AA, TA, WAVES>;
@@ -122,18 +122,16 @@ struct LossCfg {
     static constexpr int STAGE = TileA::BYTES + TileB::BYTES;
     static constexpr int LOADS = TileA::PER + TileB::PER;  // of a wavefront for a step
     static constexpr int OUT_ROW = NI * 64 + 16, OUT_BYTES = (NI == 2 ? 16 : 32) * OUT_ROW;  // a wavefront's rows on their way out
-    static constexpr int LDS_BYTES = ST * STAGE + WAVES * OUT_BYTES;
-    static_assert(LDS_BYTES <= 160 * 1024 && TileA::BLOCKS % WAVES == 0 && TileB::BLOCKS % WAVES == 0 && ST >= 2 && ST <= 4 && 3 * LOADS < 64, "");
+    static constexpr int LDS_BYTES = 2 * STAGE + WAVES * OUT_BYTES;
+    static_assert(LDS_BYTES <= 160 * 1024 && TileA::BLOCKS % WAVES == 0 && TileB::BLOCKS % WAVES == 0 && LOADS < 64, "");
 };
 
 // All but this wavefront's youngest `left` steps of LOADS loads have arrived (stores and other loads among them are younger than they
 // count here: that waits for more, never for less), its LDS reads are done, and so everybody's.
-template <int ST, int LOADS>
+template <int LOADS>
 DEVINL void loss_landed_barrier(int left)
 {
-    if (ST > 3 && left >= 3) asm volatile("s_waitcnt vmcnt(%0)\n\ts_waitcnt lgkmcnt(0)\n\ts_barrier" ::"i"(3 * LOADS) : "memory");
-    else if (ST > 2 && left == 2) asm volatile("s_waitcnt vmcnt(%0)\n\ts_waitcnt lgkmcnt(0)\n\ts_barrier" ::"i"(2 * LOADS) : "memory");
-    else if (left == 1) asm volatile("s_waitcnt vmcnt(%0)\n\ts_waitcnt lgkmcnt(0)\n\ts_barrier" ::"i"(LOADS) : "memory");
+    if (left == 1) asm volatile("s_waitcnt vmcnt(%0)\n\ts_waitcnt lgkmcnt(0)\n\ts_barrier" ::"i"(LOADS) : "memory");
     else asm volatile("s_waitcnt vmcnt(0)\n\ts_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
 }
 
@@ -156,7 +154,7 @@ template <typename Cfg, typename E, typename Place, typename Begin, typename Don
 DEVINL void loss_product(char* smem, const LossOperand& opa, const LossOperand& opb, int K, int count, int wave, int lane, Place place, Begin begin,
                          Done done)
 {
-    constexpr int MI = Cfg::MI, NI = Cfg::NI, ST = Cfg::ST;
+    constexpr int MI = Cfg::MI, NI = Cfg::NI;
     if (count <= 0) return;
     const int wa = wave % Cfg::WA, wb = wave / Cfg::WA;
     typename Cfg::TileA ta(opa, K, wave, lane);
@@ -182,13 +180,11 @@ DEVINL void loss_product(char* smem, const LossOperand& opa, const LossOperand& 
     };
     int ahead = 0;  // steps asked for behind the one that is awaited next
     fetch(0);
-#pragma unroll
-    for (int i = 1; i < ST; ++i)
-        if (f_n < count) {
-            fetch(i);
-            ++ahead;
-        }
-    loss_landed_barrier<ST, Cfg::LOADS>(ahead);
+    if (f_n < count) {
+        fetch(1);
+        ++ahead;
+    }
+    loss_landed_barrier<Cfg::LOADS>(ahead);
     frag8 fa[NI], fb[MI];
     auto read = [&](int buf, int ks) {
         const unsigned from = lds + buf * Cfg::STAGE;
@@ -217,12 +213,12 @@ DEVINL void loss_product(char* smem, const LossOperand& opa, const LossOperand& 
                 if (ks < 3) {
                     read(buf, ks + 1);
                 } else if (k + 1 < p.k1 || n + 1 < count) {
-                    loss_landed_barrier<ST, Cfg::LOADS>(--ahead);  // the next step is there, and this one in everybody's registers
+                    loss_landed_barrier<Cfg::LOADS>(--ahead);  // the next step is there, and this one in everybody's registers
                     if (f_n < count) {
                         fetch(buf);
                         ++ahead;
                     }
-                    read(buf + 1 == ST ? 0 : buf + 1, 0);
+                    read(buf ^ 1, 0);
                 }
                 __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
@@ -231,7 +227,7 @@ DEVINL void loss_product(char* smem, const LossOperand& opa, const LossOperand& 
                     for (int j = 0; j < NI; ++j) acc[i][j] = E::mfma(ca[j], cb[i], acc[i][j]);
                 __builtin_amdgcn_sched_barrier(0);
             }
-            buf = buf + 1 == ST ? 0 : buf + 1;
+            buf ^= 1;
         }
         done(n, p.a0, p.b0, acc);
     }
@@ -290,17 +286,18 @@ constexpr float kLossNone = -3.0e38f;
 // A workgroup takes TB rows through one of `slabs` runs of vocabulary tiles.  A lane holds, for each of its MI rows, the maximum and sum
 // (base 2, scaled) over the columns that its registers hold; they meet once, at the end: parts [slabs][T] of (maximum, sum).  The lane
 // that holds a row's target leaves its logit.
-template <int TA, int TB, int WA, int WB, int ST, typename E>
+template <int TA, int TB, int WA, int WB, typename E>
 __global__ void __launch_bounds__(WA* WB * 64, 2)
-avion_loss_fwd_kernel(LossArgs a, float2* __restrict__ parts, float* __restrict__ hit, int slabs)
+avion_loss_fwd_kernel(LossArgs a, float2* __restrict__ parts, float* __restrict__ hit, int slabs, unsigned* __restrict__ ticket)
 {
-    using Cfg = LossCfg<Along::kK, Along::kK, TA, TB, WA, WB, ST>;
+    using Cfg = LossCfg<Along::kK, Along::kK, TA, TB, WA, WB>;
     constexpr int MI = Cfg::MI, NI = Cfg::NI;
     extern __shared__ __attribute__((aligned(16))) char smem[];
     __shared__ float2 meet[WA][TB];
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), l32 = lane % 32, g = lane / 32;
     const int wa = wave % WA, wb = wave / WA;
     const int blocks = (a.T + TB - 1) / TB, logical = xcd_local_id(blockIdx.x, blocks * slabs);
+    if (blockIdx.x == 0 && threadIdx.x == 0) *ticket = 0;  // of the next launch
     if (logical < 0) return;
     int slab, block;
     loss_place(logical, slabs, blocks, slab, block);
@@ -372,11 +369,13 @@ avion_loss_fwd_kernel(LossArgs a, float2* __restrict__ parts, float* __restrict_
 }
 
 // Rows joined over the runs, LANES lanes a row: lse, loss; and, for a mean or sum, the losses of 256 / LANES rows and how many of them
-// have a target.  (391 runs of 5 rows: one lane 70 us, 16 lanes 8.)
+// have a target; the workgroup that comes last (a counter says which) adds these up, in their order.  (391 runs of 5 rows: one lane 70
+// us, 16 lanes 8; the total in a launch of its own 3 to 5 us more.)
+// total[0]: the mean over the rows with a target (0 where there is none) or the sum, total[1]: how many
 template <int LANES>
 __global__ void __launch_bounds__(256)
 avion_loss_join_kernel(LossArgs a, const float2* __restrict__ parts, const float* __restrict__ hit, int slabs, float* __restrict__ loss,
-                       float* __restrict__ lse, double2* __restrict__ sums)
+                       float* __restrict__ lse, double2* __restrict__ sums, unsigned* __restrict__ ticket, bool mean, float* __restrict__ total)
 {
     const int lane = threadIdx.x % LANES, m = blockIdx.x * (256 / LANES) + threadIdx.x / LANES;
     __shared__ double2 meet[256 / LANES];
@@ -405,7 +404,8 @@ avion_loss_join_kernel(LossArgs a, const float2* __restrict__ parts, const float
         }
         mine = double2{of, has ? 1. : 0.};
     }
-    if (!sums) return;
+    if (!total) return;
+    __shared__ bool last;
     if (lane == 0) meet[threadIdx.x / LANES] = mine;
     __syncthreads();
     if (threadIdx.x == 0) {
@@ -414,33 +414,36 @@ avion_loss_join_kernel(LossArgs a, const float2* __restrict__ parts, const float
             t.x += meet[i].x;
             t.y += meet[i].y;
         }
-        sums[blockIdx.x] = t;
+        // written through to where every XCD sees it, and there before the ticket; a fence would write the whole L2 back
+        __hip_atomic_store(&sums[blockIdx.x].x, t.x, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        __hip_atomic_store(&sums[blockIdx.x].y, t.y, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        last = __hip_atomic_fetch_add(ticket, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == gridDim.x - 1;
     }
-}
-// total[0]: the mean over the rows with a target (0 where there is none) or the sum, total[1]: how many
-__global__ void __launch_bounds__(256)
-avion_loss_total_kernel(const double2* __restrict__ sums, int n, bool mean, float* __restrict__ total)
-{
-    __shared__ double2 meet[256];
+    __syncthreads();
+    if (!last) return;
+    __shared__ double2 all[256];
     double2 t{0., 0.};
-    for (int i = threadIdx.x; i < n; i += 256) {
-        t.x += sums[i].x;
-        t.y += sums[i].y;
+    for (int i = threadIdx.x; i < (int)gridDim.x; i += 256) {
+        t.x += __hip_atomic_load(&sums[i].x, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        t.y += __hip_atomic_load(&sums[i].y, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     }
-    meet[threadIdx.x] = t;
+    all[threadIdx.x] = t;
     __syncthreads();
     for (int half = 128; half > 0; half /= 2) {
         if ((int)threadIdx.x < half) {
-            meet[threadIdx.x].x += meet[threadIdx.x + half].x;
-            meet[threadIdx.x].y += meet[threadIdx.x + half].y;
+            all[threadIdx.x].x += all[threadIdx.x + half].x;
+            all[threadIdx.x].y += all[threadIdx.x + half].y;
         }
         __syncthreads();
     }
     if (threadIdx.x == 0) {
-        total[0] = (float)(mean ? meet[0].y > 0. ? meet[0].x / meet[0].y : 0. : meet[0].x);
-        total[1] = (float)meet[0].y;
+        total[0] = (float)(mean ? all[0].y > 0. ? all[0].x / all[0].y : 0. : all[0].x);
+        total[1] = (float)all[0].y;
     }
 }
+// of no rows at all
+__global__ void avion_loss_none_kernel(float* __restrict__ total) { total[threadIdx.x] = 0.f; }
 
 // ------------------------------------------------------------------------------------------ backward
 // dz is held as (softmax - onehot) r_m S with r_m = dloss_m / max |dloss|, S = 1 for bf16 and 2^14 for fp16 (a softmax over many
@@ -501,20 +504,20 @@ avion_loss_rows_kernel(LossArgs a, const float* __restrict__ lse, const float* _
 // used, it made every tile wait once more.  Columns of a target are rare (a wavefront's 32 x 64 logits of 50000 columns hold one in 25),
 // and so are columns past the end: both have a copy of the loop.
 constexpr int kLossRowBytes = 3 * 1024;
-template <int TA, int TB, int WA, int WB, int ST, typename E>
+template <int TA, int TB, int WA, int WB, typename E>
 __global__ void __launch_bounds__(WA* WB * 64, 2)
 avion_loss_dz_kernel(LossArgs a, const int* __restrict__ rowdata, int padded, int v0, int n, raw16* __restrict__ dz, long ld)
 {
-    using Cfg = LossCfg<Along::kK, Along::kK, TA, TB, WA, WB, ST>;
+    using Cfg = LossCfg<Along::kK, Along::kK, TA, TB, WA, WB>;
     constexpr int MI = Cfg::MI, NI = Cfg::NI;
     extern __shared__ __attribute__((aligned(16))) char smem[];
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), l32 = lane % 32, g = lane / 32;
     const int wa = wave % WA, wb = wave / WA;
     const int na = (n + TA - 1) / TA, nb = (a.T + TB - 1) / TB, ntiles = na * nb, per = (ntiles + 7) / 8, together = gridDim.x / 8;
     const int first = blockIdx.x % 8 * per + blockIdx.x / 8, end = min(ntiles, (blockIdx.x % 8 + 1) * per);
-    char* stage = smem + ST * Cfg::STAGE + wave * Cfg::OUT_BYTES;
-    char* rowmem = smem + Cfg::LDS_BYTES;  // of ST + 1 tiles: where a tile is one step, those of ST more are on their way at its end
-    static_assert(Cfg::LDS_BYTES + (ST + 1) * kLossRowBytes <= 160 * 1024 && TB <= 256, "");
+    char* stage = smem + 2 * Cfg::STAGE + wave * Cfg::OUT_BYTES;
+    char* rowmem = smem + Cfg::LDS_BYTES;  // of three tiles: where a tile is one step, those of two more are on their way at its end
+    static_assert(Cfg::LDS_BYTES + 3 * kLossRowBytes <= 160 * 1024 && TB <= 256, "");
     const LossOperand opa{a.w + (long)v0 * a.rs_w, a.rs_w, n, 0}, opb{a.x, a.rs_x, a.T, 0};
     loss_product<Cfg, E>(
         smem, opa, opb, a.D, first < end ? (end - first + together - 1) / together : 0, wave, lane,
@@ -527,7 +530,7 @@ avion_loss_dz_kernel(LossArgs a, const int* __restrict__ rowdata, int padded, in
         },
         [&](int t, const LossPlace& p) {
             if (wave < 3)
-                load_to_lds16(RawBuffer(rowdata + (long)wave * padded + p.b0, TB * 4), lds_address(rowmem) + t % (ST + 1) * kLossRowBytes + wave * 1024, lane * 16);
+                load_to_lds16(RawBuffer(rowdata + (long)wave * padded + p.b0, TB * 4), lds_address(rowmem) + t % 3 * kLossRowBytes + wave * 1024, lane * 16);
         },
         [&](int t, int a0, int b0, f32x16(&acc)[MI][NI]) {
             const int from = a0 + wa * NI * 32;
@@ -535,7 +538,7 @@ avion_loss_dz_kernel(LossArgs a, const int* __restrict__ rowdata, int padded, in
 #pragma unroll
             for (int i = 0; i < MI; ++i) {
                 const int in = (wb * MI + i) * 32, m0 = b0 + in;
-                const char* data = rowmem + t % (ST + 1) * kLossRowBytes + (in + l32) * 4;
+                const char* data = rowmem + t % 3 * kLossRowBytes + (in + l32) * 4;
                 const int target = *reinterpret_cast<const int*>(data), at = target >= 0 ? target - v0 - from : -1;
                 const float lc = *reinterpret_cast<const float*>(data + 1024), r = *reinterpret_cast<const float*>(data + 2048);
                 raw16* out = dz + (long)m0 * ld + from;
@@ -575,7 +578,7 @@ DEVINL void loss_grad(char* smem, const LossGrad& p, float mul, int first, int s
     const int wa = wave % Cfg::WA, wb = wave / Cfg::WA, cols = p.a.extent;
     const int na = (cols + Cfg::TA - 1) / Cfg::TA, nb = (p.rows + Cfg::TB - 1) / Cfg::TB, items = na * nb * p.splits;
     const int steps = (p.K + kLossStep - 1) / kLossStep;
-    char* stage = smem + Cfg::ST * Cfg::STAGE + wave * Cfg::OUT_BYTES;
+    char* stage = smem + 2 * Cfg::STAGE + wave * Cfg::OUT_BYTES;
     loss_product<Cfg, E>(
         smem, p.a, p.b, p.K, first < items ? (items - first + step - 1) / step : 0, wave, lane,
         [&](int n) {
@@ -610,7 +613,7 @@ DEVINL void loss_grad(char* smem, const LossGrad& p, float mul, int first, int s
             }
         });
 }
-template <int TA, int TB, int WA, int WB, int ST, typename E>
+template <int TA, int TB, int WA, int WB, typename E>
 __global__ void __launch_bounds__(WA* WB * 64, 2)
 avion_loss_grad_kernel(LossGrad dx, LossGrad dw, const float* __restrict__ factors, int items_x)
 {
@@ -619,40 +622,51 @@ avion_loss_grad_kernel(LossGrad dx, LossGrad dw, const float* __restrict__ facto
     // an XCD's workgroups (they go round) take neighbouring tiles
     const int id = groups % 8 == 0 ? (int)(blockIdx.x % 8) * (groups / 8) + blockIdx.x / 8 : blockIdx.x;
     const float mul = factors[0];
-    loss_grad<LossCfg<Along::kIndex, Along::kK, TA, TB, WA, WB, ST>, E>(smem, dx, mul, id < items_x ? id : items_x, groups, wave, lane);
+    loss_grad<LossCfg<Along::kIndex, Along::kK, TA, TB, WA, WB>, E>(smem, dx, mul, id < items_x ? id : items_x, groups, wave, lane);
     // dw's tiles follow dx's in the same round
     const int taken = items_x % groups, start = id >= taken ? id - taken : id - taken + groups;
-    loss_grad<LossCfg<Along::kIndex, Along::kIndex, TA, TB, WA, WB, ST>, E>(smem, dw, mul, start, groups, wave, lane);
+    loss_grad<LossCfg<Along::kIndex, Along::kIndex, TA, TB, WA, WB>, E>(smem, dw, mul, start, groups, wave, lane);
 }
 
-// The planes' sum, in their order, times factors[0]: a wavefront a 32 x 32 block
+// The planes' sum, in their order, times factors[0]: a wavefront a 32 x 32 block, of either product
+struct LossPlanes {
+    const float* sum;
+    int planes, rows;
+    raw16* out;
+};
 template <int TA, int TB, int WA, int WB, typename E>
 __global__ void __launch_bounds__(256)
-avion_loss_sum_kernel(const float* __restrict__ sum, int planes, int rows, int cols, const float* __restrict__ factors, raw16* __restrict__ out)
+avion_loss_sum_kernel(LossPlanes x, LossPlanes w, int cols, const float* __restrict__ factors)
 {
-    using Cfg = LossCfg<Along::kK, Along::kK, TA, TB, WA, WB, 2>;
+    using Cfg = LossCfg<Along::kK, Along::kK, TA, TB, WA, WB>;
     constexpr int MI = Cfg::MI, NI = Cfg::NI, BLOCKS = Cfg::WAVES * MI * NI;
-    const int lane = threadIdx.x % 64, na = (cols + TA - 1) / TA, nb = (rows + TB - 1) / TB;
-    const long unit = blockIdx.x * 4L + threadIdx.x / 64, units = (long)na * nb * BLOCKS;
+    const int lane = threadIdx.x % 64, na = (cols + TA - 1) / TA;
+    long unit = blockIdx.x * 4L + threadIdx.x / 64;
+    const long of_x = (long)na * ((x.rows + TB - 1) / TB) * BLOCKS;
+    const bool second = unit >= of_x;
+    const LossPlanes& p = second ? w : x;
+    if (second) unit -= of_x;
+    const int nb = (p.rows + TB - 1) / TB;
+    const long units = (long)na * nb * BLOCKS;
     if (unit >= units) return;
     const int tile = (int)(unit / BLOCKS), in = (int)(unit - (long)tile * BLOCKS), wave = in / (MI * NI), i = in / NI % MI, j = in % NI;
     int a0, b0;
     loss_place(tile, na, nb, a0, b0);
     const int row = b0 * TB + (wave / WA * MI + i) * 32 + lane % 32, col = a0 * TA + (wave % WA * NI + j) * 32 + 4 * (lane / 32);
-    const f32x4* at = reinterpret_cast<const f32x4*>(sum) + unit * 256 + lane;
+    const f32x4* at = reinterpret_cast<const f32x4*>(p.sum) + unit * 256 + lane;
     f32x4 t[4];
 #pragma unroll
     for (int c = 0; c < 4; ++c) t[c] = at[c * 64];
-    for (int p = 1; p < planes; ++p) {
+    for (int k = 1; k < p.planes; ++k) {
         at += units * 256;
 #pragma unroll
         for (int c = 0; c < 4; ++c) t[c] += at[c * 64];
     }
     const float mul = factors[0];
-    if (row >= rows) return;
+    if (row >= p.rows) return;
 #pragma unroll
     for (int c = 0; c < 4; ++c)
         if (col + 8 * c < cols)
-            *reinterpret_cast<u32x2*>(out + (long)row * cols + col + 8 * c) =
+            *reinterpret_cast<u32x2*>(p.out + (long)row * cols + col + 8 * c) =
                 u32x2{E::pack(t[c][0] * mul, t[c][1] * mul), E::pack(t[c][2] * mul, t[c][3] * mul)};
 }

@@ -31,18 +31,16 @@ LossTiles loss_tiles(long long rows, long long cols)
     if (rows <= 32) return LossTiles::kFew;
     return ceil_div(rows, 256) * ceil_div(cols, 256) < kComputeUnits ? LossTiles::kSmall : LossTiles::kLarge;
 }
-// tile height and width, wavefronts, buffers
-template <int TB_, int ST_>
+// tile height and width, wavefronts
+template <int TB_>
 struct Tile {
-    static constexpr int TB = TB_, TA = TB == 256 ? 256 : 128, WA = TB == 128 ? 2 : 4, WB = TB == 32 ? 1 : 2, ST = ST_;
+    static constexpr int TB = TB_, TA = TB == 256 ? 256 : 128, WA = TB == 128 ? 2 : 4, WB = TB == 32 ? 1 : 2;
 };
-// f(Tile) for `tiles` tiles of a product: four buffers where each compute unit has one workgroup at most
 template <typename F>
-int by_tiles(LossTiles t, long long tiles, F f)
+int by_tiles(LossTiles t, F f)
 {
-    if (t == LossTiles::kFew) return f(Tile<32, 2>{});
-    if (t == LossTiles::kLarge) return f(Tile<256, 2>{});
-    return tiles <= kComputeUnits ? f(Tile<128, 4>{}) : f(Tile<128, 2>{});
+    if (t == LossTiles::kFew) return f(Tile<32>{});
+    return t == LossTiles::kLarge ? f(Tile<256>{}) : f(Tile<128>{});
 }
 
 // runs of vocabulary tiles in the forward: enough workgroups for the chip, whole rounds of them where there are many
@@ -54,12 +52,13 @@ int loss_slabs(const LossShape& s)
     return (int)std::max<long long>(1, std::min<long long>(tiles, at_once / blocks));
 }
 struct LossForward {  // offsets of its workspace
-    size_t hit, sums, bytes;
+    size_t hit, sums, ticket, bytes;
     LossForward(const LossShape& s)
     {
         hit = round256((size_t)loss_slabs(s) * s.T * sizeof(float2));
         sums = hit + round256((size_t)s.T * 4);
-        bytes = std::max<size_t>(256, sums + round256((size_t)ceil_div(s.T, 4) * sizeof(double2)));
+        ticket = sums + round256((size_t)ceil_div(s.T, 4) * sizeof(double2));
+        bytes = ticket + 256;
     }
 };
 
@@ -182,32 +181,33 @@ int avion_linear_ce_fwd(const void* x, const void* w, const void* targets, float
     char* ws = static_cast<char*>(workspace);
     float2* parts = reinterpret_cast<float2*>(ws);
     float* hit = reinterpret_cast<float*>(ws + at.hit);
-    double2* sums = total ? reinterpret_cast<double2*>(ws + at.sums) : nullptr;
+    double2* sums = reinterpret_cast<double2*>(ws + at.sums);
+    unsigned* ticket = reinterpret_cast<unsigned*>(ws + at.ticket);
+    const bool mean = (flags & AVION_FLAG_MEAN) != 0;
     static std::atomic<unsigned long long> none{0};
     if (T > 0) {
         const int slabs = loss_slabs(s);
         const int first = by_element(flags, [&](auto fmt) {
             using E = typename decltype(fmt)::type;
             const LossTiles t = loss_tiles(T, V);
-            return by_tiles(t, t == LossTiles::kSmall ? ceil_div(T, 128) * slabs : 0, [&](auto tile) {
+            return by_tiles(t, [&](auto tile) {
                 using X = decltype(tile);
-                using Cfg = LossCfg<Along::kK, Along::kK, X::TA, X::TB, X::WA, X::WB, X::ST>;
+                using Cfg = LossCfg<Along::kK, Along::kK, X::TA, X::TB, X::WA, X::WB>;
                 static std::atomic<unsigned long long> allowed{0};
-                return launch(avion_loss_fwd_kernel<X::TA, X::TB, X::WA, X::WB, X::ST, E>, X::ST * Cfg::STAGE, allowed,
-                              ceil_div(ceil_div(T, X::TB) * slabs, 8) * 8, Cfg::NT, st, "launch avion_loss_fwd_kernel", a, parts, hit, slabs);
+                return launch(avion_loss_fwd_kernel<X::TA, X::TB, X::WA, X::WB, E>, 2 * Cfg::STAGE, allowed,
+                              ceil_div(ceil_div(T, X::TB) * slabs, 8) * 8, Cfg::NT, st, "launch avion_loss_fwd_kernel", a, parts, hit, slabs, ticket);
             });
         });
         if (first != AVION_OK) return first;
-        const int second =
-            slabs > 32 ? launch(avion_loss_join_kernel<64>, 0, none, ceil_div(T, 4), 256, st, "launch avion_loss_join_kernel", a, (const float2*)parts,
-                                (const float*)hit, slabs, loss, lse, sums)
-                       : launch(avion_loss_join_kernel<16>, 0, none, ceil_div(T, 16), 256, st, "launch avion_loss_join_kernel", a, (const float2*)parts,
-                                (const float*)hit, slabs, loss, lse, sums);
-        if (second != AVION_OK) return second;
+        const auto join = [&](auto lanes) {
+            constexpr int LANES = decltype(lanes)::value;
+            return launch(avion_loss_join_kernel<LANES>, 0, none, ceil_div(T, 256 / LANES), 256, st, "launch avion_loss_join_kernel", a,
+                          (const float2*)parts, (const float*)hit, slabs, loss, lse, sums, ticket, mean, total);
+        };
+        return slabs > 32 ? join(std::integral_constant<int, 64>{}) : join(std::integral_constant<int, 16>{});
     }
     if (!total) return AVION_OK;
-    return launch(avion_loss_total_kernel, 0, none, 1, 256, st, "launch avion_loss_total_kernel", (const double2*)sums, (int)ceil_div(T, T > 0 && loss_slabs(s) > 32 ? 4 : 16),
-                  (flags & AVION_FLAG_MEAN) != 0, total);
+    return launch(avion_loss_none_kernel, 0, none, 1, 2, st, "launch avion_loss_none_kernel", total);
 }
 
 size_t avion_linear_ce_bwd_workspace_bytes(long long T, long long V, int D)
@@ -250,11 +250,11 @@ int avion_linear_ce_bwd(const void* x, const void* w, const void* targets, const
         for (long long v0 = 0; v0 < V && rc2 == AVION_OK; v0 += piece) {
             const long long n = std::min(piece, V - v0), held = std::min(ld, ceil_div(n, 8) * 8);
             if (T > 0)
-                rc2 = by_tiles(loss_tiles(T, n), ceil_div(T, 128) * ceil_div(n, 128), [&](auto tile) {
+                rc2 = by_tiles(loss_tiles(T, n), [&](auto tile) {
                     using X = decltype(tile);
-                    using Cfg = LossCfg<Along::kK, Along::kK, X::TA, X::TB, X::WA, X::WB, X::ST>;
+                    using Cfg = LossCfg<Along::kK, Along::kK, X::TA, X::TB, X::WA, X::WB>;
                     static std::atomic<unsigned long long> allowed{0};
-                    return launch(avion_loss_dz_kernel<X::TA, X::TB, X::WA, X::WB, X::ST, E>, Cfg::LDS_BYTES + (X::ST + 1) * kLossRowBytes, allowed,
+                    return launch(avion_loss_dz_kernel<X::TA, X::TB, X::WA, X::WB, E>, Cfg::LDS_BYTES + 3 * kLossRowBytes, allowed,
                                   persistent(ceil_div(T, X::TB) * ceil_div(n, X::TA), X::TB), Cfg::NT, st, "launch avion_loss_dz_kernel", a,
                                   (const int*)rows, padded, (int)v0, (int)n, dz, (long)ld);
                 });
@@ -270,33 +270,27 @@ int avion_linear_ce_bwd(const void* x, const void* w, const void* targets, const
             gx.splits = (int)std::min<long long>(gx.splits, ceil_div(held, kLossStep));
             if (!dx || T == 0) gx.rows = 0;
             if (!dw) gw.rows = 0;
-            const auto by_grads = [&](auto f) {
-                if (grads_large(s, piece)) return f(Tile<256, 2>{});
-                const long long items = ceil_div(gx.rows, 128) * ceil_div(D, 128) * gx.splits + ceil_div(gw.rows, 128) * ceil_div(D, 128) * gw.splits;
-                return items <= kComputeUnits ? f(Tile<128, 4>{}) : f(Tile<128, 2>{});
-            };
+            const auto by_grads = [&](auto f) { return grads_large(s, piece) ? f(Tile<256>{}) : f(Tile<128>{}); };
             if (gx.rows > 0 || gw.rows > 0)
                 rc2 = by_grads([&](auto tile) {
                     using X = decltype(tile);
-                    using Cfg = LossCfg<Along::kIndex, Along::kIndex, X::TA, X::TB, X::WA, X::WB, X::ST>;
+                    using Cfg = LossCfg<Along::kIndex, Along::kIndex, X::TA, X::TB, X::WA, X::WB>;
                     static std::atomic<unsigned long long> allowed{0};
                     const long long items_x = ceil_div(gx.rows, X::TB) * ceil_div(D, X::TA) * gx.splits;
                     const long long items_w = ceil_div(gw.rows, X::TB) * ceil_div(D, X::TA) * gw.splits;
-                    return launch(avion_loss_grad_kernel<X::TA, X::TB, X::WA, X::WB, X::ST, E>, Cfg::LDS_BYTES, allowed,
+                    return launch(avion_loss_grad_kernel<X::TA, X::TB, X::WA, X::WB, E>, Cfg::LDS_BYTES, allowed,
                                   persistent(items_x + items_w, X::TB), Cfg::NT, st, "launch avion_loss_grad_kernel", gx, gw,
                                   (const float*)factors, (int)items_x);
                 });
-            const auto finish = [&](const LossGrad& g, int planes, void* to) {
-                return by_grads([&](auto tile) {
+            const LossPlanes px{gx.sum, grad_splits(s, piece, false), at.planes_x && last ? gx.rows : 0, static_cast<raw16*>(dx)};
+            const LossPlanes pw{gw.sum, gw.splits, at.planes_w ? gw.rows : 0, static_cast<raw16*>(dw) + v0 * D};
+            if (rc2 == AVION_OK && (px.rows > 0 || pw.rows > 0))
+                rc2 = by_grads([&](auto tile) {
                     using X = decltype(tile);
-                    const long long blocks = ceil_div(g.rows, X::TB) * ceil_div(D, X::TA) * (X::TA / 32) * (X::TB / 32);
+                    const long long blocks = (ceil_div(px.rows, X::TB) + ceil_div(pw.rows, X::TB)) * ceil_div(D, X::TA) * (X::TA / 32) * (X::TB / 32);
                     return launch(avion_loss_sum_kernel<X::TA, X::TB, X::WA, X::WB, E>, 0, none, ceil_div(blocks, 4), 256, st,
-                                  "launch avion_loss_sum_kernel", (const float*)g.sum, planes, g.rows, D, (const float*)factors,
-                                  static_cast<raw16*>(to));
+                                  "launch avion_loss_sum_kernel", px, pw, D, (const float*)factors);
                 });
-            };
-            if (rc2 == AVION_OK && at.planes_x && last && gx.rows > 0) rc2 = finish(gx, grad_splits(s, piece, false), dx);
-            if (rc2 == AVION_OK && at.planes_w && gw.rows > 0) rc2 = finish(gw, gw.splits, static_cast<raw16*>(dw) + v0 * D);
         }
         return rc2;
     });
