@@ -75,7 +75,8 @@ DEVINL RaggedPlace ragged_place(const int* off, int S, int T, int mul, long slot
 // side come first and rows of no sequence last, all blocks of a sequence together, the last of them first where it sees the most
 // (BACK): the launch then ends with its shortest workgroups.  A lane holds an interval's length and counts the blocks of those before it.
 // More sequences keep their order, from the last one on with BACK.
-// 16 sequences of 196 to 3136 tokens, 12 heads, 64 channels, ordered and not: XXX
+// 16 sequences of 196 to 3136 tokens, 12 heads, 64 channels, forward, dQ and dK/dV: 82 + 93 + 113 us, in their own order 103 + 116 + 132; the
+// search costs half a microsecond at 37 sequences.
 constexpr int kRaggedOrdered = 61;
 template <int SHIFT, bool BACK>
 DEVINL RaggedPlace ragged_turn(const int* off, int S, int T, int mul, const int* other, int others, int slots, int turn, int lane)

@@ -51,11 +51,11 @@ size_t few_bytes(const RaggedShape& s)
 enum class RaggedWay { kShort, kWide, kSplit, kSplit4 };
 // rows: of one head, over S sequences; heads: that are worked on apart.  By how many whole blocks there are (wide, split, split4; forward
 // and backward, us):
-//   from two for a compute unit on the wide cut: 1092 blocks (17 x 500 tokens, 16 heads on 4, causal) 25 + 89, 37 + 113, 59 + 163; 616
-//   (4000 and 5700, 8 heads) 159 + 436, 191 + 465, 258 + 563; 424 (300, 2000, 900, 16 heads, causal) 38 + 95, 29 + 73, 40 + 103; 410
-//   (1000 to 5000, 4 on 2 of 128 channels, causal) 136 + 397, 149 + 396, 199 + 489; 160 (2000 and 500, 8 of 128) 54 + 149, 37 + 99, 45 + 120;
-//   split4 below 96: 125 (1000, 16 heads) 21 + 53, 15 + 53, 17 + 53; 63 (700 and 1200, 4 of 80) 26 + 66, 18 + 54, 16 + 55; 39 (5000, one
-//   head) 81 + 190, 47 + 113, 37 + 86
+//   from two for a compute unit on the wide cut: 1092 blocks (17 x 500 tokens, 16 heads on 4, causal) 26 + 88, 37 + 102, 60 + 133; 608
+//   (4000 and 5700, 8 heads) 148 + 377, 164 + 409, 220 + 504; 416 (300, 2000, 900, 16 heads, causal) 39 + 97, 26 + 70, 38 + 101; 410
+//   (1000 to 5000, 4 on 2 of 128 channels, causal) 125 + 372, 131 + 358, 181 + 464; 160 (2000 and 500, 8 of 128) 52 + 148, 36 + 96, 46 + 120;
+//   split4 below 96: 112 (1000, 16 heads) 22 + 56, 15 + 54, 16 + 55; 60 (700 and 1200, 4 of 80) 26 + 67, 18 + 55, 16 + 54; 39 (5000, one
+//   head) 82 + 192, 48 + 115, 38 + 86
 // and sequences of less than 80 rows on average by lone wavefronts: 2048 of 6 to 77 tokens (28 on average), 8 heads, forward 54, wide 130;
 // 131000 tokens in sequences of 40, 64, 77, 96, 128: 120, 115, 129, 181, 137, wide 164, 134, 160, 126, 172.
 RaggedWay ragged_way(long long rows, long long S, long long heads)
@@ -75,13 +75,18 @@ int by_way(RaggedWay way, F f)
     }
 }
 
+// dK and dV of a shared key head: by how many workgroups the query heads are walked, whose fp32 sums are added up afterwards.  Up to four
+// workgroups for a compute unit, but past one only while the sums (16 bytes a channel and part, at the memory's 5 TB/s) cost less than a
+// quarter of the walk (10 operations for a query, head and channel, at 0.7 PFLOP/s).  Whole backward, 1, 2, 4 and 8 parts, us: 400 tokens,
+// 2 heads on one, 432 blocks 67, 81; 500, 4 on one, 220 blocks 101, 98, 109; 9000, 8 on one, 140 blocks 2055, 1451, 1318, 1115; 760, 8 on one,
+// 474 blocks 298, 252, 253, 288
 int dkdv_parts(const RaggedShape& s)
 {
     const int G = s.Hq / s.Hk;
     const long long blocks = (s.Tk / (s.Tk < 80 * s.S ? 32 : 128) + s.S) * s.Hk;
     int parts = 1;
     for (int p = 2; p <= G && p <= 8; ++p)
-        if (G % p == 0 && blocks * parts < 4 * kComputeUnits) parts = p;
+        if (G % p == 0 && blocks * parts < 4 * kComputeUnits && (blocks * parts < kComputeUnits || 900 * p * s.S <= s.Tq * G)) parts = p;
     return parts;
 }
 long long ragged_npad(const RaggedShape& s) { return (s.Tq / 64 + s.S + 2) * 64; }
