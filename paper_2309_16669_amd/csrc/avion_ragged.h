@@ -108,8 +108,8 @@ DEVINL int2 ragged_tokens(const int* off, int S, int T, int i)
 // How a kernel cuts its work.  A workgroup: NW wavefronts of 32 rows (keys in dK/dV) each, in KG groups that walk over a share of the
 // other side's tiles through buffers of their own and add their sums up at the end; tiles of ROWS tokens in NBUF buffers.
 //   RaggedWide   the usual one
-//   RaggedSplit, RaggedSplit4   where such workgroups would leave compute units without work, or with one of two: shorter walks of fewer
-//                rows
+//   RaggedSplit, RaggedSplitHalf, RaggedSplit4   where such workgroups would leave compute units without work, or with one of two:
+//                shorter walks of fewer rows
 //   RaggedShort  sequences of less than two wavefronts' rows: one wavefront with one buffer of 32 rows, so that 16 of a compute unit
 //                wait for their loads at once; four of them, which know nothing of each other, to a workgroup (JOBS)
 //   RaggedLone   single tokens behind long caches
@@ -121,6 +121,7 @@ struct RaggedCut {
 };
 using RaggedWide = RaggedCut<4, 1, 64, 2, 1>;
 using RaggedSplit = RaggedCut<2, 2, 64, 2, 1>;
+using RaggedSplitHalf = RaggedCut<2, 2, 32, 2, 1>;
 using RaggedSplit4 = RaggedCut<1, 4, 32, 2, 1>;
 using RaggedShort = RaggedCut<1, 1, 32, 1, 4>;
 using RaggedLone = RaggedCut<1, 1, 64, 2, 1>;

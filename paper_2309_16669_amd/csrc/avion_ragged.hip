@@ -48,25 +48,32 @@ size_t few_bytes(const RaggedShape& s)
     return shift == 0 ? 0 : round256((size_t)few_slots(s, shift) * s.Hk * (32 * s.d + 96) * 4);
 }
 
-enum class RaggedWay { kShort, kWide, kSplit, kSplit4 };
+enum class RaggedWay { kShort, kWide, kSplitHalf, kSplit, kSplit4 };
 // rows: of one head, over S sequences; heads: that are worked on apart.  By how many whole blocks there are (wide, split, split4; forward
 // and backward, us):
 //   from two for a compute unit on the wide cut: 1092 blocks (17 x 500 tokens, 16 heads on 4, causal) 26 + 88, 37 + 102, 60 + 133; 608
 //   (4000 and 5700, 8 heads) 148 + 377, 164 + 409, 220 + 504; 416 (300, 2000, 900, 16 heads, causal) 39 + 97, 26 + 70, 38 + 101; 410
 //   (1000 to 5000, 4 on 2 of 128 channels, causal) 125 + 372, 131 + 358, 181 + 464; 160 (2000 and 500, 8 of 128) 52 + 148, 36 + 96, 46 + 120;
+//   split of more than 64 channels with tiles of 32 keys from one block for a compute unit, as two workgroups of one then work at a time and
+//   else one does: 410 (1000 to 5000, as above) 93 + 275; 386 (12 x 500, 8 on 2 of 80) 19 + 62, 31 + 83; 284 (2000 and 1000, 12 on 4 of 80)
+//   34 + 94, 37 + 100, wide 43 + 115; 218 (200 to 1000, 8 on 2 of 80) 19 + 61, 19 + 58; 160 (as above) 40 + 111;
 //   split4 below 96: 112 (1000, 16 heads) 22 + 56, 15 + 54, 16 + 55; 60 (700 and 1200, 4 of 80) 26 + 67, 18 + 55, 16 + 54; 39 (5000, one
 //   head) 82 + 192, 48 + 115, 38 + 86
 // and sequences of less than 80 rows on average by lone wavefronts: 2048 of 6 to 77 tokens (28 on average), 8 heads, forward 54, wide 130;
 // 131000 tokens in sequences of 40, 64, 77, 96, 128: 120, 115, 129, 181, 137, wide 164, 134, 160, 126, 172.
-RaggedWay ragged_way(long long rows, long long S, long long heads)
+RaggedWay ragged_way(int d, long long rows, long long S, long long heads)
 {
     if (rows < 80 * S) return RaggedWay::kShort;
     const long long blocks = (rows / 128 + S / 2) * heads;
-    return blocks >= 2 * kComputeUnits ? RaggedWay::kWide : blocks >= 96 ? RaggedWay::kSplit : RaggedWay::kSplit4;
+    if (blocks >= 2 * kComputeUnits) return RaggedWay::kWide;
+    if (d > 64 && blocks >= kComputeUnits) return RaggedWay::kSplitHalf;
+    return blocks >= 96 ? RaggedWay::kSplit : RaggedWay::kSplit4;
 }
-template <typename F>
+template <int D, typename F>
 int by_way(RaggedWay way, F f)
 {
+    if constexpr (D > 64)
+        if (way == RaggedWay::kSplitHalf) return f(RaggedSplitHalf{});
     switch (way) {
         case RaggedWay::kShort: return f(RaggedShort{});
         case RaggedWay::kWide: return f(RaggedWide{});
@@ -202,7 +209,7 @@ int avion_ragged_fwd(const void* q, const void* k, const void* v, const int* off
             return launch(avion_ragged_join_kernel<D, E>, 0, none, (S + 2) * Hk, 256, st, "launch avion_ragged_join_kernel", a, out, lse,
                           (const float*)parts, shift);
         }
-        return by_way(ragged_way(Tq * a.G, S, Hk), [&](auto cut) {
+        return by_way<D>(ragged_way(d, Tq * a.G, S, Hk), [&](auto cut) {
             using Cut = decltype(cut);
             using Cfg = RaggedFwdCfg<D, Cut>;
             static std::atomic<unsigned long long> allowed{0};
@@ -262,7 +269,7 @@ int avion_ragged_bwd(const void* q, const void* k, const void* v, const int* off
             if (rc3 != AVION_OK) return rc3;
         }
         if (Tq > 0) {
-            const int first = by_way(ragged_way(Tq * a.G, S, Hk), [&](auto cut) {
+            const int first = by_way<D>(ragged_way(d, Tq * a.G, S, Hk), [&](auto cut) {
                 using Cut = decltype(cut);
                 using Cfg = RaggedDqCfg<D, Cut>;
                 static std::atomic<unsigned long long> allowed{0};
@@ -275,7 +282,7 @@ int avion_ragged_bwd(const void* q, const void* k, const void* v, const int* off
             if (first != AVION_OK) return first;
         }
         if (Tk == 0) return AVION_OK;
-        const int second = by_way(ragged_way(Tk, S, (long long)Hk * parts), [&](auto cut) {
+        const int second = by_way<D>(ragged_way(d, Tk, S, (long long)Hk * parts), [&](auto cut) {
             using Cut = decltype(cut);
             using Cfg = RaggedDkvCfg<D, Cut>;
             static std::atomic<unsigned long long> allowed{0};

@@ -132,9 +132,11 @@ def test_single_tokens_in_chunks(d, dtype):
 @pytest.mark.parametrize("Hq,Hk,d,dtype,nq,nk", [
     (32, 32, 64, BF, [300, 129, 64, 1, 200] * 4, None), (32, 16, 128, F16, [260, 130, 7], [300, 130, 90]), (64, 32, 80, BF, [150] * 10, None),
     (12, 12, 64, F16, [300, 129, 64, 1, 600], None), (8, 8, 128, BF, [500, 700, 130], None), (20, 10, 80, F16, [513, 200, 140], [300, 900, 140]),
-    (1, 1, 64, BF, [1100, 77], None), (4, 2, 128, F16, [700], [1000])], ids=str)
+    (1, 1, 64, BF, [1100, 77], None), (4, 2, 128, F16, [700], [1000]),
+    (40, 40, 80, BF, [300, 500, 130], None), (26, 13, 128, F16, [700, 300, 513], [700, 0, 600])], ids=str)
 def test_every_cut(Hq, Hk, d, dtype, nq, nk, causal):
-    """Whole blocks of 128 rows (from 512 of them), two groups of wavefronts (from 96) and four."""
+    """Whole blocks of 128 rows (from 512 of them), two groups of wavefronts (from 96, above 64 channels with smaller tiles from 256) and
+    four."""
     _check(nq, nq if nk is None else nk, Hq, Hk, d, dtype, causal)
 
 
@@ -145,6 +147,19 @@ def test_short_sequences_whole(nq, nk, d, dtype, causal):
     """Up to 32, to 64 and above, mixed; fewer keys than queries, none on either side."""
     pad = [3] * 20          # short on average
     _check(nq + pad, (nq if nk is None else nk) + pad, 2, 2, d, dtype, causal)
+
+
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("S", [1, 2, 7, 61, 62])
+@pytest.mark.parametrize("same", [True, False])
+def test_order_of_sequences(S, same, causal):
+    """Up to 61 sequences begin by length: ties, and none on one side."""
+    g = torch.Generator().manual_seed(S)
+    nq = [150] * S if same else torch.randint(0, 300, (S,), generator=g).tolist()
+    nk = nq if same else torch.randint(0, 300, (S,), generator=g).tolist()
+    if not same:
+        nq[S // 2], nk[S // 3] = 0, 0
+    _check(nq, nk, 2, 1, 64, BF, causal)
 
 
 def test_many_sequences():
