@@ -3,6 +3,8 @@ from __future__ import annotations
 
 import os
 import subprocess
+import tempfile
+from concurrent.futures import ThreadPoolExecutor
 
 PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
@@ -11,7 +13,7 @@ LIB = os.path.join(PKG, "libavion_attn.so")
 TORCH_MODULE = os.path.join(PKG, "_avion_torch.so")
 
 HIPCC_FLAGS = [
-    "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",
+    "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
     # packed fp32 VALU forms stay off for every device function
     "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
     # MFMA accumulators live in ordinary VGPRs (no AGPR copies around the softmax arithmetic)
@@ -40,11 +42,18 @@ def is_stale() -> bool:
 
 def build_library(verbose: bool = False, extra_flags=()) -> str:
     hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
-    cmd = [hipcc, *HIPCC_FLAGS, *extra_flags, "-I", os.path.join(ROOT, "include"), "-I", CSRC,
-           "-o", LIB, *sources()]
-    if verbose:
-        print(" ".join(cmd), flush=True)
-    subprocess.run(cmd, check=True)
+    def run(*cmd):
+        if verbose:
+            print(" ".join(cmd), flush=True)
+        subprocess.run(cmd, check=True)
+
+    # the sources side by side, then one link
+    with tempfile.TemporaryDirectory() as objects, ThreadPoolExecutor(min(8, os.cpu_count() or 1)) as pool:
+        def compiled(source):
+            to = os.path.join(objects, os.path.basename(source) + ".o")
+            run(hipcc, *HIPCC_FLAGS, *extra_flags, "-I", os.path.join(ROOT, "include"), "-I", CSRC, "-c", "-o", to, source)
+            return to
+        run(hipcc, "--offload-arch=gfx950", "-shared", "-fPIC", *extra_flags, "-o", LIB, *pool.map(compiled, sources()))
     return LIB
 
 
