@@ -386,7 +386,7 @@ int avion_linear_fp8(const void *x8, const float *x_scale, const void *w8, const
  *   freqs     : fp32 [pairs], radians a step;   sections: `axes` numbers on the HOST, their sum is `pairs`
  *   Pairs are channels j and pairs + j, or with AVION_FLAG_INTERLEAVED 2 j and 2 j + 1.  Channels from 2 * pairs on are copied.
  *   AVION_FLAG_INVERSE: -theta, the backward (the gradient of q is the inverse turn of the gradient of yq).
- *   d a multiple of 8 up to 4096; pairs a multiple of 8 up to 512, 2 * pairs <= d; axes <= 4; T < 2^31 - 8; rs a multiple of 8
+ *   d a multiple of 8 up to 4096; pairs a multiple of 8 up to 512, 2 * pairs <= d; axes <= 4; T <= 2^27 - 8; rs a multiple of 8
  * Angles are formed in 64 bits and reduced to one turn before they are rounded, so far positions lose nothing; one rounding of the
  * result.  T = 0: nothing happens.  Pointers 16-byte aligned (positions and freqs naturally).
  */
@@ -412,10 +412,10 @@ int avion_rotary(const void *q, const void *k, const void *positions, const floa
  * offset, from the last one on) have o = 0 and lse = -inf, and gradients 0.  What a sequence holds reaches no other one.  Within a
  * sequence infinities and NaN are not checked and propagate, past a mask too.  Offsets are not checked: values outside 0 .. T are
  * taken as the nearest of these, and decreasing ones give rows without a defined value, never an access outside the tensors.
- *   Tq, Tk up to 2^28, S up to 2^20, Tq * Hq / Hk up to 2^30; scale as for avion_attn_fwd
+ *   Tq, Tk up to 2^28, S up to 2^20, Tq * Hq / Hk up to 2^30, (Tq * Hq / Hk + Tk + 128 S) * Hk below 2^31 - 2^16 * Hk; scale as for avion_attn_fwd
  *   workspace: 256-byte aligned, avion_ragged_fwd_workspace_bytes / _bwd_workspace_bytes bytes of these sizes (0: unsupported),
- *   contents ignored and left unspecified; calls that overlap in time must not share one.  The forward's may be NULL where every
- *   sequence has as many queries as keys.
+ *   contents ignored and left unspecified; calls that overlap in time must not share one.  The forward's may be NULL where
+ *   Tq = Tk.
  * Arithmetic as avion_attn_fwd and _bwd (sums, statistics and LSE in fp32; weights and dS rounded to the format before a product),
  * with a running maximum; no atomics: the same sizes and offsets give the same bits.
  */
@@ -447,12 +447,12 @@ int avion_ragged_bwd(const void *q, const void *k, const void *v, const int *off
  *   dloss   : in, fp32 [T], or with AVION_FLAG_ONE_GRADIENT one number, the gradient of total[0]; then with AVION_FLAG_MEAN it is divided
  *             by total[1]
  *   dx, dw  : out, fully overwritten; either may be NULL (not both)
- *   scale > 0 and finite; D a multiple of 8 up to 65536; T, V up to 2^28; rs up to 2^20
+ *   scale > 0 and finite; D a multiple of 8 up to 65536; T below 2^28, V up to 2^28; rs up to 2^20
  *   workspace: 256-byte aligned, avion_linear_ce_fwd_workspace_bytes / _bwd_workspace_bytes bytes (0: unsupported), contents ignored and
  *   left unspecified; calls that overlap in time must not share one.  The backward takes the vocabulary in pieces: dz of one piece
  *   (at most 1 GB, or 256 columns) and, where there are several, dx in fp32 lie in it
  * Logits, statistics and sums in fp32, dz rounded to the format before its products (fp16: scaled by the largest |dloss| and 2^14,
- * so that small probabilities keep their bits), results rounded once.  No atomics: the same sizes give the same bits.
+ * so that small probabilities keep their bits), results rounded once.  No order of atomics decides a sum: the same sizes give the same bits.
  * T = 0: total and dw become zeros.  Pointers 16-byte aligned (fp32 ones and targets naturally).
  */
 #define AVION_FLAG_MEAN 256u

@@ -20,7 +20,7 @@ struct LossShape {
 int loss_check(const LossShape& s)
 {
     if (s.T < 0 || s.V < 1 || s.D < 1) return AVION_EINVAL;
-    if (s.D % 8 != 0 || s.D > (1 << 16) || s.T > (1 << 28) || s.V > (1 << 28)) return AVION_EUNSUPPORTED;
+    if (s.D % 8 != 0 || s.D > (1 << 16) || s.T >= (1 << 28) || s.V > (1 << 28)) return AVION_EUNSUPPORTED;
     return AVION_OK;
 }
 long long ceil_div(long long a, long long b) { return (a + b - 1) / b; }

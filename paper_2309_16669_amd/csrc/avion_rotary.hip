@@ -42,7 +42,7 @@ int avion_rotary(const void* q, const void* k, const void* positions, const floa
         for (int j = i; j < kRotaryAxes; ++j) a.ends[j] = (int)std::min<long long>(sum, 1 << 20);
     }
     if (sum != pairs) return AVION_EINVAL;
-    if (T > (1LL << 31) - 8 || Hq > (1 << 16) || Hk > (1 << 16) || rs_q > (1LL << 31) || rs_k > (1LL << 31)) return AVION_EUNSUPPORTED;
+    if (T > (1LL << 27) - 8 || Hq > (1 << 16) || Hk > (1 << 16) || rs_q > (1LL << 31) || rs_k > (1LL << 31)) return AVION_EUNSUPPORTED;
     if (rs_q % 8 != 0 || (Hk > 0 && rs_k % 8 != 0)) return AVION_EUNSUPPORTED;
     if (T == 0) return AVION_OK;
     if (!q || !positions || !freqs || !yq || (Hk > 0 && (!k || !yk))) return AVION_EINVAL;

@@ -43,6 +43,7 @@ SHAPES = [(dict(Tq=-1), av.EINVAL), (dict(Tk=-1), av.EINVAL), (dict(S=-1), av.EI
           (dict(scale=INF), av.EINVAL), (dict(scale=1e-30), av.EINVAL), (dict(flags=4), av.EINVAL), (dict(flags=1 << 20), av.EINVAL),
           (dict(d=72, rs_q=288, rs_k=144, rs_v=144), av.EUNSUPPORTED), (dict(d=96, rs_q=384, rs_k=192, rs_v=192), av.EUNSUPPORTED),
           (dict(Tq=(1 << 28) + 1), av.EUNSUPPORTED), (dict(Tk=(1 << 28) + 1), av.EUNSUPPORTED), (dict(S=(1 << 20) + 1), av.EUNSUPPORTED),
+          (dict(S=1 << 20, Hq=32, Hk=32, rs_q=2048, rs_k=2048, rs_v=2048), av.EUNSUPPORTED),
           (dict(Tq=1 << 28, Hq=16), av.EUNSUPPORTED), (dict(rs_q=255), av.EINVAL), (dict(rs_k=64), av.EINVAL), (dict(rs_v=127), av.EINVAL),
           (dict(rs_q=260), av.EUNSUPPORTED), (dict(rs_v=(1 << 23) + 8), av.EUNSUPPORTED), (dict(q=None), av.EINVAL), (dict(k=None), av.EINVAL),
           (dict(v=None), av.EINVAL), (dict(oq=None), av.EINVAL), (dict(ok=None), av.EINVAL), (dict(o=None), av.EINVAL), (dict(lse=None), av.EINVAL),
@@ -52,7 +53,7 @@ LOSS = [(dict(T=-1), av.EINVAL), (dict(V=0), av.EINVAL), (dict(D=0), av.EINVAL),
         (dict(scale=NAN), av.EINVAL), (dict(scale=INF), av.EINVAL), (dict(flags=2), av.EINVAL), (dict(x=None), av.EINVAL), (dict(w=None), av.EINVAL),
         (dict(t=None), av.EINVAL), (dict(lse=None), av.EINVAL), (dict(rs_x=56), av.EINVAL), (dict(rs_w=63), av.EINVAL),
         (dict(D=60, rs_x=64, rs_w=64), av.EUNSUPPORTED), (dict(D=65544, rs_x=65544, rs_w=65544), av.EUNSUPPORTED),
-        (dict(T=(1 << 28) + 1), av.EUNSUPPORTED), (dict(V=(1 << 28) + 1), av.EUNSUPPORTED), (dict(rs_x=68), av.EUNSUPPORTED),
+        (dict(T=1 << 28), av.EUNSUPPORTED), (dict(V=(1 << 28) + 1), av.EUNSUPPORTED), (dict(rs_x=68), av.EUNSUPPORTED),
         (dict(rs_w=(1 << 20) + 8), av.EUNSUPPORTED), (dict(x=P + 8), av.EUNSUPPORTED), (dict(w=P + 2), av.EUNSUPPORTED), (dict(t=P + 4), av.EUNSUPPORTED),
         (dict(t=P + 2, flags=av.FLAG_TOKENS_I32), av.EUNSUPPORTED), (dict(lse=P + 2), av.EUNSUPPORTED), (dict(total=P + 1), av.EUNSUPPORTED),
         (dict(ws=None), av.EWORKSPACE), (dict(ws=P + 16), av.EWORKSPACE), (dict(n=255), av.EWORKSPACE)]
@@ -64,7 +65,7 @@ CASES = [
                (dict(k=None), av.EINVAL), (dict(yq=None), av.EINVAL), (dict(yk=None), av.EINVAL), (dict(positions=None), av.EINVAL),
                (dict(freqs=None), av.EINVAL), (dict(q=P * 2, rs_q=512), av.EINVAL), (dict(sections=(8, 8, 8, 4, 4)), av.EUNSUPPORTED),
                (dict(d=68, rs_q=512, rs_k=512), av.EUNSUPPORTED), (dict(pairs=20, sections=(20,)), av.EUNSUPPORTED), (dict(rs_q=260), av.EUNSUPPORTED),
-               (dict(d=4104, rs_q=1 << 20, rs_k=1 << 20), av.EUNSUPPORTED), (dict(T=1 << 31, P_=1 << 31), av.EUNSUPPORTED), (dict(q=P + 8), av.EUNSUPPORTED),
+               (dict(d=4104, rs_q=1 << 20, rs_k=1 << 20), av.EUNSUPPORTED), (dict(T=1 << 27, P_=1 << 27), av.EUNSUPPORTED), (dict(q=P + 8), av.EUNSUPPORTED),
                (dict(yk=P + 8), av.EUNSUPPORTED), (dict(positions=P + 4), av.EUNSUPPORTED), (dict(freqs=P + 2), av.EUNSUPPORTED),
                (dict(T=0, q=None, yq=None), av.OK)]),
     (_ragged_fwd, SHAPES + [(dict(Tq=0, q=None, o=None, lse=None), av.OK),
@@ -102,7 +103,7 @@ def test_workspace_sizes():
     assert ce_f(8, 10, 60) == 0 and ce_b(8, 0, 64) == 0 and ce_f(0, 1, 8) >= 256 and ce_b(0, 1, 8) >= 256
     assert ce_f(16384, 50000, 768) < 16384 * 50000 // 256       # no logits
     assert ce_b(16384, 50000, 768) < (1 << 30) + 16384 * (768 * 4 + 12) + (1 << 20)
-    assert ce_b(1 << 28, 1 << 28, 8) > 1 << 36                  # in size_t throughout
+    assert ce_b((1 << 28) - 1, 1 << 28, 8) > 1 << 36                  # in size_t throughout
 
 
 def test_the_front_end_refuses():
