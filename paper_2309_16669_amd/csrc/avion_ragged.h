@@ -30,7 +30,9 @@ struct RaggedArgs {
     int S, Tq, Tk, Hq, Hk, G;
     unsigned g_mul, g_shift;  // of over_heads()
     int slots;
-    int done;               // backward: sequences of at most so many queries and keys are avion_ragged_whole_kernel's (0: none)
+    int done;               // forward: sequences of at most so many rows are avion_ragged_few_kernel's, the others the next launch's (0:
+                            // one of the two has all); backward: those of at most so many queries and keys are
+                            // avion_ragged_whole_kernel's (0: none)
     int* more;              // and whether there are others, as that kernel has found
     int causal;
     float cs, scale;        // scale * log2 e, scale
@@ -528,9 +530,10 @@ avion_ragged_fwd_kernel(RaggedArgs a, raw16* __restrict__ o, float* __restrict__
     if (turn >= a.slots) return;
     const RaggedPlace p = ragged_turn<Cut::SHIFT, true>(a.off_q, a.S, a.Tq, a.G, a.off_k, a.Tk, a.slots, turn, lane);
     const int rows = p.n * a.G;
-    if (p.block < 0 || p.block * Cut::BLOCK >= rows) return;
+    if (p.block < 0 || p.block * Cut::BLOCK >= rows || rows <= a.done) return;
     const int block0 = (int)p.block * Cut::BLOCK;
     if (p.i == 0 || p.i == a.S + 1) {
+        if (a.done) return;  // (these are avion_ragged_join_kernel's then)
         const int from = ragged_first_token(block0, a.G), to = min(ragged_first_token(block0 + Cut::BLOCK, a.G), p.n);
         ragged_fwd_none<D>(a, o, lse, hk, p.begin + from, to - from, job.tid, Cut::NT);
         return;
@@ -555,8 +558,9 @@ avion_ragged_fwd_kernel(RaggedArgs a, raw16* __restrict__ o, float* __restrict__
 // ------------------------------------------------------------------------------ few rows, many keys
 // Single tokens behind long caches: bound by the keys' bytes, which must come from all of memory at once.  Slots are chunks of
 // 2^SHIFT keys (found as above, in the keys' offsets): a wavefront takes the first 32 rows of a sequence through one chunk and
-// leaves its sums; a second launch joins them.  A sequence with one chunk is finished here; rows past the first 32, where there are
-// any, take all keys in the wavefront of the first chunk.
+// leaves its sums; a second launch joins them.  A sequence with one chunk is finished here.  Rows past the first 32, which a launch of a
+// few hundred rows may hold, take all keys in the wavefront of the first chunk; in larger ones such a sequence is a launch of
+// avion_ragged_fwd_kernel's.
 template <int D>
 struct RaggedPart {
     static constexpr int FLOATS = 32 * D + 3 * 32;  // O, then reference, sum, sum of the rounded weights
@@ -568,7 +572,7 @@ avion_ragged_few_kernel(RaggedArgs a, raw16* __restrict__ o, float* __restrict__
     constexpr int CT = (D + 31) / 32;
     extern __shared__ __attribute__((aligned(16))) char smem[];
     const int lane = threadIdx.x, hk = blockIdx.x % a.Hk, slot = blockIdx.x / a.Hk;
-    // (blocks of 2^6 tokens, `shift` of them to a chunk: the search knows shifts at compile time)
+    // (the search knows shifts at compile time)
     RaggedPlace p;
     switch (shift) {
         case 8: p = ragged_place<8>(a.off_k, a.S, a.Tk, 1, slot, lane); break;
@@ -580,6 +584,7 @@ avion_ragged_few_kernel(RaggedArgs a, raw16* __restrict__ o, float* __restrict__
     if (p.i == 0 || p.i == a.S + 1 || p.block < 0 || (p.block > 0 && p.block * chunk >= p.n)) return;
     const int begin_q = ragged_border(a.off_q, a.S, a.Tq, p.i), nq = max(ragged_border(a.off_q, a.S, a.Tq, p.i + 1) - begin_q, 0);
     const int rows = nq * a.G, chunks = max((p.n + chunk - 1) >> shift, 1), tiles = (p.n + 63) / 64;
+    if (a.done && rows > a.done) return;
     for (int row0 = 0; row0 < rows; row0 += 32) {
         const bool part = row0 == 0 && chunks > 1;
         if (!part && p.block > 0) return;
@@ -627,7 +632,7 @@ avion_ragged_join_kernel(RaggedArgs a, raw16* __restrict__ o, float* __restrict_
     }
     const int begin_k = ragged_border(a.off_k, a.S, a.Tk, i), nk = max(ragged_border(a.off_k, a.S, a.Tk, i + 1) - begin_k, 0);
     const int chunks = (nk + (1 << shift) - 1) >> shift, rows = min(nq * a.G, 32);
-    if (chunks < 2) return;
+    if (chunks < 2 || (a.done && nq * a.G > a.done)) return;
     const long slot = (begin_k >> shift) + i, step = (long)a.Hk * RaggedPart<D>::FLOATS;
     const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, group = lane / LANES, col = lane % LANES * 4;
     for (int row = wave; row < rows; row += 4) {

@@ -27,20 +27,27 @@ int ragged_check(const RaggedShape& s)
     if ((s.d != 64 && s.d != 80 && s.d != 128) || s.Tq > kMostTokens || s.Tk > kMostTokens || s.S > kMostSequences) return AVION_EUNSUPPORTED;
     const long long G = s.Hq / s.Hk;
     if (s.Hq > (1 << 16) || s.Tq * G > (1LL << 30) || (s.Tq * G / 32 + s.Tk / 32 + s.S + 2) * s.Hq > 0x7fffffffLL) return AVION_EUNSUPPORTED;
+    if ((s.Tq * G / 128 + s.Tk / 128 + s.S + 4) * s.Hk * 256 > 0xffffffffLL) return AVION_EUNSUPPORTED;  // threads of a launch
     if ((long long)s.Hq * s.d > kMostStride) return AVION_EUNSUPPORTED;
     return AVION_OK;
 }
 bool stride_ok(long long rs, int H, int d) { return rs >= (long long)H * d; }
 
-// Few rows a sequence and many keys: a wavefront per chunk of keys.  2^shift keys a chunk, 0: not this way.
+// Few rows a sequence and many keys, or a batch most of whose sequences may be such: a wavefront per chunk of keys.  2^shift keys a chunk,
+// 0: not this way.  63 single tokens and a prompt of 1000, each with 9000 keys, 32 heads on 8 of 128: 648 us, in one launch 665; 15 tokens and
+// 500 with 4000 keys, 8 heads of 64: 60, 118.
 int few_shift(const RaggedShape& s)
 {
     const long long G = s.Hq / s.Hk;
-    if (s.S < 1 || s.Tq * G > 32 * s.S || s.Tk < 256 * s.S) return 0;
+    const bool few = s.Tq * G <= 32 * s.S && s.Tk >= 256 * s.S, mixed = s.S >= 4 && s.Tk >= 1024 * s.S && s.Tk >= 4 * s.Tq;
+    if (s.S < 1 || !(few || mixed)) return 0;
     int shift = 8;
     while (shift < 11 && (s.Tk >> shift) * s.Hk > 8 * kComputeUnits) ++shift;
     return shift;
 }
+// whether sequences of more than 32 rows get a launch of their own beside it: where they may have more than a few hundred (the 63 tokens
+// with a prompt of 400: 597 us, without 10300; 128 tokens with 2000 keys, which need none, 217 and 213)
+bool few_apart(const RaggedShape& s) { return s.Tq * (s.Hq / s.Hk) > 256; }
 long long few_slots(const RaggedShape& s, int shift) { return (s.Tk >> shift) + s.S + 2; }
 size_t few_bytes(const RaggedShape& s)
 {
@@ -200,24 +207,30 @@ int avion_ragged_fwd(const void* q, const void* k, const void* v, const int* off
     return by_head(d, flags, [&](auto dim, auto fmt) {
         constexpr int D = decltype(dim)::value;
         using E = typename decltype(fmt)::type;
-        if (const int shift = few_shift(s)) {
-            static std::atomic<unsigned long long> allowed{0}, none{0};
-            float* parts = static_cast<float*>(workspace);
-            const int first = launch(avion_ragged_few_kernel<D, E>, RaggedFwdCfg<D, RaggedLone>::LDS_BYTES, allowed, few_slots(s, shift) * Hk, 64, st,
-                                     "launch avion_ragged_few_kernel", a, out, lse, parts, shift);
-            if (first != AVION_OK) return first;
-            return launch(avion_ragged_join_kernel<D, E>, 0, none, (S + 2) * Hk, 256, st, "launch avion_ragged_join_kernel", a, out, lse,
-                          (const float*)parts, shift);
+        const auto forward = [&](RaggedWay way) {
+            return by_way<D>(way, [&](auto cut) {
+                using Cut = decltype(cut);
+                using Cfg = RaggedFwdCfg<D, Cut>;
+                static std::atomic<unsigned long long> allowed{0};
+                a.slots = (int)(Tq * a.G / Cut::BLOCK + S + 2);
+                return launch(avion_ragged_fwd_kernel<D, Cut, E>, Cfg::LDS_BYTES, allowed, workgroups<Cut>((long long)a.slots * Hk),
+                              Cut::NT * Cut::JOBS, st, "launch avion_ragged_fwd_kernel", a, out, lse);
+            });
+        };
+        const int shift = few_shift(s);
+        if (!shift) return forward(ragged_way(d, Tq * a.G, S, Hk));
+        static std::atomic<unsigned long long> allowed{0}, none{0};
+        float* parts = static_cast<float*>(workspace);
+        a.done = few_apart(s) ? 32 : 0;
+        if (a.done) {  // (how many sequences these are is not known: as if all rows were one's)
+            const int apart = forward(ragged_way(d, Tq * a.G, 1, Hk));
+            if (apart != AVION_OK) return apart;
         }
-        return by_way<D>(ragged_way(d, Tq * a.G, S, Hk), [&](auto cut) {
-            using Cut = decltype(cut);
-            using Cfg = RaggedFwdCfg<D, Cut>;
-            static std::atomic<unsigned long long> allowed{0};
-            a.slots = (int)(Tq * a.G / Cut::BLOCK + S + 2);
-            return launch(avion_ragged_fwd_kernel<D, Cut, E>, Cfg::LDS_BYTES, allowed, workgroups<Cut>((long long)a.slots * Hk),
-                          Cut::NT * Cut::JOBS, st,
-                          "launch avion_ragged_fwd_kernel", a, out, lse);
-        });
+        const int first = launch(avion_ragged_few_kernel<D, E>, RaggedFwdCfg<D, RaggedLone>::LDS_BYTES, allowed, few_slots(s, shift) * Hk, 64, st,
+                                 "launch avion_ragged_few_kernel", a, out, lse, parts, shift);
+        if (first != AVION_OK) return first;
+        return launch(avion_ragged_join_kernel<D, E>, 0, none, (S + 2) * Hk, 256, st, "launch avion_ragged_join_kernel", a, out, lse,
+                      (const float*)parts, shift);
     });
 }
 

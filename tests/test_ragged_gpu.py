@@ -129,6 +129,14 @@ def test_single_tokens_in_chunks(d, dtype):
 
 
 @pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("d,dtype", [(64, F16), (80, BF), (128, BF)])
+@pytest.mark.parametrize("nq,nk", [([1, 1, 300, 1, 0, 5, 40], [1100, 3000, 2100, 1, 700, 255, 700]), ([1] * 90, [256, 400, 300] * 30),
+                                   ([1] * 60 + [200], [300] * 60 + [0])], ids=["mixed", "single", "long"])
+def test_prompts_among_single_tokens(nq, nk, d, dtype, causal):
+    _check(nq, nk, 4, 1, d, dtype, causal)
+
+
+@pytest.mark.parametrize("causal", [False, True])
 @pytest.mark.parametrize("Hq,Hk,d,dtype,nq,nk", [
     (32, 32, 64, BF, [300, 129, 64, 1, 200] * 4, None), (32, 16, 128, F16, [260, 130, 7], [300, 130, 90]), (64, 32, 80, BF, [150] * 10, None),
     (12, 12, 64, F16, [300, 129, 64, 1, 600], None), (8, 8, 128, BF, [500, 700, 130], None), (20, 10, 80, F16, [513, 200, 140], [300, 900, 140]),
