@@ -25,21 +25,25 @@ int loss_check(const LossShape& s)
 }
 long long ceil_div(long long a, long long b) { return (a + b - 1) / b; }
 
-enum class LossTiles { kFew, kSmall, kLarge };  // 32 rows x 128 columns, 128 x 128, 256 x 256
+enum class LossTiles { kFew, kLow, kSmall, kLarge };  // 32 rows x 128 columns, 64 x 128, 128 x 128, 256 x 256
+// 128 x 128 where they are more than the compute units, 64 x 128 where they would leave each with one: forward and backward in a graph, us, of
+// 2048 x 2048 x 512 60.8, in tiles of 128 65.7; 512 x 4096 x 512 56.3, 62.9; 1000 x 1000 x 256 40.0, 46.6; 128 x 30000 x 2048 143.7, 154.8
 LossTiles loss_tiles(long long rows, long long cols)
 {
     if (rows <= 32) return LossTiles::kFew;
-    return ceil_div(rows, 256) * ceil_div(cols, 256) < kComputeUnits ? LossTiles::kSmall : LossTiles::kLarge;
+    if (ceil_div(rows, 256) * ceil_div(cols, 256) >= kComputeUnits) return LossTiles::kLarge;
+    return ceil_div(rows, 128) * ceil_div(cols, 128) > kComputeUnits ? LossTiles::kSmall : LossTiles::kLow;
 }
 // tile height and width, wavefronts
 template <int TB_>
 struct Tile {
-    static constexpr int TB = TB_, TA = TB == 256 ? 256 : 128, WA = TB == 128 ? 2 : 4, WB = TB == 32 ? 1 : 2;
+    static constexpr int TB = TB_, TA = TB == 256 ? 256 : 128, WA = TB == 128 ? 2 : 4, WB = TB < 128 ? 1 : 2;
 };
 template <typename F>
 int by_tiles(LossTiles t, F f)
 {
     if (t == LossTiles::kFew) return f(Tile<32>{});
+    if (t == LossTiles::kLow) return f(Tile<64>{});
     return t == LossTiles::kLarge ? f(Tile<256>{}) : f(Tile<128>{});
 }
 
@@ -47,7 +51,7 @@ int by_tiles(LossTiles t, F f)
 int loss_slabs(const LossShape& s)
 {
     const LossTiles t = loss_tiles(s.T, s.V);
-    const long long tb = t == LossTiles::kFew ? 32 : t == LossTiles::kSmall ? 128 : 256, ta = t == LossTiles::kLarge ? 256 : 128;
+    const long long tb = t == LossTiles::kFew ? 32 : t == LossTiles::kLow ? 64 : t == LossTiles::kSmall ? 128 : 256, ta = t == LossTiles::kLarge ? 256 : 128;
     const long long blocks = std::max<long long>(1, ceil_div(s.T, tb)), tiles = ceil_div(s.V, ta), at_once = t == LossTiles::kLarge ? kComputeUnits : 2 * kComputeUnits;
     return (int)std::max<long long>(1, std::min<long long>(tiles, at_once / blocks));
 }

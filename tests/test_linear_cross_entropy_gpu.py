@@ -92,7 +92,7 @@ def _check(x, w, t, scale=1.0, reduction="mean", dloss=None, where="cpu"):
 @pytest.mark.parametrize("dtype", [BF, F16], ids=["bf16", "f16"])
 @pytest.mark.parametrize("reduction", ["mean", "sum", "none"])
 @pytest.mark.parametrize("T,V,D", [(1, 1, 8), (1, 130, 64), (5, 1000, 72), (32, 129, 128), (33, 127, 8), (128, 257, 200), (129, 64, 776),
-                                   (300, 1001, 64), (1000, 77, 136)], ids=str)
+                                   (300, 1001, 64), (1000, 77, 136), (900, 5003, 72)], ids=str)
 def test_sizes(T, V, D, reduction, dtype):
     _check(*_inputs(T, V, D, dtype, none=0.2 if T > 1 else 0.0), reduction=reduction)
 
