@@ -132,14 +132,17 @@ using RaggedLone = RaggedCut<1, 1, 64, 2, 1>;
 // as TileRing's.  The descriptors begin at the tile's own first row, so that no length of a sequence and no row stride takes a
 // byte offset past 32 bits; rows past the end arrive as zeros.
 // Layout of a tile: at 64 channels quad_at's (no bank conflicts, and two addresses a lane for the loads of both tensors instead of one
-// for each load: where registers are scarce, in dK/dV, that is what keeps the accumulators out of scratch), else padded rows.
+// for each load: where registers are scarce, in dK/dV, that is what keeps the accumulators out of scratch), at 128 two such halves one
+// after the other (padded rows' bank conflicts took 30 % of the cycles: prompts of 500 to 8000 tokens, 32 heads on 8, 690 -> 665 us), else
+// padded rows.
 template <int D, typename Cut, bool SCALARS>
 struct RaggedRing {
     static constexpr int NW = Cut::NW, ROWS = Cut::ROWS, NBUF = Cut::NBUF, STRIDE = tile_stride<D>();
-    static constexpr bool QUAD = D == 64;
+    static constexpr bool QUAD = D % 64 == 0;
+    static constexpr int HALF = ROWS / 8;  // blocks of 64 channels of a tile
     // 1 KB blocks of a tile (the last one's rows past the tile, where there are any, are not read)
-    static constexpr int NTI = QUAD ? ROWS / 8 : (ROWS * STRIDE + 1023) / 1024, NBLK = 2 * NTI, NPW = (NBLK + NW - 1) / NW;
-    static_assert(!QUAD || (NTI % NW == 0 && (NW == 1 || NW % 2 == 0)), "a load's blocks belong to one tensor, a wavefront's are all even or all odd");
+    static constexpr int NTI = QUAD ? D / 64 * HALF : (ROWS * STRIDE + 1023) / 1024, NBLK = 2 * NTI, NPW = (NBLK + NW - 1) / NW;
+    static_assert(!QUAD || (HALF % NW == 0 && HALF % 2 == 0 && (NW == 1 || NW % 2 == 0)), "a load's blocks belong to 64 channels of one tensor, a wavefront's are all even or all odd");
     static constexpr int OFF_B = NTI * 1024, OFF_SCALARS = 2 * NTI * 1024;
     static constexpr int BUF_BYTES = NBLK * 1024 + (SCALARS ? 1024 : 0);
     static constexpr int LDS_BYTES = NBUF * BUF_BYTES + (D % 32 != 0 ? 64 : 0);
@@ -178,7 +181,8 @@ struct RaggedRing {
     {
         if constexpr (QUAD) {
             const bool first = NW * j < NTI;
-            const unsigned down = (unsigned)(8 * (NW * j - (first ? 0 : NTI))) * (unsigned)((first ? rs_a : rs_b) * 2);
+            const int blk = NW * j - (first ? 0 : NTI);
+            const unsigned down = (unsigned)(8 * (blk % HALF)) * (unsigned)((first ? rs_a : rs_b) * 2) + (unsigned)(blk / HALF) * 128;
             return place[first ? 0 : 1] + down + (NW == 1 ? place[2] ^ (32 * (j & 1)) : place[2]);
         } else {
             return place[j];
@@ -228,7 +232,7 @@ struct RaggedRing {
 };
 
 // A lane's fragments of a tile: rows 32 * hk .. of it (natural) and 16 tokens of step `step` (transposed)
-template <int D>
+template <int D, int ROWS>
 struct RaggedLane {
     unsigned nat, tr;
     DEVINL explicit RaggedLane(int lane)
@@ -241,21 +245,30 @@ struct RaggedLane {
     }
     DEVINL frag8 transposed(const char* tile, int ct, int step) const { return tr_frag(tile, tile_stride<D>(), (int)tr, ct, step); }
 };
-template <>
-struct RaggedLane<64> : QuadLane {
-    DEVINL explicit RaggedLane(int lane) : QuadLane(lane, 0) {}
+template <int D, int ROWS>
+struct RaggedQuadLane : QuadLane {
+    static constexpr int HALF = ROWS * 128;
+    DEVINL explicit RaggedQuadLane(int lane) : QuadLane(lane, 0) {}
     DEVINL frag8 natural(const char* tile, int hk, int ks) const
     {
-        return *reinterpret_cast<const frag8*>(tile + nat[ks & 1] + hk * 4096 + (ks >> 1) * 256);
+        return *reinterpret_cast<const frag8*>(tile + nat[ks & 1] + hk * 4096 + (ks / 2 & 1) * 256 + ks / 4 * HALF);
     }
     DEVINL frag8 transposed(const char* tile, int ct, int step) const
     {
-        const lds_char* p = (const lds_char*)tile + step * 2048 + ct * 256;
+        const lds_char* p = (const lds_char*)tile + step * 2048 + (ct & 1) * 256 + ct / 2 * HALF;
         const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(p + tr[0]));
         const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(p + tr[1]));
         const u32x2 l2 = __builtin_bit_cast(u32x2, lo), h2 = __builtin_bit_cast(u32x2, hi);
         return as_frag8(u32x4{l2[0], l2[1], h2[0], h2[1]});
     }
+};
+template <int ROWS>
+struct RaggedLane<64, ROWS> : RaggedQuadLane<64, ROWS> {
+    using RaggedQuadLane<64, ROWS>::RaggedQuadLane;
+};
+template <int ROWS>
+struct RaggedLane<128, ROWS> : RaggedQuadLane<128, ROWS> {
+    using RaggedQuadLane<128, ROWS>::RaggedQuadLane;
 };
 
 // The work of a workgroup, or, with several jobs, of each of its wavefronts
@@ -387,7 +400,7 @@ DEVINL void ragged_fwd_walk(char* smem, const RaggedArgs& a, int hk, int begin_q
     using Ring = typename RaggedFwdCfg<D, Cut>::Ring;
     constexpr int KS = D / 16, CT = (D + 31) / 32, ROWS = Cut::ROWS;
     const int l32 = lane % 32, g = lane / 32;
-    const RaggedLane<D> at(lane);
+    const RaggedLane<D, Ring::ROWS> at(lane);
     const Ring ring(a.k + (long)begin_k * a.rs_k + hk * D, a.rs_k, a.v + (long)begin_k * a.rs_v + hk * D, a.rs_v, nullptr, 0, nk, smem,
                     wave, lane);
     if (t0 < t1) ring.fetch(t0);
@@ -731,7 +744,7 @@ avion_ragged_dq_kernel(RaggedArgs a, const raw16* __restrict__ o, const raw16* _
     if (t0 < t1) ring.fetch(t0);
     if (Ring::NBUF == 2 && whole && t1 == 2) ring.fetch(1);
     const int row0 = block0 + wave * 32;
-    const RaggedLane<D> at(lane);
+    const RaggedLane<D, Ring::ROWS> at(lane);
     const bool active = row0 < rows, first = job.group == 0;
     const RaggedRow row(a, hk, row0 + l32, rows, nq, nk);
     const int seen_by_all = RaggedRow(a, hk, row0, rows, nq, nk).keys, seen_by_any = RaggedRow(a, hk, row0 + 31, rows, nq, nk).keys;
@@ -887,8 +900,8 @@ DEVINL void ragged_store_part(const f32x16 (&acc)[(D + 31) / 32], float* out, lo
 
 // One unit: queries 32 * hq .. of the tiles qt (Q) and gt (dO), whose scalars (lse as avion_ragged_dq_kernel leaves it, then, `rows` further,
 // -delta) stand at `scalars`; `from`: the first query that sees this lane's key, from_all: all keys of the wavefront
-template <int D, typename E>
-DEVINL void ragged_dkdv_unit(const RaggedLane<D>& at, const char* qt, const char* gt, const float* scalars, int rows, int hq, int query_base,
+template <int D, typename E, typename Lane>
+DEVINL void ragged_dkdv_unit(const Lane& at, const char* qt, const char* gt, const float* scalars, int rows, int hq, int query_base,
                              int from, int from_all, float cs, int g, const frag8 (&kf)[D / 16], const frag8 (&vf)[D / 16],
                              f32x16 (&dka)[(D + 31) / 32], f32x16 (&dva)[(D + 31) / 32])
 {
@@ -1008,7 +1021,7 @@ avion_ragged_dkdv_kernel(RaggedArgs a, const raw16* __restrict__ dO, const float
     hold(vf);
     Ring::landed_barrier();
     const float cs = a.cs;
-    const RaggedLane<D> at(lane);
+    const RaggedLane<D, Ring::ROWS> at(lane);
 
     for (int n = 0; n < (Cut::KG == 1 ? total : share.per); ++n) {
         if constexpr (Ring::NBUF == 2) {
@@ -1107,7 +1120,7 @@ DEVINL void ragged_whole(char* smem, const RaggedArgs& a, const raw16* __restric
     second.fetch(0);
     const char *qt = smem, *gt = smem + Ring::OFF_B, *kt = smem + Cfg::SECOND, *vt = kt + Ring::OFF_B;
     float* scalars = reinterpret_cast<float*>(smem + Cfg::SCALARS);
-    const RaggedLane<D> at(lane);
+    const RaggedLane<D, Cfg::ROWS> at(lane);
     const int row0 = 32 * wave, row = row0 + l32;
     const bool active = row0 < nq, in = row < nq;
     const float saved = in ? lse[(long)h * a.Tq + queries.x + row] : -INFINITY;
