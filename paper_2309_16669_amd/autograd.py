@@ -26,6 +26,10 @@ the length of the call in either way of calling, and run on the device of their 
 tensors, and gradients, of any strides and at any address (what is not contiguous at a multiple of 16 bytes is copied first).
 Their gradients are not differentiable: under create_graph they carry a node that raises.
 
+`rotary(q, k, positions, freqs)`, `attention_ragged(q, k, v, offsets)` and `linear_cross_entropy(x, weight, targets)` are what a decoder
+needs around these layers: positions on several axes, sequences of different lengths with shared key heads, and the loss over a
+vocabulary or a contrastive batch without its logits.  They too take their workspaces for the length of the call.
+
 `rms_norm_fp8`, `add_rms_norm_fp8`, `quantize_rows` and `linear_fp8` are the 8-bit path of a trained encoder: they
 have no backward, and refuse inputs whose gradient is being recorded.
 """

@@ -711,7 +711,7 @@ struct Planes {
 
 extern "C" {
 
-int avion_version(void) { return 20300; }  // 2.3.0
+int avion_version(void) { return 20400; }  // 2.4.0
 
 const char* avion_strerror(int code)
 {
