@@ -368,6 +368,9 @@ DEVINL void ragged_zero(raw16* out, int H, int h0, int heads, long token0, int n
 // One wavefront owns 32 rows, the workgroup's NW share (K | V) tiles of 64 keys; work in units of 32 keys as in avion_fwd_kernel,
 // but with the running maximum: the accumulators are rescaled only where a row's maximum has grown by more than 2^8 (weights then
 // stay below 2^8, which either format holds), a branch that after the first units is hardly ever taken.
+// Bound by the vector issue port (65 % of the cycles at 64 channels, matrix units 34) and, at 128, by both (49 and 47).  16 videos of 196 to 3136
+// tokens, 12 heads of 64, 81 us = 670 TFLOP/s; prompts of 500 to 8000, 32 heads on 8 of 128, 665 us = 920; 2048 captions of 6 to 77, 8 heads
+// of 64, 55 us, bound by memory.
 constexpr float kRaggedLazy = 8.f;
 constexpr float kRaggedNone = -3.0e38f;  // reference of a row that has seen nothing: finite, so that -inf - it is -inf
 
@@ -375,7 +378,7 @@ template <int D, typename Cut>
 struct RaggedFwdCfg {
     using Ring = RaggedRing<D, Cut, false>;
     static constexpr int LDS_BYTES = Ring::LDS_BYTES * Cut::KG * Cut::JOBS;
-    static_assert(LDS_BYTES <= 160 * 1024, "");
+    static_assert(LDS_BYTES <= 160 * 1024 && Cut::NW * RaggedStore<D, Bf16>::BYTES <= Ring::LDS_BYTES, "the rows on their way out take the ring's place");
     static constexpr int WAVES_PER_SIMD = Cut::KG > 1 || std::is_same<Cut, RaggedLone>::value ? 1 : D == 64 ? 4 : D == 80 ? 3 : 2;
 };
 template <int CT>
@@ -573,7 +576,7 @@ avion_ragged_fwd_kernel(RaggedArgs a, raw16* __restrict__ o, float* __restrict__
 // 2^SHIFT keys (found as above, in the keys' offsets): a wavefront takes the first 32 rows of a sequence through one chunk and
 // leaves its sums; a second launch joins them.  A sequence with one chunk is finished here.  Rows past the first 32, which a launch of a
 // few hundred rows may hold, take all keys in the wavefront of the first chunk; in larger ones such a sequence is a launch of
-// avion_ragged_fwd_kernel's.
+// avion_ragged_fwd_kernel's.  24 tokens behind up to 9000 keys, 32 heads on 8 of 128: 35 us for 182 MB, 5.2 TB/s, and 5 for the join.
 template <int D>
 struct RaggedPart {
     static constexpr int FLOATS = 32 * D + 3 * 32;  // O, then reference, sum, sum of the rounded weights
@@ -694,6 +697,7 @@ avion_ragged_join_kernel(RaggedArgs a, raw16* __restrict__ o, float* __restrict_
 //
 // fp16 weights below 2^-14 lose bits: over thousands of keys most are.  The second kernel holds them 2^8 times larger where they
 // are rounded for dV; in dS they stand beside dP, which is as large as the loss is scaled.
+// The 16 videos 92 us = 880 TFLOP/s, the logits among them (matrix units 42 % of the cycles, vector issue 60).
 template <typename E>
 constexpr float kRaggedShift = std::is_same<E, F16>::value ? 8.f : 0.f;
 
@@ -701,7 +705,7 @@ template <int D, typename Cut>
 struct RaggedDqCfg {
     using Ring = RaggedRing<D, Cut, false>;
     static constexpr int LDS_BYTES = Ring::LDS_BYTES * Cut::KG * Cut::JOBS;
-    static_assert(LDS_BYTES <= 160 * 1024, "");
+    static_assert(LDS_BYTES <= 160 * 1024 && Cut::NW * RaggedStore<D, Bf16>::BYTES <= Ring::LDS_BYTES, "the rows on their way out take the ring's place");
     static constexpr int WAVES_PER_SIMD = Cut::KG > 1 ? 1 : D == 64 ? 4 : 2;
 };
 DEVINL long ragged_scalar_at(int begin, int i) { return ((long)(begin >> 6) + i) * 64; }
@@ -880,7 +884,7 @@ template <int D, typename Cut>
 struct RaggedDkvCfg {
     using Ring = RaggedRing<D, Cut, true>;
     static constexpr int LDS_BYTES = Ring::LDS_BYTES * Cut::KG * Cut::JOBS;
-    static_assert(LDS_BYTES <= 160 * 1024, "");
+    static_assert(LDS_BYTES <= 160 * 1024 && Cut::NW * RowStore<D, Bf16>::BYTES <= Ring::LDS_BYTES, "the rows on their way out take the ring's place");
     static constexpr int WAVES_PER_SIMD = Cut::KG > 1 ? 1 : D == 64 ? 3 : D == 80 ? 2 : 1;
 };
 // 32 rows of fp32 sums, lane = row
@@ -957,6 +961,8 @@ DEVINL void ragged_dkdv_unit(const Lane& at, const char* qt, const char* gt, con
             }
 }
 
+// dK and dV: 32 keys a wavefront, K and V in registers, (Q | dO) tiles of the query heads that share them one after the other.  The 16 videos
+// 112 us = 970 TFLOP/s, the logits among them (matrix units 45 % of the cycles, LDS 35, vector issue 47).
 template <int D, typename Cut, typename E>
 __global__ void __launch_bounds__(Cut::NT * Cut::JOBS, (RaggedDkvCfg<D, Cut>::WAVES_PER_SIMD))
 avion_ragged_dkdv_kernel(RaggedArgs a, const raw16* __restrict__ dO, const float* __restrict__ rowsc, int npad, raw16* __restrict__ dk,
@@ -1090,7 +1096,8 @@ avion_ragged_sum_kernel(const float* __restrict__ sums, int parts, long n, raw16
 // A workgroup for each (sequence, head), which ends at once where the sequence is another launch's; but with four wavefronts and 65 KB of
 // LDS, of which a compute unit ends two at a time, a grid that fills the chip once, whose workgroups look at the lengths of 512 sequences
 // at a time and take the pairs number b, b + grid, ... of those that fit.  2048 captions of 6 to 77 tokens, 8 heads, 64 channels, in one and
-// in the other way: W = 1 36 and 52 us, 2 52 and 62, 4 (145 of them) 50 and 38; in two passes 171 for all.
+// in the other way: W = 1 40 and 52 us, 2 51 and 62, 4 (145 of them) 50 and 38, of which the first two move 3.7 TB/s; in two passes
+// 171 for all.
 // The first launch clears `more`, the last one sets it where a sequence (or a row of none) is left for the two passes, which
 // else end at once.
 template <int D, int W>
