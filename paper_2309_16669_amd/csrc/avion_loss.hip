@@ -26,25 +26,36 @@ int loss_check(const LossShape& s)
 long long ceil_div(long long a, long long b) { return (a + b - 1) / b; }
 
 enum class LossTiles { kFew, kLow, kSmall, kLarge };  // 32 rows x 128 columns, 64 x 128, 128 x 128, 256 x 256
-// 128 x 128 where they are more than the compute units, 64 x 128 where they would leave each with one: forward and backward in a graph, us, of
-// 2048 x 2048 x 512 60.8, in tiles of 128 65.7; 512 x 4096 x 512 56.3, 62.9; 1000 x 1000 x 256 40.0, 46.6; 128 x 30000 x 2048 143.7, 154.8
+// Forward: 256 x 256 where they are a compute unit's at least, 128 x 128 where they are more than the compute units, else 64 x 128.
+//   Of 128 and 64 rows, in a graph, us: 2048 x 2048 x 512 19.4, 18.6; 997 x 10007 x 776 41.7, 42.5; 4000 x 3700 x 1024 46, 54; 200 x 50000 x 768 36, 42
+// dz: 64 x 128, whose stores the other workgroups of a compute unit fill up, below 1.4 tiles of 256 x 256 for one.
+//   Whole backward with 128 and 64 rows: 2048 x 2048 x 512 46, 42; 997 x 10007 x 776 110, 102; 4000 x 3700 x 1024 178, 156; 200 x 50000 x 768 129, 114;
+//   with 256 and 64: 1000 x 20000 x 768 163, 149; 4200 x 4200 x 2048 343, 321; 4096 x 10000 x 1024 335, 337; 5000 x 5000 x 4096 585, 654; 16384 x 50000 x
+//   768 3655, 4108
 LossTiles loss_tiles(long long rows, long long cols)
 {
     if (rows <= 32) return LossTiles::kFew;
     if (ceil_div(rows, 256) * ceil_div(cols, 256) >= kComputeUnits) return LossTiles::kLarge;
     return ceil_div(rows, 128) * ceil_div(cols, 128) > kComputeUnits ? LossTiles::kSmall : LossTiles::kLow;
 }
+LossTiles dz_tiles(long long rows, long long cols)
+{
+    if (rows <= 32) return LossTiles::kFew;
+    return rows * cols >= kComputeUnits * 7 / 5 * 256 * 256 ? LossTiles::kLarge : LossTiles::kLow;
+}
 // tile height and width, wavefronts
 template <int TB_>
 struct Tile {
     static constexpr int TB = TB_, TA = TB == 256 ? 256 : 128, WA = TB == 128 ? 2 : 4, WB = TB < 128 ? 1 : 2;
 };
-template <typename F>
+template <bool DZ, typename F>
 int by_tiles(LossTiles t, F f)
 {
     if (t == LossTiles::kFew) return f(Tile<32>{});
     if (t == LossTiles::kLow) return f(Tile<64>{});
-    return t == LossTiles::kLarge ? f(Tile<256>{}) : f(Tile<128>{});
+    if constexpr (!DZ)
+        if (t == LossTiles::kSmall) return f(Tile<128>{});
+    return f(Tile<256>{});
 }
 
 // runs of vocabulary tiles in the forward: enough workgroups for the chip, whole rounds of them where there are many
@@ -194,7 +205,7 @@ int avion_linear_ce_fwd(const void* x, const void* w, const void* targets, float
         const int first = by_element(flags, [&](auto fmt) {
             using E = typename decltype(fmt)::type;
             const LossTiles t = loss_tiles(T, V);
-            return by_tiles(t, [&](auto tile) {
+            return by_tiles<false>(t, [&](auto tile) {
                 using X = decltype(tile);
                 using Cfg = LossCfg<Along::kK, Along::kK, X::TA, X::TB, X::WA, X::WB>;
                 static std::atomic<unsigned long long> allowed{0};
@@ -254,7 +265,7 @@ int avion_linear_ce_bwd(const void* x, const void* w, const void* targets, const
         for (long long v0 = 0; v0 < V && rc2 == AVION_OK; v0 += piece) {
             const long long n = std::min(piece, V - v0), held = std::min(ld, ceil_div(n, 8) * 8);
             if (T > 0)
-                rc2 = by_tiles(loss_tiles(T, n), [&](auto tile) {
+                rc2 = by_tiles<true>(dz_tiles(T, n), [&](auto tile) {
                     using X = decltype(tile);
                     using Cfg = LossCfg<Along::kK, Along::kK, X::TA, X::TB, X::WA, X::WB>;
                     static std::atomic<unsigned long long> allowed{0};
