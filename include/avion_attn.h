@@ -445,7 +445,7 @@ int avion_ragged_bwd(const void *q, const void *k, const void *v, const int *off
  *   loss, lse : out, fp32 [T]; loss may be NULL where total is given.   total : out, fp32 [2], or NULL: the sum of the losses (their
  *             mean over the rows with a target, 0 if there is none, with AVION_FLAG_MEAN) and the number of rows with a target
  *   dloss   : in, fp32 [T], or with AVION_FLAG_ONE_GRADIENT one number, the gradient of total[0]; then with AVION_FLAG_MEAN it is divided
- *             by total[1]
+ *             by total[1].  One that is not finite, of a row with a target, makes every gradient NaN
  *   dx, dw  : out, fully overwritten; either may be NULL (not both)
  *   scale > 0 and finite; D a multiple of 8 up to 65536; T below 2^28, V up to 2^28; rs up to 2^20
  *   workspace: 256-byte aligned, avion_linear_ce_fwd_workspace_bytes / _bwd_workspace_bytes bytes (0: unsupported), contents ignored and
@@ -453,7 +453,7 @@ int avion_ragged_bwd(const void *q, const void *k, const void *v, const int *off
  *   (at most 1 GB, or 256 columns) and, where there are several, dx in fp32 lie in it
  * Logits, statistics and sums in fp32, dz rounded to the format before its products (fp16: scaled by the largest |dloss| and 2^14,
  * so that small probabilities keep their bits), results rounded once.  No order of atomics decides a sum: the same sizes give the same bits.
- * T = 0: total and dw become zeros.  Pointers 16-byte aligned (fp32 ones and targets naturally).
+ * T = 0: total and dw become zeros, and pointers to T elements may be NULL.  Pointers 16-byte aligned (fp32 ones and targets naturally).
  */
 #define AVION_FLAG_MEAN 256u
 #define AVION_FLAG_ONE_GRADIENT 512u

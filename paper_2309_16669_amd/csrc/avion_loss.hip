@@ -186,7 +186,7 @@ int avion_linear_ce_fwd(const void* x, const void* w, const void* targets, float
     const LossShape s{T, V, D};
     const int rc = loss_inputs(s, x, w, targets, rs_x, rs_w, scale, flags, AVION_FLAG_F16 | AVION_FLAG_TOKENS_I32 | AVION_FLAG_MEAN);
     if (rc != AVION_OK) return rc;
-    if ((T > 0 && !lse) || (!loss && !total)) return AVION_EINVAL;
+    if (T > 0 && (!lse || (!loss && !total))) return AVION_EINVAL;
     for (const void* p : {(const void*)loss, (const void*)lse, (const void*)total})
         if (reinterpret_cast<uintptr_t>(p) % 4 != 0) return AVION_EUNSUPPORTED;
     const LossForward at(s);
@@ -240,12 +240,13 @@ int avion_linear_ce_bwd(const void* x, const void* w, const void* targets, const
                                AVION_FLAG_F16 | AVION_FLAG_TOKENS_I32 | AVION_FLAG_MEAN | AVION_FLAG_ONE_GRADIENT);
     if (rc != AVION_OK) return rc;
     const bool each = !(flags & AVION_FLAG_ONE_GRADIENT), mean = (flags & AVION_FLAG_MEAN) != 0;
-    if (!dloss || (!dx && !dw) || (T > 0 && !lse) || (mean && (each || !total))) return AVION_EINVAL;
+    if ((T > 0 && (!dloss || !lse || (!dx && !dw))) || (!each && !dloss) || (mean && (each || !total))) return AVION_EINVAL;
     if (!aligned16(dx) || !aligned16(dw)) return AVION_EUNSUPPORTED;
     for (const void* p : {(const void*)lse, (const void*)dloss, (const void*)total})
         if (reinterpret_cast<uintptr_t>(p) % 4 != 0) return AVION_EUNSUPPORTED;
     const LossBackward at(s);
     if (!workspace_fits(workspace, workspace_bytes, at.bytes)) return AVION_EWORKSPACE;
+    if (!dx && !dw) return AVION_OK;
     hipStream_t st = static_cast<hipStream_t>(stream);
     const LossArgs a = loss_args(s, x, w, targets, rs_x, rs_w, ignore_index, scale, flags);
     char* ws = static_cast<char*>(workspace);

@@ -75,7 +75,7 @@ def test_a_training_step(Hq, Hk, d, lengths):
     ref = {n: t.double().requires_grad_(True) for n, t in p.items()}
     loss = _step(own, tokens.cuda(), targets.cuda(), lengths, Hq, Hk, d)
     want = _step64(ref, tokens, targets, lengths, Hq, Hk, d)
-    assert abs(float(loss) - float(want)) <= 8 * 2.0 ** -8 * 2
+    assert abs(float(loss.detach()) - float(want.detach())) <= 8 * 2.0 ** -8 * 2
     got, exact = torch.autograd.grad(loss, list(own.values())), torch.autograd.grad(want, list(ref.values()))
     for n, a, b in zip(own, got, exact):
         assert float((a.cpu().double() - b).norm() / b.norm()) <= 4 * 2.0 ** -8, n
@@ -209,3 +209,86 @@ def test_one_tensor_for_queries_keys_and_values():
     total = sum(t.double() for t in want)
     size = sum(t.double().abs() for t in want)
     assert ((leaf.grad.double() - total).abs() <= 2.1 * 2.0 ** -8 * size).all()
+
+
+def test_offsets_past_32_bits():
+    """Rows 8192 elements apart, 2.3 G elements of them: the bits of contiguous copies."""
+    ag = _ag()
+    g = torch.Generator("cuda").manual_seed(7)
+    T = 280000
+    rows = torch.empty((T, 64, 128), dtype=BF, device="cuda")
+    rows[:, :2] = torch.randn((T, 2, 128), generator=g, device="cuda").to(BF)
+    rows[:, 62:] = torch.randn((T, 2, 128), generator=g, device="cuda").to(BF)
+    at, freqs = torch.arange(T, device="cuda"), ag.rotary_frequencies(64, device="cuda")
+    a, b = ag.rotary(rows[:, :2], rows[:, 62:], at, freqs), ag.rotary(rows[:, :2].contiguous(), rows[:, 62:].contiguous(), at, freqs)
+    assert all(torch.equal(x, y) for x, y in zip(a, b))
+    del a, b
+
+    def both(f, *args):
+        """Results and gradients with the rows where they lie, and with copies of them; each output's own gradient a fixed one."""
+        out = []
+        for copy in (False, True):
+            leaves = [(t.contiguous() if copy else t).detach().requires_grad_(True) for t in args]
+            y = f(*leaves)
+            out.append([y.detach(), *torch.autograd.grad(y, leaves, torch.full_like(y, 0.5))])
+        assert all(torch.equal(x, y) for x, y in zip(*out))
+
+    keys, values = rows[:, :1], rows[:, 63:]
+    for nq in ([2, 2], [300, 100]):             # chunks of keys, and blocks of queries
+        q = torch.randn((sum(nq), 2, 128), generator=g, device="cuda").to(BF)
+        both(lambda q, k, v: ag.attention_ragged(q, k, v, _offsets(nq), _offsets([T - 300, 300]), causal=True), q, keys, values)
+    both(lambda q, k, v: ag.attention_ragged(q, k, v, _offsets([70] * (T // 70))), rows[:, 1:2], keys, values)     # short sequences
+    w, t = torch.randn((300, 128), generator=g, device="cuda").to(BF), torch.randint(0, 300, (T,), generator=g, device="cuda")
+    both(lambda x, w: ag.linear_cross_entropy(x, w, t), rows[:, 0], w)
+    both(lambda x, w: ag.linear_cross_entropy(x, w, t[:64] % 64), w[:64], rows[:, 63])
+
+
+def test_two_streams_at_once():
+    """The same calls on two streams side by side, each with workspaces of its own, give what they give alone."""
+    ag = _ag()
+    g = torch.Generator().manual_seed(9)
+    rn = lambda *s: torch.randn(s, generator=g).to(BF).cuda()   # noqa: E731
+    nk = [900, 1500, 700]
+    t = torch.randint(0, 5000, (700,), generator=g).cuda()
+    cases = [(lambda q, k, v: ag.attention_ragged(q, k, v, _offsets([1, 1, 1]), _offsets(nk), causal=True), [rn(3, 8, 64), rn(sum(nk), 2, 64), rn(sum(nk), 2, 64)]),
+             (lambda q, k, v: ag.attention_ragged(q, k, v, _offsets(nk), causal=True), [rn(sum(nk), 4, 64), rn(sum(nk), 1, 64), rn(sum(nk), 1, 64)]),
+             (lambda x, w: ag.linear_cross_entropy(x, w, t), [rn(700, 256), rn(5000, 256)])]
+    alone = [_pass(f, args) for f, args in cases]
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    for s in streams:
+        s.wait_stream(torch.cuda.current_stream())
+    got = [[], []]
+    for _ in range(10):
+        for mine, s in zip(got, streams):
+            with torch.cuda.stream(s):
+                mine.append([_pass(f, args) for f, args in cases])
+    torch.cuda.synchronize()
+    for mine in got:
+        for run in mine:
+            for a, b in zip(run, alone):
+                assert all(torch.equal(x, y) for x, y in zip(a, b))
+
+
+@pytest.mark.parametrize("native", [True, False])
+def test_nothing_at_all(native, monkeypatch):
+    """No tokens, no sequences, no keys."""
+    ag = _ag()
+    if not native:
+        import types
+        none = lambda *args: None   # noqa: E731
+        monkeypatch.setattr(ag, "_native", types.SimpleNamespace(rotary=none, attention_ragged=none, linear_cross_entropy=none))
+    z = lambda *s: torch.zeros(s, dtype=BF, device="cuda", requires_grad=True)   # noqa: E731
+    q, k = z(0, 4, 64), z(0, 2, 64)
+    y = ag.rotary(q, k, torch.arange(0, device="cuda"), ag.rotary_frequencies(32, device="cuda"))
+    assert [tuple(t.shape) for t in torch.autograd.grad(y, (q, k), [torch.ones_like(t) for t in y])] == [(0, 4, 64), (0, 2, 64)]
+    for nq, nk, S in ((0, 0, 0), (0, 0, 3), (0, 5, 1), (5, 0, 1), (5, 5, 0)):
+        q, k, v = z(nq, 4, 64), z(nk, 2, 64), z(nk, 2, 64)
+        border = lambda n: torch.tensor([0] + [n] * S, dtype=torch.int32, device="cuda")   # noqa: E731
+        o = ag.attention_ragged(q, k, v, border(nq), border(nk), causal=True)
+        grads = torch.autograd.grad(o, (q, k, v), torch.ones_like(o))
+        assert o.shape == q.shape and not o.any() and [g.shape for g in grads] == [q.shape, k.shape, v.shape] and not any(g.any() for g in grads)
+    for reduction in ("mean", "sum", "none"):
+        x, w = z(0, 64), z(10, 64)
+        loss = ag.linear_cross_entropy(x, w, torch.zeros(0, dtype=torch.int64, device="cuda"), reduction=reduction)
+        dx, dw = torch.autograd.grad(loss.sum(), (x, w))
+        assert float(loss.detach().sum()) == 0 and dx.shape == x.shape and dw.shape == w.shape and not dw.any()
