@@ -87,7 +87,9 @@ long long loss_piece(const LossShape& s)
 }
 long long loss_ld(const LossShape& s) { return std::min(loss_piece(s), ceil_div(s.V, 64) * 64); }
 // The two gradients' tiles: 256 x 256 where both together have one for each compute unit and no side is narrower than one, else 128 x
-// 128.  Either way a product whose steps are more than a workgroup's fair share of all (few tiles, long K) is cut along K, at
+// 128.  Both passes in a graph with 256 and with 128, us: 16384 x 50000 x 768 4787, 5242; 65536 x 8192 x 768 3315, 3581; 8192 x 8192 x 1024 519, 549;
+// in between by how full the last round is (8192 x 20000 x 768 1049, 1089; 8192 x 32000 x 1024 2238, 2119); below, 997 x 10007 x 776 157, 142;
+// 2048 x 2048 x 512 67, 60.  Either way a product whose steps are more than a workgroup's fair share of all (few tiles, long K) is cut along K, at
 // least 4 steps a range: 213 x 112000 x 72, dx of which is two tiles of 1750 steps, 2540 us without.  A range's plane is written and
 // read again, so there are no more of them than that.
 bool grads_large(const LossShape& s, long long n)
