@@ -319,3 +319,32 @@ def test_no_second_derivative():
     (g,) = torch.autograd.grad(o, (q,), do, create_graph=True)
     with pytest.raises(RuntimeError, match="no second derivative"):
         g.float().sum().backward()
+
+
+@pytest.mark.parametrize("S", [3, 70])
+def test_offsets_outside_the_tensors(S):
+    """Taken as the nearest place inside; decreasing ones write nowhere but in the outputs."""
+    import paper_2309_16669_amd as av
+    T, Hq, Hk, d = 500, 4, 2, 64
+    q, k, v, do = _inputs([T], [T], Hq, Hk, d, BF, S)
+    inside = [0] * (S - 2) + [40, 300, T]
+    outside = [-7] * (S - 2) + [40, 300, 2 ** 31 - 1]
+    guard = 64
+
+    def run(offsets):
+        off = torch.tensor(offsets, dtype=torch.int32, device="cuda")
+        whole = {n: torch.full((T + 2 * guard, H, d), 7.0, dtype=BF, device="cuda") for n, H in (("o", Hq), ("dq", Hq), ("dk", Hk), ("dv", Hk))}
+        y = {n: t[guard:-guard] for n, t in whole.items()}
+        lse = torch.empty((Hq, T), dtype=torch.float32, device="cuda")
+        space = lambda n: torch.empty(max(n, 256), dtype=torch.uint8, device="cuda")   # noqa: E731
+        av.ragged_fwd(q, k, v, off, off, y["o"], lse, 0.125, space(av.ragged_fwd_workspace_bytes(T, T, S, Hq, Hk, d)), True)
+        av.ragged_bwd(q, k, v, off, off, y["o"], lse, do, y["dq"], y["dk"], y["dv"], 0.125, space(av.ragged_bwd_workspace_bytes(T, T, S, Hq, Hk, d)), True)
+        for n, t in whole.items():
+            assert (t[:guard] == 7).all() and (t[-guard:] == 7).all(), n
+        return y
+
+    a, b = run(inside), run(outside)
+    assert all(torch.equal(a[n], b[n]) for n in a)
+    g = torch.Generator().manual_seed(S)
+    for _ in range(3):
+        run(torch.randint(-50, 700, (S + 1,), generator=g).tolist())
