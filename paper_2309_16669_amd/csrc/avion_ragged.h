@@ -1209,7 +1209,7 @@ DEVINL void ragged_whole(char* smem, const RaggedArgs& a, const raw16* __restric
     RowStore<D, E>::run(region, dva, std::is_same<E, F16>::value ? 1.f / 256.f : 1.f, dv + k_at + row0 * rs, rs, nk - row0, lane);
 }
 template <int D, int W, typename E>
-__global__ void __launch_bounds__(W * 64, D == 128 ? 1 : 2)
+__global__ void __launch_bounds__(W * 64, (RaggedWholeCfg<D, W>::LDS_BYTES > 80 * 1024 || D == 128 ? 1 : 2))
 avion_ragged_whole_kernel(RaggedArgs a, const raw16* __restrict__ dO, const float* __restrict__ lse, raw16* __restrict__ dq,
                           raw16* __restrict__ dk, raw16* __restrict__ dv)
 {

@@ -261,9 +261,12 @@ int avion_ragged_bwd(const void* q, const void* k, const void* v, const int* off
     return by_head(d, flags, [&](auto dim, auto fmt) {
         constexpr int D = decltype(dim)::value;
         using E = typename decltype(fmt)::type;
-        // short sequences whose heads are their own: whole, up to 64 tokens (of 128 channels) or 128; the two passes below take the others
+        // short sequences whose heads are their own: whole, up to 64 tokens or 128; the two passes below take the others.  Beyond 64 tokens
+        // of 80 channels a compute unit holds one such workgroup: 16 heads, 1024 sequences of 77, 512 (8 heads) of 100 and 1024 of 128 tokens
+        // 785, 255 and 1058 us, in two passes 633, 232 and 1554; of 64 channels two, 2048 (8 heads) of 77, 1000 of 100 and of 128 384, 231 and 250,
+        // 479, 270 and 467
         if (a.G == 1 && S > 0 && std::max(Tq, Tk) <= 128 * S) {
-            a.done = D == 128 ? 64 : 128;
+            a.done = D == 128 || (D == 80 && std::max(Tq, Tk) < 112 * S) ? 64 : 128;
             a.more = reinterpret_cast<int*>(static_cast<char*>(workspace) + scalar_bytes(s) + parts_bytes(s));
             int rc3 = AVION_OK;
             const auto whole = [&](auto w) {
@@ -278,7 +281,8 @@ int avion_ragged_bwd(const void* q, const void* k, const void* v, const int* off
             };
             whole(Int<1>{});
             whole(Int<2>{});
-            if constexpr (D < 128) whole(Int<4>{});
+            if constexpr (D < 128)
+                if (a.done == 128) whole(Int<4>{});
             if (rc3 != AVION_OK) return rc3;
         }
         if (Tq > 0) {

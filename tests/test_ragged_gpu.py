@@ -158,6 +158,14 @@ def test_short_sequences_whole(nq, nk, d, dtype, causal):
 
 
 @pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("d,dtype", [(64, F16), (80, BF), (80, F16)], ids=str)
+def test_sequences_whole_up_to_128_tokens(d, dtype, causal):
+    nq = [128, 127, 120, 97, 110, 125, 128]     # 119 on average
+    _check(nq, nq, 3, 3, d, dtype, causal)
+    _check(nq, nq[::-1], 3, 3, d, dtype, causal)
+
+
+@pytest.mark.parametrize("causal", [False, True])
 @pytest.mark.parametrize("S", [1, 2, 7, 61, 62])
 @pytest.mark.parametrize("same", [True, False])
 def test_order_of_sequences(S, same, causal):
