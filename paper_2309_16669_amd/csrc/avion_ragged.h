@@ -73,12 +73,34 @@ DEVINL RaggedPlace ragged_place(const int* off, int S, int T, int mul, long slot
     p.block = slot - (((long)p.begin * mul) >> SHIFT) - p.i;
     return p;
 }
-// The block whose turn it is, the `turn`th of those that begin.  Up to kRaggedOrdered sequences the ones with the most tokens on the other
-// side come first and rows of no sequence last, all blocks of a sequence together, the last of them first where it sees the most
-// (BACK): the launch then ends with its shortest workgroups.  A lane holds an interval's length and counts the blocks of those before it.
-// More sequences keep their order, from the last one on with BACK.
-// 16 sequences of 196 to 3136 tokens, 12 heads, 64 channels, forward, dQ and dK/dV: 82 + 93 + 113 us, in their own order 103 + 116 + 132; the
-// search costs half a microsecond at 37 sequences.
+// Over the lanes up to each: the sum, the largest
+DEVINL int lanes_sum(int x)
+{
+    x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false);  // 1, 2, 4 and 8 lanes down a row of 16
+    x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);  // a row's last lane to the next row, the second row's to both behind
+    x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);
+    return x;
+}
+DEVINL int lanes_max(int x)
+{
+    x = max(x, __builtin_amdgcn_update_dpp(x, x, 0x111, 0xf, 0xf, false));
+    x = max(x, __builtin_amdgcn_update_dpp(x, x, 0x112, 0xf, 0xf, false));
+    x = max(x, __builtin_amdgcn_update_dpp(x, x, 0x114, 0xf, 0xf, false));
+    x = max(x, __builtin_amdgcn_update_dpp(x, x, 0x118, 0xf, 0xf, false));
+    x = max(x, __builtin_amdgcn_update_dpp(x, x, 0x142, 0xa, 0xf, false));
+    x = max(x, __builtin_amdgcn_update_dpp(x, x, 0x143, 0xc, 0xf, false));
+    return x;
+}
+// The block whose turn it is, the `turn`th of those that begin.  Up to kRaggedOrdered sequences, of which a lane holds one, begin in up
+// to eight classes by the tokens on the other side, the most first (the three highest bits that there are), rows of no sequence in the last
+// one; all blocks of a sequence together, the last of them first where it sees the most (BACK).  The launch then ends with its
+// shortest workgroups.  More sequences keep their order, from the last one on with BACK.
+// 16 sequences of 196 to 3136 tokens, 12 heads, 64 channels, forward, dQ and dK/dV: 80 + 92 + 113 us, in four classes
+// 83 + 95 + 118, in their own order 103 + 116 + 132; 37 of 400 to 1100, 16 heads on 2 of 80, all passes 125, wholly sorted (40 steps of a search
+// in every wavefront) 130
 constexpr int kRaggedOrdered = 61;
 template <int SHIFT, bool BACK>
 DEVINL RaggedPlace ragged_turn(const int* off, int S, int T, int mul, const int* other, int others, int slots, int turn, int lane)
@@ -88,13 +110,14 @@ DEVINL RaggedPlace ragged_turn(const int* off, int S, int T, int mul, const int*
     const bool sequence = lane > 0 && lane <= S;
     const int seen = sequence ? max(ragged_border(other, S, others, lane + 1) - ragged_border(other, S, others, lane), 0) : -1;
     const int blocks = (int)(((long)n * mul + (1 << SHIFT) - 1) >> SHIFT);
-    int before = 0;
-    for (int i = 0; i < S + 2; i += 8)
+    const int most = __builtin_amdgcn_readlane(lanes_max(seen), 63), shift = max(29 - __clz(most | 1), 0), rank = min((most >> shift) - (seen >> shift), 7);
+    int before = 0, begun = 0;
 #pragma unroll
-        for (int j = i; j < i + 8; ++j) {  // (lanes without an interval have no blocks)
-            const int s = __builtin_amdgcn_readlane(seen, j), b = __builtin_amdgcn_readlane(blocks, j);
-            before += s + (j < lane) > seen ? b : 0;
-        }
+    for (int c = 0; c < 8; ++c) {
+        const int upto = lanes_sum(rank == c ? blocks : 0);
+        before = rank == c ? begun + upto - blocks : before;
+        begun += __builtin_amdgcn_readlane(upto, 63);
+    }
     const unsigned long long owner = __ballot(turn >= before && turn - before < blocks);
     if (owner == 0) return RaggedPlace{0, 0, 0, 0};
     const int i = __builtin_ctzll(owner), in = turn - __builtin_amdgcn_readlane(before, i);
