@@ -22,6 +22,7 @@
 #pragma once
 #include "avion_bwd.h"
 #include "avion_common.h"
+#include "avion_ragged_search.h"
 
 struct RaggedArgs {
     const raw16 *q, *k, *v;
@@ -41,37 +42,24 @@ struct RaggedArgs {
     DEVINL int over_heads(int r) const { return (int)((__umulhi(g_mul, (unsigned)r) + (unsigned)r) >> g_shift); }
 };
 
-// border i of 0 .. S + 2: 0, the offsets, T
-DEVINL int ragged_border(const int* off, int S, int T, int i)
-{
-    if (i <= 0) return 0;
-    if (i > S + 1) return T;
-    return min(max(off[i - 1], 0), T);
-}
-struct RaggedPlace {
-    int i;        // interval of the borders (0 and S + 1: rows of no sequence)
-    int begin, n; // its tokens
-    long block;   // of BM rows
+// The lanes of a wavefront that search in device memory (see ragged_search)
+struct RaggedLanes {
+    const int* off;
+    int S, T, lane, border;
+    DEVINL void load(int lo, int step) { border = ragged_border(off, S, T, lo + lane * step); }
+    template <typename F>
+    DEVINL int count(F begun) const
+    {
+        return (int)__popcll(__ballot(begun(lane, border)));
+    }
+    DEVINL int at(int l) const { return __builtin_amdgcn_readlane(border, l); }
 };
 // The interval that owns `slot`, for blocks of 2^SHIFT rows and `mul` rows a token.  Wavefront-uniform.
 template <int SHIFT>
 DEVINL RaggedPlace ragged_place(const int* off, int S, int T, int mul, long slot, int lane)
 {
-    int lo = 0, n = S + 2, c = 0, border = 0;
-    do {  // the last step's lanes hold every border that is left, and the one behind them
-        const int step = (n + 62) / 63, at = lane * step;
-        border = ragged_border(off, S, T, lo + at);
-        const bool begun = at < n && (((long)border * mul) >> SHIFT) + lo + at <= slot;
-        c = max((int)__popcll(__ballot(begun)), 1) - 1;
-        lo += c * step;
-        n = min(step, n - c * step);
-    } while (n > 1);
-    RaggedPlace p;
-    p.i = lo;
-    p.begin = __builtin_amdgcn_readlane(border, c);
-    p.n = max(__builtin_amdgcn_readlane(border, c + 1) - p.begin, 0);
-    p.block = slot - (((long)p.begin * mul) >> SHIFT) - p.i;
-    return p;
+    RaggedLanes lanes{off, S, T, lane, 0};
+    return ragged_search<SHIFT>(lanes, S, mul, slot);
 }
 // Over the lanes up to each: the sum, the largest
 DEVINL int lanes_sum(int x)

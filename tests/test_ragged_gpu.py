@@ -356,3 +356,45 @@ def test_offsets_outside_the_tensors(S):
     g = torch.Generator().manual_seed(S)
     for _ in range(3):
         run(torch.randint(-50, 700, (S + 1,), generator=g).tolist())
+
+
+def _many(S, kind, seed):
+    """Queries and keys of S sequences."""
+    g = torch.Generator().manual_seed(seed)
+    if kind == "tokens":        # one behind a cache each
+        return [1] * S, torch.randint(200, 420, (S,), generator=g).tolist()
+    nq = torch.randint(0, 60 if kind != "blocks" else 190, (S,), generator=g).tolist()
+    return nq, nq if kind != "other" else torch.randint(0, 60, (S,), generator=g).tolist()
+
+
+def _some(S):
+    """Sequences at the ends of what a step of the search leaves over (every 65th of 4031, 66th of 4157, ...), their neighbours, and some."""
+    step = (S + 2 + 62) // 63
+    ends = {i + k for i in range(step - 2, S, step) for k in (-1, 0, 1, 2)}
+    return sorted(i for i in ends | {0, 1, S // 3, S // 2, S - 2, S - 1} | set(range(0, S, 97)) if 0 <= i < S)
+
+
+@pytest.mark.parametrize("S,kind,Hq,Hk,d,dtype,causal", [
+    (4031, "same", 1, 1, 64, BF, False), (4031, "same", 2, 1, 64, BF, True), (4031, "other", 1, 1, 64, F16, True), (4031, "other", 4, 1, 80, BF, False),
+    (4031, "tokens", 4, 1, 64, BF, True), (4031, "blocks", 2, 1, 64, BF, True), (4031, "blocks", 1, 1, 64, F16, False),
+    (4093, "same", 2, 2, 80, F16, True), (4093, "tokens", 8, 1, 128, BF, False), (4157, "other", 2, 1, 128, BF, True),
+    (4157, "blocks", 2, 1, 80, BF, True), (4345, "same", 2, 1, 128, F16, True), (6050, "same", 1, 1, 64, BF, True), (6050, "tokens", 2, 1, 64, F16, True),
+    (16384, "same", 1, 1, 64, BF, True), (16384, "other", 2, 1, 64, BF, False)], ids=str)
+def test_every_sequence_of_many_is_its_own(S, kind, Hq, Hk, d, dtype, causal):
+    """Numbers of sequences at which a wide step of the search leaves a single one: none may take its neighbour's tokens for its own."""
+    nq, nk = _many(S, kind, S + d)
+    g = torch.Generator("cuda").manual_seed(S)
+    q, k, v, do = (torch.randn(s, generator=g, device="cuda").to(dtype) for s in
+                   ((sum(nq), Hq, d), (sum(nk), Hk, d), (sum(nk), Hk, d), (sum(nq), Hq, d)))
+    for t in (q, k, v):
+        t.requires_grad_(True)
+    o = _ag().attention_ragged(q, k, v, _offsets(nq), None if nk is nq else _offsets(nk), causal=causal)
+    dq, dk, dv = torch.autograd.grad(o, (q, k, v), do)
+    with torch.no_grad():
+        assert torch.equal(o, _ag().attention_ragged(q, k, v, _offsets(nq), None if nk is nq else _offsets(nk), causal=causal))
+    bq, bk = _offsets(nq, "cpu").tolist(), _offsets(nk, "cpu").tolist()
+    some = _some(S)
+    rows = torch.cat([torch.arange(bq[i], bq[i + 1]) for i in some]).cuda()
+    keys = torch.cat([torch.arange(bk[i], bk[i + 1]) for i in some]).cuda()
+    out, tol = _reference(q[rows], k[keys], v[keys], do[rows], [nq[i] for i in some], [nk[i] for i in some], 1 / math.sqrt(d), causal)
+    _compare({"o": o[rows], "dq": dq[rows], "dk": dk[keys], "dv": dv[keys]}, out, tol, ("o", "dq", "dk", "dv"))
