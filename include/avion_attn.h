@@ -386,7 +386,8 @@ int avion_linear_fp8(const void *x8, const float *x_scale, const void *w8, const
  *   freqs     : fp32 [pairs], radians a step;   sections: `axes` numbers on the HOST, their sum is `pairs`
  *   Pairs are channels j and pairs + j, or with AVION_FLAG_INTERLEAVED 2 j and 2 j + 1.  Channels from 2 * pairs on are copied.
  *   AVION_FLAG_INVERSE: -theta, the backward (the gradient of q is the inverse turn of the gradient of yq).
- *   d a multiple of 8 up to 4096; pairs a multiple of 8 up to 512, 2 * pairs <= d; axes <= 4; T <= 2^27 - 8; rs a multiple of 8
+ *   d a multiple of 8 up to 4096; pairs a multiple of 8 up to 512, 2 * pairs <= d; axes <= 4; T <= 2^27 - 8; Hq and Hk up to 65536; rs a
+ *   multiple of 8 up to 2^31
  * Angles are formed in 64 bits and reduced to one turn before they are rounded, so far positions lose nothing; one rounding of the
  * result.  T = 0: nothing happens.  Pointers 16-byte aligned (positions and freqs naturally).
  */
@@ -412,7 +413,8 @@ int avion_rotary(const void *q, const void *k, const void *positions, const floa
  * offset, from the last one on) have o = 0 and lse = -inf, and gradients 0.  What a sequence holds reaches no other one.  Within a
  * sequence infinities and NaN are not checked and propagate, past a mask too.  Offsets are not checked: values outside 0 .. T are
  * taken as the nearest of these, and decreasing ones give rows without a defined value, never an access outside the tensors.
- *   Tq, Tk up to 2^28, S up to 2^20, Tq * Hq / Hk up to 2^30, (Tq * Hq / Hk + Tk + 128 S) * Hk below 2^31 - 2^16 * Hk; scale as for avion_attn_fwd
+ *   Tq, Tk up to 2^28, S up to 2^20, Hq up to 65536, Tq * Hq / Hk up to 2^30, (Tq * Hq / Hk + Tk + 128 S) * Hk below 2^31 - 2^16 * Hk, rs up
+ *   to 2^23; scale as for avion_attn_fwd
  *   workspace: 256-byte aligned, avion_ragged_fwd_workspace_bytes / _bwd_workspace_bytes bytes of these sizes (0: unsupported),
  *   contents ignored and left unspecified; calls that overlap in time must not share one.  The forward's may be NULL where
  *   Tq = Tk.

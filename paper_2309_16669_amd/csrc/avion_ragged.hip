@@ -26,9 +26,8 @@ int ragged_check(const RaggedShape& s)
     if (s.Tq < 0 || s.Tk < 0 || s.S < 0 || s.Hq < 1 || s.Hk < 1 || s.d < 1 || s.Hq % s.Hk != 0) return AVION_EINVAL;
     if ((s.d != 64 && s.d != 80 && s.d != 128) || s.Tq > kMostTokens || s.Tk > kMostTokens || s.S > kMostSequences) return AVION_EUNSUPPORTED;
     const long long G = s.Hq / s.Hk;
-    if (s.Hq > (1 << 16) || s.Tq * G > (1LL << 30) || (s.Tq * G / 32 + s.Tk / 32 + s.S + 2) * s.Hq > 0x7fffffffLL) return AVION_EUNSUPPORTED;
+    if (s.Hq > (1 << 16) || s.Tq * G > (1LL << 30)) return AVION_EUNSUPPORTED;  // (rows of up to kMostStride elements, rows' numbers in an int)
     if ((s.Tq * G / 128 + s.Tk / 128 + s.S + 4) * s.Hk * 256 > 0xffffffffLL) return AVION_EUNSUPPORTED;  // threads of a launch
-    if ((long long)s.Hq * s.d > kMostStride) return AVION_EUNSUPPORTED;
     return AVION_OK;
 }
 bool stride_ok(long long rs, int H, int d) { return rs >= (long long)H * d; }

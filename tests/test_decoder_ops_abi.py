@@ -106,6 +106,19 @@ def test_workspace_sizes():
     assert ce_b((1 << 28) - 1, 1 << 28, 8) > 1 << 36                  # in size_t throughout
 
 
+@pytest.mark.parametrize("last,first", [
+    (dict(Hq=64, Tq=1 << 24), dict(Hq=64, Tq=(1 << 24) + 1)), (dict(Hq=1 << 16, Tq=1 << 14), dict(Hq=1 << 16, Tq=(1 << 14) + 1)),
+    (dict(Tq=1 << 28), dict(Tq=(1 << 28) + 1)), (dict(Tk=1 << 28), dict(Tk=(1 << 28) + 1)), (dict(S=1 << 20), dict(S=(1 << 20) + 1)),
+    (dict(Hq=1 << 16), dict(Hq=(1 << 16) + 1)), (dict(Hq=1 << 16, d=128), dict(Hq=(1 << 16) + 1, d=128)),
+    (dict(Hq=8, Hk=8, Tq=(1 << 27) - (1 << 15), Tk=(1 << 27) - (1 << 15) - 128 * 3 - 1, S=3), dict(Hq=8, Hk=8, Tq=1 << 27, Tk=1 << 27, S=3)),
+    (dict(Hq=16, Hk=16, S=(1 << 20) - 512 - 1), dict(Hq=16, Hk=16, S=1 << 20))], ids=str)
+def test_the_limits_of_ragged_sequences_are_the_documented_ones(last, first):
+    """The last sizes that the contract gives, and the next ones; nothing is launched."""
+    for call in (av.ragged_fwd_workspace_bytes, av.ragged_bwd_workspace_bytes):
+        at = [call(*(dict(dict(Tq=64, Tk=64, S=1, Hq=1, Hk=1, d=64), **sizes).values())) for sizes in (last, first)]
+        assert at[0] >= 256 and at[1] == 0
+
+
 def test_the_front_end_refuses():
     import torch
     from paper_2309_16669_amd import autograd as ag

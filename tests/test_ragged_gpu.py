@@ -398,3 +398,21 @@ def test_every_sequence_of_many_is_its_own(S, kind, Hq, Hk, d, dtype, causal):
     keys = torch.cat([torch.arange(bk[i], bk[i + 1]) for i in some]).cuda()
     out, tol = _reference(q[rows], k[keys], v[keys], do[rows], [nq[i] for i in some], [nk[i] for i in some], 1 / math.sqrt(d), causal)
     _compare({"o": o[rows], "dq": dq[rows], "dk": dk[keys], "dv": dv[keys]}, out, tol, ("o", "dq", "dk", "dv"))
+
+
+def test_tens_of_thousands_of_heads_on_one():
+    """32768 query heads, 2048 times the same 16, on one key head: O and dQ are those of the 16, dK and dV 2048 times theirs, up to the fp32
+    sums' own roundings (each of less than 2^15 products of 16 rows, one after the other: 2^-9 of the magnitudes)."""
+    nq, times, d = [40, 30], 2048, 64
+    q, k, v, do = _inputs(nq, nq, 16, 1, d, BF, 8)
+    x = [q.repeat(1, times, 1).requires_grad_(True), k.clone().requires_grad_(True), v.clone().requires_grad_(True)]
+    o = _ag().attention_ragged(*x, _offsets(nq), causal=True)
+    dq, dk, dv = torch.autograd.grad(o, x, do.repeat(1, times, 1))
+    out, tol = _reference(q, k, v, do, nq, nq, 1 / math.sqrt(d), True)
+    for first in (0, 16 * 1023, 16 * 2047):
+        _compare({"o": o[:, first:first + 16], "dq": dq[:, first:first + 16]}, out, tol, ("o", "dq"))
+    assert torch.equal(o, o[:, :16].repeat(1, times, 1)) and torch.equal(dq, dq[:, :16].repeat(1, times, 1))
+    u = torch.finfo(BF).eps / 2
+    for got, n in ((dk, "dk"), (dv, "dv")):
+        # (what the bound of the 16 has beside the rounding of the result: at least u of the magnitudes that were summed)
+        assert ((got.cpu().double() / times - out[n]).abs() <= tol[n] * (1 + 2.0 ** -9 / u)).all(), n
