@@ -506,18 +506,20 @@ def rotary(q, k, positions, freqs, sections=None, interleaved: bool = False):
     """Queries and keys (bf16 or fp16 [..., H, d], the same leading shape; k may be None) turned by their tokens' positions: pair j of
     a head's first 2 * len(freqs) channels by positions[axis of j] * freqs[j] radians; the other channels stay.  positions (int64,
     int32 or float32): one axis, with the leading shape or its last part (then shared over what stands before it: the clips of a
-    batch); with `sections`, the pairs of up to four axes (time, height, width), such a tensor for each axis, stacked.  Pairs are
-    channels j and len(freqs) + j, or neighbours if `interleaved`.  len(freqs) and d are multiples of 8.  Returns (q, k), or q where
-    k is None.  Differentiable once in q and k; keeps neither."""
-    sections = (freqs.shape[0],) if sections is None else tuple(int(n) for n in sections)
+    batch); with `sections`, the pairs of up to four axes (time, height, width), such a tensor for each axis, stacked (that of a single
+    axis also alone).  Pairs are channels j and len(freqs) + j, or neighbours if `interleaved`.  len(freqs) and d are multiples of 8.
+    Returns (q, k), or q where k is None.  Differentiable once in q and k; keeps neither."""
+    stacked = sections is not None
+    sections = tuple(int(n) for n in sections) if stacked else (freqs.shape[0],)
     lead, place = tuple(q.shape[:-2]), tuple(positions.shape)
     if q.dim() < 3 or (k is not None and tuple(k.shape[:-2]) != lead):
         raise ValueError(f"q and k must have shape [..., H, d] with the same leading shape, got {tuple(q.shape)} and "
                          f"{None if k is None else tuple(k.shape)}")
     if len(sections) > 1 and (not place or place[0] != len(sections)):
         raise ValueError(f"positions must hold {len(sections)} axes, got shape {place}")
-    own = place[1:] if len(sections) > 1 else place
-    if not own or lead[len(lead) - len(own):] != own:
+    # (one axis may stand alone, or be a stack of one)
+    shapes = [place[1:]] if len(sections) > 1 else [place, place[1:]] if stacked and place[:1] == (1,) else [place]
+    if not any(own and lead[len(lead) - len(own):] == own for own in shapes):
         raise ValueError(f"positions of shape {place} do not fit tokens of shape {lead}")
     if positions.device != q.device or freqs.device != q.device:
         raise ValueError("tensors must live on one GPU")

@@ -141,6 +141,20 @@ def test_the_front_end_refuses():
     assert ag.rotary_frequencies((4, 4)).tolist() == ag.rotary_frequencies(4).tolist() * 2
 
 
+def test_one_axis_of_positions_may_be_a_stack_of_one():
+    """With `sections`, a tensor for each axis, stacked; for one axis also the tensor alone.  (These tensors are on the host, which is all that
+    is wrong with them.)"""
+    import torch
+    from paper_2309_16669_amd import autograd as ag
+    q, at, freqs = torch.zeros(3, 6, 4, 64, dtype=torch.bfloat16), torch.arange(6), torch.ones(32)
+    for positions, sections in ((at, (32,)), (at[None], (32,)), (at.expand(3, 6), (32,)), (at.expand(1, 3, 6), (32,)), (at, None)):
+        with pytest.raises(ValueError, match="must live on the GPU"):
+            ag.rotary(q, None, positions, freqs, sections)
+    for positions, sections in ((at[None], None), (at.expand(1, 3, 6), None), (at.expand(2, 6), (32,)), (at[None, None], (32,)), (at[:1], (32,))):
+        with pytest.raises(ValueError, match="do not fit tokens"):
+            ag.rotary(q, None, positions, freqs, sections)
+
+
 def test_headers_flags_match_the_binding():
     import os
     import re

@@ -136,3 +136,15 @@ def test_graph_and_second_derivative():
     (g,) = torch.autograd.grad(y, (q,), w, create_graph=True)
     with pytest.raises(RuntimeError, match="no second derivative"):
         g.float().sum().backward()
+
+
+@pytest.mark.parametrize("native", [True, False])
+def test_one_axis_of_positions_stacked(native, monkeypatch):
+    if not native:
+        import types
+        monkeypatch.setattr(_ag(), "_native", types.SimpleNamespace(rotary=lambda *args: None))
+    q = torch.randn((2, 30, 3, 64), generator=torch.Generator().manual_seed(6)).to(torch.bfloat16).cuda()
+    places, freqs = torch.arange(7, 37, device="cuda"), _ag().rotary_frequencies(24, device="cuda")
+    want = _ag().rotary(q, None, places, freqs)
+    for given in (places, places[None], places.expand(2, 30), places.expand(1, 2, 30)):
+        assert torch.equal(_ag().rotary(q, None, given, freqs, (24,)), want)
