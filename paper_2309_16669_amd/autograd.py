@@ -508,7 +508,8 @@ def rotary(q, k, positions, freqs, sections=None, interleaved: bool = False):
     int32 or float32): one axis, with the leading shape or its last part (then shared over what stands before it: the clips of a
     batch); with `sections`, the pairs of up to four axes (time, height, width), such a tensor for each axis, stacked (that of a single
     axis also alone).  Pairs are channels j and len(freqs) + j, or neighbours if `interleaved`.  len(freqs) and d are multiples of 8.
-    Returns (q, k), or q where k is None.  Differentiable once in q and k; keeps neither."""
+    Returns (q, k), or q where k is None.  Differentiable once in q and k, of which it keeps neither; positions and freqs whose gradient
+    is being recorded are refused."""
     stacked = sections is not None
     sections = tuple(int(n) for n in sections) if stacked else (freqs.shape[0],)
     lead, place = tuple(q.shape[:-2]), tuple(positions.shape)
@@ -521,6 +522,8 @@ def rotary(q, k, positions, freqs, sections=None, interleaved: bool = False):
     shapes = [place[1:]] if len(sections) > 1 else [place, place[1:]] if stacked and place[:1] == (1,) else [place]
     if not any(own and lead[len(lead) - len(own):] == own for own in shapes):
         raise ValueError(f"positions of shape {place} do not fit tokens of shape {lead}")
+    if torch.is_grad_enabled() and (freqs.requires_grad or positions.requires_grad):
+        raise ValueError("rotary has no gradient of positions and freqs: detach them, or call it under torch.no_grad()")
     if positions.device != q.device or freqs.device != q.device:
         raise ValueError("tensors must live on one GPU")
     out = (_native or native_calls()).rotary(q, k, positions, freqs, sections, bool(interleaved))

@@ -155,6 +155,22 @@ def test_one_axis_of_positions_may_be_a_stack_of_one():
             ag.rotary(q, None, positions, freqs, sections)
 
 
+def test_a_gradient_that_rotary_does_not_have_is_refused():
+    """A learned spectrum, or learned places between frames, would silently get none."""
+    import torch
+    from paper_2309_16669_amd import autograd as ag
+    q, at, freqs = torch.zeros(6, 4, 64, dtype=torch.bfloat16), torch.arange(6).float(), torch.ones(32)
+    for positions, f in ((at, freqs.clone().requires_grad_(True)), (at.clone().requires_grad_(True), freqs),
+                         (at, torch.nn.Parameter(freqs) * 2)):
+        for k in (None, q[:, :2]):
+            with pytest.raises(ValueError, match="no gradient of positions and freqs"):
+                ag.rotary(q, k, positions, f)
+        with torch.no_grad(), pytest.raises(ValueError, match="must live on the GPU"):
+            ag.rotary(q, None, positions, f)
+        with pytest.raises(ValueError, match="must live on the GPU"):
+            ag.rotary(q, None, positions.detach(), f.detach())
+
+
 def test_headers_flags_match_the_binding():
     import os
     import re
