@@ -463,15 +463,17 @@ def _rows(t):
 
 
 def _turn_rows(q, k, positions, freqs, sections, interleaved, inverse):
+    def tokens(t):      # (not -1: there may be no head)
+        return None if t is None else t.reshape(math.prod(t.shape[:-2]), *t.shape[-2:])
+
     def rows(t):
-        return None if t is None else _rows(t.reshape(-1, *t.shape[-2:]))
+        return None if t is None else _rows(tokens(t))
 
     def out(t):
         return None if t is None else torch.empty(t.shape, dtype=t.dtype, device=t.device)
 
     yq, yk = out(q), out(k)
-    _rotary(rows(q), rows(k), positions, freqs, sections, yq.view(-1, *q.shape[-2:]), None if yk is None else yk.view(-1, *k.shape[-2:]),
-            interleaved, inverse)
+    _rotary(rows(q), rows(k), positions, freqs, sections, tokens(yq), tokens(yk), interleaved, inverse)
     return yq, yk
 
 
@@ -529,7 +531,7 @@ def rotary(q, k, positions, freqs, sections=None, interleaved: bool = False):
     out = (_native or native_calls()).rotary(q, k, positions, freqs, sections, bool(interleaved))
     if out is not None:
         return out
-    if q.numel() == 0:
+    if q.numel() == 0 and (k is None or k.numel() == 0):
         return q.clone() if k is None else (q.clone(), k.clone())
     return _Rotary.apply(q, k, positions.contiguous().view(len(sections), -1), freqs.contiguous(), sections, bool(interleaved))
 

@@ -171,6 +171,14 @@ def test_a_gradient_that_rotary_does_not_have_is_refused():
             ag.rotary(q, None, positions.detach(), f.detach())
 
 
+def test_keys_beside_no_query_head_do_not_come_back_as_they_are():
+    import torch
+    from paper_2309_16669_amd import autograd as ag
+    q, k = torch.zeros(6, 0, 64, dtype=torch.bfloat16), torch.ones(6, 2, 64, dtype=torch.bfloat16)
+    with pytest.raises(ValueError, match="must live on the GPU"):
+        ag.rotary(q, k, torch.arange(6), torch.ones(32))
+
+
 def test_headers_flags_match_the_binding():
     import os
     import re

@@ -148,3 +148,14 @@ def test_one_axis_of_positions_stacked(native, monkeypatch):
     want = _ag().rotary(q, None, places, freqs)
     for given in (places, places[None], places.expand(2, 30), places.expand(1, 2, 30)):
         assert torch.equal(_ag().rotary(q, None, given, freqs, (24,)), want)
+
+
+def test_no_head_on_one_side():
+    """No key head: the queries turn, and nothing comes back beside them.  No query head beside keys: refused."""
+    import paper_2309_16669_amd as av
+    x, none = torch.randn((30, 3, 64), generator=torch.Generator().manual_seed(8)).to(torch.bfloat16).cuda(), torch.zeros((30, 0, 64), dtype=torch.bfloat16, device="cuda")
+    places, freqs = torch.arange(30, device="cuda"), _ag().rotary_frequencies(32, device="cuda")
+    y, z = _ag().rotary(x, none, places, freqs)
+    assert torch.equal(y, _ag().rotary(x, None, places, freqs)) and z.shape == none.shape
+    with pytest.raises(av.AvionError):
+        _ag().rotary(none, x, places, freqs)
