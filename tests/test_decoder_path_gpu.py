@@ -292,3 +292,48 @@ def test_nothing_at_all(native, monkeypatch):
         loss = ag.linear_cross_entropy(x, w, torch.zeros(0, dtype=torch.int64, device="cuda"), reduction=reduction)
         dx, dw = torch.autograd.grad(loss.sum(), (x, w))
         assert float(loss.detach().sum()) == 0 and dx.shape == x.shape and dw.shape == w.shape and not dw.any()
+
+
+def _pass_with_saved(f, args, change):
+    """_pass, with each saved tensor number i (in the order of saving) given back as change(i, tensor)."""
+    leaves = [a.detach().requires_grad_(True) for a in args]
+    count = iter(range(100))
+    with torch.autograd.graph.saved_tensors_hooks(lambda t: (next(count), t), lambda packed: change(*packed)):
+        y = f(*leaves)
+    y = y if isinstance(y, tuple) else (y,)
+    return [*(t.detach() for t in y), *torch.autograd.grad(y, leaves, [torch.full_like(t, 0.5) for t in y])]
+
+
+def _spread(t):
+    """The same numbers, rows twice as far apart, others between them."""
+    if t.dim() == 2:
+        return torch.cat([t, torch.full_like(t, 7)], 1)[:, :t.shape[1]]
+    return torch.cat([t, torch.full_like(t, 7)], 1)[:, :t.shape[1]] if t.dim() == 3 else t
+
+
+@pytest.mark.parametrize("which", ["front", "class"])
+@pytest.mark.parametrize("name,inputs", [("attention", (0, 1, 2)), ("loss", (0, 1)), ("losses", (0, 1))])
+def test_saved_inputs_of_other_strides_give_the_same_gradients(name, inputs, which):
+    """q, k and v, or x and weight, come back from a hook with their rows further apart: read where they lie, to the same bits."""
+    front, cls, args = _calls()[name]
+    f = front if which == "front" else cls
+    want, seen = _pass(f, args), []
+
+    def change(i, t):
+        if i not in inputs:
+            return t
+        seen.append(i)
+        s = _spread(t)
+        assert not s.is_contiguous() and torch.equal(s, t)
+        return s
+
+    got = _pass_with_saved(f, args, change)
+    assert sorted(set(seen)) == list(inputs)
+    assert all(torch.equal(a, b) for a, b in zip(got, want, strict=True))
+
+
+@pytest.mark.parametrize("which", ["front", "class"])
+def test_a_saved_output_of_other_strides_is_refused(which):
+    front, cls, args = _calls()["attention"]
+    with pytest.raises(ValueError, match="o must be contiguous"):
+        _pass_with_saved(front if which == "front" else cls, args, lambda i, t: _spread(t) if i == 5 else t)

@@ -273,3 +273,26 @@ def test_no_second_derivative():
     (g,) = torch.autograd.grad(_ag().linear_cross_entropy(x, w, t), (x,), create_graph=True)
     with pytest.raises(RuntimeError, match="no second derivative"):
         g.float().sum().backward()
+
+
+@pytest.mark.parametrize("dtype", [BF, F16], ids=["bf16", "f16"])
+def test_what_a_row_without_a_target_holds_reaches_no_gradient(dtype):
+    """Large finite numbers in such rows, an ignored index inside the vocabulary, int32: the bits of dw and dx of rows of zeros.  NaN and
+    infinity are multiplied by zero for dw, and show there."""
+    x, w, t = _inputs(70, 90, 64, dtype, none=0.0)
+    t[::3] = 7
+    none = t == 7
+    results = []
+    for held, targets in ((0.0, t), (3e4, t), (-6e4, t.int()), (1.0, torch.where(none, -5, t)), (2.0, torch.where(none, 90, t).int())):
+        a, b = torch.where(none[:, None], torch.full_like(x, held), x).requires_grad_(True), w.detach().clone().requires_grad_(True)
+        for reduction in ("mean", "none"):
+            out = _ag().linear_cross_entropy(a, b, targets, ignore_index=7, reduction=reduction)
+            results.append((out, *torch.autograd.grad(out, (a, b), torch.ones_like(out))))
+    for r, want in zip(results[2:], results[:2] * 4, strict=True):
+        assert all(torch.equal(p, q) for p, q in zip(r, want, strict=True))
+    assert not results[0][1][none].any() and results[0][2].isfinite().all() and results[0][2].any()
+    for held in (float("nan"), float("inf")):
+        a, b = torch.where(none[:, None], torch.full_like(x, held), x).requires_grad_(True), w.detach().clone().requires_grad_(True)
+        out = _ag().linear_cross_entropy(a, b, t, ignore_index=7)
+        dx, dw = torch.autograd.grad(out, (a, b))
+        assert torch.equal(out, results[0][0]) and torch.equal(dx, results[0][1]) and dw.isnan().all()
