@@ -447,7 +447,8 @@ int avion_ragged_bwd(const void *q, const void *k, const void *v, const int *off
  *   loss, lse : out, fp32 [T]; loss may be NULL where total is given.   total : out, fp32 [2], or NULL: the sum of the losses (their
  *             mean over the rows with a target, 0 if there is none, with AVION_FLAG_MEAN) and the number of rows with a target
  *   dloss   : in, fp32 [T], or with AVION_FLAG_ONE_GRADIENT one number, the gradient of total[0]; then with AVION_FLAG_MEAN it is divided
- *             by total[1].  One that is not finite, of a row with a target, makes every gradient NaN
+ *             by total[1].  One that is not finite makes every gradient NaN (a row's own if the row has a target, a mean's if any
+ *             row has one)
  *   dx, dw  : out, fully overwritten; either may be NULL (not both)
  *   scale > 0 and finite; D a multiple of 8 up to 65536; T below 2^28, V up to 2^28; rs up to 2^20
  *   workspace: 256-byte aligned, avion_linear_ce_fwd_workspace_bytes / _bwd_workspace_bytes bytes (0: unsupported), contents ignored and

@@ -491,6 +491,7 @@ avion_loss_rows_kernel(LossArgs a, const float* __restrict__ lse, const float* _
     if (m == 0) {
         float d = each ? top : dloss[0];
         if (!each && mean) d = total[1] > 0.f ? d / total[1] : 0.f;
+        if (!(fabsf(d) <= 3.4028235e38f)) d = __builtin_nanf("");  // (infinity would leave infinities where a sum is not zero)
         factors[0] = d * a.scale / held;
     }
     if (m >= padded) return;

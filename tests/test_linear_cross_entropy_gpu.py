@@ -296,3 +296,21 @@ def test_what_a_row_without_a_target_holds_reaches_no_gradient(dtype):
         out = _ag().linear_cross_entropy(a, b, t, ignore_index=7)
         dx, dw = torch.autograd.grad(out, (a, b))
         assert torch.equal(out, results[0][0]) and torch.equal(dx, results[0][1]) and dw.isnan().all()
+
+
+@pytest.mark.parametrize("dtype", [BF, F16], ids=["bf16", "f16"])
+@pytest.mark.parametrize("reduction", ["mean", "sum", "none"])
+@pytest.mark.parametrize("given", [float("inf"), float("-inf"), float("nan")])
+def test_a_gradient_that_is_no_finite_number_makes_all_of_them_nan(given, reduction, dtype):
+    """As the contract says: a loss scale that has overflowed cannot leave some gradients looking sound."""
+    x, w, t = _inputs(70, 300, 64, dtype)
+    t[0] = 5
+    x.requires_grad_(True)
+    w.requires_grad_(True)
+    out = _ag().linear_cross_entropy(x, w, t, reduction=reduction)
+    dloss = torch.ones_like(out)
+    if reduction == "none":
+        dloss[0] = given
+    else:
+        dloss.fill_(given)
+    assert all(g.isnan().all() for g in torch.autograd.grad(out, (x, w), dloss))
