@@ -286,8 +286,8 @@ constexpr float kLossNone = -3.0e38f;
 // A workgroup takes TB rows through one of `slabs` runs of vocabulary tiles.  A lane holds, for each of its MI rows, the maximum and sum
 // (base 2, scaled) over the columns that its registers hold; they meet once, at the end: parts [slabs][T] of (maximum, sum).  The lane
 // that holds a row's target leaves its logit.
-// 16384 x 50000 x 768: 1080 to 1170 us = 1.08 to 1.17 PFLOP/s, matrix units 52 % of the cycles; 5 x 50000 x 512: 10.5 us for 51 MB; 2048 x 2048 x
-// 512: 10.
+// Medians on two cards: 16384 x 50000 x 768 1129 and 1179 us = 1.07 to 1.11 PFLOP/s, matrix units 52 % of the cycles; 5 x 50000 x 512 11 us for 51
+// MB; 2048 x 2048 x 512 10.
 template <int TA, int TB, int WA, int WB, typename E>
 __global__ void __launch_bounds__(WA* WB * 64, 2)
 avion_loss_fwd_kernel(LossArgs a, float2* __restrict__ parts, float* __restrict__ hit, int slabs, unsigned* __restrict__ ticket)
@@ -505,7 +505,8 @@ avion_loss_rows_kernel(LossArgs a, const float* __restrict__ lse, const float* _
 // dz of the vocabulary's columns v0 .. v0 + n - 1, [T, ld]; columns from n to the next multiple of 8 are zeros
 // What a tile's rows need (their targets, lse and factors, 1 KB each for 256 rows) comes to LDS with its first step: loaded where it is
 // used, it made every tile wait once more.  Columns of a target are rare (a wavefront's 32 x 64 logits of 50000 columns hold one in 25),
-// and so are columns past the end: both have a copy of the loop.  16384 x 25088 x 768: 720 to 760 us, matrix units 38 % of the cycles; 822 MB are written.
+// and so are columns past the end: both have a copy of the loop.  16384 x 25088 x 768: 742 and 771 us (medians on two
+// cards), matrix units 38 % of the cycles; 822 MB are written.
 constexpr int kLossRowBytes = 3 * 1024;
 template <int TA, int TB, int WA, int WB, typename E>
 __global__ void __launch_bounds__(WA* WB * 64, 2)
@@ -567,7 +568,8 @@ avion_loss_dz_kernel(LossArgs a, const int* __restrict__ rowdata, int padded, in
 // range and one piece of the vocabulary: the result, times factors[0], goes to `out`; else to planes of fp32, one a range (added to
 // what earlier pieces left), of which avion_loss_sum_kernel makes it.  A plane holds whole tiles in the accumulators' order (tile,
 // wavefront, 32 x 32 block, quarter, lane: 4 numbers), so that a wavefront reads and writes 1 KB at a time.
-// 16384 x 25088 x 768: 1130 to 1180 us for both = 1.07 to 1.12 PFLOP/s, matrix units 50 % of the cycles (the library's two products 1495).
+// 16384 x 25088 x 768: 1181 and 1202 us for both (medians on two cards) = 1.05 to 1.07 PFLOP/s, matrix units 50 % of the cycles (the library's
+// two products 1495).
 struct LossGrad {
     LossOperand a, b;
     int rows, K, splits;

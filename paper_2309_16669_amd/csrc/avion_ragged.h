@@ -86,7 +86,7 @@ DEVINL int lanes_max(int x)
 // to eight classes by the tokens on the other side, the most first (the three highest bits that there are), rows of no sequence in the last
 // one; all blocks of a sequence together, the last of them first where it sees the most (BACK).  The launch then ends with its
 // shortest workgroups.  More sequences keep their order, from the last one on with BACK.
-// 16 sequences of 196 to 3136 tokens, 12 heads, 64 channels, forward, dQ and dK/dV: 80 + 92 + 113 us, in four classes
+// 16 sequences of 196 to 3136 tokens, 12 heads, 64 channels, forward, dQ and dK/dV, best launches: 80 + 92 + 113 us, in four classes
 // 83 + 95 + 118, in their own order 103 + 116 + 132; 37 of 400 to 1100, 16 heads on 2 of 80, all passes 125, wholly sorted (40 steps of a search
 // in every wavefront) 130
 constexpr int kRaggedOrdered = 61;
@@ -144,7 +144,7 @@ using RaggedLone = RaggedCut<1, 1, 64, 2, 1>;
 // byte offset past 32 bits; rows past the end arrive as zeros.
 // Layout of a tile: at 64 channels quad_at's (no bank conflicts, and two addresses a lane for the loads of both tensors instead of one
 // for each load: where registers are scarce, in dK/dV, that is what keeps the accumulators out of scratch), at 128 two such halves one
-// after the other (padded rows' bank conflicts took 30 % of the cycles: prompts of 500 to 8000 tokens, 32 heads on 8, 690 -> 665 us), else
+// after the other (padded rows' bank conflicts took 30 % of the cycles: prompts of 500 to 8000 tokens, 32 heads on 8, 690 -> 665 us a call on one card), else
 // padded rows.
 template <int D, typename Cut, bool SCALARS>
 struct RaggedRing {
@@ -379,9 +379,9 @@ DEVINL void ragged_zero(raw16* out, int H, int h0, int heads, long token0, int n
 // One wavefront owns 32 rows, the workgroup's NW share (K | V) tiles of 64 keys; work in units of 32 keys as in avion_fwd_kernel,
 // but with the running maximum: the accumulators are rescaled only where a row's maximum has grown by more than 2^8 (weights then
 // stay below 2^8, which either format holds), a branch that after the first units is hardly ever taken.
-// Bound by the vector issue port (65 % of the cycles at 64 channels, matrix units 34) and, at 128, by both (49 and 47).  16 videos of 196 to 3136
-// tokens, 12 heads of 64, 81 us = 670 TFLOP/s; prompts of 500 to 8000, 32 heads on 8 of 128, 665 us = 920; 2048 captions of 6 to 77, 8 heads
-// of 64, 55 us, bound by memory.
+// Bound by the vector issue port (63 % of the cycles at 64 channels, matrix units 33) and, at 128, by both (49 and 47).  Medians on two cards:
+// 16 videos of 196 to 3136 tokens, 12 heads of 64, 91 and 95 us = 570 to 590 TFLOP/s (best launch 81); prompts of 500 to 8000, 32 heads on
+// 8 of 128, 733 and 808 us = 760 to 830 (best 698); 2048 captions of 6 to 77, 8 heads of 64, 56 us, bound by memory.
 constexpr float kRaggedLazy = 8.f;
 constexpr float kRaggedNone = -3.0e38f;  // reference of a row that has seen nothing: finite, so that -inf - it is -inf
 
@@ -708,7 +708,8 @@ avion_ragged_join_kernel(RaggedArgs a, raw16* __restrict__ o, float* __restrict_
 //
 // fp16 weights below 2^-14 lose bits: over thousands of keys most are.  The second kernel holds them 2^8 times larger where they
 // are rounded for dV; in dS they stand beside dP, which is as large as the loss is scaled.
-// The 16 videos 92 us = 880 TFLOP/s, the logits among them (matrix units 42 % of the cycles, vector issue 60).
+// The 16 videos 101 and 106 us (medians on two cards, best launch 95) = 770 to 800 TFLOP/s, the logits among them (matrix units 42 % of the
+// cycles, vector issue 58).
 template <typename E>
 constexpr float kRaggedShift = std::is_same<E, F16>::value ? 8.f : 0.f;
 
@@ -974,7 +975,8 @@ DEVINL void ragged_dkdv_unit(const Lane& at, const char* qt, const char* gt, con
 }
 
 // dK and dV: 32 keys a wavefront, K and V in registers, (Q | dO) tiles of the query heads that share them one after the other.  The 16 videos
-// 112 us = 970 TFLOP/s, the logits among them (matrix units 45 % of the cycles, LDS 35, vector issue 47).
+// 124 and 133 us (medians on two cards, best launch 116) = 820 to 880 TFLOP/s, the logits among them (matrix units 46 % of the cycles, LDS 36,
+// vector issue 46).
 template <int D, typename Cut, typename E>
 __global__ void __launch_bounds__(Cut::NT * Cut::JOBS, (RaggedDkvCfg<D, Cut>::WAVES_PER_SIMD))
 avion_ragged_dkdv_kernel(RaggedArgs a, const raw16* __restrict__ dO, const float* __restrict__ rowsc, int npad, raw16* __restrict__ dk,

@@ -35,6 +35,8 @@ bool stride_ok(long long rs, int H, int d) { return rs >= (long long)H * d; }
 // Few rows a sequence and many keys, or a batch most of whose sequences may be such: a wavefront per chunk of keys.  2^shift keys a chunk,
 // 0: not this way.  63 single tokens and a prompt of 1000, each with 9000 keys, 32 heads on 8 of 128: 648 us, in one launch 665; 15 tokens and
 // 500 with 4000 keys, 8 heads of 64: 60, 118.
+// Not cut over workgroups: the keys of a sequence's rows past the first 32, and those of three or fewer sequences of more than 32 rows each.  64
+// heads on 8 of 128 behind 9000 keys, 4 and 8 tokens: one sequence 40 and 349 us (32 tokens 105), four 62 and 272, 64 502 and 516.
 int few_shift(const RaggedShape& s)
 {
     const long long G = s.Hq / s.Hk;
@@ -67,6 +69,8 @@ enum class RaggedWay { kShort, kWide, kSplitHalf, kSplit, kSplit4 };
 //   head) 82 + 192, 48 + 115, 38 + 86
 // and sequences of less than 80 rows on average by lone wavefronts: 2048 of 6 to 77 tokens (28 on average), 8 heads, forward 54, wide 130;
 // 131000 tokens in sequences of 40, 64, 77, 96, 128: 120, 115, 129, 181, 137, wide 164, 134, 160, 126, 172.
+// The rule sees totals, as the lengths are on the device: one sequence of 3136 tokens (8 heads of 64, causal, forward 35 us alone) among 1000 of
+// 28 (22 us) is a lone wavefronts' too, and both together take 97 us.
 RaggedWay ragged_way(int d, long long rows, long long S, long long heads)
 {
     if (rows < 80 * S) return RaggedWay::kShort;
